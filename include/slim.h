@@ -48,7 +48,8 @@ typedef enum {
   SLIM_ERR_CUDA = 6,         /* CUDA runtime/driver error, or no device             */
   SLIM_ERR_TIMEOUT = 7,      /* a bounded device-side wait ran out (device)         */
   SLIM_ERR_NO_WEIGHTS = 8,   /* slim_decode before slim_set_weights / slim_set_wkv  */
-  SLIM_ERR_STATIC_WS = 9     /* slim_decode_static_ws: scratch need above the built-in maximum */
+  SLIM_ERR_STATIC_WS = 9,    /* slim_decode_static_ws: scratch need above the built-in maximum */
+  SLIM_ERR_TREE = 10         /* a tree of drafted tokens, or a path through one, is not one (device) */
 } slim_status;
 
 /* cache / query dtype.  SLIM_FP8: the cache holds 8-bit keys (1 byte per value, the paper's own byte
@@ -279,8 +280,86 @@ slim_status slim_decode_partial(slim_ctx* ctx, const void* q, const slim_cache* 
 slim_status slim_combine_project(slim_ctx* ctx, const float* lse_all, const float* u_all, int ranks,
                                  const int32_t* total_lengths, int batch, float* o, void* workspace, void* stream);
 
+/* ---- Several drafted tokens in one step (speculative decoding) --------------------------------
+ * (The paper has no counterpart; Eq. 7 Option 2 is evaluated for every drafted token.)  A small model
+ * or a lookup drafts a tree of n <= SLIM_MAX_TREE tokens per sequence; one pass attends for all of
+ * them, the target's probabilities decide which path through the tree is accepted, and the accepted
+ * tokens' keys go into the cache:
+ *     slim_tree_decode (every layer)  ->  slim_tree_verify  ->  slim_tree_commit (every layer)
+ * The tree of a sequence: parents[i] (device int32 [batch][n]) is the index of token i's parent, an
+ * EARLIER token of the same sequence; -1 makes i a root; anything below -1 makes i padding, a token
+ * that is not there (ragged trees in one batch).  depth(i) = number of proper ancestors.  A parent that is not an
+ * earlier token, or is padding, raises SLIM_ERR_TREE on the device and the token is treated as padding.
+ *
+ * slim_tree_decode  attention of every drafted token over the cached rows, its ancestors and itself.
+ *   q, k_tree  device [batch][n][d], ctx dtype, 16-byte aligned: un-rotated queries and key rows of the
+ *              drafted tokens; token i sits at position lengths[b] + depth(i)
+ *   cache      contiguous or paged (not SLIM_FP8); it is read only: drafted keys enter it by slim_tree_commit
+ *   lengths    device int32 [batch]: cached rows of sequence b (0: the tokens attend the tree only); above t_cap:
+ *              clamped and reported as SLIM_ERR_CAPACITY.  Rows behind them may hold anything
+ *   o          device [batch][n][d], ctx dtype (float32, or bfloat16: the operand of the output projection,
+ *              rounded once at the end), 16-byte aligned; a padding token gets a zero row, and what q and
+ *              k_tree hold for it is not used
+ *   workspace  device, >= slim_tree_workspace_bytes(ctx, batch, t_cap, n) (0 on bad arguments), 256-byte
+ *              aligned; contents are scratch.  Calls that may overlap on the GPU need one each
+ *   Softmax sums and the weighted sums are float32; the tensor-core path (bf16, d % 64 == 0, d_k in {64, 96, 128})
+ *   rounds the probabilities and the weighted sums to bf16 on their way into its matrix products.
+ *
+ * slim_tree_verify  which drafted tokens are accepted, from given random numbers, so that the tokens
+ *   kept follow the target's distribution.  Node 0 is the token accepted last (the root; its own acceptance is not
+ *   in question).  All pointers device; ctx only supplies the device and the status word.
+ *   p, q       float32 [batch][n][vocab]: the target's probabilities after node i, and the distribution that the
+ *              children of node i were drawn from (rows of nodes without children are not read); rows of p sum to 1
+ *   tokens     int32 [batch][n]; a child's token outside [0, vocab) raises SLIM_ERR_TREE and makes it padding
+ *   parents    as above; roots other than node 0 are never reached
+ *   r          float32 [batch][n], uniform in [0, 1): r[i] tests node i, r[0] draws the next token
+ *   From u = 0, W = p_u, S = 1, the children c of u in index order: accepted if r_c S q_u(x_c) < W(x_c), then u = c,
+ *   W = p_c, S = 1; otherwise W = max(W - S q_u, 0), S = sum W (both stay as they were if nothing is left).
+ *   When no child is left, the next token is the first x with W(0) + .. + W(x) > r_0 sum W.  Computed in float64.
+ *   path       int32 [batch][n]: the accepted nodes, path[0] = 0, then -1;  count  int32 [batch]: how many
+ *   next_token int32 [batch]: the token drawn after the last accepted node; -1 if W has no positive value
+ *
+ * slim_tree_commit  k_tree[b][path[b][j]] -> cache row lengths[b] + j for j < count[b] (path, count as
+ *   slim_tree_verify leaves them, or any indices into the tree; count 0 writes nothing).  f32 and bf16 caches,
+ *   contiguous or paged.  The caller adds count to lengths after the last layer.  A sequence whose rows would pass
+ *   t_cap (SLIM_ERR_CAPACITY) or whose path leaves the tree (SLIM_ERR_TREE) is left unwritten.          */
+#define SLIM_MAX_TREE 64
+size_t      slim_tree_workspace_bytes(const slim_ctx* ctx, int batch, int t_cap, int n);
+slim_status slim_tree_decode(slim_ctx* ctx, const void* q, const void* k_tree, const slim_cache* cache, const int32_t* lengths,
+                             const int32_t* parents, int n, void* o, void* workspace, void* stream);
+slim_status slim_tree_verify(slim_ctx* ctx, const float* p, const float* q, const int32_t* tokens, const int32_t* parents,
+                             const float* r, int batch, int n, int vocab, int32_t* path, int32_t* count, int32_t* next_token,
+                             void* stream);
+slim_status slim_tree_commit(slim_ctx* ctx, slim_cache* cache, const void* k_tree, const int32_t* lengths, const int32_t* path,
+                             const int32_t* count, int n, void* stream);
+
+/* ---- A long cache kept inside a budget ---------------------------------------------------------
+ * (No counterpart in the paper.)  A cache row of this scheme serves all heads, so the weight of a row is the sum of
+ * its softmax probabilities over the heads.
+ *
+ * slim_accumulate_weights  acc[b][t] += sum_h softmax_t(q_h . K_h / sqrt(d_k)), t < lengths[b], for the query of
+ *   slim_decode (un-rotated, at position lengths[b]-1; same arguments).  acc: device float32 [batch][t_cap],
+ *   other elements are left alone.  Any cache that slim_decode takes.  workspace: device, >=
+ *   slim_weights_workspace_bytes(ctx, batch, t_cap), 256-byte aligned.
+ *
+ * slim_evict  brings every sequence that is longer than `budget` rows down to it: the last `recent` rows stay
+ *   (0 <= recent <= budget), and of the rows before them the budget - recent with the largest acc (equal values: the
+ *   lower row; NaN counts as the lowest value).  The kept rows move, in order, to rows 0 .. budget-1, in place; their
+ *   acc moves along and the acc of the rows that became free is cleared.  Keys are cached un-rotated, so a
+ *   row that moved sits at its new position from then on.  The caller clamps lengths to the budget
+ *   after the last layer.  Shorter sequences stay as they are.  Any cache of the library (a paged one
+ *   keeps its block table; the pages behind the budget are free to be given back).
+ *   kept       device int32 [batch][budget], written: the old row of every new row, -1 behind a shorter sequence
+ *   workspace  device, >= slim_evict_workspace_bytes(ctx, batch, t_cap), 256-byte aligned          */
+size_t      slim_weights_workspace_bytes(const slim_ctx* ctx, int batch, int t_cap);
+slim_status slim_accumulate_weights(slim_ctx* ctx, const void* q, const slim_cache* cache, const int32_t* lengths, float* acc,
+                                    void* workspace, void* stream);
+size_t      slim_evict_workspace_bytes(const slim_ctx* ctx, int batch, int t_cap);
+slim_status slim_evict(slim_ctx* ctx, slim_cache* cache, const int32_t* lengths, float* acc, int budget, int recent,
+                       int32_t* kept, void* workspace, void* stream);
+
 /* Synchronises `stream`, returns the sticky device status (SLIM_OK,
- * SLIM_ERR_CAPACITY or SLIM_ERR_TIMEOUT) and clears it.                        */
+ * SLIM_ERR_CAPACITY, SLIM_ERR_TIMEOUT or SLIM_ERR_TREE) and clears it.         */
 slim_status slim_device_status(slim_ctx* ctx, void* stream);
 
 /* Self-test of the bounded device-side waits every TMA / tcgen05 kernel relies on: runs

@@ -14,9 +14,10 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libslim.so")
 
 SLIM_OK, SLIM_ERR_INVALID_ARG, SLIM_ERR_UNSUPPORTED, SLIM_ERR_SINGULAR, SLIM_ERR_CAPACITY, \
-    SLIM_ERR_OOM, SLIM_ERR_CUDA, SLIM_ERR_TIMEOUT, SLIM_ERR_NO_WEIGHTS, SLIM_ERR_STATIC_WS = range(10)
+    SLIM_ERR_OOM, SLIM_ERR_CUDA, SLIM_ERR_TIMEOUT, SLIM_ERR_NO_WEIGHTS, SLIM_ERR_STATIC_WS, SLIM_ERR_TREE = range(11)
 SLIM_F32, SLIM_BF16, SLIM_FP8 = 0, 1, 2
 SLIM_HOST_F32, SLIM_HOST_F64 = 0, 1
+SLIM_MAX_TREE = 64
 SLIM_PATH_AUTO, SLIM_PATH_GENERIC, SLIM_PATH_TC = 0, 1, 2
 SLIM_Q_PATH_IN_USE, SLIM_Q_LAUNCHES_PER_DECODE, SLIM_Q_MAX_UNITS, SLIM_Q_NUM_SMS, SLIM_Q_WORKERS = range(5)
 
@@ -46,6 +47,14 @@ SIGNATURES = {
     "slim_reserve_positions": (c_int, [c_void_p, c_int]),
     "slim_decode_partial": (c_int, [c_void_p] * 10),
     "slim_combine_project": (c_int, [c_void_p, c_void_p, c_void_p, c_int, c_void_p, c_int, c_void_p, c_void_p, c_void_p]),
+    "slim_tree_workspace_bytes": (c_size_t, [c_void_p, c_int, c_int, c_int]),
+    "slim_tree_decode": (c_int, [c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_int, c_void_p, c_void_p, c_void_p]),
+    "slim_tree_verify": (c_int, [c_void_p] * 6 + [c_int] * 3 + [c_void_p] * 4),
+    "slim_tree_commit": (c_int, [c_void_p] * 6 + [c_int, c_void_p]),
+    "slim_weights_workspace_bytes": (c_size_t, [c_void_p, c_int, c_int]),
+    "slim_accumulate_weights": (c_int, [c_void_p] * 7),
+    "slim_evict_workspace_bytes": (c_size_t, [c_void_p, c_int, c_int]),
+    "slim_evict": (c_int, [c_void_p] * 4 + [c_int, c_int] + [c_void_p] * 3),
     "slim_device_status": (c_int, [c_void_p, c_void_p]),
     "slim_selftest_bounded_wait": (c_int, [c_void_p, c_void_p]),
     "slim_profile_enable": (c_int, [c_void_p, c_int]),
@@ -249,6 +258,48 @@ def slim_decode_partial(ctx: int, q, cache: int, lengths, first_tile, q_pos, lse
 def slim_combine_project(ctx: int, lse_all, u_all, ranks: int, total_lengths, batch: int, o, workspace, stream: int = 0) -> None:
     _check(lib().slim_combine_project(c_void_p(ctx), _ptr(lse_all), _ptr(u_all), ranks, _ptr(total_lengths), batch, _ptr(o),
                                       _ptr(workspace), c_void_p(stream)), "slim_combine_project")
+
+
+def slim_tree_workspace_bytes(ctx: int, batch: int, t_cap: int, n: int) -> int:
+    return lib().slim_tree_workspace_bytes(c_void_p(ctx), batch, t_cap, n)
+
+
+def slim_tree_decode(ctx: int, q, k_tree, cache: int, lengths, parents, n: int, o, workspace, stream: int = 0) -> None:
+    """Attention of n drafted tokens a sequence (a tree given by `parents`) over the cache, their ancestors and themselves."""
+    _check(lib().slim_tree_decode(c_void_p(ctx), _ptr(q), _ptr(k_tree), c_void_p(cache), _ptr(lengths), _ptr(parents), n, _ptr(o),
+                                  _ptr(workspace), c_void_p(stream)), "slim_tree_decode")
+
+
+def slim_tree_verify(ctx: int, p, q, tokens, parents, r, batch: int, n: int, vocab: int, path, count, next_token, stream: int = 0) -> None:
+    """Which drafted tokens are accepted (path, count) and the token drawn after them, from given random numbers."""
+    _check(lib().slim_tree_verify(c_void_p(ctx), _ptr(p), _ptr(q), _ptr(tokens), _ptr(parents), _ptr(r), batch, n, vocab, _ptr(path),
+                                  _ptr(count), _ptr(next_token), c_void_p(stream)), "slim_tree_verify")
+
+
+def slim_tree_commit(ctx: int, cache: int, k_tree, lengths, path, count, n: int, stream: int = 0) -> None:
+    """The accepted tokens' keys go to cache rows lengths[b] + j; the caller adds count to lengths after the last layer."""
+    _check(lib().slim_tree_commit(c_void_p(ctx), c_void_p(cache), _ptr(k_tree), _ptr(lengths), _ptr(path), _ptr(count), n,
+                                  c_void_p(stream)), "slim_tree_commit")
+
+
+def slim_weights_workspace_bytes(ctx: int, batch: int, t_cap: int) -> int:
+    return lib().slim_weights_workspace_bytes(c_void_p(ctx), batch, t_cap)
+
+
+def slim_accumulate_weights(ctx: int, q, cache: int, lengths, acc, workspace, stream: int = 0) -> None:
+    """acc[b][t] += the probabilities of cache row t under the query of slim_decode, summed over the heads."""
+    _check(lib().slim_accumulate_weights(c_void_p(ctx), _ptr(q), c_void_p(cache), _ptr(lengths), _ptr(acc), _ptr(workspace),
+                                         c_void_p(stream)), "slim_accumulate_weights")
+
+
+def slim_evict_workspace_bytes(ctx: int, batch: int, t_cap: int) -> int:
+    return lib().slim_evict_workspace_bytes(c_void_p(ctx), batch, t_cap)
+
+
+def slim_evict(ctx: int, cache: int, lengths, acc, budget: int, recent: int, kept, workspace, stream: int = 0) -> None:
+    """Sequences longer than `budget` rows keep the last `recent` and the heaviest of the others, moved to the front in order."""
+    _check(lib().slim_evict(c_void_p(ctx), c_void_p(cache), _ptr(lengths), _ptr(acc), budget, recent, _ptr(kept), _ptr(workspace),
+                            c_void_p(stream)), "slim_evict")
 
 
 def slim_device_status(ctx: int, stream: int = 0) -> int:

@@ -8,6 +8,7 @@
 #include <vector>
 
 #include "slim_internal.h"
+#include "slim_tree.h"
 
 size_t slim_tail_opart_floats(int d, int e, int batch);
 
@@ -143,6 +144,7 @@ const char* slim_strerror(int status) {
     case SLIM_ERR_TIMEOUT: return "a bounded device-side wait ran out";
     case SLIM_ERR_NO_WEIGHTS: return "W_KV has not been set";
     case SLIM_ERR_STATIC_WS: return "this batch / capacity needs more scratch than the built-in static workspace holds";
+    case SLIM_ERR_TREE: return "not a tree of drafted tokens, or not a path through one";
     default: return "unknown status";
   }
 }
@@ -389,7 +391,7 @@ slim_status slim_cache_create(slim_ctx* ctx, slim_cache** out, void* k_storage, 
   if (!ctx || !k_storage || batch <= 0 || t_cap <= 0) return SLIM_ERR_INVALID_ARG;
   if (batch > SLIM_MAX_BATCH || ((uintptr_t)k_storage & 15)) return SLIM_ERR_UNSUPPORTED;
   if ((long long)batch * t_cap > 0x7fffffffLL - 64) return SLIM_ERR_UNSUPPORTED;
-  slim_status st = grow_rope_base(ctx, t_cap);
+  slim_status st = grow_rope_base(ctx, t_cap + SLIM_MAX_TREE);     // a tree's tokens sit behind the last row
   if (st != SLIM_OK) return st;
   slim_cache* c = new (std::nothrow) slim_cache();
   if (!c) return SLIM_ERR_OOM;
@@ -424,7 +426,7 @@ slim_status slim_cache_create_paged(slim_ctx* ctx, slim_cache** out, void* pool,
   if ((long long)num_pages * page_rows > 0x7fffffffLL - 64 || (long long)batch * max_pages * page_rows > 0x7fffffffLL - 64)
     return SLIM_ERR_UNSUPPORTED;
   const int t_cap = max_pages * page_rows;
-  slim_status st = grow_rope_base(ctx, t_cap);
+  slim_status st = grow_rope_base(ctx, t_cap + SLIM_MAX_TREE);     // a tree's tokens sit behind the last row
   if (st != SLIM_OK) return st;
   slim_cache* c = new (std::nothrow) slim_cache();
   if (!c) return SLIM_ERR_OOM;
@@ -700,6 +702,114 @@ slim_status slim_decode_static_ws(slim_ctx* ctx, const void* q, const slim_cache
   // Nothing in the scratch has to start at zero: every word that reaches a stored output was
   // written earlier in the same call (partials, redo flags, projection operand tiles).
   return slim_decode(ctx, q, cache, lengths, o, ws, stream);
+}
+
+// ---- drafted tokens, cache budget ------------------------------------------------
+namespace {
+bool current_device_is(const slim_ctx* ctx) {
+  int dev = -1;
+  if (cudaGetDevice(&dev) != cudaSuccess) { cudaGetLastError(); return false; }
+  return dev == ctx->device;
+}
+
+// What the kernels need to walk a cache and to rotate keys and queries.
+SlimDecodeParams cache_params(const slim_ctx* ctx, const slim_cache* cache, const void* q, const int32_t* lengths) {
+  SlimDecodeParams p;
+  std::memset(&p, 0, sizeof(p));
+  p.d = ctx->d; p.e = ctx->e; p.H = ctx->H; p.d_k = ctx->d_k; p.half = ctx->d_k / 2;
+  p.batch = cache->batch; p.t_cap = cache->t_cap;
+  p.rope = ctx->rope_theta != 0.0; p.dtype = ctx->dtype; p.kdtype = ctx->kdtype; p.k_exp = cache->k_exp;
+  p.workers = ctx->gen_workers; p.min_tiles = 1;
+  p.qscale = (float)(1.4426950408889634 / std::sqrt((double)ctx->d_k));
+  p.q = q; p.k = cache->k; p.lengths = lengths;
+  p.rope_base = ctx->rope_base; p.rope_off = ctx->rope_off; p.rope_tiles = ctx->rope_base_tiles; p.wkv = ctx->wkv;
+  p.status = ctx->status; p.any_flag = ctx->any_flag;
+  p.block_table = cache->block_table; p.page_rows = cache->page_rows; p.max_pages = cache->max_pages; p.num_pages = cache->num_pages;
+  p.k_evict_first = ctx->opt_k_evict;
+  return p;
+}
+
+slim_status launched(cudaError_t e) {
+  if (e == cudaSuccess) return SLIM_OK;
+  cudaGetLastError();
+  return SLIM_ERR_CUDA;
+}
+
+struct WeightsLayout { size_t scores, m, inv_l, total; };
+WeightsLayout weights_layout(const slim_ctx* ctx, int batch, int t_cap) {
+  WeightsLayout L;
+  size_t off = 0;
+  L.scores = off; off = align256(off + sizeof(float) * (size_t)batch * ctx->H * t_cap);
+  L.m = off; off = align256(off + sizeof(float) * (size_t)batch * ctx->H);
+  L.inv_l = off; off = align256(off + sizeof(float) * (size_t)batch * ctx->H);
+  L.total = off;
+  return L;
+}
+}  // namespace
+
+size_t slim_tree_workspace_bytes(const slim_ctx* ctx, int batch, int t_cap, int n) {
+  if (!ctx || batch <= 0 || t_cap <= 0 || batch > SLIM_MAX_BATCH || n <= 0 || n > SLIM_MAX_TREE || ctx->e != ctx->d) return 0;
+  return slim_tree_ws_layout(ctx, batch, t_cap, n).total;
+}
+
+slim_status slim_tree_decode(slim_ctx* ctx, const void* q, const void* k_tree, const slim_cache* cache, const int32_t* lengths,
+                             const int32_t* parents, int n, void* o, void* workspace, void* stream) {
+  if (!ctx || !q || !k_tree || !cache || !lengths || !parents || !o || !workspace || cache->ctx != ctx) return SLIM_ERR_INVALID_ARG;
+  if (n <= 0 || n > SLIM_MAX_TREE || ((uintptr_t)workspace & 255)) return SLIM_ERR_INVALID_ARG;
+  if (((uintptr_t)q | (uintptr_t)k_tree | (uintptr_t)o) & 15) return SLIM_ERR_INVALID_ARG;
+  if (ctx->kdtype == SLIM_FP8 || ctx->e != ctx->d) return SLIM_ERR_UNSUPPORTED;
+  if (!ctx->has_weights) return SLIM_ERR_NO_WEIGHTS;
+  if (!current_device_is(ctx)) return SLIM_ERR_INVALID_ARG;
+  return launched(slim_launch_tree(ctx, cache_params(ctx, cache, q, lengths), k_tree, parents, n, o, static_cast<char*>(workspace),
+                                   (cudaStream_t)stream));
+}
+
+slim_status slim_tree_verify(slim_ctx* ctx, const float* p, const float* q, const int32_t* tokens, const int32_t* parents, const float* r,
+                             int batch, int n, int vocab, int32_t* path, int32_t* count, int32_t* next_token, void* stream) {
+  if (!ctx || !p || !q || !tokens || !parents || !r || !path || !count || !next_token) return SLIM_ERR_INVALID_ARG;
+  if (batch <= 0 || batch > SLIM_MAX_BATCH || n <= 0 || n > SLIM_MAX_TREE || vocab <= 0 || vocab > (1 << 30)) return SLIM_ERR_INVALID_ARG;
+  if (!current_device_is(ctx)) return SLIM_ERR_INVALID_ARG;
+  return launched(slim_launch_verify(p, q, tokens, parents, r, batch, n, vocab, path, count, next_token, ctx->status, (cudaStream_t)stream));
+}
+
+slim_status slim_tree_commit(slim_ctx* ctx, slim_cache* cache, const void* k_tree, const int32_t* lengths, const int32_t* path,
+                             const int32_t* count, int n, void* stream) {
+  if (!ctx || !cache || !k_tree || !lengths || !path || !count || cache->ctx != ctx) return SLIM_ERR_INVALID_ARG;
+  if (n <= 0 || n > SLIM_MAX_TREE || ((uintptr_t)k_tree & 15)) return SLIM_ERR_INVALID_ARG;
+  if (ctx->kdtype == SLIM_FP8 || ctx->e != ctx->d) return SLIM_ERR_UNSUPPORTED;
+  if (!current_device_is(ctx)) return SLIM_ERR_INVALID_ARG;
+  return launched(slim_launch_commit(ctx, cache, k_tree, lengths, path, count, n, (cudaStream_t)stream));
+}
+
+size_t slim_weights_workspace_bytes(const slim_ctx* ctx, int batch, int t_cap) {
+  if (!ctx || batch <= 0 || t_cap <= 0 || batch > SLIM_MAX_BATCH || ctx->e != ctx->d) return 0;
+  return weights_layout(ctx, batch, t_cap).total;
+}
+
+slim_status slim_accumulate_weights(slim_ctx* ctx, const void* q, const slim_cache* cache, const int32_t* lengths, float* acc,
+                                    void* workspace, void* stream) {
+  if (!ctx || !q || !cache || !lengths || !acc || !workspace || cache->ctx != ctx) return SLIM_ERR_INVALID_ARG;
+  if (((uintptr_t)workspace & 255) || ((uintptr_t)q & 15) || ((uintptr_t)acc & 3)) return SLIM_ERR_INVALID_ARG;
+  if (ctx->e != ctx->d) return SLIM_ERR_UNSUPPORTED;
+  if (!current_device_is(ctx)) return SLIM_ERR_INVALID_ARG;
+  const WeightsLayout L = weights_layout(ctx, cache->batch, cache->t_cap);
+  char* ws = static_cast<char*>(workspace);
+  return launched(slim_launch_weights(ctx, cache_params(ctx, cache, q, lengths), reinterpret_cast<float*>(ws + L.scores),
+                                      reinterpret_cast<float*>(ws + L.m), reinterpret_cast<float*>(ws + L.inv_l), acc, (cudaStream_t)stream));
+}
+
+size_t slim_evict_workspace_bytes(const slim_ctx* ctx, int batch, int t_cap) {
+  if (!ctx || batch <= 0 || t_cap <= 0 || batch > SLIM_MAX_BATCH) return 0;
+  return 256;
+}
+
+slim_status slim_evict(slim_ctx* ctx, slim_cache* cache, const int32_t* lengths, float* acc, int budget, int recent, int32_t* kept,
+                       void* workspace, void* stream) {
+  if (!ctx || !cache || !lengths || !acc || !kept || !workspace || cache->ctx != ctx) return SLIM_ERR_INVALID_ARG;
+  if (budget <= 0 || recent < 0 || recent > budget || ((uintptr_t)workspace & 255) || (((uintptr_t)acc | (uintptr_t)kept) & 3))
+    return SLIM_ERR_INVALID_ARG;
+  if (!current_device_is(ctx)) return SLIM_ERR_INVALID_ARG;
+  return launched(slim_launch_evict(ctx, cache, lengths, acc, budget, recent, kept, (cudaStream_t)stream));
 }
 
 slim_status slim_device_status(slim_ctx* ctx, void* stream) {

@@ -606,9 +606,13 @@ int slim_generic_workers(const slim_ctx* ctx) {
   return w;
 }
 
+cudaError_t slim_launch_scores(const slim_ctx* ctx, const SlimDecodeParams& p, float* scores, cudaStream_t st) {
+  return p.kdtype == SLIM_FP8 ? launch_scores<fp8code>(ctx, p, scores, st)
+         : p.dtype == SLIM_BF16 ? launch_scores<__nv_bfloat16>(ctx, p, scores, st) : launch_scores<float>(ctx, p, scores, st);
+}
+
 cudaError_t slim_launch_generic(const slim_ctx* ctx, const SlimDecodeParams& p, float* scores, cudaStream_t st) {
-  cudaError_t e = p.kdtype == SLIM_FP8 ? launch_scores<fp8code>(ctx, p, scores, st)
-                  : p.dtype == SLIM_BF16 ? launch_scores<__nv_bfloat16>(ctx, p, scores, st) : launch_scores<float>(ctx, p, scores, st);
+  cudaError_t e = slim_launch_scores(ctx, p, scores, st);
   if (e != cudaSuccess) return e;
   return slim_launch_accum(ctx, p, scores, 1, st);
 }

@@ -204,3 +204,18 @@ cudaError_t slim_launch_rank_combine(const slim_ctx* ctx, const SlimDecodeParams
 // prompt phase: V = K W_KV for n rows (slim_prompt.cu)
 cudaError_t slim_launch_values(const slim_ctx* ctx, const void* K, int n, float* V, cudaStream_t st,
                                const slim_cache* cache = nullptr, const int32_t* positions = nullptr, int n_new = 0);
+
+// drafted tokens (slim_tree.cu, slim_draft.cu)
+cudaError_t slim_launch_tree(const slim_ctx* ctx, const SlimDecodeParams& p, const void* k_tree, const int32_t* parents, int n,
+                             void* o, char* ws, cudaStream_t st);
+cudaError_t slim_launch_verify(const float* p, const float* q, const int32_t* tokens, const int32_t* parents, const float* r, int batch,
+                               int n, int vocab, int32_t* path, int32_t* count, int32_t* next_token, int* status, cudaStream_t st);
+cudaError_t slim_launch_commit(const slim_ctx* ctx, const slim_cache* c, const void* k_tree, const int32_t* lengths, const int32_t* path,
+                               const int32_t* count, int n, cudaStream_t st);
+
+// cache budget (slim_budget.cu); scores: the CUDA-core score kernel alone, [batch][H][t_cap] (slim_generic.cu)
+cudaError_t slim_launch_scores(const slim_ctx* ctx, const SlimDecodeParams& p, float* scores, cudaStream_t st);
+cudaError_t slim_launch_weights(const slim_ctx* ctx, const SlimDecodeParams& p, float* scores, float* m, float* inv_l, float* acc,
+                                cudaStream_t st);
+cudaError_t slim_launch_evict(const slim_ctx* ctx, const slim_cache* c, const int32_t* lengths, float* acc, int budget, int recent,
+                              int32_t* kept, cudaStream_t st);

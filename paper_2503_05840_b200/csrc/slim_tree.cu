@@ -1,0 +1,336 @@
+// Attention for a tree of drafted tokens over the K-cache (slim_tree_decode): the tree's layout, and the CUDA-core
+// kernels that take every shape (f32 caches, head widths and model widths outside the tensor-core kernels).
+//
+// For token i of sequence b (L cached rows, position L + depth(i)) and head h, over the rows t < L and the drafted
+// keys j that are i itself or one of its ancestors:
+//   s_t = R_{pos(i)} q . R_{pos(t)} k_t log2(e) / sqrt(d_k),   p_t = 2^(s_t - m),   l = sum p_t,
+//   u_{i,h} = sum_t (p_t / l) k_t    (the whole d-wide un-rotated row, Eq. 7 Option 2),   o_{i,h} = u_{i,h} W_KV,h.
+// One sequence has R = H n rows u of d numbers each, far more than on-chip memory holds, so the arguments are laid
+// down once ([b][h n + i][t], float) and the weighted sum is a matrix product P [R x T] K [T x d] cut into tiles;
+// where there are few tiles, T is cut too and the parts are added in a fixed order.
+#include "slim_internal.h"
+#include "slim_sched.cuh"
+#include "slim_tree.h"
+
+namespace {
+
+__device__ __forceinline__ float to_f(float v) { return v; }
+__device__ __forceinline__ float to_f(__nv_bfloat16 v) { return __bfloat162float(v); }
+__device__ __forceinline__ void put(float* p, float v) { *p = v; }
+__device__ __forceinline__ void put(__nv_bfloat16* p, float v) { *p = __float2bfloat16(v); }   // the one rounding of a bf16 context's output
+
+// One block per sequence: depth and ancestor mask of every token.  A parent that is not an earlier token of the
+// tree makes the token padding and raises SLIM_ERR_TREE; parents below -1 are padding.
+__global__ void __launch_bounds__(64) slim_tree_layout_kernel(const int32_t* __restrict__ parents, const int32_t* __restrict__ lengths,
+                                                              int n, int t_cap, unsigned long long* __restrict__ mask,
+                                                              int* __restrict__ depth, int* __restrict__ len_out, int* status) {
+  __shared__ int s_par[SLIM_MAX_TREE];
+  const int b = blockIdx.x, i = threadIdx.x;
+  slim_pdl_trigger();
+  slim_pdl_wait();
+  if (i < n) {
+    int p = parents[(size_t)b * n + i];
+    if (p >= i) { p = -2; atomicMax(status, (int)SLIM_ERR_TREE); }
+    s_par[i] = p;
+  }
+  __syncthreads();
+  if (i == 0) {
+    int len = lengths[b];
+    if (len > t_cap) { len = t_cap; atomicMax(status, (int)SLIM_ERR_CAPACITY); }
+    len_out[b] = len < 0 ? 0 : len;
+  }
+  if (i < n) {
+    unsigned long long m = 0;
+    int dep = -1, at = i;
+    bool live = s_par[i] >= -1;
+    while (live) {                                   // at most n steps: a parent is an earlier token
+      m |= 1ull << at;
+      ++dep;
+      const int p = s_par[at];
+      if (p == -1) break;
+      if (p < -1) live = false;                      // hangs on padding
+      at = p;
+    }
+    if (!live) {
+      if (s_par[i] >= -1) atomicMax(status, (int)SLIM_ERR_TREE);
+      m = 0; dep = -1;
+    }
+    mask[(size_t)b * n + i] = m;
+    depth[(size_t)b * n + i] = dep;
+  }
+}
+
+__device__ __forceinline__ float2 rope_at(const SlimDecodeParams& p, int pos, int j) {
+  const float2 cb = __ldg(p.rope_base + (size_t)(pos / SLIM_TT) * p.half + j), co = __ldg(p.rope_off + (pos % SLIM_TT) * p.half + j);
+  return make_float2(cb.x * co.x - cb.y * co.y, cb.y * co.x + cb.x * co.y);
+}
+
+// Softmax arguments (log2 units): block = 64 keys of one (sequence, head) against all its tokens; the last block
+// of the row is the drafted keys.
+constexpr int TS_KEYS = 64;
+template <typename KT>
+__global__ void __launch_bounds__(256) slim_tree_scores_kernel(const SlimDecodeParams p, const SlimTreeView t) {
+  extern __shared__ float sm[];
+  const int dk = p.d_k, half = p.half, ld = dk + 1, n = t.n, tid = threadIdx.x;
+  float* Ks = sm;                                    // [TS_KEYS][dk + 1]
+  float* Qs = Ks + TS_KEYS * ld;                     // [n][dk + 1]
+  const int b = blockIdx.z, h = blockIdx.y;
+  const bool draft = blockIdx.x == gridDim.x - 1;
+  slim_pdl_trigger();
+  slim_pdl_wait();
+  const int len = t.len[b], t0 = draft ? 0 : blockIdx.x * TS_KEYS;
+  if (!draft && t0 >= len) return;
+  const int keys = draft ? n : min(TS_KEYS, len - t0);
+  const int* dep = t.depth + (size_t)b * n;
+  const KT* Kc = reinterpret_cast<const KT*>(p.k);
+  const KT* Kt = reinterpret_cast<const KT*>(t.k_tree) + (size_t)b * n * p.d;
+  for (int e = tid; e < TS_KEYS * half; e += blockDim.x) {
+    const int r = e / half, j = e - r * half;
+    float k1 = 0.f, k2 = 0.f;
+    int pos = 0;
+    if (r < keys && !(draft && dep[r] < 0)) {
+      const KT* row = draft ? Kt + (size_t)r * p.d : Kc + (size_t)(slim_cache_row(p, b, (t0 + r) & ~(SLIM_TT - 1)) + (r & (SLIM_TT - 1))) * p.d;
+      pos = draft ? len + dep[r] : t0 + r;
+      k1 = to_f(row[h * dk + j]); k2 = to_f(row[h * dk + half + j]);
+      if (p.rope) {
+        const float2 cs = rope_at(p, pos, j);
+        const float a = k1 * cs.x + k2 * cs.y;
+        k2 = k2 * cs.x - k1 * cs.y;
+        k1 = a;
+      }
+    }
+    Ks[r * ld + j] = k1; Ks[r * ld + half + j] = k2;
+  }
+  const KT* Q = reinterpret_cast<const KT*>(p.q) + (size_t)b * n * p.d;
+  for (int e = tid; e < n * half; e += blockDim.x) {
+    const int i = e / half, j = e - i * half;
+    float q1 = 0.f, q2 = 0.f;
+    if (dep[i] >= 0) {
+      q1 = to_f(Q[(size_t)i * p.d + h * dk + j]) * p.qscale;
+      q2 = to_f(Q[(size_t)i * p.d + h * dk + half + j]) * p.qscale;
+      if (p.rope) {
+        const float2 cs = rope_at(p, len + dep[i], j);
+        const float a = q1 * cs.x + q2 * cs.y;
+        q2 = q2 * cs.x - q1 * cs.y;
+        q1 = a;
+      }
+    }
+    Qs[i * ld + j] = q1; Qs[i * ld + half + j] = q2;
+  }
+  __syncthreads();
+  const int r = tid & (TS_KEYS - 1);
+  if (r >= keys) return;
+  const unsigned long long* mask = t.mask + (size_t)b * n;
+  float* S = t.s + ((size_t)b * p.H + h) * n * t.s_ld + (draft ? t.s_draft : t0) + r;
+  for (int i0 = tid / TS_KEYS; i0 < n; i0 += 16) {   // four tokens at a time: i0, i0 + 4, i0 + 8, i0 + 12
+    float a[4] = {0.f, 0.f, 0.f, 0.f};
+    const int i1 = min(i0 + 4, n - 1), i2 = min(i0 + 8, n - 1), i3 = min(i0 + 12, n - 1);
+    for (int j = 0; j < dk; ++j) {
+      const float k = Ks[r * ld + j];
+      a[0] = fmaf(k, Qs[i0 * ld + j], a[0]); a[1] = fmaf(k, Qs[i1 * ld + j], a[1]);
+      a[2] = fmaf(k, Qs[i2 * ld + j], a[2]); a[3] = fmaf(k, Qs[i3 * ld + j], a[3]);
+    }
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      const int i = i0 + 4 * x;
+      if (i < n) S[(size_t)i * t.s_ld] = (draft && !((mask[i] >> r) & 1)) ? -INFINITY : a[x];
+    }
+  }
+}
+
+// m and 1 / l of every row (one warp a row); a token that is padding, or whose row is empty, gets 1 / l = 0.
+__global__ void __launch_bounds__(256) slim_tree_stat_kernel(const SlimDecodeParams p, const SlimTreeView t) {
+  slim_pdl_trigger();
+  slim_pdl_wait();
+  const int lane = threadIdx.x & 31, R = p.H * t.n;
+  const int row = blockIdx.x * 8 + (threadIdx.x >> 5), b = blockIdx.y;
+  if (row >= R) return;
+  const int i = row % t.n, len = t.len[b];
+  float m = -INFINITY, l = 0.f;
+  if (t.depth[(size_t)b * t.n + i] >= 0) {
+    const float* S = t.s + ((size_t)b * R + row) * t.s_ld;
+    for (int x = lane; x < len; x += 32) m = fmaxf(m, S[x]);
+    for (int x = lane; x < t.n; x += 32) m = fmaxf(m, S[t.s_draft + x]);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+    const float ms = m == -INFINITY ? 0.f : m;
+    for (int x = lane; x < len; x += 32) l += exp2f(S[x] - ms);
+    for (int x = lane; x < t.n; x += 32) l += exp2f(S[t.s_draft + x] - ms);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
+    m = ms;
+  }
+  if (lane == 0) {
+    t.m[(size_t)b * R + row] = l != 0.f ? m : 0.f;
+    t.inv_l[(size_t)b * R + row] = l != 0.f ? 1.f / l : 0.f;       // (NaN stays NaN)
+  }
+}
+
+// U = P K, 64 rows x 64 columns a block, 16 keys a step; blockIdx.z = sequence x part of the keys.
+template <typename KT>
+__global__ void __launch_bounds__(256) slim_tree_sum_kernel(const SlimDecodeParams p, const SlimTreeView t) {
+  __shared__ float Ps[16][68], Bs[16][64];
+  slim_pdl_trigger();
+  slim_pdl_wait();
+  const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4, R = p.H * t.n;
+  const int b = blockIdx.z / t.parts, part = blockIdx.z % t.parts;
+  const int r0 = blockIdx.y * 64, c0 = blockIdx.x * 64, len = t.len[b];
+  const int nb = (len + 15) / 16, nd = (t.n + 15) / 16;            // 16-key steps: cached, drafted
+  const int s0 = (int)((long long)(nb + nd) * part / t.parts), s1 = (int)((long long)(nb + nd) * (part + 1) / t.parts);
+  const KT* Kc = reinterpret_cast<const KT*>(p.k);
+  const KT* Kt = reinterpret_cast<const KT*>(t.k_tree) + (size_t)b * t.n * p.d;
+  float acc[4][4];
+#pragma unroll
+  for (int x = 0; x < 4; ++x)
+#pragma unroll
+    for (int y = 0; y < 4; ++y) acc[x][y] = 0.f;
+  for (int s = s0; s < s1; ++s) {
+    const bool draft = s >= nb;
+    const int t0 = (draft ? s - nb : s) * 16, keys = min(16, (draft ? t.n : len) - t0);
+    const KT* K0 = draft ? Kt + (size_t)t0 * p.d : Kc + (size_t)slim_cache_row(p, b, t0) * p.d;
+    __syncthreads();
+    for (int e = tid; e < 64 * 16; e += 256) {
+      const int r = e >> 4, k = e & 15;
+      float v = 0.f;
+      if (r0 + r < R && k < keys) {
+        const size_t row = (size_t)b * R + r0 + r;
+        const float il = t.inv_l[row];
+        if (il != 0.f) v = exp2f(t.s[row * t.s_ld + (draft ? t.s_draft : 0) + t0 + k] - t.m[row]) * il;
+      }
+      Ps[k][r] = v;
+    }
+    for (int e = tid; e < 16 * 64; e += 256) {
+      const int k = e >> 6, c = e & 63;
+      const bool live = k < keys && c0 + c < p.d && !(draft && t.depth[(size_t)b * t.n + t0 + k] < 0);
+      Bs[k][c] = live ? to_f(K0[(size_t)k * p.d + c0 + c]) : 0.f;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < 16; ++k) {
+      const float4 a = *reinterpret_cast<const float4*>(&Ps[k][4 * ty]), w = *reinterpret_cast<const float4*>(&Bs[k][4 * tx]);
+      const float av[4] = {a.x, a.y, a.z, a.w}, wv[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+      for (int x = 0; x < 4; ++x)
+#pragma unroll
+        for (int y = 0; y < 4; ++y) acc[x][y] = fmaf(av[x], wv[y], acc[x][y]);
+    }
+  }
+#pragma unroll
+  for (int x = 0; x < 4; ++x) {
+    const int r = r0 + 4 * ty + x;
+    if (r >= R) continue;
+    float* U = t.u + (((size_t)part * p.batch + b) * R + r) * p.d + c0 + 4 * tx;
+#pragma unroll
+    for (int y = 0; y < 4; ++y)
+      if (c0 + 4 * tx + y < p.d) U[y] = acc[x][y];
+  }
+}
+
+// o = u W_KV,h: 16 (sequence, token) rows x 32 columns of one head a block; eight threads share a column's j.
+template <typename KT>
+__global__ void __launch_bounds__(256) slim_tree_project_kernel(const SlimDecodeParams p, const SlimTreeView t, KT* __restrict__ o) {
+  __shared__ float Us[16][64 + 1], Rs[8][16][32];
+  slim_pdl_trigger();
+  slim_pdl_wait();
+  const int tid = threadIdx.x, c = tid & 31, g = tid >> 5, n = t.n, d = p.d, dk = p.d_k, h = blockIdx.z;
+  const int m0 = blockIdx.y * 16, M = p.batch * n, col = blockIdx.x * 32 + c;
+  const KT* W = reinterpret_cast<const KT*>(p.wkv) + (size_t)h * d * dk;
+  float acc[16];
+#pragma unroll
+  for (int r = 0; r < 16; ++r) acc[r] = 0.f;
+  for (int j0 = 0; j0 < d; j0 += 64) {
+    __syncthreads();
+    for (int e = tid; e < 16 * 64; e += 256) {
+      const int r = e >> 6, j = j0 + (e & 63), m = m0 + r;
+      float v = 0.f;
+      if (m < M && j < d) {
+        const float* U = t.u + (((size_t)(m / n) * p.H + h) * n + m % n) * d + j;
+        for (int s = 0; s < t.parts; ++s) v += U[(size_t)s * p.batch * p.H * n * d];
+      }
+      Us[r][e & 63] = v;
+    }
+    __syncthreads();
+    if (col < dk)
+      for (int j = g; j < 64 && j0 + j < d; j += 8) {
+        const float w = to_f(W[(size_t)(j0 + j) * dk + col]);
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[r] = fmaf(Us[r][j], w, acc[r]);
+      }
+  }
+#pragma unroll
+  for (int r = 0; r < 16; ++r) Rs[g][r][c] = acc[r];
+  __syncthreads();
+  for (int r = g; r < 16; r += 8) {
+    if (m0 + r >= M || col >= dk) continue;
+    float v = 0.f;
+#pragma unroll
+    for (int x = 0; x < 8; ++x) v += Rs[x][r][c];
+    put(o + (size_t)(m0 + r) * d + h * dk + col, v);
+  }
+}
+
+template <typename KT>
+cudaError_t launch_generic(const slim_ctx* ctx, const SlimDecodeParams& p, const SlimTreeView& t, void* o, cudaStream_t st) {
+  const size_t smem = sizeof(float) * (size_t)(TS_KEYS + t.n) * (p.d_k + 1);
+  auto ks = slim_tree_scores_kernel<KT>;
+  cudaError_t e = cudaFuncSetAttribute(ks, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  if (e != cudaSuccess) return e;
+  const int R = p.H * t.n;
+  e = slim_launch_pdl(ks, dim3((p.t_cap + TS_KEYS - 1) / TS_KEYS + 1, p.H, p.batch), dim3(256), smem, st, p, t);
+  if (e == cudaSuccess) e = slim_launch_pdl(slim_tree_stat_kernel, dim3((R + 7) / 8, p.batch), dim3(256), 0, st, p, t);
+  if (e == cudaSuccess)
+    e = slim_launch_pdl(slim_tree_sum_kernel<KT>, dim3((p.d + 63) / 64, (R + 63) / 64, p.batch * t.parts), dim3(256), 0, st, p, t);
+  if (e == cudaSuccess)
+    e = slim_launch_pdl(slim_tree_project_kernel<KT>, dim3((p.d_k + 31) / 32, (p.batch * t.n + 15) / 16, p.H), dim3(256), 0, st, p, t, (KT*)o);
+  return e;
+}
+
+inline size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
+
+}  // namespace
+
+// Parts the keys are cut into: enough blocks for two on every SM, never more than 32.
+static int tree_parts(const slim_ctx* ctx, int batch, int t_cap, int n) {
+  const long long tiles = (long long)((ctx->d + 63) / 64) * ((ctx->H * n + 63) / 64) * batch;
+  long long parts = (2 * ctx->num_sms + tiles - 1) / tiles;
+  const long long most = (t_cap + 63) / 64;
+  if (parts > most) parts = most;
+  if (parts > 32) parts = 32;
+  return parts < 1 ? 1 : (int)parts;
+}
+
+SlimTreeLayout slim_tree_ws_layout(const slim_ctx* ctx, int batch, int t_cap, int n) {
+  SlimTreeLayout L;
+  const size_t rows = (size_t)batch * ctx->H * n;
+  L.parts = tree_parts(ctx, batch, t_cap, n);
+  L.s_draft = (t_cap + 63) / 64 * 64;
+  L.s_ld = L.s_draft + 64;
+  size_t off = 0;
+  L.mask = off; off = align256(off + sizeof(unsigned long long) * (size_t)batch * n);
+  L.depth = off; off = align256(off + sizeof(int) * (size_t)batch * n);
+  L.len = off; off = align256(off + sizeof(int) * (size_t)batch);
+  L.m = off; off = align256(off + sizeof(float) * rows);
+  L.inv_l = off; off = align256(off + sizeof(float) * rows);
+  L.s = off; off = align256(off + sizeof(float) * rows * L.s_ld);
+  L.u = off; off = align256(off + sizeof(float) * (size_t)L.parts * rows * ctx->d);
+  L.total = off;
+  return L;
+}
+
+cudaError_t slim_launch_tree(const slim_ctx* ctx, const SlimDecodeParams& p, const void* k_tree, const int32_t* parents, int n,
+                             void* o, char* ws, cudaStream_t st) {
+  const SlimTreeLayout L = slim_tree_ws_layout(ctx, p.batch, p.t_cap, n);
+  SlimTreeView t;
+  t.n = n; t.k_tree = k_tree; t.parts = L.parts; t.s_ld = L.s_ld; t.s_draft = L.s_draft;
+  t.mask = reinterpret_cast<unsigned long long*>(ws + L.mask);
+  t.depth = reinterpret_cast<int*>(ws + L.depth);
+  t.len = reinterpret_cast<int*>(ws + L.len);
+  t.m = reinterpret_cast<float*>(ws + L.m);
+  t.inv_l = reinterpret_cast<float*>(ws + L.inv_l);
+  t.s = reinterpret_cast<float*>(ws + L.s);
+  t.u = reinterpret_cast<float*>(ws + L.u);
+  cudaError_t e = slim_launch_pdl(slim_tree_layout_kernel, dim3(p.batch), dim3(64), 0, st, parents, p.lengths, n, p.t_cap, t.mask,
+                                  t.depth, t.len, p.status);
+  if (e != cudaSuccess) return e;
+  return p.dtype == SLIM_BF16 ? launch_generic<__nv_bfloat16>(ctx, p, t, o, st) : launch_generic<float>(ctx, p, t, o, st);
+}

@@ -32,6 +32,7 @@ class SlimLayer:
             assert workspace.numel() >= need and workspace.data_ptr() % 256 == 0
             self.workspace = workspace
             self.o = torch.empty((batch, d), dtype=torch.float32, device=self.device)
+            self._extra = None
 
     # ---- set-up -------------------------------------------------------------
     def set_weights(self, W_K, W_V, want_wkv: bool = False):
@@ -66,6 +67,88 @@ class SlimLayer:
         B.slim_decode_step(self.ctx, q, k_new, self.cache, lengths, o, self.workspace,
                            torch.cuda.current_stream(self.device).cuda_stream)
         return o
+
+    # ---- drafted tokens, cache budget -------------------------------------------
+    def _arg(self, name: str, x: torch.Tensor, shape, dtype) -> torch.Tensor:
+        if tuple(x.shape) != tuple(shape) or x.dtype != dtype or x.device != self.device or not x.is_contiguous():
+            raise ValueError(f"{name}: a contiguous {dtype} tensor of shape {tuple(shape)} on {self.device} is needed, got "
+                             f"{x.dtype} {tuple(x.shape)} on {x.device}" + ("" if x.is_contiguous() else ", not contiguous"))
+        return x
+
+    def _scratch(self, need: int) -> torch.Tensor:
+        """Scratch of the calls below, kept and grown; calls of one layer run one after another on a stream."""
+        if need == 0:
+            raise ValueError("unsupported sizes")
+        if self._extra is None or self._extra.numel() < need:
+            self._extra = torch.empty(need, dtype=torch.uint8, device=self.device)
+        return self._extra
+
+    def tree_decode(self, q: torch.Tensor, k_tree: torch.Tensor, lengths: torch.Tensor, parents: torch.Tensor,
+                    o: torch.Tensor | None = None) -> torch.Tensor:
+        """Attention of q.shape[1] drafted tokens a sequence (binding.slim_tree_decode); o has the layer's dtype."""
+        if q.dim() != 3:
+            raise ValueError("q: [batch, n, d] is needed")
+        n, i32 = q.shape[1], torch.int32
+        self._arg("q", q, (self.batch, n, self.d), self.tdtype)
+        self._arg("k_tree", k_tree, (self.batch, n, self.d), self.tdtype)
+        self._arg("lengths", lengths, (self.batch,), i32)
+        self._arg("parents", parents, (self.batch, n), i32)
+        o = torch.empty_like(q) if o is None else self._arg("o", o, q.shape, self.tdtype)
+        with torch.cuda.device(self.device):
+            ws = self._scratch(B.slim_tree_workspace_bytes(self.ctx, self.batch, self.t_cap, n))
+            B.slim_tree_decode(self.ctx, q, k_tree, self.cache, lengths, parents, n, o, ws,
+                               torch.cuda.current_stream(self.device).cuda_stream)
+        return o
+
+    def tree_verify(self, p: torch.Tensor, q: torch.Tensor, tokens: torch.Tensor, parents: torch.Tensor, r: torch.Tensor):
+        """(path [batch, n], count [batch], next_token [batch]) of binding.slim_tree_verify."""
+        if p.dim() != 3:
+            raise ValueError("p: [batch, n, vocab] is needed")
+        b, n, vocab = p.shape
+        f32, i32 = torch.float32, torch.int32
+        self._arg("p", p, (b, n, vocab), f32)
+        self._arg("q", q, (b, n, vocab), f32)
+        self._arg("tokens", tokens, (b, n), i32)
+        self._arg("parents", parents, (b, n), i32)
+        self._arg("r", r, (b, n), f32)
+        path, count, nxt = (torch.empty(s, dtype=i32, device=self.device) for s in ((b, n), (b,), (b,)))
+        with torch.cuda.device(self.device):
+            B.slim_tree_verify(self.ctx, p, q, tokens, parents, r, b, n, vocab, path, count, nxt,
+                               torch.cuda.current_stream(self.device).cuda_stream)
+        return path, count, nxt
+
+    def tree_commit(self, k_tree: torch.Tensor, lengths: torch.Tensor, path: torch.Tensor, count: torch.Tensor) -> None:
+        """Accepted keys into the cache (binding.slim_tree_commit); the caller adds count to lengths after the last layer."""
+        n, i32 = k_tree.shape[1], torch.int32
+        self._arg("k_tree", k_tree, (self.batch, n, self.d), self.tdtype)
+        self._arg("lengths", lengths, (self.batch,), i32)
+        self._arg("path", path, (self.batch, n), i32)
+        self._arg("count", count, (self.batch,), i32)
+        with torch.cuda.device(self.device):
+            B.slim_tree_commit(self.ctx, self.cache, k_tree, lengths, path, count, n,
+                               torch.cuda.current_stream(self.device).cuda_stream)
+
+    def accumulate_weights(self, q: torch.Tensor, lengths: torch.Tensor, acc: torch.Tensor) -> torch.Tensor:
+        """acc [batch, t_cap] += the step's probabilities summed over the heads (binding.slim_accumulate_weights)."""
+        self._arg("q", q, (self.batch, self.d), self.tdtype)
+        self._arg("lengths", lengths, (self.batch,), torch.int32)
+        self._arg("acc", acc, (self.batch, self.t_cap), torch.float32)
+        with torch.cuda.device(self.device):
+            ws = self._scratch(B.slim_weights_workspace_bytes(self.ctx, self.batch, self.t_cap))
+            B.slim_accumulate_weights(self.ctx, q, self.cache, lengths, acc, ws, torch.cuda.current_stream(self.device).cuda_stream)
+        return acc
+
+    def evict(self, lengths: torch.Tensor, acc: torch.Tensor, budget: int, recent: int) -> torch.Tensor:
+        """Bring sequences longer than `budget` down to it (binding.slim_evict); returns kept [batch, budget].  The caller
+        clamps lengths to the budget after the last layer."""
+        self._arg("lengths", lengths, (self.batch,), torch.int32)
+        self._arg("acc", acc, (self.batch, self.t_cap), torch.float32)
+        kept = torch.empty((self.batch, max(int(budget), 0)), dtype=torch.int32, device=self.device)
+        with torch.cuda.device(self.device):
+            ws = self._scratch(B.slim_evict_workspace_bytes(self.ctx, self.batch, self.t_cap))
+            B.slim_evict(self.ctx, self.cache, lengths, acc, int(budget), int(recent), kept, ws,
+                         torch.cuda.current_stream(self.device).cuda_stream)
+        return kept
 
     def profile(self, enable: bool) -> None:
         B.slim_profile_enable(self.ctx, enable)

@@ -1,0 +1,441 @@
+"""Drafted tokens through the C ABI: attention for a tree over the cache, verification, commit -- against the float64
+definitions.  Cache rows behind the lengths, unused pages and padding tokens hold NaN.
+
+Tolerances are worst-case bounds worked out from the roundings (u = half a step of the type):
+  arguments     a sum of d_k products with relative errors e_s each is off by at most
+                arg e_s, arg = sum |q_j k_j| / sqrt(d_k); e_s = 2 u_tf32 + (d_k + 16) 2^-24 on the tensor cores (operands
+                rounded to tf32, u_tf32 = 2^-11 -- the instruction may cut instead of rounding, 2^-10), (d_k + 16) 2^-24 else
+  probabilities relative error 2 arg e_s + (T + 16) 2^-24 (numerator and denominator), + 2^-8 where they are rounded
+                to bf16, times mass = (sum p |k|) |W_KV|
+  u, o          2^-8 each of mass and |o| where rounded to bf16; sums of d products (d + 16) 2^-24 of mass."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import draft_oracle as do
+from paper_2503_05840_b200 import binding as B
+from paper_2503_05840_b200 import synth
+from paper_2503_05840_b200.layer import SlimLayer
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+def tolerance(o, mass, arg, T, d, d_k, dtype, tensor_cores):
+    f = 2.0 ** -24
+    es = (d_k + 16) * f + (2.0 ** -9 if tensor_cores else 0.0)
+    ep = 2 * arg[:, None] * es + (T + 16) * f + (2.0 ** -8 if tensor_cores else 0.0)
+    ep = np.expm1(ep)
+    tol = mass * (ep + (d + 16) * f + (2.0 ** -8 if tensor_cores else 0.0))
+    return tol + (2.0 ** -8 if dtype == "bf16" else 2.0 ** -24) * (np.abs(o) + tol) + 1e-30
+
+
+def random_parents(g, n, pad=True):
+    par = [-1]
+    for i in range(1, n):
+        p = int(g.integers(-1, i)) if g.random() < 0.9 else -1
+        par.append(-2 if pad and g.random() < 0.15 else p)
+    for i in range(n):          # a child of padding is padding too (otherwise the tree is refused)
+        if par[i] >= 0 and par[par[i]] < -1:
+            par[i] = -2
+    return par
+
+
+def to_dev(x, dtype):
+    return torch.from_numpy(np.ascontiguousarray(x, dtype=np.float32)).to(DEV, torch.float32 if dtype == "f32" else torch.bfloat16)
+
+
+class Case:
+    """Inputs of one batch, the library's objects over them, and the definition's answer."""
+
+    def __init__(self, d, H, theta, dtype, lengths, parents, page=0, seed=0, spread=1.0, t_cap=None):
+        g = np.random.default_rng(seed)
+        self.d, self.H, self.theta, self.dtype = d, H, theta, dtype
+        self.lengths, self.parents = np.array(lengths, np.int32), np.array(parents, np.int32)
+        self.batch, self.n = self.parents.shape
+        rnd = lambda *s: synth.round_to_dtype(spread * g.standard_normal(s), dtype)
+        self.q, self.kt = rnd(self.batch, self.n, d), rnd(self.batch, self.n, d)
+        self.K = [rnd(int(L), d) for L in lengths]
+        self.W = synth.round_to_dtype(g.standard_normal((d, d)) / np.sqrt(d), dtype).astype(np.float64)
+        for b, chains in enumerate(map(do.tree_chains, parents)):
+            for i, c in enumerate(chains):
+                if not c:
+                    self.q[b, i] = self.kt[b, i] = np.nan
+        t_cap = t_cap or max(max(lengths), 1) + 7
+        if page:
+            t_cap = -(-t_cap // page) * page
+        self.t_cap, self.page = t_cap, page
+        self.ctx = B.slim_create(d, H, d // H, theta, B.SLIM_F32 if dtype == "f32" else B.SLIM_BF16)
+        B.slim_set_wkv(self.ctx, self.W)
+        td = torch.float32 if dtype == "f32" else torch.bfloat16
+        if page:
+            mp = t_cap // page
+            pages = self.batch * mp + 3
+            tab = g.permutation(pages)[:self.batch * mp].astype(np.int32).reshape(self.batch, mp)
+            self.store = torch.full((pages, page, d), float("nan"), dtype=td, device=DEV)
+            self.table = torch.from_numpy(tab).to(DEV)
+            self.cache = B.slim_cache_create_paged(self.ctx, self.store, pages, page, self.table, self.batch, mp)
+            self.where = lambda b, t: (int(tab[b, t // page]), t % page)
+        else:
+            self.store = torch.full((self.batch, t_cap, d), float("nan"), dtype=td, device=DEV)
+            self.cache = B.slim_cache_create(self.ctx, self.store, self.batch, t_cap)
+            self.where = lambda b, t: (b, t)
+        for b in range(self.batch):
+            rows = to_dev(self.K[b], dtype)
+            if page:
+                for a in range(0, len(rows), page):
+                    self.store[self.where(b, a)[0], :len(rows[a:a + page])] = rows[a:a + page]
+            else:
+                self.store[b, :len(rows)] = rows
+        self.dq, self.dkt = to_dev(self.q, dtype), to_dev(self.kt, dtype)
+        self.dlen, self.dpar = torch.from_numpy(self.lengths).to(DEV), torch.from_numpy(self.parents).to(DEV)
+        self.o = torch.full((self.batch, self.n, d), float("nan"), dtype=td, device=DEV)
+        self.ws = torch.empty(B.slim_tree_workspace_bytes(self.ctx, self.batch, t_cap, self.n), dtype=torch.uint8, device=DEV)
+        self.ws.fill_(255)      # NaN in every scratch word
+
+    def call(self, stream=None):
+        st = (stream or torch.cuda.current_stream()).cuda_stream
+        B.slim_tree_decode(self.ctx, self.dq, self.dkt, self.cache, self.dlen, self.dpar, self.n, self.o, self.ws, st)
+
+    def status(self):
+        return B.slim_device_status(self.ctx, torch.cuda.current_stream().cuda_stream)
+
+    def check(self, got=None):
+        got = (self.o if got is None else got).float().cpu().numpy().astype(np.float64)
+        d_k = self.d // self.H
+        tc = self.dtype == "bf16" and self.d % 64 == 0 and d_k in (64, 96, 128)
+        worst = 0.0
+        for b in range(self.batch):
+            o, mass, arg = do.tree_attention(self.q[b], self.kt[b], self.K[b], list(self.parents[b]), self.W, self.H, self.theta)
+            tol = tolerance(o, mass, arg, len(self.K[b]) + self.n, self.d, d_k, self.dtype, tc)
+            err = np.abs(got[b] - o)
+            assert np.all(err <= tol), f"sequence {b}: {np.max(err / tol):.2f} of the bound"
+            for i, c in enumerate(do.tree_chains(list(self.parents[b]))):
+                if not c:
+                    assert np.all(got[b, i] == 0)
+            norm = np.linalg.norm(o)
+            if norm > 0:
+                worst = max(worst, np.linalg.norm(got[b] - o) / norm)
+        return worst
+
+    def close(self):
+        B.slim_cache_destroy(self.cache)
+        B.slim_destroy(self.ctx)
+
+    def __enter__(self):
+        return self
+
+    def __exit__(self, *a):
+        torch.cuda.synchronize()
+        self.close()
+
+
+LENGTHS = [0, 1, 15, 16, 17, 63, 64, 65, 127, 128, 129, 300]
+
+
+@pytest.mark.parametrize("d,H,theta,dtype,page,n", [
+    (384, 6, 1.0e4, "f32", 0, 8), (384, 6, 0.0, "f32", 16, 5), (200, 5, 1.0e4, "f32", 0, 3), (24, 3, 1.0e4, "f32", 0, 64),
+    (512, 4, 1.0e6, "bf16", 0, 16), (512, 4, 0.0, "bf16", 0, 64), (512, 8, 1.0e4, "bf16", 16, 7), (384, 4, 1.0e4, "bf16", 64, 33),
+    (576, 6, 1.0e4, "bf16", 48, 2), (1280, 20, 0.0, "bf16", 0, 5), (192, 2, 1.0e4, "bf16", 0, 1), (64, 1, 1.0e4, "bf16", 0, 64),
+    (128, 1, 1.0e4, "bf16", 32, 17), (1000, 10, 1.0e4, "bf16", 0, 6), (80, 2, 1.0e4, "bf16", 16, 9)])
+def test_tree_against_the_definition(d, H, theta, dtype, page, n):
+    g = np.random.default_rng(d + n)
+    parents = [random_parents(g, n) for _ in LENGTHS]
+    parents[3] = [-2] * n                                    # a sequence that drafted nothing
+    with Case(d, H, theta, dtype, LENGTHS, parents, page, seed=n) as c:
+        c.call()
+        assert c.status() == B.SLIM_OK
+        worst = c.check()
+        print(f"worst relative error of a sequence {worst:.2e}")
+
+
+@pytest.mark.parametrize("spread", [0.05, 4.0, 12.0])
+def test_flat_and_peaked_softmax(spread):
+    g = np.random.default_rng(5)
+    with Case(512, 4, 1.0e4, "bf16", [700, 257], [random_parents(g, 12) for _ in range(2)], seed=7, spread=spread) as c:
+        c.call()
+        assert c.status() == B.SLIM_OK
+        c.check()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_arguments_that_jump_between_blocks_of_rows(dtype):
+    """Every block of 128 rows lies at another level of softmax arguments, hundreds apart both ways: the reference exponent
+    changes from block to block and blocks far below the top must vanish, not overflow."""
+    d, H, L = 256, 2, 128 * 7 + 40
+    with Case(d, H, 0.0, dtype, [L], [[-1, 0, 1, -1]], seed=3) as c:
+        level = np.array([0, 40, -300, 35, 300, 299, -20, 290], np.float32)[np.arange(L) // 128]
+        c.q[:] = 0; c.q[..., ::32] = 8.0                      # every head's argument is 8 * sum of its columns' strides / sqrt(d_k)
+        c.K[0][:, ::32] = 0.01 * c.K[0][:, ::32] + level[:, None] * np.float32(np.sqrt(d // H) / 32.0)
+        c.K[0] = synth.round_to_dtype(c.K[0], dtype)
+        c.kt[0, :, ::32] = 30.0
+        c.kt = synth.round_to_dtype(c.kt, dtype)
+        c.store[0, :L] = to_dev(c.K[0], dtype)
+        c.dq, c.dkt = to_dev(c.q, dtype), to_dev(c.kt, dtype)
+        c.call()
+        assert c.status() == B.SLIM_OK
+        c.check()
+
+
+def test_broken_trees_and_lengths_are_reported():
+    with Case(128, 2, 1.0e4, "bf16", [20, 20], [[-1, 0, 1], [-1, 0, 1]], seed=1) as c:
+        c.dpar = torch.tensor([[-1, 1, 0], [-1, -2, 1]], dtype=torch.int32, device=DEV)     # its own parent; a child of padding
+        c.call()
+        assert c.status() == B.SLIM_ERR_TREE
+        c.parents = np.array([[-1, -2, 0], [-1, -2, -2]], np.int32)
+        c.check()
+        c.dlen = torch.tensor([-5, 10 ** 9], dtype=torch.int32, device=DEV)                 # nothing cached; clamped to the capacity
+        c.store[1] = 0
+        c.call()
+        assert c.status() == B.SLIM_ERR_TREE                 # the tree is still broken: of two reports the higher code stays
+        c.dpar = torch.tensor([[-1, -2, 0], [-1, -2, -2]], dtype=torch.int32, device=DEV)
+        c.call()
+        assert c.status() == B.SLIM_ERR_CAPACITY
+        assert torch.isfinite(c.o.float()).all()
+    with Case(128, 2, 1.0e4, "bf16", [20, 40], [[-1], [-1]], page=16, seed=1) as c:
+        c.store[0] = 0                                       # what a page id outside the pool is replaced by
+        c.table[1, 1] = 10 ** 6
+        c.call()
+        assert c.status() == B.SLIM_ERR_CAPACITY
+        assert torch.isfinite(c.o.float()).all()
+
+
+def test_refusals():
+    with Case(128, 2, 1.0e4, "bf16", [20], [[-1, 0]], seed=1) as c:
+        L, st = B.lib(), torch.cuda.current_stream().cuda_stream
+        p = lambda x: x.data_ptr() if torch.is_tensor(x) else x
+        call = lambda **k: L.slim_tree_decode(*[p(k.get(name, v)) for name, v in (
+            ("ctx", c.ctx), ("q", c.dq), ("k_tree", c.dkt), ("cache", c.cache), ("lengths", c.dlen), ("parents", c.dpar), ("n", c.n),
+            ("o", c.o), ("ws", c.ws), ("st", st))])
+        assert call() == B.SLIM_OK
+        for k in ("q", "k_tree", "cache", "lengths", "parents", "o", "ws"):
+            assert call(**{k: None}) == B.SLIM_ERR_INVALID_ARG, k
+        for k, x in (("q", c.dq), ("k_tree", c.dkt), ("o", c.o), ("ws", c.ws)):
+            assert call(**{k: x.data_ptr() + 8}) == B.SLIM_ERR_INVALID_ARG, k
+        for n in (0, -1, 65):
+            assert call(n=n) == B.SLIM_ERR_INVALID_ARG
+            assert L.slim_tree_workspace_bytes(c.ctx, 1, 16, n) == 0
+        other = B.slim_create(128, 2, 64, 1.0e4, B.SLIM_BF16)
+        assert call(ctx=other) == B.SLIM_ERR_INVALID_ARG       # a cache of another context
+        cache = B.slim_cache_create(other, c.store, 1, c.t_cap)
+        assert call(ctx=other, cache=cache) == B.SLIM_ERR_NO_WEIGHTS
+        B.slim_cache_destroy(cache); B.slim_destroy(other)
+        fp8 = SlimLayer(128, 2, 64, 0.0, "fp8", 1, 32, DEV)
+        fp8.set_wkv(np.eye(128))
+        with pytest.raises(B.SlimError) as e:
+            fp8.tree_decode(c.dq, c.dkt, c.dlen, c.dpar)
+        assert e.value.status == B.SLIM_ERR_UNSUPPORTED
+        with pytest.raises(B.SlimError) as e:
+            fp8.tree_commit(c.dkt, c.dlen, c.dpar, c.dlen)
+        assert e.value.status == B.SLIM_ERR_UNSUPPORTED
+        fp8.close()
+        lay = SlimLayer(128, 2, 64, 1.0e4, "bf16", 1, 32, DEV)
+        lay.set_wkv(np.eye(128))
+        for bad in (dict(q=c.dq.float()), dict(k_tree=c.dkt[:, :1]), dict(lengths=c.dlen.long()), dict(parents=c.dpar.cpu()),
+                    dict(q=c.dq.transpose(1, 2).contiguous().transpose(1, 2)), dict(o=c.o[:, :1])):
+            with pytest.raises(ValueError):
+                lay.tree_decode(**{**dict(q=c.dq, k_tree=c.dkt, lengths=c.dlen, parents=c.dpar), **bad})
+        lay.close()
+
+
+def test_repeatable_on_streams_and_in_graphs():
+    g = np.random.default_rng(11)
+    with Case(512, 4, 1.0e4, "bf16", [900, 130], [random_parents(g, 9) for _ in range(2)], seed=2) as c:
+        c.call()
+        torch.cuda.synchronize()
+        want = c.o.clone()
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        c.o.fill_(float("nan"))
+        side.wait_stream(torch.cuda.current_stream())
+        c.call(side)
+        side.synchronize()
+        assert torch.equal(c.o, want)
+        graphs = []
+        for _ in range(2):                                   # two graphs that share the workspace, replayed in turn
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph):
+                c.call()
+            graphs.append(graph)
+        for graph in graphs + graphs:
+            c.o.fill_(float("nan"))
+            graph.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(c.o, want)
+        c.lengths[:] = [500, 77]                             # a replay reads the lengths that are there then
+        c.dlen.copy_(torch.from_numpy(c.lengths))
+        c.K = [c.K[0][:500], c.K[1][:77]]
+        graphs[0].replay()
+        assert c.status() == B.SLIM_OK
+        c.check()
+
+
+def test_tree_pages_behind_four_billion_elements():
+    """A pool whose last pages lie beyond 2^32 elements from its start."""
+    d, H, page, L = 4096, 32, 64, 200
+    pages = (1 << 32) // (page * d) + 8
+    with Case(d, H, 1.0e4, "bf16", [L], [[-1, 0, 0, 1]], page=page, seed=9) as small:
+        small.call()
+        torch.cuda.synchronize()
+        pool = torch.empty((pages, page, d), dtype=torch.bfloat16, device=DEV)
+        mp = small.table.shape[1]
+        pool[-mp:] = small.store[small.table[0].long()]
+        table = torch.arange(pages - mp, pages, dtype=torch.int32, device=DEV)[None].contiguous()
+        cache = B.slim_cache_create_paged(small.ctx, pool, pages, page, table, 1, mp)
+        st = torch.cuda.current_stream().cuda_stream
+        o = torch.empty_like(small.o)
+        B.slim_tree_decode(small.ctx, small.dq, small.dkt, cache, small.dlen, small.dpar, 4, o, small.ws, st)
+        assert small.status() == B.SLIM_OK
+        assert torch.equal(o, small.o)
+        path, count = torch.tensor([[0, 1, 3, -1]], dtype=torch.int32, device=DEV), torch.tensor([3], dtype=torch.int32, device=DEV)
+        B.slim_tree_commit(small.ctx, cache, small.dkt, small.dlen, path, count, 4, st)
+        assert small.status() == B.SLIM_OK
+        rows = pool[-mp:].view(-1, d)
+        assert torch.equal(rows[L:L + 3], small.dkt[0, [0, 1, 3]]) and rows[L + 3:small.t_cap].isnan().all()
+        B.slim_cache_destroy(cache)
+
+
+# ------------------------------------------------------------------------------------------------ verification
+def run_verify(ctx, p, q, tokens, parents, r):
+    Bn, n, V = p.shape
+    dev = lambda x, t: torch.from_numpy(np.ascontiguousarray(x)).to(DEV, t)
+    path = torch.full((Bn, n), 77, dtype=torch.int32, device=DEV)
+    count, nxt = (torch.full((Bn,), 77, dtype=torch.int32, device=DEV) for _ in range(2))
+    args = [dev(p, torch.float32), dev(q, torch.float32), dev(tokens, torch.int32), dev(parents, torch.int32), dev(r, torch.float32)]
+    B.slim_tree_verify(ctx, *args, Bn, n, V, path, count, nxt, torch.cuda.current_stream().cuda_stream)
+    return path.cpu().numpy(), count.cpu().numpy(), nxt.cpu().numpy(), B.slim_device_status(ctx, torch.cuda.current_stream().cuda_stream)
+
+
+@pytest.fixture()
+def ctx():
+    c = B.slim_create(64, 1, 64, 0.0, B.SLIM_F32)
+    yield c
+    B.slim_destroy(c)
+
+
+def draws(g, Bn, n, V, kids, sharp=2.0, close=1.0):
+    lp = sharp * g.standard_normal((Bn, n, V))
+    lq = lp + close * g.standard_normal((Bn, n, V))
+    p, q = (np.exp(x - x.max(-1, keepdims=True)) for x in (lp, lq))
+    p, q = ((x / x.sum(-1, keepdims=True)).astype(np.float32) for x in (p, q))
+    parents, tokens = np.full((Bn, n), -2, np.int32), np.zeros((Bn, n), np.int32)
+    for b in range(Bn):
+        used = {0: 0}
+        parents[b, 0] = -1
+        for i in range(1, n if b % 4 else max(1, n - 2)):
+            u = int(g.choice([x for x in used if used[x] < kids][-3:]))
+            used[u] += 1
+            used[i] = 0
+            parents[b, i] = u
+            tokens[b, i] = g.choice(V, p=q[b, u].astype(np.float64) / q[b, u].astype(np.float64).sum())
+    return p, q, tokens, parents, g.random((Bn, n)).astype(np.float32)
+
+
+@pytest.mark.parametrize("Bn,n,V,kids", [(1, 1, 1, 1), (3, 4, 2, 2), (40, 8, 5, 4), (16, 12, 131, 3), (9, 64, 1000, 5), (5, 6, 32003, 2), (2, 5, 131072, 3)])
+def test_verification_against_the_definition(ctx, Bn, n, V, kids):
+    g = np.random.default_rng(V)
+    p, q, tokens, parents, r = draws(g, Bn, n, V, kids)
+    path, count, nxt, status = run_verify(ctx, p, q, tokens, parents, r)
+    assert status == B.SLIM_OK
+    for b in range(Bn):
+        want, t = do.verify(p[b], q[b], tokens[b], parents[b], r[b])
+        assert list(path[b]) == want + [-1] * (n - len(want)) and count[b] == len(want)
+        assert nxt[b] == t
+
+
+def test_verification_edges(ctx):
+    V = 700
+    one = np.zeros((1, 3, V), np.float32)
+    one[0, 0, 5] = 1.0; one[0, 1, 9] = 1.0; one[0, 2, 11] = 1.0
+    tok, par = np.array([[0, 5, 9]], np.int32), np.array([[-1, 0, 1]], np.int32)
+    # the draft is the target: everything is accepted, whatever the numbers; the draw is the only token there is
+    path, count, nxt, st = run_verify(ctx, one, one, tok, par, np.array([[0.999, 0.999, 0.0]], np.float32))
+    assert st == B.SLIM_OK and count[0] == 3 and nxt[0] == 11
+    # a token that the target gives no probability is never accepted, not even for r = 0
+    path, count, nxt, st = run_verify(ctx, one, one, np.array([[0, 6, 9]], np.int32), par, np.zeros((1, 3), np.float32))
+    assert count[0] == 1 and nxt[0] == 5 and list(path[0]) == [0, -1, -1]
+    # nothing left of the residual (p = q and a token outside both): the distribution stays; no positive value at all: -1
+    path, count, nxt, st = run_verify(ctx, 0 * one, one, tok, par, np.full((1, 3), 0.5, np.float32))
+    assert count[0] == 1 and nxt[0] == -1 and st == B.SLIM_OK
+    # tokens outside the vocabulary and parents that are not earlier nodes are padding, and reported
+    path, count, nxt, st = run_verify(ctx, one, one, np.array([[0, V, 9]], np.int32), par, np.zeros((1, 3), np.float32))
+    assert st == B.SLIM_ERR_TREE and count[0] == 1
+    path, count, nxt, st = run_verify(ctx, one, one, tok, np.array([[-1, 2, 1]], np.int32), np.zeros((1, 3), np.float32))
+    assert st == B.SLIM_ERR_TREE and count[0] == 1
+    # draws at the ends of the range
+    flat = np.full((1, 1, V), 1.0 / V, np.float32)
+    for r0, want in ((0.0, 0), (np.float32(1 - 2.0 ** -24), V - 1)):
+        _, _, nxt, _ = run_verify(ctx, flat, flat, np.zeros((1, 1), np.int32), np.array([[-1]], np.int32), np.array([[r0]], np.float32))
+        assert nxt[0] == want
+    # NaN where a row of probabilities should be: no token, and the call comes back
+    path, count, nxt, st = run_verify(ctx, one * np.nan, one, tok, par, np.full((1, 3), 0.5, np.float32))
+    assert count[0] == 1 and nxt[0] == -1
+
+
+def test_verify_refusals(ctx):
+    x = torch.zeros(64, device=DEV)
+    i = torch.zeros(64, dtype=torch.int32, device=DEV)
+    for n, V, b in ((0, 4, 1), (65, 4, 1), (1, 0, 1), (1, 4, 0), (1, 4, 4096)):
+        with pytest.raises(B.SlimError) as e:
+            B.slim_tree_verify(ctx, x, x, i, i, x, b, n, V, i, i, i)
+        assert e.value.status == B.SLIM_ERR_INVALID_ARG
+
+
+# ------------------------------------------------------------------------------------------------ commit, and the whole loop
+@pytest.mark.parametrize("d,H,dtype,page", [(128, 2, "bf16", 0), (128, 2, "bf16", 16), (10, 5, "bf16", 0), (6, 3, "f32", 0), (384, 6, "f32", 32)])
+def test_commit_writes_accepted_rows_only(d, H, dtype, page):
+    n = 6
+    with Case(d, H, 0.0, dtype, [30, 17, 0, 40, 12], [[-1] * n] * 5, page=page, seed=4, t_cap=48) as c:
+        path = torch.tensor([[0, 2, 5, -1, -1, -1], [0, 1, 2, 3, 4, 5], [3, -1, -1, -1, -1, -1], [0, 6, -1, -1, -1, -1], [-1] * 6],
+                            dtype=torch.int32, device=DEV)
+        count = torch.tensor([3, 6, 1, 2, 0], dtype=torch.int32, device=DEV)
+        before = c.store.clone()
+        st = torch.cuda.current_stream().cuda_stream
+        B.slim_tree_commit(c.ctx, c.cache, c.dkt, c.dlen, path, count, n, st)
+        assert c.status() == B.SLIM_ERR_TREE                 # sequence 3 names token 6 of 6: left as it was
+        want = before.clone()
+        for b, rows in ((0, [0, 2, 5]), (1, range(6)), (2, [3])):
+            for j, i in enumerate(rows):
+                want[c.where(b, int(c.lengths[b]) + j)] = c.dkt[b, i]
+        assert torch.equal(torch.nan_to_num(c.store.float(), nan=1e9), torch.nan_to_num(want.float(), nan=1e9))
+        over = torch.tensor([c.t_cap - 2] * 5, dtype=torch.int32, device=DEV)
+        B.slim_tree_commit(c.ctx, c.cache, c.dkt, over, path, torch.tensor([3] * 5, dtype=torch.int32, device=DEV), n, st)
+        assert c.status() in (B.SLIM_ERR_CAPACITY, B.SLIM_ERR_TREE)
+        B.slim_tree_commit(c.ctx, c.cache, c.dkt, c.dlen, path, torch.tensor([-1, 7, 0, 0, 0], dtype=torch.int32, device=DEV), n, st)
+        assert c.status() == B.SLIM_ERR_TREE
+        assert torch.equal(torch.nan_to_num(c.store.float(), nan=1e9), torch.nan_to_num(want.float(), nan=1e9))
+
+
+@pytest.mark.parametrize("dtype,tol", [("f32", 1e-4), ("bf16", 2e-2)])
+def test_draft_verify_commit_and_decode_go_together(dtype, tol):
+    """Two rounds of drafting on one layer: the accepted path's outputs are what decode steps over the committed cache give."""
+    d, H, n, V, Bn = 512, 4, 6, 50, 3
+    g = np.random.default_rng(21)
+    lay = SlimLayer(d, H, d // H, 1.0e4, dtype, Bn, 128, DEV)
+    try:
+        lay.set_wkv(synth.round_to_dtype(g.standard_normal((d, d)) / np.sqrt(d), dtype).astype(np.float64))
+        rnd = lambda *s: to_dev(synth.round_to_dtype(g.standard_normal(s), dtype), dtype)
+        lengths = torch.tensor([40, 0, 63], dtype=torch.int32, device=DEV)
+        lay.append_k(rnd(Bn, 64, d), torch.zeros(Bn, dtype=torch.int32, device=DEV))
+        for _ in range(2):
+            p, q, tokens, parents, r = draws(g, Bn, n, V, 2, close=0.3)
+            dev = lambda x, t: torch.from_numpy(np.ascontiguousarray(x)).to(DEV, t)
+            parents_d = dev(parents, torch.int32)
+            tq, tk = rnd(Bn, n, d), rnd(Bn, n, d)
+            o = lay.tree_decode(tq, tk, lengths, parents_d)
+            path, count, nxt = lay.tree_verify(dev(p, torch.float32), dev(q, torch.float32), dev(tokens, torch.int32), parents_d, dev(r, torch.float32))
+            lay.tree_commit(tk, lengths, path, count)
+            assert lay.device_status() == B.SLIM_OK
+            hp, hc = path.cpu().numpy(), count.cpu().numpy()
+            for j in range(int(hc.max())):
+                at = [hp[b, j] if j < hc[b] else hp[b, 0] for b in range(Bn)]
+                steps = torch.stack([tq[b, at[b]] for b in range(Bn)])
+                upto = (lengths + torch.tensor([j + 1 if j < hc[b] else 1 for b in range(Bn)], device=DEV)).int()
+                one = lay.decode(steps.contiguous(), upto).clone()
+                for b in range(Bn):
+                    rms = one[b].pow(2).mean().sqrt()
+                    assert ((o[b, at[b]].float() - one[b]).abs() / torch.maximum(one[b].abs(), rms)).max().item() <= tol
+            lengths += count
+            assert int(nxt.min()) >= 0
+    finally:
+        lay.close()
