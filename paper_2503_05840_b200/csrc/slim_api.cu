@@ -760,8 +760,9 @@ slim_status slim_tree_decode(slim_ctx* ctx, const void* q, const void* k_tree, c
   if (ctx->kdtype == SLIM_FP8 || ctx->e != ctx->d) return SLIM_ERR_UNSUPPORTED;
   if (!ctx->has_weights) return SLIM_ERR_NO_WEIGHTS;
   if (!current_device_is(ctx)) return SLIM_ERR_INVALID_ARG;
-  return launched(slim_launch_tree(ctx, cache_params(ctx, cache, q, lengths), k_tree, parents, n, o, static_cast<char*>(workspace),
-                                   (cudaStream_t)stream));
+  const int tc = ctx->path_req != SLIM_PATH_GENERIC && slim_tree_tc_ok(ctx);
+  return launched(slim_launch_tree(ctx, cache_params(ctx, cache, q, lengths), k_tree, parents, n, o, static_cast<char*>(workspace), tc,
+                                   cache->total_rows, (cudaStream_t)stream));
 }
 
 slim_status slim_tree_verify(slim_ctx* ctx, const float* p, const float* q, const int32_t* tokens, const int32_t* parents, const float* r,

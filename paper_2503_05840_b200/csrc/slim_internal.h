@@ -207,7 +207,7 @@ cudaError_t slim_launch_values(const slim_ctx* ctx, const void* K, int n, float*
 
 // drafted tokens (slim_tree.cu, slim_draft.cu)
 cudaError_t slim_launch_tree(const slim_ctx* ctx, const SlimDecodeParams& p, const void* k_tree, const int32_t* parents, int n,
-                             void* o, char* ws, cudaStream_t st);
+                             void* o, char* ws, int tc, long long total_rows, cudaStream_t st);
 cudaError_t slim_launch_verify(const float* p, const float* q, const int32_t* tokens, const int32_t* parents, const float* r, int batch,
                                int n, int vocab, int32_t* path, int32_t* count, int32_t* next_token, int* status, cudaStream_t st);
 cudaError_t slim_launch_commit(const slim_ctx* ctx, const slim_cache* c, const void* k_tree, const int32_t* lengths, const int32_t* path,

@@ -8,6 +8,8 @@
 // One sequence has R = H n rows u of d numbers each, far more than on-chip memory holds, so the arguments are laid
 // down once ([b][h n + i][t], float) and the weighted sum is a matrix product P [R x T] K [T x d] cut into tiles;
 // where there are few tiles, T is cut too and the parts are added in a fixed order.
+#include <cstring>
+
 #include "slim_internal.h"
 #include "slim_sched.cuh"
 #include "slim_tree.h"
@@ -309,28 +311,42 @@ SlimTreeLayout slim_tree_ws_layout(const slim_ctx* ctx, int batch, int t_cap, in
   L.mask = off; off = align256(off + sizeof(unsigned long long) * (size_t)batch * n);
   L.depth = off; off = align256(off + sizeof(int) * (size_t)batch * n);
   L.len = off; off = align256(off + sizeof(int) * (size_t)batch);
-  L.m = off; off = align256(off + sizeof(float) * rows);
   L.inv_l = off; off = align256(off + sizeof(float) * rows);
+  L.shared_end = off;
+  L.m = off; off = align256(off + sizeof(float) * rows);
   L.s = off; off = align256(off + sizeof(float) * rows * L.s_ld);
   L.u = off; off = align256(off + sizeof(float) * (size_t)L.parts * rows * ctx->d);
   L.total = off;
+  if (slim_tree_tc_ok(ctx)) slim_tree_tc_layout(ctx, batch, t_cap, n, L);
   return L;
 }
 
+// tc: run the tensor-core kernels (the caller has checked slim_tree_tc_ok); total_rows: rows of the key storage
 cudaError_t slim_launch_tree(const slim_ctx* ctx, const SlimDecodeParams& p, const void* k_tree, const int32_t* parents, int n,
-                             void* o, char* ws, cudaStream_t st) {
+                             void* o, char* ws, int tc, long long total_rows, cudaStream_t st) {
   const SlimTreeLayout L = slim_tree_ws_layout(ctx, p.batch, p.t_cap, n);
   SlimTreeView t;
-  t.n = n; t.k_tree = k_tree; t.parts = L.parts; t.s_ld = L.s_ld; t.s_draft = L.s_draft;
+  memset(&t, 0, sizeof(t));
+  t.n = n; t.k_tree = k_tree;
   t.mask = reinterpret_cast<unsigned long long*>(ws + L.mask);
   t.depth = reinterpret_cast<int*>(ws + L.depth);
   t.len = reinterpret_cast<int*>(ws + L.len);
-  t.m = reinterpret_cast<float*>(ws + L.m);
   t.inv_l = reinterpret_cast<float*>(ws + L.inv_l);
-  t.s = reinterpret_cast<float*>(ws + L.s);
-  t.u = reinterpret_cast<float*>(ws + L.u);
   cudaError_t e = slim_launch_pdl(slim_tree_layout_kernel, dim3(p.batch), dim3(64), 0, st, parents, p.lengths, n, p.t_cap, t.mask,
                                   t.depth, t.len, p.status);
   if (e != cudaSuccess) return e;
+  if (tc) {
+    t.p = reinterpret_cast<__nv_bfloat16*>(ws + L.p); t.p_ld = L.p_ld; t.s_draft = L.p_s_draft;
+    t.stat = reinterpret_cast<float2*>(ws + L.stat);
+    t.tail = reinterpret_cast<__nv_bfloat16*>(ws + L.tail);
+    t.uh = reinterpret_cast<__nv_bfloat16*>(ws + L.uh);
+    t.part = reinterpret_cast<float*>(ws + L.part);
+    t.g_tiles = L.g_tiles; t.g_ncol = L.g_ncol; t.g_split = L.g_split; t.g_pairs = L.g_pairs; t.g_whole = L.g_whole;
+    return slim_launch_tree_tc(ctx, p, t, L, total_rows, o, st);
+  }
+  t.parts = L.parts; t.s_ld = L.s_ld; t.s_draft = L.s_draft;
+  t.m = reinterpret_cast<float*>(ws + L.m);
+  t.s = reinterpret_cast<float*>(ws + L.s);
+  t.u = reinterpret_cast<float*>(ws + L.u);
   return p.dtype == SLIM_BF16 ? launch_generic<__nv_bfloat16>(ctx, p, t, o, st) : launch_generic<float>(ctx, p, t, o, st);
 }

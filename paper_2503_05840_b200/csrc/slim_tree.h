@@ -15,11 +15,27 @@ struct SlimTreeView {
   int s_ld, s_draft;
   float* u;                          // [parts][batch][H n][d]
   int parts;
+  // tensor-core path
+  __nv_bfloat16* p;                  // [batch][H n][p_ld] probabilities relative to their block's reference; drafted keys from s_draft on
+  int p_ld;
+  float2* stat;                      // [batch][blocks of 128 keys + 1 (drafted)][H n] (reference, sum)
+  __nv_bfloat16* tail;               // [batch][128][d] partial last block of cached rows, drafted keys
+  __nv_bfloat16* uh;                 // [H][batch n][d] weighted sums
+  float* part;                       // [slots][mt 256][256] sums of pieces that are not whole tiles
+  int g_tiles, g_ncol, g_split, g_pairs, g_whole;      // schedule of the product (slim_tree_tc.cu)
 };
 
 struct SlimTreeLayout {
-  size_t mask, depth, len, m, inv_l, s, u, total;
+  size_t mask, depth, len, inv_l, shared_end;
+  size_t m, s, u;                    // CUDA-core kernels
+  size_t p, stat, tail, uh, part;    // tensor-core kernels (their scratch and the other kernels' share the same memory)
+  size_t total;
   int parts, s_ld, s_draft;
+  int mt, p_ld, p_s_draft, g_tiles, g_ncol, g_split, g_pairs, g_whole;
 };
 
+int  slim_tree_tc_ok(const slim_ctx* ctx);
+void slim_tree_tc_layout(const slim_ctx* ctx, int batch, int t_cap, int n, SlimTreeLayout& L);
+cudaError_t slim_launch_tree_tc(const slim_ctx* ctx, const SlimDecodeParams& p, const SlimTreeView& t, const SlimTreeLayout& L,
+                                long long total_rows, void* o, cudaStream_t st);
 SlimTreeLayout slim_tree_ws_layout(const slim_ctx* ctx, int batch, int t_cap, int n);

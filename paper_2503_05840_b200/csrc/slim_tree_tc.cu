@@ -1,0 +1,999 @@
+// Tensor-core path of slim_tree_decode (bf16 caches, d % 64 == 0, d_k in {64, 96, 128}).
+//
+// One sequence of L rows and n tokens has R = H n rows of probabilities and a weighted sum of R x d numbers (32 MB at
+// n = 64, d = 4096): it cannot stay on chip as the one-token kernel's does, and its products, 2 L R d, are H times
+// those of the scores.  So the step is a chain of kernels around one large matrix product:
+//   layout      the trees' masks and depths; the last, partial block of 64 cached rows and the drafted keys, zero-padded,
+//               in a scratch tail, so that the product only meets whole blocks of 64 finite rows
+//   scores      P = 2^(s - ref) in bf16, [b][h n + i][t], and (ref, sum) per row and block of 128 keys
+//   finish      the row's reference and 1 / l
+//   sum         U = P K / l on tcgen05, CTA pairs (cta_group::2), bf16
+//   join        adds the parts of tiles whose keys were cut
+//   out         o = U W_KV,h on tcgen05
+#include "slim_ptx.cuh"
+#include "slim_sched.cuh"
+#include "slim_tree.h"
+
+using namespace slim_ptx;
+
+namespace {
+
+__device__ __forceinline__ uint32_t tf32(float x) { uint32_t r; asm("cvt.rna.tf32.f32 %0, %1;" : "=r"(r) : "f"(x)); return r; }
+__device__ __forceinline__ void mma_tf32(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ float2 turn(const SlimDecodeParams& p, int pos, int j) {      // (cos, sin) of pos theta_j
+  const float2 cb = __ldg(p.rope_base + (size_t)(pos / SLIM_TT) * p.half + j), co = __ldg(p.rope_off + (pos % SLIM_TT) * p.half + j);
+  return make_float2(cb.x * co.x - cb.y * co.y, cb.y * co.x + cb.x * co.y);
+}
+
+// ------------------------------------------------------------------------------------------------ tail
+// Blocks (x, b): rows 8 x .. 8 x + 7 of sequence b's tail [128][d]: 0..63 the cached rows behind the last whole block of
+// 64, 64..127 the drafted keys; everything else is zero.  Runs after the layout kernel.
+__global__ void __launch_bounds__(256) slim_tree_tail_kernel(const SlimDecodeParams p, const SlimTreeView t) {
+  slim_pdl_trigger();
+  slim_pdl_wait();
+  const int b = blockIdx.y, vecs = p.d / 8;
+  const int len = t.len[b], base = len & ~63;
+  for (int rr = 0; rr < 8; ++rr) {
+    const int r = blockIdx.x * 8 + rr;
+    const uint4* src = nullptr;
+    if (r < 64) {
+      const int row = base + r;
+      if (row < len)
+        src = reinterpret_cast<const uint4*>(p.k) + (size_t)(slim_cache_row(p, b, row & ~(SLIM_TT - 1)) + (row & (SLIM_TT - 1))) * vecs;
+    } else if (r - 64 < t.n && t.depth[(size_t)b * t.n + r - 64] >= 0) {
+      src = reinterpret_cast<const uint4*>(t.k_tree) + ((size_t)b * t.n + r - 64) * vecs;
+    }
+    uint4* dst = reinterpret_cast<uint4*>(t.tail) + ((size_t)b * 128 + r) * vecs;
+    for (int e = threadIdx.x; e < vecs; e += 256) dst[e] = src ? __ldg(src + e) : make_uint4(0, 0, 0, 0);
+  }
+}
+
+// ------------------------------------------------------------------------------------------------ scores
+// A CTA takes one (sequence, head) and every gridDim.x-th block of 128 keys; warp w has keys 16 w .. 16 w + 15 of a
+// block, rows g and g + 8 of an m16n8k8 tf32 tile in each thread, and the tokens as the tile's columns.
+//   - The contraction runs over rotation pairs: step (pc, x) puts the low element of pair j into k-slot c and the
+//     high one into slot c + 4 (c = lane % 4), j = (c + 4 pc) VW + x.  So a thread holds both halves of its pairs, loads
+//     them as VW contiguous elements and rotates in registers; the keys never pass through shared memory.
+//   - R_pos(t) = R_(128 block) R_o: keys are turned by their offset o < 128 in the block only, whose (cos, sin) are
+//     the same for every block (a table in shared memory in the order the lanes read it); the queries, turned to their
+//     positions once, are turned back by the block's angle, 64 complex factors a block.
+//   - tf32 keeps 11 bits of the rotated values; bf16 operands (8 bits) would cost as much accuracy as the rounding of
+//     P does, for a product that is 1 / H of the step's.
+//   - P is written relative to a reference that is a multiple of 64 next to the block's maximum: nearly always 0 for all
+//     blocks of a row, so that the blocks need no common maximum; `finish` shifts the exponents of the others, exactly.
+//     Sums l are taken from the rounded P, so the weights of a row add up to one.
+// Bound by (n = 16, d_k = 128) the shared-memory reads of the table and the query fragments and the rotation's FMAs.
+constexpr int SC_KEYS = 128, SC_THREADS = 256, SC_WARPS = 8;
+
+template <int DK, int NT>
+struct ScoreShape {
+  static constexpr int HALF = DK / 2, VW = DK == 96 ? 4 : 8, NPC = HALF / (4 * VW), STEPS = HALF / 4, PER = STEPS / 2 * 32;
+  static constexpr int QLD = HALF + 2;                                   // float2 per token row of the turned queries
+  static constexpr size_t CS = (size_t)SC_KEYS * HALF * 8, QF = (size_t)NT * STEPS / 2 * 32 * 16, QS = (size_t)8 * NT * QLD * 8;
+  static constexpr int PLD = SC_KEYS + 8;                                // bf16 per token row of the P tile
+  static constexpr size_t PT = (size_t)8 * NT * PLD * 2;
+  static constexpr size_t SMEM = CS + QF + QS + PT + sizeof(float) * 8 * NT * (SC_WARPS + 2) + 16;
+};
+
+template <int VW> struct KVec;
+template <> struct KVec<8> { typedef uint4 type; };
+template <> struct KVec<4> { typedef uint2 type; };
+__device__ __forceinline__ float bf_lo(uint32_t w) { return __uint_as_float(w << 16); }
+__device__ __forceinline__ float bf_hi(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
+__device__ __forceinline__ float elem(const uint4& v, int x) {
+  const uint32_t w = x < 2 ? v.x : x < 4 ? v.y : x < 6 ? v.z : v.w;
+  return (x & 1) ? bf_hi(w) : bf_lo(w);
+}
+__device__ __forceinline__ float elem(const uint2& v, int x) { const uint32_t w = x < 2 ? v.x : v.y; return (x & 1) ? bf_hi(w) : bf_lo(w); }
+__device__ __forceinline__ int ordered(float f) { const int i = __float_as_int(f); return i ^ ((i >> 31) & 0x7fffffff); }
+__device__ __forceinline__ float unordered(int i) { return __int_as_float(i ^ ((i >> 31) & 0x7fffffff)); }
+
+template <int DK, int NT, bool ROPE>
+__global__ void __launch_bounds__(SC_THREADS)
+slim_tree_p_kernel(const SlimDecodeParams p, const SlimTreeView t) {
+  typedef ScoreShape<DK, NT> S;
+  constexpr int HALF = S::HALF, VW = S::VW, NPC = S::NPC, TOK = 8 * NT;
+  typedef typename KVec<VW>::type kvec;
+  extern __shared__ __align__(16) unsigned char sm[];
+  float4* cst = reinterpret_cast<float4*>(sm);                            // [warp][row half][pc][VW / 2][lane]
+  float4* qf = reinterpret_cast<float4*>(sm + S::CS);                     // [NT][STEPS / 2][lane]
+  float2* qs = reinterpret_cast<float2*>(sm + S::CS + S::QF);             // [TOK][QLD]
+  __nv_bfloat16* pt = reinterpret_cast<__nv_bfloat16*>(sm + S::CS + S::QF + S::QS);      // [TOK][PLD]
+  float* wsum = reinterpret_cast<float*>(sm + S::CS + S::QF + S::QS + S::PT);            // [warps][TOK]
+  int* smax = reinterpret_cast<int*>(wsum + SC_WARPS * TOK);              // [2][TOK]
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, c = lane & 3;
+  const int b = blockIdx.z, h = blockIdx.y, n = t.n, R = p.H * n;
+
+  if (ROPE) {                                                             // (reads only the context's tables)
+    for (int e = tid; e < SC_KEYS * HALF / 2; e += SC_THREADS) {
+      const int ln = e & 31, xq = (e >> 5) % (VW / 2), rest = (e >> 5) / (VW / 2), pc = rest % NPC, rh = rest / NPC % 2, w = rest / NPC / 2;
+      const int o = 16 * w + 8 * rh + (ln >> 2), j = ((ln & 3) + 4 * pc) * VW + 2 * xq;
+      const float2 a = turn(p, o, j), z = turn(p, o, j + 1);
+      cst[e] = make_float4(a.x, a.y, z.x, z.y);
+    }
+  }
+  slim_pdl_trigger();
+  slim_pdl_wait();
+  const int len = t.len[b], nblk = (len + SC_KEYS - 1) / SC_KEYS, nb_cap = (p.t_cap + SC_KEYS - 1) / SC_KEYS;
+  const int* dep = t.depth + (size_t)b * n;
+  const unsigned long long* mask = t.mask + (size_t)b * n;
+  const __nv_bfloat16* Kc = reinterpret_cast<const __nv_bfloat16*>(p.k);
+  const __nv_bfloat16* Kt = reinterpret_cast<const __nv_bfloat16*>(t.k_tree) + (size_t)b * n * p.d;
+  __nv_bfloat16* Pout = t.p + ((size_t)b * R + (size_t)h * n) * t.p_ld;
+  float2* stat = t.stat + (size_t)b * (nb_cap + 1) * R + h * n;
+
+  // queries of this (sequence, head), scaled and turned to their positions
+  {
+    const __nv_bfloat16* Q = reinterpret_cast<const __nv_bfloat16*>(p.q) + (size_t)b * n * p.d + h * DK;
+    for (int e = tid; e < TOK * HALF; e += SC_THREADS) {
+      const int i = e / HALF, j = e - i * HALF;
+      float2 v = make_float2(0.f, 0.f);
+      if (i < n && dep[i] >= 0) {
+        const float q1 = __bfloat162float(Q[(size_t)i * p.d + j]) * p.qscale, q2 = __bfloat162float(Q[(size_t)i * p.d + HALF + j]) * p.qscale;
+        if (ROPE) {
+          const float2 cs = turn(p, len + dep[i], j);
+          v = make_float2(q1 * cs.x + q2 * cs.y, q2 * cs.x - q1 * cs.y);
+        } else v = make_float2(q1, q2);
+      }
+      qs[i * S::QLD + j] = v;
+    }
+    for (int i = tid; i < 2 * TOK; i += SC_THREADS) smax[i] = ordered(-INFINITY);
+  }
+  unsigned live = 0;                                                      // bit 2 nt + z: token 8 nt + 2 c + z is there
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+    for (int z = 0; z < 2; ++z) {
+      const int i = 8 * nt + 2 * c + z;
+      if (i < n && dep[i] >= 0) live |= 1u << (2 * nt + z);
+    }
+
+  // this thread's part of the query fragments: pairs j0, j0 + 1 of token 8 nt + lane / 4, for nt = nt0, nt0 + nts, ..
+  constexpr int NTS = SC_THREADS / S::PER;
+  const int nt0 = tid / S::PER, fi = tid % S::PER, fs = 2 * (fi >> 5), j0 = ((fi & 3) + 4 * (fs / VW)) * VW + fs % VW;
+  const int ftok = (fi & 31) >> 2;
+
+  // the draft block comes last, in the CTAs of column 0
+  const int mine = nblk > (int)blockIdx.x ? (nblk - 1 - blockIdx.x) / gridDim.x + 1 : 0;
+  const int total = mine + (blockIdx.x == 0 ? 1 : 0);
+  kvec k[2][NPC][2];                                                      // [row half][pc][low / high element of the pairs]
+  float4 bc = make_float4(1.f, 0.f, 1.f, 0.f);                            // (cos, sin) of the block's angle, pairs j0, j0 + 1
+  auto fetch = [&](int it) {
+    const bool draft = it == mine;
+    const int blk = blockIdx.x + it * gridDim.x;
+    if (ROPE) {
+      if (draft) {
+        const float2 a = turn(p, len, j0), z = turn(p, len, j0 + 1);
+        bc = make_float4(a.x, a.y, z.x, z.y);
+      } else {
+        bc = __ldg(reinterpret_cast<const float4*>(p.rope_base + (size_t)blk * (SC_KEYS / SLIM_TT) * HALF + j0));
+      }
+    }
+    const int t0 = draft ? 16 * warp : blk * SC_KEYS + 16 * warp;
+    const __nv_bfloat16* base = Kt + (size_t)t0 * p.d;
+    if (!draft) base = t0 < len ? Kc + (size_t)slim_cache_row(p, b, t0) * p.d : Kc;
+#pragma unroll
+    for (int rh = 0; rh < 2; ++rh) {
+      const int r = g + 8 * rh;
+      const bool ok = draft ? (t0 + r < n && dep[t0 + r] >= 0) : t0 + r < len;
+      const __nv_bfloat16* row = base + (size_t)r * p.d + h * DK + c * VW;
+#pragma unroll
+      for (int pc = 0; pc < NPC; ++pc)
+#pragma unroll
+        for (int hi = 0; hi < 2; ++hi) {
+          kvec v = {};
+          if (ok) v = __ldg(reinterpret_cast<const kvec*>(row + hi * HALF + 4 * pc * VW));
+          k[rh][pc][hi] = v;
+        }
+    }
+  };
+  if (total > 0) fetch(0);
+  __syncthreads();
+
+  for (int it = 0; it < total; ++it) {
+    const bool draft = it == mine;
+    const int blk = blockIdx.x + it * gridDim.x, t0 = draft ? 16 * warp : blk * SC_KEYS + 16 * warp;
+    // ---- query fragments of this block
+    if (nt0 < NTS) {
+#pragma unroll
+      for (int nt = nt0; nt < NT; nt += NTS) {
+        const float4 q = *reinterpret_cast<const float4*>(qs + (size_t)(8 * nt + ftok) * S::QLD + j0);
+        float4 f;
+        f.x = __uint_as_float(tf32(q.x * bc.x - q.y * bc.y)); f.y = __uint_as_float(tf32(q.y * bc.x + q.x * bc.y));
+        f.z = __uint_as_float(tf32(q.z * bc.z - q.w * bc.w)); f.w = __uint_as_float(tf32(q.w * bc.z + q.z * bc.w));
+        qf[nt * S::PER + fi] = f;
+      }
+    }
+    __syncthreads();
+    if (tid < TOK) smax[((it + 1) & 1) * TOK + tid] = ordered(-INFINITY);  // (last read before the barrier above)
+    // ---- scores
+    float s[NT][4];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) s[nt][0] = s[nt][1] = s[nt][2] = s[nt][3] = 0.f;
+#pragma unroll
+    for (int pc = 0; pc < NPC; ++pc)
+#pragma unroll
+      for (int xq = 0; xq < VW / 2; ++xq) {
+        uint32_t a[2][4];
+#pragma unroll
+        for (int rh = 0; rh < 2; ++rh) {
+          float4 cs = make_float4(1.f, 0.f, 1.f, 0.f);
+          if (ROPE) {
+            if (!draft) cs = cst[(((warp * 2 + rh) * NPC + pc) * (VW / 2) + xq) * 32 + lane];
+            else {
+              const int r = t0 + g + 8 * rh, o = r < n ? max(dep[r], 0) : 0, j = (c + 4 * pc) * VW + 2 * xq;
+              const float2 u = turn(p, o, j), v = turn(p, o, j + 1);
+              cs = make_float4(u.x, u.y, v.x, v.y);
+            }
+          }
+#pragma unroll
+          for (int z = 0; z < 2; ++z) {
+            const float k1 = elem(k[rh][pc][0], 2 * xq + z), k2 = elem(k[rh][pc][1], 2 * xq + z);
+            const float co = z ? cs.z : cs.x, si = z ? cs.w : cs.y;
+            a[z][rh] = ROPE ? tf32(k1 * co + k2 * si) : __float_as_uint(k1);      // (a bf16 is a tf32)
+            a[z][2 + rh] = ROPE ? tf32(k2 * co - k1 * si) : __float_as_uint(k2);
+          }
+        }
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          const float4 f = qf[nt * S::PER + (pc * (VW / 2) + xq) * 32 + lane];
+          mma_tf32(s[nt], a[0], __float_as_uint(f.x), __float_as_uint(f.y));
+          mma_tf32(s[nt], a[1], __float_as_uint(f.z), __float_as_uint(f.w));
+        }
+      }
+    if (it + 1 < total) fetch(it + 1);
+    // ---- what is not attended
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        const int r = t0 + g + 8 * (x >> 1);
+        bool on = (live >> (2 * nt + (x & 1))) & 1;
+        if (draft) on = on && r < n && ((mask[min(8 * nt + 2 * c + (x & 1), n - 1)] >> (r & 63)) & 1);
+        else on = on && r < len;
+        if (!on) s[nt][x] = -INFINITY;
+      }
+    // ---- block maximum per token
+    int* mx = smax + (it & 1) * TOK;
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int z = 0; z < 2; ++z) {
+        float m = fmaxf(s[nt][z], s[nt][2 + z]);
+#pragma unroll
+        for (int o = 4; o < 32; o <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+        if (g == 0) atomicMax(mx + 8 * nt + 2 * c + z, ordered(m));
+      }
+    __syncthreads();
+    // ---- probabilities relative to the reference, and their sums over this warp's keys
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int z = 0; z < 2; ++z) {
+        const int i = 8 * nt + 2 * c + z;
+        const float m = unordered(mx[i]);
+        const float ref = 64.f * rintf(fminf(fmaxf(m, -1e30f), 1e30f) * (1.f / 64.f));
+        const __nv_bfloat16 p0 = __float2bfloat16(ex2_approx(s[nt][z] - ref)), p1 = __float2bfloat16(ex2_approx(s[nt][2 + z] - ref));
+        pt[i * S::PLD + 16 * warp + g] = p0;
+        pt[i * S::PLD + 16 * warp + g + 8] = p1;
+        float l = __bfloat162float(p0) + __bfloat162float(p1);
+#pragma unroll
+        for (int o = 4; o < 32; o <<= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
+        if (g == 0) wsum[warp * TOK + i] = l;
+      }
+    __syncthreads();
+    const int col = draft ? t.s_draft : blk * SC_KEYS, vecs = draft ? 8 : 16;
+    for (int e = tid; e < n * vecs; e += SC_THREADS) {
+      const int i = e / vecs, x = e - i * vecs;
+      *reinterpret_cast<uint4*>(Pout + (size_t)i * t.p_ld + col + 8 * x) = *reinterpret_cast<const uint4*>(pt + i * S::PLD + 8 * x);
+    }
+    if (tid < n) {
+      float l = 0.f;
+#pragma unroll
+      for (int w = 0; w < SC_WARPS; ++w) l += wsum[w * TOK + tid];
+      const float m = unordered(mx[tid]);
+      stat[(size_t)(draft ? nb_cap : blk) * R + tid] = make_float2(64.f * rintf(fminf(fmaxf(m, -1e30f), 1e30f) * (1.f / 64.f)), l);
+    }
+  }
+}
+
+// ------------------------------------------------------------------------------------------------ finish
+// 32 rows a block, 32 threads a row: M = the largest reference of the row's blocks that hold anything, 1 / l, and blocks of
+// P whose reference is another (rare: a row whose block maxima are more than about 32 apart around a multiple of 64)
+// multiplied by 2^(ref - M), a power of two: exact, down to values below 2^-94 of the row's largest, which become 0.
+__global__ void __launch_bounds__(1024) slim_tree_finish_kernel(const SlimDecodeParams p, const SlimTreeView t) {
+  __shared__ float s_m[32][33], s_l[32][33];
+  slim_pdl_trigger();
+  slim_pdl_wait();
+  const int R = p.H * t.n, x = threadIdx.x & 31, y = threadIdx.x >> 5, b = blockIdx.y, row = blockIdx.x * 32 + x;
+  const int nb_cap = (p.t_cap + SC_KEYS - 1) / SC_KEYS, nblk = (t.len[b] + SC_KEYS - 1) / SC_KEYS;
+  const float2* stat = t.stat + (size_t)b * (nb_cap + 1) * R + row;
+  float m = -INFINITY, l = 0.f;
+  if (row < R)
+    for (int k = y; k <= nblk; k += 32) {
+      const float2 v = stat[(size_t)(k == nblk ? nb_cap : k) * R];
+      if (v.y == 0.f) continue;
+      const float top = fmaxf(m, v.x);
+      l = l * exp2f(m - top) + v.y * exp2f(v.x - top);
+      m = top;
+    }
+  s_m[y][x] = m; s_l[y][x] = l;
+  __syncthreads();
+  float M = -INFINITY, L = 0.f;
+  for (int k = 0; k < 32; ++k) M = fmaxf(M, s_m[k][x]);
+  if (M != -INFINITY)
+    for (int k = 0; k < 32; ++k) L += s_l[k][x] == 0.f ? 0.f : s_l[k][x] * exp2f(s_m[k][x] - M);
+  if (row >= R) return;
+  if (y == 0) t.inv_l[(size_t)b * R + row] = L != 0.f ? 1.f / L : 0.f;
+  for (int k = y; k <= nblk; k += 32) {
+    const float2 v = stat[(size_t)(k == nblk ? nb_cap : k) * R];
+    if (v.y == 0.f || v.x == M) continue;
+    const float f = exp2f(v.x - M);
+    __nv_bfloat162* P = reinterpret_cast<__nv_bfloat162*>(t.p + ((size_t)b * R + row) * t.p_ld + (k == nblk ? t.s_draft : k * SC_KEYS));
+    for (int e = 0; e < (k == nblk ? 32 : SC_KEYS / 2); ++e) {
+      const float2 w = __bfloat1622float2(P[e]);
+      P[e] = __floats2bfloat162_rn(w.x * f, w.y * f);
+    }
+  }
+}
+
+// ------------------------------------------------------------------------------------------------ schedule of the product
+// A tile is MT x 256 rows of P by 256 columns of K; its keys are walked in stages of 64 rows (the cached whole blocks,
+// the partial one, the drafted keys).  Every tile of every sequence may be cut into S equal parts of its stages
+// (subtiles; S > 1 where there are fewer tiles than CTA pairs).  The subtiles, in the order (sequence, part, tile), go
+// to the pairs in turn, F of them as a whole, so that pairs in flight walk the same keys and the same rows of P at the
+// same time and share them in L2; what is left over, about a wave, is laid on a line and cut so that every pair ends
+// up with the same number of stages.  A piece that is not a whole tile leaves float32 sums in a slot, and `join` adds
+// the slots of a tile in the order of its keys: the schedule is a function of the lengths alone, so results are repeatable.
+struct SumSched {
+  int batch, tiles, S, P, F, TS;      // tiles of a sequence, parts, pairs, whole subtiles, subtiles in all
+  const int* nk;                      // shared [batch]      stages of a sequence
+  const long long* pre;               // shared [batch + 1]  tiles x stages before it
+  const long long* cut;               // shared [P + 1]      the left-over line's cuts
+  long long g0;                       // line position of subtile F
+};
+struct SumItem { int b, tile, k0, k1, slot; };       // slot -1: a whole tile
+
+__host__ __device__ inline int stages_of(int len) { return len / 64 + (len % 64 ? 1 : 0) + 1; }
+
+__device__ __forceinline__ void subtile(const SumSched& s, int idx, int& b, int& tile, int& k0, int& k1) {
+  const int per = s.S * s.tiles;
+  b = idx / per;
+  const int in = idx - b * per, part = in / s.tiles;
+  tile = in - part * s.tiles;
+  const long long nk = s.nk[b];
+  k0 = (int)(nk * part / s.S); k1 = (int)(nk * (part + 1) / s.S);
+}
+__device__ __forceinline__ long long line_pos(const SumSched& s, int idx) {       // stages before subtile idx
+  if (idx >= s.TS) return s.pre[s.batch];
+  int b, tile, k0, k1;
+  subtile(s, idx, b, tile, k0, k1);
+  return s.pre[b] + (long long)s.tiles * k0 + (long long)tile * (k1 - k0);
+}
+// the subtile that holds line position x < pre[batch]
+__device__ __forceinline__ int at_pos(const SumSched& s, long long x) {
+  int lo = 0, hi = s.batch;
+  while (hi - lo > 1) { const int mid = (lo + hi) >> 1; if (s.pre[mid] <= x) lo = mid; else hi = mid; }
+  const long long in = x - s.pre[lo], nk = s.nk[lo];
+  const int k = (int)(in / s.tiles);                                    // in lies in the part whose [k0, k1) holds k
+  int part = (int)(((long long)(k + 1) * s.S - 1) / nk);
+  while ((int)(nk * (part + 1) / s.S) <= k) ++part;
+  while ((int)(nk * part / s.S) > k) --part;
+  const long long k0 = nk * part / s.S, k1 = nk * (part + 1) / s.S;
+  return lo * s.S * s.tiles + part * s.tiles + (int)((in - (long long)s.tiles * k0) / (k1 - k0));
+}
+
+// By all threads of a block; s_pre, s_cut, s_nk in shared memory.
+__device__ __forceinline__ SumSched build_sum_sched(const SlimTreeView& t, int batch, int* s_nk, long long* s_pre, long long* s_cut) {
+  SumSched s;
+  s.batch = batch; s.tiles = t.g_tiles; s.S = t.g_split; s.P = t.g_pairs; s.F = t.g_whole; s.TS = batch * t.g_tiles * t.g_split;
+  s.nk = s_nk; s.pre = s_pre; s.cut = s_cut;
+  const int tid = threadIdx.x, nthr = blockDim.x;
+  for (int b = tid; b < batch; b += nthr) s_nk[b] = stages_of(t.len[b]);
+  __syncthreads();
+  if (tid < 32) {
+    const int chunk = (batch + 31) / 32, lo = min(batch, tid * chunk), hi = min(batch, lo + chunk);
+    long long sum = 0;
+    for (int b = lo; b < hi; ++b) sum += s_nk[b];
+    long long incl = sum;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) { const long long v = __shfl_up_sync(0xffffffffu, incl, o); if (tid >= o) incl += v; }
+    long long run = incl - sum;
+    for (int b = lo; b < hi; ++b) { s_pre[b] = run * s.tiles; run += s_nk[b]; }
+    if (tid == 31) s_pre[batch] = incl * s.tiles;
+  }
+  __syncthreads();
+  s.g0 = line_pos(s, s.F);
+  const long long all = s_pre[batch], want = (all + s.P - 1) / s.P;
+  for (int q = tid; q < s.P; q += nthr) {                               // what pair q has left to take
+    long long load = 0;
+    for (int idx = q; idx < s.F; idx += s.P) {
+      int b, tile, k0, k1;
+      subtile(s, idx, b, tile, k0, k1);
+      load += k1 - k0;
+    }
+    s_cut[q + 1] = load < want ? want - load : 0;
+  }
+  __syncthreads();
+  if (tid == 0) {
+    const long long rest = all - s.g0;
+    long long sum = 0;
+    for (int q = 0; q < s.P; ++q) sum += s_cut[q + 1];
+    const double scale = sum > 0 ? (double)rest / (double)sum : 0.0;
+    long long run = 0;
+    s_cut[0] = 0;
+    for (int q = 0; q < s.P; ++q) {
+      run += s_cut[q + 1];
+      s_cut[q + 1] = (long long)((double)run * scale);
+      if (s_cut[q + 1] > rest || q == s.P - 1) s_cut[q + 1] = rest;
+    }
+  }
+  __syncthreads();
+  return s;
+}
+
+// The pieces of pair q, one after another.
+struct SumWalk {
+  int idx;
+  long long at;
+};
+__device__ __forceinline__ SumWalk sum_begin(const SumSched& s, int q) { SumWalk w; w.idx = q; w.at = s.cut[q]; return w; }
+__device__ __forceinline__ bool sum_next(const SumSched& s, int q, SumWalk& w, SumItem& it) {
+  while (w.idx < s.F) {
+    const int idx = w.idx;
+    w.idx += s.P;
+    subtile(s, idx, it.b, it.tile, it.k0, it.k1);
+    if (it.k0 == it.k1) continue;
+    it.slot = s.S == 1 ? -1 : 2 * s.P + idx;
+    return true;
+  }
+  const long long end = s.cut[q + 1];
+  if (w.at >= end) return false;
+  const long long x = w.at + s.g0;
+  const int idx = at_pos(s, x);
+  const long long x0 = line_pos(s, idx);
+  int k0, k1;
+  subtile(s, idx, it.b, it.tile, k0, k1);
+  const long long x1 = x0 + (k1 - k0), stop = min(x1, end + s.g0);
+  it.k0 = k0 + (int)(x - x0); it.k1 = k0 + (int)(stop - x0);
+  w.at = stop - s.g0;
+  it.slot = (x == x0 && stop == x1) ? (s.S == 1 ? -1 : 2 * s.P + idx) : x > x0 ? 2 * q : 2 * q + 1;
+  return true;
+}
+
+// ------------------------------------------------------------------------------------------------ U = P K
+// Persistent, one CTA per SM in pairs.  A stage of 64 keys holds, per CTA, MT x 128 rows of P (K-major, 128-byte
+// swizzle) and HALF of the tile's 256 columns of K (MN-major, as the cache rows come: two 64-column atoms); one
+// tcgen05.mma.cta_group::2 has M = 256, N = 256, K = 16.  MT = 2 (more than 256 rows a sequence) runs two accumulators on
+// one load of K: 48 KB of operands per 2 x 256 x 256 x 64 products instead of 64 KB, and half the trips of K through HBM;
+// MT = 1 double-buffers the accumulator instead, so that a tile's epilogue runs under the next tile's products.
+// Warp 0: TMA; warp 1 (even CTA): MMA issue; warps 2-5: epilogue.  A paged cache comes in pieces of 16 rows (a page
+// holds whole ones), a contiguous one 64 rows at a time.
+constexpr int SU_THREADS = 192, SU_ROWS = 128, SU_COLS = 256, SU_A = SU_ROWS * 128, SU_B = 64 * 256;
+template <int MT> struct SumShape {
+  static constexpr int STAGE = MT * SU_A + SU_B, NS = MT == 1 ? 6 : 4;
+  static size_t smem(int batch, int pairs) {
+    return 1024 + (size_t)NS * STAGE + 16 * NS + 32 + 64 + sizeof(long long) * (batch + 1 + pairs + 1) + sizeof(int) * batch + 16;
+  }
+};
+
+template <int MT>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(SU_THREADS, 1)
+slim_tree_u_kernel(const __grid_constant__ CUtensorMap pmap, const __grid_constant__ CUtensorMap kmap,
+                   const __grid_constant__ CUtensorMap tailmap, const SlimDecodeParams p, const SlimTreeView t) {
+  constexpr int NS = SumShape<MT>::NS;
+  constexpr uint32_t STAGE = SumShape<MT>::STAGE;
+  extern __shared__ unsigned char smem_raw[];
+  const uint32_t raw_u32 = smem_u32(smem_raw);
+  const uint32_t base = (raw_u32 + 1023u) & ~1023u;
+  unsigned char* sm = smem_raw + (base - raw_u32);
+  const uint32_t bars = base + NS * STAGE;
+  const uint32_t bar_full = bars, bar_empty = bars + 8 * NS, bar_accf = bars + 16 * NS, bar_acce = bar_accf + 16;
+  unsigned char* misc = sm + NS * STAGE + 16 * NS + 32;
+  uint32_t* s_tmem = reinterpret_cast<uint32_t*>(misc);
+  volatile int* s_abort = reinterpret_cast<volatile int*>(misc + 4);
+  long long* s_pre = reinterpret_cast<long long*>(misc + 64);
+  long long* s_cut = s_pre + p.batch + 1;
+  int* s_nk = reinterpret_cast<int*>(s_cut + t.g_pairs + 1);
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const uint32_t rank = cluster_ctarank();
+  const int pair = blockIdx.x >> 1;
+  int* status = p.status;
+
+  if (tid == 0) {
+    prefetch_tensormap(&pmap); prefetch_tensormap(&kmap); prefetch_tensormap(&tailmap);
+    for (int i = 0; i < NS; ++i) { mbar_init(bar_full + 8 * i, 1); mbar_init(bar_empty + 8 * i, 1); }
+    for (int i = 0; i < 2; ++i) { mbar_init(bar_accf + 8 * i, 1); mbar_init(bar_acce + 8 * i, 8); }
+    *s_abort = 0;
+    fence_mbar_init();
+  }
+  if (warp == 1) tmem_alloc2(smem_u32(s_tmem), 512);
+  tc_fence_before();
+  __syncthreads();
+  cluster_sync_all();
+  tc_fence_after();
+  const uint32_t tmem_base = *s_tmem;
+  slim_pdl_trigger();
+  slim_pdl_wait();
+  const SumSched sc = build_sum_sched(t, p.batch, s_nk, s_pre, s_cut);
+  const bool paged = p.block_table != nullptr;
+  const int ntile = t.g_ncol;                              // column tiles; tile = row tile * ntile + column tile
+
+  if (warp == 0) {
+    // ---- producer ----
+    fence_proxy_async_global();                            // (P and the tail were written by ordinary stores)
+    int g = 0;
+    bool ok = true;
+    SumWalk w = sum_begin(sc, pair);
+    SumItem it;
+    while (ok && sum_next(sc, pair, w, it)) {
+      const int len = t.len[it.b], whole = len / 64, nk = sc.nk[it.b];
+      const int mt0 = it.tile / ntile, chunk = (it.tile % ntile) * 4 + 2 * (int)rank, row0 = mt0 * MT * 256 + (int)rank * SU_ROWS;
+      int my_row = 0, have = -1;                           // lane x: storage row of the 16-key piece have + x
+      for (int k = it.k0; k < it.k1; ++k, ++g) {
+        if (paged && k < whole && (have < 0 || 4 * k >= have + 32)) {
+          have = 4 * k;
+          const int piece = have + lane;
+          my_row = piece < 4 * whole ? (int)slim_cache_row(p, it.b, piece * 16) : 0;
+        }
+        int r4[4];
+        if (paged && k < whole)
+#pragma unroll
+          for (int x = 0; x < 4; ++x) r4[x] = __shfl_sync(0xffffffffu, my_row, 4 * k - have + x);
+        if (lane == 0) {
+          const int st = g % NS;
+          ok = mbar_wait<false>(bar_empty + 8 * st, ((g / NS) & 1) ^ 1, s_abort, status);
+          if (ok) {
+            const uint32_t dst = base + (uint32_t)st * STAGE, full0 = mapa(bar_full + 8 * st, 0);
+            if (rank == 0) mbar_arrive_expect_tx(bar_full + 8 * st, 2 * STAGE);
+            const int pcol = k < whole ? k * 64 : k == nk - 1 ? t.s_draft : whole * 64;
+#pragma unroll
+            for (int m = 0; m < MT; ++m) tma_load_3d_pair(dst + m * SU_A, &pmap, full0, pcol, row0 + m * 256, it.b);
+            const CUtensorMap* map = k < whole ? &kmap : &tailmap;
+            const int krow = it.b * (k < whole ? p.t_cap : 128) + (k < whole ? k * 64 : k == nk - 1 ? 64 : 0);
+            if (!paged) tma_load_3d_pair(dst + MT * SU_A, map, full0, 0, krow, chunk);
+            else
+#pragma unroll
+              for (int x = 0; x < 4; ++x)
+                tma_load_3d_pair(dst + MT * SU_A + x * 4096, map, full0, 0, k < whole ? r4[x] : krow + 16 * x, chunk);
+          }
+        }
+        ok = __shfl_sync(0xffffffffu, ok ? 1 : 0, 0) != 0;
+        if (!ok) break;
+      }
+    }
+    if (!ok && lane == 0) {
+      // gave up: what was issued has long landed; the even CTA still waits, bounded, on the barriers that count both
+      // CTAs' bytes, the odd CTA lets a fixed time pass
+      if (rank == 0) {
+        const int issued = g < NS ? g : NS;
+        for (int k = 0; k < issued; ++k) {
+          const int j = g - 1 - k, st = j % NS;
+          const unsigned long long tt = globaltimer();
+          while (!mbar_try_wait(bar_full + 8 * st, (j / NS) & 1) && globaltimer() - tt < SLIM_WAIT_NS) {}
+        }
+      } else {
+        const unsigned long long tt = globaltimer();
+        while (globaltimer() - tt < 200000ull) {}
+      }
+    }
+  } else if (warp == 1) {
+    if (lane == 0 && rank == 0) {
+      // ---- MMA issuer of the pair ----
+      bool ok = true;
+      int g = 0, i = 0;
+      const uint64_t ad0 = desc_kmajor_sw128(base), bd0 = desc_a(base + MT * SU_A, paged ? 2048 : 8192);
+      const uint32_t a_lo0 = (uint32_t)ad0, a_hi = (uint32_t)(ad0 >> 32), b_lo0 = (uint32_t)bd0, b_hi = (uint32_t)(bd0 >> 32);
+      const uint32_t bstep = (paged ? 4096u : 2048u) >> 4;
+      constexpr uint32_t idesc = umma_idesc_mn(256, SU_COLS, 0, 1);
+      SumWalk w = sum_begin(sc, pair);
+      SumItem it;
+      for (; ok && sum_next(sc, pair, w, it); ++i) {
+        const int acc0 = MT == 1 ? (i & 1) : 0;
+        const uint32_t ph = MT == 1 ? (i >> 1) & 1 : i & 1;
+        for (int k = it.k0; k < it.k1; ++k, ++g) {
+          const int st = g % NS;
+          ok = mbar_wait<true>(bar_full + 8 * st, (g / NS) & 1, s_abort, status);
+          if (!ok) break;
+          tc_fence_after();
+          const uint32_t b_lo = b_lo0 + (uint32_t)st * (STAGE >> 4);
+#pragma unroll
+          for (int m = 0; m < MT; ++m) {
+            const int acc = acc0 + m;
+            if (k == it.k0) {                              // both CTAs have read the accumulator out
+              ok = mbar_wait<true>(bar_acce + 8 * acc, ph ^ 1, s_abort, status);
+              if (!ok) break;
+              tc_fence_after();
+            }
+            const uint32_t a_lo = a_lo0 + (uint32_t)st * (STAGE >> 4) + (uint32_t)m * (SU_A >> 4);
+#pragma unroll
+            for (int kk = 0; kk < 4; ++kk)
+              umma2_bf16_words(tmem_base + (uint32_t)(acc * SU_COLS), a_lo + (uint32_t)kk * (32u >> 4), a_hi, b_lo + (uint32_t)kk * bstep, b_hi,
+                               idesc, (k > it.k0 || kk) ? 1u : 0u);
+          }
+          if (!ok) break;
+          umma2_commit_pair(bar_empty + 8 * st);
+        }
+        if (ok)
+#pragma unroll
+          for (int m = 0; m < MT; ++m) umma2_commit_pair(bar_accf + 8 * (acc0 + m));
+      }
+    }
+  } else {
+    // ---- epilogue ----
+    const int q = warp & 3, R = p.H * t.n;
+    bool ok = true;
+    int i = 0;
+    SumWalk w = sum_begin(sc, pair);
+    SumItem it;
+    for (; ok && sum_next(sc, pair, w, it); ++i) {
+      const int mt0 = it.tile / ntile, col0 = (it.tile % ntile) * SU_COLS;
+#pragma unroll
+      for (int m = 0; m < MT; ++m) {
+        const int acc = MT == 1 ? (i & 1) : m;
+        const uint32_t ph = MT == 1 ? (i >> 1) & 1 : i & 1;
+        ok = mbar_wait<false>(bar_accf + 8 * acc, ph, s_abort, status);
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) break;
+        tc_fence_after();
+        const int in = m * 256 + (int)rank * SU_ROWS + q * 32 + lane, r = mt0 * MT * 256 + in;
+        const uint32_t ta = tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)(acc * SU_COLS);
+        if (it.slot < 0) {
+          const float il = r < R ? t.inv_l[(size_t)it.b * R + r] : 0.f;
+          const int h = r / t.n, tok = r - h * t.n;
+          __nv_bfloat16* out = t.uh + (((size_t)h * p.batch + it.b) * t.n + tok) * p.d + col0;
+          for (int c0 = 0; c0 < SU_COLS; c0 += 32) {
+            uint32_t v[32];
+            tmem_ld32(ta + (uint32_t)c0, v);
+            if (r < R && col0 + c0 < p.d) {
+#pragma unroll
+              for (int x = 0; x < 32; x += 8) {
+                uint4 o4;
+                uint32_t* ow = reinterpret_cast<uint32_t*>(&o4);
+#pragma unroll
+                for (int y = 0; y < 4; ++y) {
+                  const __nv_bfloat162 z = __floats2bfloat162_rn(__uint_as_float(v[x + 2 * y]) * il, __uint_as_float(v[x + 2 * y + 1]) * il);
+                  ow[y] = *reinterpret_cast<const uint32_t*>(&z);
+                }
+                *reinterpret_cast<uint4*>(out + c0 + x) = o4;
+              }
+            }
+          }
+        } else {
+          float* out = t.part + ((size_t)it.slot * MT * 256 + in) * SU_COLS;
+          for (int c0 = 0; c0 < SU_COLS; c0 += 32) {
+            uint32_t v[32];
+            tmem_ld32(ta + (uint32_t)c0, v);
+            if (r < R && col0 + c0 < p.d) {
+#pragma unroll
+              for (int x = 0; x < 32; x += 4)
+                *reinterpret_cast<uint4*>(out + c0 + x) = make_uint4(v[x], v[x + 1], v[x + 2], v[x + 3]);
+            }
+          }
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive_cluster(mapa(bar_acce + 8 * acc, 0));
+      }
+    }
+  }
+  __syncwarp();
+  tc_fence_before();
+  __syncthreads();
+  cluster_sync_all();
+  if (warp == 1) {
+    tc_fence_after();
+    tmem_dealloc2(tmem_base, 512);
+  }
+}
+
+// ------------------------------------------------------------------------------------------------ join
+// Block (tile of the batch, 16 rows of it): sums of the tile's slots in the order of its keys, times 1 / l, as bf16.
+__global__ void __launch_bounds__(256) slim_tree_join_kernel(const SlimDecodeParams p, const SlimTreeView t, int mt) {
+  extern __shared__ __align__(16) unsigned char smem_raw[];
+  long long* s_pre = reinterpret_cast<long long*>(smem_raw);
+  long long* s_cut = s_pre + p.batch + 1;
+  int* s_nk = reinterpret_cast<int*>(s_cut + t.g_pairs + 1);
+  int* s_slot = s_nk + p.batch;                            // [S + P]
+  __shared__ int s_n;
+  const int tid = threadIdx.x, R = p.H * t.n;
+  slim_pdl_trigger();
+  slim_pdl_wait();
+  const SumSched s = build_sum_sched(t, p.batch, s_nk, s_pre, s_cut);
+  const int at = blockIdx.x + (s.S == 1 ? s.F : 0), b = at / s.tiles, tile = at % s.tiles;
+  const int row0 = (tile / t.g_ncol) * mt * 256 + blockIdx.y * 16, col0 = (tile % t.g_ncol) * SU_COLS;
+  if (row0 >= R) return;
+  if (tid == 0) {
+    int cnt = 0;
+    for (int part = 0; part < s.S; ++part) {
+      const int idx = (b * s.S + part) * s.tiles + tile;
+      int bb, tt, k0, k1;
+      subtile(s, idx, bb, tt, k0, k1);
+      if (k0 == k1) continue;
+      if (idx < s.F) {
+        if (s.S > 1) s_slot[cnt++] = 2 * s.P + idx;
+        continue;
+      }
+      const long long x0 = line_pos(s, idx) - s.g0, x1 = x0 + (k1 - k0);
+      int lo = 0, hi = s.P;                                // the pair whose segment holds x0: the last one with cut <= x0 < next cut
+      while (hi - lo > 1) { const int mid = (lo + hi) >> 1; if (s_cut[mid] <= x0) lo = mid; else hi = mid; }
+      for (int q = lo; q < s.P && s_cut[q] < x1; ++q) {
+        const long long a = max(s_cut[q], x0), z = min(s_cut[q + 1], x1);
+        if (a >= z) continue;
+        if (a == x0 && z == x1) { if (s.S > 1) s_slot[cnt++] = 2 * s.P + idx; }
+        else s_slot[cnt++] = a > x0 ? 2 * q : 2 * q + 1;
+      }
+    }
+    s_n = cnt;
+  }
+  __syncthreads();
+  const int cnt = s_n;
+  if (cnt == 0) return;                                    // written as a whole by one pair
+  for (int e = tid; e < 16 * (SU_COLS / 4); e += 256) {
+    const int rr = e / (SU_COLS / 4), c = (e % (SU_COLS / 4)) * 4, r = row0 + rr;
+    if (r >= R || col0 + c >= p.d) continue;
+    const size_t off = ((size_t)(blockIdx.y * 16 + rr)) * SU_COLS + c;
+    float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int k = 0; k < cnt; ++k) {
+      const float4 v = *reinterpret_cast<const float4*>(t.part + (size_t)s_slot[k] * mt * 256 * SU_COLS + off);
+      a.x += v.x; a.y += v.y; a.z += v.z; a.w += v.w;
+    }
+    const float il = t.inv_l[(size_t)b * R + r];
+    const int h = r / t.n, tok = r - h * t.n;
+    const __nv_bfloat162 o0 = __floats2bfloat162_rn(a.x * il, a.y * il), o1 = __floats2bfloat162_rn(a.z * il, a.w * il);
+    *reinterpret_cast<uint2*>(t.uh + (((size_t)h * p.batch + b) * t.n + tok) * p.d + col0 + c) =
+        make_uint2(*reinterpret_cast<const uint32_t*>(&o0), *reinterpret_cast<const uint32_t*>(&o1));
+  }
+}
+
+// ------------------------------------------------------------------------------------------------ o = U W_KV,h
+// CTA = (part of the d rows of W_KV,h, head, 128 (sequence, token) rows); the parts form a cluster and add their
+// accumulators through distributed shared memory, in order, each the rows it writes.
+constexpr int OU_NS = 5, OU_A = 128 * 128, OU_B = 64 * 256;
+constexpr uint32_t OU_STAGE = OU_A + OU_B;
+constexpr int OU_LD = 132;                                 // floats per accumulator row in shared memory
+constexpr size_t OU_SMEM = 1024 + (size_t)OU_NS * OU_STAGE + 16 * OU_NS + 8 + 32;
+static_assert(128 * OU_LD * 4 <= OU_NS * (int)OU_STAGE, "the accumulator is staged where the operands were");
+
+__device__ __forceinline__ float4 ld_cluster_f32x4(uint32_t a) {
+  float4 v;
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(a) : "memory");
+  return v;
+}
+
+__global__ void __launch_bounds__(128) slim_tree_out_kernel(const __grid_constant__ CUtensorMap umap, const __grid_constant__ CUtensorMap wmap,
+                                                            __nv_bfloat16* __restrict__ o, int rows, int d, int d_k, int parts, int* status) {
+  extern __shared__ unsigned char smem_raw[];
+  const uint32_t raw_u32 = smem_u32(smem_raw), base = (raw_u32 + 1023u) & ~1023u;
+  unsigned char* sm = smem_raw + (base - raw_u32);
+  const uint32_t bar_full = base + OU_NS * OU_STAGE, bar_empty = bar_full + 8 * OU_NS, bar_done = bar_empty + 8 * OU_NS;
+  unsigned char* misc = sm + OU_NS * OU_STAGE + 16 * OU_NS + 8;
+  uint32_t* s_tmem = reinterpret_cast<uint32_t*>(misc);
+  volatile int* s_abort = reinterpret_cast<volatile int*>(misc + 4);
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int part = blockIdx.x, h = blockIdx.y, m0 = blockIdx.z * 128;
+  const int ns = d / 64, s0 = ns * part / parts, s1 = ns * (part + 1) / parts;
+  const uint32_t bytes = OU_A + (d_k == 64 ? OU_B / 2 : OU_B);
+  if (tid == 0) {
+    prefetch_tensormap(&umap); prefetch_tensormap(&wmap);
+    for (int i = 0; i < OU_NS; ++i) { mbar_init(bar_full + 8 * i, 1); mbar_init(bar_empty + 8 * i, 1); }
+    mbar_init(bar_done, 1);
+    *s_abort = 0;
+    fence_mbar_init();
+  }
+  if (warp == 1) tmem_alloc(smem_u32(s_tmem), 128);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem_base = *s_tmem;
+  slim_pdl_trigger();
+  slim_pdl_wait();
+  if (warp == 0 && lane == 0) {
+    fence_proxy_async_global();
+    int s = s0;
+    bool ok = true;
+    for (; s < s1; ++s) {
+      const int j = s - s0, st = j % OU_NS;
+      ok = mbar_wait<false>(bar_empty + 8 * st, ((j / OU_NS) & 1) ^ 1, s_abort, status);
+      if (!ok) break;
+      const uint32_t dst = base + (uint32_t)st * OU_STAGE;
+      mbar_arrive_expect_tx(bar_full + 8 * st, bytes);
+      tma_load_3d(dst, &umap, bar_full + 8 * st, s * 64, m0, h);
+      tma_load_3d(dst + OU_A, &wmap, bar_full + 8 * st, 0, h * d + s * 64, 0);
+    }
+    if (!ok) {
+      const int did = s - s0, issued = did < OU_NS ? did : OU_NS;
+      for (int k = 0; k < issued; ++k) {
+        const int j = did - 1 - k, st = j % OU_NS;
+        const unsigned long long tt = globaltimer();
+        while (!mbar_try_wait(bar_full + 8 * st, (j / OU_NS) & 1) && globaltimer() - tt < SLIM_WAIT_NS) {}
+      }
+    }
+  } else if (warp == 1 && lane == 0) {
+    bool ok = true;
+    const uint64_t ad0 = desc_kmajor_sw128(base), bd0 = desc_a(base + OU_A, 8192);
+    const uint32_t a_lo0 = (uint32_t)ad0, a_hi = (uint32_t)(ad0 >> 32), b_lo0 = (uint32_t)bd0, b_hi = (uint32_t)(bd0 >> 32);
+    const uint32_t idesc = umma_idesc_major((uint32_t)d_k, 0, 1);
+    for (int j = 0; j < s1 - s0; ++j) {
+      const int st = j % OU_NS;
+      ok = mbar_wait<false>(bar_full + 8 * st, (j / OU_NS) & 1, s_abort, status);
+      if (!ok) break;
+      tc_fence_after();
+      const uint32_t a_lo = a_lo0 + (uint32_t)st * (OU_STAGE >> 4), b_lo = b_lo0 + (uint32_t)st * (OU_STAGE >> 4);
+#pragma unroll
+      for (int kk = 0; kk < 4; ++kk)
+        umma_bf16_words(tmem_base, a_lo + (uint32_t)kk * (32u >> 4), a_hi, b_lo + (uint32_t)kk * (2048u >> 4), b_hi, idesc, (j | kk) ? 1u : 0u);
+      umma_commit(bar_empty + 8 * st);
+    }
+    if (ok) umma_commit(bar_done);
+  }
+  __syncwarp();
+  bool ok = mbar_wait<false>(bar_done, 0, s_abort, status);
+  ok = __all_sync(0xffffffffu, ok);
+  float* acc = reinterpret_cast<float*>(sm);
+  if (ok) {
+    tc_fence_after();
+    const int r = warp * 32 + lane;
+    for (int c0 = 0; c0 < d_k; c0 += 32) {
+      uint32_t v[32];
+      tmem_ld32(tmem_base + ((uint32_t)(warp * 32) << 16) + (uint32_t)c0, v);
+#pragma unroll
+      for (int x = 0; x < 32; x += 4) *reinterpret_cast<uint4*>(acc + r * OU_LD + c0 + x) = make_uint4(v[x], v[x + 1], v[x + 2], v[x + 3]);
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (parts > 1) cluster_sync_all();
+  if (ok) {
+    const int per = 128 / parts, vecs = d_k / 8;
+    for (int e = tid; e < per * vecs; e += 128) {
+      const int r = part * per + e / vecs, c = (e % vecs) * 8;
+      if (m0 + r >= rows) continue;
+      float4 x = make_float4(0.f, 0.f, 0.f, 0.f), y = x;
+      for (int k = 0; k < parts; ++k) {
+        const uint32_t a = mapa(base + (uint32_t)(r * OU_LD + c) * 4u, k);
+        const float4 u = ld_cluster_f32x4(a), v = ld_cluster_f32x4(a + 16);
+        x.x += u.x; x.y += u.y; x.z += u.z; x.w += u.w;
+        y.x += v.x; y.y += v.y; y.z += v.z; y.w += v.w;
+      }
+      const __nv_bfloat162 o0 = __floats2bfloat162_rn(x.x, x.y), o1 = __floats2bfloat162_rn(x.z, x.w), o2 = __floats2bfloat162_rn(y.x, y.y),
+                           o3 = __floats2bfloat162_rn(y.z, y.w);
+      *reinterpret_cast<uint4*>(o + (size_t)(m0 + r) * d + h * d_k + c) =
+          make_uint4(*reinterpret_cast<const uint32_t*>(&o0), *reinterpret_cast<const uint32_t*>(&o1), *reinterpret_cast<const uint32_t*>(&o2),
+                     *reinterpret_cast<const uint32_t*>(&o3));
+    }
+  }
+  if (parts > 1) cluster_sync_all();                       // a CTA's shared memory is read by the others until here
+  if (warp == 1) {
+    tc_fence_after();
+    tmem_dealloc(tmem_base, 128);
+  }
+}
+
+template <int DK, int NT, bool ROPE>
+cudaError_t launch_p(const slim_ctx* ctx, const SlimDecodeParams& p, const SlimTreeView& t, cudaStream_t st) {
+  constexpr size_t smem = ScoreShape<DK, NT>::SMEM;
+  auto kern = slim_tree_p_kernel<DK, NT, ROPE>;
+  cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  if (e != cudaSuccess) return e;
+  const int nblk = (p.t_cap + SC_KEYS - 1) / SC_KEYS, rows = p.H * p.batch;
+  int gx = (8 * ctx->num_sms + rows - 1) / rows;           // about eight CTAs an SM over the launch: each builds its tables once
+  if (gx > nblk) gx = nblk;
+  return slim_launch_pdl(kern, dim3(gx, p.H, p.batch), dim3(SC_THREADS), smem, st, p, t);
+}
+template <int DK, int NT>
+cudaError_t launch_p_rope(const slim_ctx* ctx, const SlimDecodeParams& p, const SlimTreeView& t, cudaStream_t st) {
+  return p.rope ? launch_p<DK, NT, true>(ctx, p, t, st) : launch_p<DK, NT, false>(ctx, p, t, st);
+}
+template <int DK>
+cudaError_t launch_p_tokens(const slim_ctx* ctx, const SlimDecodeParams& p, const SlimTreeView& t, cudaStream_t st) {
+  if (t.n <= 8) return launch_p_rope<DK, 1>(ctx, p, t, st);
+  if (t.n <= 16) return launch_p_rope<DK, 2>(ctx, p, t, st);
+  if (t.n <= 32) return launch_p_rope<DK, 4>(ctx, p, t, st);
+  return launch_p_rope<DK, 8>(ctx, p, t, st);
+}
+
+template <int MT>
+cudaError_t launch_u(const slim_ctx* ctx, const SlimDecodeParams& p, const SlimTreeView& t, const CUtensorMap& pmap, const CUtensorMap& kmap,
+                     const CUtensorMap& tailmap, cudaStream_t st) {
+  auto kern = slim_tree_u_kernel<MT>;
+  const size_t smem = SumShape<MT>::smem(p.batch, t.g_pairs);
+  cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  if (e != cudaSuccess) return e;
+  return slim_launch_pdl(kern, dim3(2 * t.g_pairs), dim3(SU_THREADS), smem, st, pmap, kmap, tailmap, p, t);
+}
+
+inline size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
+
+}  // namespace
+
+int slim_tree_tc_ok(const slim_ctx* ctx) {
+  return ctx->proj_ok && ctx->kdtype == SLIM_BF16 && ctx->e == ctx->d && ctx->d % 64 == 0;
+}
+
+void slim_tree_tc_layout(const slim_ctx* ctx, int batch, int t_cap, int n, SlimTreeLayout& L) {
+  const size_t R = (size_t)ctx->H * n;
+  const int nb = (t_cap + SC_KEYS - 1) / SC_KEYS;
+  L.mt = R > 256 ? 2 : 1;
+  L.g_ncol = (ctx->d + SU_COLS - 1) / SU_COLS;
+  L.g_tiles = L.g_ncol * (int)((R + L.mt * 256 - 1) / (L.mt * 256));
+  L.g_pairs = ctx->num_sms / 2;
+  // fewer than two tiles a pair: cut each into parts of at least eight stages, for about four parts a pair
+  const long long tiles = (long long)batch * L.g_tiles;
+  long long split = tiles < 2 * L.g_pairs ? (4LL * L.g_pairs + tiles - 1) / tiles : 1;
+  const long long most = (t_cap / 64 + 2) / 8;
+  if (split > most) split = most;
+  L.g_split = split < 1 ? 1 : (int)split;
+  const long long sub = tiles * L.g_split, waves = sub / L.g_pairs - (batch > 1 ? 1 : 0);   // (ragged lengths: level them with a wave)
+  L.g_whole = waves > 0 ? (int)(waves * L.g_pairs) : 0;
+  L.p_s_draft = nb * SC_KEYS;
+  L.p_ld = L.p_s_draft + 64;
+  const size_t slots = 2 * (size_t)L.g_pairs + (L.g_split > 1 ? (size_t)sub : 0);
+  size_t off = L.shared_end;
+  L.p = off; off = align256(off + 2 * (size_t)batch * R * L.p_ld);
+  L.stat = off; off = align256(off + 8 * (size_t)batch * (nb + 1) * R);
+  L.tail = off; off = align256(off + 2 * (size_t)batch * 128 * ctx->d);
+  L.uh = off; off = align256(off + 2 * (size_t)batch * R * ctx->d);
+  L.part = off; off = align256(off + sizeof(float) * slots * L.mt * 256 * SU_COLS);
+  if (off > L.total) L.total = off;
+}
+
+cudaError_t slim_launch_tree_tc(const slim_ctx* ctx, const SlimDecodeParams& p, const SlimTreeView& t, const SlimTreeLayout& L,
+                                long long total_rows, void* o, cudaStream_t st) {
+  const int d = p.d, dk = p.d_k, H = p.H, R = H * t.n, M = p.batch * t.n;
+  CUtensorMap pmap, kmap, tailmap, umap, wmap;
+  cudaError_t e;
+  {
+    const unsigned long long dims[3] = {(unsigned long long)t.p_ld, (unsigned long long)R, (unsigned long long)p.batch};
+    const unsigned long long str[2] = {2ull * t.p_ld, 2ull * t.p_ld * R};
+    const unsigned int box[3] = {64, SU_ROWS, 1};
+    if ((e = slim_tmap_encode_3d(&pmap, t.p, dims, str, box)) != cudaSuccess) return e;
+  }
+  for (int k = 0; k < 2; ++k) {
+    const unsigned long long dims[3] = {64, k ? 128ull * p.batch : (unsigned long long)total_rows, (unsigned long long)(d / 64)};
+    const unsigned long long str[2] = {2ull * d, 128};
+    const unsigned int box[3] = {64, p.block_table ? 16u : 64u, 2};
+    if ((e = slim_tmap_encode_3d(k ? &tailmap : &kmap, k ? t.tail : const_cast<void*>(p.k), dims, str, box)) != cudaSuccess) return e;
+  }
+  {
+    const unsigned long long dims[3] = {(unsigned long long)d, (unsigned long long)M, (unsigned long long)H};
+    const unsigned long long str[2] = {2ull * d, 2ull * d * M};
+    const unsigned int box[3] = {64, 128, 1};
+    if ((e = slim_tmap_encode_3d(&umap, t.uh, dims, str, box)) != cudaSuccess) return e;
+  }
+  {   // (d_k = 96: the second half of a row runs into the next one, finite weights that N = 96 leaves out; the allocation is padded)
+    const unsigned long long dims[3] = {64, (unsigned long long)H * d, dk == 64 ? 1ull : 2ull};
+    const unsigned long long str[2] = {2ull * dk, 128};
+    const unsigned int box[3] = {64, 64, dk == 64 ? 1u : 2u};
+    if ((e = slim_tmap_encode_3d(&wmap, const_cast<void*>(p.wkv), dims, str, box)) != cudaSuccess) return e;
+  }
+  e = slim_launch_pdl(slim_tree_tail_kernel, dim3(16, p.batch), dim3(256), 0, st, p, t);
+  if (e != cudaSuccess) return e;
+  e = dk == 64 ? launch_p_tokens<64>(ctx, p, t, st) : dk == 96 ? launch_p_tokens<96>(ctx, p, t, st) : launch_p_tokens<128>(ctx, p, t, st);
+  if (e != cudaSuccess) return e;
+  e = slim_launch_pdl(slim_tree_finish_kernel, dim3((R + 31) / 32, p.batch), dim3(1024), 0, st, p, t);
+  if (e != cudaSuccess) return e;
+  e = L.mt == 1 ? launch_u<1>(ctx, p, t, pmap, kmap, tailmap, st) : launch_u<2>(ctx, p, t, pmap, kmap, tailmap, st);
+  if (e != cudaSuccess) return e;
+  if (L.g_split > 1 || L.g_whole < p.batch * L.g_tiles) {
+    const size_t smem = sizeof(long long) * (p.batch + 1 + t.g_pairs + 1) + sizeof(int) * (p.batch + L.g_split + t.g_pairs) + 16;
+    const int tiles = p.batch * L.g_tiles - (L.g_split == 1 ? L.g_whole : 0);          // the others are written as a whole
+    e = slim_launch_pdl(slim_tree_join_kernel, dim3(tiles, L.mt * 16), dim3(256), smem, st, p, t, L.mt);
+    if (e != cudaSuccess) return e;
+  }
+  const int ns = d / 64, parts = ns >= 4 ? 4 : ns >= 2 ? 2 : 1;
+  e = cudaFuncSetAttribute(slim_tree_out_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)OU_SMEM);
+  if (e != cudaSuccess) return e;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(parts, H, (M + 127) / 128); cfg.blockDim = dim3(128); cfg.dynamicSmemBytes = OU_SMEM; cfg.stream = st;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = parts; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr; cfg.numAttrs = 2;
+  return cudaLaunchKernelEx(&cfg, slim_tree_out_kernel, umap, wmap, (__nv_bfloat16*)o, M, d, dk, parts, p.status);
+}
