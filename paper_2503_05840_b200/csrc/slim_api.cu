@@ -238,6 +238,7 @@ slim_status create_impl(slim_ctx** out, int d, int H, int d_k, double rope_theta
     if (c->tc_workers[cl - 1] > 0) c->tc_ok = 1;
   }
   c->gen_workers = slim_generic_workers(c);
+  if (slim_tree_tc_ok(c) && rope_theta != 0.0 && slim_tree_make_table(c) != cudaSuccess) { cudaGetLastError(); slim_destroy(c); return SLIM_ERR_OOM; }
   *out = c;
   return SLIM_OK;
 }
@@ -250,6 +251,7 @@ void slim_destroy(slim_ctx* ctx) {
   cudaFree(ctx->wkv_hscale);
   cudaFree(ctx->rope_off);
   cudaFree(ctx->rope_base);
+  cudaFree(ctx->rope_frag);
   cudaFree(ctx->status);
   cudaFree(ctx->any_flag);
   cudaFree(ctx->xc_wk);

@@ -73,6 +73,7 @@ struct slim_ctx {
   float* wkv_hscale;             // device [H]: 2^-a_h
   float2* rope_off;              // device [TT][half]
   float2* rope_base;             // device table, grown by slim_cache_create
+  void* rope_frag;               // tensor-core tree attention: (cos, sin) of offsets 0 .. 127 in lane order (slim_tree_tc.cu)
   int rope_base_tiles;
   int* status;                   // device status word
   int tc_ok;                     // shape fits the tensor-core path with some cluster size
@@ -150,9 +151,9 @@ cudaError_t slim_tc_make_tmap(const slim_ctx* ctx, slim_cache* c, int cl);
 cudaError_t slim_launch_wait_selftest(int* status, int* gave_up, cudaStream_t st);
 cudaError_t slim_launch_tc(const slim_ctx* ctx, const slim_cache* c, const SlimDecodeParams& p, cudaStream_t st);
 
-// 3-D tiled tensor map with 128-byte swizzle over bf16 data (driver entry point looked up once)
+// 3-D tiled tensor map over bf16 data, with 128-byte swizzle or plain rows (driver entry point looked up once)
 cudaError_t slim_tmap_encode_3d(void* out_map, void* base, const unsigned long long dims[3],
-                                const unsigned long long strides[2], const unsigned int box[3]);
+                                const unsigned long long strides[2], const unsigned int box[3], bool swizzle = true);
 
 // tensor-core combine + projection (slim_proj.cu)
 int    slim_proj_shape_ok(int d, int H, int d_k, int dtype);
@@ -205,7 +206,8 @@ cudaError_t slim_launch_rank_combine(const slim_ctx* ctx, const SlimDecodeParams
 cudaError_t slim_launch_values(const slim_ctx* ctx, const void* K, int n, float* V, cudaStream_t st,
                                const slim_cache* cache = nullptr, const int32_t* positions = nullptr, int n_new = 0);
 
-// drafted tokens (slim_tree.cu, slim_draft.cu)
+// drafted tokens (slim_tree.cu, slim_tree_tc.cu, slim_draft.cu)
+cudaError_t slim_tree_make_table(slim_ctx* ctx);
 cudaError_t slim_launch_tree(const slim_ctx* ctx, const SlimDecodeParams& p, const void* k_tree, const int32_t* parents, int n,
                              void* o, char* ws, int tc, long long total_rows, cudaStream_t st);
 cudaError_t slim_launch_verify(const float* p, const float* q, const int32_t* tokens, const int32_t* parents, const float* r, int batch,

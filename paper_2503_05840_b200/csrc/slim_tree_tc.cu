@@ -10,6 +10,9 @@
 //   sum         U = P K / l on tcgen05, CTA pairs (cta_group::2), bf16
 //   join        adds the parts of tiles whose keys were cut
 //   out         o = U W_KV,h on tcgen05
+#include <cmath>
+#include <cstdlib>
+
 #include "slim_ptx.cuh"
 #include "slim_sched.cuh"
 #include "slim_tree.h"
@@ -18,11 +21,6 @@ using namespace slim_ptx;
 
 namespace {
 
-__device__ __forceinline__ uint32_t tf32(float x) { uint32_t r; asm("cvt.rna.tf32.f32 %0, %1;" : "=r"(r) : "f"(x)); return r; }
-__device__ __forceinline__ void mma_tf32(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-  asm volatile("mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-}
 __device__ __forceinline__ float2 turn(const SlimDecodeParams& p, int pos, int j) {      // (cos, sin) of pos theta_j
   const float2 cb = __ldg(p.rope_base + (size_t)(pos / SLIM_TT) * p.half + j), co = __ldg(p.rope_off + (pos % SLIM_TT) * p.half + j);
   return make_float2(cb.x * co.x - cb.y * co.y, cb.y * co.x + cb.x * co.y);
@@ -52,250 +50,372 @@ __global__ void __launch_bounds__(256) slim_tree_tail_kernel(const SlimDecodePar
 }
 
 // ------------------------------------------------------------------------------------------------ scores
-// A CTA takes one (sequence, head) and every gridDim.x-th block of 128 keys; warp w has keys 16 w .. 16 w + 15 of a
-// block, rows g and g + 8 of an m16n8k8 tf32 tile in each thread, and the tokens as the tile's columns.
-//   - The contraction runs over rotation pairs: step (pc, x) puts the low element of pair j into k-slot c and the
-//     high one into slot c + 4 (c = lane % 4), j = (c + 4 pc) VW + x.  So a thread holds both halves of its pairs, loads
-//     them as VW contiguous elements and rotates in registers; the keys never pass through shared memory.
+// A CTA takes one (sequence, head); its two halves of eight warps share the tables and take every other block of 128
+// keys each, with barriers of their own, so that one computes while the other waits.  Warp w of a half has keys
+// 16 w .. 16 w + 15 of a block, rows g and g + 8 of m16n8k16 float16 tiles in each thread, and the tokens as the tiles'
+// columns; its key tile comes by TMA into a buffer of its own, which nobody else reads.
+//   - The contraction runs over rotation pairs: step (pc, x) puts the low elements of pairs j, j + 1 into the k-slots 2 c,
+//     2 c + 1 and the high ones into 2 c + 8, 2 c + 9 (c = lane % 4), j = chunk(c, pc) VW + 2 x.  So a thread reads both
+//     halves of its pairs as VW contiguous elements and rotates in registers (packed float32) on the way into the
+//     instruction.
 //   - R_pos(t) = R_(128 block) R_o: keys are turned by their offset o < 128 in the block only, whose (cos, sin) are
-//     the same for every block (a table in shared memory in the order the lanes read it); the queries, turned to their
-//     positions once, are turned back by the block's angle, 64 complex factors a block.
-//   - tf32 keeps 11 bits of the rotated values; bf16 operands (8 bits) would cost as much accuracy as the rounding of
-//     P does, for a product that is 1 / H of the step's.
-//   - P is written relative to a reference that is a multiple of 64 next to the block's maximum: nearly always 0 for all
-//     blocks of a row, so that the blocks need no common maximum; `finish` shifts the exponents of the others, exactly.
-//     Sums l are taken from the rounded P, so the weights of a row add up to one.
-// Bound by (n = 16, d_k = 128) the shared-memory reads of the table and the query fragments and the rotation's FMAs.
-constexpr int SC_KEYS = 128, SC_THREADS = 256, SC_WARPS = 8;
+//     the same for every block (a table of the context, in the order the lanes read it); the queries, turned to
+//     their positions once, are turned back by the block's angle, 64 complex factors a block.
+//   - float16 keeps 11 bits of the rotated values (bf16's 8 would cost as much accuracy as the rounding of P does, for a
+//     product that is 1 / H of the step's) at twice tf32's rate.  Its range: queries are scaled by a power of two per
+//     token; keys go in as they are, and a warp whose sums overflow, or whose queries are so large that the smallest
+//     float16 steps of a key would show, repeats its tile with the keys scaled by a power of two.
+//   - P is written relative to a reference that is a multiple of 64, kept from block to block while the arguments
+//     stay below reference + 60: nearly always the same for all blocks of a row, so that the blocks need no common
+//     maximum; `finish` shifts the exponents of the others, exactly.  Sums l are taken from the rounded P, so the weights
+//     of a row add up to one.
+constexpr int SC_KEYS = 128, SC_HALF = 256, SC_THREADS = 2 * SC_HALF, SC_WARPS = SC_THREADS / 32;
 
 template <int DK, int NT>
 struct ScoreShape {
-  static constexpr int HALF = DK / 2, VW = DK == 96 ? 4 : 8, NPC = HALF / (4 * VW), STEPS = HALF / 4, PER = STEPS / 2 * 32;
-  static constexpr int QLD = HALF + 2;                                   // float2 per token row of the turned queries
-  static constexpr size_t CS = (size_t)SC_KEYS * HALF * 8, QF = (size_t)NT * STEPS / 2 * 32 * 16, QS = (size_t)8 * NT * QLD * 8;
+  static constexpr int HALF = DK / 2, VW = DK == 96 ? 4 : 8, NPC = HALF / (4 * VW), STEPS = HALF / 8, PER = STEPS * 32;
+  static constexpr bool QHALF = NT > 4;                                  // kept as float16 pairs (room; a second rounding to 11 bits)
+  static constexpr int KT = 16 * DK * 2, KS = NT <= 2 ? 2 : 1;           // bytes of a warp's key tile, buffers
+  static constexpr size_t KR = (size_t)SC_WARPS * KS * KT, CS = (size_t)SC_KEYS * HALF * 8, QF = (size_t)NT * PER * 8;
+  static constexpr size_t QS = (size_t)8 * NT * HALF * (QHALF ? 4 : 8);
   static constexpr int PLD = SC_KEYS + 8;                                // bf16 per token row of the P tile
-  static constexpr size_t PT = (size_t)8 * NT * PLD * 2;
-  static constexpr size_t SMEM = CS + QF + QS + PT + sizeof(float) * 8 * NT * (SC_WARPS + 2) + 16;
+  static constexpr size_t PT = (size_t)8 * NT * PLD * 2, SR = (size_t)8 * NT * 8, MX = (size_t)8 * NT * 4;
+  static constexpr size_t OWN = QF + PT + SR + MX;                       // of a half
+  static constexpr size_t SMEM = 1024 + KR + CS + QS + 2 * OWN + 8 * SC_WARPS * KS + 16;
 };
+// which VW pairs of a head lane c takes in turn pc; for d_k = 128 even and odd key rows then meet different banks
+__host__ __device__ constexpr int chunk_of(int dk, int c, int pc) { return dk == 128 ? 2 * c + pc : c + 4 * pc; }
+// where a thread's VW low (hl = 0) or high elements lie in a warp's key tile of 16 rows (r % 8 = g): two 64-column
+// atoms with 128-byte swizzle, one of them, or plain rows
+template <int DK>
+__device__ __forceinline__ uint32_t tile_off(int r, int g, int c, int pc, int hl) {
+  if (DK == 128) return (uint32_t)(hl * 2048 + r * 128 + (((2 * c + pc) ^ g) << 4));
+  if (DK == 64) return (uint32_t)(r * 128 + (((c + 4 * hl) ^ g) << 4));
+  return (uint32_t)(r * 192 + hl * 96 + (c + 4 * pc) * 8);
+}
 
 template <int VW> struct KVec;
 template <> struct KVec<8> { typedef uint4 type; };
 template <> struct KVec<4> { typedef uint2 type; };
-__device__ __forceinline__ float bf_lo(uint32_t w) { return __uint_as_float(w << 16); }
-__device__ __forceinline__ float bf_hi(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
-__device__ __forceinline__ float elem(const uint4& v, int x) {
-  const uint32_t w = x < 2 ? v.x : x < 4 ? v.y : x < 6 ? v.z : v.w;
-  return (x & 1) ? bf_hi(w) : bf_lo(w);
+__device__ __forceinline__ uint32_t word(const uint4& v, int x) { return x == 0 ? v.x : x == 1 ? v.y : x == 2 ? v.z : v.w; }
+__device__ __forceinline__ uint32_t word(const uint2& v, int x) { return x == 0 ? v.x : v.y; }
+__device__ __forceinline__ uint32_t& word_ref(uint4& v, int x) { return x == 0 ? v.x : x == 1 ? v.y : x == 2 ? v.z : v.w; }
+__device__ __forceinline__ uint32_t& word_ref(uint2& v, int x) { return x == 0 ? v.x : v.y; }
+__device__ __forceinline__ uint32_t half2_of(f32x2 v) {                   // (low, high) -> float16 pair
+  uint32_t d;
+  asm("{\n\t.reg .f32 lo, hi;\n\tmov.b64 {lo, hi}, %1;\n\tcvt.rn.f16x2.f32 %0, hi, lo;\n\t}" : "=r"(d) : "l"(v));
+  return d;
 }
-__device__ __forceinline__ float elem(const uint2& v, int x) { const uint32_t w = x < 2 ? v.x : v.y; return (x & 1) ? bf_hi(w) : bf_lo(w); }
+__device__ __forceinline__ uint32_t bf162_of(float lo, float hi) { uint32_t d; asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo)); return d; }
+__device__ __forceinline__ f32x2 sub2(f32x2 a, f32x2 b) { f32x2 d; asm("sub.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b)); return d; }
+__device__ __forceinline__ void mma_f16(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void stmatrix_x2_trans(uint32_t addr, uint32_t a, uint32_t b) {
+  asm volatile("stmatrix.sync.aligned.m8n8.x2.trans.shared.b16 [%0], {%1, %2};" ::"r"(addr), "r"(a), "r"(b) : "memory");
+}
 __device__ __forceinline__ int ordered(float f) { const int i = __float_as_int(f); return i ^ ((i >> 31) & 0x7fffffff); }
 __device__ __forceinline__ float unordered(int i) { return __int_as_float(i ^ ((i >> 31) & 0x7fffffff)); }
+// 2^e with the exponent that brings |x| near `top`; 1 for 0, infinities and NaN
+__device__ __forceinline__ float pow2_to(float x, int top) {
+  if (!(x > 0.f) || x > 3e38f) return 1.f;
+  const int e = top - (((__float_as_int(x) >> 23) & 255) - 127);
+  return __int_as_float((min(max(e, -120), 120) + 127) << 23);
+}
+
+// barriers of one half
+__device__ __forceinline__ void half_sync(int half) { asm volatile("barrier.cta.sync %0, %1;" ::"r"(1 + half), "n"(SC_HALF) : "memory"); }
+__device__ __forceinline__ bool half_any(int half, bool v) {
+  int r;
+  asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %1, 0;\n\tbarrier.cta.red.or.pred q, %2, %3, p;\n\tselp.b32 %0, 1, 0, q;\n\t}"
+               : "=r"(r) : "r"((int)v), "r"(1 + half), "n"(SC_HALF) : "memory");
+  return r != 0;
+}
 
 template <int DK, int NT, bool ROPE>
-__global__ void __launch_bounds__(SC_THREADS)
-slim_tree_p_kernel(const SlimDecodeParams p, const SlimTreeView t) {
+__global__ void __launch_bounds__(SC_THREADS, 1)
+slim_tree_p_kernel(const __grid_constant__ CUtensorMap cmap, const __grid_constant__ CUtensorMap dmap, const SlimDecodeParams p,
+                   const SlimTreeView t, const float4* __restrict__ table) {
   typedef ScoreShape<DK, NT> S;
   constexpr int HALF = S::HALF, VW = S::VW, NPC = S::NPC, TOK = 8 * NT;
   typedef typename KVec<VW>::type kvec;
-  extern __shared__ __align__(16) unsigned char sm[];
-  float4* cst = reinterpret_cast<float4*>(sm);                            // [warp][row half][pc][VW / 2][lane]
-  float4* qf = reinterpret_cast<float4*>(sm + S::CS);                     // [NT][STEPS / 2][lane]
-  float2* qs = reinterpret_cast<float2*>(sm + S::CS + S::QF);             // [TOK][QLD]
-  __nv_bfloat16* pt = reinterpret_cast<__nv_bfloat16*>(sm + S::CS + S::QF + S::QS);      // [TOK][PLD]
-  float* wsum = reinterpret_cast<float*>(sm + S::CS + S::QF + S::QS + S::PT);            // [warps][TOK]
-  int* smax = reinterpret_cast<int*>(wsum + SC_WARPS * TOK);              // [2][TOK]
+  extern __shared__ unsigned char smem_raw[];
+  unsigned char* sm = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, c = lane & 3;
+  const int half = warp >> 3, hw = warp & 7, htid = tid & (SC_HALF - 1);
+  unsigned char* ring = sm + (size_t)warp * S::KS * S::KT;                // this warp's key tiles
+  float4* cst = reinterpret_cast<float4*>(sm + S::KR);                    // [warp][row half][pc][VW / 2][lane] (cos, cos, sin, sin)
+  unsigned char* qs = sm + S::KR + S::CS;                                 // [NT][STEPS][lane][2] the turned queries' pairs
+  unsigned char* own = sm + S::KR + S::CS + S::QS + half * S::OWN;
+  uint2* qf = reinterpret_cast<uint2*>(own);                              // [NT][STEPS][lane]
+  __nv_bfloat16* pt = reinterpret_cast<__nv_bfloat16*>(own + S::QF);      // [TOK][PLD]
+  float2* sr = reinterpret_cast<float2*>(own + S::QF + S::PT);            // [TOK] (what a token's sums are multiplied by, its reference)
+  int* smax = reinterpret_cast<int*>(own + S::QF + S::PT + S::SR);        // [TOK] largest argument, where a reference has to move
+  unsigned char* tail = sm + S::KR + S::CS + S::QS + 2 * S::OWN;
+  const uint32_t bar = smem_u32(tail) + 8u * (uint32_t)(warp * S::KS);    // this warp's barriers
+  volatile int* s_abort = reinterpret_cast<volatile int*>(tail + 8 * SC_WARPS * S::KS);
   const int b = blockIdx.z, h = blockIdx.y, n = t.n, R = p.H * n;
 
-  if (ROPE) {                                                             // (reads only the context's tables)
-    for (int e = tid; e < SC_KEYS * HALF / 2; e += SC_THREADS) {
-      const int ln = e & 31, xq = (e >> 5) % (VW / 2), rest = (e >> 5) / (VW / 2), pc = rest % NPC, rh = rest / NPC % 2, w = rest / NPC / 2;
-      const int o = 16 * w + 8 * rh + (ln >> 2), j = ((ln & 3) + 4 * pc) * VW + 2 * xq;
-      const float2 a = turn(p, o, j), z = turn(p, o, j + 1);
-      cst[e] = make_float4(a.x, a.y, z.x, z.y);
-    }
+  if (lane == 0) {
+    for (int i = 0; i < S::KS; ++i) mbar_init(bar + 8 * i, 1);
+    if (warp == 0) { prefetch_tensormap(&cmap); prefetch_tensormap(&dmap); *s_abort = 0; }
+    fence_mbar_init();
   }
+  if (ROPE)                                                               // (a table of the context: no need to wait for it)
+    for (int e = tid; e < SC_KEYS * HALF / 2; e += SC_THREADS) cst[e] = __ldg(table + e);
   slim_pdl_trigger();
   slim_pdl_wait();
   const int len = t.len[b], nblk = (len + SC_KEYS - 1) / SC_KEYS, nb_cap = (p.t_cap + SC_KEYS - 1) / SC_KEYS;
+  // the draft block comes last, in the first half of the CTAs of column 0
+  const int first = 2 * blockIdx.x + half, step = 2 * gridDim.x;
+  if (2 * (int)blockIdx.x >= nblk && blockIdx.x != 0) return;             // (both halves)
+  const int mine = nblk > first ? (nblk - 1 - first) / step + 1 : 0;
+  const int total = mine + (first == 0 ? 1 : 0);
   const int* dep = t.depth + (size_t)b * n;
-  const unsigned long long* mask = t.mask + (size_t)b * n;
-  const __nv_bfloat16* Kc = reinterpret_cast<const __nv_bfloat16*>(p.k);
-  const __nv_bfloat16* Kt = reinterpret_cast<const __nv_bfloat16*>(t.k_tree) + (size_t)b * n * p.d;
-  __nv_bfloat16* Pout = t.p + ((size_t)b * R + (size_t)h * n) * t.p_ld;
-  float2* stat = t.stat + (size_t)b * (nb_cap + 1) * R + h * n;
 
-  // queries of this (sequence, head), scaled and turned to their positions
-  {
-    const __nv_bfloat16* Q = reinterpret_cast<const __nv_bfloat16*>(p.q) + (size_t)b * n * p.d + h * DK;
-    for (int e = tid; e < TOK * HALF; e += SC_THREADS) {
-      const int i = e / HALF, j = e - i * HALF;
-      float2 v = make_float2(0.f, 0.f);
-      if (i < n && dep[i] >= 0) {
-        const float q1 = __bfloat162float(Q[(size_t)i * p.d + j]) * p.qscale, q2 = __bfloat162float(Q[(size_t)i * p.d + HALF + j]) * p.qscale;
-        if (ROPE) {
-          const float2 cs = turn(p, len + dep[i], j);
-          v = make_float2(q1 * cs.x + q2 * cs.y, q2 * cs.x - q1 * cs.y);
-        } else v = make_float2(q1, q2);
-      }
-      qs[i * S::QLD + j] = v;
-    }
-    for (int i = tid; i < 2 * TOK; i += SC_THREADS) smax[i] = ordered(-INFINITY);
-  }
-  unsigned live = 0;                                                      // bit 2 nt + z: token 8 nt + 2 c + z is there
-#pragma unroll
-  for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-    for (int z = 0; z < 2; ++z) {
-      const int i = 8 * nt + 2 * c + z;
-      if (i < n && dep[i] >= 0) live |= 1u << (2 * nt + z);
-    }
-
-  // this thread's part of the query fragments: pairs j0, j0 + 1 of token 8 nt + lane / 4, for nt = nt0, nt0 + nts, ..
-  constexpr int NTS = SC_THREADS / S::PER;
-  const int nt0 = tid / S::PER, fi = tid % S::PER, fs = 2 * (fi >> 5), j0 = ((fi & 3) + 4 * (fs / VW)) * VW + fs % VW;
-  const int ftok = (fi & 31) >> 2;
-
-  // the draft block comes last, in the CTAs of column 0
-  const int mine = nblk > (int)blockIdx.x ? (nblk - 1 - blockIdx.x) / gridDim.x + 1 : 0;
-  const int total = mine + (blockIdx.x == 0 ? 1 : 0);
-  kvec k[2][NPC][2];                                                      // [row half][pc][low / high element of the pairs]
-  float4 bc = make_float4(1.f, 0.f, 1.f, 0.f);                            // (cos, sin) of the block's angle, pairs j0, j0 + 1
-  auto fetch = [&](int it) {
+  // this thread's part of the query fragments: pairs j0, j0 + 1 of token 8 nt + lane / 4, for nt = nt0, nt0 + NTS, ..
+  constexpr int NTS = SC_HALF / S::PER;
+  const int nt0 = htid / S::PER, fi = htid % S::PER, fs = fi >> 5, j0 = chunk_of(DK, fi & 3, fs / (VW / 2)) * VW + 2 * (fs % (VW / 2));
+  auto fetch = [&](int it) {                                              // (lane 0) rows that are not there are masked later
     const bool draft = it == mine;
-    const int blk = blockIdx.x + it * gridDim.x;
-    if (ROPE) {
-      if (draft) {
-        const float2 a = turn(p, len, j0), z = turn(p, len, j0 + 1);
-        bc = make_float4(a.x, a.y, z.x, z.y);
-      } else {
-        bc = __ldg(reinterpret_cast<const float4*>(p.rope_base + (size_t)blk * (SC_KEYS / SLIM_TT) * HALF + j0));
-      }
-    }
-    const int t0 = draft ? 16 * warp : blk * SC_KEYS + 16 * warp;
-    const __nv_bfloat16* base = Kt + (size_t)t0 * p.d;
-    if (!draft) base = t0 < len ? Kc + (size_t)slim_cache_row(p, b, t0) * p.d : Kc;
-#pragma unroll
-    for (int rh = 0; rh < 2; ++rh) {
-      const int r = g + 8 * rh;
-      const bool ok = draft ? (t0 + r < n && dep[t0 + r] >= 0) : t0 + r < len;
-      const __nv_bfloat16* row = base + (size_t)r * p.d + h * DK + c * VW;
-#pragma unroll
-      for (int pc = 0; pc < NPC; ++pc)
-#pragma unroll
-        for (int hi = 0; hi < 2; ++hi) {
-          kvec v = {};
-          if (ok) v = __ldg(reinterpret_cast<const kvec*>(row + hi * HALF + 4 * pc * VW));
-          k[rh][pc][hi] = v;
-        }
-    }
+    const int blk0 = draft ? 0 : (first + it * step) * SC_KEYS;
+    int t0 = blk0 + 16 * hw;
+    if (t0 >= (draft ? n : len)) t0 = blk0;
+    const int row = draft ? b * n + t0 : (int)slim_cache_row(p, b, t0), st = it % S::KS;
+    mbar_arrive_expect_tx(bar + 8 * st, S::KT);
+    tma_load_3d(smem_u32(ring) + (uint32_t)(st * S::KT), draft ? &dmap : &cmap, bar + 8 * st, DK == 96 ? h * DK : 0, row,
+                DK == 128 ? 2 * h : DK == 64 ? h : 0);
   };
-  if (total > 0) fetch(0);
-  __syncthreads();
-
-  for (int it = 0; it < total; ++it) {
-    const bool draft = it == mine;
-    const int blk = blockIdx.x + it * gridDim.x, t0 = draft ? 16 * warp : blk * SC_KEYS + 16 * warp;
-    // ---- query fragments of this block
+  auto block_angle = [&](int it) {                                        // (cos, sin) of the block's angle, pairs j0, j0 + 1
+    if (!ROPE) return make_float4(1.f, 0.f, 1.f, 0.f);
+    if (it == mine) {
+      const float2 a = turn(p, len, j0), z = turn(p, len, j0 + 1);
+      return make_float4(a.x, a.y, z.x, z.y);
+    }
+    return __ldg(reinterpret_cast<const float4*>(p.rope_base + (size_t)(first + it * step) * (SC_KEYS / SLIM_TT) * HALF + j0));
+  };
+  auto fragments = [&](const float4& bc) {                                // queries turned back by the block's angle
     if (nt0 < NTS) {
 #pragma unroll
       for (int nt = nt0; nt < NT; nt += NTS) {
-        const float4 q = *reinterpret_cast<const float4*>(qs + (size_t)(8 * nt + ftok) * S::QLD + j0);
-        float4 f;
-        f.x = __uint_as_float(tf32(q.x * bc.x - q.y * bc.y)); f.y = __uint_as_float(tf32(q.y * bc.x + q.x * bc.y));
-        f.z = __uint_as_float(tf32(q.z * bc.z - q.w * bc.w)); f.w = __uint_as_float(tf32(q.w * bc.z + q.z * bc.w));
-        qf[nt * S::PER + fi] = f;
+        float4 q;
+        if (S::QHALF) {
+          const uint2 w = reinterpret_cast<const uint2*>(qs)[nt * S::PER + fi];
+          const float2 u = __half22float2(*reinterpret_cast<const __half2*>(&w.x)), v = __half22float2(*reinterpret_cast<const __half2*>(&w.y));
+          q = make_float4(u.x, u.y, v.x, v.y);
+        } else q = reinterpret_cast<const float4*>(qs)[nt * S::PER + fi];
+        qf[nt * S::PER + fi] = make_uint2(half2_of(pack2(q.x * bc.x - q.y * bc.y, q.z * bc.z - q.w * bc.w)),
+                                          half2_of(pack2(q.y * bc.x + q.x * bc.y, q.w * bc.z + q.z * bc.w)));
       }
     }
-    __syncthreads();
-    if (tid < TOK) smax[((it + 1) & 1) * TOK + tid] = ordered(-INFINITY);  // (last read before the barrier above)
-    // ---- scores
-    float s[NT][4];
+  };
+  __syncwarp();
+  if (lane == 0)
+    for (int i = 0; i < S::KS && i < total; ++i) fetch(i);
+  float4 bc = make_float4(1.f, 0.f, 1.f, 0.f);
+  if (total > 0) bc = block_angle(0);
+
+  // queries of this (sequence, head), scaled and turned to their positions; one warp a token
+  bool large = false;
+  {
+    const __nv_bfloat16* Q = reinterpret_cast<const __nv_bfloat16*>(p.q) + (size_t)b * n * p.d + h * DK;
+    for (int i = warp; i < TOK; i += SC_WARPS) {
+      const bool there = i < n && dep[i] >= 0;
+      float2 v[(HALF + 31) / 32];
+      float top = 0.f;
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt) s[nt][0] = s[nt][1] = s[nt][2] = s[nt][3] = 0.f;
-#pragma unroll
-    for (int pc = 0; pc < NPC; ++pc)
-#pragma unroll
-      for (int xq = 0; xq < VW / 2; ++xq) {
-        uint32_t a[2][4];
-#pragma unroll
-        for (int rh = 0; rh < 2; ++rh) {
-          float4 cs = make_float4(1.f, 0.f, 1.f, 0.f);
+      for (int x = 0; x < (HALF + 31) / 32; ++x) {
+        const int j = lane + 32 * x;
+        v[x] = make_float2(0.f, 0.f);
+        if (there && j < HALF) {
+          const float q1 = __bfloat162float(Q[(size_t)i * p.d + j]) * p.qscale, q2 = __bfloat162float(Q[(size_t)i * p.d + HALF + j]) * p.qscale;
           if (ROPE) {
-            if (!draft) cs = cst[(((warp * 2 + rh) * NPC + pc) * (VW / 2) + xq) * 32 + lane];
-            else {
-              const int r = t0 + g + 8 * rh, o = r < n ? max(dep[r], 0) : 0, j = (c + 4 * pc) * VW + 2 * xq;
-              const float2 u = turn(p, o, j), v = turn(p, o, j + 1);
-              cs = make_float4(u.x, u.y, v.x, v.y);
+            const float2 cs = turn(p, len + dep[i], j);
+            v[x] = make_float2(q1 * cs.x + q2 * cs.y, q2 * cs.x - q1 * cs.y);
+          } else v[x] = make_float2(q1, q2);
+        }
+        top = fmaxf(top, fmaxf(fabsf(v[x].x), fabsf(v[x].y)));
+      }
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+      const float sc = pow2_to(top, 4);                                   // the largest element near 16
+#pragma unroll
+      for (int x = 0; x < (HALF + 31) / 32; ++x)
+        if (lane + 32 * x < HALF) {
+          const int j = lane + 32 * x, ch = j / VW, pc = DK == 128 ? ch & 1 : ch >> 2, cc = DK == 128 ? ch >> 1 : ch & 3;
+          const int at = 2 * ((i >> 3) * S::PER + (pc * (VW / 2) + (j % VW) / 2) * 32 + (i & 7) * 4 + cc) + (j & 1);
+          if (S::QHALF) reinterpret_cast<uint32_t*>(qs)[at] = half2_of(pack2(v[x].x * sc, v[x].y * sc));
+          else reinterpret_cast<float2*>(qs)[at] = make_float2(v[x].x * sc, v[x].y * sc);
+        }
+      if (lane < 2) {                                                     // both halves' copies; a token that is not there: P = 2^(s - inf) = 0
+        unsigned char* o = sm + S::KR + S::CS + S::QS + lane * S::OWN + S::QF + S::PT;
+        reinterpret_cast<float2*>(o)[i] = make_float2(1.f / sc, there ? -INFINITY : INFINITY);
+        reinterpret_cast<int*>(o + S::SR)[i] = ordered(-INFINITY);
+      }
+      // keys near 1 lose at most 2^-12 of themselves; steps of 2^-25 of smaller ones show where DK |q| 2^-25 does
+      large = large || !(top <= 64.f);
+    }
+  }
+  const bool careful = __syncthreads_or(large);
+  const uint32_t pt_addr = smem_u32(pt) + (uint32_t)((lane & 7) * S::PLD + 16 * hw + 8 * ((lane >> 3) & 1)) * 2;
+  if (total > 0) fragments(bc);
+  if (total > 1) bc = block_angle(1);
+  half_sync(half);
+
+  for (int it = 0; it < total; ++it) {
+    const bool draft = it == mine;
+    const int blk = first + it * step, t0 = draft ? 16 * hw : blk * SC_KEYS + 16 * hw;
+    // ---- scores
+    // a thread's rows of the table: its keys' offsets in the block; a drafted key's offset is its depth
+    const ulonglong2* row_cs[2];
+#pragma unroll
+    for (int rh = 0; rh < 2; ++rh) {
+      int o = 16 * hw + 8 * rh + g;
+      if (draft) o = o < n ? max(dep[o], 0) : 0;
+      row_cs[rh] = reinterpret_cast<const ulonglong2*>(cst) + (o >> 3) * (NPC * (VW / 2) * 32) + ((o & 7) << 2) + c;
+    }
+    unsigned char* tile = ring + (it % S::KS) * S::KT;
+    mbar_wait<false>(bar + 8 * (it % S::KS), (it / S::KS) & 1, s_abort, p.status);      // (gave up: reported, and the loop runs on to its end)
+    float s[NT][4];
+    float back = 1.f;                                                     // undoes the keys' scaling
+    for (bool again = false;;) {
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) s[nt][0] = s[nt][1] = s[nt][2] = s[nt][3] = 0.f;
+#pragma unroll
+      for (int pc = 0; pc < NPC; ++pc) {
+        kvec k[2][2];                                                     // [row half][low / high elements of the pairs]
+#pragma unroll
+        for (int rh = 0; rh < 2; ++rh)
+#pragma unroll
+          for (int hl = 0; hl < 2; ++hl) k[rh][hl] = *reinterpret_cast<const kvec*>(tile + tile_off<DK>(g + 8 * rh, g, c, pc, hl));
+#pragma unroll
+        for (int xq = 0; xq < VW / 2; ++xq) {
+          uint32_t a[4];
+#pragma unroll
+          for (int rh = 0; rh < 2; ++rh) {
+            const f32x2 k1 = unpack2(word(k[rh][0], xq)), k2 = unpack2(word(k[rh][1], xq));
+            if (ROPE) {
+              const ulonglong2 cs = row_cs[rh][(pc * (VW / 2) + xq) * 32];
+              a[rh] = half2_of(fma2(k2, cs.y, mul2(k1, cs.x)));
+              a[2 + rh] = half2_of(sub2(mul2(k2, cs.x), mul2(k1, cs.y)));
+            } else {
+              a[rh] = half2_of(k1);
+              a[2 + rh] = half2_of(k2);
             }
           }
 #pragma unroll
-          for (int z = 0; z < 2; ++z) {
-            const float k1 = elem(k[rh][pc][0], 2 * xq + z), k2 = elem(k[rh][pc][1], 2 * xq + z);
-            const float co = z ? cs.z : cs.x, si = z ? cs.w : cs.y;
-            a[z][rh] = ROPE ? tf32(k1 * co + k2 * si) : __float_as_uint(k1);      // (a bf16 is a tf32)
-            a[z][2 + rh] = ROPE ? tf32(k2 * co - k1 * si) : __float_as_uint(k2);
+          for (int nt = 0; nt < NT; ++nt) {
+            const uint2 f = qf[nt * S::PER + (pc * (VW / 2) + xq) * 32 + lane];
+            mma_f16(s[nt], a, f.x, f.y);
           }
         }
+      }
+      // an overflow shows as an infinity or a NaN, and 0 x it is a NaN
+      float odd = 0.f;
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-          const float4 f = qf[nt * S::PER + (pc * (VW / 2) + xq) * 32 + lane];
-          mma_tf32(s[nt], a[0], __float_as_uint(f.x), __float_as_uint(f.y));
-          mma_tf32(s[nt], a[1], __float_as_uint(f.z), __float_as_uint(f.w));
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int x = 0; x < 4; ++x) odd = fmaf(s[nt][x], 0.f, odd);
+      if (again || !__any_sync(0xffffffffu, careful || odd != 0.f)) break;
+      again = true;
+      float top = 0.f, ks = 0.f;
+      for (int turn2 = 0; turn2 < 2; ++turn2) {                           // the largest element, then the scaling, in place: a thread's own elements
+#pragma unroll
+        for (int rh = 0; rh < 2; ++rh)
+#pragma unroll
+          for (int pc = 0; pc < NPC; ++pc)
+#pragma unroll
+            for (int hl = 0; hl < 2; ++hl) {
+              kvec* at = reinterpret_cast<kvec*>(tile + tile_off<DK>(g + 8 * rh, g, c, pc, hl));
+              kvec v = *at;
+#pragma unroll
+              for (int x = 0; x < VW / 2; ++x) {
+                const uint32_t w = word(v, x);
+                const float e0 = __uint_as_float(w << 16), e1 = __uint_as_float(w & 0xffff0000u);
+                if (turn2 == 0) top = fmaxf(top, fmaxf(fabsf(e0), fabsf(e1)));
+                else word_ref(v, x) = bf162_of(e0 * ks, e1 * ks);         // (a power of two: exact, but for what is 2^-100 of the largest)
+              }
+              if (turn2 == 1) *at = v;
+            }
+        if (turn2 == 0) {
+#pragma unroll
+          for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+          ks = pow2_to(top, 10);
+          back = 1.f / ks;
         }
       }
-    if (it + 1 < total) fetch(it + 1);
-    // ---- what is not attended
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-      for (int x = 0; x < 4; ++x) {
-        const int r = t0 + g + 8 * (x >> 1);
-        bool on = (live >> (2 * nt + (x & 1))) & 1;
-        if (draft) on = on && r < n && ((mask[min(8 * nt + 2 * c + (x & 1), n - 1)] >> (r & 63)) & 1);
-        else on = on && r < len;
-        if (!on) s[nt][x] = -INFINITY;
-      }
-    // ---- block maximum per token
-    int* mx = smax + (it & 1) * TOK;
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-      for (int z = 0; z < 2; ++z) {
-        float m = fmaxf(s[nt][z], s[nt][2 + z]);
-#pragma unroll
-        for (int o = 4; o < 32; o <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-        if (g == 0) atomicMax(mx + 8 * nt + 2 * c + z, ordered(m));
-      }
-    __syncthreads();
-    // ---- probabilities relative to the reference, and their sums over this warp's keys
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-      for (int z = 0; z < 2; ++z) {
-        const int i = 8 * nt + 2 * c + z;
-        const float m = unordered(mx[i]);
-        const float ref = 64.f * rintf(fminf(fmaxf(m, -1e30f), 1e30f) * (1.f / 64.f));
-        const __nv_bfloat16 p0 = __float2bfloat16(ex2_approx(s[nt][z] - ref)), p1 = __float2bfloat16(ex2_approx(s[nt][2 + z] - ref));
-        pt[i * S::PLD + 16 * warp + g] = p0;
-        pt[i * S::PLD + 16 * warp + g + 8] = p1;
-        float l = __bfloat162float(p0) + __bfloat162float(p1);
-#pragma unroll
-        for (int o = 4; o < 32; o <<= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
-        if (g == 0) wsum[warp * TOK + i] = l;
-      }
-    __syncthreads();
-    const int col = draft ? t.s_draft : blk * SC_KEYS, vecs = draft ? 8 : 16;
-    for (int e = tid; e < n * vecs; e += SC_THREADS) {
-      const int i = e / vecs, x = e - i * vecs;
-      *reinterpret_cast<uint4*>(Pout + (size_t)i * t.p_ld + col + 8 * x) = *reinterpret_cast<const uint4*>(pt + i * S::PLD + 8 * x);
+      fence_proxy_async_smem();                                           // (the next tile comes by the async proxy)
     }
-    if (tid < n) {
-      float l = 0.f;
+    __syncwarp();                                                         // all lanes have read the tile
+    if (lane == 0 && it + S::KS < total && !*s_abort) fetch(it + S::KS);
+    // ---- what is not attended
+    if (draft || t0 + 16 > len) {
+      const unsigned long long* mask = t.mask + (size_t)b * n;
 #pragma unroll
-      for (int w = 0; w < SC_WARPS; ++w) l += wsum[w * TOK + tid];
-      const float m = unordered(mx[tid]);
-      stat[(size_t)(draft ? nb_cap : blk) * R + tid] = make_float2(64.f * rintf(fminf(fmaxf(m, -1e30f), 1e30f) * (1.f / 64.f)), l);
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          const int r = t0 + g + 8 * (x >> 1);
+          const bool on = draft ? r < n && ((mask[min(8 * nt + 2 * c + (x & 1), n - 1)] >> (r & 63)) & 1) : r < len;
+          if (!on) s[nt][x] = -INFINITY;
+        }
+    }
+    // ---- arguments relative to the references; does one have to move?  (always in the first block: -inf)
+    bool moves = false;
+    float y[NT][4];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      const float4 v = *reinterpret_cast<const float4*>(sr + 8 * nt + 2 * c);
+      const float s0 = v.x * back, s1 = v.z * back;
+      y[nt][0] = fmaf(s[nt][0], s0, -v.y); y[nt][1] = fmaf(s[nt][1], s1, -v.w);
+      y[nt][2] = fmaf(s[nt][2], s0, -v.y); y[nt][3] = fmaf(s[nt][3], s1, -v.w);
+      moves = moves || fmaxf(fmaxf(y[nt][0], y[nt][1]), fmaxf(y[nt][2], y[nt][3])) > 60.f;
+    }
+    if (half_any(half, moves)) {                                          // (the barrier also: everyone is done with qf and pt)
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int z = 0; z < 2; ++z) {
+          float m = fmaxf(s[nt][z], s[nt][2 + z]) * (sr[8 * nt + 2 * c + z].x * back);
+#pragma unroll
+          for (int o = 4; o < 32; o <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+          if (g == 0) atomicMax(smax + 8 * nt + 2 * c + z, ordered(m));
+        }
+      half_sync(half);
+      if (htid < TOK) {
+        const float m = unordered(smax[htid]);                            // (of the blocks that came here)
+        if (m > sr[htid].y + 60.f) sr[htid].y = 64.f * rintf(fminf(m, 1e30f) * (1.f / 64.f));
+      }
+      half_sync(half);
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        const float4 v = *reinterpret_cast<const float4*>(sr + 8 * nt + 2 * c);
+        const float s0 = v.x * back, s1 = v.z * back;
+        y[nt][0] = fmaf(s[nt][0], s0, -v.y); y[nt][1] = fmaf(s[nt][1], s1, -v.w);
+        y[nt][2] = fmaf(s[nt][2], s0, -v.y); y[nt][3] = fmaf(s[nt][3], s1, -v.w);
+      }
+    }
+    // ---- probabilities; the next block's query fragments
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+      stmatrix_x2_trans(pt_addr + (uint32_t)(nt * 8 * S::PLD) * 2, bf162_of(ex2_approx(y[nt][0]), ex2_approx(y[nt][1])),
+                        bf162_of(ex2_approx(y[nt][2]), ex2_approx(y[nt][3])));
+    if (it + 1 < total) fragments(bc);
+    if (it + 2 < total) bc = block_angle(it + 2);
+    half_sync(half);
+    // ---- P tile out, 16 bytes a thread, and the rows' sums
+    const int col = draft ? t.s_draft : blk * SC_KEYS;
+    __nv_bfloat16* Pout = t.p + ((size_t)b * R + (size_t)h * n) * t.p_ld + col;
+    float2* stat = t.stat + ((size_t)b * (nb_cap + 1) + (draft ? nb_cap : blk)) * R + h * n;
+    for (int e = htid; e < (n + 1) / 2 * 32; e += SC_HALF) {              // 16 lanes a token (a warp is whole or idle)
+      const int i = e >> 4, x = e & 15;
+      const uint4 v = *reinterpret_cast<const uint4*>(pt + i * S::PLD + 8 * x);
+      if (i < n && (!draft || x < 8)) *reinterpret_cast<uint4*>(Pout + (size_t)i * t.p_ld + 8 * x) = v;
+      float l = sum2(add2(add2(unpack2(v.x), unpack2(v.y)), add2(unpack2(v.z), unpack2(v.w))));
+#pragma unroll
+      for (int o = 1; o < 16; o <<= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
+      if (x == 0 && i < n) stat[i] = make_float2(sr[i].y, l);
     }
   }
 }
@@ -327,7 +447,8 @@ __global__ void __launch_bounds__(1024) slim_tree_finish_kernel(const SlimDecode
   if (M != -INFINITY)
     for (int k = 0; k < 32; ++k) L += s_l[k][x] == 0.f ? 0.f : s_l[k][x] * exp2f(s_m[k][x] - M);
   if (row >= R) return;
-  if (y == 0) t.inv_l[(size_t)b * R + row] = L != 0.f ? 1.f / L : 0.f;
+  const bool there = t.depth[(size_t)b * t.n + row % t.n] >= 0;
+  if (y == 0) t.inv_l[(size_t)b * R + row] = there && L != 0.f ? 1.f / L : 0.f;
   for (int k = y; k <= nblk; k += 32) {
     const float2 v = stat[(size_t)(k == nblk ? nb_cap : k) * R];
     if (v.y == 0.f || v.x == M) continue;
@@ -656,7 +777,7 @@ slim_tree_u_kernel(const __grid_constant__ CUtensorMap pmap, const __grid_consta
 #pragma unroll
                 for (int y = 0; y < 4; ++y) {
                   const __nv_bfloat162 z = __floats2bfloat162_rn(__uint_as_float(v[x + 2 * y]) * il, __uint_as_float(v[x + 2 * y + 1]) * il);
-                  ow[y] = *reinterpret_cast<const uint32_t*>(&z);
+                  ow[y] = il != 0.f ? *reinterpret_cast<const uint32_t*>(&z) : 0u;      // (an empty row is 0 whatever the keys hold)
                 }
                 *reinterpret_cast<uint4*>(out + c0 + x) = o4;
               }
@@ -742,6 +863,7 @@ __global__ void __launch_bounds__(256) slim_tree_join_kernel(const SlimDecodePar
       a.x += v.x; a.y += v.y; a.z += v.z; a.w += v.w;
     }
     const float il = t.inv_l[(size_t)b * R + r];
+    if (il == 0.f) a = make_float4(0.f, 0.f, 0.f, 0.f);    // (an empty row is 0 whatever the keys hold)
     const int h = r / t.n, tok = r - h * t.n;
     const __nv_bfloat162 o0 = __floats2bfloat162_rn(a.x * il, a.y * il), o1 = __floats2bfloat162_rn(a.z * il, a.w * il);
     *reinterpret_cast<uint2*>(t.uh + (((size_t)h * p.batch + b) * t.n + tok) * p.d + col0 + c) =
@@ -874,26 +996,33 @@ __global__ void __launch_bounds__(128) slim_tree_out_kernel(const __grid_constan
 }
 
 template <int DK, int NT, bool ROPE>
-cudaError_t launch_p(const slim_ctx* ctx, const SlimDecodeParams& p, const SlimTreeView& t, cudaStream_t st) {
+cudaError_t launch_p(const slim_ctx* ctx, const CUtensorMap& cmap, const CUtensorMap& dmap, const SlimDecodeParams& p, const SlimTreeView& t,
+                     cudaStream_t st) {
   constexpr size_t smem = ScoreShape<DK, NT>::SMEM;
+  static_assert(smem <= 227 * 1024, "shared memory of an SM");
   auto kern = slim_tree_p_kernel<DK, NT, ROPE>;
   cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
   if (e != cudaSuccess) return e;
   const int nblk = (p.t_cap + SC_KEYS - 1) / SC_KEYS, rows = p.H * p.batch;
-  int gx = (8 * ctx->num_sms + rows - 1) / rows;           // about eight CTAs an SM over the launch: each builds its tables once
-  if (gx > nblk) gx = nblk;
-  return slim_launch_pdl(kern, dim3(gx, p.H, p.batch), dim3(SC_THREADS), smem, st, p, t);
-}
-template <int DK, int NT>
-cudaError_t launch_p_rope(const slim_ctx* ctx, const SlimDecodeParams& p, const SlimTreeView& t, cudaStream_t st) {
-  return p.rope ? launch_p<DK, NT, true>(ctx, p, t, st) : launch_p<DK, NT, false>(ctx, p, t, st);
+  int gx = (8 * ctx->num_sms + rows - 1) / rows;           // about eight CTAs an SM over the launch: each loads its tables once
+  if (gx > (nblk + 1) / 2) gx = (nblk + 1) / 2;
+  return slim_launch_pdl(kern, dim3(gx, p.H, p.batch), dim3(SC_THREADS), smem, st, cmap, dmap, p, t,
+                         reinterpret_cast<const float4*>(ctx->rope_frag));
 }
 template <int DK>
-cudaError_t launch_p_tokens(const slim_ctx* ctx, const SlimDecodeParams& p, const SlimTreeView& t, cudaStream_t st) {
-  if (t.n <= 8) return launch_p_rope<DK, 1>(ctx, p, t, st);
-  if (t.n <= 16) return launch_p_rope<DK, 2>(ctx, p, t, st);
-  if (t.n <= 32) return launch_p_rope<DK, 4>(ctx, p, t, st);
-  return launch_p_rope<DK, 8>(ctx, p, t, st);
+cudaError_t launch_p_tokens(const slim_ctx* ctx, const SlimDecodeParams& p, const SlimTreeView& t, long long total_rows, cudaStream_t st) {
+  CUtensorMap map[2];                                      // cached rows, drafted keys: a warp's tile of 16 rows of one head
+  for (int k = 0; k < 2; ++k) {
+    const unsigned long long rows = k ? (unsigned long long)p.batch * t.n : (unsigned long long)total_rows;
+    const unsigned long long dims[3] = {DK == 96 ? (unsigned long long)p.d : 64ull, rows, DK == 96 ? 1ull : (unsigned long long)(p.d / 64)};
+    const unsigned long long str[2] = {2ull * p.d, DK == 96 ? 2ull * p.d * rows : 128ull};
+    const unsigned int box[3] = {DK == 96 ? 96u : 64u, 16, DK == 128 ? 2u : 1u};
+    cudaError_t e = slim_tmap_encode_3d(&map[k], k ? const_cast<void*>(t.k_tree) : const_cast<void*>(p.k), dims, str, box, DK != 96);
+    if (e != cudaSuccess) return e;
+  }
+#define SLIM_P(NT) (p.rope ? launch_p<DK, NT, true>(ctx, map[0], map[1], p, t, st) : launch_p<DK, NT, false>(ctx, map[0], map[1], p, t, st))
+  return t.n <= 8 ? SLIM_P(1) : t.n <= 16 ? SLIM_P(2) : t.n <= 32 ? SLIM_P(4) : SLIM_P(8);
+#undef SLIM_P
 }
 
 template <int MT>
@@ -909,6 +1038,24 @@ cudaError_t launch_u(const slim_ctx* ctx, const SlimDecodeParams& p, const SlimT
 inline size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
 }  // namespace
+
+// (cos, sin) of the key offsets 0 .. 127 in the order the score kernel's lanes read them.
+cudaError_t slim_tree_make_table(slim_ctx* ctx) {
+  const int half = ctx->d_k / 2, vw = ctx->d_k == 96 ? 4 : 8, npc = half / (4 * vw);
+  const size_t n = (size_t)SC_KEYS * half / 2;
+  float4* host = static_cast<float4*>(malloc(sizeof(float4) * n));
+  if (!host) return cudaErrorMemoryAllocation;
+  for (size_t e = 0; e < n; ++e) {
+    const int ln = e & 31, xq = (int)(e >> 5) % (vw / 2), rest = (int)(e >> 5) / (vw / 2), pc = rest % npc, rh = rest / npc % 2, w = rest / npc / 2;
+    const int o = 16 * w + 8 * rh + (ln >> 2), j = chunk_of(ctx->d_k, ln & 3, pc) * vw + 2 * xq;
+    const double a = o * std::pow(ctx->rope_theta, -2.0 * j / ctx->d_k), z = o * std::pow(ctx->rope_theta, -2.0 * (j + 1) / ctx->d_k);
+    host[e] = make_float4((float)std::cos(a), (float)std::cos(z), (float)std::sin(a), (float)std::sin(z));
+  }
+  cudaError_t e = cudaMalloc(&ctx->rope_frag, sizeof(float4) * n);
+  if (e == cudaSuccess) e = cudaMemcpy(ctx->rope_frag, host, sizeof(float4) * n, cudaMemcpyHostToDevice);
+  free(host);
+  return e;
+}
 
 int slim_tree_tc_ok(const slim_ctx* ctx) {
   return ctx->proj_ok && ctx->kdtype == SLIM_BF16 && ctx->e == ctx->d && ctx->d % 64 == 0;
@@ -972,7 +1119,8 @@ cudaError_t slim_launch_tree_tc(const slim_ctx* ctx, const SlimDecodeParams& p, 
   }
   e = slim_launch_pdl(slim_tree_tail_kernel, dim3(16, p.batch), dim3(256), 0, st, p, t);
   if (e != cudaSuccess) return e;
-  e = dk == 64 ? launch_p_tokens<64>(ctx, p, t, st) : dk == 96 ? launch_p_tokens<96>(ctx, p, t, st) : launch_p_tokens<128>(ctx, p, t, st);
+  e = dk == 64 ? launch_p_tokens<64>(ctx, p, t, total_rows, st) : dk == 96 ? launch_p_tokens<96>(ctx, p, t, total_rows, st)
+                                                                          : launch_p_tokens<128>(ctx, p, t, total_rows, st);
   if (e != cudaSuccess) return e;
   e = slim_launch_pdl(slim_tree_finish_kernel, dim3((R + 31) / 32, p.batch), dim3(1024), 0, st, p, t);
   if (e != cudaSuccess) return e;
