@@ -50,8 +50,8 @@ __global__ void __launch_bounds__(256) slim_tree_tail_kernel(const SlimDecodePar
 }
 
 // ------------------------------------------------------------------------------------------------ scores
-// A CTA takes one (sequence, head); its two halves of eight warps share the tables and take every other block of 128
-// keys each, with barriers of their own, so that one computes while the other waits.  Warp w of a half has keys
+// A CTA takes one (sequence, head); its groups of eight warps share the tables and take the blocks of 128 keys in
+// turn, with barriers of their own, so that one computes while the others wait.  Warp w of a group has keys
 // 16 w .. 16 w + 15 of a block, rows g and g + 8 of m16n8k16 float16 tiles in each thread, and the tokens as the tiles'
 // columns; its key tile comes by TMA into a buffer of its own, which nobody else reads.
 //   - The contraction runs over rotation pairs: step (pc, x) puts the low elements of pairs j, j + 1 into the k-slots 2 c,
@@ -69,28 +69,29 @@ __global__ void __launch_bounds__(256) slim_tree_tail_kernel(const SlimDecodePar
 //     stay below reference + 60: nearly always the same for all blocks of a row, so that the blocks need no common
 //     maximum; `finish` shifts the exponents of the others, exactly.  Sums l are taken from the rounded P, so the weights
 //     of a row add up to one.
-constexpr int SC_KEYS = 128, SC_HALF = 256, SC_THREADS = 2 * SC_HALF, SC_WARPS = SC_THREADS / 32;
+constexpr int SC_KEYS = 128, SC_GROUP = 256;
 
 template <int DK, int NT>
 struct ScoreShape {
   static constexpr int HALF = DK / 2, VW = DK == 96 ? 4 : 8, NPC = HALF / (4 * VW), STEPS = HALF / 8, PER = STEPS * 32;
-  static constexpr bool QHALF = NT > 4;                                  // kept as float16 pairs (room; a second rounding to 11 bits)
-  static constexpr int KT = 16 * DK * 2, KS = NT <= 2 ? 2 : 1;           // bytes of a warp's key tile, buffers
-  static constexpr size_t KR = (size_t)SC_WARPS * KS * KT, CS = (size_t)SC_KEYS * HALF * 8, QF = (size_t)NT * PER * 8;
+  // a thread's (cos, sin) live in registers where they fit beside the sums (up to 16 tokens), else in shared memory
+  static constexpr bool CSR = NT <= 2, QHALF = NT > 4;                   // QHALF: queries as float16 pairs (room; a second rounding to 11 bits)
+  static constexpr int GROUPS = 2, THREADS = GROUPS * SC_GROUP, WARPS = THREADS / 32;
+  static constexpr int KT = 16 * DK * 2, KS = CSR ? 2 : 1;               // bytes of a warp's key tile, buffers
+  static constexpr size_t KR = (size_t)WARPS * KS * KT, CS = CSR ? 0 : (size_t)SC_KEYS * HALF * 8, QF = (size_t)NT * PER * 8;
   static constexpr size_t QS = (size_t)8 * NT * HALF * (QHALF ? 4 : 8);
-  static constexpr int PLD = SC_KEYS + 8;                                // bf16 per token row of the P tile
-  static constexpr size_t PT = (size_t)8 * NT * PLD * 2, SR = (size_t)8 * NT * 8, MX = (size_t)8 * NT * 4;
-  static constexpr size_t OWN = QF + PT + SR + MX;                       // of a half
-  static constexpr size_t SMEM = 1024 + KR + CS + QS + 2 * OWN + 8 * SC_WARPS * KS + 16;
+  static constexpr size_t SR = (size_t)8 * NT * 8, MX = (size_t)8 * NT * 4, WS = (size_t)8 * NT * 8 * 4;
+  static constexpr size_t OWN = 2 * QF + SR + MX + 2 * WS;               // of a group
+  static constexpr size_t SMEM = 1024 + KR + CS + QS + GROUPS * OWN + 8 * (WARPS * KS + 1) + 16;
 };
 // which VW pairs of a head lane c takes in turn pc; for d_k = 128 even and odd key rows then meet different banks
 __host__ __device__ constexpr int chunk_of(int dk, int c, int pc) { return dk == 128 ? 2 * c + pc : c + 4 * pc; }
-// where a thread's VW low (hl = 0) or high elements lie in a warp's key tile of 16 rows (r % 8 = g): two 64-column
-// atoms with 128-byte swizzle, one of them, or plain rows
+// where a thread's VW low (hl = 0) or high elements of key r lie in a warp's tile of 16 keys: two 64-column atoms with
+// 128-byte swizzle, one of them, or plain rows
 template <int DK>
-__device__ __forceinline__ uint32_t tile_off(int r, int g, int c, int pc, int hl) {
-  if (DK == 128) return (uint32_t)(hl * 2048 + r * 128 + (((2 * c + pc) ^ g) << 4));
-  if (DK == 64) return (uint32_t)(r * 128 + (((c + 4 * hl) ^ g) << 4));
+__device__ __forceinline__ uint32_t tile_off(int r, int c, int pc, int hl) {
+  if (DK == 128) return (uint32_t)(hl * 2048 + r * 128 + (((2 * c + pc) ^ (r & 7)) << 4));
+  if (DK == 64) return (uint32_t)(r * 128 + (((c + 4 * hl) ^ (r & 7)) << 4));
   return (uint32_t)(r * 192 + hl * 96 + (c + 4 * pc) * 8);
 }
 
@@ -112,8 +113,10 @@ __device__ __forceinline__ void mma_f16(float (&c)[4], const uint32_t (&a)[4], u
   asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-__device__ __forceinline__ void stmatrix_x2_trans(uint32_t addr, uint32_t a, uint32_t b) {
-  asm volatile("stmatrix.sync.aligned.m8n8.x2.trans.shared.b16 [%0], {%1, %2};" ::"r"(addr), "r"(a), "r"(b) : "memory");
+__device__ __forceinline__ uint32_t movmatrix_trans(uint32_t a) {
+  uint32_t d;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(a));
+  return d;
 }
 __device__ __forceinline__ int ordered(float f) { const int i = __float_as_int(f); return i ^ ((i >> 31) & 0x7fffffff); }
 __device__ __forceinline__ float unordered(int i) { return __int_as_float(i ^ ((i >> 31) & 0x7fffffff)); }
@@ -124,17 +127,17 @@ __device__ __forceinline__ float pow2_to(float x, int top) {
   return __int_as_float((min(max(e, -120), 120) + 127) << 23);
 }
 
-// barriers of one half
-__device__ __forceinline__ void half_sync(int half) { asm volatile("barrier.cta.sync %0, %1;" ::"r"(1 + half), "n"(SC_HALF) : "memory"); }
-__device__ __forceinline__ bool half_any(int half, bool v) {
+// barriers of one group
+__device__ __forceinline__ void group_sync(int group) { asm volatile("barrier.cta.sync %0, %1;" ::"r"(1 + group), "n"(SC_GROUP) : "memory"); }
+__device__ __forceinline__ bool group_any(int group, bool v) {
   int r;
   asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %1, 0;\n\tbarrier.cta.red.or.pred q, %2, %3, p;\n\tselp.b32 %0, 1, 0, q;\n\t}"
-               : "=r"(r) : "r"((int)v), "r"(1 + half), "n"(SC_HALF) : "memory");
+               : "=r"(r) : "r"((int)v), "r"(1 + group), "n"(SC_GROUP) : "memory");
   return r != 0;
 }
 
 template <int DK, int NT, bool ROPE>
-__global__ void __launch_bounds__(SC_THREADS, 1)
+__global__ void __launch_bounds__((ScoreShape<DK, NT>::THREADS), 1)
 slim_tree_p_kernel(const __grid_constant__ CUtensorMap cmap, const __grid_constant__ CUtensorMap dmap, const SlimDecodeParams p,
                    const SlimTreeView t, const float4* __restrict__ table) {
   typedef ScoreShape<DK, NT> S;
@@ -143,39 +146,40 @@ slim_tree_p_kernel(const __grid_constant__ CUtensorMap cmap, const __grid_consta
   extern __shared__ unsigned char smem_raw[];
   unsigned char* sm = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, c = lane & 3;
-  const int half = warp >> 3, hw = warp & 7, htid = tid & (SC_HALF - 1);
+  const int group = warp >> 3, hw = warp & 7, htid = tid & (SC_GROUP - 1);
   unsigned char* ring = sm + (size_t)warp * S::KS * S::KT;                // this warp's key tiles
   float4* cst = reinterpret_cast<float4*>(sm + S::KR);                    // [warp][row half][pc][VW / 2][lane] (cos, cos, sin, sin)
   unsigned char* qs = sm + S::KR + S::CS;                                 // [NT][STEPS][lane][2] the turned queries' pairs
-  unsigned char* own = sm + S::KR + S::CS + S::QS + half * S::OWN;
-  uint2* qf = reinterpret_cast<uint2*>(own);                              // [NT][STEPS][lane]
-  __nv_bfloat16* pt = reinterpret_cast<__nv_bfloat16*>(own + S::QF);      // [TOK][PLD]
-  float2* sr = reinterpret_cast<float2*>(own + S::QF + S::PT);            // [TOK] (what a token's sums are multiplied by, its reference)
-  int* smax = reinterpret_cast<int*>(own + S::QF + S::PT + S::SR);        // [TOK] largest argument, where a reference has to move
-  unsigned char* tail = sm + S::KR + S::CS + S::QS + 2 * S::OWN;
-  const uint32_t bar = smem_u32(tail) + 8u * (uint32_t)(warp * S::KS);    // this warp's barriers
-  volatile int* s_abort = reinterpret_cast<volatile int*>(tail + 8 * SC_WARPS * S::KS);
+  unsigned char* own = sm + S::KR + S::CS + S::QS + group * S::OWN;
+  uint2* qf = reinterpret_cast<uint2*>(own);                              // [2][NT][STEPS][lane]
+  float2* sr = reinterpret_cast<float2*>(own + 2 * S::QF);                // [TOK] (what a token's sums are multiplied by, its reference)
+  int* smax = reinterpret_cast<int*>(own + 2 * S::QF + S::SR);            // [TOK] largest argument, where a reference has to move
+  float* wsum = reinterpret_cast<float*>(own + 2 * S::QF + S::SR + S::MX);        // [2][warp][TOK] sums of a block's rows
+  unsigned char* tail = sm + S::KR + S::CS + S::QS + S::GROUPS * S::OWN;
+  const uint32_t bar_table = smem_u32(tail), bar = bar_table + 8u * (uint32_t)(1 + warp * S::KS);      // this warp's barriers
+  volatile int* s_abort = reinterpret_cast<volatile int*>(tail + 8 * (S::WARPS * S::KS + 1));
   const int b = blockIdx.z, h = blockIdx.y, n = t.n, R = p.H * n;
 
   if (lane == 0) {
     for (int i = 0; i < S::KS; ++i) mbar_init(bar + 8 * i, 1);
-    if (warp == 0) { prefetch_tensormap(&cmap); prefetch_tensormap(&dmap); *s_abort = 0; }
+    if (warp == 0) { mbar_init(bar_table, 1); prefetch_tensormap(&cmap); prefetch_tensormap(&dmap); *s_abort = 0; }
     fence_mbar_init();
   }
-  if (ROPE)                                                               // (a table of the context: no need to wait for it)
-    for (int e = tid; e < SC_KEYS * HALF / 2; e += SC_THREADS) cst[e] = __ldg(table + e);
+  if (ROPE && !S::CSR && tid == 0) {                                               // (a table of the context: no need to wait for it)
+    mbar_arrive_expect_tx(bar_table, (uint32_t)S::CS);
+    bulk_load(smem_u32(cst), table, (uint32_t)S::CS, bar_table);
+  }
   slim_pdl_trigger();
   slim_pdl_wait();
   const int len = t.len[b], nblk = (len + SC_KEYS - 1) / SC_KEYS, nb_cap = (p.t_cap + SC_KEYS - 1) / SC_KEYS;
-  // the draft block comes last, in the first half of the CTAs of column 0
-  const int first = 2 * blockIdx.x + half, step = 2 * gridDim.x;
-  if (2 * (int)blockIdx.x >= nblk && blockIdx.x != 0) return;             // (both halves)
+  // the draft block comes last, in the first group of the CTAs of column 0
+  const int first = S::GROUPS * blockIdx.x + group, step = S::GROUPS * gridDim.x;
   const int mine = nblk > first ? (nblk - 1 - first) / step + 1 : 0;
   const int total = mine + (first == 0 ? 1 : 0);
   const int* dep = t.depth + (size_t)b * n;
 
   // this thread's part of the query fragments: pairs j0, j0 + 1 of token 8 nt + lane / 4, for nt = nt0, nt0 + NTS, ..
-  constexpr int NTS = SC_HALF / S::PER;
+  constexpr int NTS = SC_GROUP / S::PER;
   const int nt0 = htid / S::PER, fi = htid % S::PER, fs = fi >> 5, j0 = chunk_of(DK, fi & 3, fs / (VW / 2)) * VW + 2 * (fs % (VW / 2));
   auto fetch = [&](int it) {                                              // (lane 0) rows that are not there are masked later
     const bool draft = it == mine;
@@ -195,7 +199,7 @@ slim_tree_p_kernel(const __grid_constant__ CUtensorMap cmap, const __grid_consta
     }
     return __ldg(reinterpret_cast<const float4*>(p.rope_base + (size_t)(first + it * step) * (SC_KEYS / SLIM_TT) * HALF + j0));
   };
-  auto fragments = [&](const float4& bc) {                                // queries turned back by the block's angle
+  auto fragments = [&](const float4& bc, int buf) {                       // queries turned back by the block's angle
     if (nt0 < NTS) {
 #pragma unroll
       for (int nt = nt0; nt < NT; nt += NTS) {
@@ -205,7 +209,7 @@ slim_tree_p_kernel(const __grid_constant__ CUtensorMap cmap, const __grid_consta
           const float2 u = __half22float2(*reinterpret_cast<const __half2*>(&w.x)), v = __half22float2(*reinterpret_cast<const __half2*>(&w.y));
           q = make_float4(u.x, u.y, v.x, v.y);
         } else q = reinterpret_cast<const float4*>(qs)[nt * S::PER + fi];
-        qf[nt * S::PER + fi] = make_uint2(half2_of(pack2(q.x * bc.x - q.y * bc.y, q.z * bc.z - q.w * bc.w)),
+        qf[(buf * NT + nt) * S::PER + fi] = make_uint2(half2_of(pack2(q.x * bc.x - q.y * bc.y, q.z * bc.z - q.w * bc.w)),
                                           half2_of(pack2(q.y * bc.x + q.x * bc.y, q.w * bc.z + q.z * bc.w)));
       }
     }
@@ -220,7 +224,7 @@ slim_tree_p_kernel(const __grid_constant__ CUtensorMap cmap, const __grid_consta
   bool large = false;
   {
     const __nv_bfloat16* Q = reinterpret_cast<const __nv_bfloat16*>(p.q) + (size_t)b * n * p.d + h * DK;
-    for (int i = warp; i < TOK; i += SC_WARPS) {
+    for (int i = warp; i < TOK; i += S::WARPS) {
       const bool there = i < n && dep[i] >= 0;
       float2 v[(HALF + 31) / 32];
       float top = 0.f;
@@ -248,8 +252,8 @@ slim_tree_p_kernel(const __grid_constant__ CUtensorMap cmap, const __grid_consta
           if (S::QHALF) reinterpret_cast<uint32_t*>(qs)[at] = half2_of(pack2(v[x].x * sc, v[x].y * sc));
           else reinterpret_cast<float2*>(qs)[at] = make_float2(v[x].x * sc, v[x].y * sc);
         }
-      if (lane < 2) {                                                     // both halves' copies; a token that is not there: P = 2^(s - inf) = 0
-        unsigned char* o = sm + S::KR + S::CS + S::QS + lane * S::OWN + S::QF + S::PT;
+      if (lane < S::GROUPS) {                                             // every group's copy; a token that is not there: P = 2^(s - inf) = 0
+        unsigned char* o = sm + S::KR + S::CS + S::QS + lane * S::OWN + 2 * S::QF;
         reinterpret_cast<float2*>(o)[i] = make_float2(1.f / sc, there ? -INFINITY : INFINITY);
         reinterpret_cast<int*>(o + S::SR)[i] = ordered(-INFINITY);
       }
@@ -258,24 +262,47 @@ slim_tree_p_kernel(const __grid_constant__ CUtensorMap cmap, const __grid_consta
     }
   }
   const bool careful = __syncthreads_or(large);
-  const uint32_t pt_addr = smem_u32(pt) + (uint32_t)((lane & 7) * S::PLD + 16 * hw + 8 * ((lane >> 3) & 1)) * 2;
-  if (total > 0) fragments(bc);
+  // MMA rows g and g + 8 are keys key0 and key0 + 2 of the warp's tile: turned around, a thread then holds four
+  // neighbouring keys of a token
+  const int key0 = 4 * (g >> 1) + (g & 1);
+  constexpr int NCS = S::CSR && ROPE ? NPC * (VW / 2) : 1;
+  ulonglong2 csr[2][NCS];                                                 // (cos, cos), (sin, sin) of this thread's keys and pairs
+  auto angles = [&](int rh, int o) {                                      // of key offset o
+#pragma unroll
+    for (int x = 0; x < NCS; ++x) csr[rh][x] = __ldg(reinterpret_cast<const ulonglong2*>(table) + ((o >> 3) * NCS + x) * 32 + ((o & 7) << 2) + c);
+  };
+  if (S::CSR && ROPE) { angles(0, 16 * hw + key0); angles(1, 16 * hw + key0 + 2); }
+  if (ROPE && !S::CSR) mbar_wait<false>(bar_table, 0, s_abort, p.status);
+  if (total > 0) fragments(bc, 0);
   if (total > 1) bc = block_angle(1);
-  half_sync(half);
+  group_sync(group);
+  // sums and references of block `it`, once all warps have left theirs
+  auto stats = [&](int it) {
+    if (htid < n) {
+      float l = 0.f;
+#pragma unroll
+      for (int w = 0; w < 8; ++w) l += wsum[((it & 1) * 8 + w) * TOK + htid];
+      t.stat[((size_t)b * (nb_cap + 1) + (it == mine ? nb_cap : first + it * step)) * R + h * n + htid] = make_float2(sr[htid].y, l);
+    }
+  };
 
   for (int it = 0; it < total; ++it) {
     const bool draft = it == mine;
     const int blk = first + it * step, t0 = draft ? 16 * hw : blk * SC_KEYS + 16 * hw;
     // ---- scores
-    // a thread's rows of the table: its keys' offsets in the block; a drafted key's offset is its depth
+    // a drafted key's offset in its block is its depth
     const ulonglong2* row_cs[2];
+    if (ROPE) {
 #pragma unroll
-    for (int rh = 0; rh < 2; ++rh) {
-      int o = 16 * hw + 8 * rh + g;
-      if (draft) o = o < n ? max(dep[o], 0) : 0;
-      row_cs[rh] = reinterpret_cast<const ulonglong2*>(cst) + (o >> 3) * (NPC * (VW / 2) * 32) + ((o & 7) << 2) + c;
+      for (int rh = 0; rh < 2; ++rh) {
+        int o = 16 * hw + key0 + 2 * rh;
+        if (draft) o = o < n ? max(dep[o], 0) : 0;
+        if (S::CSR) { if (draft) angles(rh, o); }
+        else row_cs[rh] = reinterpret_cast<const ulonglong2*>(cst) + (o >> 3) * (NPC * (VW / 2) * 32) + ((o & 7) << 2) + c;
+      }
     }
     unsigned char* tile = ring + (it % S::KS) * S::KT;
+    const uint2* qb = qf + (it & 1) * NT * S::PER;
     mbar_wait<false>(bar + 8 * (it % S::KS), (it / S::KS) & 1, s_abort, p.status);      // (gave up: reported, and the loop runs on to its end)
     float s[NT][4];
     float back = 1.f;                                                     // undoes the keys' scaling
@@ -288,7 +315,7 @@ slim_tree_p_kernel(const __grid_constant__ CUtensorMap cmap, const __grid_consta
 #pragma unroll
         for (int rh = 0; rh < 2; ++rh)
 #pragma unroll
-          for (int hl = 0; hl < 2; ++hl) k[rh][hl] = *reinterpret_cast<const kvec*>(tile + tile_off<DK>(g + 8 * rh, g, c, pc, hl));
+          for (int hl = 0; hl < 2; ++hl) k[rh][hl] = *reinterpret_cast<const kvec*>(tile + tile_off<DK>(key0 + 2 * rh, c, pc, hl));
 #pragma unroll
         for (int xq = 0; xq < VW / 2; ++xq) {
           uint32_t a[4];
@@ -296,7 +323,7 @@ slim_tree_p_kernel(const __grid_constant__ CUtensorMap cmap, const __grid_consta
           for (int rh = 0; rh < 2; ++rh) {
             const f32x2 k1 = unpack2(word(k[rh][0], xq)), k2 = unpack2(word(k[rh][1], xq));
             if (ROPE) {
-              const ulonglong2 cs = row_cs[rh][(pc * (VW / 2) + xq) * 32];
+              const ulonglong2 cs = S::CSR ? csr[rh][(pc * (VW / 2) + xq) % NCS] : row_cs[rh][(pc * (VW / 2) + xq) * 32];
               a[rh] = half2_of(fma2(k2, cs.y, mul2(k1, cs.x)));
               a[2 + rh] = half2_of(sub2(mul2(k2, cs.x), mul2(k1, cs.y)));
             } else {
@@ -306,7 +333,7 @@ slim_tree_p_kernel(const __grid_constant__ CUtensorMap cmap, const __grid_consta
           }
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt) {
-            const uint2 f = qf[nt * S::PER + (pc * (VW / 2) + xq) * 32 + lane];
+            const uint2 f = qb[nt * S::PER + (pc * (VW / 2) + xq) * 32 + lane];
             mma_f16(s[nt], a, f.x, f.y);
           }
         }
@@ -327,7 +354,7 @@ slim_tree_p_kernel(const __grid_constant__ CUtensorMap cmap, const __grid_consta
           for (int pc = 0; pc < NPC; ++pc)
 #pragma unroll
             for (int hl = 0; hl < 2; ++hl) {
-              kvec* at = reinterpret_cast<kvec*>(tile + tile_off<DK>(g + 8 * rh, g, c, pc, hl));
+              kvec* at = reinterpret_cast<kvec*>(tile + tile_off<DK>(key0 + 2 * rh, c, pc, hl));
               kvec v = *at;
 #pragma unroll
               for (int x = 0; x < VW / 2; ++x) {
@@ -356,7 +383,7 @@ slim_tree_p_kernel(const __grid_constant__ CUtensorMap cmap, const __grid_consta
       for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
         for (int x = 0; x < 4; ++x) {
-          const int r = t0 + g + 8 * (x >> 1);
+          const int r = t0 + key0 + (x & 2);
           const bool on = draft ? r < n && ((mask[min(8 * nt + 2 * c + (x & 1), n - 1)] >> (r & 63)) & 1) : r < len;
           if (!on) s[nt][x] = -INFINITY;
         }
@@ -372,7 +399,11 @@ slim_tree_p_kernel(const __grid_constant__ CUtensorMap cmap, const __grid_consta
       y[nt][2] = fmaf(s[nt][2], s0, -v.y); y[nt][3] = fmaf(s[nt][3], s1, -v.w);
       moves = moves || fmaxf(fmaxf(y[nt][0], y[nt][1]), fmaxf(y[nt][2], y[nt][3])) > 60.f;
     }
-    if (half_any(half, moves)) {                                          // (the barrier also: everyone is done with qf and pt)
+    if (it + 1 < total) fragments(bc, (it + 1) & 1);
+    if (it + 2 < total) bc = block_angle(it + 2);
+    const bool any_moves = group_any(group, moves);
+    if (it > 0) stats(it - 1);
+    if (any_moves) {
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -382,12 +413,12 @@ slim_tree_p_kernel(const __grid_constant__ CUtensorMap cmap, const __grid_consta
           for (int o = 4; o < 32; o <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
           if (g == 0) atomicMax(smax + 8 * nt + 2 * c + z, ordered(m));
         }
-      half_sync(half);
+      group_sync(group);
       if (htid < TOK) {
         const float m = unordered(smax[htid]);                            // (of the blocks that came here)
         if (m > sr[htid].y + 60.f) sr[htid].y = 64.f * rintf(fminf(m, 1e30f) * (1.f / 64.f));
       }
-      half_sync(half);
+      group_sync(group);
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
         const float4 v = *reinterpret_cast<const float4*>(sr + 8 * nt + 2 * c);
@@ -396,28 +427,23 @@ slim_tree_p_kernel(const __grid_constant__ CUtensorMap cmap, const __grid_consta
         y[nt][2] = fmaf(s[nt][2], s0, -v.y); y[nt][3] = fmaf(s[nt][3], s1, -v.w);
       }
     }
-    // ---- probabilities; the next block's query fragments
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
-      stmatrix_x2_trans(pt_addr + (uint32_t)(nt * 8 * S::PLD) * 2, bf162_of(ex2_approx(y[nt][0]), ex2_approx(y[nt][1])),
-                        bf162_of(ex2_approx(y[nt][2]), ex2_approx(y[nt][3])));
-    if (it + 1 < total) fragments(bc);
-    if (it + 2 < total) bc = block_angle(it + 2);
-    half_sync(half);
-    // ---- P tile out, 16 bytes a thread, and the rows' sums
-    const int col = draft ? t.s_draft : blk * SC_KEYS;
+    // ---- probabilities, turned around to [token][4 keys], out; their sums over this warp's keys
+    const int col = (draft ? t.s_draft : blk * SC_KEYS) + 16 * hw + 4 * c;
     __nv_bfloat16* Pout = t.p + ((size_t)b * R + (size_t)h * n) * t.p_ld + col;
-    float2* stat = t.stat + ((size_t)b * (nb_cap + 1) + (draft ? nb_cap : blk)) * R + h * n;
-    for (int e = htid; e < (n + 1) / 2 * 32; e += SC_HALF) {              // 16 lanes a token (a warp is whole or idle)
-      const int i = e >> 4, x = e & 15;
-      const uint4 v = *reinterpret_cast<const uint4*>(pt + i * S::PLD + 8 * x);
-      if (i < n && (!draft || x < 8)) *reinterpret_cast<uint4*>(Pout + (size_t)i * t.p_ld + 8 * x) = v;
-      float l = sum2(add2(add2(unpack2(v.x), unpack2(v.y)), add2(unpack2(v.z), unpack2(v.w))));
 #pragma unroll
-      for (int o = 1; o < 16; o <<= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
-      if (x == 0 && i < n) stat[i] = make_float2(sr[i].y, l);
+    for (int nt = 0; nt < NT; ++nt) {
+      const uint32_t d0 = movmatrix_trans(bf162_of(ex2_approx(y[nt][0]), ex2_approx(y[nt][1])));
+      const uint32_t d1 = movmatrix_trans(bf162_of(ex2_approx(y[nt][2]), ex2_approx(y[nt][3])));
+      const int i = 8 * nt + g;
+      if (i < n && (!draft || hw < 4)) *reinterpret_cast<uint2*>(Pout + (size_t)i * t.p_ld) = make_uint2(d0, d1);
+      float l = sum2(add2(unpack2(d0), unpack2(d1)));
+      l += __shfl_xor_sync(0xffffffffu, l, 1);
+      l += __shfl_xor_sync(0xffffffffu, l, 2);
+      if (c == 0) wsum[((it & 1) * 8 + hw) * TOK + i] = l;
     }
   }
+  group_sync(group);
+  if (total > 0) stats(total - 1);
 }
 
 // ------------------------------------------------------------------------------------------------ finish
@@ -1004,9 +1030,16 @@ cudaError_t launch_p(const slim_ctx* ctx, const CUtensorMap& cmap, const CUtenso
   cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
   if (e != cudaSuccess) return e;
   const int nblk = (p.t_cap + SC_KEYS - 1) / SC_KEYS, rows = p.H * p.batch;
-  int gx = (8 * ctx->num_sms + rows - 1) / rows;           // about eight CTAs an SM over the launch: each loads its tables once
-  if (gx > (nblk + 1) / 2) gx = (nblk + 1) / 2;
-  return slim_launch_pdl(kern, dim3(gx, p.H, p.batch), dim3(SC_THREADS), smem, st, cmap, dmap, p, t,
+  // CTAs a (sequence, head): the fewest rounds of one CTA per SM, each a set-up of about eight blocks' time and its share
+  // of the blocks
+  constexpr int groups = ScoreShape<DK, NT>::GROUPS;
+  int gx = 1;
+  long long best = -1;
+  for (int x = 1; x <= 64 && x <= (nblk + groups - 1) / groups; ++x) {
+    const long long cost = ((long long)rows * x + ctx->num_sms - 1) / ctx->num_sms * (8 + (nblk + groups * x - 1) / (groups * x));
+    if (best < 0 || cost < best) { best = cost; gx = x; }
+  }
+  return slim_launch_pdl(kern, dim3(gx, p.H, p.batch), dim3(ScoreShape<DK, NT>::THREADS), smem, st, cmap, dmap, p, t,
                          reinterpret_cast<const float4*>(ctx->rope_frag));
 }
 template <int DK>
