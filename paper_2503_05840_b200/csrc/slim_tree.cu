@@ -31,9 +31,8 @@ __global__ void __launch_bounds__(64) slim_tree_layout_kernel(const int32_t* __r
   slim_pdl_trigger();
   slim_pdl_wait();
   if (i < n) {
-    int p = parents[(size_t)b * n + i];
-    if (p >= i) { p = -2; atomicMax(status, (int)SLIM_ERR_TREE); }
-    s_par[i] = p;
+    const int p = parents[(size_t)b * n + i];
+    s_par[i] = p >= i ? -3 : p < -1 ? -2 : p;
   }
   __syncthreads();
   if (i == 0) {
@@ -42,21 +41,11 @@ __global__ void __launch_bounds__(64) slim_tree_layout_kernel(const int32_t* __r
     len_out[b] = len < 0 ? 0 : len;
   }
   if (i < n) {
-    unsigned long long m = 0;
-    int dep = -1, at = i;
-    bool live = s_par[i] >= -1;
-    while (live) {                                   // at most n steps: a parent is an earlier token
-      m |= 1ull << at;
-      ++dep;
-      const int p = s_par[at];
-      if (p == -1) break;
-      if (p < -1) live = false;                      // hangs on padding
-      at = p;
-    }
-    if (!live) {
-      if (s_par[i] >= -1) atomicMax(status, (int)SLIM_ERR_TREE);
-      m = 0; dep = -1;
-    }
+    unsigned long long m;
+    int dep;
+    bool broken;
+    slim_tree_chain(s_par, i, m, dep, broken);
+    if (broken) atomicMax(status, (int)SLIM_ERR_TREE);
     mask[(size_t)b * n + i] = m;
     depth[(size_t)b * n + i] = dep;
   }
@@ -332,18 +321,19 @@ cudaError_t slim_launch_tree(const slim_ctx* ctx, const SlimDecodeParams& p, con
   t.depth = reinterpret_cast<int*>(ws + L.depth);
   t.len = reinterpret_cast<int*>(ws + L.len);
   t.inv_l = reinterpret_cast<float*>(ws + L.inv_l);
-  cudaError_t e = slim_launch_pdl(slim_tree_layout_kernel, dim3(p.batch), dim3(64), 0, st, parents, p.lengths, n, p.t_cap, t.mask,
-                                  t.depth, t.len, p.status);
-  if (e != cudaSuccess) return e;
   if (tc) {
     t.p = reinterpret_cast<__nv_bfloat16*>(ws + L.p); t.p_ld = L.p_ld; t.s_draft = L.p_s_draft;
     t.stat = reinterpret_cast<float2*>(ws + L.stat);
     t.tail = reinterpret_cast<__nv_bfloat16*>(ws + L.tail);
     t.uh = reinterpret_cast<__nv_bfloat16*>(ws + L.uh);
     t.part = reinterpret_cast<float*>(ws + L.part);
+    t.sched = reinterpret_cast<long long*>(ws + L.sched);
     t.g_tiles = L.g_tiles; t.g_ncol = L.g_ncol; t.g_split = L.g_split; t.g_pairs = L.g_pairs; t.g_whole = L.g_whole;
-    return slim_launch_tree_tc(ctx, p, t, L, total_rows, o, st);
+    return slim_launch_tree_tc(ctx, p, t, L, parents, total_rows, o, st);
   }
+  cudaError_t e = slim_launch_pdl(slim_tree_layout_kernel, dim3(p.batch), dim3(64), 0, st, parents, p.lengths, n, p.t_cap, t.mask,
+                                  t.depth, t.len, p.status);
+  if (e != cudaSuccess) return e;
   t.parts = L.parts; t.s_ld = L.s_ld; t.s_draft = L.s_draft;
   t.m = reinterpret_cast<float*>(ws + L.m);
   t.s = reinterpret_cast<float*>(ws + L.s);

@@ -3,7 +3,7 @@
 // One sequence of L rows and n tokens has R = H n rows of probabilities and a weighted sum of R x d numbers (32 MB at
 // n = 64, d = 4096): it cannot stay on chip as the one-token kernel's does, and its products, 2 L R d, are H times
 // those of the scores.  So the step is a chain of kernels around one large matrix product:
-//   layout      the trees' masks and depths; the last, partial block of 64 cached rows and the drafted keys, zero-padded,
+//   tail        the trees' masks and depths; the last, partial block of 64 cached rows and the drafted keys, zero-padded,
 //               in a scratch tail, so that the product only meets whole blocks of 64 finite rows
 //   scores      P = 2^(s - ref) in bf16, [b][h n + i][t], and (ref, sum) per row and block of 128 keys
 //   finish      the row's reference and 1 / l
@@ -27,25 +27,48 @@ __device__ __forceinline__ float2 turn(const SlimDecodeParams& p, int pos, int j
 }
 
 // ------------------------------------------------------------------------------------------------ tail
-// Blocks (x, b): rows 8 x .. 8 x + 7 of sequence b's tail [128][d]: 0..63 the cached rows behind the last whole block of
-// 64, 64..127 the drafted keys; everything else is zero.  Runs after the layout kernel.
-__global__ void __launch_bounds__(256) slim_tree_tail_kernel(const SlimDecodeParams p, const SlimTreeView t) {
+// Block (x, b): rows 2 x, 2 x + 1 of sequence b's tail [128][d]: 0..63 the cached rows behind the last whole block of
+// 64, 64..127 the drafted keys; everything else is zero.  Block 0 also writes the tree's masks and depths.
+__global__ void __launch_bounds__(256) slim_tree_tail_kernel(const SlimDecodeParams p, const SlimTreeView t, const int32_t* __restrict__ parents) {
+  __shared__ int s_par[SLIM_MAX_TREE];
   slim_pdl_trigger();
   slim_pdl_wait();
-  const int b = blockIdx.y, vecs = p.d / 8;
-  const int len = t.len[b], base = len & ~63;
-  for (int rr = 0; rr < 8; ++rr) {
-    const int r = blockIdx.x * 8 + rr;
+  const int b = blockIdx.y, n = t.n, tid = threadIdx.x, vecs = p.d / 8;
+  if (tid < n) {
+    const int q = parents[(size_t)b * n + tid];
+    s_par[tid] = q >= tid ? -3 : q < -1 ? -2 : q;
+  }
+  int len = p.lengths[b];
+  const bool over = len > p.t_cap;
+  len = len < 0 ? 0 : over ? p.t_cap : len;
+  __syncthreads();
+  if (blockIdx.x == 0) {
+    if (tid == 0) { t.len[b] = len; if (over) atomicMax(p.status, (int)SLIM_ERR_CAPACITY); }
+    if (tid < n) {
+      unsigned long long m;
+      int dep;
+      bool broken;
+      slim_tree_chain(s_par, tid, m, dep, broken);
+      if (broken) atomicMax(p.status, (int)SLIM_ERR_TREE);
+      t.mask[(size_t)b * n + tid] = m;
+      t.depth[(size_t)b * n + tid] = dep;
+    }
+  }
+#pragma unroll
+  for (int rr = 0; rr < 2; ++rr) {
+    const int r = blockIdx.x * 2 + rr, row = (len & ~63) + r;
     const uint4* src = nullptr;
     if (r < 64) {
-      const int row = base + r;
-      if (row < len)
-        src = reinterpret_cast<const uint4*>(p.k) + (size_t)(slim_cache_row(p, b, row & ~(SLIM_TT - 1)) + (row & (SLIM_TT - 1))) * vecs;
-    } else if (r - 64 < t.n && t.depth[(size_t)b * t.n + r - 64] >= 0) {
-      src = reinterpret_cast<const uint4*>(t.k_tree) + ((size_t)b * t.n + r - 64) * vecs;
+      if (row < len) src = reinterpret_cast<const uint4*>(p.k) + (size_t)(slim_cache_row(p, b, row & ~(SLIM_TT - 1)) + (row & (SLIM_TT - 1))) * vecs;
+    } else if (r - 64 < n) {
+      unsigned long long m;
+      int dep;
+      bool broken;
+      slim_tree_chain(s_par, r - 64, m, dep, broken);
+      if (dep >= 0) src = reinterpret_cast<const uint4*>(t.k_tree) + ((size_t)b * n + r - 64) * vecs;
     }
     uint4* dst = reinterpret_cast<uint4*>(t.tail) + ((size_t)b * 128 + r) * vecs;
-    for (int e = threadIdx.x; e < vecs; e += 256) dst[e] = src ? __ldg(src + e) : make_uint4(0, 0, 0, 0);
+    for (int e = tid; e < vecs; e += 256) dst[e] = src ? __ldg(src + e) : make_uint4(0, 0, 0, 0);
   }
 }
 
@@ -108,6 +131,11 @@ __device__ __forceinline__ uint32_t half2_of(f32x2 v) {                   // (lo
   return d;
 }
 __device__ __forceinline__ uint32_t bf162_of(float lo, float hi) { uint32_t d; asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo)); return d; }
+// two values as bf16 pairs hi + lo: what the first rounding leaves is kept in a second (16 bits in all)
+__device__ __forceinline__ void split2(float a, float b, uint32_t& hi, uint32_t& lo) {
+  hi = bf162_of(a, b);
+  lo = bf162_of(a - __uint_as_float(hi << 16), b - __uint_as_float(hi & 0xffff0000u));
+}
 __device__ __forceinline__ f32x2 sub2(f32x2 a, f32x2 b) { f32x2 d; asm("sub.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b)); return d; }
 __device__ __forceinline__ void mma_f16(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
   asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
@@ -458,13 +486,24 @@ __global__ void __launch_bounds__(1024) slim_tree_finish_kernel(const SlimDecode
   const int nb_cap = (p.t_cap + SC_KEYS - 1) / SC_KEYS, nblk = (t.len[b] + SC_KEYS - 1) / SC_KEYS;
   const float2* stat = t.stat + (size_t)b * (nb_cap + 1) * R + row;
   float m = -INFINITY, l = 0.f;
+  bool same = true;                                        // every block this thread saw has the same reference
   if (row < R)
-    for (int k = y; k <= nblk; k += 32) {
-      const float2 v = stat[(size_t)(k == nblk ? nb_cap : k) * R];
-      if (v.y == 0.f) continue;
-      const float top = fmaxf(m, v.x);
-      l = l * exp2f(m - top) + v.y * exp2f(v.x - top);
-      m = top;
+    for (int k0 = y; k0 <= nblk; k0 += 128) {
+      float2 v[4];
+#pragma unroll
+      for (int x4 = 0; x4 < 4; ++x4) {
+        const int k = k0 + 32 * x4;
+        v[x4] = k <= nblk ? stat[(size_t)(k == nblk ? nb_cap : k) * R] : make_float2(0.f, 0.f);
+      }
+#pragma unroll
+      for (int x4 = 0; x4 < 4; ++x4) {
+        if (v[x4].y == 0.f) continue;
+        if (v[x4].x == m) { l += v[x4].y; continue; }
+        same = same && m == -INFINITY;
+        const float top = fmaxf(m, v[x4].x);
+        l = l * exp2f(m - top) + v[x4].y * exp2f(v[x4].x - top);
+        m = top;
+      }
     }
   s_m[y][x] = m; s_l[y][x] = l;
   __syncthreads();
@@ -475,6 +514,7 @@ __global__ void __launch_bounds__(1024) slim_tree_finish_kernel(const SlimDecode
   if (row >= R) return;
   const bool there = t.depth[(size_t)b * t.n + row % t.n] >= 0;
   if (y == 0) t.inv_l[(size_t)b * R + row] = there && L != 0.f ? 1.f / L : 0.f;
+  if (same && (m == M || m == -INFINITY)) return;
   for (int k = y; k <= nblk; k += 32) {
     const float2 v = stat[(size_t)(k == nblk ? nb_cap : k) * R];
     if (v.y == 0.f || v.x == M) continue;
@@ -506,13 +546,17 @@ struct SumItem { int b, tile, k0, k1, slot; };       // slot -1: a whole tile
 
 __host__ __device__ inline int stages_of(int len) { return len / 64 + (len % 64 ? 1 : 0) + 1; }
 
+__device__ __forceinline__ int part_begin(int nk, int part, int S) {     // floor(nk part / S)
+  if (S == 1) return part ? nk : 0;
+  return nk < (1 << 21) ? (int)((unsigned)nk * (unsigned)part / (unsigned)S) : (int)((long long)nk * part / S);      // (S <= 1024)
+}
 __device__ __forceinline__ void subtile(const SumSched& s, int idx, int& b, int& tile, int& k0, int& k1) {
   const int per = s.S * s.tiles;
   b = idx / per;
   const int in = idx - b * per, part = in / s.tiles;
   tile = in - part * s.tiles;
-  const long long nk = s.nk[b];
-  k0 = (int)(nk * part / s.S); k1 = (int)(nk * (part + 1) / s.S);
+  const int nk = s.nk[b];
+  k0 = part_begin(nk, part, s.S); k1 = part_begin(nk, part + 1, s.S);
 }
 __device__ __forceinline__ long long line_pos(const SumSched& s, int idx) {       // stages before subtile idx
   if (idx >= s.TS) return s.pre[s.batch];
@@ -524,13 +568,15 @@ __device__ __forceinline__ long long line_pos(const SumSched& s, int idx) {     
 __device__ __forceinline__ int at_pos(const SumSched& s, long long x) {
   int lo = 0, hi = s.batch;
   while (hi - lo > 1) { const int mid = (lo + hi) >> 1; if (s.pre[mid] <= x) lo = mid; else hi = mid; }
-  const long long in = x - s.pre[lo], nk = s.nk[lo];
-  const int k = (int)(in / s.tiles);                                    // in lies in the part whose [k0, k1) holds k
-  int part = (int)(((long long)(k + 1) * s.S - 1) / nk);
-  while ((int)(nk * (part + 1) / s.S) <= k) ++part;
-  while ((int)(nk * part / s.S) > k) --part;
-  const long long k0 = nk * part / s.S, k1 = nk * (part + 1) / s.S;
-  return lo * s.S * s.tiles + part * s.tiles + (int)((in - (long long)s.tiles * k0) / (k1 - k0));
+  const long long in = x - s.pre[lo];
+  const int nk = s.nk[lo];
+  const int k = in < (1ll << 31) ? (int)((unsigned)in / (unsigned)s.tiles) : (int)(in / s.tiles);   // in lies in the part whose [k0, k1) holds k
+  int part = s.S == 1 ? 0 : (int)(((long long)(k + 1) * s.S - 1) / nk);
+  while (part_begin(nk, part + 1, s.S) <= k) ++part;
+  while (part_begin(nk, part, s.S) > k) --part;
+  const int k0 = part_begin(nk, part, s.S), k1 = part_begin(nk, part + 1, s.S);
+  const long long off = in - (long long)s.tiles * k0;
+  return lo * s.S * s.tiles + part * s.tiles + (off < (1ll << 31) ? (int)((unsigned)off / (unsigned)(k1 - k0)) : (int)(off / (k1 - k0)));
 }
 
 // By all threads of a block; s_pre, s_cut, s_nk in shared memory.
@@ -565,17 +611,22 @@ __device__ __forceinline__ SumSched build_sum_sched(const SlimTreeView& t, int b
     s_cut[q + 1] = load < want ? want - load : 0;
   }
   __syncthreads();
-  if (tid == 0) {
+  if (tid < 32) {                                                       // lane x: pairs x per .. x per + per - 1
+    const int per = (s.P + 31) / 32, lo = min(s.P, tid * per), hi = min(s.P, lo + per);
     const long long rest = all - s.g0;
-    long long sum = 0;
-    for (int q = 0; q < s.P; ++q) sum += s_cut[q + 1];
+    long long mine = 0;
+    for (int q = lo; q < hi; ++q) mine += s_cut[q + 1];
+    long long incl = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) { const long long v = __shfl_up_sync(0xffffffffu, incl, o); if (tid >= o) incl += v; }
+    const long long sum = __shfl_sync(0xffffffffu, incl, 31);
     const double scale = sum > 0 ? (double)rest / (double)sum : 0.0;
-    long long run = 0;
-    s_cut[0] = 0;
-    for (int q = 0; q < s.P; ++q) {
+    long long run = incl - mine;
+    if (tid == 0) s_cut[0] = 0;
+    for (int q = lo; q < hi; ++q) {
       run += s_cut[q + 1];
-      s_cut[q + 1] = (long long)((double)run * scale);
-      if (s_cut[q + 1] > rest || q == s.P - 1) s_cut[q + 1] = rest;
+      const long long cut = (long long)((double)run * scale);
+      s_cut[q + 1] = (cut > rest || q == s.P - 1) ? rest : cut;
     }
   }
   __syncthreads();
@@ -666,6 +717,8 @@ slim_tree_u_kernel(const __grid_constant__ CUtensorMap pmap, const __grid_consta
   slim_pdl_trigger();
   slim_pdl_wait();
   const SumSched sc = build_sum_sched(t, p.batch, s_nk, s_pre, s_cut);
+  if (blockIdx.x == 0)
+    for (int i = tid; i < p.batch + 1 + sc.P + 1; i += SU_THREADS) t.sched[i] = i <= p.batch ? s_pre[i] : s_cut[i - p.batch - 1];
   const bool paged = p.block_table != nullptr;
   const int ntile = t.g_ncol;                              // column tiles; tile = row tile * ntile + column tile
 
@@ -792,20 +845,20 @@ slim_tree_u_kernel(const __grid_constant__ CUtensorMap pmap, const __grid_consta
           const float il = r < R ? t.inv_l[(size_t)it.b * R + r] : 0.f;
           const int h = r / t.n, tok = r - h * t.n;
           __nv_bfloat16* out = t.uh + (((size_t)h * p.batch + it.b) * t.n + tok) * p.d + col0;
+          __nv_bfloat16* out_lo = out + (size_t)p.H * p.batch * t.n * p.d;
           for (int c0 = 0; c0 < SU_COLS; c0 += 32) {
             uint32_t v[32];
             tmem_ld32(ta + (uint32_t)c0, v);
             if (r < R && col0 + c0 < p.d) {
 #pragma unroll
               for (int x = 0; x < 32; x += 8) {
-                uint4 o4;
-                uint32_t* ow = reinterpret_cast<uint32_t*>(&o4);
+                uint4 o4, l4;
 #pragma unroll
-                for (int y = 0; y < 4; ++y) {
-                  const __nv_bfloat162 z = __floats2bfloat162_rn(__uint_as_float(v[x + 2 * y]) * il, __uint_as_float(v[x + 2 * y + 1]) * il);
-                  ow[y] = il != 0.f ? *reinterpret_cast<const uint32_t*>(&z) : 0u;      // (an empty row is 0 whatever the keys hold)
-                }
+                for (int y = 0; y < 4; ++y)
+                  split2(__uint_as_float(v[x + 2 * y]) * il, __uint_as_float(v[x + 2 * y + 1]) * il, word_ref(o4, y), word_ref(l4, y));
+                if (il == 0.f) o4 = l4 = make_uint4(0, 0, 0, 0);           // (an empty row is 0 whatever the keys hold)
                 *reinterpret_cast<uint4*>(out + c0 + x) = o4;
+                *reinterpret_cast<uint4*>(out_lo + c0 + x) = l4;
               }
             }
           }
@@ -838,33 +891,37 @@ slim_tree_u_kernel(const __grid_constant__ CUtensorMap pmap, const __grid_consta
 }
 
 // ------------------------------------------------------------------------------------------------ join
-// Block (tile of the batch, 16 rows of it): sums of the tile's slots in the order of its keys, times 1 / l, as bf16.
+// Block (tile of the batch, 16 rows of it): sums of the tile's slots in the order of its keys, times 1 / l.
 __global__ void __launch_bounds__(256) slim_tree_join_kernel(const SlimDecodeParams p, const SlimTreeView t, int mt) {
   extern __shared__ __align__(16) unsigned char smem_raw[];
-  long long* s_pre = reinterpret_cast<long long*>(smem_raw);
-  long long* s_cut = s_pre + p.batch + 1;
-  int* s_nk = reinterpret_cast<int*>(s_cut + t.g_pairs + 1);
-  int* s_slot = s_nk + p.batch;                            // [S + P]
+  long long* s_cut = reinterpret_cast<long long*>(smem_raw);       // [P + 1]
+  int* s_slot = reinterpret_cast<int*>(s_cut + t.g_pairs + 1);     // [S + P]
   __shared__ int s_n;
   const int tid = threadIdx.x, R = p.H * t.n;
   slim_pdl_trigger();
   slim_pdl_wait();
-  const SumSched s = build_sum_sched(t, p.batch, s_nk, s_pre, s_cut);
+  SumSched s;
+  s.batch = p.batch; s.tiles = t.g_tiles; s.S = t.g_split; s.P = t.g_pairs; s.F = t.g_whole; s.TS = p.batch * t.g_tiles * t.g_split;
   const int at = blockIdx.x + (s.S == 1 ? s.F : 0), b = at / s.tiles, tile = at % s.tiles;
   const int row0 = (tile / t.g_ncol) * mt * 256 + blockIdx.y * 16, col0 = (tile % t.g_ncol) * SU_COLS;
   if (row0 >= R) return;
+  for (int q = tid; q <= s.P; q += 256) s_cut[q] = t.sched[p.batch + 1 + q];
+  const int bf = s.F / (s.S * s.tiles), inf = s.F - bf * s.S * s.tiles;                 // subtile F
+  __syncthreads();
   if (tid == 0) {
     int cnt = 0;
+    const int nk = stages_of(t.len[b]), nkf = bf < p.batch ? stages_of(t.len[bf]) : 0;
+    const int f0 = part_begin(nkf, inf / s.tiles, s.S), f1 = part_begin(nkf, inf / s.tiles + 1, s.S);
+    const long long g0 = t.sched[bf] + (long long)s.tiles * f0 + (long long)(inf % s.tiles) * (f1 - f0);
     for (int part = 0; part < s.S; ++part) {
       const int idx = (b * s.S + part) * s.tiles + tile;
-      int bb, tt, k0, k1;
-      subtile(s, idx, bb, tt, k0, k1);
+      const int k0 = part_begin(nk, part, s.S), k1 = part_begin(nk, part + 1, s.S);
       if (k0 == k1) continue;
       if (idx < s.F) {
         if (s.S > 1) s_slot[cnt++] = 2 * s.P + idx;
         continue;
       }
-      const long long x0 = line_pos(s, idx) - s.g0, x1 = x0 + (k1 - k0);
+      const long long x0 = t.sched[b] + (long long)s.tiles * k0 + (long long)tile * (k1 - k0) - g0, x1 = x0 + (k1 - k0);
       int lo = 0, hi = s.P;                                // the pair whose segment holds x0: the last one with cut <= x0 < next cut
       while (hi - lo > 1) { const int mid = (lo + hi) >> 1; if (s_cut[mid] <= x0) lo = mid; else hi = mid; }
       for (int q = lo; q < s.P && s_cut[q] < x1; ++q) {
@@ -879,29 +936,45 @@ __global__ void __launch_bounds__(256) slim_tree_join_kernel(const SlimDecodePar
   __syncthreads();
   const int cnt = s_n;
   if (cnt == 0) return;                                    // written as a whole by one pair
-  for (int e = tid; e < 16 * (SU_COLS / 4); e += 256) {
-    const int rr = e / (SU_COLS / 4), c = (e % (SU_COLS / 4)) * 4, r = row0 + rr;
-    if (r >= R || col0 + c >= p.d) continue;
-    const size_t off = ((size_t)(blockIdx.y * 16 + rr)) * SU_COLS + c;
-    float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int k = 0; k < cnt; ++k) {
-      const float4 v = *reinterpret_cast<const float4*>(t.part + (size_t)s_slot[k] * mt * 256 * SU_COLS + off);
-      a.x += v.x; a.y += v.y; a.z += v.z; a.w += v.w;
+  // four rows a thread (tid / 64 + 4 m), four columns each; the slots one after another
+  const int c = (tid % 64) * 4;
+  if (col0 + c >= p.d) return;
+  float4 a[4];
+#pragma unroll
+  for (int m = 0; m < 4; ++m) a[m] = make_float4(0.f, 0.f, 0.f, 0.f);
+  const float* src = t.part + (size_t)(blockIdx.y * 16 + tid / 64) * SU_COLS + c;
+#pragma unroll 4
+  for (int k = 0; k < cnt; ++k) {
+    const float* slot = src + (size_t)s_slot[k] * mt * 256 * SU_COLS;
+#pragma unroll
+    for (int m = 0; m < 4; ++m) {
+      if (row0 + tid / 64 + 4 * m >= R) continue;
+      const float4 v = *reinterpret_cast<const float4*>(slot + (size_t)4 * m * SU_COLS);
+      a[m].x += v.x; a[m].y += v.y; a[m].z += v.z; a[m].w += v.w;
     }
+  }
+#pragma unroll
+  for (int m = 0; m < 4; ++m) {
+    const int r = row0 + tid / 64 + 4 * m;
+    if (r >= R) continue;
     const float il = t.inv_l[(size_t)b * R + r];
-    if (il == 0.f) a = make_float4(0.f, 0.f, 0.f, 0.f);    // (an empty row is 0 whatever the keys hold)
+    if (il == 0.f) a[m] = make_float4(0.f, 0.f, 0.f, 0.f);    // (an empty row is 0 whatever the keys hold)
     const int h = r / t.n, tok = r - h * t.n;
-    const __nv_bfloat162 o0 = __floats2bfloat162_rn(a.x * il, a.y * il), o1 = __floats2bfloat162_rn(a.z * il, a.w * il);
-    *reinterpret_cast<uint2*>(t.uh + (((size_t)h * p.batch + b) * t.n + tok) * p.d + col0 + c) =
-        make_uint2(*reinterpret_cast<const uint32_t*>(&o0), *reinterpret_cast<const uint32_t*>(&o1));
+    uint2 hi, lo;
+    split2(a[m].x * il, a[m].y * il, hi.x, lo.x);
+    split2(a[m].z * il, a[m].w * il, hi.y, lo.y);
+    __nv_bfloat16* out = t.uh + (((size_t)h * p.batch + b) * t.n + tok) * p.d + col0 + c;
+    *reinterpret_cast<uint2*>(out) = hi;
+    *reinterpret_cast<uint2*>(out + (size_t)p.H * p.batch * t.n * p.d) = lo;
   }
 }
 
 // ------------------------------------------------------------------------------------------------ o = U W_KV,h
 // CTA = (part of the d rows of W_KV,h, head, 128 (sequence, token) rows); the parts form a cluster and add their
-// accumulators through distributed shared memory, in order, each the rows it writes.
-constexpr int OU_NS = 5, OU_A = 128 * 128, OU_B = 64 * 256;
-constexpr uint32_t OU_STAGE = OU_A + OU_B;
+// accumulators through distributed shared memory, in order, each the rows it writes.  U comes as two bf16 terms (one
+// would cost as much accuracy as the rounding of the output does), both against the same tile of W_KV,h.
+constexpr int OU_NS = 4, OU_A = 128 * 128, OU_B = 64 * 256;
+constexpr uint32_t OU_STAGE = 2 * OU_A + OU_B;
 constexpr int OU_LD = 132;                                 // floats per accumulator row in shared memory
 constexpr size_t OU_SMEM = 1024 + (size_t)OU_NS * OU_STAGE + 16 * OU_NS + 8 + 32;
 static_assert(128 * OU_LD * 4 <= OU_NS * (int)OU_STAGE, "the accumulator is staged where the operands were");
@@ -913,7 +986,7 @@ __device__ __forceinline__ float4 ld_cluster_f32x4(uint32_t a) {
 }
 
 __global__ void __launch_bounds__(128) slim_tree_out_kernel(const __grid_constant__ CUtensorMap umap, const __grid_constant__ CUtensorMap wmap,
-                                                            __nv_bfloat16* __restrict__ o, int rows, int d, int d_k, int parts, int* status) {
+                                                            __nv_bfloat16* __restrict__ o, int rows, int d, int d_k, int H, int parts, int* status) {
   extern __shared__ unsigned char smem_raw[];
   const uint32_t raw_u32 = smem_u32(smem_raw), base = (raw_u32 + 1023u) & ~1023u;
   unsigned char* sm = smem_raw + (base - raw_u32);
@@ -924,7 +997,7 @@ __global__ void __launch_bounds__(128) slim_tree_out_kernel(const __grid_constan
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int part = blockIdx.x, h = blockIdx.y, m0 = blockIdx.z * 128;
   const int ns = d / 64, s0 = ns * part / parts, s1 = ns * (part + 1) / parts;
-  const uint32_t bytes = OU_A + (d_k == 64 ? OU_B / 2 : OU_B);
+  const uint32_t bytes = 2 * OU_A + (d_k == 64 ? OU_B / 2 : OU_B);
   if (tid == 0) {
     prefetch_tensormap(&umap); prefetch_tensormap(&wmap);
     for (int i = 0; i < OU_NS; ++i) { mbar_init(bar_full + 8 * i, 1); mbar_init(bar_empty + 8 * i, 1); }
@@ -950,7 +1023,8 @@ __global__ void __launch_bounds__(128) slim_tree_out_kernel(const __grid_constan
       const uint32_t dst = base + (uint32_t)st * OU_STAGE;
       mbar_arrive_expect_tx(bar_full + 8 * st, bytes);
       tma_load_3d(dst, &umap, bar_full + 8 * st, s * 64, m0, h);
-      tma_load_3d(dst + OU_A, &wmap, bar_full + 8 * st, 0, h * d + s * 64, 0);
+      tma_load_3d(dst + OU_A, &umap, bar_full + 8 * st, s * 64, m0, H + h);
+      tma_load_3d(dst + 2 * OU_A, &wmap, bar_full + 8 * st, 0, h * d + s * 64, 0);
     }
     if (!ok) {
       const int did = s - s0, issued = did < OU_NS ? did : OU_NS;
@@ -962,7 +1036,7 @@ __global__ void __launch_bounds__(128) slim_tree_out_kernel(const __grid_constan
     }
   } else if (warp == 1 && lane == 0) {
     bool ok = true;
-    const uint64_t ad0 = desc_kmajor_sw128(base), bd0 = desc_a(base + OU_A, 8192);
+    const uint64_t ad0 = desc_kmajor_sw128(base), bd0 = desc_a(base + 2 * OU_A, 8192);
     const uint32_t a_lo0 = (uint32_t)ad0, a_hi = (uint32_t)(ad0 >> 32), b_lo0 = (uint32_t)bd0, b_hi = (uint32_t)(bd0 >> 32);
     const uint32_t idesc = umma_idesc_major((uint32_t)d_k, 0, 1);
     for (int j = 0; j < s1 - s0; ++j) {
@@ -972,8 +1046,9 @@ __global__ void __launch_bounds__(128) slim_tree_out_kernel(const __grid_constan
       tc_fence_after();
       const uint32_t a_lo = a_lo0 + (uint32_t)st * (OU_STAGE >> 4), b_lo = b_lo0 + (uint32_t)st * (OU_STAGE >> 4);
 #pragma unroll
-      for (int kk = 0; kk < 4; ++kk)
-        umma_bf16_words(tmem_base, a_lo + (uint32_t)kk * (32u >> 4), a_hi, b_lo + (uint32_t)kk * (2048u >> 4), b_hi, idesc, (j | kk) ? 1u : 0u);
+      for (int x = 0; x < 8; ++x)
+        umma_bf16_words(tmem_base, a_lo + (uint32_t)(x >> 2) * (OU_A >> 4) + (uint32_t)(x & 3) * (32u >> 4), a_hi,
+                        b_lo + (uint32_t)(x & 3) * (2048u >> 4), b_hi, idesc, (j | x) ? 1u : 0u);
       umma_commit(bar_empty + 8 * st);
     }
     if (ok) umma_commit(bar_done);
@@ -1116,13 +1191,14 @@ void slim_tree_tc_layout(const slim_ctx* ctx, int batch, int t_cap, int n, SlimT
   L.p = off; off = align256(off + 2 * (size_t)batch * R * L.p_ld);
   L.stat = off; off = align256(off + 8 * (size_t)batch * (nb + 1) * R);
   L.tail = off; off = align256(off + 2 * (size_t)batch * 128 * ctx->d);
-  L.uh = off; off = align256(off + 2 * (size_t)batch * R * ctx->d);
+  L.uh = off; off = align256(off + 2 * 2 * (size_t)batch * R * ctx->d);
   L.part = off; off = align256(off + sizeof(float) * slots * L.mt * 256 * SU_COLS);
+  L.sched = off; off = align256(off + sizeof(long long) * ((size_t)batch + L.g_pairs + 2));
   if (off > L.total) L.total = off;
 }
 
 cudaError_t slim_launch_tree_tc(const slim_ctx* ctx, const SlimDecodeParams& p, const SlimTreeView& t, const SlimTreeLayout& L,
-                                long long total_rows, void* o, cudaStream_t st) {
+                                const int32_t* parents, long long total_rows, void* o, cudaStream_t st) {
   const int d = p.d, dk = p.d_k, H = p.H, R = H * t.n, M = p.batch * t.n;
   CUtensorMap pmap, kmap, tailmap, umap, wmap;
   cudaError_t e;
@@ -1139,7 +1215,7 @@ cudaError_t slim_launch_tree_tc(const slim_ctx* ctx, const SlimDecodeParams& p, 
     if ((e = slim_tmap_encode_3d(k ? &tailmap : &kmap, k ? t.tail : const_cast<void*>(p.k), dims, str, box)) != cudaSuccess) return e;
   }
   {
-    const unsigned long long dims[3] = {(unsigned long long)d, (unsigned long long)M, (unsigned long long)H};
+    const unsigned long long dims[3] = {(unsigned long long)d, (unsigned long long)M, 2ull * H};
     const unsigned long long str[2] = {2ull * d, 2ull * d * M};
     const unsigned int box[3] = {64, 128, 1};
     if ((e = slim_tmap_encode_3d(&umap, t.uh, dims, str, box)) != cudaSuccess) return e;
@@ -1150,7 +1226,7 @@ cudaError_t slim_launch_tree_tc(const slim_ctx* ctx, const SlimDecodeParams& p, 
     const unsigned int box[3] = {64, 64, dk == 64 ? 1u : 2u};
     if ((e = slim_tmap_encode_3d(&wmap, const_cast<void*>(p.wkv), dims, str, box)) != cudaSuccess) return e;
   }
-  e = slim_launch_pdl(slim_tree_tail_kernel, dim3(16, p.batch), dim3(256), 0, st, p, t);
+  e = slim_launch_pdl(slim_tree_tail_kernel, dim3(64, p.batch), dim3(256), 0, st, p, t, parents);
   if (e != cudaSuccess) return e;
   e = dk == 64 ? launch_p_tokens<64>(ctx, p, t, total_rows, st) : dk == 96 ? launch_p_tokens<96>(ctx, p, t, total_rows, st)
                                                                           : launch_p_tokens<128>(ctx, p, t, total_rows, st);
@@ -1160,7 +1236,7 @@ cudaError_t slim_launch_tree_tc(const slim_ctx* ctx, const SlimDecodeParams& p, 
   e = L.mt == 1 ? launch_u<1>(ctx, p, t, pmap, kmap, tailmap, st) : launch_u<2>(ctx, p, t, pmap, kmap, tailmap, st);
   if (e != cudaSuccess) return e;
   if (L.g_split > 1 || L.g_whole < p.batch * L.g_tiles) {
-    const size_t smem = sizeof(long long) * (p.batch + 1 + t.g_pairs + 1) + sizeof(int) * (p.batch + L.g_split + t.g_pairs) + 16;
+    const size_t smem = sizeof(long long) * (t.g_pairs + 1) + sizeof(int) * (L.g_split + t.g_pairs) + 16;
     const int tiles = p.batch * L.g_tiles - (L.g_split == 1 ? L.g_whole : 0);          // the others are written as a whole
     e = slim_launch_pdl(slim_tree_join_kernel, dim3(tiles, L.mt * 16), dim3(256), smem, st, p, t, L.mt);
     if (e != cudaSuccess) return e;
@@ -1176,5 +1252,5 @@ cudaError_t slim_launch_tree_tc(const slim_ctx* ctx, const SlimDecodeParams& p, 
   attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr; cfg.numAttrs = 2;
-  return cudaLaunchKernelEx(&cfg, slim_tree_out_kernel, umap, wmap, (__nv_bfloat16*)o, M, d, dk, parts, p.status);
+  return cudaLaunchKernelEx(&cfg, slim_tree_out_kernel, umap, wmap, (__nv_bfloat16*)o, M, d, dk, H, parts, p.status);
 }
