@@ -737,11 +737,12 @@ slim_status launched(cudaError_t e) {
   return SLIM_ERR_CUDA;
 }
 
-struct WeightsLayout { size_t scores, m, inv_l, total; };
+struct WeightsLayout { size_t scores, part, m, inv_l, total; };
 WeightsLayout weights_layout(const slim_ctx* ctx, int batch, int t_cap) {
   WeightsLayout L;
   size_t off = 0;
   L.scores = off; off = align256(off + sizeof(float) * (size_t)batch * ctx->H * t_cap);
+  L.part = off; off = align256(off + sizeof(float2) * ((size_t)slim_weights_workers(ctx) + batch) * ctx->H);
   L.m = off; off = align256(off + sizeof(float) * (size_t)batch * ctx->H);
   L.inv_l = off; off = align256(off + sizeof(float) * (size_t)batch * ctx->H);
   L.total = off;
@@ -798,7 +799,7 @@ slim_status slim_accumulate_weights(slim_ctx* ctx, const void* q, const slim_cac
   const WeightsLayout L = weights_layout(ctx, cache->batch, cache->t_cap);
   char* ws = static_cast<char*>(workspace);
   return launched(slim_launch_weights(ctx, cache_params(ctx, cache, q, lengths), reinterpret_cast<float*>(ws + L.scores),
-                                      reinterpret_cast<float*>(ws + L.m), reinterpret_cast<float*>(ws + L.inv_l), acc, (cudaStream_t)stream));
+                                      reinterpret_cast<float2*>(ws + L.part), reinterpret_cast<float*>(ws + L.m), reinterpret_cast<float*>(ws + L.inv_l), acc, (cudaStream_t)stream));
 }
 
 size_t slim_evict_workspace_bytes(const slim_ctx* ctx, int batch, int t_cap) {

@@ -1,12 +1,188 @@
 // A long cache kept inside a budget: attention weights accumulated per cache row (slim_accumulate_weights) and
 // eviction of the rows with the least of it (slim_evict).
 #include "slim_internal.h"
+#include "slim_ptx.cuh"
 #include "slim_sched.cuh"
+
+using namespace slim_ptx;
 
 namespace {
 
+__device__ __forceinline__ f32x2 sub2(f32x2 a, f32x2 b) { f32x2 d; asm("sub.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b)); return d; }
+
 // ---------------------------------------------------------------- accumulated weights
-// Reference exponent and denominator of every (sequence, head) from the softmax arguments [b][h][t_cap].
+// Softmax arguments of one query per sequence, all heads, and the running (maximum, sum) of every head over a worker's
+// rows.  The context is cut into tiles of 16 rows dealt out evenly over the ragged batch (slim_sched.cuh).  A thread owns
+// a unit: VEC rotation pairs (16 bytes of the low half of a head, 16 of the high half) of one head, so that a warp reads
+// whole contiguous rows.  The rotation is moved onto the query, q^ . R_t k = (R_(pos - t) q) . k, which is seeded from the
+// tables at a tile's first row (float32 products of entries made in float64) and turned by one position a row with a
+// packed complex product: at most 16 steps, so that its error stays below 2^-20.  Where a row has fewer units than a block
+// has threads, groups of threads take different rows of the tile.  Everything is float32: sums of a unit's products in a
+// register, of a head's units in order through shared memory.
+// Bound by HBM: every key byte is read once, about 50 instructions a thread and row against the 340 clocks that an
+// 8 KB row costs an SM at the copy rate.
+constexpr int WT = 256;
+
+template <typename KT> struct KeyVec;
+template <> struct KeyVec<float> {
+  static constexpr int N = 4;
+  static __device__ __forceinline__ void unpack(const uint4& v, f32x2 (&f)[2]) {
+    f[0] = pack2(__uint_as_float(v.x), __uint_as_float(v.y)); f[1] = pack2(__uint_as_float(v.z), __uint_as_float(v.w));
+  }
+};
+template <> struct KeyVec<__nv_bfloat16> {
+  static constexpr int N = 8;
+  static __device__ __forceinline__ void unpack(const uint4& v, f32x2 (&f)[4]) {
+    f[0] = unpack2(v.x); f[1] = unpack2(v.y); f[2] = unpack2(v.z); f[3] = unpack2(v.w);
+  }
+};
+
+template <typename KT, bool ROPE>
+__global__ void __launch_bounds__(WT, 2)
+slim_weights_scores_kernel(const SlimDecodeParams p, float* __restrict__ scores, float2* __restrict__ part) {
+  constexpr int VEC = KeyVec<KT>::N, NP = VEC / 2;
+  extern __shared__ __align__(16) float s_part[];                  // [2][16][units + 4]
+  const int d = p.d, H = p.H, dk = p.d_k, half = p.half, tid = threadIdx.x;
+  const int units = d / (2 * VEC), per_head = half / VEC, ld = units + 4;
+  int* s_prefix = reinterpret_cast<int*>(s_part + 2 * SLIM_TT * ld);
+  slim_pdl_trigger();
+  slim_pdl_wait();
+  const SlimSched sc = slim_sched_build(p.lengths, p.batch, p.t_cap, p.workers, 1, s_prefix, p.status, 0);
+  const int w = blockIdx.x;
+  if (sc.total_tiles == 0 || w >= sc.workers_eff) return;
+  const int g_begin = slim_worker_start(sc, w), g_end = slim_worker_start(sc, w + 1);
+  int groups = 1;                                                  // row groups of a tile
+  while (groups < SLIM_TT && 2 * groups * units <= WT) groups *= 2;
+  const int rpg = SLIM_TT / groups, stride = groups > 1 ? units : WT;
+  const int rg = groups > 1 ? min(tid / units, groups) : 0, u0 = groups > 1 ? tid % units : tid;      // rg == groups: no unit
+  const KT* Kc = reinterpret_cast<const KT*>(p.k);
+
+  int buf = 0;
+  for (int g = g_begin; g < g_end;) {
+    const int b = slim_seq_of_tile(s_prefix, p.batch, g);
+    const int seg_end = min(g_end, s_prefix[b + 1]);
+    const int len = min(max(p.lengths[b], 0), p.t_cap), pos = len - 1;
+    const KT* q = reinterpret_cast<const KT*>(p.q) + (size_t)b * d;
+    float run_m[4], run_l[4];                                      // of (head, row of the tile) number tid + 256 x
+#pragma unroll
+    for (int x = 0; x < 4; ++x) { run_m[x] = -INFINITY; run_l[x] = 0.f; }
+    for (; g < seg_end; ++g, buf ^= 1) {
+      const int t0 = (g - s_prefix[b]) * SLIM_TT;
+      const KT* rows = Kc + (size_t)slim_cache_row(p, b, t0) * d;
+      const int last = min(SLIM_TT - 1, len - 1 - t0);             // rows behind it are read as it, and not used
+      float* out = s_part + buf * SLIM_TT * ld;
+      for (int u = u0; u < units && rg < groups; u += stride) {
+        const int h = u / per_head, j0 = (u - h * per_head) * VEC, at = h * dk + j0, r0 = rg * rpg;
+        // the query, scaled and turned to the distance of this thread's first row
+        f32x2 z1[NP], z2[NP], co[NP], si[NP];
+        KeyVec<KT>::unpack(__ldg(reinterpret_cast<const uint4*>(q + at)), z1);
+        KeyVec<KT>::unpack(__ldg(reinterpret_cast<const uint4*>(q + at + half)), z2);
+        const int dist = max(pos - t0 - r0, 0);
+#pragma unroll
+        for (int x = 0; x < NP; ++x) {
+          const f32x2 sc2 = pack2(p.qscale, p.qscale);
+          z1[x] = mul2(z1[x], sc2); z2[x] = mul2(z2[x], sc2);
+          if (ROPE) {
+            const float4 cb = __ldg(reinterpret_cast<const float4*>(p.rope_base + (size_t)(dist / SLIM_TT) * half + j0) + x);
+            const float4 cf = __ldg(reinterpret_cast<const float4*>(p.rope_off + (dist % SLIM_TT) * half + j0) + x);
+            const float4 st = __ldg(reinterpret_cast<const float4*>(p.rope_off + half + j0) + x);      // one position
+            const f32x2 c = pack2(cb.x * cf.x - cb.y * cf.y, cb.z * cf.z - cb.w * cf.w), s = pack2(cb.y * cf.x + cb.x * cf.y, cb.w * cf.z + cb.z * cf.w);
+            const f32x2 a = fma2(z2[x], s, mul2(z1[x], c));
+            z2[x] = sub2(mul2(z2[x], c), mul2(z1[x], s));
+            z1[x] = a;
+            co[x] = pack2(st.x, st.z); si[x] = pack2(st.y, st.w);
+          }
+        }
+        for (int r = 0; r < rpg; r += 4) {
+          uint4 k1[4], k2[4];
+#pragma unroll
+          for (int x = 0; x < 4; ++x) {
+            const KT* row = rows + (size_t)min(r0 + min(r + x, rpg - 1), last) * d + at;
+            k1[x] = __ldg(reinterpret_cast<const uint4*>(row));
+            k2[x] = __ldg(reinterpret_cast<const uint4*>(row + half));
+          }
+#pragma unroll
+          for (int x = 0; x < 4; ++x) {
+            f32x2 f1[NP], f2[NP];
+            KeyVec<KT>::unpack(k1[x], f1);
+            KeyVec<KT>::unpack(k2[x], f2);
+            f32x2 a = mul2(f1[0], z1[0]), c = mul2(f2[0], z2[0]);
+#pragma unroll
+            for (int y = 1; y < NP; ++y) { a = fma2(f1[y], z1[y], a); c = fma2(f2[y], z2[y], c); }
+            if (r + x < rpg) out[(r0 + r + x) * ld + u] = sum2(add2(a, c));
+            if (ROPE)
+#pragma unroll
+              for (int y = 0; y < NP; ++y) {                       // one position nearer: times e^{i theta}
+                const f32x2 n1 = sub2(mul2(z1[y], co[y]), mul2(z2[y], si[y]));
+                z2[y] = fma2(z1[y], si[y], mul2(z2[y], co[y]));
+                z1[y] = n1;
+              }
+          }
+        }
+      }
+      __syncthreads();                                             // (two buffers: the next tile may be written while this one is read)
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        const int e = tid + WT * x, h = e / SLIM_TT, r = e % SLIM_TT;
+        if (h >= H || t0 + r >= len) continue;
+        const float* a = out + r * ld + h * per_head;
+        float s = 0.f;
+        for (int y = 0; y < per_head; ++y) s += a[y];
+        scores[((size_t)b * H + h) * p.t_cap + t0 + r] = s;
+        const float top = fmaxf(run_m[x], s);
+        if (top != -INFINITY) run_l[x] = run_l[x] * exp2f(run_m[x] - top) + exp2f(s - top);
+        run_m[x] = top;
+      }
+    }
+    // the unit's (maximum, sum) of every head: over the 16 threads that share it
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      float m = run_m[x], l = run_l[x];
+#pragma unroll
+      for (int o = 8; o > 0; o >>= 1) {
+        const float m1 = __shfl_xor_sync(0xffffffffu, m, o), l1 = __shfl_xor_sync(0xffffffffu, l, o), top = fmaxf(m, m1);
+        if (top != -INFINITY) l = l * exp2f(m - top) + l1 * exp2f(m1 - top);
+        m = top;
+      }
+      const int e = tid + WT * x, h = e / SLIM_TT;
+      if (e % SLIM_TT == 0 && h < H) part[(size_t)(w + b) * H + h] = make_float2(m, l);
+    }
+  }
+}
+
+// Reference exponent and 1 / denominator of every (sequence, head) from its units' parts: a warp each.
+__global__ void __launch_bounds__(256) slim_weights_join_kernel(const SlimDecodeParams p, const float2* __restrict__ part, float* __restrict__ m_out,
+                                                                float* __restrict__ inv_out) {
+  extern __shared__ int s_prefix2[];
+  slim_pdl_trigger();
+  slim_pdl_wait();
+  const SlimSched sc = slim_sched_build(p.lengths, p.batch, p.t_cap, p.workers, 1, s_prefix2, p.status, 0);
+  const int b = blockIdx.y, h = blockIdx.x * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+  if (h >= p.H) return;
+  float m = -INFINITY, l = 0.f;
+  if (s_prefix2[b + 1] > s_prefix2[b]) {
+    const int w0 = slim_worker_of_tile(sc, s_prefix2[b]), w1 = slim_worker_of_tile(sc, s_prefix2[b + 1] - 1);
+    for (int w = w0 + lane; w <= w1; w += 32) {
+      const float2 v = part[(size_t)(w + b) * p.H + h];
+      const float top = fmaxf(m, v.x);
+      if (top != -INFINITY) l = l * exp2f(m - top) + v.y * exp2f(v.x - top);
+      m = top;
+    }
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    const float m1 = __shfl_xor_sync(0xffffffffu, m, o), l1 = __shfl_xor_sync(0xffffffffu, l, o), top = fmaxf(m, m1);
+    if (top != -INFINITY) l = l * exp2f(m - top) + l1 * exp2f(m1 - top);
+    m = top;
+  }
+  if (lane == 0) {
+    m_out[(size_t)b * p.H + h] = m == -INFINITY ? 0.f : m;
+    inv_out[(size_t)b * p.H + h] = l != 0.f ? 1.f / l : 0.f;
+  }
+}
+
+// The same from the softmax arguments [b][h][t_cap] themselves (8-bit caches and shapes whose arguments come from
+// slim_scores_kernel).
 __global__ void __launch_bounds__(256) slim_weights_stat_kernel(const SlimDecodeParams p, const float* __restrict__ scores,
                                                                 float* __restrict__ m_out, float* __restrict__ inv_out) {
   __shared__ float s_m[8], s_l[8];
@@ -226,10 +402,30 @@ cudaError_t launch_move(const slim_ctx* ctx, const slim_cache* c, void* base, si
 
 }  // namespace
 
-cudaError_t slim_launch_weights(const slim_ctx* ctx, const SlimDecodeParams& p, float* scores, float* m, float* inv_l, float* acc,
-                                cudaStream_t st) {
-  cudaError_t e = slim_launch_scores(ctx, p, scores, st);
-  if (e == cudaSuccess) e = slim_launch_pdl(slim_weights_stat_kernel, dim3(p.H, p.batch), dim3(256), 0, st, p, (const float*)scores, m, inv_l);
+// Workers of the score kernel: two CTAs an SM.
+int slim_weights_workers(const slim_ctx* ctx) { return 2 * ctx->num_sms; }
+
+cudaError_t slim_launch_weights(const slim_ctx* ctx, const SlimDecodeParams& p_in, float* scores, float2* part, float* m, float* inv_l,
+                                float* acc, cudaStream_t st) {
+  SlimDecodeParams p = p_in;
+  // whole 16-byte vectors of a head's halves (rows are then 16-byte aligned too); 8-bit codes and other widths take the
+  // score kernel of slim_decode's CUDA-core path
+  const int vec = p.kdtype == SLIM_BF16 ? 8 : 4;
+  const size_t smem = sizeof(float) * 2 * SLIM_TT * (size_t)(p.d / (2 * vec) + 4) + sizeof(int) * (p.batch + 1);
+  cudaError_t e;
+  if (p.kdtype != SLIM_FP8 && p.half % vec == 0 && smem <= 200 * 1024) {
+    p.workers = slim_weights_workers(ctx);
+    auto kern = p.kdtype == SLIM_BF16 ? (p.rope ? slim_weights_scores_kernel<__nv_bfloat16, true> : slim_weights_scores_kernel<__nv_bfloat16, false>)
+                                      : (p.rope ? slim_weights_scores_kernel<float, true> : slim_weights_scores_kernel<float, false>);
+    if (smem > 48 * 1024 && (e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem)) != cudaSuccess) return e;
+    e = slim_launch_pdl(kern, dim3(p.workers), dim3(WT), smem, st, p, scores, part);
+    if (e == cudaSuccess)
+      e = slim_launch_pdl(slim_weights_join_kernel, dim3((p.H + 7) / 8, p.batch), dim3(256), sizeof(int) * (p.batch + 1), st, p,
+                          (const float2*)part, m, inv_l);
+  } else {
+    e = slim_launch_scores(ctx, p, scores, st);
+    if (e == cudaSuccess) e = slim_launch_pdl(slim_weights_stat_kernel, dim3(p.H, p.batch), dim3(256), 0, st, p, (const float*)scores, m, inv_l);
+  }
   if (e == cudaSuccess)
     e = slim_launch_pdl(slim_weights_add_kernel, dim3((p.t_cap + 255) / 256, p.batch), dim3(256), 0, st, p, (const float*)scores,
                         (const float*)m, (const float*)inv_l, acc);
