@@ -742,7 +742,7 @@ WeightsLayout weights_layout(const slim_ctx* ctx, int batch, int t_cap) {
   WeightsLayout L;
   size_t off = 0;
   L.scores = off; off = align256(off + sizeof(float) * (size_t)batch * ctx->H * t_cap);
-  L.part = off; off = align256(off + sizeof(float2) * ((size_t)slim_weights_workers(ctx) + batch) * ctx->H);
+  L.part = off; off = align256(off + sizeof(float2) * ((size_t)slim_weights_workers(ctx) + batch) * SLIM_TT * ctx->H);       // (up to 16 row groups)
   L.m = off; off = align256(off + sizeof(float) * (size_t)batch * ctx->H);
   L.inv_l = off; off = align256(off + sizeof(float) * (size_t)batch * ctx->H);
   L.total = off;

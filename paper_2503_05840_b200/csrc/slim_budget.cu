@@ -12,16 +12,16 @@ __device__ __forceinline__ f32x2 sub2(f32x2 a, f32x2 b) { f32x2 d; asm("sub.rn.f
 
 // ---------------------------------------------------------------- accumulated weights
 // Softmax arguments of one query per sequence, all heads, and the running (maximum, sum) of every head over a worker's
-// rows.  The context is cut into tiles of 16 rows dealt out evenly over the ragged batch (slim_sched.cuh).  A thread owns
-// a unit: VEC rotation pairs (16 bytes of the low half of a head, 16 of the high half) of one head, so that a warp reads
-// whole contiguous rows.  The rotation is moved onto the query, q^ . R_t k = (R_(pos - t) q) . k, which is seeded from the
-// tables at a tile's first row (float32 products of entries made in float64) and turned by one position a row with a
-// packed complex product: at most 16 steps, so that its error stays below 2^-20.  Where a row has fewer units than a block
-// has threads, groups of threads take different rows of the tile.  Everything is float32: sums of a unit's products in a
-// register, of a head's units in order through shared memory.
-// Bound by HBM: every key byte is read once, about 50 instructions a thread and row against the 340 clocks that an
-// 8 KB row costs an SM at the copy rate.
-constexpr int WT = 256;
+// rows.  The context is cut into tiles of 16 rows dealt out evenly over the ragged batch (slim_sched.cuh), one CTA per
+// SM; a producer warp brings whole rows (a tile is contiguous, in a page too) into a ring in shared memory with bulk
+// copies.  LPH neighbouring lanes share a head, each with VEC rotation pairs (16 bytes of its low half, 16 of its high
+// half); enough warps for all heads make a row group, and the groups take different rows of a tile.  A warp keeps
+// (maximum, sum) of its heads and rows to itself, so nothing waits but for the ring.
+// The rotation is moved onto the query, q^ . R_t k = (R_(pos - t) q) . k, which is seeded from the tables at the group's
+// first row of a tile (float32 products of entries made in float64) and turned by one position a row with a packed
+// complex product: at most 16 steps, so that its error stays below 2^-20.  Everything is float32.
+// Bound by HBM: every key byte is read once.
+constexpr int WC = 512, WT = WC + 32;                              // consumers; and the producer warp
 
 template <typename KT> struct KeyVec;
 template <> struct KeyVec<float> {
@@ -37,122 +37,162 @@ template <> struct KeyVec<__nv_bfloat16> {
   }
 };
 
-template <typename KT, bool ROPE>
-__global__ void __launch_bounds__(WT, 2)
-slim_weights_scores_kernel(const SlimDecodeParams p, float* __restrict__ scores, float2* __restrict__ part) {
-  constexpr int VEC = KeyVec<KT>::N, NP = VEC / 2;
-  extern __shared__ __align__(16) float s_part[];                  // [2][16][units + 4]
-  const int d = p.d, H = p.H, dk = p.d_k, half = p.half, tid = threadIdx.x;
-  const int units = d / (2 * VEC), per_head = half / VEC, ld = units + 4;
-  int* s_prefix = reinterpret_cast<int*>(s_part + 2 * SLIM_TT * ld);
+struct WeightsRing { int rows, stages, groups, warps; };           // rows of a stage (a power of two up to 16); row groups and warps of one
+
+template <typename KT, bool ROPE, int LPH>
+__global__ void __launch_bounds__(WT, 1)
+slim_weights_scores_kernel(const SlimDecodeParams p, float* __restrict__ scores, float2* __restrict__ part, const WeightsRing ring) {
+  constexpr int VEC = KeyVec<KT>::N, NP = VEC / 2, HPW = 32 / LPH;
+  extern __shared__ __align__(128) unsigned char sm[];
+  const int d = p.d, H = p.H, dk = p.d_k, half = p.half, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const uint32_t row_bytes = (uint32_t)(d * sizeof(KT)), stage_bytes = row_bytes * ring.rows;
+  unsigned char* keys = sm;                                        // [stages][rows][row_bytes]
+  uint64_t* bars = reinterpret_cast<uint64_t*>(sm + (size_t)ring.stages * stage_bytes);  // [stages] full, [stages] empty
+  volatile int* s_abort = reinterpret_cast<volatile int*>(bars + 2 * ring.stages);
+  int* s_prefix = const_cast<int*>(s_abort) + 2;
+  const uint32_t bar_full = smem_u32(bars), bar_empty = bar_full + 8u * ring.stages;
+  const int used = ring.groups * ring.warps;                       // consumer warps that have work
+  if (tid == 0) {
+    for (int i = 0; i < ring.stages; ++i) { mbar_init(bar_full + 8 * i, 1); mbar_init(bar_empty + 8 * i, used); }
+    *s_abort = 0;
+    fence_mbar_init();
+  }
   slim_pdl_trigger();
   slim_pdl_wait();
-  const SlimSched sc = slim_sched_build(p.lengths, p.batch, p.t_cap, p.workers, 1, s_prefix, p.status, 0);
+  const SlimSched sc = slim_sched_build(p.lengths, p.batch, p.t_cap, p.workers, 1, s_prefix, p.status, 0);      // (has block barriers)
   const int w = blockIdx.x;
   if (sc.total_tiles == 0 || w >= sc.workers_eff) return;
   const int g_begin = slim_worker_start(sc, w), g_end = slim_worker_start(sc, w + 1);
-  int groups = 1;                                                  // row groups of a tile
-  while (groups < SLIM_TT && 2 * groups * units <= WT) groups *= 2;
-  const int rpg = SLIM_TT / groups, stride = groups > 1 ? units : WT;
-  const int rg = groups > 1 ? min(tid / units, groups) : 0, u0 = groups > 1 ? tid % units : tid;      // rg == groups: no unit
-  const KT* Kc = reinterpret_cast<const KT*>(p.k);
+  const int per_tile = SLIM_TT / ring.rows;                        // stages of a tile
 
-  int buf = 0;
+  if (tid >= WC) {
+    // ---- producer ----
+    if (tid == WC) {
+      const unsigned char* Kc = reinterpret_cast<const unsigned char*>(p.k);
+      int c = 0;
+      bool ok = true;
+      for (int g = g_begin; g < g_end && ok; ++g) {
+        const int b = slim_seq_of_tile(s_prefix, p.batch, g), t0 = (g - s_prefix[b]) * SLIM_TT;
+        const int rows = min(SLIM_TT, min(p.lengths[b], p.t_cap) - t0);
+        const unsigned char* src = Kc + (size_t)slim_cache_row(p, b, t0) * row_bytes;
+        for (int x = 0; x < per_tile; ++x, ++c) {                  // (rows behind the last one are not fetched: their sums are not used)
+          const int st = c % ring.stages, n = min(ring.rows, rows - x * ring.rows);
+          ok = mbar_wait<false>(bar_empty + 8 * st, ((c / ring.stages) & 1) ^ 1, s_abort, p.status);
+          if (!ok) break;
+          if (n <= 0) { mbar_arrive(bar_full + 8 * st); continue; }
+          mbar_arrive_expect_tx(bar_full + 8 * st, (uint32_t)n * row_bytes);
+          bulk_load(smem_u32(keys) + (uint32_t)st * stage_bytes, src + (size_t)x * stage_bytes, (uint32_t)n * row_bytes, bar_full + 8 * st);
+        }
+      }
+      // (the consumers wait for every stage; after a time-out what was issued has landed long since)
+    }
+    return;
+  }
+  if (warp >= used) return;
+  const int rpg = SLIM_TT / ring.groups, rg = warp / ring.warps, r0 = rg * rpg;
+  const int li = lane % LPH, h = (warp - rg * ring.warps) * HPW + lane / LPH;
+  const bool mine = h < H && li * VEC < half;                      // (lanes without pairs add zero)
+  const int j0 = mine ? li * VEC : 0, at = (mine ? h : 0) * dk + j0;
+  f32x2 co[NP], si[NP];                                            // one position
+  if (ROPE)
+#pragma unroll
+    for (int x = 0; x < NP; ++x) {
+      const float4 st = __ldg(reinterpret_cast<const float4*>(p.rope_off + half + j0) + x);
+      co[x] = pack2(st.x, st.z); si[x] = pack2(st.y, st.w);
+    }
+  int c = 0;
   for (int g = g_begin; g < g_end;) {
     const int b = slim_seq_of_tile(s_prefix, p.batch, g);
     const int seg_end = min(g_end, s_prefix[b + 1]);
     const int len = min(max(p.lengths[b], 0), p.t_cap), pos = len - 1;
-    const KT* q = reinterpret_cast<const KT*>(p.q) + (size_t)b * d;
-    float run_m[4], run_l[4];                                      // of (head, row of the tile) number tid + 256 x
+    f32x2 q1[NP], q2[NP];                                          // the query, scaled; zero in lanes without pairs
+    {
+      const KT* q = reinterpret_cast<const KT*>(p.q) + (size_t)b * d + at;
+      KeyVec<KT>::unpack(__ldg(reinterpret_cast<const uint4*>(q)), q1);
+      KeyVec<KT>::unpack(__ldg(reinterpret_cast<const uint4*>(q + half)), q2);
+      const float f = mine ? p.qscale : 0.f;
 #pragma unroll
-    for (int x = 0; x < 4; ++x) { run_m[x] = -INFINITY; run_l[x] = 0.f; }
-    for (; g < seg_end; ++g, buf ^= 1) {
+      for (int x = 0; x < NP; ++x) {
+        q1[x] = mine ? mul2(q1[x], pack2(f, f)) : pack2(0.f, 0.f);
+        q2[x] = mine ? mul2(q2[x], pack2(f, f)) : pack2(0.f, 0.f);
+      }
+    }
+    float* out = scores + ((size_t)b * H + (h < H ? h : 0)) * p.t_cap;
+    float run_m = -INFINITY, run_l = 0.f;
+    for (; g < seg_end; ++g) {
       const int t0 = (g - s_prefix[b]) * SLIM_TT;
-      const KT* rows = Kc + (size_t)slim_cache_row(p, b, t0) * d;
-      const int last = min(SLIM_TT - 1, len - 1 - t0);             // rows behind it are read as it, and not used
-      float* out = s_part + buf * SLIM_TT * ld;
-      for (int u = u0; u < units && rg < groups; u += stride) {
-        const int h = u / per_head, j0 = (u - h * per_head) * VEC, at = h * dk + j0, r0 = rg * rpg;
-        // the query, scaled and turned to the distance of this thread's first row
-        f32x2 z1[NP], z2[NP], co[NP], si[NP];
-        KeyVec<KT>::unpack(__ldg(reinterpret_cast<const uint4*>(q + at)), z1);
-        KeyVec<KT>::unpack(__ldg(reinterpret_cast<const uint4*>(q + at + half)), z2);
-        const int dist = max(pos - t0 - r0, 0);
+      // turned to the distance of this group's first row
+      f32x2 z1[NP], z2[NP];
+      const int dist = max(pos - t0 - r0, 0);
 #pragma unroll
-        for (int x = 0; x < NP; ++x) {
-          const f32x2 sc2 = pack2(p.qscale, p.qscale);
-          z1[x] = mul2(z1[x], sc2); z2[x] = mul2(z2[x], sc2);
-          if (ROPE) {
-            const float4 cb = __ldg(reinterpret_cast<const float4*>(p.rope_base + (size_t)(dist / SLIM_TT) * half + j0) + x);
-            const float4 cf = __ldg(reinterpret_cast<const float4*>(p.rope_off + (dist % SLIM_TT) * half + j0) + x);
-            const float4 st = __ldg(reinterpret_cast<const float4*>(p.rope_off + half + j0) + x);      // one position
-            const f32x2 c = pack2(cb.x * cf.x - cb.y * cf.y, cb.z * cf.z - cb.w * cf.w), s = pack2(cb.y * cf.x + cb.x * cf.y, cb.w * cf.z + cb.z * cf.w);
-            const f32x2 a = fma2(z2[x], s, mul2(z1[x], c));
-            z2[x] = sub2(mul2(z2[x], c), mul2(z1[x], s));
-            z1[x] = a;
-            co[x] = pack2(st.x, st.z); si[x] = pack2(st.y, st.w);
-          }
+      for (int x = 0; x < NP; ++x) {
+        z1[x] = q1[x]; z2[x] = q2[x];
+        if (ROPE) {
+          const float4 cb = __ldg(reinterpret_cast<const float4*>(p.rope_base + (size_t)(dist / SLIM_TT) * half + j0) + x);
+          const float4 cf = __ldg(reinterpret_cast<const float4*>(p.rope_off + (dist % SLIM_TT) * half + j0) + x);
+          const f32x2 fx = pack2(cf.x, cf.z), fy = pack2(cf.y, cf.w), bx = pack2(cb.x, cb.z), by = pack2(cb.y, cb.w);
+          const f32x2 cs = sub2(mul2(bx, fx), mul2(by, fy)), sn = fma2(by, fx, mul2(bx, fy));
+          z1[x] = fma2(q2[x], sn, mul2(q1[x], cs));
+          z2[x] = sub2(mul2(q2[x], cs), mul2(q1[x], sn));
         }
-        for (int r = 0; r < rpg; r += 4) {
-          uint4 k1[4], k2[4];
-#pragma unroll
-          for (int x = 0; x < 4; ++x) {
-            const KT* row = rows + (size_t)min(r0 + min(r + x, rpg - 1), last) * d + at;
-            k1[x] = __ldg(reinterpret_cast<const uint4*>(row));
-            k2[x] = __ldg(reinterpret_cast<const uint4*>(row + half));
-          }
-#pragma unroll
-          for (int x = 0; x < 4; ++x) {
+      }
+      float keep = -INFINITY;                                      // this lane's row of the last LPH ones
+      for (int y = 0; y < per_tile; ++y, ++c) {
+        const int st = c % ring.stages, a0 = max(r0, y * ring.rows), a1 = min(r0 + rpg, (y + 1) * ring.rows);
+        // (also for stages of other groups' rows: a warp must not arrive twice on a barrier before the others have once.
+        // Gave up: reported, and the loop runs on)
+        mbar_wait<false>(bar_full + 8 * st, (c / ring.stages) & 1, s_abort, p.status);
+        if (a0 < a1) {
+          const unsigned char* row = keys + (size_t)st * stage_bytes + (size_t)(a0 - y * ring.rows) * row_bytes + (size_t)at * sizeof(KT);
+#pragma unroll 2
+          for (int r = a0; r < a1; ++r, row += row_bytes) {
             f32x2 f1[NP], f2[NP];
-            KeyVec<KT>::unpack(k1[x], f1);
-            KeyVec<KT>::unpack(k2[x], f2);
-            f32x2 a = mul2(f1[0], z1[0]), c = mul2(f2[0], z2[0]);
+            KeyVec<KT>::unpack(*reinterpret_cast<const uint4*>(row), f1);
+            KeyVec<KT>::unpack(*reinterpret_cast<const uint4*>(row + half * sizeof(KT)), f2);
+            f32x2 a = mul2(f1[0], z1[0]), e = mul2(f2[0], z2[0]);
 #pragma unroll
-            for (int y = 1; y < NP; ++y) { a = fma2(f1[y], z1[y], a); c = fma2(f2[y], z2[y], c); }
-            if (r + x < rpg) out[(r0 + r + x) * ld + u] = sum2(add2(a, c));
+            for (int x = 1; x < NP; ++x) { a = fma2(f1[x], z1[x], a); e = fma2(f2[x], z2[x], e); }
+            float v = sum2(add2(a, e));
+            if (!mine) v = 0.f;                 // (a key element times zero could be NaN)
+#pragma unroll
+            for (int o = 1; o < LPH; o <<= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+            if (r % LPH == li) keep = v;
             if (ROPE)
 #pragma unroll
-              for (int y = 0; y < NP; ++y) {                       // one position nearer: times e^{i theta}
-                const f32x2 n1 = sub2(mul2(z1[y], co[y]), mul2(z2[y], si[y]));
-                z2[y] = fma2(z1[y], si[y], mul2(z2[y], co[y]));
-                z1[y] = n1;
+              for (int x = 0; x < NP; ++x) {                       // one position nearer: times e^{i theta}
+                const f32x2 n1 = sub2(mul2(z1[x], co[x]), mul2(z2[x], si[x]));
+                z2[x] = fma2(z1[x], si[x], mul2(z2[x], co[x]));
+                z1[x] = n1;
               }
+            if ((r + 1) % LPH == 0 || r + 1 == r0 + rpg) {         // every lane of the head has its row: row r - r % LPH + li
+              const int t = t0 + r - r % LPH + li;
+              if (li <= r % LPH && li >= r0 % LPH && t < len && h < H) {
+                out[t] = keep;
+                const float top = fmaxf(run_m, keep);
+                if (top != -INFINITY) run_l = run_l * ex2_approx(run_m - top) + ex2_approx(keep - top);
+                run_m = top;
+              }
+            }
           }
         }
-      }
-      __syncthreads();                                             // (two buffers: the next tile may be written while this one is read)
-#pragma unroll
-      for (int x = 0; x < 4; ++x) {
-        const int e = tid + WT * x, h = e / SLIM_TT, r = e % SLIM_TT;
-        if (h >= H || t0 + r >= len) continue;
-        const float* a = out + r * ld + h * per_head;
-        float s = 0.f;
-        for (int y = 0; y < per_head; ++y) s += a[y];
-        scores[((size_t)b * H + h) * p.t_cap + t0 + r] = s;
-        const float top = fmaxf(run_m[x], s);
-        if (top != -INFINITY) run_l[x] = run_l[x] * exp2f(run_m[x] - top) + exp2f(s - top);
-        run_m[x] = top;
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar_empty + 8 * st);
       }
     }
-    // the unit's (maximum, sum) of every head: over the 16 threads that share it
+    // (maximum, sum) of the head over this group's rows
 #pragma unroll
-    for (int x = 0; x < 4; ++x) {
-      float m = run_m[x], l = run_l[x];
-#pragma unroll
-      for (int o = 8; o > 0; o >>= 1) {
-        const float m1 = __shfl_xor_sync(0xffffffffu, m, o), l1 = __shfl_xor_sync(0xffffffffu, l, o), top = fmaxf(m, m1);
-        if (top != -INFINITY) l = l * exp2f(m - top) + l1 * exp2f(m1 - top);
-        m = top;
-      }
-      const int e = tid + WT * x, h = e / SLIM_TT;
-      if (e % SLIM_TT == 0 && h < H) part[(size_t)(w + b) * H + h] = make_float2(m, l);
+    for (int o = 1; o < LPH; o <<= 1) {
+      const float m1 = __shfl_xor_sync(0xffffffffu, run_m, o), l1 = __shfl_xor_sync(0xffffffffu, run_l, o), top = fmaxf(run_m, m1);
+      if (top != -INFINITY) run_l = run_l * ex2_approx(run_m - top) + l1 * ex2_approx(m1 - top);
+      run_m = top;
     }
+    if (li == 0 && h < H) part[((size_t)(w + b) * ring.groups + rg) * H + h] = make_float2(run_m, run_l);
   }
 }
 
 // Reference exponent and 1 / denominator of every (sequence, head) from its units' parts: a warp each.
-__global__ void __launch_bounds__(256) slim_weights_join_kernel(const SlimDecodeParams p, const float2* __restrict__ part, float* __restrict__ m_out,
-                                                                float* __restrict__ inv_out) {
+__global__ void __launch_bounds__(256) slim_weights_join_kernel(const SlimDecodeParams p, const float2* __restrict__ part, int groups,
+                                                                float* __restrict__ m_out, float* __restrict__ inv_out) {
   extern __shared__ int s_prefix2[];
   slim_pdl_trigger();
   slim_pdl_wait();
@@ -162,8 +202,8 @@ __global__ void __launch_bounds__(256) slim_weights_join_kernel(const SlimDecode
   float m = -INFINITY, l = 0.f;
   if (s_prefix2[b + 1] > s_prefix2[b]) {
     const int w0 = slim_worker_of_tile(sc, s_prefix2[b]), w1 = slim_worker_of_tile(sc, s_prefix2[b + 1] - 1);
-    for (int w = w0 + lane; w <= w1; w += 32) {
-      const float2 v = part[(size_t)(w + b) * p.H + h];
+    for (int i = (w0 + b) * groups + lane; i < (w1 + 1 + b) * groups; i += 32) {
+      const float2 v = part[(size_t)i * p.H + h];
       const float top = fmaxf(m, v.x);
       if (top != -INFINITY) l = l * exp2f(m - top) + v.y * exp2f(v.x - top);
       m = top;
@@ -402,26 +442,37 @@ cudaError_t launch_move(const slim_ctx* ctx, const slim_cache* c, void* base, si
 
 }  // namespace
 
-// Workers of the score kernel: two CTAs an SM.
-int slim_weights_workers(const slim_ctx* ctx) { return 2 * ctx->num_sms; }
+int slim_weights_workers(const slim_ctx* ctx) { return ctx->num_sms; }
 
 cudaError_t slim_launch_weights(const slim_ctx* ctx, const SlimDecodeParams& p_in, float* scores, float2* part, float* m, float* inv_l,
                                 float* acc, cudaStream_t st) {
   SlimDecodeParams p = p_in;
-  // whole 16-byte vectors of a head's halves (rows are then 16-byte aligned too); 8-bit codes and other widths take the
-  // score kernel of slim_decode's CUDA-core path
-  const int vec = p.kdtype == SLIM_BF16 ? 8 : 4;
-  const size_t smem = sizeof(float) * 2 * SLIM_TT * (size_t)(p.d / (2 * vec) + 4) + sizeof(int) * (p.batch + 1);
+  // The one-pass kernel wants whole 16-byte vectors of a head's halves (rows are then multiples of 16 bytes too), all
+  // heads of a row in 16 warps, and a ring of at least four rows; 8-bit codes and other shapes take the score kernel of
+  // slim_decode's CUDA-core path.
+  const int vec = p.kdtype == SLIM_BF16 ? 8 : 4, per_head = (p.half + vec - 1) / vec;
+  const int lph = per_head <= 4 ? 4 : per_head <= 8 ? 8 : per_head <= 16 ? 16 : 32;
+  const size_t row = (size_t)p.d * (p.kdtype == SLIM_BF16 ? 2 : 4);
+  const size_t fixed = sizeof(int) * (p.batch + 4) + 16 * 16 + 128, room = 227 * 1024 - fixed;
+  WeightsRing ring = {SLIM_TT, 0, 1, (p.H * lph + 31) / 32};
+  while (2 * ring.groups * ring.warps <= WC / 32 && ring.groups < SLIM_TT) ring.groups *= 2;
+  while (ring.rows > 1 && room / (row * ring.rows) < 4) ring.rows /= 2;
+  ring.stages = (int)(room / (row * ring.rows));
+  if (ring.stages > 8) ring.stages = 8;
   cudaError_t e;
-  if (p.kdtype != SLIM_FP8 && p.half % vec == 0 && smem <= 200 * 1024) {
+  if (p.kdtype != SLIM_FP8 && p.half % vec == 0 && ring.warps <= WC / 32 && ring.stages >= 4) {
     p.workers = slim_weights_workers(ctx);
-    auto kern = p.kdtype == SLIM_BF16 ? (p.rope ? slim_weights_scores_kernel<__nv_bfloat16, true> : slim_weights_scores_kernel<__nv_bfloat16, false>)
-                                      : (p.rope ? slim_weights_scores_kernel<float, true> : slim_weights_scores_kernel<float, false>);
-    if (smem > 48 * 1024 && (e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem)) != cudaSuccess) return e;
-    e = slim_launch_pdl(kern, dim3(p.workers), dim3(WT), smem, st, p, scores, part);
+    const size_t smem = (size_t)ring.stages * ring.rows * row + fixed;
+#define SLIM_W(KT, L) (p.rope ? slim_weights_scores_kernel<KT, true, L> : slim_weights_scores_kernel<KT, false, L>)
+#define SLIM_WL(KT) (lph == 4 ? SLIM_W(KT, 4) : lph == 8 ? SLIM_W(KT, 8) : lph == 16 ? SLIM_W(KT, 16) : SLIM_W(KT, 32))
+    auto kern = p.kdtype == SLIM_BF16 ? SLIM_WL(__nv_bfloat16) : SLIM_WL(float);
+#undef SLIM_WL
+#undef SLIM_W
+    if ((e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem)) != cudaSuccess) return e;
+    e = slim_launch_pdl(kern, dim3(p.workers), dim3(WT), smem, st, p, scores, part, ring);
     if (e == cudaSuccess)
       e = slim_launch_pdl(slim_weights_join_kernel, dim3((p.H + 7) / 8, p.batch), dim3(256), sizeof(int) * (p.batch + 1), st, p,
-                          (const float2*)part, m, inv_l);
+                          (const float2*)part, ring.groups, m, inv_l);
   } else {
     e = slim_launch_scores(ctx, p, scores, st);
     if (e == cudaSuccess) e = slim_launch_pdl(slim_weights_stat_kernel, dim3(p.H, p.batch), dim3(256), 0, st, p, (const float*)scores, m, inv_l);

@@ -218,7 +218,7 @@ cudaError_t slim_launch_commit(const slim_ctx* ctx, const slim_cache* c, const v
 // cache budget (slim_budget.cu); scores: the CUDA-core score kernel alone, [batch][H][t_cap] (slim_generic.cu)
 cudaError_t slim_launch_scores(const slim_ctx* ctx, const SlimDecodeParams& p, float* scores, cudaStream_t st);
 int slim_weights_workers(const slim_ctx* ctx);
-// part: (workers + batch) x H (maximum, sum)
+// part: (workers + batch) x up to 16 row groups x H (maximum, sum)
 cudaError_t slim_launch_weights(const slim_ctx* ctx, const SlimDecodeParams& p, float* scores, float2* part, float* m, float* inv_l,
                                 float* acc, cudaStream_t st);
 cudaError_t slim_launch_evict(const slim_ctx* ctx, const slim_cache* c, const int32_t* lengths, float* acc, int budget, int recent,
