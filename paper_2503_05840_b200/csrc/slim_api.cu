@@ -804,7 +804,7 @@ slim_status slim_accumulate_weights(slim_ctx* ctx, const void* q, const slim_cac
 
 size_t slim_evict_workspace_bytes(const slim_ctx* ctx, int batch, int t_cap) {
   if (!ctx || batch <= 0 || t_cap <= 0 || batch > SLIM_MAX_BATCH) return 0;
-  return 256;
+  return align256(sizeof(float) * (size_t)batch * t_cap);              // the kept rows' weights, on their way
 }
 
 slim_status slim_evict(slim_ctx* ctx, slim_cache* cache, const int32_t* lengths, float* acc, int budget, int recent, int32_t* kept,
@@ -813,7 +813,7 @@ slim_status slim_evict(slim_ctx* ctx, slim_cache* cache, const int32_t* lengths,
   if (budget <= 0 || recent < 0 || recent > budget || ((uintptr_t)workspace & 255) || (((uintptr_t)acc | (uintptr_t)kept) & 3))
     return SLIM_ERR_INVALID_ARG;
   if (!current_device_is(ctx)) return SLIM_ERR_INVALID_ARG;
-  return launched(slim_launch_evict(ctx, cache, lengths, acc, budget, recent, kept, (cudaStream_t)stream));
+  return launched(slim_launch_evict(ctx, cache, lengths, acc, budget, recent, kept, static_cast<float*>(workspace), (cudaStream_t)stream));
 }
 
 slim_status slim_device_status(slim_ctx* ctx, void* stream) {

@@ -269,11 +269,13 @@ __global__ void __launch_bounds__(256) slim_weights_add_kernel(const SlimDecodeP
 }
 
 // ---------------------------------------------------------------- eviction
-// Which rows stay.  One block per sequence: the (budget - recent)-th largest weight of the candidate rows by a radix
-// selection on the order-preserving integer form of the floats (four passes of eight bits), then one pass that counts
-// per warp and one that writes the kept indices in order: every row above the threshold, and of the rows equal to it
-// the first ones.
-constexpr int SEL_THREADS = 1024, SEL_WARPS = SEL_THREADS / 32;
+// Which rows stay.  A cluster of CL CTAs per sequence, each warp a contiguous piece of the rows: the (budget - recent)-th
+// largest weight of the candidate rows by a radix selection on the order-preserving integer form of the floats (four
+// passes of eight bits; the counts of a pass are summed over the cluster), then one pass that counts per warp and one
+// that writes the kept indices in order: every row above the threshold, and of the rows equal to it the first ones.
+// Latency-bound: the keys are read once into shared memory (a CTA's share up to SEL_KEYS; longer ones are read again from
+// L2 in every pass), and long contexts take eight CTAs, short ones one, which saves the cluster's barriers.
+constexpr int SEL_THREADS = 1024, SEL_WARPS = SEL_THREADS / 32, SEL_KEYS = 48 * 1024;
 
 __device__ __forceinline__ uint32_t order_key(float f) {
   if (f != f) return 0u;                              // NaN: below every number
@@ -281,44 +283,83 @@ __device__ __forceinline__ uint32_t order_key(float f) {
   return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
 }
 
+struct SelShared {
+  unsigned hist[2][256], sum[256];                    // this CTA's counts of a pass (two buffers), the cluster's
+  int gt[SEL_WARPS], eq[SEL_WARPS];
+  int total[2];                                       // rows above and equal to the threshold in this CTA
+  unsigned prefix, need;
+};
+
+template <int CL>
 __global__ void __launch_bounds__(SEL_THREADS)
-slim_evict_select_kernel(const int32_t* __restrict__ lengths, const float* __restrict__ acc, int t_cap, int budget, int recent,
-                         int32_t* __restrict__ kept, int* status) {
-  __shared__ unsigned hist[256];
-  __shared__ int s_gt[SEL_WARPS], s_eq[SEL_WARPS];
-  __shared__ unsigned s_prefix, s_need;
-  const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+slim_evict_select_kernel(const int32_t* __restrict__ lengths, const float* __restrict__ acc, int t_cap, int budget, int recent, int staged_cap,
+                         int32_t* __restrict__ kept, float* __restrict__ kept_acc, int* status) {
+  __shared__ SelShared sh;
+  extern __shared__ uint32_t s_key[];                 // [staged_cap]
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, b = blockIdx.x / CL, rank = CL > 1 ? (int)cluster_ctarank() : 0;
+  const uint32_t sh_addr = smem_u32(&sh);
+  auto sync_all = [&]() { if (CL > 1) cluster_sync_all(); else __syncthreads(); };
+  auto peer_word = [&](const void* mine, int r) -> unsigned {           // the word at this place in CTA r's shared memory
+    if (CL == 1) return *reinterpret_cast<const unsigned*>(mine);
+    unsigned v;
+    asm volatile("ld.shared::cluster.u32 %0, [%1];"
+                 : "=r"(v) : "r"(mapa(sh_addr + (uint32_t)(reinterpret_cast<const char*>(mine) - reinterpret_cast<const char*>(&sh)), r)));
+    return v;
+  };
   slim_pdl_trigger();
   slim_pdl_wait();
   int len = lengths[b];
-  if (len > t_cap) { len = t_cap; if (tid == 0) atomicMax(status, (int)SLIM_ERR_CAPACITY); }
+  if (len > t_cap) { len = t_cap; if (tid == 0 && rank == 0) atomicMax(status, (int)SLIM_ERR_CAPACITY); }
   if (len < 0) len = 0;
   int32_t* K = kept + (size_t)b * budget;
-  if (len <= budget) {
-    for (int j = tid; j < budget; j += SEL_THREADS) K[j] = j < len ? j : -1;
+  if (len <= budget) {                                // (the whole cluster)
+    for (int j = rank * SEL_THREADS + tid; j < budget; j += CL * SEL_THREADS) K[j] = j < len ? j : -1;
     return;
   }
   const int cand = len - recent, need = budget - recent;          // 0 <= need < cand
   const float* A = acc + (size_t)b * t_cap;
+  const int seg = ((len + CL * SEL_WARPS - 1) / (CL * SEL_WARPS) + 31) & ~31;
+  const int c0 = min(len, rank * SEL_WARPS * seg), c1 = min(len, c0 + SEL_WARPS * seg);       // this CTA's rows
+  const int lo = min(len, c0 + warp * seg), hi = min(c1, lo + seg);                           // this warp's
+  const bool staged = c1 - c0 <= staged_cap;
+  if (staged) {
+#pragma unroll 4
+    for (int t = c0 + tid; t < c1; t += SEL_THREADS) s_key[t - c0] = order_key(A[t]);
+  }
+  auto key_at = [&](int t) -> uint32_t { return staged ? s_key[t - c0] : order_key(A[t]); };
+  for (int i = tid; i < 512; i += SEL_THREADS) (&sh.hist[0][0])[i] = 0;
+  __syncthreads();
   unsigned prefix = 0, left = (unsigned)need;                      // the left-th largest among the keys that share the prefix
   if (need > 0) {
-    for (int shift = 24; shift >= 0; shift -= 8) {
-      for (int i = tid; i < 256; i += SEL_THREADS) hist[i] = 0;
-      __syncthreads();
-      for (int t0 = 0; t0 < cand; t0 += SEL_THREADS) {
-        const int t = t0 + tid;
-        const uint32_t key = t < cand ? order_key(A[t]) : 0u;
-        const bool in = t < cand && (shift == 24 || (key >> (shift + 8)) == prefix);
+    int pass = 0;
+    for (int shift = 24; shift >= 0; shift -= 8, ++pass) {
+      unsigned* hist = sh.hist[pass & 1];
+      for (int t0 = lo; t0 < min(hi, cand); t0 += 32) {
+        const int t = t0 + lane;
+        const uint32_t key = t < hi && t < cand ? key_at(t) : 0u;
+        const bool in = t < hi && t < cand && (shift == 24 || (key >> (shift + 8)) == prefix);
         const unsigned active = __ballot_sync(0xffffffffu, in);
         if (in) {                                                  // one atomic a distinct digit and warp
           const unsigned digit = (key >> shift) & 255u, same = __match_any_sync(active, digit);
           if (lane == __ffs(same) - 1) atomicAdd(&hist[digit], __popc(same));
         }
       }
+      sync_all();
+      if (tid < 256) {
+        unsigned v[CL], a = 0;
+#pragma unroll
+        for (int r = 0; r < CL; ++r) v[r] = peer_word(&hist[tid], r);
+#pragma unroll
+        for (int r = 0; r < CL; ++r) a += v[r];
+        sh.sum[tid] = a;
+      } else if (pass > 0 && tid < 512) {
+        sh.hist[(pass + 1) & 1][tid - 256] = 0;                    // (last read before the barrier above: clear for the next pass)
+      }
       __syncthreads();
       if (warp == 0) {                                             // lane k: digits 255 - 8 k .. 248 - 8 k, from the top
         unsigned c[8], sum = 0;
-        for (int i = 0; i < 8; ++i) { c[i] = hist[255 - 8 * lane - i]; sum += c[i]; }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) { c[i] = sh.sum[255 - 8 * lane - i]; sum += c[i]; }
         unsigned incl = sum;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
@@ -328,52 +369,70 @@ slim_evict_select_kernel(const int32_t* __restrict__ lengths, const float* __res
         unsigned above = incl - sum;
         if (above < left && left <= incl)
           for (int i = 0; i < 8; ++i) {
-            if (left <= above + c[i]) { s_prefix = (prefix << 8) | (255 - 8 * lane - i); s_need = left - above; break; }
+            if (left <= above + c[i]) { sh.prefix = (prefix << 8) | (255 - 8 * lane - i); sh.need = left - above; break; }
             above += c[i];
           }
       }
       __syncthreads();
-      prefix = s_prefix; left = s_need;
+      prefix = sh.prefix; left = sh.need;
+      // (a buffer is counted into again two passes later, behind the next pass's barrier, by when all CTAs have read it)
     }
   }
   // rows with key > prefix stay, and the first `left` of those equal to it (none of either when need = 0)
   const uint32_t thr = need > 0 ? prefix : 0xffffffffu;
-  const int seg = ((len + SEL_WARPS - 1) / SEL_WARPS + 31) & ~31, lo = min(len, warp * seg), hi = min(len, lo + seg);
   int gt = 0, eq = 0;
   for (int t0 = lo; t0 < hi; t0 += 32) {
     const int t = t0 + lane;
-    const uint32_t key = t < hi && t < cand ? order_key(A[t]) : 0u;
+    const uint32_t key = t < hi && t < cand ? key_at(t) : 0u;
     gt += __popc(__ballot_sync(0xffffffffu, t < hi && (t >= cand || (need > 0 && key > thr))));
     eq += __popc(__ballot_sync(0xffffffffu, t < hi && t < cand && need > 0 && key == thr));
   }
-  if (lane == 0) { s_gt[warp] = gt; s_eq[warp] = eq; }
+  if (lane == 0) { sh.gt[warp] = gt; sh.eq[warp] = eq; }
   __syncthreads();
-  int eq_before = 0, out = 0;
+  if (warp == 0) {
+    int a = sh.gt[lane], e = sh.eq[lane];
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) { a += __shfl_xor_sync(0xffffffffu, a, o); e += __shfl_xor_sync(0xffffffffu, e, o); }
+    if (lane == 0) { sh.total[0] = a; sh.total[1] = e; }
+  }
+  sync_all();
+  int eq_before = 0, out = 0;                                      // equal rows, and kept rows, before this warp's
+  int ta[CL], te[CL];
+#pragma unroll
+  for (int r = 0; r < CL; ++r) { ta[r] = (int)peer_word(&sh.total[0], r); te[r] = (int)peer_word(&sh.total[1], r); }
+#pragma unroll
+  for (int r = 0; r < CL; ++r) {
+    if (r >= rank) break;
+    const int a = ta[r], e = te[r];
+    out += a + min(e, max((int)left - eq_before, 0));
+    eq_before += e;
+  }
   for (int w = 0; w < warp; ++w) {
-    out += s_gt[w] + min(s_eq[w], max((int)left - eq_before, 0));
-    eq_before += s_eq[w];
+    out += sh.gt[w] + min(sh.eq[w], max((int)left - eq_before, 0));
+    eq_before += sh.eq[w];
   }
   for (int t0 = lo; t0 < hi; t0 += 32) {
     const int t = t0 + lane;
-    const uint32_t key = t < hi && t < cand ? order_key(A[t]) : 0u;
+    const uint32_t key = t < hi && t < cand ? key_at(t) : 0u;
     const bool is_eq = t < hi && t < cand && need > 0 && key == thr;
     const unsigned eqs = __ballot_sync(0xffffffffu, is_eq), below = (1u << lane) - 1u;
     const bool keep = t < hi && (t >= cand || (need > 0 && key > thr) || (is_eq && eq_before + __popc(eqs & below) < (int)left));
     const unsigned ks = __ballot_sync(0xffffffffu, keep);
     if (keep) {
       const int j = out + __popc(ks & below);
-      if (j < budget) K[j] = t;
+      if (j < budget) { K[j] = t; kept_acc[(size_t)b * t_cap + j] = A[t]; }
     }
     out += __popc(ks);
     eq_before += __popc(eqs);
   }
+  sync_all();                                                      // (a CTA's totals may still be read by the others)
 }
 
 // The kept rows move to rows 0 .. budget - 1, in place.  Row j comes from row kept[j] >= j, so a block that owns a
 // column slice and goes through the rows in order may write a chunk as soon as all sources up to that chunk have been
-// read: sources of later chunks lie behind everything it overwrites.  The last block of a sequence moves the weights
-// and clears those of the rows that became free.
-constexpr int MV_THREADS = 256, MV_COLS = 8, MV_ROWS = MV_THREADS / MV_COLS, MV_UNROLL = 4;
+// read; sources of later chunks lie behind everything it overwrites, so the next chunk is on its way meanwhile.
+// The last MV_ACC blocks of a sequence write the weights and clear those of the rows that became free.
+constexpr int MV_THREADS = 256, MV_COLS = 8, MV_ROWS = MV_THREADS / MV_COLS, MV_UNROLL = 4, MV_ACC = 4;
 
 __device__ __forceinline__ long long storage_row(const int32_t* table, int page_rows, int max_pages, int num_pages, int t_cap, int b, int t,
                                                  int* status) {
@@ -387,57 +446,86 @@ template <typename VT>
 __global__ void __launch_bounds__(MV_THREADS)
 slim_evict_move_kernel(unsigned char* __restrict__ base, int vecs, const int32_t* __restrict__ lengths, int t_cap, int budget,
                        const int32_t* __restrict__ kept, const int32_t* __restrict__ table, int page_rows, int max_pages, int num_pages,
-                       float* __restrict__ acc, int* status) {
+                       float* __restrict__ acc, const float* __restrict__ kept_acc, int* status) {
   const int b = blockIdx.y, tid = threadIdx.x;
   slim_pdl_trigger();
   slim_pdl_wait();
   const int len = min(max(lengths[b], 0), t_cap);
   if (len <= budget) return;
   const int32_t* K = kept + (size_t)b * budget;
-  if (acc && blockIdx.x == gridDim.x - 1) {
+  const int slices = (vecs + MV_COLS - 1) / MV_COLS;
+  if ((int)blockIdx.x >= slices) {
     float* A = acc + (size_t)b * t_cap;
-    for (int j0 = 0; j0 < budget; j0 += MV_THREADS) {
-      const int j = j0 + tid;
-      const float v = j < budget ? A[K[j]] : 0.f;
-      __syncthreads();
-      if (j < budget) A[j] = v;
-      __syncthreads();
-    }
-    for (int t = budget + tid; t < len; t += MV_THREADS) A[t] = 0.f;
+    const float* N = kept_acc + (size_t)b * t_cap;
+    for (int t = ((int)blockIdx.x - slices) * MV_THREADS + tid; t < len; t += MV_ACC * MV_THREADS) A[t] = t < budget ? N[t] : 0.f;
     return;
   }
   const int col = blockIdx.x * MV_COLS + tid % MV_COLS, r = tid / MV_COLS;
   VT* K0 = reinterpret_cast<VT*>(base);
-  for (int j0 = 0; j0 < budget; j0 += MV_ROWS * MV_UNROLL) {
-    VT v[MV_UNROLL];
-    long long dst[MV_UNROLL];
+  constexpr int CHUNK = MV_ROWS * MV_UNROLL;
+  VT v[2][MV_UNROLL];
+  long long dst[2][MV_UNROLL];
+  int from[MV_UNROLL];                                             // old rows of the chunk after the next
+  auto indices = [&](int j0) {
+#pragma unroll
+    for (int x = 0; x < MV_UNROLL; ++x) {
+      const int j = j0 + x * MV_ROWS + r;
+      from[x] = j < budget ? K[j] : -1;
+    }
+  };
+  auto load = [&](int j0, VT (&v)[MV_UNROLL], long long (&dst)[MV_UNROLL]) {
 #pragma unroll
     for (int x = 0; x < MV_UNROLL; ++x) {
       const int j = j0 + x * MV_ROWS + r;
       dst[x] = -1;
-      if (j < budget && col < vecs) {
-        const int t = K[j];
-        if (t != j) {
-          const long long from = storage_row(table, page_rows, max_pages, num_pages, t_cap, b, t, status);
-          const long long to = storage_row(table, page_rows, max_pages, num_pages, t_cap, b, j, status);
-          if (from >= 0 && to >= 0) { dst[x] = to * vecs + col; v[x] = K0[from * vecs + col]; }
-        }
+      if (from[x] >= 0 && from[x] != j && col < vecs) {
+        const long long a = storage_row(table, page_rows, max_pages, num_pages, t_cap, b, from[x], status);
+        const long long z = storage_row(table, page_rows, max_pages, num_pages, t_cap, b, j, status);
+        if (a >= 0 && z >= 0) { dst[x] = z * vecs + col; v[x] = K0[a * vecs + col]; }
       }
     }
-    __syncthreads();                 // all sources up to here have been read
+  };
+  indices(0);
+  load(0, v[0], dst[0]);
+  indices(CHUNK);
+  for (int j0 = 0, k = 0; j0 < budget; j0 += CHUNK, k ^= 1) {
+    // (both arms are the same code with the buffers' names exchanged, so that they stay in registers)
+    if (k == 0) load(j0 + CHUNK, v[1], dst[1]); else load(j0 + CHUNK, v[0], dst[0]);
+    indices(j0 + 2 * CHUNK);
+    __syncthreads();                 // all sources up to this chunk have been read
 #pragma unroll
-    for (int x = 0; x < MV_UNROLL; ++x)
-      if (dst[x] >= 0) K0[dst[x]] = v[x];
+    for (int x = 0; x < MV_UNROLL; ++x) {
+      if (k == 0) { if (dst[0][x] >= 0) K0[dst[0][x]] = v[0][x]; }
+      else        { if (dst[1][x] >= 0) K0[dst[1][x]] = v[1][x]; }
+    }
   }
 }
 
 template <typename VT>
 cudaError_t launch_move(const slim_ctx* ctx, const slim_cache* c, void* base, size_t row_bytes, const int32_t* lengths, int budget,
-                        const int32_t* kept, float* acc, cudaStream_t st) {
+                        const int32_t* kept, float* acc, const float* kept_acc, cudaStream_t st) {
   const int vecs = (int)(row_bytes / sizeof(VT));
-  return slim_launch_pdl(slim_evict_move_kernel<VT>, dim3((vecs + MV_COLS - 1) / MV_COLS + (acc ? 1 : 0), c->batch), dim3(MV_THREADS), 0, st,
+  return slim_launch_pdl(slim_evict_move_kernel<VT>, dim3((vecs + MV_COLS - 1) / MV_COLS + (acc ? MV_ACC : 0), c->batch), dim3(MV_THREADS), 0, st,
                          (unsigned char*)base, vecs, lengths, c->t_cap, budget, kept, c->block_table, c->page_rows, c->max_pages,
-                         c->num_pages, acc, ctx->status);
+                         c->num_pages, acc, kept_acc, ctx->status);
+}
+
+template <int CL>
+cudaError_t launch_select(const slim_ctx* ctx, const slim_cache* c, const int32_t* lengths, const float* acc, int budget, int recent,
+                          int32_t* kept, float* kept_acc, cudaStream_t st) {
+  const int share = ((c->t_cap + CL * SEL_WARPS - 1) / (CL * SEL_WARPS) + 31) / 32 * 32 * SEL_WARPS, staged = share <= SEL_KEYS ? share : 0;
+  auto kern = slim_evict_select_kernel<CL>;
+  cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, SEL_KEYS * 4);
+  if (e != cudaSuccess) return e;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(CL * c->batch); cfg.blockDim = dim3(SEL_THREADS); cfg.dynamicSmemBytes = sizeof(uint32_t) * (size_t)staged; cfg.stream = st;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = CL; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr; cfg.numAttrs = 2;
+  return cudaLaunchKernelEx(&cfg, kern, lengths, acc, c->t_cap, budget, recent, staged, kept, kept_acc, ctx->status);
 }
 
 }  // namespace
@@ -483,19 +571,20 @@ cudaError_t slim_launch_weights(const slim_ctx* ctx, const SlimDecodeParams& p_i
   return e;
 }
 
+// kept_acc: float scratch [batch][t_cap]
 cudaError_t slim_launch_evict(const slim_ctx* ctx, const slim_cache* c, const int32_t* lengths, float* acc, int budget, int recent,
-                              int32_t* kept, cudaStream_t st) {
-  cudaError_t e = slim_launch_pdl(slim_evict_select_kernel, dim3(c->batch), dim3(SEL_THREADS), 0, st, lengths, (const float*)acc, c->t_cap,
-                                  budget, recent, kept, ctx->status);
+                              int32_t* kept, float* kept_acc, cudaStream_t st) {
+  cudaError_t e = c->t_cap >= 8192 ? launch_select<8>(ctx, c, lengths, acc, budget, recent, kept, kept_acc, st)
+                                   : launch_select<1>(ctx, c, lengths, acc, budget, recent, kept, kept_acc, st);
   if (e != cudaSuccess) return e;
   if (ctx->kdtype == SLIM_FP8) {     // codes, then the exponents of the same rows
     const size_t row = (size_t)ctx->d;
-    e = (row & 15) == 0 ? launch_move<uint4>(ctx, c, c->k, row, lengths, budget, kept, acc, st)
-                        : launch_move<unsigned short>(ctx, c, c->k, row, lengths, budget, kept, acc, st);
-    if (e == cudaSuccess) e = launch_move<unsigned char>(ctx, c, c->k_exp, ctx->H, lengths, budget, kept, nullptr, st);
+    e = (row & 15) == 0 ? launch_move<uint4>(ctx, c, c->k, row, lengths, budget, kept, acc, kept_acc, st)
+                        : launch_move<unsigned short>(ctx, c, c->k, row, lengths, budget, kept, acc, kept_acc, st);
+    if (e == cudaSuccess) e = launch_move<unsigned char>(ctx, c, c->k_exp, ctx->H, lengths, budget, kept, nullptr, nullptr, st);
     return e;
   }
   const size_t row = (size_t)ctx->d * (ctx->kdtype == SLIM_BF16 ? 2 : 4);
-  if ((row & 15) == 0) return launch_move<uint4>(ctx, c, c->k, row, lengths, budget, kept, acc, st);
-  return launch_move<unsigned short>(ctx, c, c->k, row, lengths, budget, kept, acc, st);
+  if ((row & 15) == 0) return launch_move<uint4>(ctx, c, c->k, row, lengths, budget, kept, acc, kept_acc, st);
+  return launch_move<unsigned short>(ctx, c, c->k, row, lengths, budget, kept, acc, kept_acc, st);
 }

@@ -222,4 +222,4 @@ int slim_weights_workers(const slim_ctx* ctx);
 cudaError_t slim_launch_weights(const slim_ctx* ctx, const SlimDecodeParams& p, float* scores, float2* part, float* m, float* inv_l,
                                 float* acc, cudaStream_t st);
 cudaError_t slim_launch_evict(const slim_ctx* ctx, const slim_cache* c, const int32_t* lengths, float* acc, int budget, int recent,
-                              int32_t* kept, cudaStream_t st);
+                              int32_t* kept, float* kept_acc, cudaStream_t st);

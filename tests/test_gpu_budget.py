@@ -230,3 +230,62 @@ def test_decode_with_weights_and_eviction_go_together():
         assert [len(h) for h in host] == [48, 34]
     finally:
         lay.close()
+
+
+@pytest.mark.parametrize("d,H,lengths,budget,recent", [(16, 1, [20000, 8191, 700, 0, 12345], 5000, 100), (16, 1, [9000, 8999], 8998, 0),
+                                                       (2, 1, [450_001], 100_000, 7), (16, 1, [8192], 1, 0), (16, 1, [30000], 29999, 29999)])
+def test_evict_of_long_contexts(d, H, lengths, budget, recent):
+    g = np.random.default_rng(budget)
+    t_cap, batch = max(max(lengths) + 3, 8192), len(lengths)
+    lay = SlimLayer(d, H, d // H, 0.0, "f32", batch, t_cap, DEV)
+    try:
+        a = np.where(g.random((batch, t_cap)) < 0.4, 0.25, g.random((batch, t_cap))).astype(np.float32)
+        k = g.standard_normal((batch, t_cap, d)).astype(np.float32)
+        lay.k.copy_(torch.from_numpy(k))
+        acc = torch.from_numpy(a).to(DEV)
+        kept = lay.evict(torch.tensor(lengths, dtype=torch.int32, device=DEV), acc, budget, recent).cpu().numpy()
+        assert lay.device_status() == B.SLIM_OK
+        got, got_acc = lay.k.cpu().numpy(), acc.cpu().numpy()
+        for b, L in enumerate(lengths):
+            keep = do.evict(a[b], L, budget, recent)
+            assert list(kept[b]) == keep + [-1] * (budget - len(keep)), b
+            want, want_acc = k[b].copy(), a[b].copy()
+            if L > budget:
+                want[:budget] = k[b][keep]
+                want_acc[:L] = 0
+                want_acc[:budget] = a[b][keep]
+            assert np.array_equal(got[b], want) and np.array_equal(got_acc[b], want_acc)
+    finally:
+        lay.close()
+
+
+def test_evict_and_weights_behind_four_billion_elements():
+    """A pool whose pages in use lie beyond 2^32 elements from its start, against the same rows near its start."""
+    d, H, page, L = 4096, 32, 64, 320
+    pages, mp = (1 << 32) // (page * d) + 8, L // page
+    ctx = B.slim_create(d, H, 128, 1.0e4, B.SLIM_BF16)
+    pool = torch.empty((pages, page, d), dtype=torch.bfloat16, device=DEV)
+    g = torch.Generator(device=DEV).manual_seed(3)
+    rows = torch.randn(mp, page, d, device=DEV, generator=g).bfloat16()
+    pool[:mp] = rows
+    pool[-mp:] = rows
+    q = torch.randn(1, d, device=DEV, generator=g).bfloat16()
+    lens = torch.tensor([L - 5], dtype=torch.int32, device=DEV)
+    st = torch.cuda.current_stream().cuda_stream
+    got = []
+    for first in (0, pages - mp):
+        table = torch.arange(first, first + mp, dtype=torch.int32, device=DEV)[None].contiguous()
+        cache = B.slim_cache_create_paged(ctx, pool, pages, page, table, 1, mp)
+        acc = torch.zeros((1, L), device=DEV)
+        ws = torch.empty(max(B.slim_weights_workspace_bytes(ctx, 1, L), B.slim_evict_workspace_bytes(ctx, 1, L)), dtype=torch.uint8, device=DEV)
+        kept = torch.empty((1, 100), dtype=torch.int32, device=DEV)
+        B.slim_accumulate_weights(ctx, q, cache, lens, acc, ws, st)
+        total = acc.sum().item()
+        B.slim_evict(ctx, cache, lens, acc, 100, 10, kept, ws, st)
+        assert B.slim_device_status(ctx, st) == B.SLIM_OK
+        got.append((acc.clone(), kept.clone(), pool[first:first + mp].clone(), total))
+        B.slim_cache_destroy(cache)
+    assert abs(got[0][3] - H) < 1e-3
+    for x, y in zip(got[0][:3], got[1][:3]):
+        assert torch.equal(x, y)
+    B.slim_destroy(ctx)
