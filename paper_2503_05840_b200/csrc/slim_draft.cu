@@ -18,33 +18,81 @@ namespace {
 // Everything is float64: a test next to its border and a draw next to a token's edge must not depend on the order of
 // a sum.  Bound: latency of the passes (V = 131072: 128 KB of p and q a CTA); a cluster of eight keeps a pass near a
 // microsecond where one CTA would take eight.
-constexpr int VC = 8, VT = 512, VW = VT / 32;
+constexpr int VC = 8;
 
+template <int VW>
 struct VerifyShared {
   int par[SLIM_MAX_TREE], tok[SLIM_MAX_TREE], path[SLIM_MAX_TREE];
   double r[SLIM_MAX_TREE], px[SLIM_MAX_TREE], qx[SLIM_MAX_TREE];
   double stage[SLIM_MAX_TREE];       // masses S of the rejections at the current node
   double warp_sum[VW];               // this CTA's ranges, last pass
   double cta_sum[2][VC];             // every CTA's sum of a pass (written by its owner into all; double-buffered)
-  int next;
+  double piece[VW];                  // the final draw: sums of the warps' pieces
+  int first, last, next;
 };
 
-// W(x) after `ns` rejections: the products and differences are rounded one by one, so a stage is a function of its
-// inputs alone.
+// W(x) after the rejections whose masses are in `stage`: the products and differences are rounded one by one, so a stage
+// is a function of its inputs alone.  NS >= 0: that many, in registers; NS < 0: ns of them, in shared memory.
+template <int NS>
 __device__ __forceinline__ double residual(float p, float q, const double* stage, int ns) {
   double w = (double)p;
+  if (NS == 0) return w;
   const double qd = (double)q;
-  for (int k = 0; k < ns; ++k) w = fmax(__dsub_rn(w, __dmul_rn(stage[k], qd)), 0.0);
+  if (NS > 0) {
+#pragma unroll
+    for (int k = 0; k < (NS > 0 ? NS : 1); ++k) w = fmax(__dsub_rn(w, __dmul_rn(stage[k], qd)), 0.0);
+  } else {
+    for (int k = 0; k < ns; ++k) w = fmax(__dsub_rn(w, __dmul_rn(stage[k], qd)), 0.0);
+  }
   return w;
 }
 
-__global__ void __cluster_dims__(VC, 1, 1) __launch_bounds__(VT)
+// This lane's share of sum W over [lo, hi) of a row: two 16-byte loads of p and q each in flight.
+template <int NS>
+__device__ __forceinline__ double range_sum(const float* __restrict__ pu, const float* __restrict__ qu, int lo, int hi, int lane, bool vec,
+                                            const double* s_stage, int ns) {
+  double stage[NS > 0 ? NS : 1];
+  if (NS > 0)
+#pragma unroll
+    for (int k = 0; k < (NS > 0 ? NS : 1); ++k) stage[k] = s_stage[k];
+  const double* st = NS > 0 ? stage : s_stage;
+  double a = 0.0;
+  if (vec) {
+    for (int x0 = lo + 4 * lane; x0 < hi; x0 += 256) {
+      float4 p4[2], q4[2];
+#pragma unroll
+      for (int y = 0; y < 2; ++y) {
+        const int x = x0 + 128 * y;
+        p4[y] = q4[y] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (x < hi) {
+          p4[y] = __ldg(reinterpret_cast<const float4*>(pu + x));
+          if (NS != 0) q4[y] = __ldg(reinterpret_cast<const float4*>(qu + x));
+        }
+      }
+#pragma unroll
+      for (int y = 0; y < 2; ++y) {
+        a += residual<NS>(p4[y].x, q4[y].x, st, ns) + residual<NS>(p4[y].y, q4[y].y, st, ns);
+        a += residual<NS>(p4[y].z, q4[y].z, st, ns) + residual<NS>(p4[y].w, q4[y].w, st, ns);
+      }
+    }
+  } else {
+#pragma unroll 4
+    for (int x = lo + lane; x < hi; x += 32) a += residual<NS>(pu[x], NS != 0 ? qu[x] : 0.f, st, ns);
+  }
+  return a;
+}
+
+// VT threads a CTA: 512 while all CTAs fit the SMs twice over, 256 above (64 registers a thread: four of them an SM).
+template <int VT>
+__global__ void __cluster_dims__(VC, 1, 1) __launch_bounds__(VT, 1024 / VT)
 slim_tree_verify_kernel(const float* __restrict__ P, const float* __restrict__ Q, const int32_t* __restrict__ tokens,
                         const int32_t* __restrict__ parents, const float* __restrict__ rnd, int n, int V, int32_t* __restrict__ path,
                         int32_t* __restrict__ count, int32_t* __restrict__ next_token, int* status) {
-  __shared__ VerifyShared sh;
+  constexpr int VW = VT / 32;
+  __shared__ VerifyShared<VW> sh;
   cg::cluster_group cluster = cg::this_cluster();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, rank = (int)cluster.block_rank(), b = blockIdx.x / VC;
+  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");      // (waited for before anything is written into a peer)
   slim_pdl_trigger();
   slim_pdl_wait();
   const float* Pb = P + (size_t)b * n * V;
@@ -64,7 +112,7 @@ slim_tree_verify_kernel(const float* __restrict__ P, const float* __restrict__ Q
   }
   if (tid == 0) sh.next = -1;
   __syncthreads();
-  cluster.sync();                    // (every CTA of the cluster runs before its shared memory is written from outside)
+  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 
   // warp ranges: multiples of 4 elements, so that rows of a vocabulary that is one are read 16 bytes at a time
   const int range = ((V + VC * VW - 1) / (VC * VW) + 3) & ~3;
@@ -76,16 +124,13 @@ slim_tree_verify_kernel(const float* __restrict__ P, const float* __restrict__ Q
   auto sum_pass = [&](int u, int ns) {
     const float* pu = Pb + (size_t)u * V;
     const float* qu = Qb + (size_t)u * V;
-    double a = 0.0;
-    if (vec) {
-      for (int x = lo + 4 * lane; x < hi; x += 128) {
-        const float4 p4 = __ldg(reinterpret_cast<const float4*>(pu + x));
-        const float4 q4 = ns ? __ldg(reinterpret_cast<const float4*>(qu + x)) : make_float4(0.f, 0.f, 0.f, 0.f);
-        a += residual(p4.x, q4.x, sh.stage, ns) + residual(p4.y, q4.y, sh.stage, ns);
-        a += residual(p4.z, q4.z, sh.stage, ns) + residual(p4.w, q4.w, sh.stage, ns);
-      }
-    } else {
-      for (int x = lo + lane; x < hi; x += 32) a += residual(pu[x], ns ? qu[x] : 0.f, sh.stage, ns);
+    double a;
+    switch (ns) {
+      case 0: a = range_sum<0>(pu, qu, lo, hi, lane, vec, sh.stage, 0); break;
+      case 1: a = range_sum<1>(pu, qu, lo, hi, lane, vec, sh.stage, 1); break;
+      case 2: a = range_sum<2>(pu, qu, lo, hi, lane, vec, sh.stage, 2); break;
+      case 3: a = range_sum<3>(pu, qu, lo, hi, lane, vec, sh.stage, 3); break;
+      default: a = range_sum<-1>(pu, qu, lo, hi, lane, vec, sh.stage, ns);
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) a += __shfl_xor_sync(0xffffffffu, a, o);
@@ -151,27 +196,41 @@ slim_tree_verify_kernel(const float* __restrict__ P, const float* __restrict__ Q
         }
         run += s;
       }
-      if (own_warp == warp) {
-        const float* pu = Pb + (size_t)u * V;
-        const float* qu = Qb + (size_t)u * V;
-        int found = -1, last = -1;
-        double base = before;
-        for (int x0 = lo; x0 < hi && found < 0; x0 += 32) {
-          const int x = x0 + lane;
-          const double w = x < hi ? residual(pu[x], ns ? qu[x] : 0.f, sh.stage, ns) : 0.0;
-          double cum = w;
-#pragma unroll
-          for (int o = 1; o < 32; o <<= 1) {
-            const double y = __shfl_up_sync(0xffffffffu, cum, o);
-            if (lane >= o) cum += y;
-          }
-          const unsigned hit = __ballot_sync(0xffffffffu, base + cum > target && w > 0.0), pos = __ballot_sync(0xffffffffu, w > 0.0);
-          if (hit) found = x0 + __ffs(hit) - 1;
-          if (pos) last = x0 + 31 - __clz(pos);
-          base += __shfl_sync(0xffffffffu, cum, 31);
-        }
-        if (lane == 0) sh.next = found >= 0 ? found : last;
+      // the range again, by the whole CTA: every thread a contiguous piece, a scan of their sums, and the thread whose
+      // piece holds the target goes through it
+      const float* pu = Pb + (size_t)u * V;
+      const float* qu = Qb + (size_t)u * V;
+      const int b0 = min(V, (rank * VW + own_warp) * range), b1 = min(V, b0 + range), per = (range + VT - 1) / VT;
+      const int x0 = min(b1, b0 + tid * per), x1 = min(b1, x0 + per);
+      double sum = 0.0;
+      int last = -1;
+      for (int x = x0; x < x1; ++x) {
+        const double w = residual<-1>(pu[x], ns ? qu[x] : 0.f, sh.stage, ns);
+        if (w > 0.0) last = x;
+        sum += w;
       }
+      double incl = sum;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const double y = __shfl_up_sync(0xffffffffu, incl, o);
+        if (lane >= o) incl += y;
+      }
+      if (lane == 31) sh.piece[warp] = incl;
+      if (tid == 0) { sh.first = 0x7fffffff; sh.last = -1; }
+      __syncthreads();
+      double base = before;
+      for (int w = 0; w < warp; ++w) base += sh.piece[w];
+      base += incl - sum;
+      if (last >= 0) atomicMax(&sh.last, last);
+      if (sum > 0.0 && base + sum > target) {                       // (the pieces behind the first of these find a higher index)
+        for (int x = x0; x < x1; ++x) {
+          const double w = residual<-1>(pu[x], ns ? qu[x] : 0.f, sh.stage, ns);
+          base += w;
+          if (w > 0.0 && base > target) { atomicMin(&sh.first, x); break; }
+        }
+      }
+      __syncthreads();
+      if (tid == 0) sh.next = sh.first != 0x7fffffff ? sh.first : sh.last;
     }
   }
   __syncthreads();
@@ -179,7 +238,7 @@ slim_tree_verify_kernel(const float* __restrict__ P, const float* __restrict__ Q
     if (tid == 0) { next_token[b] = sh.next; count[b] = cnt; }
     for (int i = tid; i < n; i += VT) path[(size_t)b * n + i] = i < cnt ? sh.path[i] : -1;
   }
-  cluster.sync();                    // no CTA leaves while another may still write into its shared memory
+  // (a CTA may leave: after the last pass's cluster barrier each reads its own shared memory only)
 }
 
 // One block per (accepted token, sequence): k_tree[b][path[b][j]] -> cache row lengths[b] + j.  A sequence whose path
@@ -224,7 +283,8 @@ slim_tree_commit_kernel(unsigned char* __restrict__ cache, const unsigned char* 
 
 cudaError_t slim_launch_verify(const float* p, const float* q, const int32_t* tokens, const int32_t* parents, const float* r, int batch,
                                int n, int vocab, int32_t* path, int32_t* count, int32_t* next_token, int* status, cudaStream_t st) {
-  return slim_launch_pdl(slim_tree_verify_kernel, dim3(VC * batch), dim3(VT), 0, st, p, q, tokens, parents, r, n, vocab, path, count,
+  auto kern = batch * VC <= 296 ? slim_tree_verify_kernel<512> : slim_tree_verify_kernel<256>;
+  return slim_launch_pdl(kern, dim3(VC * batch), dim3(batch * VC <= 296 ? 512 : 256), 0, st, p, q, tokens, parents, r, n, vocab, path, count,
                          next_token, status);
 }
 
