@@ -75,7 +75,8 @@ __global__ void __launch_bounds__(256) slim_tree_scores_kernel(const SlimDecodeP
   const int* dep = t.depth + (size_t)b * n;
   const KT* Kc = reinterpret_cast<const KT*>(p.k);
   const KT* Kt = reinterpret_cast<const KT*>(t.k_tree) + (size_t)b * n * p.d;
-  for (int e = tid; e < TS_KEYS * half; e += blockDim.x) {
+#pragma unroll 4
+  for (int e = tid; e < TS_KEYS * half; e += 256) {
     const int r = e / half, j = e - r * half;
     float k1 = 0.f, k2 = 0.f;
     int pos = 0;
@@ -93,7 +94,8 @@ __global__ void __launch_bounds__(256) slim_tree_scores_kernel(const SlimDecodeP
     Ks[r * ld + j] = k1; Ks[r * ld + half + j] = k2;
   }
   const KT* Q = reinterpret_cast<const KT*>(p.q) + (size_t)b * n * p.d;
-  for (int e = tid; e < n * half; e += blockDim.x) {
+#pragma unroll 2
+  for (int e = tid; e < n * half; e += 256) {
     const int i = e / half, j = e - i * half;
     float q1 = 0.f, q2 = 0.f;
     if (dep[i] >= 0) {
@@ -116,6 +118,7 @@ __global__ void __launch_bounds__(256) slim_tree_scores_kernel(const SlimDecodeP
   for (int i0 = tid / TS_KEYS; i0 < n; i0 += 16) {   // four tokens at a time: i0, i0 + 4, i0 + 8, i0 + 12
     float a[4] = {0.f, 0.f, 0.f, 0.f};
     const int i1 = min(i0 + 4, n - 1), i2 = min(i0 + 8, n - 1), i3 = min(i0 + 12, n - 1);
+#pragma unroll 8
     for (int j = 0; j < dk; ++j) {
       const float k = Ks[r * ld + j];
       a[0] = fmaf(k, Qs[i0 * ld + j], a[0]); a[1] = fmaf(k, Qs[i1 * ld + j], a[1]);
@@ -140,16 +143,26 @@ __global__ void __launch_bounds__(256) slim_tree_stat_kernel(const SlimDecodePar
   float m = -INFINITY, l = 0.f;
   if (t.depth[(size_t)b * t.n + i] >= 0) {
     const float* S = t.s + ((size_t)b * R + row) * t.s_ld;
-    for (int x = lane; x < len; x += 32) m = fmaxf(m, S[x]);
-    for (int x = lane; x < t.n; x += 32) m = fmaxf(m, S[t.s_draft + x]);
+    auto take = [&](float v) {
+      const float top = fmaxf(m, v);
+      if (top != -INFINITY) l = l * exp2f(m - top) + exp2f(v - top);
+      m = top;
+    };
+    for (int x = lane; x < len; x += 128) {
+      float v[4];
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-    const float ms = m == -INFINITY ? 0.f : m;
-    for (int x = lane; x < len; x += 32) l += exp2f(S[x] - ms);
-    for (int x = lane; x < t.n; x += 32) l += exp2f(S[t.s_draft + x] - ms);
+      for (int y = 0; y < 4; ++y) v[y] = x + 32 * y < len ? S[x + 32 * y] : -INFINITY;
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
-    m = ms;
+      for (int y = 0; y < 4; ++y) take(v[y]);
+    }
+    for (int x = lane; x < t.n; x += 32) take(S[t.s_draft + x]);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+      const float m1 = __shfl_xor_sync(0xffffffffu, m, o), l1 = __shfl_xor_sync(0xffffffffu, l, o), top = fmaxf(m, m1);
+      if (top != -INFINITY) l = l * exp2f(m - top) + l1 * exp2f(m1 - top);
+      m = top;
+    }
+    if (m == -INFINITY) m = 0.f;
   }
   if (lane == 0) {
     t.m[(size_t)b * R + row] = l != 0.f ? m : 0.f;
@@ -160,7 +173,7 @@ __global__ void __launch_bounds__(256) slim_tree_stat_kernel(const SlimDecodePar
 // U = P K, 64 rows x 64 columns a block, 16 keys a step; blockIdx.z = sequence x part of the keys.
 template <typename KT>
 __global__ void __launch_bounds__(256) slim_tree_sum_kernel(const SlimDecodeParams p, const SlimTreeView t) {
-  __shared__ float Ps[16][68], Bs[16][64];
+  __shared__ float Ps[16][68], Bs[16][64], s_m[64], s_il[64];
   slim_pdl_trigger();
   slim_pdl_wait();
   const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4, R = p.H * t.n;
@@ -170,6 +183,11 @@ __global__ void __launch_bounds__(256) slim_tree_sum_kernel(const SlimDecodePara
   const int s0 = (int)((long long)(nb + nd) * part / t.parts), s1 = (int)((long long)(nb + nd) * (part + 1) / t.parts);
   const KT* Kc = reinterpret_cast<const KT*>(p.k);
   const KT* Kt = reinterpret_cast<const KT*>(t.k_tree) + (size_t)b * t.n * p.d;
+  if (tid < 64) {
+    const bool in = r0 + tid < R;
+    s_m[tid] = in ? t.m[(size_t)b * R + r0 + tid] : 0.f;
+    s_il[tid] = in ? t.inv_l[(size_t)b * R + r0 + tid] : 0.f;
+  }
   float acc[4][4];
 #pragma unroll
   for (int x = 0; x < 4; ++x)
@@ -180,20 +198,24 @@ __global__ void __launch_bounds__(256) slim_tree_sum_kernel(const SlimDecodePara
     const int t0 = (draft ? s - nb : s) * 16, keys = min(16, (draft ? t.n : len) - t0);
     const KT* K0 = draft ? Kt + (size_t)t0 * p.d : Kc + (size_t)slim_cache_row(p, b, t0) * p.d;
     __syncthreads();
-    for (int e = tid; e < 64 * 16; e += 256) {
-      const int r = e >> 4, k = e & 15;
-      float v = 0.f;
-      if (r0 + r < R && k < keys) {
-        const size_t row = (size_t)b * R + r0 + r;
-        const float il = t.inv_l[row];
-        if (il != 0.f) v = exp2f(t.s[row * t.s_ld + (draft ? t.s_draft : 0) + t0 + k] - t.m[row]) * il;
-      }
-      Ps[k][r] = v;
+    float sv[4], kv[4];
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      const int e = tid + 256 * x, r = e >> 4, k = e & 15;
+      sv[x] = r0 + r < R && k < keys ? t.s[((size_t)b * R + r0 + r) * t.s_ld + (draft ? t.s_draft : 0) + t0 + k] : -INFINITY;
     }
-    for (int e = tid; e < 16 * 64; e += 256) {
-      const int k = e >> 6, c = e & 63;
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      const int e = tid + 256 * x, k = e >> 6, c = e & 63;
       const bool live = k < keys && c0 + c < p.d && !(draft && t.depth[(size_t)b * t.n + t0 + k] < 0);
-      Bs[k][c] = live ? to_f(K0[(size_t)k * p.d + c0 + c]) : 0.f;
+      kv[x] = live ? to_f(K0[(size_t)k * p.d + c0 + c]) : 0.f;
+    }
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      const int e = tid + 256 * x, r = e >> 4;
+      const float il = s_il[r];
+      Ps[e & 15][r] = il != 0.f ? exp2f(sv[x] - s_m[r]) * il : 0.f;
+      Bs[e >> 6][e & 63] = kv[x];
     }
     __syncthreads();
 #pragma unroll
@@ -217,47 +239,62 @@ __global__ void __launch_bounds__(256) slim_tree_sum_kernel(const SlimDecodePara
   }
 }
 
-// o = u W_KV,h: 16 (sequence, token) rows x 32 columns of one head a block; eight threads share a column's j.
-template <typename KT>
-__global__ void __launch_bounds__(256) slim_tree_project_kernel(const SlimDecodeParams p, const SlimTreeView t, KT* __restrict__ o) {
-  __shared__ float Us[16][64 + 1], Rs[8][16][32];
+// The parts of U added, in order, into the first one.
+__global__ void __launch_bounds__(256) slim_tree_parts_kernel(const SlimTreeView t, size_t n) {
   slim_pdl_trigger();
   slim_pdl_wait();
+  const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= n) return;
+  float v = t.u[i];
+#pragma unroll 8
+  for (int s = 1; s < t.parts; ++s) v += t.u[(size_t)s * n + i];
+  t.u[i] = v;
+}
+
+// o = u W_KV,h: 8 (sequence, token) rows x 32 columns of one head a block; eight threads share a column's j, eight rows
+// of W_KV in flight each.
+constexpr int TP_ROWS = 8, TP_J = 64;
+template <typename KT>
+__global__ void __launch_bounds__(256) slim_tree_project_kernel(const SlimDecodeParams p, const SlimTreeView t, KT* __restrict__ o) {
+  __shared__ float Us[TP_ROWS][TP_J + 1], Rs[8][TP_ROWS][32];
   const int tid = threadIdx.x, c = tid & 31, g = tid >> 5, n = t.n, d = p.d, dk = p.d_k, h = blockIdx.z;
-  const int m0 = blockIdx.y * 16, M = p.batch * n, col = blockIdx.x * 32 + c;
+  const int m0 = blockIdx.y * TP_ROWS, M = p.batch * n, col = blockIdx.x * 32 + c;
   const KT* W = reinterpret_cast<const KT*>(p.wkv) + (size_t)h * d * dk;
-  float acc[16];
+  slim_pdl_trigger();
+  slim_pdl_wait();
+  float acc[TP_ROWS];
 #pragma unroll
-  for (int r = 0; r < 16; ++r) acc[r] = 0.f;
-  for (int j0 = 0; j0 < d; j0 += 64) {
-    __syncthreads();
-    for (int e = tid; e < 16 * 64; e += 256) {
-      const int r = e >> 6, j = j0 + (e & 63), m = m0 + r;
-      float v = 0.f;
-      if (m < M && j < d) {
-        const float* U = t.u + (((size_t)(m / n) * p.H + h) * n + m % n) * d + j;
-        for (int s = 0; s < t.parts; ++s) v += U[(size_t)s * p.batch * p.H * n * d];
-      }
-      Us[r][e & 63] = v;
+  for (int r = 0; r < TP_ROWS; ++r) acc[r] = 0.f;
+  for (int j0 = 0; j0 < d; j0 += TP_J) {
+    float w[TP_J / 8], u[2];
+#pragma unroll
+    for (int x = 0; x < TP_J / 8; ++x) {
+      const int j = j0 + g + 8 * x;
+      w[x] = col < dk && j < d ? to_f(W[(size_t)j * dk + col]) : 0.f;
+    }
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      const int e = tid + 256 * x, m = m0 + (e >> 6), j = j0 + (e & 63);
+      u[x] = m < M && j < d ? t.u[(((size_t)(m / n) * p.H + h) * n + m % n) * d + j] : 0.f;
     }
     __syncthreads();
-    if (col < dk)
-      for (int j = g; j < 64 && j0 + j < d; j += 8) {
-        const float w = to_f(W[(size_t)(j0 + j) * dk + col]);
 #pragma unroll
-        for (int r = 0; r < 16; ++r) acc[r] = fmaf(Us[r][j], w, acc[r]);
-      }
+    for (int x = 0; x < 2; ++x) Us[(tid + 256 * x) >> 6][(tid + 256 * x) & 63] = u[x];
+    __syncthreads();
+#pragma unroll
+    for (int x = 0; x < TP_J / 8; ++x)
+#pragma unroll
+      for (int r = 0; r < TP_ROWS; ++r) acc[r] = fmaf(Us[r][g + 8 * x], w[x], acc[r]);
   }
 #pragma unroll
-  for (int r = 0; r < 16; ++r) Rs[g][r][c] = acc[r];
+  for (int r = 0; r < TP_ROWS; ++r) Rs[g][r][c] = acc[r];
   __syncthreads();
-  for (int r = g; r < 16; r += 8) {
-    if (m0 + r >= M || col >= dk) continue;
-    float v = 0.f;
+  const int r = g;
+  if (m0 + r >= M || col >= dk) return;
+  float v = 0.f;
 #pragma unroll
-    for (int x = 0; x < 8; ++x) v += Rs[x][r][c];
-    put(o + (size_t)(m0 + r) * d + h * dk + col, v);
-  }
+  for (int x = 0; x < 8; ++x) v += Rs[x][r][c];
+  put(o + (size_t)(m0 + r) * d + h * dk + col, v);
 }
 
 template <typename KT>
@@ -271,8 +308,10 @@ cudaError_t launch_generic(const slim_ctx* ctx, const SlimDecodeParams& p, const
   if (e == cudaSuccess) e = slim_launch_pdl(slim_tree_stat_kernel, dim3((R + 7) / 8, p.batch), dim3(256), 0, st, p, t);
   if (e == cudaSuccess)
     e = slim_launch_pdl(slim_tree_sum_kernel<KT>, dim3((p.d + 63) / 64, (R + 63) / 64, p.batch * t.parts), dim3(256), 0, st, p, t);
+  const size_t un = (size_t)p.batch * R * p.d;
+  if (e == cudaSuccess && t.parts > 1) e = slim_launch_pdl(slim_tree_parts_kernel, dim3((unsigned)((un + 255) / 256)), dim3(256), 0, st, t, un);
   if (e == cudaSuccess)
-    e = slim_launch_pdl(slim_tree_project_kernel<KT>, dim3((p.d_k + 31) / 32, (p.batch * t.n + 15) / 16, p.H), dim3(256), 0, st, p, t, (KT*)o);
+    e = slim_launch_pdl(slim_tree_project_kernel<KT>, dim3((p.d_k + 31) / 32, (p.batch * t.n + TP_ROWS - 1) / TP_ROWS, p.H), dim3(256), 0, st, p, t, (KT*)o);
   return e;
 }
 
