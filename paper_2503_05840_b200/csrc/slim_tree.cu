@@ -132,40 +132,43 @@ __global__ void __launch_bounds__(256) slim_tree_scores_kernel(const SlimDecodeP
   }
 }
 
-// m and 1 / l of every row (one warp a row); a token that is padding, or whose row is empty, gets 1 / l = 0.
+// m and 1 / l of every row (one block a row); a token that is padding, or whose row is empty, gets 1 / l = 0.
 __global__ void __launch_bounds__(256) slim_tree_stat_kernel(const SlimDecodeParams p, const SlimTreeView t) {
+  __shared__ float s_m[8], s_l[8];
   slim_pdl_trigger();
   slim_pdl_wait();
-  const int lane = threadIdx.x & 31, R = p.H * t.n;
-  const int row = blockIdx.x * 8 + (threadIdx.x >> 5), b = blockIdx.y;
-  if (row >= R) return;
+  const int tid = threadIdx.x, lane = tid & 31, R = p.H * t.n, row = blockIdx.x, b = blockIdx.y;
   const int i = row % t.n, len = t.len[b];
   float m = -INFINITY, l = 0.f;
+  auto join = [&](float m1, float l1) {
+    const float top = fmaxf(m, m1);
+    if (top != -INFINITY) l = l * exp2f(m - top) + l1 * exp2f(m1 - top);
+    m = top;
+  };
   if (t.depth[(size_t)b * t.n + i] >= 0) {
     const float* S = t.s + ((size_t)b * R + row) * t.s_ld;
-    auto take = [&](float v) {
-      const float top = fmaxf(m, v);
-      if (top != -INFINITY) l = l * exp2f(m - top) + exp2f(v - top);
-      m = top;
-    };
-    for (int x = lane; x < len; x += 128) {
+    for (int x = tid; x < len; x += 1024) {
       float v[4];
 #pragma unroll
-      for (int y = 0; y < 4; ++y) v[y] = x + 32 * y < len ? S[x + 32 * y] : -INFINITY;
+      for (int y = 0; y < 4; ++y) v[y] = x + 256 * y < len ? S[x + 256 * y] : -INFINITY;
 #pragma unroll
-      for (int y = 0; y < 4; ++y) take(v[y]);
+      for (int y = 0; y < 4; ++y) join(v[y], v[y] == -INFINITY ? 0.f : 1.f);
     }
-    for (int x = lane; x < t.n; x += 32) take(S[t.s_draft + x]);
+    if (tid < t.n) {
+      const float v = S[t.s_draft + tid];
+      join(v, v == -INFINITY ? 0.f : 1.f);
+    }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) {
-      const float m1 = __shfl_xor_sync(0xffffffffu, m, o), l1 = __shfl_xor_sync(0xffffffffu, l, o), top = fmaxf(m, m1);
-      if (top != -INFINITY) l = l * exp2f(m - top) + l1 * exp2f(m1 - top);
-      m = top;
+      const float m1 = __shfl_xor_sync(0xffffffffu, m, o), l1 = __shfl_xor_sync(0xffffffffu, l, o);
+      join(m1, l1);
     }
-    if (m == -INFINITY) m = 0.f;
   }
-  if (lane == 0) {
-    t.m[(size_t)b * R + row] = l != 0.f ? m : 0.f;
+  if (lane == 0) { s_m[tid >> 5] = m; s_l[tid >> 5] = l; }
+  __syncthreads();
+  if (tid == 0) {
+    for (int w = 1; w < 8; ++w) join(s_m[w], s_l[w]);
+    t.m[(size_t)b * R + row] = m == -INFINITY ? 0.f : m;
     t.inv_l[(size_t)b * R + row] = l != 0.f ? 1.f / l : 0.f;       // (NaN stays NaN)
   }
 }
@@ -305,7 +308,7 @@ cudaError_t launch_generic(const slim_ctx* ctx, const SlimDecodeParams& p, const
   if (e != cudaSuccess) return e;
   const int R = p.H * t.n;
   e = slim_launch_pdl(ks, dim3((p.t_cap + TS_KEYS - 1) / TS_KEYS + 1, p.H, p.batch), dim3(256), smem, st, p, t);
-  if (e == cudaSuccess) e = slim_launch_pdl(slim_tree_stat_kernel, dim3((R + 7) / 8, p.batch), dim3(256), 0, st, p, t);
+  if (e == cudaSuccess) e = slim_launch_pdl(slim_tree_stat_kernel, dim3(R, p.batch), dim3(256), 0, st, p, t);
   if (e == cudaSuccess)
     e = slim_launch_pdl(slim_tree_sum_kernel<KT>, dim3((p.d + 63) / 64, (R + 63) / 64, p.batch * t.parts), dim3(256), 0, st, p, t);
   const size_t un = (size_t)p.batch * R * p.d;

@@ -211,10 +211,13 @@ slim_tree_p_kernel(const __grid_constant__ CUtensorMap cmap, const __grid_consta
   const int nt0 = htid / S::PER, fi = htid % S::PER, fs = fi >> 5, j0 = chunk_of(DK, fi & 3, fs / (VW / 2)) * VW + 2 * (fs % (VW / 2));
   auto fetch = [&](int it) {                                              // (lane 0) rows that are not there are masked later
     const bool draft = it == mine;
-    const int blk0 = draft ? 0 : (first + it * step) * SC_KEYS;
-    int t0 = blk0 + 16 * hw;
-    if (t0 >= (draft ? n : len)) t0 = blk0;
-    const int row = draft ? b * n + t0 : (int)slim_cache_row(p, b, t0), st = it % S::KS;
+    const int blk0 = draft ? 0 : (first + it * step) * SC_KEYS, st = it % S::KS;
+    int t0 = blk0 + 16 * hw, row;
+    if (it + 1 < mine && !p.block_table) row = b * p.t_cap + t0;          // (a whole block)
+    else {
+      if (t0 >= (draft ? n : len)) t0 = blk0;
+      row = draft ? b * n + t0 : (int)slim_cache_row(p, b, t0);
+    }
     mbar_arrive_expect_tx(bar + 8 * st, S::KT);
     tma_load_3d(smem_u32(ring) + (uint32_t)(st * S::KT), draft ? &dmap : &cmap, bar + 8 * st, DK == 96 ? h * DK : 0, row,
                 DK == 128 ? 2 * h : DK == 64 ? h : 0);
@@ -314,6 +317,8 @@ slim_tree_p_kernel(const __grid_constant__ CUtensorMap cmap, const __grid_consta
     }
   };
 
+  __nv_bfloat16* p_base = t.p + ((size_t)b * R + (size_t)h * n + g) * t.p_ld + 16 * hw + 4 * c;      // of token g
+  const size_t p_step = 8 * (size_t)t.p_ld;
   for (int it = 0; it < total; ++it) {
     const bool draft = it == mine;
     const int blk = first + it * step, t0 = draft ? 16 * hw : blk * SC_KEYS + 16 * hw;
@@ -456,14 +461,13 @@ slim_tree_p_kernel(const __grid_constant__ CUtensorMap cmap, const __grid_consta
       }
     }
     // ---- probabilities, turned around to [token][4 keys], out; their sums over this warp's keys
-    const int col = (draft ? t.s_draft : blk * SC_KEYS) + 16 * hw + 4 * c;
-    __nv_bfloat16* Pout = t.p + ((size_t)b * R + (size_t)h * n) * t.p_ld + col;
+    __nv_bfloat16* Pout = p_base + (draft ? t.s_draft : blk * SC_KEYS);
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
       const uint32_t d0 = movmatrix_trans(bf162_of(ex2_approx(y[nt][0]), ex2_approx(y[nt][1])));
       const uint32_t d1 = movmatrix_trans(bf162_of(ex2_approx(y[nt][2]), ex2_approx(y[nt][3])));
       const int i = 8 * nt + g;
-      if (i < n && (!draft || hw < 4)) *reinterpret_cast<uint2*>(Pout + (size_t)i * t.p_ld) = make_uint2(d0, d1);
+      if (i < n && (!draft || hw < 4)) *reinterpret_cast<uint2*>(Pout + (size_t)nt * p_step) = make_uint2(d0, d1);
       float l = sum2(add2(unpack2(d0), unpack2(d1)));
       l += __shfl_xor_sync(0xffffffffu, l, 1);
       l += __shfl_xor_sync(0xffffffffu, l, 2);
@@ -1182,6 +1186,7 @@ void slim_tree_tc_layout(const slim_ctx* ctx, int batch, int t_cap, int n, SlimT
   const long long most = (t_cap / 64 + 2) / 8;
   if (split > most) split = most;
   L.g_split = split < 1 ? 1 : (int)split;
+  if (tiles * L.g_split < L.g_pairs) L.g_split = 1;       // (no whole part for every pair: the tiles are cut where the pairs' shares end)
   const long long sub = tiles * L.g_split, waves = sub / L.g_pairs - (batch > 1 ? 1 : 0);   // (ragged lengths: level them with a wave)
   L.g_whole = waves > 0 ? (int)(waves * L.g_pairs) : 0;
   L.p_s_draft = nb * SC_KEYS;
@@ -1241,7 +1246,9 @@ cudaError_t slim_launch_tree_tc(const slim_ctx* ctx, const SlimDecodeParams& p, 
     e = slim_launch_pdl(slim_tree_join_kernel, dim3(tiles, L.mt * 16), dim3(256), smem, st, p, t, L.mt);
     if (e != cudaSuccess) return e;
   }
-  const int ns = d / 64, parts = ns >= 4 ? 4 : ns >= 2 ? 2 : 1;
+  // parts of the d rows: as many as leave one CTA an SM (a CTA fills an SM's shared memory), at most four
+  const int ns = d / 64, ctas = H * ((M + 127) / 128);
+  const int parts = ns >= 4 && 4 * ctas <= ctx->num_sms ? 4 : ns >= 2 && 2 * ctas <= ctx->num_sms ? 2 : 1;
   e = cudaFuncSetAttribute(slim_tree_out_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)OU_SMEM);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
