@@ -73,8 +73,9 @@ __global__ void __launch_bounds__(256) slim_tree_tail_kernel(const SlimDecodePar
 }
 
 // ------------------------------------------------------------------------------------------------ scores
-// A CTA takes one (sequence, head); its groups of eight warps share the tables and take the blocks of 128 keys in
-// turn, with barriers of their own, so that one computes while the others wait.  Warp w of a group has keys
+// The blocks of 128 keys of all heads of all sequences (a row's last block is its drafted keys) are dealt out evenly, one
+// CTA per SM.  A CTA goes through its (sequence, head) rows one after another; its groups of eight warps share the tables and
+// take a row's blocks in turn, with barriers of their own, so that one computes while the others wait.  Warp w of a group has keys
 // 16 w .. 16 w + 15 of a block, rows g and g + 8 of m16n8k16 float16 tiles in each thread, and the tokens as the tiles'
 // columns; its key tile comes by TMA into a buffer of its own, which nobody else reads.
 //   - The contraction runs over rotation pairs: step (pc, x) puts the low elements of pairs j, j + 1 into the k-slots 2 c,
@@ -186,7 +187,7 @@ slim_tree_p_kernel(const __grid_constant__ CUtensorMap cmap, const __grid_consta
   unsigned char* tail = sm + S::KR + S::CS + S::QS + S::GROUPS * S::OWN;
   const uint32_t bar_table = smem_u32(tail), bar = bar_table + 8u * (uint32_t)(1 + warp * S::KS);      // this warp's barriers
   volatile int* s_abort = reinterpret_cast<volatile int*>(tail + 8 * (S::WARPS * S::KS + 1));
-  const int b = blockIdx.z, h = blockIdx.y, n = t.n, R = p.H * n;
+  const int n = t.n, R = p.H * n;
 
   if (lane == 0) {
     for (int i = 0; i < S::KS; ++i) mbar_init(bar + 8 * i, 1);
@@ -199,21 +200,46 @@ slim_tree_p_kernel(const __grid_constant__ CUtensorMap cmap, const __grid_consta
   }
   slim_pdl_trigger();
   slim_pdl_wait();
-  const int len = t.len[b], nblk = (len + SC_KEYS - 1) / SC_KEYS, nb_cap = (p.t_cap + SC_KEYS - 1) / SC_KEYS;
-  // the draft block comes last, in the first group of the CTAs of column 0
-  const int first = S::GROUPS * blockIdx.x + group, step = S::GROUPS * gridDim.x;
-  const int mine = nblk > first ? (nblk - 1 - first) / step + 1 : 0;
-  const int total = mine + (first == 0 ? 1 : 0);
-  const int* dep = t.depth + (size_t)b * n;
+  const int nb_cap = (p.t_cap + SC_KEYS - 1) / SC_KEYS;
+  // this CTA's share of the line of blocks, and where it begins; the same in every warp
+  int b = 0, h = 0, k0 = 0, remaining;
+  {
+    auto row_blocks = [&](int q) { return q < p.batch ? p.H * ((t.len[q] + SC_KEYS - 1) / SC_KEYS + 1) : 0; };
+    int all = 0;
+    for (int q = lane; q < p.batch; q += 32) all += row_blocks(q);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) all += __shfl_xor_sync(0xffffffffu, all, o);
+    const int a0 = (int)((long long)all * blockIdx.x / gridDim.x);
+    remaining = (int)((long long)all * (blockIdx.x + 1) / gridDim.x) - a0;
+    if (remaining == 0) return;
+    for (int q0 = 0, before = 0; q0 < p.batch; q0 += 32) {
+      const int mine = row_blocks(q0 + lane);
+      int incl = mine;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) { const int v = __shfl_up_sync(0xffffffffu, incl, o); if (lane >= o) incl += v; }
+      const unsigned hit = __ballot_sync(0xffffffffu, before + incl > a0);
+      if (hit) {
+        const int l = __ffs(hit) - 1, in = a0 - before - (__shfl_sync(0xffffffffu, incl, l) - __shfl_sync(0xffffffffu, mine, l));
+        b = q0 + l;
+        const int nb = (t.len[b] + SC_KEYS - 1) / SC_KEYS + 1;
+        h = in / nb; k0 = in - h * nb;
+        break;
+      }
+      before += __shfl_sync(0xffffffffu, incl, 31);
+    }
+  }
+  int len = 0, nblk = 0, first = 0, mine = 0, total = 0, base = 0;        // of the current row; base: key tiles of the rows before
+  constexpr int step = S::GROUPS;
+  const int* dep;
 
   // this thread's part of the query fragments: pairs j0, j0 + 1 of token 8 nt + lane / 4, for nt = nt0, nt0 + NTS, ..
   constexpr int NTS = SC_GROUP / S::PER;
   const int nt0 = htid / S::PER, fi = htid % S::PER, fs = fi >> 5, j0 = chunk_of(DK, fi & 3, fs / (VW / 2)) * VW + 2 * (fs % (VW / 2));
   auto fetch = [&](int it) {                                              // (lane 0) rows that are not there are masked later
     const bool draft = it == mine;
-    const int blk0 = draft ? 0 : (first + it * step) * SC_KEYS, st = it % S::KS;
+    const int blk0 = draft ? 0 : (first + it * step) * SC_KEYS, st = (base + it) % S::KS;
     int t0 = blk0 + 16 * hw, row;
-    if (it + 1 < mine && !p.block_table) row = b * p.t_cap + t0;          // (a whole block)
+    if (!draft && blk0 + SC_KEYS <= len && !p.block_table) row = b * p.t_cap + t0;
     else {
       if (t0 >= (draft ? n : len)) t0 = blk0;
       row = draft ? b * n + t0 : (int)slim_cache_row(p, b, t0);
@@ -245,54 +271,6 @@ slim_tree_p_kernel(const __grid_constant__ CUtensorMap cmap, const __grid_consta
       }
     }
   };
-  __syncwarp();
-  if (lane == 0)
-    for (int i = 0; i < S::KS && i < total; ++i) fetch(i);
-  float4 bc = make_float4(1.f, 0.f, 1.f, 0.f);
-  if (total > 0) bc = block_angle(0);
-
-  // queries of this (sequence, head), scaled and turned to their positions; one warp a token
-  bool large = false;
-  {
-    const __nv_bfloat16* Q = reinterpret_cast<const __nv_bfloat16*>(p.q) + (size_t)b * n * p.d + h * DK;
-    for (int i = warp; i < TOK; i += S::WARPS) {
-      const bool there = i < n && dep[i] >= 0;
-      float2 v[(HALF + 31) / 32];
-      float top = 0.f;
-#pragma unroll
-      for (int x = 0; x < (HALF + 31) / 32; ++x) {
-        const int j = lane + 32 * x;
-        v[x] = make_float2(0.f, 0.f);
-        if (there && j < HALF) {
-          const float q1 = __bfloat162float(Q[(size_t)i * p.d + j]) * p.qscale, q2 = __bfloat162float(Q[(size_t)i * p.d + HALF + j]) * p.qscale;
-          if (ROPE) {
-            const float2 cs = turn(p, len + dep[i], j);
-            v[x] = make_float2(q1 * cs.x + q2 * cs.y, q2 * cs.x - q1 * cs.y);
-          } else v[x] = make_float2(q1, q2);
-        }
-        top = fmaxf(top, fmaxf(fabsf(v[x].x), fabsf(v[x].y)));
-      }
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-      const float sc = pow2_to(top, 4);                                   // the largest element near 16
-#pragma unroll
-      for (int x = 0; x < (HALF + 31) / 32; ++x)
-        if (lane + 32 * x < HALF) {
-          const int j = lane + 32 * x, ch = j / VW, pc = DK == 128 ? ch & 1 : ch >> 2, cc = DK == 128 ? ch >> 1 : ch & 3;
-          const int at = 2 * ((i >> 3) * S::PER + (pc * (VW / 2) + (j % VW) / 2) * 32 + (i & 7) * 4 + cc) + (j & 1);
-          if (S::QHALF) reinterpret_cast<uint32_t*>(qs)[at] = half2_of(pack2(v[x].x * sc, v[x].y * sc));
-          else reinterpret_cast<float2*>(qs)[at] = make_float2(v[x].x * sc, v[x].y * sc);
-        }
-      if (lane < S::GROUPS) {                                             // every group's copy; a token that is not there: P = 2^(s - inf) = 0
-        unsigned char* o = sm + S::KR + S::CS + S::QS + lane * S::OWN + 2 * S::QF;
-        reinterpret_cast<float2*>(o)[i] = make_float2(1.f / sc, there ? -INFINITY : INFINITY);
-        reinterpret_cast<int*>(o + S::SR)[i] = ordered(-INFINITY);
-      }
-      // keys near 1 lose at most 2^-12 of themselves; steps of 2^-25 of smaller ones show where DK |q| 2^-25 does
-      large = large || !(top <= 64.f);
-    }
-  }
-  const bool careful = __syncthreads_or(large);
   // MMA rows g and g + 8 are keys key0 and key0 + 2 of the warp's tile: turned around, a thread then holds four
   // neighbouring keys of a token
   const int key0 = 4 * (g >> 1) + (g & 1);
@@ -302,11 +280,6 @@ slim_tree_p_kernel(const __grid_constant__ CUtensorMap cmap, const __grid_consta
 #pragma unroll
     for (int x = 0; x < NCS; ++x) csr[rh][x] = __ldg(reinterpret_cast<const ulonglong2*>(table) + ((o >> 3) * NCS + x) * 32 + ((o & 7) << 2) + c);
   };
-  if (S::CSR && ROPE) { angles(0, 16 * hw + key0); angles(1, 16 * hw + key0 + 2); }
-  if (ROPE && !S::CSR) mbar_wait<false>(bar_table, 0, s_abort, p.status);
-  if (total > 0) fragments(bc, 0);
-  if (total > 1) bc = block_angle(1);
-  group_sync(group);
   // sums and references of block `it`, once all warps have left theirs
   auto stats = [&](int it) {
     if (htid < n) {
@@ -317,165 +290,233 @@ slim_tree_p_kernel(const __grid_constant__ CUtensorMap cmap, const __grid_consta
     }
   };
 
-  __nv_bfloat16* p_base = t.p + ((size_t)b * R + (size_t)h * n + g) * t.p_ld + 16 * hw + 4 * c;      // of token g
-  const size_t p_step = 8 * (size_t)t.p_ld;
-  for (int it = 0; it < total; ++it) {
-    const bool draft = it == mine;
-    const int blk = first + it * step, t0 = draft ? 16 * hw : blk * SC_KEYS + 16 * hw;
-    // ---- scores
-    // a drafted key's offset in its block is its depth
-    const ulonglong2* row_cs[2];
-    if (ROPE) {
+  __syncwarp();
+  for (;;) {
+    // ---- the next row: blocks k0 .. k1 - 1 of (b, h), the drafted keys' being number nblk
+    len = t.len[b]; nblk = (len + SC_KEYS - 1) / SC_KEYS;
+    const int k1 = min(nblk + 1, k0 + remaining);
+    first = k0 + group;
+    total = k1 > first ? (k1 - 1 - first) / step + 1 : 0;
+    mine = total > 0 && k1 == nblk + 1 && first + (total - 1) * step == nblk ? total - 1 : 0x7fffffff;      // which block is the drafted keys'
+    dep = t.depth + (size_t)b * n;
+    if (lane == 0 && !*s_abort)
+      for (int i = 0; i < S::KS && i < total; ++i) fetch(i);
+    float4 bc = make_float4(1.f, 0.f, 1.f, 0.f);
+    if (total > 0) bc = block_angle(0);
+    // queries of this (sequence, head), scaled and turned to their positions; one warp a token
+    bool large = false;
+    {
+      const __nv_bfloat16* Q = reinterpret_cast<const __nv_bfloat16*>(p.q) + (size_t)b * n * p.d + h * DK;
+      for (int i = warp; i < TOK; i += S::WARPS) {
+        const bool there = i < n && dep[i] >= 0;
+        float2 v[(HALF + 31) / 32];
+        float top = 0.f;
 #pragma unroll
-      for (int rh = 0; rh < 2; ++rh) {
-        int o = 16 * hw + key0 + 2 * rh;
-        if (draft) o = o < n ? max(dep[o], 0) : 0;
-        if (S::CSR) { if (draft) angles(rh, o); }
-        else row_cs[rh] = reinterpret_cast<const ulonglong2*>(cst) + (o >> 3) * (NPC * (VW / 2) * 32) + ((o & 7) << 2) + c;
-      }
-    }
-    unsigned char* tile = ring + (it % S::KS) * S::KT;
-    const uint2* qb = qf + (it & 1) * NT * S::PER;
-    mbar_wait<false>(bar + 8 * (it % S::KS), (it / S::KS) & 1, s_abort, p.status);      // (gave up: reported, and the loop runs on to its end)
-    float s[NT][4];
-    float back = 1.f;                                                     // undoes the keys' scaling
-    for (bool again = false;;) {
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt) s[nt][0] = s[nt][1] = s[nt][2] = s[nt][3] = 0.f;
-#pragma unroll
-      for (int pc = 0; pc < NPC; ++pc) {
-        kvec k[2][2];                                                     // [row half][low / high elements of the pairs]
-#pragma unroll
-        for (int rh = 0; rh < 2; ++rh)
-#pragma unroll
-          for (int hl = 0; hl < 2; ++hl) k[rh][hl] = *reinterpret_cast<const kvec*>(tile + tile_off<DK>(key0 + 2 * rh, c, pc, hl));
-#pragma unroll
-        for (int xq = 0; xq < VW / 2; ++xq) {
-          uint32_t a[4];
-#pragma unroll
-          for (int rh = 0; rh < 2; ++rh) {
-            const f32x2 k1 = unpack2(word(k[rh][0], xq)), k2 = unpack2(word(k[rh][1], xq));
+        for (int x = 0; x < (HALF + 31) / 32; ++x) {
+          const int j = lane + 32 * x;
+          v[x] = make_float2(0.f, 0.f);
+          if (there && j < HALF) {
+            const float q1 = __bfloat162float(Q[(size_t)i * p.d + j]) * p.qscale, q2 = __bfloat162float(Q[(size_t)i * p.d + HALF + j]) * p.qscale;
             if (ROPE) {
-              const ulonglong2 cs = S::CSR ? csr[rh][(pc * (VW / 2) + xq) % NCS] : row_cs[rh][(pc * (VW / 2) + xq) * 32];
-              a[rh] = half2_of(fma2(k2, cs.y, mul2(k1, cs.x)));
-              a[2 + rh] = half2_of(sub2(mul2(k2, cs.x), mul2(k1, cs.y)));
-            } else {
-              a[rh] = half2_of(k1);
-              a[2 + rh] = half2_of(k2);
-            }
+              const float2 cs = turn(p, len + dep[i], j);
+              v[x] = make_float2(q1 * cs.x + q2 * cs.y, q2 * cs.x - q1 * cs.y);
+            } else v[x] = make_float2(q1, q2);
           }
+          top = fmaxf(top, fmaxf(fabsf(v[x].x), fabsf(v[x].y)));
+        }
 #pragma unroll
-          for (int nt = 0; nt < NT; ++nt) {
-            const uint2 f = qb[nt * S::PER + (pc * (VW / 2) + xq) * 32 + lane];
-            mma_f16(s[nt], a, f.x, f.y);
+        for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+        const float sc = pow2_to(top, 4);                                   // the largest element near 16
+#pragma unroll
+        for (int x = 0; x < (HALF + 31) / 32; ++x)
+          if (lane + 32 * x < HALF) {
+            const int j = lane + 32 * x, ch = j / VW, pc = DK == 128 ? ch & 1 : ch >> 2, cc = DK == 128 ? ch >> 1 : ch & 3;
+            const int at = 2 * ((i >> 3) * S::PER + (pc * (VW / 2) + (j % VW) / 2) * 32 + (i & 7) * 4 + cc) + (j & 1);
+            if (S::QHALF) reinterpret_cast<uint32_t*>(qs)[at] = half2_of(pack2(v[x].x * sc, v[x].y * sc));
+            else reinterpret_cast<float2*>(qs)[at] = make_float2(v[x].x * sc, v[x].y * sc);
           }
+        if (lane < S::GROUPS) {                                             // every group's copy; a token that is not there: P = 2^(s - inf) = 0
+          unsigned char* o = sm + S::KR + S::CS + S::QS + lane * S::OWN + 2 * S::QF;
+          reinterpret_cast<float2*>(o)[i] = make_float2(1.f / sc, there ? -INFINITY : INFINITY);
+          reinterpret_cast<int*>(o + S::SR)[i] = ordered(-INFINITY);
+        }
+        // keys near 1 lose at most 2^-12 of themselves; steps of 2^-25 of smaller ones show where DK |q| 2^-25 does
+        large = large || !(top <= 64.f);
+      }
+    }
+    const bool careful = __syncthreads_or(large);
+    if (S::CSR && ROPE) { angles(0, 16 * hw + key0); angles(1, 16 * hw + key0 + 2); }
+    if (ROPE && !S::CSR) mbar_wait<false>(bar_table, 0, s_abort, p.status);
+    if (total > 0) fragments(bc, 0);
+    if (total > 1) bc = block_angle(1);
+    group_sync(group);
+    __nv_bfloat16* p_base = t.p + ((size_t)b * R + (size_t)h * n + g) * t.p_ld + 16 * hw + 4 * c;      // of token g
+    const size_t p_step = 8 * (size_t)t.p_ld;
+    for (int it = 0; it < total; ++it) {
+      const bool draft = it == mine;
+      const int blk = first + it * step, t0 = draft ? 16 * hw : blk * SC_KEYS + 16 * hw;
+      // ---- scores
+      // a drafted key's offset in its block is its depth
+      const ulonglong2* row_cs[2];
+      if (ROPE) {
+#pragma unroll
+        for (int rh = 0; rh < 2; ++rh) {
+          int o = 16 * hw + key0 + 2 * rh;
+          if (draft) o = o < n ? max(dep[o], 0) : 0;
+          if (S::CSR) { if (draft) angles(rh, o); }
+          else row_cs[rh] = reinterpret_cast<const ulonglong2*>(cst) + (o >> 3) * (NPC * (VW / 2) * 32) + ((o & 7) << 2) + c;
         }
       }
-      // an overflow shows as an infinity or a NaN, and 0 x it is a NaN
-      float odd = 0.f;
+      unsigned char* tile = ring + ((base + it) % S::KS) * S::KT;
+      const uint2* qb = qf + (it & 1) * NT * S::PER;
+      mbar_wait<false>(bar + 8 * ((base + it) % S::KS), ((base + it) / S::KS) & 1, s_abort, p.status);      // (gave up: reported, and the loop runs on to its end)
+      float s[NT][4];
+      float back = 1.f;                                                     // undoes the keys' scaling
+      for (bool again = false;;) {
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
+        for (int nt = 0; nt < NT; ++nt) s[nt][0] = s[nt][1] = s[nt][2] = s[nt][3] = 0.f;
 #pragma unroll
-        for (int x = 0; x < 4; ++x) odd = fmaf(s[nt][x], 0.f, odd);
-      if (again || !__any_sync(0xffffffffu, careful || odd != 0.f)) break;
-      again = true;
-      float top = 0.f, ks = 0.f;
-      for (int turn2 = 0; turn2 < 2; ++turn2) {                           // the largest element, then the scaling, in place: a thread's own elements
+        for (int pc = 0; pc < NPC; ++pc) {
+          kvec k[2][2];                                                     // [row half][low / high elements of the pairs]
 #pragma unroll
-        for (int rh = 0; rh < 2; ++rh)
+          for (int rh = 0; rh < 2; ++rh)
 #pragma unroll
-          for (int pc = 0; pc < NPC; ++pc)
+            for (int hl = 0; hl < 2; ++hl) k[rh][hl] = *reinterpret_cast<const kvec*>(tile + tile_off<DK>(key0 + 2 * rh, c, pc, hl));
 #pragma unroll
-            for (int hl = 0; hl < 2; ++hl) {
-              kvec* at = reinterpret_cast<kvec*>(tile + tile_off<DK>(key0 + 2 * rh, c, pc, hl));
-              kvec v = *at;
+          for (int xq = 0; xq < VW / 2; ++xq) {
+            uint32_t a[4];
 #pragma unroll
-              for (int x = 0; x < VW / 2; ++x) {
-                const uint32_t w = word(v, x);
-                const float e0 = __uint_as_float(w << 16), e1 = __uint_as_float(w & 0xffff0000u);
-                if (turn2 == 0) top = fmaxf(top, fmaxf(fabsf(e0), fabsf(e1)));
-                else word_ref(v, x) = bf162_of(e0 * ks, e1 * ks);         // (a power of two: exact, but for what is 2^-100 of the largest)
+            for (int rh = 0; rh < 2; ++rh) {
+              const f32x2 k1 = unpack2(word(k[rh][0], xq)), k2 = unpack2(word(k[rh][1], xq));
+              if (ROPE) {
+                const ulonglong2 cs = S::CSR ? csr[rh][(pc * (VW / 2) + xq) % NCS] : row_cs[rh][(pc * (VW / 2) + xq) * 32];
+                a[rh] = half2_of(fma2(k2, cs.y, mul2(k1, cs.x)));
+                a[2 + rh] = half2_of(sub2(mul2(k2, cs.x), mul2(k1, cs.y)));
+              } else {
+                a[rh] = half2_of(k1);
+                a[2 + rh] = half2_of(k2);
               }
-              if (turn2 == 1) *at = v;
             }
-        if (turn2 == 0) {
 #pragma unroll
-          for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-          ks = pow2_to(top, 10);
-          back = 1.f / ks;
+            for (int nt = 0; nt < NT; ++nt) {
+              const uint2 f = qb[nt * S::PER + (pc * (VW / 2) + xq) * 32 + lane];
+              mma_f16(s[nt], a, f.x, f.y);
+            }
+          }
         }
+        // an overflow shows as an infinity or a NaN, and 0 x it is a NaN
+        float odd = 0.f;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int x = 0; x < 4; ++x) odd = fmaf(s[nt][x], 0.f, odd);
+        if (again || !__any_sync(0xffffffffu, careful || odd != 0.f)) break;
+        again = true;
+        float top = 0.f, ks = 0.f;
+        for (int turn2 = 0; turn2 < 2; ++turn2) {                           // the largest element, then the scaling, in place: a thread's own elements
+#pragma unroll
+          for (int rh = 0; rh < 2; ++rh)
+#pragma unroll
+            for (int pc = 0; pc < NPC; ++pc)
+#pragma unroll
+              for (int hl = 0; hl < 2; ++hl) {
+                kvec* at = reinterpret_cast<kvec*>(tile + tile_off<DK>(key0 + 2 * rh, c, pc, hl));
+                kvec v = *at;
+#pragma unroll
+                for (int x = 0; x < VW / 2; ++x) {
+                  const uint32_t w = word(v, x);
+                  const float e0 = __uint_as_float(w << 16), e1 = __uint_as_float(w & 0xffff0000u);
+                  if (turn2 == 0) top = fmaxf(top, fmaxf(fabsf(e0), fabsf(e1)));
+                  else word_ref(v, x) = bf162_of(e0 * ks, e1 * ks);         // (a power of two: exact, but for what is 2^-100 of the largest)
+                }
+                if (turn2 == 1) *at = v;
+              }
+          if (turn2 == 0) {
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+            ks = pow2_to(top, 10);
+            back = 1.f / ks;
+          }
+        }
+        fence_proxy_async_smem();                                           // (the next tile comes by the async proxy)
       }
-      fence_proxy_async_smem();                                           // (the next tile comes by the async proxy)
-    }
-    __syncwarp();                                                         // all lanes have read the tile
-    if (lane == 0 && it + S::KS < total && !*s_abort) fetch(it + S::KS);
-    // ---- what is not attended
-    if (draft || t0 + 16 > len) {
-      const unsigned long long* mask = t.mask + (size_t)b * n;
+      __syncwarp();                                                         // all lanes have read the tile
+      if (lane == 0 && it + S::KS < total && !*s_abort) fetch(it + S::KS);
+      // ---- what is not attended
+      if (draft || t0 + 16 > len) {
+        const unsigned long long* mask = t.mask + (size_t)b * n;
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
+        for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-        for (int x = 0; x < 4; ++x) {
-          const int r = t0 + key0 + (x & 2);
-          const bool on = draft ? r < n && ((mask[min(8 * nt + 2 * c + (x & 1), n - 1)] >> (r & 63)) & 1) : r < len;
-          if (!on) s[nt][x] = -INFINITY;
-        }
-    }
-    // ---- arguments relative to the references; does one have to move?  (always in the first block: -inf)
-    bool moves = false;
-    float y[NT][4];
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-      const float4 v = *reinterpret_cast<const float4*>(sr + 8 * nt + 2 * c);
-      const float s0 = v.x * back, s1 = v.z * back;
-      y[nt][0] = fmaf(s[nt][0], s0, -v.y); y[nt][1] = fmaf(s[nt][1], s1, -v.w);
-      y[nt][2] = fmaf(s[nt][2], s0, -v.y); y[nt][3] = fmaf(s[nt][3], s1, -v.w);
-      moves = moves || fmaxf(fmaxf(y[nt][0], y[nt][1]), fmaxf(y[nt][2], y[nt][3])) > 60.f;
-    }
-    if (it + 1 < total) fragments(bc, (it + 1) & 1);
-    if (it + 2 < total) bc = block_angle(it + 2);
-    const bool any_moves = group_any(group, moves);
-    if (it > 0) stats(it - 1);
-    if (any_moves) {
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-        for (int z = 0; z < 2; ++z) {
-          float m = fmaxf(s[nt][z], s[nt][2 + z]) * (sr[8 * nt + 2 * c + z].x * back);
-#pragma unroll
-          for (int o = 4; o < 32; o <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-          if (g == 0) atomicMax(smax + 8 * nt + 2 * c + z, ordered(m));
-        }
-      group_sync(group);
-      if (htid < TOK) {
-        const float m = unordered(smax[htid]);                            // (of the blocks that came here)
-        if (m > sr[htid].y + 60.f) sr[htid].y = 64.f * rintf(fminf(m, 1e30f) * (1.f / 64.f));
+          for (int x = 0; x < 4; ++x) {
+            const int r = t0 + key0 + (x & 2);
+            const bool on = draft ? r < n && ((mask[min(8 * nt + 2 * c + (x & 1), n - 1)] >> (r & 63)) & 1) : r < len;
+            if (!on) s[nt][x] = -INFINITY;
+          }
       }
-      group_sync(group);
+      // ---- arguments relative to the references; does one have to move?  (always in the first block: -inf)
+      bool moves = false;
+      float y[NT][4];
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
         const float4 v = *reinterpret_cast<const float4*>(sr + 8 * nt + 2 * c);
         const float s0 = v.x * back, s1 = v.z * back;
         y[nt][0] = fmaf(s[nt][0], s0, -v.y); y[nt][1] = fmaf(s[nt][1], s1, -v.w);
         y[nt][2] = fmaf(s[nt][2], s0, -v.y); y[nt][3] = fmaf(s[nt][3], s1, -v.w);
+        moves = moves || fmaxf(fmaxf(y[nt][0], y[nt][1]), fmaxf(y[nt][2], y[nt][3])) > 60.f;
+      }
+      if (it + 1 < total) fragments(bc, (it + 1) & 1);
+      if (it + 2 < total) bc = block_angle(it + 2);
+      const bool any_moves = group_any(group, moves);
+      if (it > 0) stats(it - 1);
+      if (any_moves) {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int z = 0; z < 2; ++z) {
+            float m = fmaxf(s[nt][z], s[nt][2 + z]) * (sr[8 * nt + 2 * c + z].x * back);
+#pragma unroll
+            for (int o = 4; o < 32; o <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+            if (g == 0) atomicMax(smax + 8 * nt + 2 * c + z, ordered(m));
+          }
+        group_sync(group);
+        if (htid < TOK) {
+          const float m = unordered(smax[htid]);                            // (of the blocks that came here)
+          if (m > sr[htid].y + 60.f) sr[htid].y = 64.f * rintf(fminf(m, 1e30f) * (1.f / 64.f));
+        }
+        group_sync(group);
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          const float4 v = *reinterpret_cast<const float4*>(sr + 8 * nt + 2 * c);
+          const float s0 = v.x * back, s1 = v.z * back;
+          y[nt][0] = fmaf(s[nt][0], s0, -v.y); y[nt][1] = fmaf(s[nt][1], s1, -v.w);
+          y[nt][2] = fmaf(s[nt][2], s0, -v.y); y[nt][3] = fmaf(s[nt][3], s1, -v.w);
+        }
+      }
+      // ---- probabilities, turned around to [token][4 keys], out; their sums over this warp's keys
+      __nv_bfloat16* Pout = p_base + (draft ? t.s_draft : blk * SC_KEYS);
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        const uint32_t d0 = movmatrix_trans(bf162_of(ex2_approx(y[nt][0]), ex2_approx(y[nt][1])));
+        const uint32_t d1 = movmatrix_trans(bf162_of(ex2_approx(y[nt][2]), ex2_approx(y[nt][3])));
+        const int i = 8 * nt + g;
+        if (i < n && (!draft || hw < 4)) *reinterpret_cast<uint2*>(Pout + (size_t)nt * p_step) = make_uint2(d0, d1);
+        float l = sum2(add2(unpack2(d0), unpack2(d1)));
+        l += __shfl_xor_sync(0xffffffffu, l, 1);
+        l += __shfl_xor_sync(0xffffffffu, l, 2);
+        if (c == 0) wsum[((it & 1) * 8 + hw) * TOK + i] = l;
       }
     }
-    // ---- probabilities, turned around to [token][4 keys], out; their sums over this warp's keys
-    __nv_bfloat16* Pout = p_base + (draft ? t.s_draft : blk * SC_KEYS);
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-      const uint32_t d0 = movmatrix_trans(bf162_of(ex2_approx(y[nt][0]), ex2_approx(y[nt][1])));
-      const uint32_t d1 = movmatrix_trans(bf162_of(ex2_approx(y[nt][2]), ex2_approx(y[nt][3])));
-      const int i = 8 * nt + g;
-      if (i < n && (!draft || hw < 4)) *reinterpret_cast<uint2*>(Pout + (size_t)nt * p_step) = make_uint2(d0, d1);
-      float l = sum2(add2(unpack2(d0), unpack2(d1)));
-      l += __shfl_xor_sync(0xffffffffu, l, 1);
-      l += __shfl_xor_sync(0xffffffffu, l, 2);
-      if (c == 0) wsum[((it & 1) * 8 + hw) * TOK + i] = l;
-    }
+    group_sync(group);
+    if (total > 0) stats(total - 1);
+    // ---- on to the next row
+    base += total;
+    remaining -= k1 - k0;
+    if (remaining == 0) break;
+    k0 = 0;
+    if (++h == p.H) { h = 0; ++b; }
+    __syncthreads();                                                      // (everyone is done with the queries, references and sums)
   }
-  group_sync(group);
-  if (total > 0) stats(total - 1);
 }
 
 // ------------------------------------------------------------------------------------------------ finish
@@ -1108,17 +1149,7 @@ cudaError_t launch_p(const slim_ctx* ctx, const CUtensorMap& cmap, const CUtenso
   auto kern = slim_tree_p_kernel<DK, NT, ROPE>;
   cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
   if (e != cudaSuccess) return e;
-  const int nblk = (p.t_cap + SC_KEYS - 1) / SC_KEYS, rows = p.H * p.batch;
-  // CTAs a (sequence, head): the fewest rounds of one CTA per SM, each a set-up of about eight blocks' time and its share
-  // of the blocks
-  constexpr int groups = ScoreShape<DK, NT>::GROUPS;
-  int gx = 1;
-  long long best = -1;
-  for (int x = 1; x <= 64 && x <= (nblk + groups - 1) / groups; ++x) {
-    const long long cost = ((long long)rows * x + ctx->num_sms - 1) / ctx->num_sms * (8 + (nblk + groups * x - 1) / (groups * x));
-    if (best < 0 || cost < best) { best = cost; gx = x; }
-  }
-  return slim_launch_pdl(kern, dim3(gx, p.H, p.batch), dim3(ScoreShape<DK, NT>::THREADS), smem, st, cmap, dmap, p, t,
+  return slim_launch_pdl(kern, dim3(ctx->num_sms), dim3(ScoreShape<DK, NT>::THREADS), smem, st, cmap, dmap, p, t,
                          reinterpret_cast<const float4*>(ctx->rope_frag));
 }
 template <int DK>
