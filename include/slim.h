@@ -296,14 +296,16 @@ slim_status slim_combine_project(slim_ctx* ctx, const float* lse_all, const floa
  *              drafted tokens; token i sits at position lengths[b] + depth(i)
  *   cache      contiguous or paged (not SLIM_FP8); it is read only: drafted keys enter it by slim_tree_commit
  *   lengths    device int32 [batch]: cached rows of sequence b (0: the tokens attend the tree only); above t_cap:
- *              clamped and reported as SLIM_ERR_CAPACITY.  Rows behind them may hold anything
+ *              clamped and reported as SLIM_ERR_CAPACITY.  Rows behind them may hold anything; a number that is not finite
+ *              in a cached row, or in the key of a token that is there, reaches every token of its sequence
  *   o          device [batch][n][d], ctx dtype (float32, or bfloat16: the operand of the output projection,
  *              rounded once at the end), 16-byte aligned; a padding token gets a zero row, and what q and
  *              k_tree hold for it is not used
  *   workspace  device, >= slim_tree_workspace_bytes(ctx, batch, t_cap, n) (0 on bad arguments), 256-byte
  *              aligned; contents are scratch.  Calls that may overlap on the GPU need one each
- *   Softmax sums and the weighted sums are float32; the tensor-core path (bf16, d % 64 == 0, d_k in {64, 96, 128})
- *   rounds the probabilities and the weighted sums to bf16 on their way into its matrix products.
+ *   Softmax sums and the weighted sums are float32.  The tensor-core path (bf16, d % 64 == 0, d_k in {64, 96, 128};
+ *   slim_set_path chooses as for slim_decode) rounds rotated queries and keys to 11 bits for the scores and the
+ *   probabilities to bf16 for the weighted sum.
  *
  * slim_tree_verify  which drafted tokens are accepted, from given random numbers, so that the tokens
  *   kept follow the target's distribution.  Node 0 is the token accepted last (the root; its own acceptance is not

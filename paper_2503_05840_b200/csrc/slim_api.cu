@@ -3,6 +3,7 @@
 #include <cstdio>
 #include <cstdlib>
 #include <cstring>
+#include <exception>
 #include <mutex>
 #include <new>
 #include <vector>
@@ -59,12 +60,13 @@ int min_tiles_for(const slim_ctx* ctx) {
   return v < 2 ? 2 : v;
 }
 
-slim_status grow_rope_base(slim_ctx* ctx, int t_cap) {
+slim_status grow_rope_base(slim_ctx* ctx, long long rows) {
   if (ctx->rope_theta == 0.0) return SLIM_OK;
-  const int tiles = (t_cap + SLIM_TT - 1) / SLIM_TT + 1;
+  const int tiles = (int)((rows + SLIM_TT - 1) / SLIM_TT) + 1;
   if (tiles <= ctx->rope_base_tiles) return SLIM_OK;
   const int half = ctx->d_k / 2;
-  std::vector<float2> tab((size_t)tiles * half);
+  std::vector<float2> tab;
+  try { tab.resize((size_t)tiles * half); } catch (const std::exception&) { return SLIM_ERR_OOM; }      // (nothing throws across the ABI)
   for (int j = 0; j < half; ++j) {
     const double th = std::pow(ctx->rope_theta, -2.0 * j / ctx->d_k);
     for (int t = 0; t < tiles; ++t) {
@@ -393,7 +395,7 @@ slim_status slim_cache_create(slim_ctx* ctx, slim_cache** out, void* k_storage, 
   if (!ctx || !k_storage || batch <= 0 || t_cap <= 0) return SLIM_ERR_INVALID_ARG;
   if (batch > SLIM_MAX_BATCH || ((uintptr_t)k_storage & 15)) return SLIM_ERR_UNSUPPORTED;
   if ((long long)batch * t_cap > 0x7fffffffLL - 64) return SLIM_ERR_UNSUPPORTED;
-  slim_status st = grow_rope_base(ctx, t_cap + SLIM_MAX_TREE);     // a tree's tokens sit behind the last row
+  slim_status st = grow_rope_base(ctx, (long long)t_cap + SLIM_MAX_TREE);     // a tree's tokens sit behind the last row
   if (st != SLIM_OK) return st;
   slim_cache* c = new (std::nothrow) slim_cache();
   if (!c) return SLIM_ERR_OOM;
@@ -428,7 +430,7 @@ slim_status slim_cache_create_paged(slim_ctx* ctx, slim_cache** out, void* pool,
   if ((long long)num_pages * page_rows > 0x7fffffffLL - 64 || (long long)batch * max_pages * page_rows > 0x7fffffffLL - 64)
     return SLIM_ERR_UNSUPPORTED;
   const int t_cap = max_pages * page_rows;
-  slim_status st = grow_rope_base(ctx, t_cap + SLIM_MAX_TREE);     // a tree's tokens sit behind the last row
+  slim_status st = grow_rope_base(ctx, (long long)t_cap + SLIM_MAX_TREE);     // a tree's tokens sit behind the last row
   if (st != SLIM_OK) return st;
   slim_cache* c = new (std::nothrow) slim_cache();
   if (!c) return SLIM_ERR_OOM;
@@ -764,6 +766,7 @@ slim_status slim_tree_decode(slim_ctx* ctx, const void* q, const void* k_tree, c
   if (!ctx->has_weights) return SLIM_ERR_NO_WEIGHTS;
   if (!current_device_is(ctx)) return SLIM_ERR_INVALID_ARG;
   const int tc = ctx->path_req != SLIM_PATH_GENERIC && slim_tree_tc_ok(ctx);
+  if (ctx->path_req == SLIM_PATH_TC && !tc) return SLIM_ERR_UNSUPPORTED;
   return launched(slim_launch_tree(ctx, cache_params(ctx, cache, q, lengths), k_tree, parents, n, o, static_cast<char*>(workspace), tc,
                                    cache->total_rows, (cudaStream_t)stream));
 }

@@ -32,7 +32,7 @@ class SlimLayer:
             assert workspace.numel() >= need and workspace.data_ptr() % 256 == 0
             self.workspace = workspace
             self.o = torch.empty((batch, d), dtype=torch.float32, device=self.device)
-            self._extra = None
+            self._extra = []
 
     # ---- set-up -------------------------------------------------------------
     def set_weights(self, W_K, W_V, want_wkv: bool = False):
@@ -76,12 +76,15 @@ class SlimLayer:
         return x
 
     def _scratch(self, need: int) -> torch.Tensor:
-        """Scratch of the calls below, kept and grown; calls of one layer run one after another on a stream."""
+        """Scratch of the calls below; calls of one layer run one after another on a stream.  It grows with the largest call
+        so far, and what was handed out before stays allocated: a captured graph keeps using it."""
         if need == 0:
             raise ValueError("unsupported sizes")
-        if self._extra is None or self._extra.numel() < need:
-            self._extra = torch.empty(need, dtype=torch.uint8, device=self.device)
-        return self._extra
+        if not self._extra or self._extra[-1].numel() < need:
+            if torch.cuda.is_current_stream_capturing():
+                raise RuntimeError("the layer's scratch has to exist before a capture: make a call of these sizes first")
+            self._extra.append(torch.empty(need, dtype=torch.uint8, device=self.device))
+        return self._extra[-1]
 
     def tree_decode(self, q: torch.Tensor, k_tree: torch.Tensor, lengths: torch.Tensor, parents: torch.Tensor,
                     o: torch.Tensor | None = None) -> torch.Tensor:

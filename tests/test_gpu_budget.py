@@ -190,7 +190,7 @@ def test_evict_refusals_and_reports():
         assert lay.device_status() == B.SLIM_ERR_CAPACITY
         with torch.cuda.device(DEV):
             kept = torch.empty((2, 8), dtype=torch.int32, device=DEV)
-            for args in ((None, acc, kept, lay._extra), (lens, None, kept, lay._extra), (lens, acc, None, lay._extra), (lens, acc, kept, None)):
+            for args in ((None, acc, kept, lay._extra[-1]), (lens, None, kept, lay._extra[-1]), (lens, acc, None, lay._extra[-1]), (lens, acc, kept, None)):
                 with pytest.raises(B.SlimError):
                     B.slim_evict(lay.ctx, lay.cache, args[0], args[1], 8, 2, args[2], args[3])
     finally:

@@ -177,6 +177,61 @@ def test_arguments_that_jump_between_blocks_of_rows(dtype):
         c.check()
 
 
+@pytest.mark.parametrize("key,query", [(3.0e5, 2.0e-6), (1.0e9, 1.0e-9), (1.0e-7, 1.0e7), (2.0e-5, 3.0e4), (1.0e-30, 1.0e3)])
+def test_keys_and_queries_of_any_magnitude(key, query):
+    """Keys beyond the range of the 16-bit products, and far below it, against queries that make up for it."""
+    with Case(256, 2, 1.0e4, "bf16", [200, 17], [[-1, 0, 1, 0], [-1, -1, 0, 2]], seed=6) as c:
+        c.K = [synth.round_to_dtype(k * np.float32(key), "bf16") for k in c.K]
+        c.kt = synth.round_to_dtype(c.kt * np.float32(key), "bf16")
+        c.q = synth.round_to_dtype(c.q * np.float32(query), "bf16")
+        for b, k in enumerate(c.K):
+            c.store[b, :len(k)] = to_dev(k, "bf16")
+        c.dq, c.dkt = to_dev(c.q, "bf16"), to_dev(c.kt, "bf16")
+        c.call()
+        assert c.status() == B.SLIM_OK
+        c.check()
+
+
+def test_many_sequences_and_the_cuda_core_kernels_agree():
+    g = np.random.default_rng(13)
+    lengths = [int(x) for x in g.integers(0, 70, 150)]
+    with Case(128, 2, 1.0e4, "bf16", lengths, [random_parents(g, 3) for _ in lengths], page=16, seed=8) as c:
+        c.call()
+        assert c.status() == B.SLIM_OK
+        c.check()
+        fast = c.o.clone()
+        B.slim_set_path(c.ctx, B.SLIM_PATH_GENERIC)
+        c.o.fill_(float("nan"))
+        c.call()
+        assert c.status() == B.SLIM_OK
+        c.check()
+        assert torch.equal(fast == 0, c.o == 0)
+
+
+def test_a_layer_keeps_the_scratch_that_a_graph_uses():
+    lay = SlimLayer(128, 2, 64, 1.0e4, "bf16", 1, 64, DEV)
+    try:
+        lay.set_wkv(np.eye(128))
+        lay.k.normal_()
+        q, kt = (torch.randn(1, 4, 128, device=DEV).bfloat16() for _ in range(2))
+        lens, par = torch.tensor([50], dtype=torch.int32, device=DEV), torch.tensor([[-1, 0, 1, 1]], dtype=torch.int32, device=DEV)
+        graph, o = torch.cuda.CUDAGraph(), torch.empty_like(q)
+        with pytest.raises(RuntimeError):
+            with torch.cuda.graph(torch.cuda.CUDAGraph()):
+                lay.tree_decode(q, kt, lens, par, o)
+        want = lay.tree_decode(q, kt, lens, par).clone()
+        with torch.cuda.graph(graph):
+            lay.tree_decode(q, kt, lens, par, o)
+        big = [torch.randn(1, 64, 128, device=DEV).bfloat16() for _ in range(2)]
+        lay.tree_decode(*big, lens, torch.arange(-1, 63, dtype=torch.int32, device=DEV)[None].contiguous())      # a larger scratch
+        other = [torch.full((1 << 20,), 255, dtype=torch.uint8, device=DEV) for _ in range(64)]
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(o, want) and all(bool((x == 255).all()) for x in other)
+    finally:
+        lay.close()
+
+
 def test_broken_trees_and_lengths_are_reported():
     with Case(128, 2, 1.0e4, "bf16", [20, 20], [[-1, 0, 1], [-1, 0, 1]], seed=1) as c:
         c.dpar = torch.tensor([[-1, 1, 0], [-1, -2, 1]], dtype=torch.int32, device=DEV)     # its own parent; a child of padding
