@@ -69,19 +69,23 @@ slim_weights_scores_kernel(const SlimDecodeParams p, float* __restrict__ scores,
     // ---- producer ----
     if (tid == WC) {
       const unsigned char* Kc = reinterpret_cast<const unsigned char*>(p.k);
-      int c = 0;
+      int st = 0;
+      uint32_t ph = 1;                                             // parity of a stage's "empty" that means free
       bool ok = true;
       for (int g = g_begin; g < g_end && ok; ++g) {
         const int b = slim_seq_of_tile(s_prefix, p.batch, g), t0 = (g - s_prefix[b]) * SLIM_TT;
         const int rows = min(SLIM_TT, min(p.lengths[b], p.t_cap) - t0);
         const unsigned char* src = Kc + (size_t)slim_cache_row(p, b, t0) * row_bytes;
-        for (int x = 0; x < per_tile; ++x, ++c) {                  // (rows behind the last one are not fetched: their sums are not used)
-          const int st = c % ring.stages, n = min(ring.rows, rows - x * ring.rows);
-          ok = mbar_wait<false>(bar_empty + 8 * st, ((c / ring.stages) & 1) ^ 1, s_abort, p.status);
+        for (int x = 0; x < per_tile; ++x) {                       // (rows behind the last one are not fetched: their sums are not used)
+          const int n = min(ring.rows, rows - x * ring.rows);
+          ok = mbar_wait<false>(bar_empty + 8 * st, ph, s_abort, p.status);
           if (!ok) break;
-          if (n <= 0) { mbar_arrive(bar_full + 8 * st); continue; }
-          mbar_arrive_expect_tx(bar_full + 8 * st, (uint32_t)n * row_bytes);
-          bulk_load(smem_u32(keys) + (uint32_t)st * stage_bytes, src + (size_t)x * stage_bytes, (uint32_t)n * row_bytes, bar_full + 8 * st);
+          if (n <= 0) mbar_arrive(bar_full + 8 * st);
+          else {
+            mbar_arrive_expect_tx(bar_full + 8 * st, (uint32_t)n * row_bytes);
+            bulk_load(smem_u32(keys) + (uint32_t)st * stage_bytes, src + (size_t)x * stage_bytes, (uint32_t)n * row_bytes, bar_full + 8 * st);
+          }
+          if (++st == ring.stages) { st = 0; ph ^= 1; }
         }
       }
       // (the consumers wait for every stage; after a time-out what was issued has landed long since)
@@ -100,7 +104,8 @@ slim_weights_scores_kernel(const SlimDecodeParams p, float* __restrict__ scores,
       const float4 st = __ldg(reinterpret_cast<const float4*>(p.rope_off + half + j0) + x);
       co[x] = pack2(st.x, st.z); si[x] = pack2(st.y, st.w);
     }
-  int c = 0;
+  int st = 0;
+  uint32_t ph = 0;                                                 // stage and parity of "full"
   for (int g = g_begin; g < g_end;) {
     const int b = slim_seq_of_tile(s_prefix, p.batch, g);
     const int seg_end = min(g_end, s_prefix[b + 1]);
@@ -137,11 +142,11 @@ slim_weights_scores_kernel(const SlimDecodeParams p, float* __restrict__ scores,
         }
       }
       float keep = -INFINITY;                                      // this lane's row of the last LPH ones
-      for (int y = 0; y < per_tile; ++y, ++c) {
-        const int st = c % ring.stages, a0 = max(r0, y * ring.rows), a1 = min(r0 + rpg, (y + 1) * ring.rows);
+      for (int y = 0; y < per_tile; ++y) {
+        const int a0 = max(r0, y * ring.rows), a1 = min(r0 + rpg, (y + 1) * ring.rows);
         // (also for stages of other groups' rows: a warp must not arrive twice on a barrier before the others have once.
         // Gave up: reported, and the loop runs on)
-        mbar_wait<false>(bar_full + 8 * st, (c / ring.stages) & 1, s_abort, p.status);
+        mbar_wait<false>(bar_full + 8 * st, ph, s_abort, p.status);
         if (a0 < a1) {
           const unsigned char* row = keys + (size_t)st * stage_bytes + (size_t)(a0 - y * ring.rows) * row_bytes + (size_t)at * sizeof(KT);
 #pragma unroll 2
@@ -177,6 +182,7 @@ slim_weights_scores_kernel(const SlimDecodeParams p, float* __restrict__ scores,
         }
         __syncwarp();
         if (lane == 0) mbar_arrive(bar_empty + 8 * st);
+        if (++st == ring.stages) { st = 0; ph ^= 1; }
       }
     }
     // (maximum, sum) of the head over this group's rows
