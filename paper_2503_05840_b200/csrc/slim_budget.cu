@@ -149,34 +149,55 @@ slim_weights_scores_kernel(const SlimDecodeParams p, float* __restrict__ scores,
         mbar_wait<false>(bar_full + 8 * st, ph, s_abort, p.status);
         if (a0 < a1) {
           const unsigned char* row = keys + (size_t)st * stage_bytes + (size_t)(a0 - y * ring.rows) * row_bytes + (size_t)at * sizeof(KT);
-#pragma unroll 2
-          for (int r = a0; r < a1; ++r, row += row_bytes) {
+          // this lane's product with a row, and the query turned one position nearer (times e^{i theta})
+          auto row_sum = [&]() {
             f32x2 f1[NP], f2[NP];
             KeyVec<KT>::unpack(*reinterpret_cast<const uint4*>(row), f1);
             KeyVec<KT>::unpack(*reinterpret_cast<const uint4*>(row + half * sizeof(KT)), f2);
+            row += row_bytes;
             f32x2 a = mul2(f1[0], z1[0]), e = mul2(f2[0], z2[0]);
 #pragma unroll
             for (int x = 1; x < NP; ++x) { a = fma2(f1[x], z1[x], a); e = fma2(f2[x], z2[x], e); }
-            float v = sum2(add2(a, e));
-            if (!mine) v = 0.f;                 // (a key element times zero could be NaN)
-#pragma unroll
-            for (int o = 1; o < LPH; o <<= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-            if (r % LPH == li) keep = v;
+            const float v = sum2(add2(a, e));
             if (ROPE)
 #pragma unroll
-              for (int x = 0; x < NP; ++x) {                       // one position nearer: times e^{i theta}
+              for (int x = 0; x < NP; ++x) {
                 const f32x2 n1 = sub2(mul2(z1[x], co[x]), mul2(z2[x], si[x]));
                 z2[x] = fma2(z1[x], si[x], mul2(z2[x], co[x]));
                 z1[x] = n1;
               }
-            if ((r + 1) % LPH == 0 || r + 1 == r0 + rpg) {         // every lane of the head has its row: row r - r % LPH + li
-              const int t = t0 + r - r % LPH + li;
-              if (li <= r % LPH && li >= r0 % LPH && t < len && h < H) {
-                out[t] = keep;
-                const float top = fmaxf(run_m, keep);
-                if (top != -INFINITY) run_l = run_l * ex2_approx(run_m - top) + ex2_approx(keep - top);
-                run_m = top;
-              }
+            return mine ? v : 0.f;                                 // (a key element times zero could be NaN)
+          };
+          // rows r - r % LPH + li, up to r, lie in the lanes that keep them
+          auto take = [&](int r) {
+            const int t = t0 + r - r % LPH + li;
+            if (li <= r % LPH && li >= r0 % LPH && t < len && h < H) {
+              out[t] = keep;
+              const float top = fmaxf(run_m, keep);
+              if (top != -INFINITY) run_l = run_l * ex2_approx(run_m - top) + ex2_approx(keep - top);
+              run_m = top;
+            }
+          };
+          if (((a0 | a1) & 3) == 0) {
+            // four rows at a time: the sums over the lanes of a head turn the rows around, lane li ends with row li % 4
+            for (int r = a0; r < a1; r += 4) {
+              const float v0 = row_sum(), v1 = row_sum(), v2 = row_sum(), v3 = row_sum();
+              const bool b0 = li & 1, b1 = li & 2;
+              const float x0 = (b0 ? v1 : v0) + __shfl_xor_sync(0xffffffffu, b0 ? v0 : v1, 1);
+              const float x1 = (b0 ? v3 : v2) + __shfl_xor_sync(0xffffffffu, b0 ? v2 : v3, 1);
+              float y4 = (b1 ? x1 : x0) + __shfl_xor_sync(0xffffffffu, b1 ? x0 : x1, 2);
+#pragma unroll
+              for (int o = 4; o < LPH; o <<= 1) y4 += __shfl_xor_sync(0xffffffffu, y4, o);
+              if (li / 4 == r / 4 % (LPH / 4)) keep = y4;
+              if ((r + 4) % LPH == 0 || r + 4 == r0 + rpg) take(r + 3);
+            }
+          } else {
+            for (int r = a0; r < a1; ++r) {
+              float v = row_sum();
+#pragma unroll
+              for (int o = 1; o < LPH; o <<= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+              if (r % LPH == li) keep = v;
+              if ((r + 1) % LPH == 0 || r + 1 == r0 + rpg) take(r);
             }
           }
         }
@@ -208,11 +229,17 @@ __global__ void __launch_bounds__(256) slim_weights_join_kernel(const SlimDecode
   float m = -INFINITY, l = 0.f;
   if (s_prefix2[b + 1] > s_prefix2[b]) {
     const int w0 = slim_worker_of_tile(sc, s_prefix2[b]), w1 = slim_worker_of_tile(sc, s_prefix2[b + 1] - 1);
-    for (int i = (w0 + b) * groups + lane; i < (w1 + 1 + b) * groups; i += 32) {
-      const float2 v = part[(size_t)i * p.H + h];
-      const float top = fmaxf(m, v.x);
-      if (top != -INFINITY) l = l * exp2f(m - top) + v.y * exp2f(v.x - top);
-      m = top;
+    const int end = (w1 + 1 + b) * groups;
+    for (int i = (w0 + b) * groups + lane; i < end; i += 128) {
+      float2 v[4];
+#pragma unroll
+      for (int x = 0; x < 4; ++x) v[x] = i + 32 * x < end ? part[(size_t)(i + 32 * x) * p.H + h] : make_float2(-INFINITY, 0.f);
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        const float top = fmaxf(m, v[x].x);
+        if (top != -INFINITY) l = l * exp2f(m - top) + v[x].y * exp2f(v[x].x - top);
+        m = top;
+      }
     }
   }
 #pragma unroll
