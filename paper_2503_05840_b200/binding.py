@@ -101,15 +101,13 @@ def _check(status: int, where: str) -> None:
         raise SlimError(status, where)
 
 
-def _ptr(x) -> c_void_p:
-    """Raw address of a torch tensor / numpy array / int / None."""
-    if x is None:
-        return c_void_p(0)
-    if isinstance(x, int):
-        return c_void_p(x)
+def _ptr(x):
+    """Raw address of a torch tensor / numpy array / int / None, as ctypes takes it for a void pointer."""
+    if x is None or isinstance(x, int):
+        return x
     if isinstance(x, np.ndarray):
-        return c_void_p(x.ctypes.data)
-    return c_void_p(x.data_ptr())        # torch.Tensor
+        return x.ctypes.data
+    return x.data_ptr()        # torch.Tensor
 
 
 def _host_mat(a):
@@ -266,20 +264,20 @@ def slim_tree_workspace_bytes(ctx: int, batch: int, t_cap: int, n: int) -> int:
 
 def slim_tree_decode(ctx: int, q, k_tree, cache: int, lengths, parents, n: int, o, workspace, stream: int = 0) -> None:
     """Attention of n drafted tokens a sequence (a tree given by `parents`) over the cache, their ancestors and themselves."""
-    _check(lib().slim_tree_decode(c_void_p(ctx), _ptr(q), _ptr(k_tree), c_void_p(cache), _ptr(lengths), _ptr(parents), n, _ptr(o),
-                                  _ptr(workspace), c_void_p(stream)), "slim_tree_decode")
+    _check(lib().slim_tree_decode(ctx, _ptr(q), _ptr(k_tree), cache, _ptr(lengths), _ptr(parents), n, _ptr(o),
+                                  _ptr(workspace), stream), "slim_tree_decode")
 
 
 def slim_tree_verify(ctx: int, p, q, tokens, parents, r, batch: int, n: int, vocab: int, path, count, next_token, stream: int = 0) -> None:
     """Which drafted tokens are accepted (path, count) and the token drawn after them, from given random numbers."""
-    _check(lib().slim_tree_verify(c_void_p(ctx), _ptr(p), _ptr(q), _ptr(tokens), _ptr(parents), _ptr(r), batch, n, vocab, _ptr(path),
-                                  _ptr(count), _ptr(next_token), c_void_p(stream)), "slim_tree_verify")
+    _check(lib().slim_tree_verify(ctx, _ptr(p), _ptr(q), _ptr(tokens), _ptr(parents), _ptr(r), batch, n, vocab, _ptr(path),
+                                  _ptr(count), _ptr(next_token), stream), "slim_tree_verify")
 
 
 def slim_tree_commit(ctx: int, cache: int, k_tree, lengths, path, count, n: int, stream: int = 0) -> None:
     """The accepted tokens' keys go to cache rows lengths[b] + j; the caller adds count to lengths after the last layer."""
-    _check(lib().slim_tree_commit(c_void_p(ctx), c_void_p(cache), _ptr(k_tree), _ptr(lengths), _ptr(path), _ptr(count), n,
-                                  c_void_p(stream)), "slim_tree_commit")
+    _check(lib().slim_tree_commit(ctx, cache, _ptr(k_tree), _ptr(lengths), _ptr(path), _ptr(count), n,
+                                  stream), "slim_tree_commit")
 
 
 def slim_weights_workspace_bytes(ctx: int, batch: int, t_cap: int) -> int:
@@ -288,8 +286,8 @@ def slim_weights_workspace_bytes(ctx: int, batch: int, t_cap: int) -> int:
 
 def slim_accumulate_weights(ctx: int, q, cache: int, lengths, acc, workspace, stream: int = 0) -> None:
     """acc[b][t] += the probabilities of cache row t under the query of slim_decode, summed over the heads."""
-    _check(lib().slim_accumulate_weights(c_void_p(ctx), _ptr(q), c_void_p(cache), _ptr(lengths), _ptr(acc), _ptr(workspace),
-                                         c_void_p(stream)), "slim_accumulate_weights")
+    _check(lib().slim_accumulate_weights(ctx, _ptr(q), cache, _ptr(lengths), _ptr(acc), _ptr(workspace),
+                                         stream), "slim_accumulate_weights")
 
 
 def slim_evict_workspace_bytes(ctx: int, batch: int, t_cap: int) -> int:
@@ -298,8 +296,8 @@ def slim_evict_workspace_bytes(ctx: int, batch: int, t_cap: int) -> int:
 
 def slim_evict(ctx: int, cache: int, lengths, acc, budget: int, recent: int, kept, workspace, stream: int = 0) -> None:
     """Sequences longer than `budget` rows keep the last `recent` and the heaviest of the others, moved to the front in order."""
-    _check(lib().slim_evict(c_void_p(ctx), c_void_p(cache), _ptr(lengths), _ptr(acc), budget, recent, _ptr(kept), _ptr(workspace),
-                            c_void_p(stream)), "slim_evict")
+    _check(lib().slim_evict(ctx, cache, _ptr(lengths), _ptr(acc), budget, recent, _ptr(kept), _ptr(workspace),
+                            stream), "slim_evict")
 
 
 def slim_device_status(ctx: int, stream: int = 0) -> int:
