@@ -577,7 +577,7 @@ __global__ void __launch_bounds__(1024) slim_tree_finish_kernel(const SlimDecode
 // the partial one, the drafted keys).  Every tile of every sequence may be cut into S equal parts of its stages
 // (subtiles; S > 1 where there are fewer tiles than CTA pairs).  The subtiles, in the order (sequence, part, tile), go
 // to the pairs in turn, F of them as a whole, so that pairs in flight walk the same keys and the same rows of P at the
-// same time and share them in L2; what is left over, about a wave, is laid on a line and cut so that every pair ends
+// same time and share them in L2; what is left over, about a round, is laid on a line and cut so that every pair ends
 // up with the same number of stages.  A piece that is not a whole tile leaves float32 sums in a slot, and `join` adds
 // the slots of a tile in the order of its keys: the schedule is a function of the lengths alone, so results are repeatable.
 struct SumSched {
@@ -1211,14 +1211,20 @@ void slim_tree_tc_layout(const slim_ctx* ctx, int batch, int t_cap, int n, SlimT
   L.g_ncol = (ctx->d + SU_COLS - 1) / SU_COLS;
   L.g_tiles = L.g_ncol * (int)((R + L.mt * 256 - 1) / (L.mt * 256));
   L.g_pairs = ctx->num_sms / 2;
-  // fewer than two tiles a pair: cut each into parts of at least eight stages, for about four parts a pair
+  // Fewer tiles than pairs, and more probabilities than stay in L2 beside the keys: every tile is cut into parts of at
+  // least eight stages, for about five parts a pair, so that the pairs in flight walk the same rows of P (64 drafts over
+  // 131001 rows: 1.90 ms whole, 1.46 ms in five parts).  Otherwise parts only cost: every one drains its sums, and they
+  // make a trip to memory and back (16 drafts over 8 x 12000 rows: 0.30 ms whole, 0.34 ms in three parts).
   const long long tiles = (long long)batch * L.g_tiles;
-  long long split = tiles < 2 * L.g_pairs ? (4LL * L.g_pairs + tiles - 1) / tiles : 1;
+  const bool p_in_l2 = 2.0 * batch * (double)R * t_cap <= 96e6;
+  long long split = tiles < L.g_pairs && !p_in_l2 ? (4LL * L.g_pairs + tiles - 1) / tiles : 1;
   const long long most = (t_cap / 64 + 2) / 8;
   if (split > most) split = most;
   L.g_split = split < 1 ? 1 : (int)split;
   if (tiles * L.g_split < L.g_pairs) L.g_split = 1;       // (no whole part for every pair: the tiles are cut where the pairs' shares end)
-  const long long sub = tiles * L.g_split, waves = sub / L.g_pairs - (batch > 1 ? 1 : 0);   // (ragged lengths: level them with a wave)
+  // whole rounds of tiles; what is left over levels the pairs' loads, so a batch (ragged, perhaps) keeps a quarter of a
+  // round for that
+  const long long sub = tiles * L.g_split, waves = sub / L.g_pairs - (batch > 1 && sub % L.g_pairs < L.g_pairs / 4 ? 1 : 0);
   L.g_whole = waves > 0 ? (int)(waves * L.g_pairs) : 0;
   L.p_s_draft = nb * SC_KEYS;
   L.p_ld = L.p_s_draft + 64;
