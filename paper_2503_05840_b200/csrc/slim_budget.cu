@@ -535,12 +535,20 @@ slim_evict_move_kernel(unsigned char* __restrict__ base, int vecs, const int32_t
 }
 
 template <typename VT>
-cudaError_t launch_move(const slim_ctx* ctx, const slim_cache* c, void* base, size_t row_bytes, const int32_t* lengths, int budget,
+cudaError_t launch_move_as(const slim_ctx* ctx, const slim_cache* c, void* base, size_t row_bytes, const int32_t* lengths, int budget,
                         const int32_t* kept, float* acc, const float* kept_acc, cudaStream_t st) {
   const int vecs = (int)(row_bytes / sizeof(VT));
   return slim_launch_pdl(slim_evict_move_kernel<VT>, dim3((vecs + MV_COLS - 1) / MV_COLS + (acc ? MV_ACC : 0), c->batch), dim3(MV_THREADS), 0, st,
                          (unsigned char*)base, vecs, lengths, c->t_cap, budget, kept, c->block_table, c->page_rows, c->max_pages,
                          c->num_pages, acc, kept_acc, ctx->status);
+}
+
+// Rows in the widest vectors that divide them (storage and exponents begin on 16-byte boundaries).
+cudaError_t launch_move(const slim_ctx* ctx, const slim_cache* c, void* base, size_t row_bytes, const int32_t* lengths, int budget,
+                        const int32_t* kept, float* acc, const float* kept_acc, cudaStream_t st) {
+  if (row_bytes % 16 == 0) return launch_move_as<uint4>(ctx, c, base, row_bytes, lengths, budget, kept, acc, kept_acc, st);
+  if (row_bytes % 4 == 0) return launch_move_as<unsigned>(ctx, c, base, row_bytes, lengths, budget, kept, acc, kept_acc, st);
+  return launch_move_as<unsigned char>(ctx, c, base, row_bytes, lengths, budget, kept, acc, kept_acc, st);
 }
 
 template <int CL>
@@ -610,14 +618,9 @@ cudaError_t slim_launch_evict(const slim_ctx* ctx, const slim_cache* c, const in
   cudaError_t e = c->t_cap >= 8192 ? launch_select<8>(ctx, c, lengths, acc, budget, recent, kept, kept_acc, st)
                                    : launch_select<1>(ctx, c, lengths, acc, budget, recent, kept, kept_acc, st);
   if (e != cudaSuccess) return e;
-  if (ctx->kdtype == SLIM_FP8) {     // codes, then the exponents of the same rows
-    const size_t row = (size_t)ctx->d;
-    e = (row & 15) == 0 ? launch_move<uint4>(ctx, c, c->k, row, lengths, budget, kept, acc, kept_acc, st)
-                        : launch_move<unsigned short>(ctx, c, c->k, row, lengths, budget, kept, acc, kept_acc, st);
-    if (e == cudaSuccess) e = launch_move<unsigned char>(ctx, c, c->k_exp, ctx->H, lengths, budget, kept, nullptr, nullptr, st);
-    return e;
-  }
-  const size_t row = (size_t)ctx->d * (ctx->kdtype == SLIM_BF16 ? 2 : 4);
-  if ((row & 15) == 0) return launch_move<uint4>(ctx, c, c->k, row, lengths, budget, kept, acc, kept_acc, st);
-  return launch_move<unsigned short>(ctx, c, c->k, row, lengths, budget, kept, acc, kept_acc, st);
+  const size_t row = (size_t)ctx->d * (ctx->kdtype == SLIM_FP8 ? 1 : ctx->kdtype == SLIM_BF16 ? 2 : 4);
+  e = launch_move(ctx, c, c->k, row, lengths, budget, kept, acc, kept_acc, st);
+  if (e == cudaSuccess && ctx->kdtype == SLIM_FP8)       // the exponents of the same rows
+    e = launch_move(ctx, c, c->k_exp, ctx->H, lengths, budget, kept, nullptr, nullptr, st);
+  return e;
 }

@@ -194,10 +194,11 @@ slim_tree_p_kernel(const __grid_constant__ CUtensorMap cmap, const __grid_consta
     if (warp == 0) { mbar_init(bar_table, 1); prefetch_tensormap(&cmap); prefetch_tensormap(&dmap); *s_abort = 0; }
     fence_mbar_init();
   }
-  if (ROPE && !S::CSR && tid == 0) {                                               // (a table of the context: no need to wait for it)
+  if (ROPE && !S::CSR && tid == 0) {                                      // (a table of the context: no need to wait for it)
     mbar_arrive_expect_tx(bar_table, (uint32_t)S::CS);
     bulk_load(smem_u32(cst), table, (uint32_t)S::CS, bar_table);
   }
+  __syncthreads();                                                        // (the abort flag is read from here on)
   slim_pdl_trigger();
   slim_pdl_wait();
   const int nb_cap = (p.t_cap + SC_KEYS - 1) / SC_KEYS;
@@ -211,7 +212,10 @@ slim_tree_p_kernel(const __grid_constant__ CUtensorMap cmap, const __grid_consta
     for (int o = 16; o > 0; o >>= 1) all += __shfl_xor_sync(0xffffffffu, all, o);
     const int a0 = (int)((long long)all * blockIdx.x / gridDim.x);
     remaining = (int)((long long)all * (blockIdx.x + 1) / gridDim.x) - a0;
-    if (remaining == 0) return;
+    if (remaining == 0) {                                                 // (not before the table has landed)
+      if (ROPE && !S::CSR && tid == 0) mbar_wait<false>(bar_table, 0, s_abort, p.status);
+      return;
+    }
     for (int q0 = 0, before = 0; q0 < p.batch; q0 += 32) {
       const int mine = row_blocks(q0 + lane);
       int incl = mine;

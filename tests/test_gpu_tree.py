@@ -325,6 +325,21 @@ def test_repeatable_on_streams_and_in_graphs():
         c.check()
 
 
+@pytest.mark.parametrize("d,H,n,lengths", [(512, 4, 40, [130, 5]), (4096, 32, 17, [3000, 64, 0]), (1280, 20, 64, [700])])
+def test_two_hundred_calls_give_the_same_bits(d, H, n, lengths):
+    """Calls back to back, with CTAs that have no block of their own among them."""
+    g = np.random.default_rng(n)
+    with Case(d, H, 1.0e4, "bf16", lengths, [random_parents(g, n) for _ in lengths], seed=4) as c:
+        c.call()
+        want = c.o.clone()
+        differ = torch.zeros((), dtype=torch.int64, device=DEV)
+        for _ in range(200):
+            c.call()
+            differ += (c.o != want).sum()
+        assert c.status() == B.SLIM_OK
+        assert differ.item() == 0
+
+
 def test_tree_pages_behind_four_billion_elements():
     """A pool whose last pages lie beyond 2^32 elements from its start."""
     d, H, page, L = 4096, 32, 64, 200
