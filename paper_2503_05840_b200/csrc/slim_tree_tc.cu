@@ -956,31 +956,32 @@ __global__ void __launch_bounds__(256) slim_tree_join_kernel(const SlimDecodePar
   if (row0 >= R) return;
   for (int q = tid; q <= s.P; q += 256) s_cut[q] = t.sched[p.batch + 1 + q];
   const int bf = s.F / (s.S * s.tiles), inf = s.F - bf * s.S * s.tiles;                 // subtile F
+  const int nk = stages_of(t.len[b]), nkf = bf < p.batch ? stages_of(t.len[bf]) : 0;
+  const long long pre_b = t.sched[b], pre_f = t.sched[bf];
   __syncthreads();
-  if (tid == 0) {
+  if (tid < 32) {
     int cnt = 0;
-    const int nk = stages_of(t.len[b]), nkf = bf < p.batch ? stages_of(t.len[bf]) : 0;
     const int f0 = part_begin(nkf, inf / s.tiles, s.S), f1 = part_begin(nkf, inf / s.tiles + 1, s.S);
-    const long long g0 = t.sched[bf] + (long long)s.tiles * f0 + (long long)(inf % s.tiles) * (f1 - f0);
+    const long long g0 = pre_f + (long long)s.tiles * f0 + (long long)(inf % s.tiles) * (f1 - f0);
     for (int part = 0; part < s.S; ++part) {
       const int idx = (b * s.S + part) * s.tiles + tile;
       const int k0 = part_begin(nk, part, s.S), k1 = part_begin(nk, part + 1, s.S);
       if (k0 == k1) continue;
       if (idx < s.F) {
-        if (s.S > 1) s_slot[cnt++] = 2 * s.P + idx;
+        if (s.S > 1) { if (tid == 0) s_slot[cnt] = 2 * s.P + idx; ++cnt; }
         continue;
       }
-      const long long x0 = t.sched[b] + (long long)s.tiles * k0 + (long long)tile * (k1 - k0) - g0, x1 = x0 + (k1 - k0);
-      int lo = 0, hi = s.P;                                // the pair whose segment holds x0: the last one with cut <= x0 < next cut
-      while (hi - lo > 1) { const int mid = (lo + hi) >> 1; if (s_cut[mid] <= x0) lo = mid; else hi = mid; }
-      for (int q = lo; q < s.P && s_cut[q] < x1; ++q) {
-        const long long a = max(s_cut[q], x0), z = min(s_cut[q + 1], x1);
-        if (a >= z) continue;
-        if (a == x0 && z == x1) { if (s.S > 1) s_slot[cnt++] = 2 * s.P + idx; }
-        else s_slot[cnt++] = a > x0 ? 2 * q : 2 * q + 1;
+      const long long x0 = pre_b + (long long)s.tiles * k0 + (long long)tile * (k1 - k0) - g0, x1 = x0 + (k1 - k0);
+      for (int q0 = 0; q0 < s.P; q0 += 32) {               // the pairs whose segments meet [x0, x1), in order
+        const int q = q0 + tid;
+        const long long a = q < s.P ? max(s_cut[q], x0) : 0, z = q < s.P ? min(s_cut[q + 1], x1) : 0;
+        const bool whole = a == x0 && z == x1, in = a < z && !(whole && s.S == 1);
+        const unsigned hit = __ballot_sync(0xffffffffu, in);
+        if (in) s_slot[cnt + __popc(hit & ((1u << tid) - 1u))] = whole ? 2 * s.P + idx : a > x0 ? 2 * q : 2 * q + 1;
+        cnt += __popc(hit);
       }
     }
-    s_n = cnt;
+    if (tid == 0) s_n = cnt;
   }
   __syncthreads();
   const int cnt = s_n;
@@ -996,8 +997,7 @@ __global__ void __launch_bounds__(256) slim_tree_join_kernel(const SlimDecodePar
   for (int k = 0; k < cnt; ++k) {
     const float* slot = src + (size_t)s_slot[k] * mt * 256 * SU_COLS;
 #pragma unroll
-    for (int m = 0; m < 4; ++m) {
-      if (row0 + tid / 64 + 4 * m >= R) continue;
+    for (int m = 0; m < 4; ++m) {                          // (rows behind the last one are in the slot too, and not used)
       const float4 v = *reinterpret_cast<const float4*>(slot + (size_t)4 * m * SU_COLS);
       a[m].x += v.x; a[m].y += v.y; a[m].z += v.z; a[m].w += v.w;
     }
