@@ -22,7 +22,7 @@ struct SlimTreeView {
   __nv_bfloat16* tail;               // [batch][128][d] partial last block of cached rows, drafted keys
   __nv_bfloat16* uh;                 // [2][H][batch n][d] weighted sums as (bf16, bf16 of what that leaves)
   float* part;                       // [slots][mt 256][256] sums of pieces that are not whole tiles
-  long long* sched;                  // [batch + 1 + pairs + 1] the product's schedule, for the join
+  long long* sched;                  // [batch + 1 + pairs + 1 + 1] the product's schedule
   int g_tiles, g_ncol, g_split, g_pairs, g_whole;      // schedule of the product (slim_tree_tc.cu)
 };
 

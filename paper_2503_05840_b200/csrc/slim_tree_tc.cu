@@ -3,10 +3,9 @@
 // One sequence of L rows and n tokens has R = H n rows of probabilities and a weighted sum of R x d numbers (32 MB at
 // n = 64, d = 4096): it cannot stay on chip as the one-token kernel's does, and its products, 2 L R d, are H times
 // those of the scores.  So the step is a chain of kernels around one large matrix product:
-//   tail        the trees' masks and depths; the last, partial block of 64 cached rows and the drafted keys, zero-padded,
-//               in a scratch tail, so that the product only meets whole blocks of 64 finite rows
 //   scores      P = 2^(s - ref) in bf16, [b][h n + i][t], and (ref, sum) per row and block of 128 keys
-//   finish      the row's reference and 1 / l
+//   finish      the row's reference and 1 / l; the last, partial block of 64 cached rows and the drafted keys, zero-padded,
+//               in a scratch tail, so that the product only meets whole blocks of 64 finite rows; the product's schedule
 //   sum         U = P K / l on tcgen05, CTA pairs (cta_group::2), bf16
 //   join        adds the parts of tiles whose keys were cut
 //   out         o = U W_KV,h on tcgen05
@@ -24,52 +23,6 @@ namespace {
 __device__ __forceinline__ float2 turn(const SlimDecodeParams& p, int pos, int j) {      // (cos, sin) of pos theta_j
   const float2 cb = __ldg(p.rope_base + (size_t)(pos / SLIM_TT) * p.half + j), co = __ldg(p.rope_off + (pos % SLIM_TT) * p.half + j);
   return make_float2(cb.x * co.x - cb.y * co.y, cb.y * co.x + cb.x * co.y);
-}
-
-// ------------------------------------------------------------------------------------------------ tail
-// Block (x, b): rows 2 x, 2 x + 1 of sequence b's tail [128][d]: 0..63 the cached rows behind the last whole block of
-// 64, 64..127 the drafted keys; everything else is zero.  Block 0 also writes the tree's masks and depths.
-__global__ void __launch_bounds__(256) slim_tree_tail_kernel(const SlimDecodeParams p, const SlimTreeView t, const int32_t* __restrict__ parents) {
-  __shared__ int s_par[SLIM_MAX_TREE];
-  slim_pdl_trigger();
-  slim_pdl_wait();
-  const int b = blockIdx.y, n = t.n, tid = threadIdx.x, vecs = p.d / 8;
-  if (tid < n) {
-    const int q = parents[(size_t)b * n + tid];
-    s_par[tid] = q >= tid ? -3 : q < -1 ? -2 : q;
-  }
-  int len = p.lengths[b];
-  const bool over = len > p.t_cap;
-  len = len < 0 ? 0 : over ? p.t_cap : len;
-  __syncthreads();
-  if (blockIdx.x == 0) {
-    if (tid == 0) { t.len[b] = len; if (over) atomicMax(p.status, (int)SLIM_ERR_CAPACITY); }
-    if (tid < n) {
-      unsigned long long m;
-      int dep;
-      bool broken;
-      slim_tree_chain(s_par, tid, m, dep, broken);
-      if (broken) atomicMax(p.status, (int)SLIM_ERR_TREE);
-      t.mask[(size_t)b * n + tid] = m;
-      t.depth[(size_t)b * n + tid] = dep;
-    }
-  }
-#pragma unroll
-  for (int rr = 0; rr < 2; ++rr) {
-    const int r = blockIdx.x * 2 + rr, row = (len & ~63) + r;
-    const uint4* src = nullptr;
-    if (r < 64) {
-      if (row < len) src = reinterpret_cast<const uint4*>(p.k) + (size_t)(slim_cache_row(p, b, row & ~(SLIM_TT - 1)) + (row & (SLIM_TT - 1))) * vecs;
-    } else if (r - 64 < n) {
-      unsigned long long m;
-      int dep;
-      bool broken;
-      slim_tree_chain(s_par, r - 64, m, dep, broken);
-      if (dep >= 0) src = reinterpret_cast<const uint4*>(t.k_tree) + ((size_t)b * n + r - 64) * vecs;
-    }
-    uint4* dst = reinterpret_cast<uint4*>(t.tail) + ((size_t)b * 128 + r) * vecs;
-    for (int e = tid; e < vecs; e += 256) dst[e] = src ? __ldg(src + e) : make_uint4(0, 0, 0, 0);
-  }
 }
 
 // ------------------------------------------------------------------------------------------------ scores
@@ -168,7 +121,7 @@ __device__ __forceinline__ bool group_any(int group, bool v) {
 template <int DK, int NT, bool ROPE>
 __global__ void __launch_bounds__((ScoreShape<DK, NT>::THREADS), 1)
 slim_tree_p_kernel(const __grid_constant__ CUtensorMap cmap, const __grid_constant__ CUtensorMap dmap, const SlimDecodeParams p,
-                   const SlimTreeView t, const float4* __restrict__ table) {
+                   const SlimTreeView t, const int32_t* __restrict__ parents, const float4* __restrict__ table) {
   typedef ScoreShape<DK, NT> S;
   constexpr int HALF = S::HALF, VW = S::VW, NPC = S::NPC, TOK = 8 * NT;
   typedef typename KVec<VW>::type kvec;
@@ -188,6 +141,8 @@ slim_tree_p_kernel(const __grid_constant__ CUtensorMap cmap, const __grid_consta
   const uint32_t bar_table = smem_u32(tail), bar = bar_table + 8u * (uint32_t)(1 + warp * S::KS);      // this warp's barriers
   volatile int* s_abort = reinterpret_cast<volatile int*>(tail + 8 * (S::WARPS * S::KS + 1));
   const int n = t.n, R = p.H * n;
+  __shared__ int s_par[SLIM_MAX_TREE], s_dep[SLIM_MAX_TREE];              // the current sequence's tree
+  __shared__ unsigned long long s_mask[SLIM_MAX_TREE];
 
   if (lane == 0) {
     for (int i = 0; i < S::KS; ++i) mbar_init(bar + 8 * i, 1);
@@ -198,6 +153,16 @@ slim_tree_p_kernel(const __grid_constant__ CUtensorMap cmap, const __grid_consta
     mbar_arrive_expect_tx(bar_table, (uint32_t)S::CS);
     bulk_load(smem_u32(cst), table, (uint32_t)S::CS, bar_table);
   }
+  // MMA rows g and g + 8 are keys key0 and key0 + 2 of the warp's tile: turned around, a thread then holds four
+  // neighbouring keys of a token
+  const int key0 = 4 * (g >> 1) + (g & 1);
+  constexpr int NCS = S::CSR && ROPE ? NPC * (VW / 2) : 1;
+  ulonglong2 csr[2][NCS];                                                 // (cos, cos), (sin, sin) of this thread's keys and pairs
+  auto angles = [&](int rh, int o) {                                      // of key offset o
+#pragma unroll
+    for (int x = 0; x < NCS; ++x) csr[rh][x] = __ldg(reinterpret_cast<const ulonglong2*>(table) + ((o >> 3) * NCS + x) * 32 + ((o & 7) << 2) + c);
+  };
+  if (S::CSR && ROPE) { angles(0, 16 * hw + key0); angles(1, 16 * hw + key0 + 2); }
   __syncthreads();                                                        // (the abort flag is read from here on)
   slim_pdl_trigger();
   slim_pdl_wait();
@@ -205,9 +170,11 @@ slim_tree_p_kernel(const __grid_constant__ CUtensorMap cmap, const __grid_consta
   // this CTA's share of the line of blocks, and where it begins; the same in every warp
   int b = 0, h = 0, k0 = 0, remaining;
   {
-    auto row_blocks = [&](int q) { return q < p.batch ? p.H * ((t.len[q] + SC_KEYS - 1) / SC_KEYS + 1) : 0; };
+    auto row_blocks = [&](int q) { return q < p.batch ? p.H * ((min(max(p.lengths[q], 0), p.t_cap) + SC_KEYS - 1) / SC_KEYS + 1) : 0; };
     int all = 0;
-    for (int q = lane; q < p.batch; q += 32) all += row_blocks(q);
+    const int first32 = row_blocks(lane);
+    for (int q = lane + 32; q < p.batch; q += 32) all += row_blocks(q);
+    all += first32;
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) all += __shfl_xor_sync(0xffffffffu, all, o);
     const int a0 = (int)((long long)all * blockIdx.x / gridDim.x);
@@ -217,15 +184,15 @@ slim_tree_p_kernel(const __grid_constant__ CUtensorMap cmap, const __grid_consta
       return;
     }
     for (int q0 = 0, before = 0; q0 < p.batch; q0 += 32) {
-      const int mine = row_blocks(q0 + lane);
+      const int mine = q0 ? row_blocks(q0 + lane) : first32;
       int incl = mine;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) { const int v = __shfl_up_sync(0xffffffffu, incl, o); if (lane >= o) incl += v; }
       const unsigned hit = __ballot_sync(0xffffffffu, before + incl > a0);
       if (hit) {
-        const int l = __ffs(hit) - 1, in = a0 - before - (__shfl_sync(0xffffffffu, incl, l) - __shfl_sync(0xffffffffu, mine, l));
+        const int l = __ffs(hit) - 1, row = __shfl_sync(0xffffffffu, mine, l), in = a0 - before - (__shfl_sync(0xffffffffu, incl, l) - row);
+        const int nb = row / p.H;
         b = q0 + l;
-        const int nb = (t.len[b] + SC_KEYS - 1) / SC_KEYS + 1;
         h = in / nb; k0 = in - h * nb;
         break;
       }
@@ -234,7 +201,7 @@ slim_tree_p_kernel(const __grid_constant__ CUtensorMap cmap, const __grid_consta
   }
   int len = 0, nblk = 0, first = 0, mine = 0, total = 0, base = 0;        // of the current row; base: key tiles of the rows before
   constexpr int step = S::GROUPS;
-  const int* dep;
+  int tree = -1;                                                          // the sequence whose tree is in shared memory
 
   // this thread's part of the query fragments: pairs j0, j0 + 1 of token 8 nt + lane / 4, for nt = nt0, nt0 + NTS, ..
   constexpr int NTS = SC_GROUP / S::PER;
@@ -275,15 +242,6 @@ slim_tree_p_kernel(const __grid_constant__ CUtensorMap cmap, const __grid_consta
       }
     }
   };
-  // MMA rows g and g + 8 are keys key0 and key0 + 2 of the warp's tile: turned around, a thread then holds four
-  // neighbouring keys of a token
-  const int key0 = 4 * (g >> 1) + (g & 1);
-  constexpr int NCS = S::CSR && ROPE ? NPC * (VW / 2) : 1;
-  ulonglong2 csr[2][NCS];                                                 // (cos, cos), (sin, sin) of this thread's keys and pairs
-  auto angles = [&](int rh, int o) {                                      // of key offset o
-#pragma unroll
-    for (int x = 0; x < NCS; ++x) csr[rh][x] = __ldg(reinterpret_cast<const ulonglong2*>(table) + ((o >> 3) * NCS + x) * 32 + ((o & 7) << 2) + c);
-  };
   // sums and references of block `it`, once all warps have left theirs
   auto stats = [&](int it) {
     if (htid < n) {
@@ -297,22 +255,44 @@ slim_tree_p_kernel(const __grid_constant__ CUtensorMap cmap, const __grid_consta
   __syncwarp();
   for (;;) {
     // ---- the next row: blocks k0 .. k1 - 1 of (b, h), the drafted keys' being number nblk
-    len = t.len[b]; nblk = (len + SC_KEYS - 1) / SC_KEYS;
+    const int stored = p.lengths[b];
+    len = min(max(stored, 0), p.t_cap); nblk = (len + SC_KEYS - 1) / SC_KEYS;
     const int k1 = min(nblk + 1, k0 + remaining);
     first = k0 + group;
     total = k1 > first ? (k1 - 1 - first) / step + 1 : 0;
     mine = total > 0 && k1 == nblk + 1 && first + (total - 1) * step == nblk ? total - 1 : 0x7fffffff;      // which block is the drafted keys'
-    dep = t.depth + (size_t)b * n;
+    const bool opens = h == 0 && k0 == 0;                                 // this CTA leaves the sequence's length and depths for the others
     if (lane == 0 && !*s_abort)
       for (int i = 0; i < S::KS && i < total; ++i) fetch(i);
     float4 bc = make_float4(1.f, 0.f, 1.f, 0.f);
     if (total > 0) bc = block_angle(0);
+    if (b != tree) {
+      if (tid < n) {
+        const int q = parents[(size_t)b * n + tid];
+        s_par[tid] = q >= tid ? -3 : q < -1 ? -2 : q;
+      }
+      __syncthreads();
+      if (tid < n) {
+        bool broken;
+        slim_tree_chain(s_par, tid, s_mask[tid], s_dep[tid], broken);
+        if (opens) {
+          t.depth[(size_t)b * n + tid] = s_dep[tid];
+          if (broken) atomicMax(p.status, (int)SLIM_ERR_TREE);
+        }
+      }
+      __syncthreads();
+      tree = b;
+    }
+    if (opens && tid == 0) {
+      t.len[b] = len;
+      if (stored > p.t_cap) atomicMax(p.status, (int)SLIM_ERR_CAPACITY);
+    }
     // queries of this (sequence, head), scaled and turned to their positions; one warp a token
     bool large = false;
     {
       const __nv_bfloat16* Q = reinterpret_cast<const __nv_bfloat16*>(p.q) + (size_t)b * n * p.d + h * DK;
       for (int i = warp; i < TOK; i += S::WARPS) {
-        const bool there = i < n && dep[i] >= 0;
+        const bool there = i < n && s_dep[i] >= 0;
         float2 v[(HALF + 31) / 32];
         float top = 0.f;
 #pragma unroll
@@ -322,7 +302,7 @@ slim_tree_p_kernel(const __grid_constant__ CUtensorMap cmap, const __grid_consta
           if (there && j < HALF) {
             const float q1 = __bfloat162float(Q[(size_t)i * p.d + j]) * p.qscale, q2 = __bfloat162float(Q[(size_t)i * p.d + HALF + j]) * p.qscale;
             if (ROPE) {
-              const float2 cs = turn(p, len + dep[i], j);
+              const float2 cs = turn(p, len + s_dep[i], j);
               v[x] = make_float2(q1 * cs.x + q2 * cs.y, q2 * cs.x - q1 * cs.y);
             } else v[x] = make_float2(q1, q2);
           }
@@ -349,7 +329,6 @@ slim_tree_p_kernel(const __grid_constant__ CUtensorMap cmap, const __grid_consta
       }
     }
     const bool careful = __syncthreads_or(large);
-    if (S::CSR && ROPE) { angles(0, 16 * hw + key0); angles(1, 16 * hw + key0 + 2); }
     if (ROPE && !S::CSR) mbar_wait<false>(bar_table, 0, s_abort, p.status);
     if (total > 0) fragments(bc, 0);
     if (total > 1) bc = block_angle(1);
@@ -366,7 +345,7 @@ slim_tree_p_kernel(const __grid_constant__ CUtensorMap cmap, const __grid_consta
 #pragma unroll
         for (int rh = 0; rh < 2; ++rh) {
           int o = 16 * hw + key0 + 2 * rh;
-          if (draft) o = o < n ? max(dep[o], 0) : 0;
+          if (draft) o = o < n ? max(s_dep[o], 0) : 0;
           if (S::CSR) { if (draft) angles(rh, o); }
           else row_cs[rh] = reinterpret_cast<const ulonglong2*>(cst) + (o >> 3) * (NPC * (VW / 2) * 32) + ((o & 7) << 2) + c;
         }
@@ -448,13 +427,12 @@ slim_tree_p_kernel(const __grid_constant__ CUtensorMap cmap, const __grid_consta
       if (lane == 0 && it + S::KS < total && !*s_abort) fetch(it + S::KS);
       // ---- what is not attended
       if (draft || t0 + 16 > len) {
-        const unsigned long long* mask = t.mask + (size_t)b * n;
-#pragma unroll
+  #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
           for (int x = 0; x < 4; ++x) {
             const int r = t0 + key0 + (x & 2);
-            const bool on = draft ? r < n && ((mask[min(8 * nt + 2 * c + (x & 1), n - 1)] >> (r & 63)) & 1) : r < len;
+            const bool on = draft ? r < n && ((s_mask[min(8 * nt + 2 * c + (x & 1), n - 1)] >> (r & 63)) & 1) : r < len;
             if (!on) s[nt][x] = -INFINITY;
           }
       }
@@ -514,65 +492,13 @@ slim_tree_p_kernel(const __grid_constant__ CUtensorMap cmap, const __grid_consta
     group_sync(group);
     if (total > 0) stats(total - 1);
     // ---- on to the next row
+    if (S::CSR && ROPE && mine < total) { angles(0, 16 * hw + key0); angles(1, 16 * hw + key0 + 2); }      // (the drafted keys' took their place)
     base += total;
     remaining -= k1 - k0;
     if (remaining == 0) break;
     k0 = 0;
     if (++h == p.H) { h = 0; ++b; }
     __syncthreads();                                                      // (everyone is done with the queries, references and sums)
-  }
-}
-
-// ------------------------------------------------------------------------------------------------ finish
-// 32 rows a block, 32 threads a row: M = the largest reference of the row's blocks that hold anything, 1 / l, and blocks of
-// P whose reference is another (rare: a row whose block maxima are more than about 32 apart around a multiple of 64)
-// multiplied by 2^(ref - M), a power of two: exact, down to values below 2^-94 of the row's largest, which become 0.
-__global__ void __launch_bounds__(1024) slim_tree_finish_kernel(const SlimDecodeParams p, const SlimTreeView t) {
-  __shared__ float s_m[32][33], s_l[32][33];
-  slim_pdl_trigger();
-  slim_pdl_wait();
-  const int R = p.H * t.n, x = threadIdx.x & 31, y = threadIdx.x >> 5, b = blockIdx.y, row = blockIdx.x * 32 + x;
-  const int nb_cap = (p.t_cap + SC_KEYS - 1) / SC_KEYS, nblk = (t.len[b] + SC_KEYS - 1) / SC_KEYS;
-  const float2* stat = t.stat + (size_t)b * (nb_cap + 1) * R + row;
-  float m = -INFINITY, l = 0.f;
-  bool same = true;                                        // every block this thread saw has the same reference
-  if (row < R)
-    for (int k0 = y; k0 <= nblk; k0 += 128) {
-      float2 v[4];
-#pragma unroll
-      for (int x4 = 0; x4 < 4; ++x4) {
-        const int k = k0 + 32 * x4;
-        v[x4] = k <= nblk ? stat[(size_t)(k == nblk ? nb_cap : k) * R] : make_float2(0.f, 0.f);
-      }
-#pragma unroll
-      for (int x4 = 0; x4 < 4; ++x4) {
-        if (v[x4].y == 0.f) continue;
-        if (v[x4].x == m) { l += v[x4].y; continue; }
-        same = same && m == -INFINITY;
-        const float top = fmaxf(m, v[x4].x);
-        l = l * exp2f(m - top) + v[x4].y * exp2f(v[x4].x - top);
-        m = top;
-      }
-    }
-  s_m[y][x] = m; s_l[y][x] = l;
-  __syncthreads();
-  float M = -INFINITY, L = 0.f;
-  for (int k = 0; k < 32; ++k) M = fmaxf(M, s_m[k][x]);
-  if (M != -INFINITY)
-    for (int k = 0; k < 32; ++k) L += s_l[k][x] == 0.f ? 0.f : s_l[k][x] * exp2f(s_m[k][x] - M);
-  if (row >= R) return;
-  const bool there = t.depth[(size_t)b * t.n + row % t.n] >= 0;
-  if (y == 0) t.inv_l[(size_t)b * R + row] = there && L != 0.f ? 1.f / L : 0.f;
-  if (same && (m == M || m == -INFINITY)) return;
-  for (int k = y; k <= nblk; k += 32) {
-    const float2 v = stat[(size_t)(k == nblk ? nb_cap : k) * R];
-    if (v.y == 0.f || v.x == M) continue;
-    const float f = exp2f(v.x - M);
-    __nv_bfloat162* P = reinterpret_cast<__nv_bfloat162*>(t.p + ((size_t)b * R + row) * t.p_ld + (k == nblk ? t.s_draft : k * SC_KEYS));
-    for (int e = 0; e < (k == nblk ? 32 : SC_KEYS / 2); ++e) {
-      const float2 w = __bfloat1622float2(P[e]);
-      P[e] = __floats2bfloat162_rn(w.x * f, w.y * f);
-    }
   }
 }
 
@@ -711,6 +637,85 @@ __device__ __forceinline__ bool sum_next(const SumSched& s, int q, SumWalk& w, S
   return true;
 }
 
+// ------------------------------------------------------------------------------------------------ finish
+// 32 rows a block, 32 threads a row: M = the largest reference of the row's blocks that hold anything, 1 / l, and blocks of
+// P whose reference is another (rare: a row whose block maxima are more than about 32 apart around a multiple of 64)
+// multiplied by 2^(ref - M), a power of two: exact, down to values below 2^-94 of the row's largest, which become 0.
+// FIN_TAIL blocks of a sequence behind these write its tail [128][d]: 0..63 the cached rows behind the last whole block of
+// 64, 64..127 the drafted keys, everything else zero; one last block of the grid lays down the product's schedule.
+constexpr int FIN_TAIL = 16;
+__global__ void __launch_bounds__(1024) slim_tree_finish_kernel(const SlimDecodeParams p, const SlimTreeView t) {
+  __shared__ float s_m[32][33], s_l[32][33];
+  extern __shared__ __align__(16) unsigned char smem_raw[];
+  slim_pdl_trigger();
+  slim_pdl_wait();
+  const int row_grid = (p.H * t.n + 31) / 32, tail_block = (int)blockIdx.x - row_grid;
+  if (tail_block >= FIN_TAIL) {
+    if (blockIdx.y != 0) return;
+    long long* s_pre = reinterpret_cast<long long*>(smem_raw);
+    long long* s_cut = s_pre + p.batch + 1;
+    const SumSched sc = build_sum_sched(t, p.batch, reinterpret_cast<int*>(s_cut + t.g_pairs + 1), s_pre, s_cut);
+    for (int i = threadIdx.x; i < p.batch + 1 + sc.P + 1; i += 1024) t.sched[i] = i <= p.batch ? s_pre[i] : s_cut[i - p.batch - 1];
+    if (threadIdx.x == 0) t.sched[p.batch + sc.P + 2] = sc.g0;
+    return;
+  }
+  if (tail_block >= 0) {
+    const int b = blockIdx.y, r = tail_block * 8 + ((int)threadIdx.x >> 7), vecs = p.d / 8, len = t.len[b], row = (len & ~63) + r;
+    const uint4* src = nullptr;
+    if (r < 64) {
+      if (row < len) src = reinterpret_cast<const uint4*>(p.k) + (size_t)(slim_cache_row(p, b, row & ~(SLIM_TT - 1)) + (row & (SLIM_TT - 1))) * vecs;
+    } else if (r - 64 < t.n && t.depth[(size_t)b * t.n + r - 64] >= 0) {
+      src = reinterpret_cast<const uint4*>(t.k_tree) + ((size_t)b * t.n + r - 64) * vecs;
+    }
+    uint4* dst = reinterpret_cast<uint4*>(t.tail) + ((size_t)b * 128 + r) * vecs;
+    for (int e = threadIdx.x & 127; e < vecs; e += 128) dst[e] = src ? __ldg(src + e) : make_uint4(0, 0, 0, 0);
+    return;
+  }
+  const int R = p.H * t.n, x = threadIdx.x & 31, y = threadIdx.x >> 5, b = blockIdx.y, row = blockIdx.x * 32 + x;
+  const int nb_cap = (p.t_cap + SC_KEYS - 1) / SC_KEYS, nblk = (t.len[b] + SC_KEYS - 1) / SC_KEYS;
+  const float2* stat = t.stat + (size_t)b * (nb_cap + 1) * R + row;
+  float m = -INFINITY, l = 0.f;
+  bool same = true;                                        // every block this thread saw has the same reference
+  if (row < R)
+    for (int k0 = y; k0 <= nblk; k0 += 128) {
+      float2 v[4];
+#pragma unroll
+      for (int x4 = 0; x4 < 4; ++x4) {
+        const int k = k0 + 32 * x4;
+        v[x4] = k <= nblk ? stat[(size_t)(k == nblk ? nb_cap : k) * R] : make_float2(0.f, 0.f);
+      }
+#pragma unroll
+      for (int x4 = 0; x4 < 4; ++x4) {
+        if (v[x4].y == 0.f) continue;
+        if (v[x4].x == m) { l += v[x4].y; continue; }
+        same = same && m == -INFINITY;
+        const float top = fmaxf(m, v[x4].x);
+        l = l * exp2f(m - top) + v[x4].y * exp2f(v[x4].x - top);
+        m = top;
+      }
+    }
+  s_m[y][x] = m; s_l[y][x] = l;
+  __syncthreads();
+  float M = -INFINITY, L = 0.f;
+  for (int k = 0; k < 32; ++k) M = fmaxf(M, s_m[k][x]);
+  if (M != -INFINITY)
+    for (int k = 0; k < 32; ++k) L += s_l[k][x] == 0.f ? 0.f : s_l[k][x] * exp2f(s_m[k][x] - M);
+  if (row >= R) return;
+  const bool there = t.depth[(size_t)b * t.n + row % t.n] >= 0;
+  if (y == 0) t.inv_l[(size_t)b * R + row] = there && L != 0.f ? 1.f / L : 0.f;
+  if (same && (m == M || m == -INFINITY)) return;
+  for (int k = y; k <= nblk; k += 32) {
+    const float2 v = stat[(size_t)(k == nblk ? nb_cap : k) * R];
+    if (v.y == 0.f || v.x == M) continue;
+    const float f = exp2f(v.x - M);
+    __nv_bfloat162* P = reinterpret_cast<__nv_bfloat162*>(t.p + ((size_t)b * R + row) * t.p_ld + (k == nblk ? t.s_draft : k * SC_KEYS));
+    for (int e = 0; e < (k == nblk ? 32 : SC_KEYS / 2); ++e) {
+      const float2 w = __bfloat1622float2(P[e]);
+      P[e] = __floats2bfloat162_rn(w.x * f, w.y * f);
+    }
+  }
+}
+
 // ------------------------------------------------------------------------------------------------ U = P K
 // Persistent, one CTA per SM in pairs.  A stage of 64 keys holds, per CTA, MT x 128 rows of P (K-major, 128-byte
 // swizzle) and HALF of the tile's 256 columns of K (MN-major, as the cache rows come: two 64-column atoms); one
@@ -765,9 +770,14 @@ slim_tree_u_kernel(const __grid_constant__ CUtensorMap pmap, const __grid_consta
   const uint32_t tmem_base = *s_tmem;
   slim_pdl_trigger();
   slim_pdl_wait();
-  const SumSched sc = build_sum_sched(t, p.batch, s_nk, s_pre, s_cut);
-  if (blockIdx.x == 0)
-    for (int i = tid; i < p.batch + 1 + sc.P + 1; i += SU_THREADS) t.sched[i] = i <= p.batch ? s_pre[i] : s_cut[i - p.batch - 1];
+  // the schedule that `finish` laid down
+  SumSched sc;
+  sc.batch = p.batch; sc.tiles = t.g_tiles; sc.S = t.g_split; sc.P = t.g_pairs; sc.F = t.g_whole; sc.TS = p.batch * t.g_tiles * t.g_split;
+  sc.nk = s_nk; sc.pre = s_pre; sc.cut = s_cut;
+  for (int i = tid; i < p.batch + 1 + sc.P + 1; i += SU_THREADS) (i <= p.batch ? s_pre[i] : s_cut[i - p.batch - 1]) = t.sched[i];
+  for (int i = tid; i < p.batch; i += SU_THREADS) s_nk[i] = stages_of(t.len[i]);
+  sc.g0 = t.sched[p.batch + sc.P + 2];
+  __syncthreads();
   const bool paged = p.block_table != nullptr;
   const int ntile = t.g_ncol;                              // column tiles; tile = row tile * ntile + column tile
 
@@ -955,14 +965,11 @@ __global__ void __launch_bounds__(256) slim_tree_join_kernel(const SlimDecodePar
   const int row0 = (tile / t.g_ncol) * mt * 256 + blockIdx.y * 16, col0 = (tile % t.g_ncol) * SU_COLS;
   if (row0 >= R) return;
   for (int q = tid; q <= s.P; q += 256) s_cut[q] = t.sched[p.batch + 1 + q];
-  const int bf = s.F / (s.S * s.tiles), inf = s.F - bf * s.S * s.tiles;                 // subtile F
-  const int nk = stages_of(t.len[b]), nkf = bf < p.batch ? stages_of(t.len[bf]) : 0;
-  const long long pre_b = t.sched[b], pre_f = t.sched[bf];
+  const int nk = stages_of(t.len[b]);
+  const long long pre_b = t.sched[b], g0 = t.sched[p.batch + s.P + 2];
   __syncthreads();
   if (tid < 32) {
     int cnt = 0;
-    const int f0 = part_begin(nkf, inf / s.tiles, s.S), f1 = part_begin(nkf, inf / s.tiles + 1, s.S);
-    const long long g0 = pre_f + (long long)s.tiles * f0 + (long long)(inf % s.tiles) * (f1 - f0);
     for (int part = 0; part < s.S; ++part) {
       const int idx = (b * s.S + part) * s.tiles + tile;
       const int k0 = part_begin(nk, part, s.S), k1 = part_begin(nk, part + 1, s.S);
@@ -1147,17 +1154,18 @@ __global__ void __launch_bounds__(128) slim_tree_out_kernel(const __grid_constan
 
 template <int DK, int NT, bool ROPE>
 cudaError_t launch_p(const slim_ctx* ctx, const CUtensorMap& cmap, const CUtensorMap& dmap, const SlimDecodeParams& p, const SlimTreeView& t,
-                     cudaStream_t st) {
+                     const int32_t* parents, cudaStream_t st) {
   constexpr size_t smem = ScoreShape<DK, NT>::SMEM;
   static_assert(smem <= 227 * 1024, "shared memory of an SM");
   auto kern = slim_tree_p_kernel<DK, NT, ROPE>;
   cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
   if (e != cudaSuccess) return e;
-  return slim_launch_pdl(kern, dim3(ctx->num_sms), dim3(ScoreShape<DK, NT>::THREADS), smem, st, cmap, dmap, p, t,
+  return slim_launch_pdl(kern, dim3(ctx->num_sms), dim3(ScoreShape<DK, NT>::THREADS), smem, st, cmap, dmap, p, t, parents,
                          reinterpret_cast<const float4*>(ctx->rope_frag));
 }
 template <int DK>
-cudaError_t launch_p_tokens(const slim_ctx* ctx, const SlimDecodeParams& p, const SlimTreeView& t, long long total_rows, cudaStream_t st) {
+cudaError_t launch_p_tokens(const slim_ctx* ctx, const SlimDecodeParams& p, const SlimTreeView& t, const int32_t* parents, long long total_rows,
+                            cudaStream_t st) {
   CUtensorMap map[2];                                      // cached rows, drafted keys: a warp's tile of 16 rows of one head
   for (int k = 0; k < 2; ++k) {
     const unsigned long long rows = k ? (unsigned long long)p.batch * t.n : (unsigned long long)total_rows;
@@ -1167,7 +1175,7 @@ cudaError_t launch_p_tokens(const slim_ctx* ctx, const SlimDecodeParams& p, cons
     cudaError_t e = slim_tmap_encode_3d(&map[k], k ? const_cast<void*>(t.k_tree) : const_cast<void*>(p.k), dims, str, box, DK != 96);
     if (e != cudaSuccess) return e;
   }
-#define SLIM_P(NT) (p.rope ? launch_p<DK, NT, true>(ctx, map[0], map[1], p, t, st) : launch_p<DK, NT, false>(ctx, map[0], map[1], p, t, st))
+#define SLIM_P(NT) (p.rope ? launch_p<DK, NT, true>(ctx, map[0], map[1], p, t, parents, st) : launch_p<DK, NT, false>(ctx, map[0], map[1], p, t, parents, st))
   return t.n <= 8 ? SLIM_P(1) : t.n <= 16 ? SLIM_P(2) : t.n <= 32 ? SLIM_P(4) : SLIM_P(8);
 #undef SLIM_P
 }
@@ -1239,7 +1247,7 @@ void slim_tree_tc_layout(const slim_ctx* ctx, int batch, int t_cap, int n, SlimT
   L.tail = off; off = align256(off + 2 * (size_t)batch * 128 * ctx->d);
   L.uh = off; off = align256(off + 2 * 2 * (size_t)batch * R * ctx->d);
   L.part = off; off = align256(off + sizeof(float) * slots * L.mt * 256 * SU_COLS);
-  L.sched = off; off = align256(off + sizeof(long long) * ((size_t)batch + L.g_pairs + 2));
+  L.sched = off; off = align256(off + sizeof(long long) * ((size_t)batch + L.g_pairs + 3));
   if (off > L.total) L.total = off;
 }
 
@@ -1272,12 +1280,11 @@ cudaError_t slim_launch_tree_tc(const slim_ctx* ctx, const SlimDecodeParams& p, 
     const unsigned int box[3] = {64, 64, dk == 64 ? 1u : 2u};
     if ((e = slim_tmap_encode_3d(&wmap, const_cast<void*>(p.wkv), dims, str, box)) != cudaSuccess) return e;
   }
-  e = slim_launch_pdl(slim_tree_tail_kernel, dim3(64, p.batch), dim3(256), 0, st, p, t, parents);
+  e = dk == 64 ? launch_p_tokens<64>(ctx, p, t, parents, total_rows, st) : dk == 96 ? launch_p_tokens<96>(ctx, p, t, parents, total_rows, st)
+                                                                          : launch_p_tokens<128>(ctx, p, t, parents, total_rows, st);
   if (e != cudaSuccess) return e;
-  e = dk == 64 ? launch_p_tokens<64>(ctx, p, t, total_rows, st) : dk == 96 ? launch_p_tokens<96>(ctx, p, t, total_rows, st)
-                                                                          : launch_p_tokens<128>(ctx, p, t, total_rows, st);
-  if (e != cudaSuccess) return e;
-  e = slim_launch_pdl(slim_tree_finish_kernel, dim3((R + 31) / 32, p.batch), dim3(1024), 0, st, p, t);
+  const size_t fin_smem = sizeof(long long) * (p.batch + 1 + t.g_pairs + 1) + sizeof(int) * p.batch + 16;
+  e = slim_launch_pdl(slim_tree_finish_kernel, dim3((R + 31) / 32 + FIN_TAIL + 1, p.batch), dim3(1024), fin_smem, st, p, t);
   if (e != cudaSuccess) return e;
   e = L.mt == 1 ? launch_u<1>(ctx, p, t, pmap, kmap, tailmap, st) : launch_u<2>(ctx, p, t, pmap, kmap, tailmap, st);
   if (e != cudaSuccess) return e;
