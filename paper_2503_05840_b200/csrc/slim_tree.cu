@@ -1,5 +1,5 @@
-// Attention for a tree of drafted tokens over the K-cache (slim_tree_decode): the tree's layout, and the CUDA-core
-// kernels that take every shape (f32 caches, head widths and model widths outside the tensor-core kernels).
+// Attention for a tree of drafted tokens over the K-cache (slim_tree_decode): the CUDA-core kernels, which take every
+// shape (f32 caches, head widths and model widths outside the tensor-core kernels).
 //
 // For token i of sequence b (L cached rows, position L + depth(i)) and head h, over the rows t < L and the drafted
 // keys j that are i itself or one of its ancestors:
@@ -11,8 +11,11 @@
 #include <cstring>
 
 #include "slim_internal.h"
+#include "slim_ptx.cuh"
 #include "slim_sched.cuh"
 #include "slim_tree.h"
+
+using namespace slim_ptx;
 
 namespace {
 
@@ -21,47 +24,20 @@ __device__ __forceinline__ float to_f(__nv_bfloat16 v) { return __bfloat162float
 __device__ __forceinline__ void put(float* p, float v) { *p = v; }
 __device__ __forceinline__ void put(__nv_bfloat16* p, float v) { *p = __float2bfloat16(v); }   // the one rounding of a bf16 context's output
 
-// One block per sequence: depth and ancestor mask of every token.  A parent that is not an earlier token of the
-// tree makes the token padding and raises SLIM_ERR_TREE; parents below -1 are padding.
-__global__ void __launch_bounds__(64) slim_tree_layout_kernel(const int32_t* __restrict__ parents, const int32_t* __restrict__ lengths,
-                                                              int n, int t_cap, unsigned long long* __restrict__ mask,
-                                                              int* __restrict__ depth, int* __restrict__ len_out, int* status) {
-  __shared__ int s_par[SLIM_MAX_TREE];
-  const int b = blockIdx.x, i = threadIdx.x;
-  slim_pdl_trigger();
-  slim_pdl_wait();
-  if (i < n) {
-    const int p = parents[(size_t)b * n + i];
-    s_par[i] = p >= i ? -3 : p < -1 ? -2 : p;
-  }
-  __syncthreads();
-  if (i == 0) {
-    int len = lengths[b];
-    if (len > t_cap) { len = t_cap; atomicMax(status, (int)SLIM_ERR_CAPACITY); }
-    len_out[b] = len < 0 ? 0 : len;
-  }
-  if (i < n) {
-    unsigned long long m;
-    int dep;
-    bool broken;
-    slim_tree_chain(s_par, i, m, dep, broken);
-    if (broken) atomicMax(status, (int)SLIM_ERR_TREE);
-    mask[(size_t)b * n + i] = m;
-    depth[(size_t)b * n + i] = dep;
-  }
-}
-
 __device__ __forceinline__ float2 rope_at(const SlimDecodeParams& p, int pos, int j) {
   const float2 cb = __ldg(p.rope_base + (size_t)(pos / SLIM_TT) * p.half + j), co = __ldg(p.rope_off + (pos % SLIM_TT) * p.half + j);
   return make_float2(cb.x * co.x - cb.y * co.y, cb.y * co.x + cb.x * co.y);
 }
 
 // Softmax arguments (log2 units): block = 64 keys of one (sequence, head) against all its tokens; the last block
-// of the row is the drafted keys.
+// of the row is the drafted keys, and that of head 0 leaves the length and the depths for the kernels behind.  A parent
+// that is not an earlier token of the tree makes the token padding and raises SLIM_ERR_TREE; parents below -1 are padding.
 constexpr int TS_KEYS = 64;
 template <typename KT>
-__global__ void __launch_bounds__(256) slim_tree_scores_kernel(const SlimDecodeParams p, const SlimTreeView t) {
+__global__ void __launch_bounds__(256) slim_tree_scores_kernel(const SlimDecodeParams p, const SlimTreeView t, const int32_t* __restrict__ parents) {
   extern __shared__ float sm[];
+  __shared__ int s_par[SLIM_MAX_TREE], dep[SLIM_MAX_TREE];
+  __shared__ unsigned long long mask[SLIM_MAX_TREE];
   const int dk = p.d_k, half = p.half, ld = dk + 1, n = t.n, tid = threadIdx.x;
   float* Ks = sm;                                    // [TS_KEYS][dk + 1]
   float* Qs = Ks + TS_KEYS * ld;                     // [n][dk + 1]
@@ -69,10 +45,28 @@ __global__ void __launch_bounds__(256) slim_tree_scores_kernel(const SlimDecodeP
   const bool draft = blockIdx.x == gridDim.x - 1;
   slim_pdl_trigger();
   slim_pdl_wait();
-  const int len = t.len[b], t0 = draft ? 0 : blockIdx.x * TS_KEYS;
+  const int stored = p.lengths[b], len = min(max(stored, 0), p.t_cap), t0 = draft ? 0 : blockIdx.x * TS_KEYS;
   if (!draft && t0 >= len) return;
   const int keys = draft ? n : min(TS_KEYS, len - t0);
-  const int* dep = t.depth + (size_t)b * n;
+  const bool opens = draft && h == 0;
+  if (tid < n) {
+    const int q = parents[(size_t)b * n + tid];
+    s_par[tid] = q >= tid ? -3 : q < -1 ? -2 : q;
+  }
+  __syncthreads();
+  if (tid < n) {
+    bool broken;
+    slim_tree_chain(s_par, tid, mask[tid], dep[tid], broken);
+    if (opens) {
+      t.depth[(size_t)b * n + tid] = dep[tid];
+      if (broken) atomicMax(p.status, (int)SLIM_ERR_TREE);
+    }
+  }
+  if (opens && tid == 0) {
+    t.len[b] = len;
+    if (stored > p.t_cap) atomicMax(p.status, (int)SLIM_ERR_CAPACITY);
+  }
+  __syncthreads();
   const KT* Kc = reinterpret_cast<const KT*>(p.k);
   const KT* Kt = reinterpret_cast<const KT*>(t.k_tree) + (size_t)b * n * p.d;
 #pragma unroll 4
@@ -113,7 +107,6 @@ __global__ void __launch_bounds__(256) slim_tree_scores_kernel(const SlimDecodeP
   __syncthreads();
   const int r = tid & (TS_KEYS - 1);
   if (r >= keys) return;
-  const unsigned long long* mask = t.mask + (size_t)b * n;
   float* S = t.s + ((size_t)b * p.H + h) * n * t.s_ld + (draft ? t.s_draft : t0) + r;
   for (int i0 = tid / TS_KEYS; i0 < n; i0 += 16) {   // four tokens at a time: i0, i0 + 4, i0 + 8, i0 + 12
     float a[4] = {0.f, 0.f, 0.f, 0.f};
@@ -242,43 +235,50 @@ __global__ void __launch_bounds__(256) slim_tree_sum_kernel(const SlimDecodePara
   }
 }
 
-// The parts of U added, in order, into the first one.
-__global__ void __launch_bounds__(256) slim_tree_parts_kernel(const SlimTreeView t, size_t n) {
-  slim_pdl_trigger();
-  slim_pdl_wait();
-  const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
-  if (i >= n) return;
-  float v = t.u[i];
-#pragma unroll 8
-  for (int s = 1; s < t.parts; ++s) v += t.u[(size_t)s * n + i];
-  t.u[i] = v;
-}
-
-// o = u W_KV,h: 8 (sequence, token) rows x 32 columns of one head a block; eight threads share a column's j, eight rows
-// of W_KV in flight each.
-constexpr int TP_ROWS = 8, TP_J = 64;
+// o = u W_KV,h, the parts of u added in order: 8 (sequence, token) rows x 32 columns of one head a cluster, whose CTAs
+// share the d rows of W_KV,h and add their sums through distributed shared memory, in order.  In a CTA eight threads share
+// a column's j, eight rows of W_KV in flight each.  (The bound on the blocks an SM holds gives the loads their registers.)
+constexpr int TP_ROWS = 8, TP_J = 64, TP_MAX = 8;
 template <typename KT>
-__global__ void __launch_bounds__(256) slim_tree_project_kernel(const SlimDecodeParams p, const SlimTreeView t, KT* __restrict__ o) {
+__global__ void __launch_bounds__(256, 2) slim_tree_project_kernel(const SlimDecodeParams p, const SlimTreeView t, KT* __restrict__ o, int share) {
   __shared__ float Us[TP_ROWS][TP_J + 1], Rs[8][TP_ROWS][32];
+  __shared__ __align__(16) float s_out[TP_ROWS][32];
   const int tid = threadIdx.x, c = tid & 31, g = tid >> 5, n = t.n, d = p.d, dk = p.d_k, h = blockIdx.z;
-  const int m0 = blockIdx.y * TP_ROWS, M = p.batch * n, col = blockIdx.x * 32 + c;
+  const int rank = blockIdx.x % share, m0 = blockIdx.y * TP_ROWS, M = p.batch * n, col = blockIdx.x / share * 32 + c;
+  const int ns = (d + TP_J - 1) / TP_J, j_end = ns * (rank + 1) / share * TP_J;
+  const size_t un = (size_t)p.batch * p.H * n * d;
   const KT* W = reinterpret_cast<const KT*>(p.wkv) + (size_t)h * d * dk;
   slim_pdl_trigger();
   slim_pdl_wait();
   float acc[TP_ROWS];
 #pragma unroll
   for (int r = 0; r < TP_ROWS; ++r) acc[r] = 0.f;
-  for (int j0 = 0; j0 < d; j0 += TP_J) {
+  for (int j0 = ns * rank / share * TP_J; j0 < j_end; j0 += TP_J) {
     float w[TP_J / 8], u[2];
 #pragma unroll
     for (int x = 0; x < TP_J / 8; ++x) {
       const int j = j0 + g + 8 * x;
       w[x] = col < dk && j < d ? to_f(W[(size_t)j * dk + col]) : 0.f;
     }
+    const float* src[2];
+    bool in[2];
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
       const int e = tid + 256 * x, m = m0 + (e >> 6), j = j0 + (e & 63);
-      u[x] = m < M && j < d ? t.u[(((size_t)(m / n) * p.H + h) * n + m % n) * d + j] : 0.f;
+      in[x] = m < M && j < d;
+      src[x] = in[x] ? t.u + (((size_t)(m / n) * p.H + h) * n + m % n) * d + j : t.u;
+      u[x] = 0.f;
+    }
+    for (int s0 = 0; s0 < t.parts; s0 += 12) {             // 24 loads in flight
+      float v[12][2];
+#pragma unroll
+      for (int s = 0; s < 12; ++s)
+#pragma unroll
+        for (int x = 0; x < 2; ++x) v[s][x] = src[x][(size_t)min(s0 + s, t.parts - 1) * un];
+#pragma unroll
+      for (int s = 0; s < 12; ++s)
+#pragma unroll
+        for (int x = 0; x < 2; ++x) u[x] += in[x] && s0 + s < t.parts ? v[s][x] : 0.f;
     }
     __syncthreads();
 #pragma unroll
@@ -292,30 +292,48 @@ __global__ void __launch_bounds__(256) slim_tree_project_kernel(const SlimDecode
 #pragma unroll
   for (int r = 0; r < TP_ROWS; ++r) Rs[g][r][c] = acc[r];
   __syncthreads();
-  const int r = g;
-  if (m0 + r >= M || col >= dk) return;
   float v = 0.f;
 #pragma unroll
-  for (int x = 0; x < 8; ++x) v += Rs[x][r][c];
-  put(o + (size_t)(m0 + r) * d + h * dk + col, v);
+  for (int x = 0; x < 8; ++x) v += Rs[x][g][c];
+  if (share > 1) {                                         // row g is written by CTA g % share
+    s_out[g][c] = v;
+    cluster_sync_all();
+    if (g % share == rank) {
+      v = 0.f;
+      for (int k = 0; k < share; ++k) v += ld_cluster_f32(mapa(smem_u32(&s_out[g][c]), k));
+    }
+    cluster_sync_all();                                    // a CTA's shared memory is read by the others until here
+    if (g % share != rank) return;
+  }
+  if (m0 + g < M && col < dk) put(o + (size_t)(m0 + g) * d + h * dk + col, v);
 }
 
 template <typename KT>
-cudaError_t launch_generic(const slim_ctx* ctx, const SlimDecodeParams& p, const SlimTreeView& t, void* o, cudaStream_t st) {
+cudaError_t launch_generic(const slim_ctx* ctx, const SlimDecodeParams& p, const SlimTreeView& t, const int32_t* parents, void* o, cudaStream_t st) {
   const size_t smem = sizeof(float) * (size_t)(TS_KEYS + t.n) * (p.d_k + 1);
   auto ks = slim_tree_scores_kernel<KT>;
   cudaError_t e = cudaFuncSetAttribute(ks, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
   if (e != cudaSuccess) return e;
   const int R = p.H * t.n;
-  e = slim_launch_pdl(ks, dim3((p.t_cap + TS_KEYS - 1) / TS_KEYS + 1, p.H, p.batch), dim3(256), smem, st, p, t);
+  e = slim_launch_pdl(ks, dim3((p.t_cap + TS_KEYS - 1) / TS_KEYS + 1, p.H, p.batch), dim3(256), smem, st, p, t, parents);
   if (e == cudaSuccess) e = slim_launch_pdl(slim_tree_stat_kernel, dim3(R, p.batch), dim3(256), 0, st, p, t);
   if (e == cudaSuccess)
     e = slim_launch_pdl(slim_tree_sum_kernel<KT>, dim3((p.d + 63) / 64, (R + 63) / 64, p.batch * t.parts), dim3(256), 0, st, p, t);
-  const size_t un = (size_t)p.batch * R * p.d;
-  if (e == cudaSuccess && t.parts > 1) e = slim_launch_pdl(slim_tree_parts_kernel, dim3((unsigned)((un + 255) / 256)), dim3(256), 0, st, t, un);
-  if (e == cudaSuccess)
-    e = slim_launch_pdl(slim_tree_project_kernel<KT>, dim3((p.d_k + 31) / 32, (p.batch * t.n + TP_ROWS - 1) / TP_ROWS, p.H), dim3(256), 0, st, p, t, (KT*)o);
-  return e;
+  if (e != cudaSuccess) return e;
+  const int col_blocks = (p.d_k + 31) / 32, row_blocks = (p.batch * t.n + TP_ROWS - 1) / TP_ROWS;
+  const long long blocks = (long long)col_blocks * row_blocks * p.H, ns = (p.d + TP_J - 1) / TP_J;
+  long long fit = 2LL * ctx->num_sms / blocks;             // CTAs of a cluster: as many as leave two an SM
+  if (fit > TP_MAX) fit = TP_MAX;
+  const int share = (int)(fit > ns ? ns : fit < 1 ? 1 : fit);
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(col_blocks * share, row_blocks, p.H); cfg.blockDim = dim3(256); cfg.stream = st;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = share; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr; cfg.numAttrs = 2;
+  return cudaLaunchKernelEx(&cfg, slim_tree_project_kernel<KT>, p, t, (KT*)o, share);
 }
 
 inline size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
@@ -339,7 +357,6 @@ SlimTreeLayout slim_tree_ws_layout(const slim_ctx* ctx, int batch, int t_cap, in
   L.s_draft = (t_cap + 63) / 64 * 64;
   L.s_ld = L.s_draft + 64;
   size_t off = 0;
-  L.mask = off; off = align256(off + sizeof(unsigned long long) * (size_t)batch * n);
   L.depth = off; off = align256(off + sizeof(int) * (size_t)batch * n);
   L.len = off; off = align256(off + sizeof(int) * (size_t)batch);
   L.inv_l = off; off = align256(off + sizeof(float) * rows);
@@ -359,7 +376,6 @@ cudaError_t slim_launch_tree(const slim_ctx* ctx, const SlimDecodeParams& p, con
   SlimTreeView t;
   memset(&t, 0, sizeof(t));
   t.n = n; t.k_tree = k_tree;
-  t.mask = reinterpret_cast<unsigned long long*>(ws + L.mask);
   t.depth = reinterpret_cast<int*>(ws + L.depth);
   t.len = reinterpret_cast<int*>(ws + L.len);
   t.inv_l = reinterpret_cast<float*>(ws + L.inv_l);
@@ -373,12 +389,9 @@ cudaError_t slim_launch_tree(const slim_ctx* ctx, const SlimDecodeParams& p, con
     t.g_tiles = L.g_tiles; t.g_ncol = L.g_ncol; t.g_split = L.g_split; t.g_pairs = L.g_pairs; t.g_whole = L.g_whole;
     return slim_launch_tree_tc(ctx, p, t, L, parents, total_rows, o, st);
   }
-  cudaError_t e = slim_launch_pdl(slim_tree_layout_kernel, dim3(p.batch), dim3(64), 0, st, parents, p.lengths, n, p.t_cap, t.mask,
-                                  t.depth, t.len, p.status);
-  if (e != cudaSuccess) return e;
   t.parts = L.parts; t.s_ld = L.s_ld; t.s_draft = L.s_draft;
   t.m = reinterpret_cast<float*>(ws + L.m);
   t.s = reinterpret_cast<float*>(ws + L.s);
   t.u = reinterpret_cast<float*>(ws + L.u);
-  return p.dtype == SLIM_BF16 ? launch_generic<__nv_bfloat16>(ctx, p, t, o, st) : launch_generic<float>(ctx, p, t, o, st);
+  return p.dtype == SLIM_BF16 ? launch_generic<__nv_bfloat16>(ctx, p, t, parents, o, st) : launch_generic<float>(ctx, p, t, parents, o, st);
 }

@@ -6,7 +6,6 @@
 struct SlimTreeView {
   int n;                             // drafted tokens of a sequence (padding included)
   const void* k_tree;                // [batch][n][d]
-  unsigned long long* mask;          // [batch][n]  bit j: token i attends drafted key j (0 = padding)
   int* depth;                        // [batch][n]  number of proper ancestors, -1 = padding
   int* len;                          // [batch]     cached rows, clamped into [0, t_cap]
   float* m;                          // [batch][H n] reference exponent of a row (log2 units)
@@ -46,7 +45,7 @@ __device__ __forceinline__ void slim_tree_chain(const int* s_par, int i, unsigne
 #endif
 
 struct SlimTreeLayout {
-  size_t mask, depth, len, inv_l, shared_end;
+  size_t depth, len, inv_l, shared_end;
   size_t m, s, u;                    // CUDA-core kernels
   size_t p, stat, tail, uh, part, sched;    // tensor-core kernels (their scratch and the other kernels' share the same memory)
   size_t total;

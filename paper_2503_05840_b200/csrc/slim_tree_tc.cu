@@ -1041,7 +1041,7 @@ __device__ __forceinline__ float4 ld_cluster_f32x4(uint32_t a) {
   return v;
 }
 
-__global__ void __launch_bounds__(128) slim_tree_out_kernel(const __grid_constant__ CUtensorMap umap, const __grid_constant__ CUtensorMap wmap,
+__global__ void __launch_bounds__(128, 1) slim_tree_out_kernel(const __grid_constant__ CUtensorMap umap, const __grid_constant__ CUtensorMap wmap,
                                                             __nv_bfloat16* __restrict__ o, int rows, int d, int d_k, int H, int parts, int* status) {
   extern __shared__ unsigned char smem_raw[];
   const uint32_t raw_u32 = smem_u32(smem_raw), base = (raw_u32 + 1023u) & ~1023u;
