@@ -465,7 +465,7 @@ slim_evict_select_kernel(const int32_t* __restrict__ lengths, const float* __res
 // column slice and goes through the rows in order may write a chunk as soon as all sources up to that chunk have been
 // read; sources of later chunks lie behind everything it overwrites, so the next chunk is on its way meanwhile.
 // The last MV_ACC blocks of a sequence write the weights and clear those of the rows that became free.
-constexpr int MV_THREADS = 256, MV_COLS = 8, MV_ROWS = MV_THREADS / MV_COLS, MV_UNROLL = 4, MV_ACC = 4;
+constexpr int MV_THREADS = 256, MV_UNROLL = 4, MV_ACC = 4;
 
 __device__ __forceinline__ long long storage_row(const int32_t* table, int page_rows, int max_pages, int num_pages, int t_cap, int b, int t,
                                                  int* status) {
@@ -475,11 +475,12 @@ __device__ __forceinline__ long long storage_row(const int32_t* table, int page_
   return (long long)pg * page_rows + t % page_rows;
 }
 
-template <typename VT>
+template <typename VT, int MV_COLS>
 __global__ void __launch_bounds__(MV_THREADS)
 slim_evict_move_kernel(unsigned char* __restrict__ base, int vecs, const int32_t* __restrict__ lengths, int t_cap, int budget,
                        const int32_t* __restrict__ kept, const int32_t* __restrict__ table, int page_rows, int max_pages, int num_pages,
                        float* __restrict__ acc, const float* __restrict__ kept_acc, int* status) {
+  constexpr int MV_ROWS = MV_THREADS / MV_COLS;
   const int b = blockIdx.y, tid = threadIdx.x;
   slim_pdl_trigger();
   slim_pdl_wait();
@@ -534,13 +535,22 @@ slim_evict_move_kernel(unsigned char* __restrict__ base, int vecs, const int32_t
   }
 }
 
+template <typename VT, int MV_COLS>
+cudaError_t launch_move_cols(const slim_ctx* ctx, const slim_cache* c, void* base, int vecs, const int32_t* lengths, int budget,
+                             const int32_t* kept, float* acc, const float* kept_acc, cudaStream_t st) {
+  return slim_launch_pdl(slim_evict_move_kernel<VT, MV_COLS>, dim3((vecs + MV_COLS - 1) / MV_COLS + (acc ? MV_ACC : 0), c->batch), dim3(MV_THREADS),
+                         0, st, (unsigned char*)base, vecs, lengths, c->t_cap, budget, kept, c->block_table, c->page_rows, c->max_pages,
+                         c->num_pages, acc, kept_acc, ctx->status);
+}
 template <typename VT>
 cudaError_t launch_move_as(const slim_ctx* ctx, const slim_cache* c, void* base, size_t row_bytes, const int32_t* lengths, int budget,
-                        const int32_t* kept, float* acc, const float* kept_acc, cudaStream_t st) {
+                           const int32_t* kept, float* acc, const float* kept_acc, cudaStream_t st) {
   const int vecs = (int)(row_bytes / sizeof(VT));
-  return slim_launch_pdl(slim_evict_move_kernel<VT>, dim3((vecs + MV_COLS - 1) / MV_COLS + (acc ? MV_ACC : 0), c->batch), dim3(MV_THREADS), 0, st,
-                         (unsigned char*)base, vecs, lengths, c->t_cap, budget, kept, c->block_table, c->page_rows, c->max_pages,
-                         c->num_pages, acc, kept_acc, ctx->status);
+  // Slices of 8 vectors, or of 2 where those would be fewer than the SMs: four times the blocks, each through a quarter of
+  // the chunks.  4096 of 12000 rows of 8 KB, one sequence 37 -> 19 us, two (128 blocks of the wider) 40 -> 37, four 51 -> 63.
+  return (long long)((vecs + 7) / 8) * c->batch >= ctx->num_sms
+             ? launch_move_cols<VT, 8>(ctx, c, base, vecs, lengths, budget, kept, acc, kept_acc, st)
+             : launch_move_cols<VT, 2>(ctx, c, base, vecs, lengths, budget, kept, acc, kept_acc, st);
 }
 
 // Rows in the widest vectors that divide them (storage and exponents begin on 16-byte boundaries).
