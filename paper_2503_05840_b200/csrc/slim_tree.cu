@@ -29,6 +29,12 @@ __device__ __forceinline__ float2 rope_at(const SlimDecodeParams& p, int pos, in
   return make_float2(cb.x * co.x - cb.y * co.y, cb.y * co.x + cb.x * co.y);
 }
 
+__device__ __forceinline__ void turn_pair(float& u, float& v, float2 cs) {
+  const float a = u * cs.x + v * cs.y;
+  v = v * cs.x - u * cs.y;
+  u = a;
+}
+
 // Softmax arguments (log2 units): block = 64 keys of one (sequence, head) against all its tokens; the last block
 // of the row is the drafted keys, and that of head 0 leaves the length and the depths for the kernels behind.  A parent
 // that is not an earlier token of the tree makes the token padding and raises SLIM_ERR_TREE; parents below -1 are padding.
@@ -38,9 +44,9 @@ __global__ void __launch_bounds__(256) slim_tree_scores_kernel(const SlimDecodeP
   extern __shared__ float sm[];
   __shared__ int s_par[SLIM_MAX_TREE], dep[SLIM_MAX_TREE];
   __shared__ unsigned long long mask[SLIM_MAX_TREE];
-  const int dk = p.d_k, half = p.half, ld = dk + 1, n = t.n, tid = threadIdx.x;
-  float* Ks = sm;                                    // [TS_KEYS][dk + 1]
-  float* Qs = Ks + TS_KEYS * ld;                     // [n][dk + 1]
+  const int dk = p.d_k, half = p.half, dk4 = (dk + 3) & ~3, ld = dk4 + 1, n = t.n, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  float* Qs = sm;                                    // [n][dk4], zeros behind dk: four elements a read, the same ones in a warp
+  float* Ks = Qs + n * dk4;                          // [TS_KEYS][dk4 + 1], an odd stride: the lanes' keys in different banks
   const int b = blockIdx.z, h = blockIdx.y;
   const bool draft = blockIdx.x == gridDim.x - 1;
   slim_pdl_trigger();
@@ -49,10 +55,36 @@ __global__ void __launch_bounds__(256) slim_tree_scores_kernel(const SlimDecodeP
   if (!draft && t0 >= len) return;
   const int keys = draft ? n : min(TS_KEYS, len - t0);
   const bool opens = draft && h == 0;
+  const KT* Kc = reinterpret_cast<const KT*>(p.k);
+  const KT* Kt = reinterpret_cast<const KT*>(t.k_tree) + (size_t)b * n * p.d;
+  auto load_keys = [&]() {                           // a warp's eight rows at a time
+    const KT* row[8];
+    int pos[8];
+#pragma unroll
+    for (int x = 0; x < 8; ++x) {
+      const int r = min(warp + 8 * x, keys - 1);
+      row[x] = draft ? Kt + (size_t)r * p.d : Kc + (size_t)(slim_cache_row(p, b, (t0 + r) & ~(SLIM_TT - 1)) + (r & (SLIM_TT - 1))) * p.d;
+      pos[x] = draft ? len + max(dep[r], 0) : t0 + r;
+    }
+    for (int j = lane; j < half; j += 32) {
+      KT k1[8], k2[8];
+#pragma unroll
+      for (int x = 0; x < 8; ++x) { k1[x] = row[x][h * dk + j]; k2[x] = row[x][h * dk + half + j]; }
+#pragma unroll
+      for (int x = 0; x < 8; ++x) {
+        const int r = warp + 8 * x;
+        const bool live = r < keys && !(draft && dep[r] < 0);
+        float u = live ? to_f(k1[x]) : 0.f, v = live ? to_f(k2[x]) : 0.f;
+        if (p.rope) turn_pair(u, v, rope_at(p, pos[x], j));
+        Ks[r * ld + j] = u; Ks[r * ld + half + j] = v;
+      }
+    }
+  };
   if (tid < n) {
     const int q = parents[(size_t)b * n + tid];
     s_par[tid] = q >= tid ? -3 : q < -1 ? -2 : q;
   }
+  if (!draft) load_keys();                           // (cached keys need not wait for the tree)
   __syncthreads();
   if (tid < n) {
     bool broken;
@@ -67,43 +99,30 @@ __global__ void __launch_bounds__(256) slim_tree_scores_kernel(const SlimDecodeP
     if (stored > p.t_cap) atomicMax(p.status, (int)SLIM_ERR_CAPACITY);
   }
   __syncthreads();
-  const KT* Kc = reinterpret_cast<const KT*>(p.k);
-  const KT* Kt = reinterpret_cast<const KT*>(t.k_tree) + (size_t)b * n * p.d;
-#pragma unroll 4
-  for (int e = tid; e < TS_KEYS * half; e += 256) {
-    const int r = e / half, j = e - r * half;
-    float k1 = 0.f, k2 = 0.f;
-    int pos = 0;
-    if (r < keys && !(draft && dep[r] < 0)) {
-      const KT* row = draft ? Kt + (size_t)r * p.d : Kc + (size_t)(slim_cache_row(p, b, (t0 + r) & ~(SLIM_TT - 1)) + (r & (SLIM_TT - 1))) * p.d;
-      pos = draft ? len + dep[r] : t0 + r;
-      k1 = to_f(row[h * dk + j]); k2 = to_f(row[h * dk + half + j]);
-      if (p.rope) {
-        const float2 cs = rope_at(p, pos, j);
-        const float a = k1 * cs.x + k2 * cs.y;
-        k2 = k2 * cs.x - k1 * cs.y;
-        k1 = a;
-      }
-    }
-    Ks[r * ld + j] = k1; Ks[r * ld + half + j] = k2;
+  if (draft) load_keys();
+  if (dk4 != dk) {                                   // (an even width: two zeros)
+    if (tid < TS_KEYS) Ks[tid * ld + dk] = Ks[tid * ld + dk + 1] = 0.f;
+    if (tid < n) Qs[tid * dk4 + dk] = Qs[tid * dk4 + dk + 1] = 0.f;
   }
   const KT* Q = reinterpret_cast<const KT*>(p.q) + (size_t)b * n * p.d;
-#pragma unroll 2
-  for (int e = tid; e < n * half; e += 256) {
-    const int i = e / half, j = e - i * half;
-    float q1 = 0.f, q2 = 0.f;
-    if (dep[i] >= 0) {
-      q1 = to_f(Q[(size_t)i * p.d + h * dk + j]) * p.qscale;
-      q2 = to_f(Q[(size_t)i * p.d + h * dk + half + j]) * p.qscale;
-      if (p.rope) {
-        const float2 cs = rope_at(p, len + dep[i], j);
-        const float a = q1 * cs.x + q2 * cs.y;
-        q2 = q2 * cs.x - q1 * cs.y;
-        q1 = a;
+  for (int i0 = warp; i0 < n; i0 += 16)              // a warp's two tokens at a time
+    for (int j = lane; j < half; j += 32) {
+      KT q1[2], q2[2];
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        const size_t at = (size_t)min(i0 + 8 * x, n - 1) * p.d + h * dk + j;
+        q1[x] = Q[at]; q2[x] = Q[at + half];
+      }
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        const int i = i0 + 8 * x;
+        if (i >= n) break;
+        const bool live = dep[i] >= 0;
+        float u = live ? to_f(q1[x]) * p.qscale : 0.f, v = live ? to_f(q2[x]) * p.qscale : 0.f;
+        if (p.rope && live) turn_pair(u, v, rope_at(p, len + dep[i], j));
+        Qs[i * dk4 + j] = u; Qs[i * dk4 + half + j] = v;
       }
     }
-    Qs[i * ld + j] = q1; Qs[i * ld + half + j] = q2;
-  }
   __syncthreads();
   const int r = tid & (TS_KEYS - 1);
   if (r >= keys) return;
@@ -111,11 +130,17 @@ __global__ void __launch_bounds__(256) slim_tree_scores_kernel(const SlimDecodeP
   for (int i0 = tid / TS_KEYS; i0 < n; i0 += 16) {   // four tokens at a time: i0, i0 + 4, i0 + 8, i0 + 12
     float a[4] = {0.f, 0.f, 0.f, 0.f};
     const int i1 = min(i0 + 4, n - 1), i2 = min(i0 + 8, n - 1), i3 = min(i0 + 12, n - 1);
-#pragma unroll 8
-    for (int j = 0; j < dk; ++j) {
-      const float k = Ks[r * ld + j];
-      a[0] = fmaf(k, Qs[i0 * ld + j], a[0]); a[1] = fmaf(k, Qs[i1 * ld + j], a[1]);
-      a[2] = fmaf(k, Qs[i2 * ld + j], a[2]); a[3] = fmaf(k, Qs[i3 * ld + j], a[3]);
+    const float4* q0 = reinterpret_cast<const float4*>(Qs + i0 * dk4);
+    const float4* q1 = reinterpret_cast<const float4*>(Qs + i1 * dk4);
+    const float4* q2 = reinterpret_cast<const float4*>(Qs + i2 * dk4);
+    const float4* q3 = reinterpret_cast<const float4*>(Qs + i3 * dk4);
+    const float* kr = Ks + r * ld;
+#pragma unroll 4
+    for (int j = 0; j < dk4; j += 4) {
+      const float4 u[4] = {q0[j / 4], q1[j / 4], q2[j / 4], q3[j / 4]};
+      const float k0 = kr[j], k1 = kr[j + 1], k2 = kr[j + 2], k3 = kr[j + 3];
+#pragma unroll
+      for (int x = 0; x < 4; ++x) a[x] = fmaf(k3, u[x].w, fmaf(k2, u[x].z, fmaf(k1, u[x].y, fmaf(k0, u[x].x, a[x]))));
     }
 #pragma unroll
     for (int x = 0; x < 4; ++x) {
@@ -189,12 +214,15 @@ __global__ void __launch_bounds__(256) slim_tree_sum_kernel(const SlimDecodePara
   for (int x = 0; x < 4; ++x)
 #pragma unroll
     for (int y = 0; y < 4; ++y) acc[x][y] = 0.f;
-  for (int s = s0; s < s1; ++s) {
+  // arguments and keys of a step, used only after the step before; the page of the step after it is looked up meanwhile
+  float sv[4];
+  KT kv[4];
+  long long row = s0 < min(s1, nb) ? slim_cache_row(p, b, s0 * 16) : 0;
+  auto load = [&](int s) {
     const bool draft = s >= nb;
     const int t0 = (draft ? s - nb : s) * 16, keys = min(16, (draft ? t.n : len) - t0);
-    const KT* K0 = draft ? Kt + (size_t)t0 * p.d : Kc + (size_t)slim_cache_row(p, b, t0) * p.d;
-    __syncthreads();
-    float sv[4], kv[4];
+    const KT* K0 = draft ? Kt + (size_t)t0 * p.d : Kc + (size_t)row * p.d;
+    if (s + 1 < min(s1, nb)) row = slim_cache_row(p, b, (s + 1) * 16);
 #pragma unroll
     for (int x = 0; x < 4; ++x) {
       const int e = tid + 256 * x, r = e >> 4, k = e & 15;
@@ -204,16 +232,21 @@ __global__ void __launch_bounds__(256) slim_tree_sum_kernel(const SlimDecodePara
     for (int x = 0; x < 4; ++x) {
       const int e = tid + 256 * x, k = e >> 6, c = e & 63;
       const bool live = k < keys && c0 + c < p.d && !(draft && t.depth[(size_t)b * t.n + t0 + k] < 0);
-      kv[x] = live ? to_f(K0[(size_t)k * p.d + c0 + c]) : 0.f;
+      kv[x] = live ? K0[(size_t)k * p.d + c0 + c] : KT(0.f);
     }
+  };
+  if (s0 < s1) load(s0);
+  for (int s = s0; s < s1; ++s) {
+    __syncthreads();
 #pragma unroll
     for (int x = 0; x < 4; ++x) {
       const int e = tid + 256 * x, r = e >> 4;
       const float il = s_il[r];
       Ps[e & 15][r] = il != 0.f ? exp2f(sv[x] - s_m[r]) * il : 0.f;
-      Bs[e >> 6][e & 63] = kv[x];
+      Bs[e >> 6][e & 63] = to_f(kv[x]);
     }
     __syncthreads();
+    if (s + 1 < s1) load(s + 1);                                   // on their way while this step's are used
 #pragma unroll
     for (int k = 0; k < 16; ++k) {
       const float4 a = *reinterpret_cast<const float4*>(&Ps[k][4 * ty]), w = *reinterpret_cast<const float4*>(&Bs[k][4 * tx]);
@@ -237,12 +270,24 @@ __global__ void __launch_bounds__(256) slim_tree_sum_kernel(const SlimDecodePara
 
 // o = u W_KV,h, the parts of u added in order: 8 (sequence, token) rows x 32 columns of one head a cluster, whose CTAs
 // share the d rows of W_KV,h and add their sums through distributed shared memory, in order.  In a CTA eight threads share
-// a column's j, eight rows of W_KV in flight each.  (The bound on the blocks an SM holds gives the loads their registers.)
+// a column's j, eight rows of W_KV each, the next ones on their way meanwhile.  (The bound on the blocks an SM holds gives the loads their registers.)
 constexpr int TP_ROWS = 8, TP_J = 64, TP_MAX = 8;
+template <int N>
+__device__ __forceinline__ void add_parts(const float* const (&src)[2], size_t un, int s0, float (&u)[2]) {
+  float v[N][2];
+#pragma unroll
+  for (int s = 0; s < N; ++s)
+#pragma unroll
+    for (int x = 0; x < 2; ++x) v[s][x] = src[x][(size_t)(s0 + s) * un];
+#pragma unroll
+  for (int s = 0; s < N; ++s)
+#pragma unroll
+    for (int x = 0; x < 2; ++x) u[x] += v[s][x];
+}
 template <typename KT>
-__global__ void __launch_bounds__(256, 2) slim_tree_project_kernel(const SlimDecodeParams p, const SlimTreeView t, KT* __restrict__ o, int share) {
-  __shared__ float Us[TP_ROWS][TP_J + 1], Rs[8][TP_ROWS][32];
-  __shared__ __align__(16) float s_out[TP_ROWS][32];
+__global__ void __launch_bounds__(256, 3) slim_tree_project_kernel(const SlimDecodeParams p, const SlimTreeView t, KT* __restrict__ o, int share) {
+  __shared__ __align__(16) float Us[TP_ROWS][TP_J + 4];
+  __shared__ float Rs[8][TP_ROWS][32], s_out[TP_ROWS][32];
   const int tid = threadIdx.x, c = tid & 31, g = tid >> 5, n = t.n, d = p.d, dk = p.d_k, h = blockIdx.z;
   const int rank = blockIdx.x % share, m0 = blockIdx.y * TP_ROWS, M = p.batch * n, col = blockIdx.x / share * 32 + c;
   const int ns = (d + TP_J - 1) / TP_J, j_end = ns * (rank + 1) / share * TP_J;
@@ -253,41 +298,47 @@ __global__ void __launch_bounds__(256, 2) slim_tree_project_kernel(const SlimDec
   float acc[TP_ROWS];
 #pragma unroll
   for (int r = 0; r < TP_ROWS; ++r) acc[r] = 0.f;
-  for (int j0 = ns * rank / share * TP_J; j0 < j_end; j0 += TP_J) {
-    float w[TP_J / 8], u[2];
+  // what a step loads, used (and converted) only after the step before; addresses behind the end are clamped
+  KT w[TP_J / 8];
+  float u[2];
+  const float* row[2];
 #pragma unroll
-    for (int x = 0; x < TP_J / 8; ++x) {
-      const int j = j0 + g + 8 * x;
-      w[x] = col < dk && j < d ? to_f(W[(size_t)j * dk + col]) : 0.f;
-    }
+  for (int x = 0; x < 2; ++x) {
+    const int m = min(m0 + ((tid + 256 * x) >> 6), M - 1);
+    row[x] = t.u + (((size_t)(m / n) * p.H + h) * n + m % n) * d;
+  }
+  const KT* wcol = W + min(col, dk - 1);
+  auto load = [&](int j0) {
+#pragma unroll
+    for (int x = 0; x < TP_J / 8; ++x) w[x] = wcol[(size_t)min(j0 + 8 * g + x, d - 1) * dk];
     const float* src[2];
-    bool in[2];
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
-      const int e = tid + 256 * x, m = m0 + (e >> 6), j = j0 + (e & 63);
-      in[x] = m < M && j < d;
-      src[x] = in[x] ? t.u + (((size_t)(m / n) * p.H + h) * n + m % n) * d + j : t.u;
-      u[x] = 0.f;
+      src[x] = row[x] + min(j0 + (tid & 63), d - 1);
+      u[x] = *src[x];
     }
-    for (int s0 = 0; s0 < t.parts; s0 += 12) {             // 24 loads in flight
-      float v[12][2];
-#pragma unroll
-      for (int s = 0; s < 12; ++s)
-#pragma unroll
-        for (int x = 0; x < 2; ++x) v[s][x] = src[x][(size_t)min(s0 + s, t.parts - 1) * un];
-#pragma unroll
-      for (int s = 0; s < 12; ++s)
-#pragma unroll
-        for (int x = 0; x < 2; ++x) u[x] += in[x] && s0 + s < t.parts ? v[s][x] : 0.f;
-    }
+    int s0 = 1;
+    for (; s0 + 12 <= t.parts; s0 += 12) add_parts<12>(src, un, s0, u);      // 24 loads in flight
+    for (; s0 + 4 <= t.parts; s0 += 4) add_parts<4>(src, un, s0, u);
+    for (; s0 < t.parts; ++s0) add_parts<1>(src, un, s0, u);
+  };
+  const int j_begin = ns * rank / share * TP_J;
+  if (j_begin < j_end) load(j_begin);
+  for (int j0 = j_begin; j0 < j_end; j0 += TP_J) {
+    float wc[TP_J / 8];
     __syncthreads();
 #pragma unroll
-    for (int x = 0; x < 2; ++x) Us[(tid + 256 * x) >> 6][(tid + 256 * x) & 63] = u[x];
+    for (int x = 0; x < 2; ++x) Us[(tid + 256 * x) >> 6][tid & 63] = j0 + (tid & 63) < d ? u[x] : 0.f;
+#pragma unroll
+    for (int x = 0; x < TP_J / 8; ++x) wc[x] = j0 + 8 * g + x < d ? to_f(w[x]) : 0.f;
     __syncthreads();
+    if (j0 + TP_J < j_end) load(j0 + TP_J);                // on their way while this step's are used
 #pragma unroll
-    for (int x = 0; x < TP_J / 8; ++x)
-#pragma unroll
-      for (int r = 0; r < TP_ROWS; ++r) acc[r] = fmaf(Us[r][g + 8 * x], w[x], acc[r]);
+    for (int r = 0; r < TP_ROWS; ++r) {
+      const float4 a = *reinterpret_cast<const float4*>(&Us[r][8 * g]), z = *reinterpret_cast<const float4*>(&Us[r][8 * g + 4]);
+      acc[r] = fmaf(a.w, wc[3], fmaf(a.z, wc[2], fmaf(a.y, wc[1], fmaf(a.x, wc[0], acc[r]))));
+      acc[r] = fmaf(z.w, wc[7], fmaf(z.z, wc[6], fmaf(z.y, wc[5], fmaf(z.x, wc[4], acc[r]))));
+    }
   }
 #pragma unroll
   for (int r = 0; r < TP_ROWS; ++r) Rs[g][r][c] = acc[r];
@@ -310,7 +361,7 @@ __global__ void __launch_bounds__(256, 2) slim_tree_project_kernel(const SlimDec
 
 template <typename KT>
 cudaError_t launch_generic(const slim_ctx* ctx, const SlimDecodeParams& p, const SlimTreeView& t, const int32_t* parents, void* o, cudaStream_t st) {
-  const size_t smem = sizeof(float) * (size_t)(TS_KEYS + t.n) * (p.d_k + 1);
+  const size_t dk4 = (p.d_k + 3) & ~3, smem = sizeof(float) * (TS_KEYS * (dk4 + 1) + t.n * dk4);
   auto ks = slim_tree_scores_kernel<KT>;
   cudaError_t e = cudaFuncSetAttribute(ks, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
   if (e != cudaSuccess) return e;
