@@ -46,6 +46,11 @@ __device__ __forceinline__ float2 turn(const SlimDecodeParams& p, int pos, int j
 //     stay below reference + 60: nearly always the same for all blocks of a row, so that the blocks need no common
 //     maximum; `finish` shifts the exponents of the others, exactly.  Sums l are taken from the rounded P, so the weights
 //     of a row add up to one.
+// Bound by the instructions and shared-memory reads around a score (rotation, conversion, exponent, store), not by the
+// keys' bytes, d = 4096, d_k = 128: 16 ragged sequences, 196 k rows, 16 drafts 0.41 ms (3.9 TB/s of keys); 131001 rows, 64
+// drafts 0.56 ms; 8 x 12000 rows with 1, 8, 16, 32, 64 drafts 0.16, 0.17, 0.20, 0.28, 0.43 ms (4.9 TB/s at one draft).
+// Blocks dealt to CTAs as they come, not to (sequence, head) CTAs, and loads by the warp that uses them: a CTA per row left
+// SMs idle at its end, block-wide tiles made every warp wait for the slowest load.
 constexpr int SC_KEYS = 128, SC_GROUP = 256;
 
 template <int DK, int NT>
@@ -722,6 +727,10 @@ __global__ void __launch_bounds__(1024) slim_tree_finish_kernel(const SlimDecode
 // tcgen05.mma.cta_group::2 has M = 256, N = 256, K = 16.  MT = 2 (more than 256 rows a sequence) runs two accumulators on
 // one load of K: 48 KB of operands per 2 x 256 x 256 x 64 products instead of 64 KB, and half the trips of K through HBM;
 // MT = 1 double-buffers the accumulator instead, so that a tile's epilogue runs under the next tile's products.
+// Bound by the tensor cores: 64 drafts over 131001 rows (2.2 TFLOP) 1.40 ms, 1575 TFLOP/s, 0.95 of what a library product
+// reaches in a burst; 16 ragged sequences, 196 k rows, 16 drafts (0.82 TFLOP) 0.567 ms, 1450 TFLOP/s, the power cap's rate.  With
+// few drafts the 256 rows of an MMA are not all there, and it is bound by reading K: 8 x 12000 rows, one draft 0.15 ms
+// (5.2 TB/s).
 // Warp 0: TMA; warp 1 (even CTA): MMA issue; warps 2-5: epilogue.  A paged cache comes in pieces of 16 rows (a page
 // holds whole ones), a contiguous one 64 rows at a time.
 constexpr int SU_THREADS = 192, SU_ROWS = 128, SU_COLS = 256, SU_A = SU_ROWS * 128, SU_B = 64 * 256, SU_TURN = 4 * 2048;
@@ -983,7 +992,8 @@ slim_tree_u_kernel(const __grid_constant__ CUtensorMap pmap, const __grid_consta
 }
 
 // ------------------------------------------------------------------------------------------------ join
-// Block (tile of the batch, 16 rows of it): sums of the tile's slots in the order of its keys, times 1 / l.
+// Block (tile of the batch, 16 rows of it): sums of the tile's slots in the order of its keys, times 1 / l.  Bound by reading
+// the slots (168 MB for 64 drafts over 131001 rows: 44 us, 3.8 TB/s, part of it from L2), by latency where they are few (12 us).
 __global__ void __launch_bounds__(256) slim_tree_join_kernel(const SlimDecodeParams p, const SlimTreeView t, int mt) {
   extern __shared__ __align__(16) unsigned char smem_raw[];
   long long* s_cut = reinterpret_cast<long long*>(smem_raw);       // [P + 1]
@@ -1061,7 +1071,8 @@ __global__ void __launch_bounds__(256) slim_tree_join_kernel(const SlimDecodePar
 // ------------------------------------------------------------------------------------------------ o = U W_KV,h
 // CTA = (part of the d rows of W_KV,h, head, 128 (sequence, token) rows); the parts form a cluster and add their
 // accumulators through distributed shared memory, in order, each the rows it writes.  U comes as two bf16 terms (one
-// would cost as much accuracy as the rounding of the output does), both against the same tile of W_KV,h.
+// would cost as much accuracy as the rounding of the output does), both against the same tile of W_KV,h.  16 x 16 rows,
+// d = 4096, 32 heads: 34 us for 168 MB of U and weights (4.9 TB/s), a third of it still in L2; a single sequence 9 us (latency).
 constexpr int OU_NS = 4, OU_A = 128 * 128, OU_B = 64 * 256;
 constexpr uint32_t OU_STAGE = 2 * OU_A + OU_B;
 constexpr int OU_LD = 132;                                 // floats per accumulator row in shared memory
