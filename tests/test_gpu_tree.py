@@ -3,8 +3,8 @@ definitions.  Cache rows behind the lengths, unused pages and padding tokens hol
 
 Tolerances are worst-case bounds worked out from the roundings (u = half a step of the type):
   arguments     a sum of d_k products with relative errors e_s each is off by at most
-                arg e_s, arg = sum |q_j k_j| / sqrt(d_k); e_s = 2 u_tf32 + (d_k + 16) 2^-24 on the tensor cores (operands
-                rounded to tf32, u_tf32 = 2^-11 -- the instruction may cut instead of rounding, 2^-10), (d_k + 16) 2^-24 else
+                arg e_s, arg = sum |q_j k_j| / sqrt(d_k); e_s = 2^-9 + (d_k + 16) 2^-24 on the tensor cores (operands rounded
+                to 11 bits, 2^-11 each time: keys once, queries once or twice), (d_k + 16) 2^-24 else
   probabilities relative error 2 arg e_s + (T + 16) 2^-24 (numerator and denominator), + 2^-8 where they are rounded
                 to bf16, times mass = (sum p |k|) |W_KV|
   u, o          2^-8 each of mass and |o| where rounded to bf16; sums of d products (d + 16) 2^-24 of mass."""
@@ -187,6 +187,26 @@ def test_keys_and_queries_of_any_magnitude(key, query):
         for b, k in enumerate(c.K):
             c.store[b, :len(k)] = to_dev(k, "bf16")
         c.dq, c.dkt = to_dev(c.q, "bf16"), to_dev(c.kt, "bf16")
+        c.call()
+        assert c.status() == B.SLIM_OK
+        c.check()
+
+
+@pytest.mark.parametrize("d,H,dtype,lengths,n", [(384, 6, "f32", [1500], 8), (384, 6, "f32", [5003], 3), (1000, 10, "bf16", [2100, 40], 1), (200, 5, "f32", [900] * 3, 64)])
+def test_long_rows_in_parts_on_the_cuda_cores(d, H, dtype, lengths, n):
+    """The keys cut into up to 32 parts, whose sums the projection adds."""
+    g = np.random.default_rng(n)
+    with Case(d, H, 1.0e4, dtype, lengths, [random_parents(g, n) for _ in lengths], seed=6) as c:
+        c.call()
+        assert c.status() == B.SLIM_OK
+        c.check()
+
+
+@pytest.mark.parametrize("d,H,dtype,n", [(128, 2, "bf16", 2), (64, 1, "bf16", 1), (24, 3, "f32", 2)])
+def test_the_largest_batch(d, H, dtype, n):
+    g = np.random.default_rng(15)
+    lengths = [int(x) for x in g.integers(0, 41, 2048)]
+    with Case(d, H, 1.0e4, dtype, lengths, [random_parents(g, n) for _ in lengths], page=16, seed=9) as c:
         c.call()
         assert c.status() == B.SLIM_OK
         c.check()
