@@ -310,7 +310,7 @@ __global__ void __launch_bounds__(256) slim_weights_add_kernel(const SlimDecodeP
 // that writes the kept indices in order: every row above the threshold, and of the rows equal to it the first ones.
 // Latency-bound: the keys are read once into shared memory (a CTA's share up to SEL_KEYS; longer ones are read again from
 // L2 in every pass), and long contexts take eight CTAs, short ones one, which saves the cluster's barriers.  1500 rows: 10 us;
-// 16 sequences of 8192 to 16384: 20 us.
+// 16 sequences of 8192 to 16384: 18 us.
 constexpr int SEL_THREADS = 1024, SEL_WARPS = SEL_THREADS / 32, SEL_KEYS = 48 * 1024;
 
 __device__ __forceinline__ uint32_t order_key(float f) {
@@ -323,7 +323,7 @@ struct SelShared {
   unsigned hist[2][256], sum[256];                    // this CTA's counts of a pass (two buffers), the cluster's
   int gt[SEL_WARPS], eq[SEL_WARPS];
   int total[2];                                       // rows above and equal to the threshold in this CTA
-  unsigned prefix, need;
+  unsigned prefix, need, done;
 };
 
 template <int CL>
@@ -364,6 +364,7 @@ slim_evict_select_kernel(const int32_t* __restrict__ lengths, const float* __res
   }
   auto key_at = [&](int t) -> uint32_t { return staged ? s_key[t - c0] : order_key(A[t]); };
   for (int i = tid; i < 512; i += SEL_THREADS) (&sh.hist[0][0])[i] = 0;
+  if (tid == 0) sh.done = 0;
   __syncthreads();
   unsigned prefix = 0, left = (unsigned)need;                      // the left-th largest among the keys that share the prefix
   if (need > 0) {
@@ -405,12 +406,21 @@ slim_evict_select_kernel(const int32_t* __restrict__ lengths, const float* __res
         unsigned above = incl - sum;
         if (above < left && left <= incl)
           for (int i = 0; i < 8; ++i) {
-            if (left <= above + c[i]) { sh.prefix = (prefix << 8) | (255 - 8 * lane - i); sh.need = left - above; break; }
+            if (left <= above + c[i]) {
+              const unsigned longer = (prefix << 8) | (255 - 8 * lane - i);
+              sh.prefix = longer; sh.need = left - above;
+              sh.done = left - above == c[i] && longer != 0;       // every key with these digits stays: no need to know the others
+              break;
+            }
             above += c[i];
           }
       }
       __syncthreads();
       prefix = sh.prefix; left = sh.need;
+      if (sh.done) {                                               // (the same in all CTAs)
+        prefix = (prefix << shift) - 1; left = 0;
+        break;
+      }
       // (a buffer is counted into again two passes later, behind the next pass's barrier, by when all CTAs have read it)
     }
   }

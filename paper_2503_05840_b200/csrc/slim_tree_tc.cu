@@ -992,9 +992,10 @@ slim_tree_u_kernel(const __grid_constant__ CUtensorMap pmap, const __grid_consta
 }
 
 // ------------------------------------------------------------------------------------------------ join
-// Block (tile of the batch, 16 rows of it): sums of the tile's slots in the order of its keys, times 1 / l.  Bound by reading
+// Block (tile of the batch, 4 RPT rows of it): sums of the tile's slots in the order of its keys, times 1 / l.  Bound by reading
 // the slots (168 MB for 64 drafts over 131001 rows: 44 us, 3.8 TB/s, part of it from L2), by latency where they are few (12 us).
-__global__ void __launch_bounds__(256) slim_tree_join_kernel(const SlimDecodeParams p, const SlimTreeView t, int mt) {
+template <int RPT>
+__global__ void __launch_bounds__(256, 2) slim_tree_join_kernel(const SlimDecodeParams p, const SlimTreeView t, int mt) {
   extern __shared__ __align__(16) unsigned char smem_raw[];
   long long* s_cut = reinterpret_cast<long long*>(smem_raw);       // [P + 1]
   int* s_slot = reinterpret_cast<int*>(s_cut + t.g_pairs + 1);     // [S + P]
@@ -1005,7 +1006,7 @@ __global__ void __launch_bounds__(256) slim_tree_join_kernel(const SlimDecodePar
   SumSched s;
   s.batch = p.batch; s.tiles = t.g_tiles; s.S = t.g_split; s.P = t.g_pairs; s.F = t.g_whole; s.TS = p.batch * t.g_tiles * t.g_split;
   const int at = blockIdx.x + (s.S == 1 ? s.F : 0), b = at / s.tiles, tile = at % s.tiles;
-  const int row0 = (tile / t.g_ncol) * mt * 256 + blockIdx.y * 16, col0 = (tile % t.g_ncol) * SU_COLS;
+  const int row0 = (tile / t.g_ncol) * mt * 256 + blockIdx.y * 4 * RPT, col0 = (tile % t.g_ncol) * SU_COLS;
   if (row0 >= R) return;
   for (int q = tid; q <= s.P; q += 256) s_cut[q] = t.sched[p.batch + 1 + q];
   const int nk = stages_of(t.len[b]);
@@ -1036,24 +1037,30 @@ __global__ void __launch_bounds__(256) slim_tree_join_kernel(const SlimDecodePar
   __syncthreads();
   const int cnt = s_n;
   if (cnt == 0) return;                                    // written as a whole by one pair
-  // four rows a thread (tid / 64 + 4 m), four columns each; the slots one after another
+  // RPT rows a thread (tid / 64 + 4 m), four columns each; the slots one after another, 16 loads in flight
   const int c = (tid % 64) * 4;
   if (col0 + c >= p.d) return;
-  float4 a[4];
+  float4 a[RPT];
 #pragma unroll
-  for (int m = 0; m < 4; ++m) a[m] = make_float4(0.f, 0.f, 0.f, 0.f);
-  const float* src = t.part + (size_t)(blockIdx.y * 16 + tid / 64) * SU_COLS + c;
-#pragma unroll 4
-  for (int k = 0; k < cnt; ++k) {
-    const float* slot = src + (size_t)s_slot[k] * mt * 256 * SU_COLS;
+  for (int m = 0; m < RPT; ++m) a[m] = make_float4(0.f, 0.f, 0.f, 0.f);
+  const float* src = t.part + (size_t)(blockIdx.y * 4 * RPT + tid / 64) * SU_COLS + c;
+  for (int k0 = 0; k0 < cnt; k0 += 16 / RPT) {
+    float4 v[16 / RPT][RPT];
 #pragma unroll
-    for (int m = 0; m < 4; ++m) {                          // (rows behind the last one are in the slot too, and not used)
-      const float4 v = *reinterpret_cast<const float4*>(slot + (size_t)4 * m * SU_COLS);
-      a[m].x += v.x; a[m].y += v.y; a[m].z += v.z; a[m].w += v.w;
+    for (int k = 0; k < 16 / RPT; ++k) {
+      const float* slot = src + (size_t)s_slot[min(k0 + k, cnt - 1)] * mt * 256 * SU_COLS;
+#pragma unroll
+      for (int m = 0; m < RPT; ++m) v[k][m] = *reinterpret_cast<const float4*>(slot + (size_t)4 * m * SU_COLS);      // (rows behind the last one are in the slot too, and not used)
+    }
+#pragma unroll
+    for (int k = 0; k < 16 / RPT; ++k) {
+      if (k0 + k >= cnt) break;
+#pragma unroll
+      for (int m = 0; m < RPT; ++m) { a[m].x += v[k][m].x; a[m].y += v[k][m].y; a[m].z += v[k][m].z; a[m].w += v[k][m].w; }
     }
   }
 #pragma unroll
-  for (int m = 0; m < 4; ++m) {
+  for (int m = 0; m < RPT; ++m) {
     const int r = row0 + tid / 64 + 4 * m;
     if (r >= R) continue;
     const float il = t.inv_l[(size_t)b * R + r];
@@ -1111,6 +1118,11 @@ __global__ void __launch_bounds__(128, 1) slim_tree_out_kernel(const __grid_cons
   tc_fence_after();
   const uint32_t tmem_base = *s_tmem;
   slim_pdl_trigger();
+  if (warp == 0 && lane == 0)                              // W_KV is no kernel's output: the first stages' tiles need not wait
+    for (int j = 0; j < OU_NS && j < s1 - s0; ++j) {
+      mbar_arrive_expect_tx(bar_full + 8 * j, bytes);
+      tma_load_3d(base + (uint32_t)j * OU_STAGE + 2 * OU_A, &wmap, bar_full + 8 * j, 0, h * d + (s0 + j) * 64, 0);
+    }
   slim_pdl_wait();
   if (warp == 0 && lane == 0) {
     fence_proxy_async_global();
@@ -1121,10 +1133,10 @@ __global__ void __launch_bounds__(128, 1) slim_tree_out_kernel(const __grid_cons
       ok = mbar_wait<false>(bar_empty + 8 * st, ((j / OU_NS) & 1) ^ 1, s_abort, status);
       if (!ok) break;
       const uint32_t dst = base + (uint32_t)st * OU_STAGE;
-      mbar_arrive_expect_tx(bar_full + 8 * st, bytes);
+      if (j >= OU_NS) mbar_arrive_expect_tx(bar_full + 8 * st, bytes);
       tma_load_3d(dst, &umap, bar_full + 8 * st, s * 64, m0, h);
       tma_load_3d(dst + OU_A, &umap, bar_full + 8 * st, s * 64, m0, H + h);
-      tma_load_3d(dst + 2 * OU_A, &wmap, bar_full + 8 * st, 0, h * d + s * 64, 0);
+      if (j >= OU_NS) tma_load_3d(dst + 2 * OU_A, &wmap, bar_full + 8 * st, 0, h * d + s * 64, 0);
     }
     if (!ok) {
       const int did = s - s0, issued = did < OU_NS ? did : OU_NS;
@@ -1335,7 +1347,11 @@ cudaError_t slim_launch_tree_tc(const slim_ctx* ctx, const SlimDecodeParams& p, 
   if (L.g_split > 1 || L.g_whole < p.batch * L.g_tiles) {
     const size_t smem = sizeof(long long) * (t.g_pairs + 1) + sizeof(int) * (L.g_split + t.g_pairs) + 16;
     const int tiles = p.batch * L.g_tiles - (L.g_split == 1 ? L.g_whole : 0);          // the others are written as a whole
-    e = slim_launch_pdl(slim_tree_join_kernel, dim3(tiles, L.mt * 16), dim3(256), smem, st, p, t, L.mt);
+    // four rows a thread, or one where that leaves SMs without a block (4093 rows, 5 drafts, 80 rows of U: 13.0 -> 11.5 us)
+    const int tile_rows = R < L.mt * 256 ? R : L.mt * 256;
+    e = (long long)tiles * ((R + 15) / 16) >= ctx->num_sms
+            ? slim_launch_pdl(slim_tree_join_kernel<4>, dim3(tiles, (tile_rows + 15) / 16), dim3(256), smem, st, p, t, L.mt)
+            : slim_launch_pdl(slim_tree_join_kernel<1>, dim3(tiles, (tile_rows + 3) / 4), dim3(256), smem, st, p, t, L.mt);
     if (e != cudaSuccess) return e;
   }
   // parts of the d rows: as many as leave one CTA an SM (a CTA fills an SM's shared memory), at most four
