@@ -1280,12 +1280,18 @@ void slim_tree_tc_layout(const slim_ctx* ctx, int batch, int t_cap, int n, SlimT
   L.g_tiles = L.g_ncol * (int)((R + L.mt * 256 - 1) / (L.mt * 256));
   L.g_pairs = ctx->num_sms / 2;
   // Fewer tiles than pairs, and more probabilities than stay in L2 beside the keys: every tile is cut into parts of at
-  // least eight stages, for about five parts a pair, so that the pairs in flight walk the same rows of P (64 drafts over
-  // 131001 rows: 1.90 ms whole, 1.46 ms in five parts).  Otherwise parts only cost: every one drains its sums, and they
-  // make a trip to memory and back (16 drafts over 8 x 12000 rows: 0.30 ms whole, 0.34 ms in three parts).
+  // least eight stages, a part for every pair or more, so that the pairs in flight walk the same 100 MB of P, but no more
+  // than five where that suffices: each drains its sums (product and join, 64 drafts over 131001 rows, 537 MB of P: 1.93 ms
+  // whole, 1.55 in three parts, 1.50 in five, 1.52 in six; over 70000 rows, 287 MB: 0.79 in three, 0.80 in five; 16 drafts
+  // over 4 x 50000 rows, 205 MB: 0.77 whole, 0.61 in three, 0.63 in five).  Otherwise parts only cost (16 drafts over
+  // 8 x 12000 rows: 0.30 ms whole, 0.34 ms in three parts).
   const long long tiles = (long long)batch * L.g_tiles;
-  const bool p_in_l2 = 2.0 * batch * (double)R * t_cap <= 96e6;
-  long long split = tiles < L.g_pairs && !p_in_l2 ? (4LL * L.g_pairs + tiles - 1) / tiles : 1;
+  const double p_bytes = 2.0 * batch * (double)R * t_cap;
+  long long split = 1;
+  if (tiles < L.g_pairs && p_bytes > 96e6) {
+    const long long each = (L.g_pairs + tiles - 1) / tiles, fit = p_bytes < 5e8 ? (long long)(p_bytes / 1e8) + 1 : 5;
+    split = each > fit ? each : fit;
+  }
   const long long most = (t_cap / 64 + 2) / 8;
   if (split > most) split = most;
   L.g_split = split < 1 ? 1 : (int)split;
