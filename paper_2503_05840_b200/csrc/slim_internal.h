@@ -151,9 +151,9 @@ cudaError_t slim_tc_make_tmap(const slim_ctx* ctx, slim_cache* c, int cl);
 cudaError_t slim_launch_wait_selftest(int* status, int* gave_up, cudaStream_t st);
 cudaError_t slim_launch_tc(const slim_ctx* ctx, const slim_cache* c, const SlimDecodeParams& p, cudaStream_t st);
 
-// 3-D tiled tensor map over bf16 data, with 128-byte swizzle or plain rows (driver entry point looked up once)
+// 3-D tiled tensor map with 128-byte swizzle over bf16 data (driver entry point looked up once)
 cudaError_t slim_tmap_encode_3d(void* out_map, void* base, const unsigned long long dims[3],
-                                const unsigned long long strides[2], const unsigned int box[3], bool swizzle = true);
+                                const unsigned long long strides[2], const unsigned int box[3]);
 
 // tensor-core combine + projection (slim_proj.cu)
 int    slim_proj_shape_ok(int d, int H, int d_k, int dtype);

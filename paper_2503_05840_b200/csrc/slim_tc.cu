@@ -818,7 +818,7 @@ int slim_tc_workers(const slim_ctx* ctx, int cl) {
 }
 
 cudaError_t slim_tmap_encode_3d(void* out_map, void* base, const unsigned long long dims_in[3],
-                                const unsigned long long strides_in[2], const unsigned int box_in[3], bool swizzle) {
+                                const unsigned long long strides_in[2], const unsigned int box_in[3]) {
   typedef CUresult (*encode_t)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
                                const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
                                CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
@@ -836,7 +836,7 @@ cudaError_t slim_tmap_encode_3d(void* out_map, void* base, const unsigned long l
   const cuuint32_t box[3] = {box_in[0], box_in[1], box_in[2]};
   const cuuint32_t estr[3] = {1, 1, 1};
   CUresult r = encode(reinterpret_cast<CUtensorMap*>(out_map), CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, base, dims,
-                      strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE,
+                      strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
                       CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
 }

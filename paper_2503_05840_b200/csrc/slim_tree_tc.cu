@@ -1208,6 +1208,27 @@ __global__ void __launch_bounds__(128, 1) slim_tree_out_kernel(const __grid_cons
   }
 }
 
+// Tensor map of whole 16-row tiles of d_k = 96 elements of a head: 192 bytes, wider than a swizzle's rows, so plain ones.
+cudaError_t encode_plain_rows(CUtensorMap* map, const void* base, unsigned long long cols, unsigned long long rows) {
+  typedef CUresult (*encode_t)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
+                               const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+  static encode_t encode = nullptr;
+  if (!encode) {
+    void* fn = nullptr;
+    cudaDriverEntryPointQueryResult found;
+    const cudaError_t e = cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &found);
+    if (e != cudaSuccess) return e;
+    if (found != cudaDriverEntryPointSuccess || !fn) return cudaErrorNotSupported;
+    encode = (encode_t)fn;
+  }
+  const cuuint64_t dims[3] = {cols, rows, 1}, strides[2] = {2 * cols, 2 * cols * rows};
+  const cuuint32_t box[3] = {96, 16, 1}, step[3] = {1, 1, 1};
+  const CUresult r = encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides, box, step,
+                            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
+}
+
 template <int DK, int NT, bool ROPE>
 cudaError_t launch_p(const slim_ctx* ctx, const CUtensorMap& cmap, const CUtensorMap& dmap, const SlimDecodeParams& p, const SlimTreeView& t,
                      const int32_t* parents, cudaStream_t st) {
@@ -1225,10 +1246,10 @@ cudaError_t launch_p_tokens(const slim_ctx* ctx, const SlimDecodeParams& p, cons
   CUtensorMap map[2];                                      // cached rows, drafted keys: a warp's tile of 16 rows of one head
   for (int k = 0; k < 2; ++k) {
     const unsigned long long rows = k ? (unsigned long long)p.batch * t.n : (unsigned long long)total_rows;
-    const unsigned long long dims[3] = {DK == 96 ? (unsigned long long)p.d : 64ull, rows, DK == 96 ? 1ull : (unsigned long long)(p.d / 64)};
-    const unsigned long long str[2] = {2ull * p.d, DK == 96 ? 2ull * p.d * rows : 128ull};
-    const unsigned int box[3] = {DK == 96 ? 96u : 64u, 16, DK == 128 ? 2u : 1u};
-    cudaError_t e = slim_tmap_encode_3d(&map[k], k ? const_cast<void*>(t.k_tree) : const_cast<void*>(p.k), dims, str, box, DK != 96);
+    const unsigned long long dims[3] = {64, rows, (unsigned long long)(p.d / 64)}, str[2] = {2ull * p.d, 128};
+    const unsigned int box[3] = {64, 16, DK == 128 ? 2u : 1u};
+    void* base = k ? const_cast<void*>(t.k_tree) : const_cast<void*>(p.k);
+    const cudaError_t e = DK == 96 ? encode_plain_rows(&map[k], base, (unsigned long long)p.d, rows) : slim_tmap_encode_3d(&map[k], base, dims, str, box);
     if (e != cudaSuccess) return e;
   }
 #define SLIM_P(NT) (p.rope ? launch_p<DK, NT, true>(ctx, map[0], map[1], p, t, parents, st) : launch_p<DK, NT, false>(ctx, map[0], map[1], p, t, parents, st))
