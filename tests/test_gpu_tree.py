@@ -252,6 +252,56 @@ def test_a_layer_keeps_the_scratch_that_a_graph_uses():
         lay.close()
 
 
+def test_layers_on_streams_at_once_and_eviction_in_a_graph():
+    torch.manual_seed(0)
+    layers, calls = [], []
+    try:
+        for d, H, dtype, batch, t_cap in [(1024, 8, "bf16", 3, 700), (768, 8, "bf16", 2, 900), (640, 10, "bf16", 4, 500), (384, 6, "f32", 2, 900)]:
+            lay = SlimLayer(d, H, d // H, 1.0e4, dtype, batch, t_cap, DEV)
+            layers.append(lay)
+            lay.set_wkv(np.random.default_rng(d).standard_normal((d, d)) / np.sqrt(d))
+            lay.k.normal_()
+            q, kt = (torch.randn(batch, 7, d, device=DEV).to(lay.tdtype) for _ in range(2))
+            lens = torch.randint(300, t_cap - 64, (batch,), dtype=torch.int32, device=DEV)
+            par = torch.tensor([[-1, 0, 0, 1, 2, 3, 3]] * batch, dtype=torch.int32, device=DEV)
+            calls.append((lay, q, kt, lens, par, q[:, 0].contiguous()))
+        run = lambda lay, q, kt, lens, par, q1: (lay.tree_decode(q, kt, lens, par),
+                                                 lay.accumulate_weights(q1, lens, torch.zeros(lay.batch, lay.t_cap, device=DEV)))
+        want = [tuple(x.clone() for x in run(*c)) for c in calls]
+        torch.cuda.synchronize()
+        streams, got = [torch.cuda.Stream() for _ in calls], [[] for _ in calls]
+        for _ in range(20):
+            for k, c in enumerate(calls):
+                with torch.cuda.stream(streams[k]):
+                    got[k].append(run(*c))
+        torch.cuda.synchronize()
+        for k in range(len(calls)):
+            assert all(torch.equal(x, y) for g in got[k] for x, y in zip(g, want[k])), k
+            assert layers[k].device_status() == B.SLIM_OK
+        # one layer's scratch in a graph that evicts and attends, eager calls of the same layer between the replays
+        lay, q, kt, lens, par, _ = calls[0]
+        K0, acc0 = lay.k.clone(), torch.rand(lay.batch, lay.t_cap, device=DEV)
+        acc = acc0.clone()
+
+        def shorten():
+            return lay.evict(lens, acc, 200, 30), lay.tree_decode(q, kt, torch.clamp(lens, max=200), par)
+
+        first = [x.clone() for x in shorten()]
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            later = shorten()
+        for _ in range(3):
+            lay.k.copy_(K0)
+            acc.copy_(acc0)
+            graph.replay()
+            assert all(torch.equal(x, y) for x, y in zip(first, later))
+            lay.tree_decode(q, kt, lens, par)
+    finally:
+        torch.cuda.synchronize()
+        for lay in layers:
+            lay.close()
+
+
 def test_broken_trees_and_lengths_are_reported():
     with Case(128, 2, 1.0e4, "bf16", [20, 20], [[-1, 0, 1], [-1, 0, 1]], seed=1) as c:
         c.dpar = torch.tensor([[-1, 1, 0], [-1, -2, 1]], dtype=torch.int32, device=DEV)     # its own parent; a child of padding
