@@ -108,24 +108,23 @@ __global__ void __launch_bounds__(256) slim_tree_scores_kernel(const SlimDecodeP
     if (tid < n) Qs[tid * dk4 + dk] = Qs[tid * dk4 + dk + 1] = 0.f;
   }
   const KT* Q = reinterpret_cast<const KT*>(p.q) + (size_t)b * n * p.d;
-  for (int i0 = warp; i0 < n; i0 += 16)              // a warp's two tokens at a time
-    for (int j = lane; j < half; j += 32) {
-      KT q1[2], q2[2];
+  for (int j = lane; j < half; j += 32) {            // all of a warp's tokens at a time
+    KT q1[SLIM_MAX_TREE / 8], q2[SLIM_MAX_TREE / 8];
 #pragma unroll
-      for (int x = 0; x < 2; ++x) {
-        const size_t at = (size_t)min(i0 + 8 * x, n - 1) * p.d + h * dk + j;
-        q1[x] = Q[at]; q2[x] = Q[at + half];
-      }
-#pragma unroll
-      for (int x = 0; x < 2; ++x) {
-        const int i = i0 + 8 * x;
-        if (i >= n) break;
-        const bool live = dep[i] >= 0;
-        float u = live ? to_f(q1[x]) * p.qscale : 0.f, v = live ? to_f(q2[x]) * p.qscale : 0.f;
-        if (p.rope && live) turn_pair(u, v, rope_at(p, len + dep[i], j));
-        Qs[i * dk4 + j] = u; Qs[i * dk4 + half + j] = v;
-      }
+    for (int x = 0; x < SLIM_MAX_TREE / 8; ++x) {
+      const size_t at = (size_t)(warp + 8 * x) * p.d + h * dk + j;
+      if (warp + 8 * x < n) { q1[x] = Q[at]; q2[x] = Q[at + half]; }
     }
+#pragma unroll
+    for (int x = 0; x < SLIM_MAX_TREE / 8; ++x) {
+      const int i = warp + 8 * x;
+      if (i >= n) break;
+      const bool live = dep[i] >= 0;
+      float u = live ? to_f(q1[x]) * p.qscale : 0.f, v = live ? to_f(q2[x]) * p.qscale : 0.f;
+      if (p.rope && live) turn_pair(u, v, rope_at(p, len + dep[i], j));
+      Qs[i * dk4 + j] = u; Qs[i * dk4 + half + j] = v;
+    }
+  }
   __syncthreads();
   const int r = tid & (TS_KEYS - 1);
   if (r >= keys) return;
