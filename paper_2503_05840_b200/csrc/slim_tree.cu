@@ -9,8 +9,8 @@
 // down once ([b][h n + i][t], float) and the weighted sum is a matrix product P [R x T] K [T x d] cut into tiles;
 // where there are few tiles, T is cut too and the parts are added in a fixed order.
 //
-// Bound by latency at the sizes these serve: 1500 float32 rows, d = 384, 6 heads, 8 drafts 27 us in four launches (scores 12,
-// statistics 5, sums 10, projection 7, overlapping).  Loads of the next step run under a step's products throughout.
+// Bound by latency at the sizes these serve: 1500 float32 rows, d = 384, 6 heads, 8 drafts 27 us in four launches (scores 9.5,
+// statistics 5.5, sums 10, projection 6.5, overlapping).  Loads of the next step run under a step's products throughout.
 #include <cstring>
 
 #include "slim_internal.h"
@@ -272,7 +272,8 @@ __global__ void __launch_bounds__(256) slim_tree_sum_kernel(const SlimDecodePara
 
 // o = u W_KV,h, the parts of u added in order: 8 (sequence, token) rows x 32 columns of one head a cluster, whose CTAs
 // share the d rows of W_KV,h and add their sums through distributed shared memory, in order.  In a CTA eight threads share
-// a column's j, eight rows of W_KV each, the next ones on their way meanwhile.  (The bound on the blocks an SM holds gives the loads their registers.)
+// a column's j, eight rows of W_KV each, the next ones on their way meanwhile.  (The bound on the blocks an SM holds
+// gives the loads their registers: without it the compiler allows 32, and the loads wait for one another, 34 us for 8.)
 constexpr int TP_ROWS = 8, TP_J = 64, TP_MAX = 8;
 template <int N>
 __device__ __forceinline__ void add_parts(const float* const (&src)[2], size_t un, int s0, float (&u)[2]) {
