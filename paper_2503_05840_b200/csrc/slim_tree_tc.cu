@@ -40,8 +40,9 @@ __device__ __forceinline__ float2 turn(const SlimDecodeParams& p, int pos, int j
 //     their positions once, are turned back by the block's angle, 64 complex factors a block.
 //   - float16 keeps 11 bits of the rotated values (bf16's 8 would cost as much accuracy as the rounding of P does, for a
 //     product that is 1 / H of the step's) at twice tf32's rate.  Its range: queries are scaled by a power of two per
-//     token; keys go in as they are, and a warp whose sums overflow, or whose queries are so large that the smallest
-//     float16 steps of a key would show, repeats its tile with the keys scaled by a power of two.
+//     token; keys go in as they are (those that are not attended as zeros), and a warp whose sums overflow, or whose queries
+//     are so large that the smallest float16 steps of a key would show, repeats its tile with every key scaled by a power of
+//     two of its own.
 //   - P is written relative to a reference that is a multiple of 64, kept from block to block while the arguments
 //     stay below reference + 60: nearly always the same for all blocks of a row, so that the blocks need no common
 //     maximum; `finish` shifts the exponents of the others, exactly.  Sums l are taken from the rounded P, so the weights
@@ -359,8 +360,21 @@ slim_tree_p_kernel(const __grid_constant__ CUtensorMap cmap, const __grid_consta
       const uint2* qb = qf + (it & 1) * NT * S::PER;
       mbar_wait<false>(bar + 8 * ((base + it) % S::KS), ((base + it) / S::KS) & 1, s_abort, p.status);      // (gave up: reported, and the loop runs on to its end)
       float s[NT][4];
-      float back = 1.f;                                                     // undoes the keys' scaling
-      for (bool again = false;;) {
+      bool whole = false;                                                   // s are arguments, without a factor left out
+      const bool edge = draft || t0 + 16 > len;                             // rows of the tile may not be attended
+      auto attended = [&](int r) { return draft ? r < n && s_dep[min(r, n - 1)] >= 0 : r < len; };
+      if (edge) {
+        // rows behind the sequence's last, padding and the next sequence's rows may hold anything: they are cleared (a
+        // thread's own elements) before they can meet the overflow test or the scaling
+#pragma unroll 1
+        for (int rh = 0; rh < 2; ++rh)
+          if (!attended(t0 + key0 + 2 * rh)) {
+#pragma unroll 1
+            for (int e = 0; e < 2 * NPC; ++e) *reinterpret_cast<kvec*>(tile + tile_off<DK>(key0 + 2 * rh, c, e >> 1, e & 1)) = kvec{};
+          }
+        fence_proxy_async_smem();                                           // (the next tile comes by the async proxy)
+      }
+      for (float back0 = 1.f, back1 = 1.f;;) {                              // what undoes the scaling of keys key0, key0 + 2
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) s[nt][0] = s[nt][1] = s[nt][2] = s[nt][3] = 0.f;
 #pragma unroll
@@ -393,37 +407,43 @@ slim_tree_p_kernel(const __grid_constant__ CUtensorMap cmap, const __grid_consta
           }
         }
         // an overflow shows as an infinity or a NaN, and 0 x it is a NaN
+        if (whole) {
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int x = 0; x < 4; ++x) s[nt][x] *= sr[8 * nt + 2 * c + (x & 1)].x * (x < 2 ? back0 : back1);
+          break;
+        }
         float odd = 0.f;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
           for (int x = 0; x < 4; ++x) odd = fmaf(s[nt][x], 0.f, odd);
-        if (again || !__any_sync(0xffffffffu, careful || odd != 0.f)) break;
-        again = true;
-        float top = 0.f, ks = 0.f;
-        for (int turn2 = 0; turn2 < 2; ++turn2) {                           // the largest element, then the scaling, in place: a thread's own elements
+        if (!__any_sync(0xffffffffu, careful || odd != 0.f)) break;
+        whole = true;
+        // every key by its own largest element (its four lanes have it in common), so that none wipes out another; in place
+#pragma unroll 1                                                            // (rare: no registers for it)
+        for (int rh = 0; rh < 2; ++rh) {
+          float top = 0.f;
+#pragma unroll 1
+          for (int e = 0; e < 2 * NPC; ++e) {
+            const kvec v = *reinterpret_cast<const kvec*>(tile + tile_off<DK>(key0 + 2 * rh, c, e >> 1, e & 1));
 #pragma unroll
-          for (int rh = 0; rh < 2; ++rh)
+            for (int x = 0; x < VW / 2; ++x)
+              top = fmaxf(top, fmaxf(fabsf(__uint_as_float(word(v, x) << 16)), fabsf(__uint_as_float(word(v, x) & 0xffff0000u))));
+          }
+          top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+          top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+          const float ks = pow2_to(top, 10);
+          if (rh == 0) back0 = 1.f / ks; else back1 = 1.f / ks;
+#pragma unroll 1
+          for (int e = 0; e < 2 * NPC; ++e) {
+            kvec* at = reinterpret_cast<kvec*>(tile + tile_off<DK>(key0 + 2 * rh, c, e >> 1, e & 1));
+            kvec v = *at;
 #pragma unroll
-            for (int pc = 0; pc < NPC; ++pc)
-#pragma unroll
-              for (int hl = 0; hl < 2; ++hl) {
-                kvec* at = reinterpret_cast<kvec*>(tile + tile_off<DK>(key0 + 2 * rh, c, pc, hl));
-                kvec v = *at;
-#pragma unroll
-                for (int x = 0; x < VW / 2; ++x) {
-                  const uint32_t w = word(v, x);
-                  const float e0 = __uint_as_float(w << 16), e1 = __uint_as_float(w & 0xffff0000u);
-                  if (turn2 == 0) top = fmaxf(top, fmaxf(fabsf(e0), fabsf(e1)));
-                  else word_ref(v, x) = bf162_of(e0 * ks, e1 * ks);         // (a power of two: exact, but for what is 2^-100 of the largest)
-                }
-                if (turn2 == 1) *at = v;
-              }
-          if (turn2 == 0) {
-#pragma unroll
-            for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-            ks = pow2_to(top, 10);
-            back = 1.f / ks;
+            for (int x = 0; x < VW / 2; ++x)                                // (a power of two: exact, but for what is 2^-100 of the largest)
+              word_ref(v, x) = bf162_of(__uint_as_float(word(v, x) << 16) * ks, __uint_as_float(word(v, x) & 0xffff0000u) * ks);
+            *at = v;
           }
         }
         fence_proxy_async_smem();                                           // (the next tile comes by the async proxy)
@@ -431,7 +451,7 @@ slim_tree_p_kernel(const __grid_constant__ CUtensorMap cmap, const __grid_consta
       __syncwarp();                                                         // all lanes have read the tile
       if (lane == 0 && it + S::KS < total && !*s_abort) fetch(it + S::KS);
       // ---- what is not attended
-      if (draft || t0 + 16 > len) {
+      if (edge) {
   #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -447,7 +467,7 @@ slim_tree_p_kernel(const __grid_constant__ CUtensorMap cmap, const __grid_consta
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
         const float4 v = *reinterpret_cast<const float4*>(sr + 8 * nt + 2 * c);
-        const float s0 = v.x * back, s1 = v.z * back;
+        const float s0 = whole ? 1.f : v.x, s1 = whole ? 1.f : v.z;
         y[nt][0] = fmaf(s[nt][0], s0, -v.y); y[nt][1] = fmaf(s[nt][1], s1, -v.w);
         y[nt][2] = fmaf(s[nt][2], s0, -v.y); y[nt][3] = fmaf(s[nt][3], s1, -v.w);
         moves = moves || fmaxf(fmaxf(y[nt][0], y[nt][1]), fmaxf(y[nt][2], y[nt][3])) > 60.f;
@@ -461,7 +481,7 @@ slim_tree_p_kernel(const __grid_constant__ CUtensorMap cmap, const __grid_consta
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
           for (int z = 0; z < 2; ++z) {
-            float m = fmaxf(s[nt][z], s[nt][2 + z]) * (sr[8 * nt + 2 * c + z].x * back);
+            float m = fmaxf(s[nt][z], s[nt][2 + z]) * (whole ? 1.f : sr[8 * nt + 2 * c + z].x);
 #pragma unroll
             for (int o = 4; o < 32; o <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
             if (g == 0) atomicMax(smax + 8 * nt + 2 * c + z, ordered(m));
@@ -475,7 +495,7 @@ slim_tree_p_kernel(const __grid_constant__ CUtensorMap cmap, const __grid_consta
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
           const float4 v = *reinterpret_cast<const float4*>(sr + 8 * nt + 2 * c);
-          const float s0 = v.x * back, s1 = v.z * back;
+          const float s0 = whole ? 1.f : v.x, s1 = whole ? 1.f : v.z;
           y[nt][0] = fmaf(s[nt][0], s0, -v.y); y[nt][1] = fmaf(s[nt][1], s1, -v.w);
           y[nt][2] = fmaf(s[nt][2], s0, -v.y); y[nt][3] = fmaf(s[nt][3], s1, -v.w);
         }

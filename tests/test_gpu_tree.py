@@ -579,3 +579,65 @@ def test_draft_verify_commit_and_decode_go_together(dtype, tol):
             assert int(nxt.min()) >= 0
     finally:
         lay.close()
+
+
+# ------------------------------------------------------------------------------------------------ rows that are not attended, numbers that are not finite
+@pytest.mark.parametrize("value", [1.0e5, -1.0e10, 1.0e30, 3.0e38, float("inf")])
+@pytest.mark.parametrize("d,H,theta,dtype,page,n", [
+    (512, 4, 1.0e4, "bf16", 0, 16), (512, 8, 1.0e4, "bf16", 16, 9), (384, 4, 0.0, "bf16", 64, 33), (384, 6, 1.0e4, "f32", 0, 5)])
+def test_rows_that_are_not_attended_hold_large_numbers(d, H, theta, dtype, page, n, value):
+    """Rows behind the lengths, unused pages and padding drafts hold numbers beyond the range of the 16-bit products."""
+    g = np.random.default_rng(n)
+    lengths = [1, 15, 17, 100, 130, 0, 250]
+    parents = [random_parents(g, n) for _ in lengths]
+    parents[1] = [-1, 0] + [-2] * (n - 2)
+    with Case(d, H, theta, dtype, lengths, parents, page, seed=n + 1) as c:
+        was = [(x, x.isnan()) for x in (c.store, c.dq, c.dkt)]
+        for x, dead in was:
+            x[dead] = 0
+        c.call()
+        want = c.o.clone()
+        for x, dead in was:
+            x[dead] = value
+        c.call()
+        assert c.status() == B.SLIM_OK
+        c.check()
+        assert torch.equal(c.o, want)
+
+
+@pytest.mark.parametrize("key", [1.0e6, 1.0e12, 1.0e30])
+def test_neighbouring_sequences_and_drafts_hold_large_numbers(key):
+    """A tile of 16 rows reaches into the next sequence's rows and drafts, which lie `key` times higher (and its queries as
+    much lower); a capacity and a number of drafts that are no multiples of 16."""
+    g = np.random.default_rng(3)
+    with Case(512, 4, 1.0e4, "bf16", [107, 107, 50, 107], [random_parents(g, 5, pad=False) for _ in range(4)], seed=8, t_cap=107) as c:
+        for b in (1, 3):
+            c.K[b] = synth.round_to_dtype(c.K[b] * np.float32(key), "bf16")
+            c.kt[b] = synth.round_to_dtype(c.kt[b] * np.float32(key), "bf16")
+            c.q[b] = synth.round_to_dtype(c.q[b] / np.float32(key), "bf16")
+            c.store[b, :107] = to_dev(c.K[b], "bf16")
+        c.dq, c.dkt = to_dev(c.q, "bf16"), to_dev(c.kt, "bf16")
+        c.call()
+        assert c.status() == B.SLIM_OK
+        c.check()
+
+
+@pytest.mark.parametrize("dtype,key", [("bf16", 1.0e6), ("bf16", 1.0e10), ("bf16", 1.0e30), ("f32", 1.0e10)])
+def test_a_key_far_above_its_neighbours(dtype, key):
+    """Rows that are `key` in one element, against which the queries are positive: their argument is so low that their
+    probability is 0, so the others' results are those without them (no rotation, so the positions do not matter)."""
+    d, H, n = 256, 2, 9
+    out = np.array([3, 40, 41, 77, 199, 255])
+    with Case(d, H, 0.0, dtype, [260, 140], [[-1, 0, 1, -1, 0, 4, 5, 6, -1], [-1] * 9], seed=5) as c:
+        c.q[..., ::128] = 1.0 + np.abs(c.q[..., ::128])
+        for b in range(2):
+            rows = out[out < len(c.K[b])]
+            c.K[b][rows, ::128] = -key
+            c.K[b] = synth.round_to_dtype(c.K[b], dtype)
+            c.store[b, :len(c.K[b])] = to_dev(c.K[b], dtype)
+            c.K[b] = np.delete(c.K[b], rows, axis=0)
+        c.q = synth.round_to_dtype(c.q, dtype)
+        c.dq = to_dev(c.q, dtype)
+        c.call()
+        assert c.status() == B.SLIM_OK
+        c.check()
