@@ -264,9 +264,10 @@ __global__ void __launch_bounds__(256) slim_tree_sum_kernel(const SlimDecodePara
     const int r = r0 + 4 * ty + x;
     if (r >= R) continue;
     float* U = t.u + (((size_t)part * p.batch + b) * R + r) * p.d + c0 + 4 * tx;
+    const bool none = s_il[4 * ty + x] == 0.f;                     // (padding: 0 whatever the keys hold)
 #pragma unroll
     for (int y = 0; y < 4; ++y)
-      if (c0 + 4 * tx + y < p.d) U[y] = acc[x][y];
+      if (c0 + 4 * tx + y < p.d) U[y] = none ? 0.f : acc[x][y];
   }
 }
 

@@ -641,3 +641,16 @@ def test_a_key_far_above_its_neighbours(dtype, key):
         c.call()
         assert c.status() == B.SLIM_OK
         c.check()
+
+
+@pytest.mark.parametrize("d,H,dtype,L", [(512, 4, "bf16", 40), (512, 8, "bf16", 300), (384, 6, "f32", 40), (384, 6, "f32", 1500), (200, 2, "bf16", 100)])
+def test_padding_gets_zeros_beside_keys_that_are_not_finite(d, H, dtype, L):
+    """0 x infinity is no number: a padding token's row is 0 all the same, whatever the cached rows and live drafts hold."""
+    with Case(d, H, 1.0e4, dtype, [L, L], [[-1, 0, -2, 0, -7], [-2] * 5], seed=2) as c:
+        c.dkt[0, 3, 3] = float("inf")
+        c.store[0, 11, 5:9] = float("nan")
+        c.store[1, 7, d - 1] = float("-inf")
+        c.call()
+        assert c.status() == B.SLIM_OK
+        assert (c.o[0, [2, 4]] == 0).all() and (c.o[1] == 0).all()
+        assert not torch.isfinite(c.o[0, [0, 1, 3]].float()).any()
