@@ -298,6 +298,7 @@ slim_status slim_combine_project(slim_ctx* ctx, const float* lse_all, const floa
  *   lengths    device int32 [batch]: cached rows of sequence b (0: the tokens attend the tree only); above t_cap:
  *              clamped and reported as SLIM_ERR_CAPACITY.  Rows behind them may hold anything; a number that is not finite
  *              in a cached row, or in the key of a token that is there, reaches every token of its sequence
+ *              that is not padding; one in a token's query makes that token's heads NaN
  *   o          device [batch][n][d], ctx dtype (float32, or bfloat16: the operand of the output projection,
  *              rounded once at the end), 16-byte aligned; a padding token gets a zero row, and what q and
  *              k_tree hold for it is not used

@@ -152,7 +152,8 @@ __global__ void __launch_bounds__(256) slim_tree_scores_kernel(const SlimDecodeP
   }
 }
 
-// m and 1 / l of every row (one block a row); a token that is padding, or whose row is empty, gets 1 / l = 0.
+// m and 1 / l of every row (one block a row); padding gets 1 / l = 0.  A token that is there attends itself at least, so a
+// sum that is not a positive number (arguments that are NaN or infinite) is no empty row: its 1 / l is NaN.
 __global__ void __launch_bounds__(256) slim_tree_stat_kernel(const SlimDecodeParams p, const SlimTreeView t) {
   __shared__ float s_m[8], s_l[8];
   slim_pdl_trigger();
@@ -162,21 +163,23 @@ __global__ void __launch_bounds__(256) slim_tree_stat_kernel(const SlimDecodePar
   float m = -INFINITY, l = 0.f;
   auto join = [&](float m1, float l1) {
     const float top = fmaxf(m, m1);
-    if (top != -INFINITY) l = l * exp2f(m - top) + l1 * exp2f(m1 - top);
+    l = top != -INFINITY ? l * exp2f(m - top) + l1 * exp2f(m1 - top) : l + l1;       // (the maximum passes over NaN, the sum keeps it)
     m = top;
   };
-  if (t.depth[(size_t)b * t.n + i] >= 0) {
+  auto one = [](float v) { return v == -INFINITY ? 0.f : v == v ? 1.f : v; };
+  const bool there = t.depth[(size_t)b * t.n + i] >= 0;
+  if (there) {
     const float* S = t.s + ((size_t)b * R + row) * t.s_ld;
     for (int x = tid; x < len; x += 1024) {
       float v[4];
 #pragma unroll
       for (int y = 0; y < 4; ++y) v[y] = x + 256 * y < len ? S[x + 256 * y] : -INFINITY;
 #pragma unroll
-      for (int y = 0; y < 4; ++y) join(v[y], v[y] == -INFINITY ? 0.f : 1.f);
+      for (int y = 0; y < 4; ++y) join(v[y], one(v[y]));
     }
     if (tid < t.n) {
       const float v = S[t.s_draft + tid];
-      join(v, v == -INFINITY ? 0.f : 1.f);
+      join(v, one(v));
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) {
@@ -189,7 +192,7 @@ __global__ void __launch_bounds__(256) slim_tree_stat_kernel(const SlimDecodePar
   if (tid == 0) {
     for (int w = 1; w < 8; ++w) join(s_m[w], s_l[w]);
     t.m[(size_t)b * R + row] = m == -INFINITY ? 0.f : m;
-    t.inv_l[(size_t)b * R + row] = l != 0.f ? 1.f / l : 0.f;       // (NaN stays NaN)
+    t.inv_l[(size_t)b * R + row] = !there ? 0.f : l > 0.f && l < INFINITY ? 1.f / l : NAN;
   }
 }
 

@@ -666,8 +666,10 @@ __device__ __forceinline__ bool sum_next(const SumSched& s, int q, SumWalk& w, S
 // 32 rows a block, 32 threads a row: M = the largest reference of the row's blocks that hold anything, 1 / l, and blocks of
 // P whose reference is another (rare: a row whose block maxima are more than about 32 apart around a multiple of 64)
 // multiplied by 2^(ref - M), a power of two: exact, down to values below 2^-94 of the row's largest, which become 0.
-// FIN_TAIL blocks of a sequence behind these write its tail [128][d]: 0..63 the cached rows behind the last whole block of
-// 64, 64..127 the drafted keys, everything else zero; one last block of the grid lays down the product's schedule.
+// A token that is there attends itself at least: a sum that is not a positive number (arguments that are NaN or infinite) is
+// no empty row, its 1 / l is NaN.  FIN_TAIL blocks of a sequence behind these write its tail [128][d]: 0..63 the cached rows
+// behind the last whole block of 64, 64..127 the drafted keys, everything else zero; one last block of the grid lays down the
+// product's schedule.
 constexpr int FIN_TAIL = 16;
 __global__ void __launch_bounds__(1024) slim_tree_finish_kernel(const SlimDecodeParams p, const SlimTreeView t) {
   __shared__ float s_m[32][33], s_l[32][33];
@@ -712,7 +714,7 @@ __global__ void __launch_bounds__(1024) slim_tree_finish_kernel(const SlimDecode
 #pragma unroll
       for (int x4 = 0; x4 < 4; ++x4) {
         if (v[x4].y == 0.f) continue;
-        if (v[x4].x == m) { l += v[x4].y; continue; }
+        if (v[x4].x == m) { l += v[x4].y; continue; }      // (also -inf: a sum without a reference is NaN, and stays)
         same = same && m == -INFINITY;
         const float top = fmaxf(m, v[x4].x);
         l = l * exp2f(m - top) + v[x4].y * exp2f(v[x4].x - top);
@@ -723,11 +725,10 @@ __global__ void __launch_bounds__(1024) slim_tree_finish_kernel(const SlimDecode
   __syncthreads();
   float M = -INFINITY, L = 0.f;
   for (int k = 0; k < 32; ++k) M = fmaxf(M, s_m[k][x]);
-  if (M != -INFINITY)
-    for (int k = 0; k < 32; ++k) L += s_l[k][x] == 0.f ? 0.f : s_l[k][x] * exp2f(s_m[k][x] - M);
+  for (int k = 0; k < 32; ++k) L += s_l[k][x] == 0.f ? 0.f : M == -INFINITY ? s_l[k][x] : s_l[k][x] * exp2f(s_m[k][x] - M);
   if (row >= R) return;
   const bool there = t.depth[(size_t)b * t.n + row % t.n] >= 0;
-  if (y == 0) t.inv_l[(size_t)b * R + row] = there && L != 0.f ? 1.f / L : 0.f;
+  if (y == 0) t.inv_l[(size_t)b * R + row] = !there ? 0.f : L > 0.f && L < INFINITY ? 1.f / L : NAN;
   if (same && (m == M || m == -INFINITY)) return;
   for (int k = y; k <= nblk; k += 32) {
     const float2 v = stat[(size_t)(k == nblk ? nb_cap : k) * R];
@@ -964,7 +965,7 @@ slim_tree_u_kernel(const __grid_constant__ CUtensorMap pmap, const __grid_consta
 #pragma unroll
               for (int y = 0; y < 4; ++y)
                 split2(__uint_as_float(v[8 * x + 2 * y]) * il, __uint_as_float(v[8 * x + 2 * y + 1]) * il, word_ref(hi[x], y), word_ref(lo[x], y));
-              if (il == 0.f) hi[x] = lo[x] = make_uint4(0, 0, 0, 0);         // (an empty row is 0 whatever the keys hold)
+              if (il == 0.f) hi[x] = lo[x] = make_uint4(0, 0, 0, 0);         // (padding is 0 whatever the keys hold)
             }
             turned(hi, o4);
 #pragma unroll
@@ -1084,7 +1085,7 @@ __global__ void __launch_bounds__(256, 2) slim_tree_join_kernel(const SlimDecode
     const int r = row0 + tid / 64 + 4 * m;
     if (r >= R) continue;
     const float il = t.inv_l[(size_t)b * R + r];
-    if (il == 0.f) a[m] = make_float4(0.f, 0.f, 0.f, 0.f);    // (an empty row is 0 whatever the keys hold)
+    if (il == 0.f) a[m] = make_float4(0.f, 0.f, 0.f, 0.f);    // (padding is 0 whatever the keys hold)
     const int h = r / t.n, tok = r - h * t.n;
     uint2 hi, lo;
     split2(a[m].x * il, a[m].y * il, hi.x, lo.x);

@@ -654,3 +654,48 @@ def test_padding_gets_zeros_beside_keys_that_are_not_finite(d, H, dtype, L):
         assert c.status() == B.SLIM_OK
         assert (c.o[0, [2, 4]] == 0).all() and (c.o[1] == 0).all()
         assert not torch.isfinite(c.o[0, [0, 1, 3]].float()).any()
+
+
+@pytest.mark.parametrize("value", [float("nan"), float("inf")])
+@pytest.mark.parametrize("d,H,dtype,n", [(512, 4, "bf16", 12), (512, 8, "bf16", 3), (384, 4, "bf16", 40), (384, 6, "f32", 5), (200, 2, "bf16", 5)])
+def test_a_query_that_is_not_finite_gives_no_numbers(d, H, dtype, n, value):
+    """One token's query, and one head of another's: NaN in what they determine, nothing else changes."""
+    g = np.random.default_rng(n)
+    lengths = [0, 40, 300]
+    d_k = d // H
+    with Case(d, H, 1.0e4, dtype, lengths, [random_parents(g, n, pad=False) for _ in lengths], seed=n) as c:
+        c.call()
+        torch.cuda.synchronize()
+        want = c.o.clone()
+        c.check(want)
+        c.dq[:, 1] = value
+        c.dq[:, 2, d_k] = value                              # an element of head 1
+        c.call()
+        assert c.status() == B.SLIM_OK
+        bad = torch.zeros_like(c.o, dtype=torch.bool)
+        bad[:, 1] = True
+        bad[:, 2, d_k:2 * d_k] = True
+        assert c.o[bad].isnan().all()
+        c.check(torch.where(bad, want, c.o))
+
+
+@pytest.mark.parametrize("d,H,dtype", [(512, 4, "bf16"), (512, 8, "bf16"), (384, 6, "f32"), (200, 2, "bf16")])
+def test_a_key_that_is_not_finite_reaches_every_token(d, H, dtype):
+    """... of its sequence, also the first token of an empty context; padding still gets a zero row."""
+    n = 5
+    parents = [[-1, 0, -2, 0, 3]] * 5
+    with Case(d, H, 1.0e4, dtype, [0, 40, 40, 150, 40], parents, seed=2) as c:
+        c.dkt[0, 0, 7] = float("nan")                        # nothing cached: the tokens' own keys are all there is
+        c.dkt[1, 4, 3] = float("inf")                        # a leaf, which the others do not attend
+        c.store[2, 11] = float("nan")
+        c.store[3, 5, d - 1] = float("-inf")
+        c.call()
+        assert c.status() == B.SLIM_OK
+        live = torch.tensor([0, 1, 3, 4], device=DEV)
+        assert not torch.isfinite(c.o[:4, live].float()).any()
+        assert (c.o[:, 2] == 0).all()
+        got = c.o.clone()
+        got[:4] = 0
+        c.lengths, c.K = c.lengths[4:], c.K[4:]
+        c.q, c.kt, c.parents, c.batch = c.q[4:], c.kt[4:], c.parents[4:], 1
+        c.check(got[4:])
