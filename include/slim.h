@@ -314,7 +314,8 @@ slim_status slim_combine_project(slim_ctx* ctx, const float* lse_all, const floa
  *   p, q       float32 [batch][n][vocab]: the target's probabilities after node i, and the distribution that the
  *              children of node i were drawn from (rows of nodes without children are not read); rows of p sum to 1
  *   tokens     int32 [batch][n]; a child's token outside [0, vocab) raises SLIM_ERR_TREE and makes it padding
- *   parents    as above; roots other than node 0 are never reached
+ *   parents    as above (SLIM_ERR_TREE included), but node 0 is the root whatever parents[0] holds; other roots are never
+ *              reached
  *   r          float32 [batch][n], uniform in [0, 1): r[i] tests node i, r[0] draws the next token
  *   From u = 0, W = p_u, S = 1, the children c of u in index order: accepted if r_c S q_u(x_c) < W(x_c), then u = c,
  *   W = p_c, S = 1; otherwise W = max(W - S q_u, 0), S = sum W (both stay as they were if nothing is left).

@@ -101,7 +101,8 @@ slim_tree_verify_kernel(const float* __restrict__ P, const float* __restrict__ Q
   if (tid < n) {
     const int par = parents[(size_t)b * n + tid], tok = tokens[(size_t)b * n + tid];
     bool child = tid > 0 && par >= 0;
-    if (child && (par >= tid || tok < 0 || tok >= V)) {
+    // (node 0 is the root whatever its parent says, so a parent that is padding is another node below -1)
+    if (child && (par >= tid || tok < 0 || tok >= V || (par > 0 && parents[(size_t)b * n + par] < -1))) {
       child = false;
       if (rank == 0) atomicMax(status, (int)SLIM_ERR_TREE);
     }

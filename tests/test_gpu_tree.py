@@ -699,3 +699,17 @@ def test_a_key_that_is_not_finite_reaches_every_token(d, H, dtype):
         c.lengths, c.K = c.lengths[4:], c.K[4:]
         c.q, c.kt, c.parents, c.batch = c.q[4:], c.kt[4:], c.parents[4:], 1
         c.check(got[4:])
+
+
+def test_verification_reports_children_of_padding(ctx):
+    V = 40
+    one = np.zeros((2, 4, V), np.float32)
+    one[..., 5] = 1.0
+    tok = np.full((2, 4), 5, np.int32)
+    par = np.array([[-1, -2, 1, 0], [-1, 0, 1, 2]], np.int32)          # token 2 of the first hangs on padding
+    path, count, nxt, st = run_verify(ctx, one, one, tok, par, np.zeros((2, 4), np.float32))
+    assert st == B.SLIM_ERR_TREE
+    assert list(path[0]) == [0, 3, -1, -1] and list(path[1]) == [0, 1, 2, 3] and list(count) == [2, 4] and list(nxt) == [5, 5]
+    par[0] = [-5, -2, -2, 0]                                           # node 0 is the root whatever stands there
+    path, count, nxt, st = run_verify(ctx, one, one, tok, par, np.zeros((2, 4), np.float32))
+    assert st == B.SLIM_OK and list(path[0]) == [0, 3, -1, -1]
