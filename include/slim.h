@@ -321,7 +321,7 @@ slim_status slim_combine_project(slim_ctx* ctx, const float* lse_all, const floa
  *   W = p_c, S = 1; otherwise W = max(W - S q_u, 0), S = sum W (both stay as they were if nothing is left).
  *   When no child is left, the next token is the first x with W(0) + .. + W(x) > r_0 sum W.  Computed in float64.
  *   path       int32 [batch][n]: the accepted nodes, path[0] = 0, then -1;  count  int32 [batch]: how many
- *   next_token int32 [batch]: the token drawn after the last accepted node; -1 if W has no positive value
+ *   next_token int32 [batch]: the token drawn after the last accepted node; -1 if W has no positive value, or a NaN
  *
  * slim_tree_commit  k_tree[b][path[b][j]] -> cache row lengths[b] + j for j < count[b] (path, count as
  *   slim_tree_verify leaves them, or any indices into the tree; count 0 writes nothing).  f32 and bf16 caches,

@@ -63,7 +63,7 @@ def verify(p, q, tokens, parents, r):
             path.append(c)
         else:
             rest = np.maximum(W - S * q[u], 0.0)
-            if rest.sum() > 0:
+            if not rest.sum() <= 0:         # (a NaN is not nothing)
                 W, S = rest, rest.sum()
     cum = np.cumsum(W)
     if not cum[-1] > 0:

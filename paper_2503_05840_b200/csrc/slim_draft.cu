@@ -32,6 +32,9 @@ struct VerifyShared {
   int first, last, next;
 };
 
+// max(x, 0), and NaN for a NaN (fmax would return the 0): a row with a NaN has no mass, before a rejection as behind it
+__device__ __forceinline__ double positive(double x) { return x < 0.0 ? 0.0 : x; }
+
 // W(x) after the rejections whose masses are in `stage`: the products and differences are rounded one by one, so a stage
 // is a function of its inputs alone.  NS >= 0: that many, in registers; NS < 0: ns of them, in shared memory.
 template <int NS>
@@ -41,9 +44,9 @@ __device__ __forceinline__ double residual(float p, float q, const double* stage
   const double qd = (double)q;
   if (NS > 0) {
 #pragma unroll
-    for (int k = 0; k < (NS > 0 ? NS : 1); ++k) w = fmax(__dsub_rn(w, __dmul_rn(stage[k], qd)), 0.0);
+    for (int k = 0; k < (NS > 0 ? NS : 1); ++k) w = positive(__dsub_rn(w, __dmul_rn(stage[k], qd)));
   } else {
-    for (int k = 0; k < ns; ++k) w = fmax(__dsub_rn(w, __dmul_rn(stage[k], qd)), 0.0);
+    for (int k = 0; k < ns; ++k) w = positive(__dsub_rn(w, __dmul_rn(stage[k], qd)));
   }
   return w;
 }
@@ -158,7 +161,7 @@ slim_tree_verify_kernel(const float* __restrict__ P, const float* __restrict__ Q
     if (sh.par[c] != u) continue;
     double w = sh.px[c];
     const double q = sh.qx[c];
-    for (int k = 0; k < ns; ++k) w = fmax(__dsub_rn(w, __dmul_rn(sh.stage[k], q)), 0.0);
+    for (int k = 0; k < ns; ++k) w = positive(__dsub_rn(w, __dmul_rn(sh.stage[k], q)));
     if (__dmul_rn(__dmul_rn(sh.r[c], S), q) < w) {
       u = c; ns = 0; S = 1.0; fresh = false;
       if (tid == 0) sh.path[cnt] = c;
@@ -168,7 +171,7 @@ slim_tree_verify_kernel(const float* __restrict__ P, const float* __restrict__ Q
       if (tid == 0) sh.stage[ns] = S;
       __syncthreads();
       const double mass = sum_pass(u, ns + 1);
-      if (mass > 0.0) { ++ns; S = mass; total = mass; fresh = true; }
+      if (!(mass <= 0.0)) { ++ns; S = mass; total = mass; fresh = true; }      // (a NaN stays: nothing is accepted or drawn behind it)
       else fresh = false;            // nothing left: the distribution stays as it was
     }
   }

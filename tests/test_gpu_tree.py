@@ -713,3 +713,21 @@ def test_verification_reports_children_of_padding(ctx):
     par[0] = [-5, -2, -2, 0]                                           # node 0 is the root whatever stands there
     path, count, nxt, st = run_verify(ctx, one, one, tok, par, np.zeros((2, 4), np.float32))
     assert st == B.SLIM_OK and list(path[0]) == [0, 3, -1, -1]
+
+
+@pytest.mark.parametrize("V", [700, 701])
+@pytest.mark.parametrize("rejections", [1, 2, 3, 5])
+def test_a_nan_among_the_probabilities_is_not_lost_by_a_rejection(ctx, V, rejections):
+    """W = max(W - S q, 0) of a NaN is a NaN, in p or in q: no token is drawn from such a row."""
+    n = rejections + 1
+    g = np.random.default_rng(V)
+    p = np.full((3, n, V), 1.0 / V, np.float32)
+    q = p.copy()
+    tok = np.tile(np.arange(n, dtype=np.int32), (3, 1))
+    p[:, 0, :n] = 0.0                                                  # none of the drafted tokens is accepted
+    p[0, 0, V - 2] = np.nan
+    q[1, 0, 300] = np.nan
+    par = np.tile(np.array([-1] + [0] * rejections, np.int32), (3, 1))
+    path, count, nxt, st = run_verify(ctx, p, q, tok, par, g.random((3, n)).astype(np.float32))
+    assert st == B.SLIM_OK and list(count) == [1, 1, 1]
+    assert list(nxt[:2]) == [-1, -1] and nxt[2] >= n
