@@ -343,8 +343,8 @@ slim_status slim_tree_commit(slim_ctx* ctx, slim_cache* cache, const void* k_tre
  *
  * slim_accumulate_weights  acc[b][t] += sum_h softmax_t(q_h . K_h / sqrt(d_k)), t < lengths[b], for the query of
  *   slim_decode (un-rotated, at position lengths[b]-1; same arguments).  acc: device float32 [batch][t_cap],
- *   other elements are left alone.  Any cache that slim_decode takes.  workspace: device, >=
- *   slim_weights_workspace_bytes(ctx, batch, t_cap), 256-byte aligned.
+ *   other elements are left alone.  A NaN in an attended row or in the query makes every acc of its sequence NaN.  Any
+ *   cache that slim_decode takes.  workspace: device, >= slim_weights_workspace_bytes(ctx, batch, t_cap), 256-byte aligned.
  *
  * slim_evict  brings every sequence that is longer than `budget` rows down to it: the last `recent` rows stay
  *   (0 <= recent <= budget), and of the rows before them the budget - recent with the largest acc (equal values: the

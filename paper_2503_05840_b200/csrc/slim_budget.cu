@@ -20,6 +20,7 @@ __device__ __forceinline__ f32x2 sub2(f32x2 a, f32x2 b) { f32x2 d; asm("sub.rn.f
 // The rotation is moved onto the query, q^ . R_t k = (R_(pos - t) q) . k, which is seeded from the tables at the group's
 // first row of a tile (float32 products of entries made in float64) and turned by one position a row with a packed
 // complex product: at most 16 steps, so that its error stays below 2^-20.  Everything is float32.
+// A maximum passes over NaN, so the sums carry it: one NaN makes its whole softmax NaN, wherever it stands.
 // Bound by HBM: every key byte is read once.  16 ragged sequences, 196 k rows of 8 KB: 289 us, 5.6 TB/s, 0.86 of a copy's rate
 // (305 us with the two kernels behind it, 20 us for 1500 float32 rows of 1.5 KB, three launches).  A rotation seeded per row,
 // sums through shared memory, and four rows a round instead of two were slower.
@@ -177,6 +178,7 @@ slim_weights_scores_kernel(const SlimDecodeParams p, float* __restrict__ scores,
               out[t] = keep;
               const float top = fmaxf(run_m, keep);
               if (top != -INFINITY) run_l = run_l * ex2_approx(run_m - top) + ex2_approx(keep - top);
+              else if (keep != keep) run_l = keep;
               run_m = top;
             }
           };
@@ -212,12 +214,15 @@ slim_weights_scores_kernel(const SlimDecodeParams p, float* __restrict__ scores,
 #pragma unroll
     for (int o = 1; o < LPH; o <<= 1) {
       const float m1 = __shfl_xor_sync(0xffffffffu, run_m, o), l1 = __shfl_xor_sync(0xffffffffu, run_l, o), top = fmaxf(run_m, m1);
-      if (top != -INFINITY) run_l = run_l * ex2_approx(run_m - top) + l1 * ex2_approx(m1 - top);
+      run_l = top != -INFINITY ? run_l * ex2_approx(run_m - top) + l1 * ex2_approx(m1 - top) : run_l + l1;
       run_m = top;
     }
     if (li == 0 && h < H) part[((size_t)(w + b) * ring.groups + rg) * H + h] = make_float2(run_m, run_l);
   }
 }
+
+// 1 / denominator; of an empty sequence nobody reads it, so what is no positive number comes of arguments that are NaN or infinite.
+__device__ __forceinline__ float inverse_sum(float l) { return l > 0.f && l < INFINITY ? 1.f / l : NAN; }
 
 // Reference exponent and 1 / denominator of every (sequence, head) from its units' parts: a warp each.
 __global__ void __launch_bounds__(256) slim_weights_join_kernel(const SlimDecodeParams p, const float2* __restrict__ part, int groups,
@@ -239,7 +244,7 @@ __global__ void __launch_bounds__(256) slim_weights_join_kernel(const SlimDecode
 #pragma unroll
       for (int x = 0; x < 4; ++x) {
         const float top = fmaxf(m, v[x].x);
-        if (top != -INFINITY) l = l * exp2f(m - top) + v[x].y * exp2f(v[x].x - top);
+        l = top != -INFINITY ? l * exp2f(m - top) + v[x].y * exp2f(v[x].x - top) : l + v[x].y;
         m = top;
       }
     }
@@ -247,12 +252,12 @@ __global__ void __launch_bounds__(256) slim_weights_join_kernel(const SlimDecode
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) {
     const float m1 = __shfl_xor_sync(0xffffffffu, m, o), l1 = __shfl_xor_sync(0xffffffffu, l, o), top = fmaxf(m, m1);
-    if (top != -INFINITY) l = l * exp2f(m - top) + l1 * exp2f(m1 - top);
+    l = top != -INFINITY ? l * exp2f(m - top) + l1 * exp2f(m1 - top) : l + l1;
     m = top;
   }
   if (lane == 0) {
     m_out[(size_t)b * p.H + h] = m == -INFINITY ? 0.f : m;
-    inv_out[(size_t)b * p.H + h] = l != 0.f ? 1.f / l : 0.f;
+    inv_out[(size_t)b * p.H + h] = inverse_sum(l);
   }
 }
 
@@ -270,12 +275,12 @@ __global__ void __launch_bounds__(256) slim_weights_stat_kernel(const SlimDecode
   for (int t = tid; t < len; t += 256) {
     const float s = S[t], top = fmaxf(m, s);
     if (top != -INFINITY) l = l * exp2f(m - top) + exp2f(s - top);
+    else if (s != s) l = s;
     m = top;
   }
   auto join = [](float& m0, float& l0, float m1, float l1) {
     const float top = fmaxf(m0, m1);
-    if (top == -INFINITY) return;
-    l0 = l0 * exp2f(m0 - top) + l1 * exp2f(m1 - top);
+    l0 = top != -INFINITY ? l0 * exp2f(m0 - top) + l1 * exp2f(m1 - top) : l0 + l1;
     m0 = top;
   };
 #pragma unroll
@@ -285,7 +290,7 @@ __global__ void __launch_bounds__(256) slim_weights_stat_kernel(const SlimDecode
   if (tid == 0) {
     for (int w = 1; w < 8; ++w) join(m, l, s_m[w], s_l[w]);
     m_out[(size_t)b * p.H + h] = m == -INFINITY ? 0.f : m;
-    inv_out[(size_t)b * p.H + h] = l != 0.f ? 1.f / l : 0.f;
+    inv_out[(size_t)b * p.H + h] = inverse_sum(l);
   }
 }
 

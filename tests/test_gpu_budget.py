@@ -289,3 +289,32 @@ def test_evict_and_weights_behind_four_billion_elements():
     for x, y in zip(got[0][:3], got[1][:3]):
         assert torch.equal(x, y)
     B.slim_destroy(ctx)
+
+
+@pytest.mark.parametrize("d,H,dtype", [(512, 4, "bf16"), (384, 6, "f32"), (1000, 10, "bf16"), (512, 8, "fp8")])
+def test_a_weight_that_is_no_number_reaches_its_whole_sequence(d, H, dtype):
+    """A row of keys, or one head of it, that is NaN: every softmax over it is, wherever the row stands and however the
+    context is cut."""
+    lay = SlimLayer(d, H, d // H, 1.0e4, dtype, 4, 520, DEV)
+    try:
+        torch.manual_seed(1)
+        lens = torch.tensor([500, 500, 37, 300], dtype=torch.int32, device=DEV)
+        if dtype == "fp8":
+            lay.append_k(torch.randn(4, 520, d, device=DEV).bfloat16(), torch.zeros(4, dtype=torch.int32, device=DEV))
+            codes = lay.k[:4 * 520 * d].view(4, 520, d)
+            codes[0, 0], codes[1, 333, :d // H], codes[2, 36] = 0x7f, 0x7f, 0x7f
+        else:
+            lay.k.normal_()
+            lay.k[0, 0], lay.k[1, 333, :d // H], lay.k[2, 36] = float("nan"), float("nan"), float("nan")
+        q = torch.randn(4, d, device=DEV).to(lay.tdtype)
+        acc = torch.ones(4, 520, device=DEV)
+        lay.accumulate_weights(q, lens, acc)
+        assert lay.device_status() == B.SLIM_OK
+        for b, L in enumerate(lens.tolist()):
+            assert acc[b, :L].isnan().all() if b < 3 else torch.isfinite(acc[b, :L]).all(), b
+            assert (acc[b, L:] == 1).all()
+        q[3, 0] = float("nan")                               # the query of the one that was left
+        lay.accumulate_weights(q, lens, acc)
+        assert acc[3, :300].isnan().all() and (acc[3, 300:] == 1).all()
+    finally:
+        lay.close()
