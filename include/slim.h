@@ -302,8 +302,10 @@ slim_status slim_combine_project(slim_ctx* ctx, const float* lse_all, const floa
  *   o          device [batch][n][d], ctx dtype (float32, or bfloat16: the operand of the output projection,
  *              rounded once at the end), 16-byte aligned; a padding token gets a zero row, and what q and
  *              k_tree hold for it is not used
- *   workspace  device, >= slim_tree_workspace_bytes(ctx, batch, t_cap, n) (0 on bad arguments), 256-byte
- *              aligned; contents are scratch.  Calls that may overlap on the GPU need one each
+ *   workspace  device, >= slim_tree_workspace_bytes(ctx, batch, t_cap, n) (0 on bad arguments; enough for either path of
+ *              slim_set_path, and not always growing with n: take the largest of the sizes in use), 256-byte aligned;
+ *              contents are scratch.  Calls that run one after another, of any layer, may share one; those that may overlap
+ *              on the GPU need one each
  *   Softmax sums and the weighted sums are float32.  The tensor-core path (bf16, d % 64 == 0, d_k in {64, 96, 128};
  *   slim_set_path chooses as for slim_decode) rounds rotated queries and keys to 11 bits for the scores and the
  *   probabilities to bf16 for the weighted sum.

@@ -9,12 +9,45 @@ import torch
 from . import binding as B
 
 
+class Scratch:
+    """Device memory of SlimLayer.tree_decode, accumulate_weights and evict.  Layers whose calls run one after another on a
+    stream may share one.  It grows with the largest call so far; what it grew out of is given back, unless a graph has been
+    captured on it."""
+
+    def __init__(self, device):
+        self.device = torch.device(device)
+        self.buffers = []        # the one in use last; before it those that captured graphs hold on to
+        self.captured = False    # a graph uses the last one
+        self.home = None         # the stream that it was allocated on
+
+    def take(self, need: int) -> torch.Tensor:
+        """At least `need` bytes for a call on the current stream."""
+        if need == 0:
+            raise ValueError("unsupported sizes")
+        capturing, stream = torch.cuda.is_current_stream_capturing(), torch.cuda.current_stream(self.device)
+        if not self.buffers or self.buffers[-1].numel() < need:
+            if capturing:
+                raise RuntimeError("the layer's scratch has to exist before a capture: reserve_scratch, or make a call of these "
+                                   "sizes first")
+            if self.buffers and not self.captured:
+                self.buffers.pop()
+            self.buffers.append(torch.empty(need, dtype=torch.uint8, device=self.device))
+            self.captured, self.home = False, stream
+        if capturing:
+            self.captured = True
+        elif stream != self.home:                # the allocator must not hand it out before this call has run
+            self.buffers[-1].record_stream(stream)
+        return self.buffers[-1]
+
+
 class SlimLayer:
     def __init__(self, d: int, H: int, d_k: int, rope_theta: float, dtype: str, batch: int, t_cap: int,
-                 device: str = "cuda:0", workspace: "torch.Tensor | None" = None):
+                 device: str = "cuda:0", workspace: "torch.Tensor | None" = None, scratch: "Scratch | None" = None):
         if not torch.cuda.is_available():
             raise RuntimeError("SlimLayer needs a CUDA device (there is no CPU fallback)")
         self.device = torch.device(device)
+        if scratch is not None and (not isinstance(scratch, Scratch) or scratch.device != self.device):
+            raise ValueError(f"scratch: a Scratch on {self.device} is needed, e.g. another layer's .scratch")
         self.d, self.H, self.d_k, self.batch, self.t_cap = d, H, d_k, batch, t_cap
         self.dtype = dtype
         # type of q, of new key rows and of W_KV; an "fp8" layer keeps only its cache in 8 bits
@@ -32,7 +65,8 @@ class SlimLayer:
             assert workspace.numel() >= need and workspace.data_ptr() % 256 == 0
             self.workspace = workspace
             self.o = torch.empty((batch, d), dtype=torch.float32, device=self.device)
-            self._extra = []
+            self.scratch = Scratch(self.device) if scratch is None else scratch
+            self._extra = self.scratch.buffers
 
     # ---- set-up -------------------------------------------------------------
     def set_weights(self, W_K, W_V, want_wkv: bool = False):
@@ -75,16 +109,15 @@ class SlimLayer:
                              f"{x.dtype} {tuple(x.shape)} on {x.device}" + ("" if x.is_contiguous() else ", not contiguous"))
         return x
 
-    def _scratch(self, need: int) -> torch.Tensor:
-        """Scratch of the calls below; calls of one layer run one after another on a stream.  It grows with the largest call
-        so far, and what was handed out before stays allocated: a captured graph keeps using it."""
-        if need == 0:
-            raise ValueError("unsupported sizes")
-        if not self._extra or self._extra[-1].numel() < need:
-            if torch.cuda.is_current_stream_capturing():
-                raise RuntimeError("the layer's scratch has to exist before a capture: make a call of these sizes first")
-            self._extra.append(torch.empty(need, dtype=torch.uint8, device=self.device))
-        return self._extra[-1]
+    def reserve_scratch(self, n: int = 0) -> None:
+        """Size the scratch for trees of up to n tokens, accumulate_weights and evict at once (before a capture, for instance).
+        Without it the scratch grows with the calls."""
+        sizes = [B.slim_tree_workspace_bytes(self.ctx, self.batch, self.t_cap, i) for i in range(1, n + 1)]
+        if n < 0 or 0 in sizes:
+            raise ValueError(f"n: 0 to {B.SLIM_MAX_TREE} drafted tokens are possible, got {n}")
+        sizes += [B.slim_weights_workspace_bytes(self.ctx, self.batch, self.t_cap), B.slim_evict_workspace_bytes(self.ctx, self.batch, self.t_cap)]
+        with torch.cuda.device(self.device):
+            self.scratch.take(max(sizes))
 
     def tree_decode(self, q: torch.Tensor, k_tree: torch.Tensor, lengths: torch.Tensor, parents: torch.Tensor,
                     o: torch.Tensor | None = None) -> torch.Tensor:
@@ -98,7 +131,7 @@ class SlimLayer:
         self._arg("parents", parents, (self.batch, n), i32)
         o = torch.empty_like(q) if o is None else self._arg("o", o, q.shape, self.tdtype)
         with torch.cuda.device(self.device):
-            ws = self._scratch(B.slim_tree_workspace_bytes(self.ctx, self.batch, self.t_cap, n))
+            ws = self.scratch.take(B.slim_tree_workspace_bytes(self.ctx, self.batch, self.t_cap, n))
             B.slim_tree_decode(self.ctx, q, k_tree, self.cache, lengths, parents, n, o, ws,
                                torch.cuda.current_stream(self.device).cuda_stream)
         return o
@@ -137,7 +170,7 @@ class SlimLayer:
         self._arg("lengths", lengths, (self.batch,), torch.int32)
         self._arg("acc", acc, (self.batch, self.t_cap), torch.float32)
         with torch.cuda.device(self.device):
-            ws = self._scratch(B.slim_weights_workspace_bytes(self.ctx, self.batch, self.t_cap))
+            ws = self.scratch.take(B.slim_weights_workspace_bytes(self.ctx, self.batch, self.t_cap))
             B.slim_accumulate_weights(self.ctx, q, self.cache, lengths, acc, ws, torch.cuda.current_stream(self.device).cuda_stream)
         return acc
 
@@ -148,7 +181,7 @@ class SlimLayer:
         self._arg("acc", acc, (self.batch, self.t_cap), torch.float32)
         kept = torch.empty((self.batch, max(int(budget), 0)), dtype=torch.int32, device=self.device)
         with torch.cuda.device(self.device):
-            ws = self._scratch(B.slim_evict_workspace_bytes(self.ctx, self.batch, self.t_cap))
+            ws = self.scratch.take(B.slim_evict_workspace_bytes(self.ctx, self.batch, self.t_cap))
             B.slim_evict(self.ctx, self.cache, lengths, acc, int(budget), int(recent), kept, ws,
                          torch.cuda.current_stream(self.device).cuda_stream)
         return kept

@@ -731,3 +731,81 @@ def test_a_nan_among_the_probabilities_is_not_lost_by_a_rejection(ctx, V, reject
     path, count, nxt, st = run_verify(ctx, p, q, tok, par, g.random((3, n)).astype(np.float32))
     assert st == B.SLIM_OK and list(count) == [1, 1, 1]
     assert list(nxt[:2]) == [-1, -1] and nxt[2] >= n
+
+
+def test_scratch_is_given_back_and_shared():
+    """A layer holds one scratch however its calls grow, captured ones aside; layers may share one."""
+    d, H, batch, t_cap = 512, 4, 2, 600
+    lens, W = torch.tensor([500, 77], dtype=torch.int32, device=DEV), np.eye(d)
+    par = lambda n: torch.arange(-1, n - 1, dtype=torch.int32, device=DEV).repeat(batch, 1)
+    rnd = lambda n: torch.randn(batch, n, d, device=DEV).bfloat16()
+    lay = SlimLayer(d, H, d // H, 1.0e4, "bf16", batch, t_cap, DEV)
+    other = None
+    try:
+        lay.set_wkv(W)
+        lay.k.normal_()
+        most = max(B.slim_tree_workspace_bytes(lay.ctx, batch, t_cap, n) for n in range(1, 65))
+        q, kt, o = rnd(64), rnd(64), torch.empty(batch, 64, d, dtype=torch.bfloat16, device=DEV)
+        torch.cuda.synchronize()
+        before = torch.cuda.memory_allocated()
+        for n in range(1, 65):
+            lay.tree_decode(q[:, :n].contiguous(), kt[:, :n].contiguous(), lens, par(n), o.view(-1)[:batch * n * d].view(batch, n, d))
+        held = torch.cuda.memory_allocated() - before
+        assert held <= most + (4 << 20), (held, most)
+        want = lay.tree_decode(q, kt, lens, par(64)).clone()
+        other = SlimLayer(d, H, d // H, 1.0e4, "bf16", batch, t_cap, DEV, scratch=lay.scratch)
+        other.set_wkv(W)
+        other.k.copy_(lay.k)
+        torch.cuda.synchronize()
+        before = torch.cuda.memory_allocated()
+        assert torch.equal(other.tree_decode(q, kt, lens, par(64), o), want)
+        assert torch.cuda.memory_allocated() == before
+        # sized ahead: a capture may be the first call
+        third = SlimLayer(d, H, d // H, 1.0e4, "bf16", batch, t_cap, DEV)
+        third.set_wkv(W)
+        third.k.copy_(lay.k)
+        third.reserve_scratch(64)
+        graph, o3 = torch.cuda.CUDAGraph(), torch.empty_like(o)
+        p64 = par(64)
+        with torch.cuda.graph(graph):
+            third.tree_decode(q, kt, lens, p64, o3)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(o3, want)
+        third.close()
+        for n in (-1, 65):
+            with pytest.raises(ValueError):
+                lay.reserve_scratch(n)
+        with pytest.raises(ValueError):
+            SlimLayer(d, H, d // H, 1.0e4, "bf16", batch, t_cap, DEV, scratch=torch.empty(5, device=DEV))
+    finally:
+        lay.close()
+        if other is not None:
+            other.close()
+
+
+def test_scratch_that_grows_on_another_stream():
+    """Calls on a stream that the scratch was not made on; when it grows there, the smaller one must not be handed to the
+    first stream while calls still use it."""
+    d, H, batch, t_cap = 1024, 8, 4, 4000
+    lay = SlimLayer(d, H, d // H, 1.0e4, "bf16", batch, t_cap, DEV)
+    try:
+        lay.set_wkv(np.eye(d))
+        lay.k.normal_()
+        lens = torch.full((batch,), 3900, dtype=torch.int32, device=DEV)
+        args = [[torch.randn(batch, n, d, device=DEV).bfloat16() for _ in range(2)] +
+                [lens, torch.arange(-1, n - 1, dtype=torch.int32, device=DEV).repeat(batch, 1)] for n in (8, 64)]
+        want = lay.tree_decode(*args[0]).clone()
+        size, side = lay._extra[-1].numel(), torch.cuda.Stream()
+        outs = [torch.empty_like(want) for _ in range(40)]
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            for o in outs:
+                lay.tree_decode(*args[0], o)
+            lay.tree_decode(*args[1])
+        junk = [torch.full((size,), 255, dtype=torch.uint8, device=DEV) for _ in range(3)]
+        torch.cuda.synchronize()
+        assert all(torch.equal(o, want) for o in outs) and len(junk) == 3
+        assert lay.device_status() == B.SLIM_OK
+    finally:
+        lay.close()
