@@ -9,13 +9,19 @@ import torch
 from . import binding as B
 
 
+def _device(device) -> torch.device:
+    """With its index: a bare "cuda" is the current device, as tensors name it."""
+    device = torch.device(device)
+    return torch.device("cuda", torch.cuda.current_device()) if device.type == "cuda" and device.index is None else device
+
+
 class Scratch:
     """Device memory of SlimLayer.tree_decode, accumulate_weights and evict.  Layers whose calls run one after another on a
     stream may share one.  It grows with the largest call so far; what it grew out of is given back, unless a graph has been
     captured on it."""
 
     def __init__(self, device):
-        self.device = torch.device(device)
+        self.device = _device(device)
         self.buffers = []        # the one in use last; before it those that captured graphs hold on to
         self.captured = False    # a graph uses the last one
         self.home = None         # the stream that it was allocated on
@@ -45,7 +51,7 @@ class SlimLayer:
                  device: str = "cuda:0", workspace: "torch.Tensor | None" = None, scratch: "Scratch | None" = None):
         if not torch.cuda.is_available():
             raise RuntimeError("SlimLayer needs a CUDA device (there is no CPU fallback)")
-        self.device = torch.device(device)
+        self.device = _device(device)
         if scratch is not None and (not isinstance(scratch, Scratch) or scratch.device != self.device):
             raise ValueError(f"scratch: a Scratch on {self.device} is needed, e.g. another layer's .scratch")
         self.d, self.H, self.d_k, self.batch, self.t_cap = d, H, d_k, batch, t_cap

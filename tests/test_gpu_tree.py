@@ -809,3 +809,19 @@ def test_scratch_that_grows_on_another_stream():
         assert lay.device_status() == B.SLIM_OK
     finally:
         lay.close()
+
+
+def test_a_layer_on_the_current_device():
+    """A device without an index is the current one."""
+    lay = SlimLayer(128, 2, 64, 1.0e4, "bf16", 1, 64, "cuda")
+    try:
+        lay.set_wkv(np.eye(128))
+        lay.k.normal_()
+        q, kt = (torch.randn(1, 4, 128, device=DEV).bfloat16() for _ in range(2))
+        i = lambda *x: torch.tensor(x, dtype=torch.int32, device=DEV)
+        o = lay.tree_decode(q, kt, i(50), i([-1, 0, 1, 1]))
+        assert torch.isfinite(o.float()).all() and lay.device_status() == B.SLIM_OK
+        acc = lay.accumulate_weights(q[:, 0].contiguous(), i(50), torch.zeros(1, 64, device=DEV))
+        assert abs(acc.sum().item() - 2) < 100 * 2.0 ** -23     # two heads, 50 rows: a hundred roundings
+    finally:
+        lay.close()
