@@ -161,6 +161,8 @@ class SlimLayer:
 
     def tree_commit(self, k_tree: torch.Tensor, lengths: torch.Tensor, path: torch.Tensor, count: torch.Tensor) -> None:
         """Accepted keys into the cache (binding.slim_tree_commit); the caller adds count to lengths after the last layer."""
+        if k_tree.dim() != 3:
+            raise ValueError("k_tree: [batch, n, d] is needed")
         n, i32 = k_tree.shape[1], torch.int32
         self._arg("k_tree", k_tree, (self.batch, n, self.d), self.tdtype)
         self._arg("lengths", lengths, (self.batch,), i32)

@@ -825,3 +825,17 @@ def test_a_layer_on_the_current_device():
         assert abs(acc.sum().item() - 2) < 100 * 2.0 ** -23     # two heads, 50 rows: a hundred roundings
     finally:
         lay.close()
+
+
+def test_commit_refuses_other_numbers_of_dimensions():
+    lay = SlimLayer(128, 2, 64, 1.0e4, "bf16", 1, 64, DEV)
+    try:
+        kt = torch.randn(1, 4, 128, device=DEV).bfloat16()
+        i = lambda *x: torch.tensor(x, dtype=torch.int32, device=DEV)
+        for bad in (kt[0], kt[0, 0], kt[None]):
+            with pytest.raises(ValueError):
+                lay.tree_commit(bad, i(50), i([0, 1, -1, -1]), i(2))
+        lay.tree_commit(kt, i(50), i([0, 1, -1, -1]), i(2))
+        assert lay.device_status() == B.SLIM_OK
+    finally:
+        lay.close()
