@@ -291,6 +291,9 @@ slim_status slim_combine_project(slim_ctx* ctx, const float* lse_all, const floa
  * that is not there (ragged trees in one batch).  depth(i) = number of proper ancestors.  A parent that is not an
  * earlier token, or is padding, raises SLIM_ERR_TREE on the device and the token is treated as padding.
  *
+ * The calls of this section and the next one take caches of at most 2^30 rows a sequence (SLIM_ERR_UNSUPPORTED; the sizes
+ * are 0 then).
+ *
  * slim_tree_decode  attention of every drafted token over the cached rows, its ancestors and itself.
  *   q, k_tree  device [batch][n][d], ctx dtype, 16-byte aligned: un-rotated queries and key rows of the
  *              drafted tokens; token i sits at position lengths[b] + depth(i)
@@ -349,7 +352,7 @@ slim_status slim_tree_commit(slim_ctx* ctx, slim_cache* cache, const void* k_tre
  *   cache that slim_decode takes.  workspace: device, >= slim_weights_workspace_bytes(ctx, batch, t_cap), 256-byte aligned.
  *
  * slim_evict  brings every sequence that is longer than `budget` rows down to it: the last `recent` rows stay
- *   (0 <= recent <= budget), and of the rows before them the budget - recent with the largest acc (equal values: the
+ *   (0 <= recent <= budget <= 2^30), and of the rows before them the budget - recent with the largest acc (equal values: the
  *   lower row; NaN counts as the lowest value).  The kept rows move, in order, to rows 0 .. budget-1, in place; their
  *   acc moves along and the acc of the rows that became free is cleared.  Keys are cached un-rotated, so a
  *   row that moved sits at its new position from then on.  The caller clamps lengths to the budget

@@ -710,6 +710,9 @@ slim_status slim_decode_static_ws(slim_ctx* ctx, const void* q, const slim_cache
 
 // ---- drafted tokens, cache budget ------------------------------------------------
 namespace {
+// Their kernels round row counts up and step past the last row in 32 bits, so a capacity or a budget is at most this.
+constexpr int kMaxRows = 1 << 30;
+
 bool current_device_is(const slim_ctx* ctx) {
   int dev = -1;
   if (cudaGetDevice(&dev) != cudaSuccess) { cudaGetLastError(); return false; }
@@ -753,7 +756,7 @@ WeightsLayout weights_layout(const slim_ctx* ctx, int batch, int t_cap) {
 }  // namespace
 
 size_t slim_tree_workspace_bytes(const slim_ctx* ctx, int batch, int t_cap, int n) {
-  if (!ctx || batch <= 0 || t_cap <= 0 || batch > SLIM_MAX_BATCH || n <= 0 || n > SLIM_MAX_TREE || ctx->e != ctx->d) return 0;
+  if (!ctx || batch <= 0 || t_cap <= 0 || t_cap > kMaxRows || batch > SLIM_MAX_BATCH || n <= 0 || n > SLIM_MAX_TREE || ctx->e != ctx->d) return 0;
   return slim_tree_ws_layout(ctx, batch, t_cap, n).total;
 }
 
@@ -762,7 +765,7 @@ slim_status slim_tree_decode(slim_ctx* ctx, const void* q, const void* k_tree, c
   if (!ctx || !q || !k_tree || !cache || !lengths || !parents || !o || !workspace || cache->ctx != ctx) return SLIM_ERR_INVALID_ARG;
   if (n <= 0 || n > SLIM_MAX_TREE || ((uintptr_t)workspace & 255)) return SLIM_ERR_INVALID_ARG;
   if (((uintptr_t)q | (uintptr_t)k_tree | (uintptr_t)o) & 15) return SLIM_ERR_INVALID_ARG;
-  if (ctx->kdtype == SLIM_FP8 || ctx->e != ctx->d) return SLIM_ERR_UNSUPPORTED;
+  if (ctx->kdtype == SLIM_FP8 || ctx->e != ctx->d || cache->t_cap > kMaxRows) return SLIM_ERR_UNSUPPORTED;
   if (!ctx->has_weights) return SLIM_ERR_NO_WEIGHTS;
   if (!current_device_is(ctx)) return SLIM_ERR_INVALID_ARG;
   const int tc = ctx->path_req != SLIM_PATH_GENERIC && slim_tree_tc_ok(ctx);
@@ -783,13 +786,13 @@ slim_status slim_tree_commit(slim_ctx* ctx, slim_cache* cache, const void* k_tre
                              const int32_t* count, int n, void* stream) {
   if (!ctx || !cache || !k_tree || !lengths || !path || !count || cache->ctx != ctx) return SLIM_ERR_INVALID_ARG;
   if (n <= 0 || n > SLIM_MAX_TREE || ((uintptr_t)k_tree & 15)) return SLIM_ERR_INVALID_ARG;
-  if (ctx->kdtype == SLIM_FP8 || ctx->e != ctx->d) return SLIM_ERR_UNSUPPORTED;
+  if (ctx->kdtype == SLIM_FP8 || ctx->e != ctx->d || cache->t_cap > kMaxRows) return SLIM_ERR_UNSUPPORTED;
   if (!current_device_is(ctx)) return SLIM_ERR_INVALID_ARG;
   return launched(slim_launch_commit(ctx, cache, k_tree, lengths, path, count, n, (cudaStream_t)stream));
 }
 
 size_t slim_weights_workspace_bytes(const slim_ctx* ctx, int batch, int t_cap) {
-  if (!ctx || batch <= 0 || t_cap <= 0 || batch > SLIM_MAX_BATCH || ctx->e != ctx->d) return 0;
+  if (!ctx || batch <= 0 || t_cap <= 0 || t_cap > kMaxRows || batch > SLIM_MAX_BATCH || ctx->e != ctx->d) return 0;
   return weights_layout(ctx, batch, t_cap).total;
 }
 
@@ -797,7 +800,7 @@ slim_status slim_accumulate_weights(slim_ctx* ctx, const void* q, const slim_cac
                                     void* workspace, void* stream) {
   if (!ctx || !q || !cache || !lengths || !acc || !workspace || cache->ctx != ctx) return SLIM_ERR_INVALID_ARG;
   if (((uintptr_t)workspace & 255) || ((uintptr_t)q & 15) || ((uintptr_t)acc & 3)) return SLIM_ERR_INVALID_ARG;
-  if (ctx->e != ctx->d) return SLIM_ERR_UNSUPPORTED;
+  if (ctx->e != ctx->d || cache->t_cap > kMaxRows) return SLIM_ERR_UNSUPPORTED;
   if (!current_device_is(ctx)) return SLIM_ERR_INVALID_ARG;
   const WeightsLayout L = weights_layout(ctx, cache->batch, cache->t_cap);
   char* ws = static_cast<char*>(workspace);
@@ -806,15 +809,16 @@ slim_status slim_accumulate_weights(slim_ctx* ctx, const void* q, const slim_cac
 }
 
 size_t slim_evict_workspace_bytes(const slim_ctx* ctx, int batch, int t_cap) {
-  if (!ctx || batch <= 0 || t_cap <= 0 || batch > SLIM_MAX_BATCH) return 0;
+  if (!ctx || batch <= 0 || t_cap <= 0 || t_cap > kMaxRows || batch > SLIM_MAX_BATCH) return 0;
   return align256(sizeof(float) * (size_t)batch * t_cap);              // the kept rows' weights, on their way
 }
 
 slim_status slim_evict(slim_ctx* ctx, slim_cache* cache, const int32_t* lengths, float* acc, int budget, int recent, int32_t* kept,
                        void* workspace, void* stream) {
   if (!ctx || !cache || !lengths || !acc || !kept || !workspace || cache->ctx != ctx) return SLIM_ERR_INVALID_ARG;
-  if (budget <= 0 || recent < 0 || recent > budget || ((uintptr_t)workspace & 255) || (((uintptr_t)acc | (uintptr_t)kept) & 3))
+  if (budget <= 0 || budget > kMaxRows || recent < 0 || recent > budget || ((uintptr_t)workspace & 255) || (((uintptr_t)acc | (uintptr_t)kept) & 3))
     return SLIM_ERR_INVALID_ARG;
+  if (cache->t_cap > kMaxRows) return SLIM_ERR_UNSUPPORTED;
   if (!current_device_is(ctx)) return SLIM_ERR_INVALID_ARG;
   return launched(slim_launch_evict(ctx, cache, lengths, acc, budget, recent, kept, static_cast<float*>(workspace), (cudaStream_t)stream));
 }

@@ -318,3 +318,31 @@ def test_a_weight_that_is_no_number_reaches_its_whole_sequence(d, H, dtype):
         assert acc[3, :300].isnan().all() and (acc[3, 300:] == 1).all()
     finally:
         lay.close()
+
+
+def test_sizes_next_to_two_to_the_31_are_refused():
+    """Row counts are walked in 32-bit steps: capacities and budgets above 2^30 are refused by the calls that would."""
+    c = B.slim_create(2, 1, 2, 0.0, B.SLIM_F32)
+    try:
+        for t_cap in ((1 << 30) + 1, (1 << 31) - 1):
+            assert B.slim_tree_workspace_bytes(c, 1, t_cap, 1) == 0
+            assert B.slim_weights_workspace_bytes(c, 1, t_cap) == 0
+            assert B.slim_evict_workspace_bytes(c, 1, t_cap) == 0
+        assert B.slim_evict_workspace_bytes(c, 1, 1 << 30) > 0
+        k, x, i = torch.zeros(64, 2, device=DEV), torch.zeros(64, device=DEV), torch.zeros(64, dtype=torch.int32, device=DEV)
+        cache = B.slim_cache_create(c, k, 1, 64)
+        ws = torch.empty(1 << 16, dtype=torch.uint8, device=DEV)
+        with pytest.raises(B.SlimError) as e:
+            B.slim_evict(c, cache, i, x, (1 << 30) + 1, 0, i, ws)
+        assert e.value.status == B.SLIM_ERR_INVALID_ARG
+        B.slim_cache_destroy(cache)
+        B.slim_set_wkv(c, np.eye(2))
+        far = B.slim_cache_create(c, k, 1, (1 << 30) + 1)   # (only the address is taken here; every call on it is refused)
+        for call in (lambda: B.slim_tree_decode(c, x, x, far, i, i, 1, x, ws), lambda: B.slim_tree_commit(c, far, x, i, i, i, 1),
+                     lambda: B.slim_accumulate_weights(c, x, far, i, x, ws), lambda: B.slim_evict(c, far, i, x, 4, 0, i, ws)):
+            with pytest.raises(B.SlimError) as e:
+                call()
+            assert e.value.status == B.SLIM_ERR_UNSUPPORTED
+        B.slim_cache_destroy(far)
+    finally:
+        B.slim_destroy(c)
