@@ -80,9 +80,14 @@ slim_status grow_rope_base(slim_ctx* ctx, long long rows) {
     cudaFree(dev);
     return SLIM_ERR_CUDA;
   }
-  // the old table may still be referenced by enqueued work
-  cudaDeviceSynchronize();
-  cudaFree(ctx->rope_base);
+  // the old table stays until the context goes: enqueued work may refer to it, and captured graphs do
+  if (ctx->rope_base) {
+    slim_old_table* old = new (std::nothrow) slim_old_table();
+    if (!old) { cudaFree(dev); return SLIM_ERR_OOM; }
+    old->dev = ctx->rope_base;
+    old->next = ctx->rope_old;
+    ctx->rope_old = old;
+  }
   ctx->rope_base = dev;
   ctx->rope_base_tiles = tiles;
   return SLIM_OK;
@@ -253,6 +258,12 @@ void slim_destroy(slim_ctx* ctx) {
   cudaFree(ctx->wkv_hscale);
   cudaFree(ctx->rope_off);
   cudaFree(ctx->rope_base);
+  for (slim_old_table* t = ctx->rope_old; t;) {
+    slim_old_table* next = t->next;
+    cudaFree(t->dev);
+    delete t;
+    t = next;
+  }
   cudaFree(ctx->rope_frag);
   cudaFree(ctx->status);
   cudaFree(ctx->any_flag);
@@ -616,7 +627,7 @@ slim_status slim_decode_step(slim_ctx* ctx, const void* q, const void* k_new, sl
 
 slim_status slim_reserve_positions(slim_ctx* ctx, int max_position) {
   if (!ctx || max_position <= 0) return SLIM_ERR_INVALID_ARG;
-  return grow_rope_base(ctx, max_position);
+  return grow_rope_base(ctx, (long long)max_position + SLIM_MAX_TREE);      // (as a cache of that many rows does)
 }
 
 slim_status slim_decode_partial(slim_ctx* ctx, const void* q, const slim_cache* cache, const int32_t* lengths,

@@ -58,6 +58,9 @@ struct SlimDecodeParams {
   int redo_in_combine;           // 1: the combine kernel recomputes the sequences that have a flagged unit (no redo kernel runs)
 };
 
+// A position table that has been replaced by a longer one.
+struct slim_old_table { float2* dev; slim_old_table* next; };
+
 struct slim_ctx {
   int d, H, d_k, dtype;          // d: width of a cache row; dtype: q and W_KV (f32 or bf16)
   int e;                         // width of q and o: H * d_k; differs from d only for an X-cache context with non-square projections
@@ -73,6 +76,7 @@ struct slim_ctx {
   float* wkv_hscale;             // device [H]: 2^-a_h
   float2* rope_off;              // device [TT][half]
   float2* rope_base;             // device table, grown by slim_cache_create
+  slim_old_table* rope_old;      // shorter ones that captured graphs may refer to
   void* rope_frag;               // tensor-core tree attention: (cos, sin) of offsets 0 .. 127 in lane order (slim_tree_tc.cu)
   int rope_base_tiles;
   int* status;                   // device status word

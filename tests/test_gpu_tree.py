@@ -839,3 +839,25 @@ def test_commit_refuses_other_numbers_of_dimensions():
         assert lay.device_status() == B.SLIM_OK
     finally:
         lay.close()
+
+
+def test_a_graph_outlives_longer_position_tables():
+    """A larger cache of the context, or more reserved positions, make longer position tables; a graph captured before goes on
+    with those that it was captured with."""
+    with Case(512, 4, 1.0e4, "bf16", [900, 130], [[-1, 0, 1, 0]] * 2, seed=2) as c:
+        c.call()
+        torch.cuda.synchronize()
+        want = c.o.clone()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            c.call()
+        for rows in (5000, 100_000, 1_000_000):
+            B.slim_reserve_positions(c.ctx, rows)
+            other = [torch.full((1 << 20,), 255, dtype=torch.uint8, device=DEV) for _ in range(32)]
+            c.o.zero_()
+            graph.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(c.o, want) and all(bool((x == 255).all()) for x in other)
+        c.o.zero_()
+        c.call()
+        assert c.status() == B.SLIM_OK and torch.equal(c.o, want)
