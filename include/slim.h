@@ -331,7 +331,8 @@ slim_status slim_combine_project(slim_ctx* ctx, const float* lse_all, const floa
  * slim_tree_commit  k_tree[b][path[b][j]] -> cache row lengths[b] + j for j < count[b] (path, count as
  *   slim_tree_verify leaves them, or any indices into the tree; count 0 writes nothing).  f32 and bf16 caches,
  *   contiguous or paged.  The caller adds count to lengths after the last layer.  A sequence whose rows would pass
- *   t_cap (SLIM_ERR_CAPACITY) or whose path leaves the tree (SLIM_ERR_TREE) is left unwritten.          */
+ *   t_cap (SLIM_ERR_CAPACITY) or whose path leaves the tree (SLIM_ERR_TREE) is left unwritten.  Pages are written in
+ *   place: one that two sequences of a block table share (a common prefix) must lie wholly below the row where each writes. */
 #define SLIM_MAX_TREE 64
 size_t      slim_tree_workspace_bytes(const slim_ctx* ctx, int batch, int t_cap, int n);
 slim_status slim_tree_decode(slim_ctx* ctx, const void* q, const void* k_tree, const slim_cache* cache, const int32_t* lengths,
@@ -357,7 +358,8 @@ slim_status slim_tree_commit(slim_ctx* ctx, slim_cache* cache, const void* k_tre
  *   acc moves along and the acc of the rows that became free is cleared.  Keys are cached un-rotated, so a
  *   row that moved sits at its new position from then on.  The caller clamps lengths to the budget
  *   after the last layer.  Shorter sequences stay as they are.  Any cache of the library (a paged one
- *   keeps its block table; the pages behind the budget are free to be given back).
+ *   keeps its block table; the pages behind the budget are free to be given back).  Rows move in place: a sequence that
+ *   is brought down must not share a page with another one, whose rows would change with it.
  *   kept       device int32 [batch][budget], written: the old row of every new row, -1 behind a shorter sequence
  *   workspace  device, >= slim_evict_workspace_bytes(ctx, batch, t_cap), 256-byte aligned          */
 size_t      slim_weights_workspace_bytes(const slim_ctx* ctx, int batch, int t_cap);

@@ -861,3 +861,63 @@ def test_a_graph_outlives_longer_position_tables():
         c.o.zero_()
         c.call()
         assert c.status() == B.SLIM_OK and torch.equal(c.o, want)
+
+
+def attention_in_64_bits(c, b):
+    """(o, mass, arg) of oracle.draft_oracle.tree_attention for sequence b, by plain torch operations on the device."""
+    n, d, H, L = c.n, c.d, c.H, len(c.K[b])
+    d_k, half = d // H, d // H // 2
+    chains = do.tree_chains(list(c.parents[b]))
+    see = torch.zeros(n, L + n, dtype=torch.bool, device=DEV)
+    depth = torch.zeros(n, dtype=torch.float64, device=DEV)
+    for i, chain in enumerate(chains):
+        if chain:
+            see[i, :L] = True
+            see[i, [L + j for j in chain]] = True
+            depth[i] = len(chain) - 1
+    rows = torch.cat([to_dev(c.K[b], c.dtype), to_dev(np.nan_to_num(c.kt[b]), c.dtype)]).double()
+    q = to_dev(np.nan_to_num(c.q[b]), c.dtype).double()
+    W = torch.from_numpy(c.W).to(DEV)
+    pos = torch.cat([torch.arange(L, device=DEV, dtype=torch.float64), L + depth])
+    freq = c.theta ** (-torch.arange(half, dtype=torch.float64, device=DEV) / half) if c.theta else torch.zeros(half, dtype=torch.float64, device=DEV)
+
+    def turned(x, at):
+        a = at[:, None] * freq
+        x1, x2 = x[:, :half], x[:, half:]
+        return torch.cat([x1 * a.cos() + x2 * a.sin(), x2 * a.cos() - x1 * a.sin()], 1)
+
+    o, mass = (torch.zeros(n, d, dtype=torch.float64, device=DEV) for _ in range(2))
+    arg = torch.zeros(n, dtype=torch.float64, device=DEV)
+    for h in range(H):
+        cols = slice(h * d_k, (h + 1) * d_k)
+        qh, kh = turned(q[:, cols], L + depth), turned(rows[:, cols], pos)
+        p = torch.softmax((qh @ kh.T / d_k ** 0.5).masked_fill(~see, -torch.inf), 1).nan_to_num()
+        o[:, cols] = (p @ rows) @ W[:, cols]
+        mass[:, cols] = (p @ rows.abs()) @ W[:, cols].abs()
+        arg = torch.maximum(arg, (qh.abs() @ kh.abs().T / d_k ** 0.5).masked_fill(~see, 0).amax(1))
+    return o.cpu().numpy(), mass.cpu().numpy(), arg.cpu().numpy()
+
+
+@pytest.mark.parametrize("d,H,n,lengths,page", [
+    (512, 8, 32, [200_003], 0),                              # the keys of every tile in parts, each taken as a whole by a pair
+    (1024, 8, 64, [120_017], 0),                             # ... and two accumulators, a rest that is cut once more
+    (1024, 16, 40, [70_001, 30_000], 64),                    # ragged, paged: all of it cut where the pairs' shares end
+    (4096, 32, 17, [3000, 64, 0, 1], 0), (1280, 20, 64, [700, 2047], 16)])
+def test_long_contexts_and_wide_models_on_the_tensor_cores(d, H, n, lengths, page):
+    g = np.random.default_rng(n + d)
+    with Case(d, H, 1.0e4, "bf16", lengths, [random_parents(g, n) for _ in lengths], page, seed=n) as c:
+        c.call()
+        assert c.status() == B.SLIM_OK
+        got = c.o.float().cpu().numpy().astype(np.float64)
+        for b in range(c.batch):
+            o, mass, arg = attention_in_64_bits(c, b)
+            tol = tolerance(o, mass, arg, len(c.K[b]) + n, d, d // H, "bf16", True)
+            err = np.abs(got[b] - o)
+            assert np.all(err <= tol), f"sequence {b}: {np.max(err / tol):.2f} of the bound"
+            # In norm: the keys are random and know nothing of the roundings, so a weight's relative error moves the sum by no
+            # more than its size.  P's half step 2^-8 and the output's, 2^-8; the arguments' (2 x 2^-11 of each of d_k products
+            # of random signs, whose sum has variance 1) are a tenth of that, and half steps are half as large on average
+            assert np.linalg.norm(err) <= 2.0 ** -7 * np.linalg.norm(o)
+            for i, chain in enumerate(do.tree_chains(list(c.parents[b]))):
+                if not chain:
+                    assert np.all(got[b, i] == 0)
