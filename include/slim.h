@@ -297,7 +297,8 @@ slim_status slim_combine_project(slim_ctx* ctx, const float* lse_all, const floa
  * slim_tree_decode  attention of every drafted token over the cached rows, its ancestors and itself.
  *   q, k_tree  device [batch][n][d], ctx dtype, 16-byte aligned: un-rotated queries and key rows of the
  *              drafted tokens; token i sits at position lengths[b] + depth(i)
- *   cache      contiguous or paged (not SLIM_FP8); it is read only: drafted keys enter it by slim_tree_commit
+ *   cache      contiguous or paged keys (not SLIM_FP8, not an X-cache: SLIM_ERR_UNSUPPORTED); it is read only: drafted keys
+ *              enter it by slim_tree_commit
  *   lengths    device int32 [batch]: cached rows of sequence b (0: the tokens attend the tree only); above t_cap:
  *              clamped and reported as SLIM_ERR_CAPACITY.  Rows behind them may hold anything; a number that is not finite
  *              in a cached row, or in the key of a token that is there, reaches every token of its sequence
@@ -350,7 +351,8 @@ slim_status slim_tree_commit(slim_ctx* ctx, slim_cache* cache, const void* k_tre
  * slim_accumulate_weights  acc[b][t] += sum_h softmax_t(q_h . K_h / sqrt(d_k)), t < lengths[b], for the query of
  *   slim_decode (un-rotated, at position lengths[b]-1; same arguments).  acc: device float32 [batch][t_cap],
  *   other elements are left alone.  A NaN in an attended row or in the query makes every acc of its sequence NaN.  Any
- *   cache that slim_decode takes.  workspace: device, >= slim_weights_workspace_bytes(ctx, batch, t_cap), 256-byte aligned.
+ *   cache of keys that slim_decode takes.  workspace: device, >= slim_weights_workspace_bytes(ctx, batch, t_cap), 256-byte
+ *   aligned.
  *
  * slim_evict  brings every sequence that is longer than `budget` rows down to it: the last `recent` rows stay
  *   (0 <= recent <= budget <= 2^30), and of the rows before them the budget - recent with the largest acc (equal values: the

@@ -776,7 +776,7 @@ slim_status slim_tree_decode(slim_ctx* ctx, const void* q, const void* k_tree, c
   if (!ctx || !q || !k_tree || !cache || !lengths || !parents || !o || !workspace || cache->ctx != ctx) return SLIM_ERR_INVALID_ARG;
   if (n <= 0 || n > SLIM_MAX_TREE || ((uintptr_t)workspace & 255)) return SLIM_ERR_INVALID_ARG;
   if (((uintptr_t)q | (uintptr_t)k_tree | (uintptr_t)o) & 15) return SLIM_ERR_INVALID_ARG;
-  if (ctx->kdtype == SLIM_FP8 || ctx->e != ctx->d || cache->t_cap > kMaxRows) return SLIM_ERR_UNSUPPORTED;
+  if (ctx->kdtype == SLIM_FP8 || ctx->e != ctx->d || ctx->xc_wk || cache->t_cap > kMaxRows) return SLIM_ERR_UNSUPPORTED;     // (xc_wk: the rows are X, not keys)
   if (!ctx->has_weights) return SLIM_ERR_NO_WEIGHTS;
   if (!current_device_is(ctx)) return SLIM_ERR_INVALID_ARG;
   const int tc = ctx->path_req != SLIM_PATH_GENERIC && slim_tree_tc_ok(ctx);
@@ -811,7 +811,7 @@ slim_status slim_accumulate_weights(slim_ctx* ctx, const void* q, const slim_cac
                                     void* workspace, void* stream) {
   if (!ctx || !q || !cache || !lengths || !acc || !workspace || cache->ctx != ctx) return SLIM_ERR_INVALID_ARG;
   if (((uintptr_t)workspace & 255) || ((uintptr_t)q & 15) || ((uintptr_t)acc & 3)) return SLIM_ERR_INVALID_ARG;
-  if (ctx->e != ctx->d || cache->t_cap > kMaxRows) return SLIM_ERR_UNSUPPORTED;
+  if (ctx->e != ctx->d || ctx->xc_wk || cache->t_cap > kMaxRows) return SLIM_ERR_UNSUPPORTED;
   if (!current_device_is(ctx)) return SLIM_ERR_INVALID_ARG;
   const WeightsLayout L = weights_layout(ctx, cache->batch, cache->t_cap);
   char* ws = static_cast<char*>(workspace);

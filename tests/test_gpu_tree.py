@@ -921,3 +921,26 @@ def test_long_contexts_and_wide_models_on_the_tensor_cores(d, H, n, lengths, pag
             for i, chain in enumerate(do.tree_chains(list(c.parents[b]))):
                 if not chain:
                     assert np.all(got[b, i] == 0)
+
+
+@pytest.mark.parametrize("dtype", [B.SLIM_F32, B.SLIM_BF16])
+def test_a_cache_of_x_rows_is_refused(dtype):
+    """An X-cache with square projections: its rows are no keys, so products of the query with them are no scores."""
+    d, H, td = 128, 2, torch.float32 if dtype == B.SLIM_F32 else torch.bfloat16
+    c = B.slim_xcache_create(d, H, 64, dtype)
+    try:
+        g = np.random.default_rng(0)
+        B.slim_xcache_set_weights(c, g.standard_normal((d, d)), g.standard_normal((d, d)))
+        store, x = torch.zeros(1, 32, d, dtype=td, device=DEV), torch.zeros(1, 2, d, dtype=td, device=DEV)
+        cache = B.slim_cache_create(c, store, 1, 32)
+        i = lambda *v: torch.tensor(v, dtype=torch.int32, device=DEV)
+        need = max(B.slim_tree_workspace_bytes(c, 1, 32, 2), B.slim_weights_workspace_bytes(c, 1, 32))
+        ws, acc = torch.empty(need, dtype=torch.uint8, device=DEV), torch.zeros(1, 32, device=DEV)
+        for call in (lambda: B.slim_tree_decode(c, x, x, cache, i(9), i([-1, 0]), 2, torch.empty_like(x), ws),
+                     lambda: B.slim_accumulate_weights(c, x, cache, i(9), acc, ws)):
+            with pytest.raises(B.SlimError) as e:
+                call()
+            assert e.value.status == B.SLIM_ERR_UNSUPPORTED
+        B.slim_cache_destroy(cache)
+    finally:
+        B.slim_destroy(c)
