@@ -71,6 +71,7 @@ slim_weights_scores_kernel(const SlimDecodeParams p, float* __restrict__ scores,
   if (tid >= WC) {
     // ---- producer ----
     if (tid == WC) {
+      fence_proxy_async_global();                                  // (the keys may be an earlier kernel's ordinary stores)
       const unsigned char* Kc = reinterpret_cast<const unsigned char*>(p.k);
       int st = 0;
       uint32_t ph = 1;                                             // parity of a stage's "empty" that means free

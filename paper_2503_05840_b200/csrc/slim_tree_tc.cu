@@ -172,6 +172,7 @@ slim_tree_p_kernel(const __grid_constant__ CUtensorMap cmap, const __grid_consta
   __syncthreads();                                                        // (the abort flag is read from here on)
   slim_pdl_trigger();
   slim_pdl_wait();
+  if (lane == 0) fence_proxy_async_global();                              // (keys and drafts may be an earlier kernel's ordinary stores)
   const int nb_cap = (p.t_cap + SC_KEYS - 1) / SC_KEYS;
   // this CTA's share of the line of blocks, and where it begins; the same in every warp
   int b = 0, h = 0, k0 = 0, remaining;

@@ -944,3 +944,39 @@ def test_a_cache_of_x_rows_is_refused(dtype):
         B.slim_cache_destroy(cache)
     finally:
         B.slim_destroy(c)
+
+
+@pytest.mark.parametrize("page", [0, 16])
+def test_keys_of_the_kernel_before_are_read(page):
+    """Commit, weights, eviction and attention right behind one another, a hundred times on a stream without a pause: each
+    reads by bulk copies what the one before has just stored.  The same calls with a pause between them give the same."""
+    d, H, n, L0 = 512, 4, 16, 64
+    with Case(d, H, 1.0e4, "bf16", [L0] * 4, [[-1] * n] * 4, page, seed=3, t_cap=160) as c:
+        i = lambda v: torch.full((4,), v, dtype=torch.int32, device=DEV)
+        acc, kept = torch.zeros(4, c.t_cap, device=DEV), torch.empty(4, L0, dtype=torch.int32, device=DEV)
+        path = torch.arange(n, dtype=torch.int32, device=DEV).repeat(4, 1)
+        ws = torch.empty(B.slim_weights_workspace_bytes(c.ctx, 4, c.t_cap), dtype=torch.uint8, device=DEV)
+        ev = torch.empty(B.slim_evict_workspace_bytes(c.ctx, 4, c.t_cap), dtype=torch.uint8, device=DEV)
+        lens0, lens1, counts = i(L0), i(L0 + n), i(n)
+        torch.manual_seed(5)
+        drafts, q1 = torch.randn(100, 4, n, d, device=DEV).bfloat16(), torch.randn(4, d, device=DEV).bfloat16()
+        start, st = c.store.clone(), torch.cuda.current_stream().cuda_stream
+
+        def loop(pause):
+            c.store.copy_(start)
+            acc.zero_()
+            outs = torch.empty(100, 4, n, d, dtype=torch.bfloat16, device=DEV)
+            torch.cuda.synchronize()
+            for k in range(100):
+                for call in (lambda: B.slim_tree_commit(c.ctx, c.cache, drafts[k], lens0, path, counts, n, st),
+                             lambda: B.slim_accumulate_weights(c.ctx, q1, c.cache, lens1, acc, ws, st),
+                             lambda: B.slim_evict(c.ctx, c.cache, lens1, acc, L0, 8, kept, ev, st),
+                             lambda: B.slim_tree_decode(c.ctx, c.dq, drafts[k], c.cache, lens0, c.dpar, n, outs[k], c.ws, st)):
+                    call()
+                    if pause:
+                        torch.cuda.synchronize()
+            assert c.status() == B.SLIM_OK
+            return outs, acc.clone(), kept.clone(), c.store.clone().nan_to_num(7.0)
+
+        for x, y in zip(loop(True), loop(False)):
+            assert torch.equal(x, y)
