@@ -9,6 +9,7 @@
 //   sum         U = P K / l on tcgen05, CTA pairs (cta_group::2), bf16
 //   join        adds the parts of tiles whose keys were cut
 //   out         o = U W_KV,h on tcgen05
+#include <cfloat>
 #include <cmath>
 #include <cstdlib>
 
@@ -40,13 +41,12 @@ __device__ __forceinline__ float2 turn(const SlimDecodeParams& p, int pos, int j
 //     their positions once, are turned back by the block's angle, 64 complex factors a block.
 //   - float16 keeps 11 bits of the rotated values (bf16's 8 would cost as much accuracy as the rounding of P does, for a
 //     product that is 1 / H of the step's) at twice tf32's rate.  Its range: queries are scaled by a power of two per
-//     token; keys go in as they are (those that are not attended as zeros), and a warp whose sums overflow, or whose queries
-//     are so large that the smallest float16 steps of a key would show, repeats its tile with every key scaled by a power of
-//     two of its own.
+//     token; keys go in as they are, and a warp whose sums overflow (those of attended keys), or whose queries are so large
+//     that the smallest float16 steps of a key would show, repeats its tile with every key scaled by a power of two of its own.
 //   - P is written relative to a reference that is a multiple of 64, kept from block to block while the arguments
-//     stay below reference + 60: nearly always the same for all blocks of a row, so that the blocks need no common
-//     maximum; `finish` shifts the exponents of the others, exactly.  Sums l are taken from the rounded P, so the weights
-//     of a row add up to one.
+//     stay below reference + 60 (the reference itself beside keys so large that P K could overflow): nearly always the
+//     same for all blocks of a row, so that the blocks need no common maximum; `finish` shifts the exponents of the others,
+//     exactly.  Sums l are taken from the rounded P, so the weights of a row add up to one.
 // Bound by the instructions and shared-memory reads around a score (rotation, conversion, exponent, store), not by the
 // keys' bytes, d = 4096, d_k = 128: 16 ragged sequences, 196 k rows, 16 drafts 0.41 ms (3.9 TB/s of keys); 131001 rows, 64
 // drafts 0.56 ms; 8 x 12000 rows with 1, 8, 16, 32, 64 drafts 0.16, 0.17, 0.20, 0.28, 0.43 ms (4.9 TB/s at one draft).
@@ -361,21 +361,12 @@ slim_tree_p_kernel(const __grid_constant__ CUtensorMap cmap, const __grid_consta
       const uint2* qb = qf + (it & 1) * NT * S::PER;
       mbar_wait<false>(bar + 8 * ((base + it) % S::KS), ((base + it) / S::KS) & 1, s_abort, p.status);      // (gave up: reported, and the loop runs on to its end)
       float s[NT][4];
-      bool whole = false;                                                   // s are arguments, without a factor left out
-      const bool edge = draft || t0 + 16 > len;                             // rows of the tile may not be attended
-      auto attended = [&](int r) { return draft ? r < n && s_dep[min(r, n - 1)] >= 0 : r < len; };
-      if (edge) {
-        // rows behind the sequence's last, padding and the next sequence's rows may hold anything: they are cleared (a
-        // thread's own elements) before they can meet the overflow test or the scaling
-#pragma unroll 1
-        for (int rh = 0; rh < 2; ++rh)
-          if (!attended(t0 + key0 + 2 * rh)) {
-#pragma unroll 1
-            for (int e = 0; e < 2 * NPC; ++e) *reinterpret_cast<kvec*>(tile + tile_off<DK>(key0 + 2 * rh, c, e >> 1, e & 1)) = kvec{};
-          }
-        fence_proxy_async_smem();                                           // (the next tile comes by the async proxy)
-      }
-      for (float back0 = 1.f, back1 = 1.f;;) {                              // what undoes the scaling of keys key0, key0 + 2
+      float back = 1.f;                                                     // undoes the keys' scaling, but for the keys' own parts
+      // Rows behind the sequence's last, padding and the next sequence's rows may hold anything; they must meet neither the
+      // overflow test nor the scaling of others
+      const bool edge = draft || t0 + 16 > len;
+      auto attended = [&](int r) { return !edge || (draft ? r < n && s_dep[min(r, n - 1)] >= 0 : r < len); };
+      for (int own2 = 0;;) {                                                // what is left of it for keys key0, key0 + 2: two exponents, above 0
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) s[nt][0] = s[nt][1] = s[nt][2] = s[nt][3] = 0.f;
 #pragma unroll
@@ -407,21 +398,28 @@ slim_tree_p_kernel(const __grid_constant__ CUtensorMap cmap, const __grid_consta
             }
           }
         }
-        // an overflow shows as an infinity or a NaN, and 0 x it is a NaN
-        if (whole) {
+        if (own2) {
+          const float f0 = ldexpf(1.f, (own2 & 0xffff) - 512), f1 = ldexpf(1.f, (own2 >> 16) - 512);
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-            for (int x = 0; x < 4; ++x) s[nt][x] *= sr[8 * nt + 2 * c + (x & 1)].x * (x < 2 ? back0 : back1);
+            for (int x = 0; x < 4; ++x) s[nt][x] *= x < 2 ? f0 : f1;
           break;
         }
+        if (edge)
+#pragma unroll
+          for (int rh = 0; rh < 2; ++rh)
+            if (!attended(t0 + key0 + 2 * rh))
+#pragma unroll
+              for (int nt = 0; nt < NT; ++nt) s[nt][2 * rh] = s[nt][2 * rh + 1] = 0.f;
+        // an overflow shows as an infinity or a NaN, and 0 x it is a NaN
         float odd = 0.f;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
           for (int x = 0; x < 4; ++x) odd = fmaf(s[nt][x], 0.f, odd);
         if (!__any_sync(0xffffffffu, careful || odd != 0.f)) break;
-        whole = true;
+        int most = -127, least = 127, all = -127;                           // exponents: the tokens' factors, the keys'
         // every key by its own largest element (its four lanes have it in common), so that none wipes out another; in place
 #pragma unroll 1                                                            // (rare: no registers for it)
         for (int rh = 0; rh < 2; ++rh) {
@@ -436,7 +434,9 @@ slim_tree_p_kernel(const __grid_constant__ CUtensorMap cmap, const __grid_consta
           top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
           top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
           const float ks = pow2_to(top, 10);
-          if (rh == 0) back0 = 1.f / ks; else back1 = 1.f / ks;
+          const int e_back = 127 - (__float_as_int(ks) >> 23);
+          own2 |= (e_back + 512) << (16 * rh);
+          if (attended(t0 + key0 + 2 * rh)) all = max(all, e_back);
 #pragma unroll 1
           for (int e = 0; e < 2 * NPC; ++e) {
             kvec* at = reinterpret_cast<kvec*>(tile + tile_off<DK>(key0 + 2 * rh, c, e >> 1, e & 1));
@@ -447,6 +447,16 @@ slim_tree_p_kernel(const __grid_constant__ CUtensorMap cmap, const __grid_consta
             *at = v;
           }
         }
+        // one factor for the warp, so that no token's factor times it overflows or vanishes: a sum far below the largest then
+        // loses at most 2^-149 2^126 of its argument
+        for (int i = lane; i < TOK; i += 32) {
+          const int e = (__float_as_int(sr[i].x) >> 23) - 127;
+          most = max(most, e); least = min(least, e);
+        }
+        most = __reduce_max_sync(0xffffffffu, most); least = __reduce_min_sync(0xffffffffu, least);
+        all = min(max(__reduce_max_sync(0xffffffffu, all), -126 - least), 126 - most);
+        back = __int_as_float((all + 127) << 23);
+        own2 -= all * 0x10001;
         fence_proxy_async_smem();                                           // (the next tile comes by the async proxy)
       }
       __syncwarp();                                                         // all lanes have read the tile
@@ -463,15 +473,17 @@ slim_tree_p_kernel(const __grid_constant__ CUtensorMap cmap, const __grid_consta
           }
       }
       // ---- arguments relative to the references; does one have to move?  (always in the first block: -inf)
+      // P may reach 2^60, but only 1 beside keys that were scaled down (above 2^10, that is): P K must not overflow
+      const float room = back > 1.f ? 0.f : 60.f;
       bool moves = false;
       float y[NT][4];
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
         const float4 v = *reinterpret_cast<const float4*>(sr + 8 * nt + 2 * c);
-        const float s0 = whole ? 1.f : v.x, s1 = whole ? 1.f : v.z;
+        const float s0 = v.x * back, s1 = v.z * back;
         y[nt][0] = fmaf(s[nt][0], s0, -v.y); y[nt][1] = fmaf(s[nt][1], s1, -v.w);
         y[nt][2] = fmaf(s[nt][2], s0, -v.y); y[nt][3] = fmaf(s[nt][3], s1, -v.w);
-        moves = moves || fmaxf(fmaxf(y[nt][0], y[nt][1]), fmaxf(y[nt][2], y[nt][3])) > 60.f;
+        moves = moves || fmaxf(fmaxf(y[nt][0], y[nt][1]), fmaxf(y[nt][2], y[nt][3])) > room;
       }
       if (it + 1 < total) fragments(bc, (it + 1) & 1);
       if (it + 2 < total) bc = block_angle(it + 2);
@@ -482,7 +494,7 @@ slim_tree_p_kernel(const __grid_constant__ CUtensorMap cmap, const __grid_consta
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
           for (int z = 0; z < 2; ++z) {
-            float m = fmaxf(s[nt][z], s[nt][2 + z]) * (whole ? 1.f : sr[8 * nt + 2 * c + z].x);
+            float m = fmaf(fmaxf(s[nt][z], s[nt][2 + z]), sr[8 * nt + 2 * c + z].x * back, 60.f - room);
 #pragma unroll
             for (int o = 4; o < 32; o <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
             if (g == 0) atomicMax(smax + 8 * nt + 2 * c + z, ordered(m));
@@ -490,13 +502,13 @@ slim_tree_p_kernel(const __grid_constant__ CUtensorMap cmap, const __grid_consta
         group_sync(group);
         if (htid < TOK) {
           const float m = unordered(smax[htid]);                            // (of the blocks that came here)
-          if (m > sr[htid].y + 60.f) sr[htid].y = 64.f * rintf(fminf(m, 1e30f) * (1.f / 64.f));
+          if (m > sr[htid].y + 60.f) sr[htid].y = 64.f * rintf(fminf(m, FLT_MAX) * (1.f / 64.f));
         }
         group_sync(group);
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
           const float4 v = *reinterpret_cast<const float4*>(sr + 8 * nt + 2 * c);
-          const float s0 = whole ? 1.f : v.x, s1 = whole ? 1.f : v.z;
+          const float s0 = v.x * back, s1 = v.z * back;
           y[nt][0] = fmaf(s[nt][0], s0, -v.y); y[nt][1] = fmaf(s[nt][1], s1, -v.w);
           y[nt][2] = fmaf(s[nt][2], s0, -v.y); y[nt][3] = fmaf(s[nt][3], s1, -v.w);
         }

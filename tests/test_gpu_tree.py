@@ -980,3 +980,22 @@ def test_keys_of_the_kernel_before_are_read(page):
 
         for x, y in zip(loop(True), loop(False)):
             assert torch.equal(x, y)
+
+
+@pytest.mark.parametrize("key,query", [(1.0e36, 1.0e-36), (3.0e37, 1.0e-32), (1.0e-33, 1.0e36), (1.0e-36, 1.0e30), (1.0e30, 1.0e-30)])
+def test_keys_and_queries_at_the_ends_of_the_range(key, query):
+    """... of bfloat16, one against the other; each third token's query is 1e-6 of the others', each fifth key 1e-8."""
+    with Case(256, 2, 1.0e4, "bf16", [200, 17, 0], [[-1, 0, 1, 0, 3, -2], [-1, -1, 0, 2, 3, 3], [-1, 0, 0, -2, 2, 2]], seed=6) as c:
+        c.K = [k * np.float32(key) for k in c.K]
+        for k in c.K:
+            k[::5] *= np.float32(1.0e-8 if key > 1 else 1.0)
+        c.K = [synth.round_to_dtype(k, "bf16") for k in c.K]
+        c.q[:, ::3] *= np.float32(1.0e-6 if query > 1 else 1.0)
+        c.kt = synth.round_to_dtype(c.kt * np.float32(key), "bf16")
+        c.q = synth.round_to_dtype(c.q * np.float32(query), "bf16")
+        for b, k in enumerate(c.K):
+            c.store[b, :len(k)] = to_dev(k, "bf16")
+        c.dq, c.dkt = to_dev(c.q, "bf16"), to_dev(c.kt, "bf16")
+        c.call()
+        assert c.status() == B.SLIM_OK
+        c.check()
