@@ -18,7 +18,8 @@ namespace {
 // Everything is float64: a test next to its border and a draw next to a token's edge must not depend on the order of
 // a sum.  Bound: latency of the passes (V = 131072: 128 KB of p and q a CTA); a cluster of eight keeps a pass near a
 // microsecond where one CTA would take eight.  One sequence of 5 nodes, V = 32000: 9.6 us; 64 sequences of 16 nodes,
-// V = 131072: 41 us, 1.6 TB/s of the rows that a walk without rejections reads, about three times that with them.
+// V = 131072: 37 to 47 us, by box and clock (1.4 to 1.8 TB/s of the rows that a walk without rejections reads, about three
+// times that with them).
 constexpr int VC = 8;
 
 template <int VW>

@@ -9,8 +9,11 @@
 // down once ([b][h n + i][t], float) and the weighted sum is a matrix product P [R x T] K [T x d] cut into tiles;
 // where there are few tiles, T is cut too and the parts are added in a fixed order.
 //
-// Bound by latency at the sizes these serve: 1500 float32 rows, d = 384, 6 heads, 8 drafts 27 us in four launches (scores 9.5,
-// statistics 5.5, sums 10, projection 6.5, overlapping).  Loads of the next step run under a step's products throughout.
+// Short contexts are bound by latency: 1500 float32 rows, d = 384, 6 heads, 8 drafts 27 us in four launches (scores 9.5,
+// statistics 5.5, sums 10, projection 6.5, overlapping); loads of the next step run under a step's products throughout.
+// Long ones are bound by the shared-memory reads of the weighted sum's 64 x 64 tile: 4 x 16384 float32 rows, d = 2048, 16 heads,
+// 8 drafts 1.99 ms (18.5 TFLOP/s; elementary torch operations 4.08 ms); 16 x 8192 bf16 rows, d = 2560, head width 80,
+// 16 drafts 15.2 ms (23.6 TFLOP/s, as elementary torch operations).
 #include <cstring>
 
 #include "slim_internal.h"

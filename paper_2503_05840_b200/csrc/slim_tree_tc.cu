@@ -47,8 +47,9 @@ __device__ __forceinline__ float2 turn(const SlimDecodeParams& p, int pos, int j
 //     stay below reference + 60 (the reference itself beside keys so large that P K could overflow): nearly always the
 //     same for all blocks of a row, so that the blocks need no common maximum; `finish` shifts the exponents of the others,
 //     exactly.  Sums l are taken from the rounded P, so the weights of a row add up to one.
-// Bound by the instructions and shared-memory reads around a score (rotation, conversion, exponent, store), not by the
-// keys' bytes, d = 4096, d_k = 128: 16 ragged sequences, 196 k rows, 16 drafts 0.41 ms (3.9 TB/s of keys); 131001 rows, 64
+// No unit is full (4 x 12000 rows, 16 drafts: issue slots 53 %, shared memory 48 %, DRAM 48 %, tensor pipe 11 %): with the
+// four warps a scheduler that 128 registers allow, a warp issues every 7.5 cycles and spends 1.6 of them on fixed latencies,
+// 1.3 on shared memory, 0.8 on the math pipes, 0.65 at barriers, 0.4 on loads.  d = 4096, d_k = 128: 16 ragged sequences, 196 k rows, 16 drafts 0.41 ms (3.9 TB/s of keys); 131001 rows, 64
 // drafts 0.56 ms; 8 x 12000 rows with 1, 8, 16, 32, 64 drafts 0.16, 0.17, 0.20, 0.28, 0.43 ms (4.9 TB/s at one draft).
 // Blocks dealt to CTAs as they come, not to (sequence, head) CTAs, and loads by the warp that uses them: a CTA per row left
 // SMs idle at its end, block-wide tiles made every warp wait for the slowest load.
