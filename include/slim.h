@@ -362,6 +362,7 @@ slim_status slim_tree_commit(slim_ctx* ctx, slim_cache* cache, const void* k_tre
  *   after the last layer.  Shorter sequences stay as they are.  Any cache of the library (a paged one
  *   keeps its block table; the pages behind the budget are free to be given back).  Rows move in place: a sequence that
  *   is brought down must not share a page with another one, whose rows would change with it.
+ *   A page id outside the pool raises SLIM_ERR_CAPACITY; the rows on that page do not move.
  *   kept       device int32 [batch][budget], written: the old row of every new row, -1 behind a shorter sequence
  *   workspace  device, >= slim_evict_workspace_bytes(ctx, batch, t_cap), 256-byte aligned          */
 size_t      slim_weights_workspace_bytes(const slim_ctx* ctx, int batch, int t_cap);

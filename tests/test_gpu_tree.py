@@ -999,3 +999,52 @@ def test_keys_and_queries_at_the_ends_of_the_range(key, query):
         c.call()
         assert c.status() == B.SLIM_OK
         c.check()
+
+
+def test_a_drafting_round_in_a_graph():
+    """Attention, verification and commit captured once and replayed on new inputs give what eager calls give."""
+    d, H, n, V, Bn = 512, 4, 7, 131, 3
+    g = np.random.default_rng(8)
+    lay = SlimLayer(d, H, d // H, 1.0e4, "bf16", Bn, 128, DEV)
+    try:
+        lay.set_wkv(np.eye(d))
+        lay.k.normal_()
+        lay.reserve_scratch(n)
+        lens = torch.zeros(Bn, dtype=torch.int32, device=DEV)
+        dev = lambda x, t: torch.from_numpy(np.ascontiguousarray(x)).to(DEV, t)
+        rounds = []
+        for _ in range(3):
+            p, q, tok, par, r = draws(g, Bn, n, V, 2, close=0.3)
+            rounds.append((dev(p, torch.float32), dev(q, torch.float32), dev(tok, torch.int32), dev(par, torch.int32), dev(r, torch.float32),
+                           *(torch.randn(Bn, n, d, device=DEV).bfloat16() for _ in range(2)), dev(g.integers(0, 100, Bn), torch.int32)))
+        held = [x.clone() for x in rounds[0]]
+
+        def one(p, q, tok, par, r, tq, tk, at):
+            lens.copy_(at)
+            o = lay.tree_decode(tq, tk, lens, par)
+            path, count, nxt = lay.tree_verify(p, q, tok, par, r)
+            lay.tree_commit(tk, lens, path, count)
+            lens.add_(count)
+            return o, path, count, nxt
+
+        K0 = lay.k.clone()
+        side = torch.cuda.Stream()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            later = one(*held)
+        for k in (0, 1, 2, 1):
+            lay.k.copy_(K0)
+            want = [x.clone() for x in one(*rounds[k])] + [lay.k.clone(), lens.clone()]
+            lay.k.copy_(K0)
+            for x, y in zip(held, rounds[k]):
+                x.copy_(y)
+            side.wait_stream(torch.cuda.current_stream())
+            with torch.cuda.stream(side):
+                graph.replay()
+            torch.cuda.current_stream().wait_stream(side)
+            for x, y in zip(want, list(later) + [lay.k, lens]):
+                assert torch.equal(x, y)
+        assert lay.device_status() == B.SLIM_OK
+    finally:
+        torch.cuda.synchronize()
+        lay.close()
