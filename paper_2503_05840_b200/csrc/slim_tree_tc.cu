@@ -111,7 +111,7 @@ __device__ __forceinline__ int ordered(float f) { const int i = __float_as_int(f
 __device__ __forceinline__ float unordered(int i) { return __int_as_float(i ^ ((i >> 31) & 0x7fffffff)); }
 // 2^e with the exponent that brings |x| near `top`; 1 for 0, infinities and NaN
 __device__ __forceinline__ float pow2_to(float x, int top) {
-  if (!(x > 0.f) || x > 3e38f) return 1.f;
+  if (!(x > 0.f) || x > FLT_MAX) return 1.f;
   const int e = top - (((__float_as_int(x) >> 23) & 255) - 127);
   return __int_as_float((min(max(e, -120), 120) + 127) << 23);
 }

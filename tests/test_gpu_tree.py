@@ -1048,3 +1048,19 @@ def test_a_drafting_round_in_a_graph():
     finally:
         torch.cuda.synchronize()
         lay.close()
+
+
+@pytest.mark.parametrize("key,query", [(3.2e38, 1.0e-38), (1.0e-38, 3.2e38)])
+def test_the_largest_numbers_of_bfloat16(key, query):
+    """Every element of the keys, or of the queries, within a tenth of the largest finite number."""
+    with Case(256, 2, 1.0e4, "bf16", [200, 17, 0], [[-1, 0, 1, 0], [-1, -1, 0, 2], [-1, 0, -2, 1]], seed=6) as c:
+        c.W *= 2.0 ** -10                                    # the outputs stay in range
+        B.slim_set_wkv(c.ctx, c.W)
+        size = lambda x, f: synth.round_to_dtype((np.sign(x) if f > 1 else x) * np.float32(f), "bf16")
+        c.K, c.kt, c.q = [size(k, key) for k in c.K], size(c.kt, key), size(c.q, query)
+        for b, k in enumerate(c.K):
+            c.store[b, :len(k)] = to_dev(k, "bf16")
+        c.dq, c.dkt = to_dev(c.q, "bf16"), to_dev(c.kt, "bf16")
+        c.call()
+        assert c.status() == B.SLIM_OK
+        c.check()
