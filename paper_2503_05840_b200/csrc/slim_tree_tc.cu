@@ -49,8 +49,9 @@ __device__ __forceinline__ float2 turn(const SlimDecodeParams& p, int pos, int j
 //     exactly.  Sums l are taken from the rounded P, so the weights of a row add up to one.
 // No unit is full (4 x 12000 rows, 16 drafts: issue slots 53 %, shared memory 48 %, DRAM 48 %, tensor pipe 11 %): with the
 // four warps a scheduler that 128 registers allow, a warp issues every 7.5 cycles and spends 1.6 of them on fixed latencies,
-// 1.3 on shared memory, 0.8 on the math pipes, 0.65 at barriers, 0.4 on loads.  d = 4096, d_k = 128: 16 ragged sequences, 196 k rows, 16 drafts 0.41 ms (3.9 TB/s of keys); 131001 rows, 64
-// drafts 0.56 ms; 8 x 12000 rows with 1, 8, 16, 32, 64 drafts 0.16, 0.17, 0.20, 0.28, 0.43 ms (4.9 TB/s at one draft).
+// 1.3 on shared memory, 0.8 on the math pipes, 0.65 at barriers, 0.4 on loads.  d = 4096, d_k = 128: 16 ragged sequences,
+// 196 k rows, 16 drafts 0.41 ms (3.9 TB/s of keys); 131001 rows, 64 drafts 0.56 ms; 8 x 12000 rows with 1, 8, 16, 32, 64
+// drafts 0.16, 0.17, 0.20, 0.28, 0.43 ms (4.9 TB/s at one draft).
 // Blocks dealt to CTAs as they come, not to (sequence, head) CTAs, and loads by the warp that uses them: a CTA per row left
 // SMs idle at its end, block-wide tiles made every warp wait for the slowest load.
 constexpr int SC_KEYS = 128, SC_GROUP = 256;
