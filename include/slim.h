@@ -53,8 +53,9 @@ typedef enum {
 } slim_status;
 
 /* cache / query dtype.  SLIM_FP8: the cache holds 8-bit keys (1 byte per value, the paper's own byte
- * accounting in its introduction), queries, new key rows and W_KV are bf16 -- see slim_cache_bytes. */
-typedef enum { SLIM_F32 = 0, SLIM_BF16 = 1, SLIM_FP8 = 2 } slim_dtype;
+ * accounting in its introduction), queries, new key rows and W_KV are bf16 -- see slim_cache_bytes.
+ * SLIM_FP4: the same with 4-bit keys and a scale byte for 32 of them (17/32 byte per value). */
+typedef enum { SLIM_F32 = 0, SLIM_BF16 = 1, SLIM_FP8 = 2, SLIM_FP4 = 3 } slim_dtype;
 typedef enum { SLIM_HOST_F32 = 0, SLIM_HOST_F64 = 1 } slim_host_dtype;
 
 /* Kernel selection for slim_decode (slim_set_path). */
@@ -120,7 +121,17 @@ slim_status slim_set_wkv(slim_ctx* ctx, const void* W_KV, int host_dtype);
  * mode.  Where the shape fits the tensor-core kernels, slim_decode first decodes the live rows
  * exactly into a bf16 copy inside the workspace (slim_workspace_bytes then includes
  * 2 * batch * t_cap * d bytes for it) and runs the bf16 kernels on the copy; otherwise, and with
- * SLIM_PATH_GENERIC, the CUDA-core kernels read the codes directly.                       */
+ * SLIM_PATH_GENERIC, the CUDA-core kernels read the codes directly.
+ * SLIM_FP4 caches: the storage holds the codes, one row after another (contiguous: [batch][t_cap], paged:
+ * [num_pages][page_rows] rows), a row being d/2 bytes padded to a multiple of 16, column 2i in the low and column 2i + 1
+ * in the high half of byte i; behind all codes the scales, a row being one byte for 32 columns, padded to a multiple of 16
+ * bytes.  A code is a sign bit and one of 0, 0.5, 1, 1.5, 2, 3, 4, 6 (OCP E2M1); a scale byte holds the bits 14 .. 7 of a
+ * float16 whose other bits are zero.  The stored key is code * scale.  Rows are quantised as they are written: the scale is
+ * the smallest s, at most 10240, with 6 s >= max |k| of the 32 columns, a code the nearest of the values times s, on a
+ * border the even code (magnitudes above 61440 saturate); a group with a number that is not finite reads back as NaN.
+ * Such a cache is filled through slim_append_k, slim_append_rows, slim_decode_step, slim_decode_typed or slim_prefill, and
+ * may be paged: a pool takes slim_cache_bytes(ctx, num_pages, page_rows).  slim_decode_partial, slim_tree_*,
+ * slim_accumulate_weights, slim_evict and the X-cache calls do not take it (SLIM_ERR_UNSUPPORTED).          */
 size_t slim_cache_bytes(const slim_ctx* ctx, int batch, int t_cap);
 size_t slim_workspace_bytes(const slim_ctx* ctx, int batch, int t_cap);
 
@@ -195,6 +206,12 @@ slim_status slim_decode(slim_ctx* ctx, const void* q, const slim_cache* cache,
  * paths launch the append kernel first.                                                 */
 slim_status slim_decode_step(slim_ctx* ctx, const void* q, const void* k_new, slim_cache* cache,
                              const int32_t* lengths, float* o, void* workspace, void* stream);
+
+/* slim_decode (k_new NULL) or slim_decode_step (k_new given) with the type of the output chosen: o is device [batch][d]
+ * float32 (SLIM_F32) or bfloat16 (SLIM_BF16: rounded once as it is stored, the operand of the output projection),
+ * 16-byte aligned.  Any cache of keys that slim_decode takes.                                       */
+slim_status slim_decode_typed(slim_ctx* ctx, const void* q, const void* k_new, slim_cache* cache, const int32_t* lengths,
+                              void* o, int o_dtype, void* workspace, void* stream);
 
 /* slim_decode for callers that cannot allocate device memory.  (The paper has no
  * counterpart; this is a convenience of the library.)  Some hosts of this code must
@@ -280,6 +297,47 @@ slim_status slim_decode_partial(slim_ctx* ctx, const void* q, const slim_cache* 
 slim_status slim_combine_project(slim_ctx* ctx, const float* lse_all, const float* u_all, int ranks,
                                  const int32_t* total_lengths, int batch, float* o, void* workspace, void* stream);
 
+/* ---- Prompts of several sequences, packed ------------------------------------------------------
+ * (Eq. 4 and 5 for a whole prompt, Fig. 3(a): the values are formed once from the keys, the attention is the usual one.)
+ * Sequences of different lengths lie one behind another in one array; cu_* (device int32 [batch + 1]) says where each
+ * begins, sequence b being rows cu[b] .. cu[b + 1] - 1.  Starts that do not ascend from 0 or more to the array's rows raise SLIM_ERR_CAPACITY
+ * on the device, and the sequences that they bound are left out.  Rows in front of the first and behind the last sequence are
+ * neither read nor written.
+ *     slim_prompt_attention (values from slim_prefill or slim_values_from_keys)  and  slim_append_rows;
+ *     for the next chunk of a prompt: slim_read_rows gives the keys that are cached, slim_values_from_keys their values
+ *
+ * slim_prompt_attention  o_i = sum_j softmax_j(q_i . k_j / sqrt(d_k)) v_j, head by head.  With nq queries and nk keys in a
+ *   sequence, key j sits at position j and query i at position nk - nq + i, so that the last query meets the last key (a chunk's
+ *   queries come with all keys up to the chunk's end); where the context has RoPE, both are rotated.
+ *   q          device [total_q][H][d_k], ctx dtype, un-rotated;  k  device [total_k][kv_heads][d_k], ctx dtype, un-rotated
+ *   v          device [total_k][kv_heads][d_k], v_dtype: SLIM_F32, or in a bf16 context SLIM_BF16
+ *   kv_heads   divides H; query heads h H/kv_heads .. share key head h.  (The values of slim attention have kv_heads = H.)
+ *   max_k      no sequence has more keys (more: left out, SLIM_ERR_CAPACITY on the device).  With RoPE the position tables
+ *              have to cover it: slim_reserve_positions, or a cache of that capacity; else SLIM_ERR_CAPACITY, nothing launched
+ *   causal     1: query i attends keys 0 .. nk - nq + i; 0: all nk.  A query that attends no key gets a zero row
+ *   o          device [total_q][H][d_k], ctx dtype.  q, k, v, o 16-byte aligned and contiguous; o may not overlap the inputs
+ *   workspace  device, >= slim_prompt_workspace_bytes (0 on bad arguments), 256-byte aligned; contents are scratch, shared
+ *              like that of slim_tree_decode
+ *   Softmax sums and weighted sums are float32; in a bf16 context rotated queries and keys are rounded to 11 bits, and the
+ *   probabilities and float32 values to bf16.  A number that is not finite in a key or a value reaches the rows that attend it, and
+ *   no other.  bf16, d_k in {64, 96, 128}: tensor cores; other shapes: CUDA cores (slim_set_path chooses as for slim_decode).
+ *   No weights need to be set.  total_q, total_k at most 2^29.
+ *
+ * slim_append_rows  packed rows k_new [total][d] (device, ctx dtype, un-rotated) into the cache: the rows of sequence b go to cache
+ *   rows positions[b], positions[b] + 1, ..  A sequence whose rows would pass t_cap is left unwritten (SLIM_ERR_CAPACITY); a row on
+ *   a page outside the pool likewise.  A 4-bit cache quantises them.
+ * slim_read_rows    the inverse: those cache rows as they are stored, to k_out [total][d] (device, ctx dtype; a 4-bit cache's
+ *   keys are exact in bf16); rows that cannot be read are left as they were.
+ *   Both: f32, bf16 and 4-bit caches, contiguous or paged (not SLIM_FP8: SLIM_ERR_UNSUPPORTED); cu_rows[batch] <= total <= 2^30. */
+size_t      slim_prompt_workspace_bytes(const slim_ctx* ctx, int kv_heads, int batch, int total_q, int total_k);
+slim_status slim_prompt_attention(slim_ctx* ctx, const void* q, const void* k, const void* v, int v_dtype, int kv_heads,
+                                  const int32_t* cu_q, const int32_t* cu_k, int batch, int total_q, int total_k, int max_k,
+                                  int causal, void* o, void* workspace, void* stream);
+slim_status slim_append_rows(slim_ctx* ctx, slim_cache* cache, const void* k_new, const int32_t* positions, const int32_t* cu_rows,
+                             int total, void* stream);
+slim_status slim_read_rows(slim_ctx* ctx, const slim_cache* cache, const int32_t* positions, const int32_t* cu_rows, int total,
+                           void* k_out, void* stream);
+
 /* ---- Several drafted tokens in one step (speculative decoding) --------------------------------
  * (The paper has no counterpart; Eq. 7 Option 2 is evaluated for every drafted token.)  A small model
  * or a lookup drafts a tree of n <= SLIM_MAX_TREE tokens per sequence; one pass attends for all of
@@ -297,7 +355,7 @@ slim_status slim_combine_project(slim_ctx* ctx, const float* lse_all, const floa
  * slim_tree_decode  attention of every drafted token over the cached rows, its ancestors and itself.
  *   q, k_tree  device [batch][n][d], ctx dtype, 16-byte aligned: un-rotated queries and key rows of the
  *              drafted tokens; token i sits at position lengths[b] + depth(i)
- *   cache      contiguous or paged keys (not SLIM_FP8, not an X-cache: SLIM_ERR_UNSUPPORTED); it is read only: drafted keys
+ *   cache      contiguous or paged keys (not SLIM_FP8 or SLIM_FP4, not an X-cache: SLIM_ERR_UNSUPPORTED); it is read only: drafted keys
  *              enter it by slim_tree_commit
  *   lengths    device int32 [batch]: cached rows of sequence b (0: the tokens attend the tree only); above t_cap:
  *              clamped and reported as SLIM_ERR_CAPACITY.  Rows behind them may hold anything; a number that is not finite

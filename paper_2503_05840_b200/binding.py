@@ -15,7 +15,7 @@ LIB_PATH = os.path.join(_HERE, "libslim.so")
 
 SLIM_OK, SLIM_ERR_INVALID_ARG, SLIM_ERR_UNSUPPORTED, SLIM_ERR_SINGULAR, SLIM_ERR_CAPACITY, \
     SLIM_ERR_OOM, SLIM_ERR_CUDA, SLIM_ERR_TIMEOUT, SLIM_ERR_NO_WEIGHTS, SLIM_ERR_STATIC_WS, SLIM_ERR_TREE = range(11)
-SLIM_F32, SLIM_BF16, SLIM_FP8 = 0, 1, 2
+SLIM_F32, SLIM_BF16, SLIM_FP8, SLIM_FP4 = 0, 1, 2, 3
 SLIM_HOST_F32, SLIM_HOST_F64 = 0, 1
 SLIM_MAX_TREE = 64
 SLIM_PATH_AUTO, SLIM_PATH_GENERIC, SLIM_PATH_TC = 0, 1, 2
@@ -38,6 +38,7 @@ SIGNATURES = {
     "slim_append_k": (c_int, [c_void_p, c_void_p, c_void_p, c_void_p, c_int, c_void_p]),
     "slim_decode": (c_int, [c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p]),
     "slim_decode_step": (c_int, [c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p]),
+    "slim_decode_typed": (c_int, [c_void_p] * 6 + [c_int, c_void_p, c_void_p]),
     "slim_static_workspace_max": (c_size_t, []),
     "slim_decode_static_ws": (c_int, [c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p]),
     "slim_xcache_create": (c_int, [POINTER(c_void_p), c_int, c_int, c_int, c_int]),
@@ -47,6 +48,10 @@ SIGNATURES = {
     "slim_reserve_positions": (c_int, [c_void_p, c_int]),
     "slim_decode_partial": (c_int, [c_void_p] * 10),
     "slim_combine_project": (c_int, [c_void_p, c_void_p, c_void_p, c_int, c_void_p, c_int, c_void_p, c_void_p, c_void_p]),
+    "slim_prompt_workspace_bytes": (c_size_t, [c_void_p] + [c_int] * 4),
+    "slim_prompt_attention": (c_int, [c_void_p] * 4 + [c_int, c_int, c_void_p, c_void_p] + [c_int] * 5 + [c_void_p] * 3),
+    "slim_append_rows": (c_int, [c_void_p] * 5 + [c_int, c_void_p]),
+    "slim_read_rows": (c_int, [c_void_p] * 4 + [c_int, c_void_p, c_void_p]),
     "slim_tree_workspace_bytes": (c_size_t, [c_void_p, c_int, c_int, c_int]),
     "slim_tree_decode": (c_int, [c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_int, c_void_p, c_void_p, c_void_p]),
     "slim_tree_verify": (c_int, [c_void_p] * 6 + [c_int] * 3 + [c_void_p] * 4),
@@ -212,6 +217,12 @@ def slim_decode_step(ctx: int, q, k_new, cache: int, lengths, o, workspace, stre
                                   _ptr(workspace), c_void_p(stream)), "slim_decode_step")
 
 
+def slim_decode_typed(ctx: int, q, k_new, cache: int, lengths, o, o_dtype: int, workspace, stream: int = 0) -> None:
+    """slim_decode (k_new None) or slim_decode_step with the type of o chosen (SLIM_F32, SLIM_BF16)."""
+    _check(lib().slim_decode_typed(ctx, _ptr(q), _ptr(k_new), cache, _ptr(lengths), _ptr(o), o_dtype, _ptr(workspace),
+                                   stream), "slim_decode_typed")
+
+
 def slim_static_workspace_max() -> int:
     return lib().slim_static_workspace_max()
 
@@ -256,6 +267,27 @@ def slim_decode_partial(ctx: int, q, cache: int, lengths, first_tile, q_pos, lse
 def slim_combine_project(ctx: int, lse_all, u_all, ranks: int, total_lengths, batch: int, o, workspace, stream: int = 0) -> None:
     _check(lib().slim_combine_project(c_void_p(ctx), _ptr(lse_all), _ptr(u_all), ranks, _ptr(total_lengths), batch, _ptr(o),
                                       _ptr(workspace), c_void_p(stream)), "slim_combine_project")
+
+
+def slim_prompt_workspace_bytes(ctx: int, kv_heads: int, batch: int, total_q: int, total_k: int) -> int:
+    return lib().slim_prompt_workspace_bytes(ctx, kv_heads, batch, total_q, total_k)
+
+
+def slim_prompt_attention(ctx: int, q, k, v, v_dtype: int, kv_heads: int, cu_q, cu_k, batch: int, total_q: int, total_k: int, max_k: int,
+                          causal: bool, o, workspace, stream: int = 0) -> None:
+    """Attention over packed prompts (Eq. 4 and 5 for all tokens): rotation, softmax and weighted sum of the values."""
+    _check(lib().slim_prompt_attention(ctx, _ptr(q), _ptr(k), _ptr(v), v_dtype, kv_heads, _ptr(cu_q), _ptr(cu_k), batch, total_q, total_k, max_k,
+                                       1 if causal else 0, _ptr(o), _ptr(workspace), stream), "slim_prompt_attention")
+
+
+def slim_append_rows(ctx: int, cache: int, k_new, positions, cu_rows, total: int, stream: int = 0) -> None:
+    """Packed rows of several sequences into the cache, quantised where it holds 4 bits."""
+    _check(lib().slim_append_rows(ctx, cache, _ptr(k_new), _ptr(positions), _ptr(cu_rows), total, stream), "slim_append_rows")
+
+
+def slim_read_rows(ctx: int, cache: int, positions, cu_rows, total: int, k_out, stream: int = 0) -> None:
+    """Cached rows of several sequences, packed, as they are stored."""
+    _check(lib().slim_read_rows(ctx, cache, _ptr(positions), _ptr(cu_rows), total, _ptr(k_out), stream), "slim_read_rows")
 
 
 def slim_tree_workspace_bytes(ctx: int, batch: int, t_cap: int, n: int) -> int:

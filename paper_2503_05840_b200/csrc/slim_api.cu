@@ -8,6 +8,8 @@
 #include <new>
 #include <vector>
 
+#include "slim_attn.h"
+#include "slim_fp4.cuh"
 #include "slim_internal.h"
 #include "slim_tree.h"
 
@@ -174,12 +176,12 @@ namespace {
 slim_status create_impl(slim_ctx** out, int d, int H, int d_k, double rope_theta, int dtype, bool xcache_only) {
   if (!out) return SLIM_ERR_INVALID_ARG;
   *out = nullptr;
-  if (d <= 0 || H <= 0 || d_k <= 0 || !(rope_theta >= 0.0) || (dtype != SLIM_F32 && dtype != SLIM_BF16 && dtype != SLIM_FP8))
+  if (d <= 0 || H <= 0 || d_k <= 0 || !(rope_theta >= 0.0) || (dtype != SLIM_F32 && dtype != SLIM_BF16 && dtype != SLIM_FP8 && dtype != SLIM_FP4))
     return SLIM_ERR_INVALID_ARG;
   const int kdtype = dtype;
-  if (dtype == SLIM_FP8) dtype = SLIM_BF16;            // 8-bit cache; queries, new rows and W_KV are bf16
+  if (dtype == SLIM_FP8 || dtype == SLIM_FP4) dtype = SLIM_BF16;            // 8-bit, 4-bit cache; queries, new rows and W_KV are bf16
   if ((long long)H * d_k != d && !xcache_only) return SLIM_ERR_UNSUPPORTED;       // Eq. 6 needs a square W_K
-  if (xcache_only && dtype == SLIM_FP8) return SLIM_ERR_UNSUPPORTED;
+  if (xcache_only && (dtype == SLIM_FP8 || kdtype == SLIM_FP4)) return SLIM_ERR_UNSUPPORTED;
   if (H > SLIM_MAX_H || d_k > 256 || (d_k % 2) != 0 || d > 16384 || (long long)H * d_k > 16384) return SLIM_ERR_UNSUPPORTED;      // rotation pairs need an even width
   const int e = H * d_k;
   int dev = 0;
@@ -359,7 +361,7 @@ slim_status slim_set_weights_nonsquare(slim_ctx* ctx, const void* W_K, const voi
 slim_status slim_xcache_set_weights(slim_ctx* ctx, const void* W_K, const void* W_V, int host_dtype) {
   if (!ctx || !W_K || !W_V || (host_dtype != SLIM_HOST_F32 && host_dtype != SLIM_HOST_F64)) return SLIM_ERR_INVALID_ARG;
   if (ctx->rope_theta != 0.0) return SLIM_ERR_UNSUPPORTED;          // the scheme has no place for RoPE
-  if (ctx->kdtype == SLIM_FP8) return SLIM_ERR_UNSUPPORTED;
+  if (ctx->kdtype == SLIM_FP8 || ctx->kdtype == SLIM_FP4) return SLIM_ERR_UNSUPPORTED;
   const size_t nn = (size_t)ctx->d * ctx->e;              // W_K, W_V: [d][e]
   std::vector<float> wk(nn);
   if (host_dtype == SLIM_HOST_F64) { const double* s = static_cast<const double*>(W_K); for (size_t i = 0; i < nn; ++i) wk[i] = (float)s[i]; }
@@ -392,6 +394,7 @@ size_t slim_cache_bytes(const slim_ctx* ctx, int batch, int t_cap) {
   if (!ctx || batch <= 0 || t_cap <= 0) return 0;
   if (ctx->kdtype == SLIM_FP8)                             // codes, then one exponent per (row, head)
     return ((((size_t)batch * t_cap * ctx->d) + 15) & ~(size_t)15) + (size_t)batch * t_cap * ctx->H;
+  if (ctx->kdtype == SLIM_FP4) return (size_t)batch * t_cap * (slim_fp4_code_pitch(ctx->d) + slim_fp4_scale_pitch(ctx->d));
   return esize(ctx->dtype) * (size_t)batch * t_cap * ctx->d;
 }
 
@@ -413,17 +416,18 @@ slim_status slim_cache_create(slim_ctx* ctx, slim_cache** out, void* k_storage, 
   c->ctx = ctx; c->k = k_storage; c->batch = batch; c->t_cap = t_cap;
   c->k_exp = ctx->kdtype == SLIM_FP8
                  ? reinterpret_cast<signed char*>(k_storage) + ((((size_t)batch * t_cap * ctx->d) + 15) & ~(size_t)15) : nullptr;
+  c->k_sc4 = ctx->kdtype == SLIM_FP4 ? reinterpret_cast<unsigned char*>(k_storage) + (size_t)batch * t_cap * slim_fp4_code_pitch(ctx->d) : nullptr;
   c->block_table = nullptr; c->page_rows = 0; c->max_pages = 0; c->num_pages = 0;
   c->total_rows = (long long)batch * t_cap;
   for (int cl = 1; cl <= 2; ++cl) {
     c->has_tmap[cl - 1] = 0;
-    if (ctx->tc_workers[cl - 1] > 0 && ctx->kdtype != SLIM_FP8) {       // (an 8-bit cache is read through a bf16 scratch)
+    if (ctx->tc_workers[cl - 1] > 0 && ctx->kdtype != SLIM_FP8 && ctx->kdtype != SLIM_FP4) {       // (an 8-bit cache is read through a bf16 scratch)
       if (slim_tc_make_tmap(ctx, c, cl) == cudaSuccess) c->has_tmap[cl - 1] = 1;
       else cudaGetLastError();
     }
   }
   c->has_xmap = 0;
-  if (ctx->proj_ok && ctx->kdtype != SLIM_FP8 && slim_xscores_tc_ok(ctx)) {
+  if (ctx->proj_ok && ctx->kdtype != SLIM_FP8 && ctx->kdtype != SLIM_FP4 && slim_xscores_tc_ok(ctx)) {
     if (slim_xscores_make_tmap(ctx, c) == cudaSuccess) c->has_xmap = 1;
     else cudaGetLastError();
   }
@@ -446,11 +450,12 @@ slim_status slim_cache_create_paged(slim_ctx* ctx, slim_cache** out, void* pool,
   slim_cache* c = new (std::nothrow) slim_cache();
   if (!c) return SLIM_ERR_OOM;
   c->ctx = ctx; c->k = pool; c->k_exp = nullptr; c->batch = batch; c->t_cap = t_cap;
+  c->k_sc4 = ctx->kdtype == SLIM_FP4 ? reinterpret_cast<unsigned char*>(pool) + (size_t)num_pages * page_rows * slim_fp4_code_pitch(ctx->d) : nullptr;
   c->block_table = block_table; c->page_rows = page_rows; c->max_pages = max_pages; c->num_pages = num_pages;
   c->total_rows = (long long)num_pages * page_rows;
   for (int cl = 1; cl <= 2; ++cl) {
     c->has_tmap[cl - 1] = 0;
-    if (ctx->tc_workers[cl - 1] > 0) {
+    if (ctx->tc_workers[cl - 1] > 0 && ctx->kdtype != SLIM_FP4) {
       if (slim_tc_make_tmap(ctx, c, cl) == cudaSuccess) c->has_tmap[cl - 1] = 1;
       else cudaGetLastError();
     }
@@ -483,7 +488,8 @@ struct PartialOut {
 
 // k_new != NULL: the generate-phase step (newest key rows written at lengths[b] - 1 first)
 slim_status decode_impl(slim_ctx* ctx, const void* q, const slim_cache* cache, const int32_t* lengths, float* o,
-                        void* workspace, void* stream, bool xcache, const void* k_new = nullptr, const PartialOut* part = nullptr) {
+                        void* workspace, void* stream, bool xcache, const void* k_new = nullptr, const PartialOut* part = nullptr,
+                        int o_bf16 = 0) {
   if (!ctx || !q || !cache || !lengths || (!o && !part) || !workspace || cache->ctx != ctx) return SLIM_ERR_INVALID_ARG;
   if (((uintptr_t)workspace & 255) || ((uintptr_t)q & 15) || ((uintptr_t)o & 15)) return SLIM_ERR_INVALID_ARG;
   if (!ctx->has_weights) return SLIM_ERR_NO_WEIGHTS;
@@ -491,6 +497,8 @@ slim_status decode_impl(slim_ctx* ctx, const void* q, const slim_cache* cache, c
   if (xcache && !ctx->xc_wk) return SLIM_ERR_NO_WEIGHTS;
   if (!xcache && ctx->e != ctx->d) return SLIM_ERR_UNSUPPORTED;   // the K-cache scheme needs square projections
   if (xcache && cache->block_table) return SLIM_ERR_UNSUPPORTED;
+  const bool fp4 = ctx->kdtype == SLIM_FP4;
+  if (fp4) path = SLIM_PATH_GENERIC;
   if (path < 0) return SLIM_ERR_UNSUPPORTED;
   // CTAs per worker: the pair when the kernel computes the scores, the lone CTA with external scores
   int cl = 0;
@@ -509,7 +517,7 @@ slim_status decode_impl(slim_ctx* ctx, const void* q, const slim_cache* cache, c
   SlimDecodeParams p;
   p.d = ctx->d; p.e = ctx->e; p.H = ctx->H; p.d_k = ctx->d_k; p.half = ctx->d_k / 2;
   p.batch = cache->batch; p.t_cap = cache->t_cap;
-  p.rope = ctx->rope_theta != 0.0; p.dtype = ctx->dtype; p.kdtype = ctx->kdtype; p.k_exp = cache->k_exp;
+  p.rope = ctx->rope_theta != 0.0; p.dtype = ctx->dtype; p.kdtype = ctx->kdtype; p.k_exp = cache->k_exp; p.k_sc4 = cache->k_sc4;
   p.workers = path == SLIM_PATH_TC ? ctx->tc_workers[cl - 1] : ctx->gen_workers;
   p.cl = cl;
   p.min_tiles = min_tiles_for(ctx);
@@ -524,7 +532,7 @@ slim_status decode_impl(slim_ctx* ctx, const void* q, const slim_cache* cache, c
   p.part_l = reinterpret_cast<float*>(ws + L.part_l);
   p.unit_flags = reinterpret_cast<int*>(ws + L.flags);
   p.u = reinterpret_cast<float*>(ws + L.o_part);
-  p.o = o; p.status = ctx->status; p.any_flag = ctx->any_flag;
+  p.o = o; p.o_bf16 = o_bf16; p.status = ctx->status; p.any_flag = ctx->any_flag;
   p.ext_scores = nullptr;
   p.block_table = cache->block_table; p.page_rows = cache->page_rows; p.max_pages = cache->max_pages;
   p.num_pages = cache->num_pages;
@@ -590,7 +598,7 @@ slim_status decode_impl(slim_ctx* ctx, const void* q, const slim_cache* cache, c
     ++launches;
     if (e == cudaSuccess && !p.redo_in_combine) { e = slim_launch_exact_flagged(ctx, p, st); ++launches; }
   } else {
-    e = slim_launch_generic(ctx, p, scores, st);
+    e = fp4 ? slim_launch_fp4_decode(ctx, p, scores, st) : slim_launch_generic(ctx, p, scores, st);
     launches += 2;                                   // scores, accumulation
   }
   if (ctx->prof_on) cudaEventRecord(ctx->prof_ev[1], st);
@@ -625,6 +633,12 @@ slim_status slim_decode_step(slim_ctx* ctx, const void* q, const void* k_new, sl
   return decode_impl(ctx, q, cache, lengths, o, workspace, stream, false, k_new);
 }
 
+slim_status slim_decode_typed(slim_ctx* ctx, const void* q, const void* k_new, slim_cache* cache, const int32_t* lengths, void* o,
+                              int o_dtype, void* workspace, void* stream) {
+  if ((o_dtype != SLIM_F32 && o_dtype != SLIM_BF16) || ((uintptr_t)k_new & 15)) return SLIM_ERR_INVALID_ARG;
+  return decode_impl(ctx, q, cache, lengths, static_cast<float*>(o), workspace, stream, false, k_new, nullptr, o_dtype == SLIM_BF16);
+}
+
 slim_status slim_reserve_positions(slim_ctx* ctx, int max_position) {
   if (!ctx || max_position <= 0) return SLIM_ERR_INVALID_ARG;
   return grow_rope_base(ctx, (long long)max_position + SLIM_MAX_TREE);      // (as a cache of that many rows does)
@@ -634,7 +648,7 @@ slim_status slim_decode_partial(slim_ctx* ctx, const void* q, const slim_cache* 
                                 const int32_t* first_tile, const int32_t* q_pos, float* lse_out, float* u_out,
                                 void* workspace, void* stream) {
   if (!first_tile || !q_pos || !lse_out || !u_out) return SLIM_ERR_INVALID_ARG;
-  if (ctx && ctx->kdtype == SLIM_FP8) return SLIM_ERR_UNSUPPORTED;
+  if (ctx && (ctx->kdtype == SLIM_FP8 || ctx->kdtype == SLIM_FP4)) return SLIM_ERR_UNSUPPORTED;
   const PartialOut part = {first_tile, q_pos, lse_out, u_out};
   return decode_impl(ctx, q, cache, lengths, nullptr, workspace, stream, false, nullptr, &part);
 }
@@ -719,7 +733,7 @@ slim_status slim_decode_static_ws(slim_ctx* ctx, const void* q, const slim_cache
   return slim_decode(ctx, q, cache, lengths, o, ws, stream);
 }
 
-// ---- drafted tokens, cache budget ------------------------------------------------
+// ---- packed prompts, packed rows ---------------------------------------------------
 namespace {
 // Their kernels round row counts up and step past the last row in 32 bits, so a capacity or a budget is at most this.
 constexpr int kMaxRows = 1 << 30;
@@ -766,6 +780,60 @@ WeightsLayout weights_layout(const slim_ctx* ctx, int batch, int t_cap) {
 }
 }  // namespace
 
+size_t slim_prompt_workspace_bytes(const slim_ctx* ctx, int kv_heads, int batch, int total_q, int total_k) {
+  if (!ctx || ctx->e != ctx->d || kv_heads <= 0 || ctx->H % kv_heads || batch <= 0 || batch > SLIM_MAX_BATCH) return 0;
+  if (total_q <= 0 || total_k < 0 || total_q > kMaxRows / 2 || total_k > kMaxRows / 2) return 0;
+  return slim_attn_layout(ctx, kv_heads, batch, total_q, total_k).total;
+}
+
+slim_status slim_prompt_attention(slim_ctx* ctx, const void* q, const void* k, const void* v, int v_dtype, int kv_heads, const int32_t* cu_q,
+                                  const int32_t* cu_k, int batch, int total_q, int total_k, int max_k, int causal, void* o, void* workspace,
+                                  void* stream) {
+  if (!ctx || !q || !cu_q || !cu_k || !o || !workspace || (total_k > 0 && (!k || !v))) return SLIM_ERR_INVALID_ARG;
+  if (total_q <= 0 || total_k < 0 || max_k < 0 || batch <= 0 || kv_heads <= 0 || ((uintptr_t)workspace & 255)) return SLIM_ERR_INVALID_ARG;
+  if (((uintptr_t)q | (uintptr_t)k | (uintptr_t)v | (uintptr_t)o) & 15) return SLIM_ERR_INVALID_ARG;
+  if (v_dtype != SLIM_F32 && v_dtype != SLIM_BF16) return SLIM_ERR_INVALID_ARG;
+  if (ctx->e != ctx->d || ctx->H % kv_heads || batch > SLIM_MAX_BATCH || total_q > kMaxRows / 2 || total_k > kMaxRows / 2 ||
+      (ctx->dtype == SLIM_F32 && v_dtype != SLIM_F32))
+    return SLIM_ERR_UNSUPPORTED;
+  if (!current_device_is(ctx)) return SLIM_ERR_INVALID_ARG;
+  if (ctx->rope_theta != 0.0 && max_k > (ctx->rope_base_tiles - 1) * SLIM_TT) return SLIM_ERR_CAPACITY;      // slim_reserve_positions(max_k) first
+  const int tc = ctx->path_req != SLIM_PATH_GENERIC && slim_attn_tc_ok(ctx);
+  if (ctx->path_req == SLIM_PATH_TC && !tc) return SLIM_ERR_UNSUPPORTED;
+  SlimAttn a = {};
+  a.H = ctx->H; a.KV = kv_heads; a.d_k = ctx->d_k; a.half = ctx->d_k / 2;
+  a.batch = batch; a.total_q = total_q; a.total_k = total_k; a.max_k = max_k; a.causal = causal != 0;
+  a.f32 = ctx->dtype == SLIM_F32; a.v32 = v_dtype == SLIM_F32;
+  a.qscale = (float)(1.4426950408889634 / std::sqrt((double)ctx->d_k));
+  a.q = q; a.k = k; a.v = v; a.o = o; a.cu_q = cu_q; a.cu_k = cu_k;
+  if (ctx->rope_theta != 0.0) { a.rope_base = ctx->rope_base; a.rope_off = ctx->rope_off; }
+  a.status = ctx->status;
+  return launched(slim_launch_attn(ctx, a, static_cast<char*>(workspace), tc, (cudaStream_t)stream));
+}
+
+namespace {
+slim_status rows_impl(slim_ctx* ctx, const slim_cache* cache, void* rows, const int32_t* positions, const int32_t* cu_rows, int total, int to_cache,
+                      void* stream) {
+  if (!ctx || !cache || !rows || !positions || !cu_rows || cache->ctx != ctx || total <= 0) return SLIM_ERR_INVALID_ARG;
+  const uintptr_t unit = ctx->dtype == SLIM_F32 ? 3 : 1;
+  if ((uintptr_t)rows & unit) return SLIM_ERR_INVALID_ARG;
+  if (ctx->kdtype == SLIM_FP8 || ctx->e != ctx->d || total > kMaxRows) return SLIM_ERR_UNSUPPORTED;
+  if (!current_device_is(ctx)) return SLIM_ERR_INVALID_ARG;
+  return launched(slim_launch_rows(ctx, cache, rows, positions, cu_rows, total, to_cache, (cudaStream_t)stream));
+}
+}  // namespace
+
+slim_status slim_append_rows(slim_ctx* ctx, slim_cache* cache, const void* k_new, const int32_t* positions, const int32_t* cu_rows, int total,
+                             void* stream) {
+  return rows_impl(ctx, cache, const_cast<void*>(k_new), positions, cu_rows, total, 1, stream);
+}
+
+slim_status slim_read_rows(slim_ctx* ctx, const slim_cache* cache, const int32_t* positions, const int32_t* cu_rows, int total, void* k_out,
+                           void* stream) {
+  return rows_impl(ctx, cache, k_out, positions, cu_rows, total, 0, stream);
+}
+
+// ---- drafted tokens, cache budget ------------------------------------------------
 size_t slim_tree_workspace_bytes(const slim_ctx* ctx, int batch, int t_cap, int n) {
   if (!ctx || batch <= 0 || t_cap <= 0 || t_cap > kMaxRows || batch > SLIM_MAX_BATCH || n <= 0 || n > SLIM_MAX_TREE || ctx->e != ctx->d) return 0;
   return slim_tree_ws_layout(ctx, batch, t_cap, n).total;
@@ -776,7 +844,7 @@ slim_status slim_tree_decode(slim_ctx* ctx, const void* q, const void* k_tree, c
   if (!ctx || !q || !k_tree || !cache || !lengths || !parents || !o || !workspace || cache->ctx != ctx) return SLIM_ERR_INVALID_ARG;
   if (n <= 0 || n > SLIM_MAX_TREE || ((uintptr_t)workspace & 255)) return SLIM_ERR_INVALID_ARG;
   if (((uintptr_t)q | (uintptr_t)k_tree | (uintptr_t)o) & 15) return SLIM_ERR_INVALID_ARG;
-  if (ctx->kdtype == SLIM_FP8 || ctx->e != ctx->d || ctx->xc_wk || cache->t_cap > kMaxRows) return SLIM_ERR_UNSUPPORTED;     // (xc_wk: the rows are X, not keys)
+  if (ctx->kdtype == SLIM_FP8 || ctx->kdtype == SLIM_FP4 || ctx->e != ctx->d || ctx->xc_wk || cache->t_cap > kMaxRows) return SLIM_ERR_UNSUPPORTED;     // (xc_wk: the rows are X, not keys)
   if (!ctx->has_weights) return SLIM_ERR_NO_WEIGHTS;
   if (!current_device_is(ctx)) return SLIM_ERR_INVALID_ARG;
   const int tc = ctx->path_req != SLIM_PATH_GENERIC && slim_tree_tc_ok(ctx);
@@ -797,7 +865,7 @@ slim_status slim_tree_commit(slim_ctx* ctx, slim_cache* cache, const void* k_tre
                              const int32_t* count, int n, void* stream) {
   if (!ctx || !cache || !k_tree || !lengths || !path || !count || cache->ctx != ctx) return SLIM_ERR_INVALID_ARG;
   if (n <= 0 || n > SLIM_MAX_TREE || ((uintptr_t)k_tree & 15)) return SLIM_ERR_INVALID_ARG;
-  if (ctx->kdtype == SLIM_FP8 || ctx->e != ctx->d || cache->t_cap > kMaxRows) return SLIM_ERR_UNSUPPORTED;
+  if (ctx->kdtype == SLIM_FP8 || ctx->kdtype == SLIM_FP4 || ctx->e != ctx->d || cache->t_cap > kMaxRows) return SLIM_ERR_UNSUPPORTED;
   if (!current_device_is(ctx)) return SLIM_ERR_INVALID_ARG;
   return launched(slim_launch_commit(ctx, cache, k_tree, lengths, path, count, n, (cudaStream_t)stream));
 }
@@ -811,7 +879,7 @@ slim_status slim_accumulate_weights(slim_ctx* ctx, const void* q, const slim_cac
                                     void* workspace, void* stream) {
   if (!ctx || !q || !cache || !lengths || !acc || !workspace || cache->ctx != ctx) return SLIM_ERR_INVALID_ARG;
   if (((uintptr_t)workspace & 255) || ((uintptr_t)q & 15) || ((uintptr_t)acc & 3)) return SLIM_ERR_INVALID_ARG;
-  if (ctx->e != ctx->d || ctx->xc_wk || cache->t_cap > kMaxRows) return SLIM_ERR_UNSUPPORTED;
+  if (ctx->kdtype == SLIM_FP4 || ctx->e != ctx->d || ctx->xc_wk || cache->t_cap > kMaxRows) return SLIM_ERR_UNSUPPORTED;
   if (!current_device_is(ctx)) return SLIM_ERR_INVALID_ARG;
   const WeightsLayout L = weights_layout(ctx, cache->batch, cache->t_cap);
   char* ws = static_cast<char*>(workspace);
@@ -829,7 +897,7 @@ slim_status slim_evict(slim_ctx* ctx, slim_cache* cache, const int32_t* lengths,
   if (!ctx || !cache || !lengths || !acc || !kept || !workspace || cache->ctx != ctx) return SLIM_ERR_INVALID_ARG;
   if (budget <= 0 || budget > kMaxRows || recent < 0 || recent > budget || ((uintptr_t)workspace & 255) || (((uintptr_t)acc | (uintptr_t)kept) & 3))
     return SLIM_ERR_INVALID_ARG;
-  if (cache->t_cap > kMaxRows) return SLIM_ERR_UNSUPPORTED;
+  if (ctx->kdtype == SLIM_FP4 || cache->t_cap > kMaxRows) return SLIM_ERR_UNSUPPORTED;
   if (!current_device_is(ctx)) return SLIM_ERR_INVALID_ARG;
   return launched(slim_launch_evict(ctx, cache, lengths, acc, budget, recent, kept, static_cast<float*>(workspace), (cudaStream_t)stream));
 }

@@ -1,0 +1,302 @@
+// Attention over packed prompts (slim_prompt_attention): preparation and the CUDA-core kernel.
+//
+//   o_i = sum_j p_ij v_j,  p_ij = softmax_j(R(i) q_i . R(j) k_j / sqrt(d_k)),  j <= i + nk - nq where causal
+//
+// Preparation (one kernel): rotated queries and keys into the workspace, each once instead of once a tile that reads them,
+// and the list of query tiles, most keys first, so that the last tiles to start are the short ones.
+// attn_kernel: one CTA a (tile of 64 query rows, head); online softmax over tiles of 64 keys, everything float32.
+#include <cuda_fp16.h>
+
+#include "slim_attn.h"
+
+namespace {
+
+constexpr int THREADS = 256;
+constexpr int BINS = 64;
+
+// ------------------------------------------------------------------------------------------------ preparation
+// The list of query tiles, by one CTA: a counting sort on the number of keys.
+__device__ void plan_tiles(const SlimAttn& a, int* s_mem) {
+  int* s_prefix = s_mem;                            // [batch + 1] tiles before a sequence
+  int* s_bin = s_mem + a.batch + 1;                 // [BINS]
+  const int tid = threadIdx.x;
+  for (int b = tid; b < a.batch; b += THREADS) s_prefix[b + 1] = (slim_attn_seq(a, b).nq + a.tile_rows - 1) / a.tile_rows;
+  if (tid == 0) s_prefix[0] = 0;
+  if (tid < BINS) s_bin[tid] = 0;
+  __syncthreads();
+  if (tid < 32) {
+    const int chunk = (a.batch + 31) / 32, lo = tid * chunk, hi = min(a.batch, lo + chunk);
+    int sum = 0;
+    for (int b = lo; b < hi; ++b) sum += s_prefix[b + 1];
+    int incl = sum;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int v = __shfl_up_sync(0xffffffffu, incl, o);
+      if (tid >= o) incl += v;
+    }
+    int run = incl - sum;
+    for (int b = lo; b < hi; ++b) { run += s_prefix[b + 1]; s_prefix[b + 1] = run; }
+  }
+  __syncthreads();
+  const int n = min(s_prefix[a.batch], a.most_tiles);         // (more only where sequences overlap)
+  if (tid == 0 && n < s_prefix[a.batch]) atomicMax(a.status, (int)SLIM_ERR_CAPACITY);
+  for (int pass = 0; pass < 2; ++pass) {
+    for (int g = tid; g < n; g += THREADS) {
+      int lo = 0, hi = a.batch;
+      while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (s_prefix[mid] <= g) lo = mid; else hi = mid;
+      }
+      const SlimSeq s = slim_attn_seq(a, lo);
+      const int row = (g - s_prefix[lo]) * a.tile_rows;
+      const int keys = slim_attn_keys(a, s, min(s.nq, row + a.tile_rows) - 1);
+      const int bin = BINS - 1 - (int)((long long)keys * (BINS - 1) / max(a.max_k, 1));
+      if (pass == 0) atomicAdd(&s_bin[bin], 1);
+      else a.tiles[atomicAdd(&s_bin[bin], 1)] = make_int4(lo, row, 0, 0);
+    }
+    __syncthreads();
+    if (pass == 0 && tid == 0) {
+      int run = 0;
+      for (int i = 0; i < BINS; ++i) { const int c = s_bin[i]; s_bin[i] = run; run += c; }
+      *a.n_tiles = n;
+    }
+    __syncthreads();
+  }
+}
+
+// Position of packed row r among the queries (keys); -1: it belongs to no sequence.
+__device__ int packed_position(const SlimAttn& a, int r, bool query) {
+  const int32_t* cu = query ? a.cu_q : a.cu_k;
+  int lo = 0, hi = a.batch;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (cu[mid] <= r) lo = mid; else hi = mid;
+  }
+  const SlimSeq s = slim_attn_seq(a, lo);
+  if (query) return r >= s.q0 && r < s.q0 + s.nq ? r - s.q0 + s.nk - s.nq : -1;
+  return r >= s.k0 && r < s.k0 + s.nk ? r - s.k0 : -1;
+}
+
+// One warp a packed row: all its heads, rotated.  A query before the first key (negative position) attends nothing.
+template <bool F32>
+__device__ void rotate_row(const SlimAttn& a, int r, bool query) {
+  const int lane = threadIdx.x & 31, heads = query ? a.H : a.KV;
+  const int pos = packed_position(a, r, query);
+  if (pos < 0) return;
+  const size_t at = (size_t)r * heads * a.d_k;
+  const void* src = query ? a.q : a.k;
+  void* dst = query ? a.qr : a.kr;
+  for (int j = lane; j < a.half; j += 32) {
+    const float2 cs = a.rope_base ? slim_attn_turn(a, pos, j) : make_float2(1.f, 0.f);
+    for (int h = 0; h < heads; ++h) {
+      const size_t i = at + (size_t)h * a.d_k + j;
+      const float x1 = slim_attn_ld(src, i, F32), x2 = slim_attn_ld(src, i + a.half, F32);
+      reinterpret_cast<float*>(dst)[i] = a.rope_base ? x1 * cs.x + x2 * cs.y : x1;
+      reinterpret_cast<float*>(dst)[i + a.half] = a.rope_base ? x2 * cs.x - x1 * cs.y : x2;
+    }
+  }
+}
+
+template <bool F32>
+__global__ void __launch_bounds__(THREADS) attn_prepare_kernel(const __grid_constant__ SlimAttn a) {
+  extern __shared__ int s_mem[];
+  slim_pdl_trigger();
+  slim_pdl_wait();
+  if (blockIdx.x == 0) { plan_tiles(a, s_mem); return; }
+  const int warps = (gridDim.x - 1) * (THREADS / 32);
+  for (int r = (blockIdx.x - 1) * (THREADS / 32) + (threadIdx.x >> 5); r < a.total_q + a.total_k; r += warps)
+    rotate_row<F32>(a, r < a.total_q ? r : r - a.total_q, r < a.total_q);
+}
+
+// ------------------------------------------------------------------------------------------------ CUDA cores
+constexpr int TR = SLIM_ATTN_ROWS, TK = 64;
+// DKP: the head width rounded up to a multiple of 64, columns behind d_k are zero.
+// Thread (ty, tx) = (tid / 16, tid % 16): rows 4 ty .. 4 ty + 3; scores of keys tx, tx + 16, ..; outputs 4 tx + 64 c.
+template <int DKP, bool F32>
+__global__ void __launch_bounds__(THREADS) attn_kernel(const __grid_constant__ SlimAttn a) {
+  constexpr int PQ = DKP + 4, PP = TK + 4;                       // pitches that spread rows over the banks
+  constexpr int NC = DKP / 64;
+  extern __shared__ __align__(16) float smem[];
+  float* s_q = smem;                                             // [TR][PQ]
+  float* s_k = s_q + TR * PQ;                                    // [TK][PQ]
+  float* s_v = s_k + TK * PQ;                                    // [TK][DKP]
+  float* s_p = s_v + TK * DKP;                                   // [TR][PP]
+  slim_pdl_trigger();
+  slim_pdl_wait();
+  const int item = blockIdx.x / a.H, h = blockIdx.x % a.H;
+  if (item >= *a.n_tiles) return;
+  const int4 tile = a.tiles[item];
+  const SlimSeq s = slim_attn_seq(a, tile.x);
+  const int row0 = tile.y, rows = min(TR, s.nq - row0), dk = a.d_k, kvh = h / (a.H / a.KV);
+  const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
+  const float* qr = reinterpret_cast<const float*>(a.qr) + ((size_t)(s.q0 + row0) * a.H + h) * dk;
+  const float* kr = reinterpret_cast<const float*>(a.kr) + ((size_t)s.k0 * a.KV + kvh) * dk;
+  for (int e = tid; e < TR * DKP; e += THREADS) {
+    const int r = e / DKP, c = e % DKP;
+    s_q[r * PQ + c] = r < rows && c < dk ? qr[(size_t)r * a.H * dk + c] * a.qscale : 0.f;
+  }
+  int lim[4];
+  float m[4], l[4], acc[4][NC][4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    lim[i] = slim_attn_keys(a, s, row0 + ty * 4 + i);
+    m[i] = -INFINITY; l[i] = 0.f;
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
+#pragma unroll
+      for (int x = 0; x < 4; ++x) acc[i][c][x] = 0.f;
+  }
+  const int keys = slim_attn_keys(a, s, row0 + rows - 1);
+  for (int t0 = 0; t0 < keys; t0 += TK) {
+    __syncthreads();
+    for (int e = tid; e < TK * DKP; e += THREADS) {
+      const int r = e / DKP, c = e % DKP;
+      const bool in = t0 + r < keys && c < dk;
+      s_k[r * PQ + c] = in ? kr[(size_t)(t0 + r) * a.KV * dk + c] : 0.f;
+      s_v[r * DKP + c] = in ? slim_attn_ld(a.v, ((size_t)(s.k0 + t0 + r) * a.KV + kvh) * dk + c, a.v32) : 0.f;
+    }
+    __syncthreads();
+    float sv[4][4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) sv[i][j] = 0.f;
+#pragma unroll 4
+    for (int c = 0; c < DKP; c += 4) {
+      float4 qv[4], kv[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) qv[i] = *reinterpret_cast<const float4*>(s_q + (ty * 4 + i) * PQ + c);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) kv[j] = *reinterpret_cast<const float4*>(s_k + (tx + 16 * j) * PQ + c);
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          sv[i][j] = fmaf(qv[i].x, kv[j].x, sv[i][j]); sv[i][j] = fmaf(qv[i].y, kv[j].y, sv[i][j]);
+          sv[i][j] = fmaf(qv[i].z, kv[j].z, sv[i][j]); sv[i][j] = fmaf(qv[i].w, kv[j].w, sv[i][j]);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      float mx = m[i];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        if (t0 + tx + 16 * j >= lim[i]) sv[i][j] = -INFINITY;
+        mx = fmaxf(mx, sv[i][j]);
+      }
+#pragma unroll
+      for (int o = 8; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+      const float alpha = mx == m[i] ? 1.f : exp2f(m[i] - mx);
+      float ps = 0.f;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const float p = t0 + tx + 16 * j >= lim[i] ? 0.f : exp2f(sv[i][j] - mx);
+        s_p[(ty * 4 + i) * PP + tx + 16 * j] = p;
+        ps += p;
+      }
+#pragma unroll
+      for (int o = 8; o > 0; o >>= 1) ps += __shfl_xor_sync(0xffffffffu, ps, o);
+      l[i] = l[i] * alpha + ps;
+      m[i] = mx;
+#pragma unroll
+      for (int c = 0; c < NC; ++c)
+#pragma unroll
+        for (int x = 0; x < 4; ++x) acc[i][c][x] *= alpha;
+    }
+    __syncwarp();                                                // a row's probabilities come from its own half warp
+#pragma unroll 2
+    for (int t = 0; t < TK; t += 4) {
+      float pv[4][4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float4 v = *reinterpret_cast<const float4*>(s_p + (ty * 4 + i) * PP + t);
+        pv[i][0] = v.x; pv[i][1] = v.y; pv[i][2] = v.z; pv[i][3] = v.w;
+      }
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+          const float4 v = *reinterpret_cast<const float4*>(s_v + (t + u) * DKP + c * 64 + tx * 4);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            acc[i][c][0] = fmaf(pv[i][u], v.x, acc[i][c][0]); acc[i][c][1] = fmaf(pv[i][u], v.y, acc[i][c][1]);
+            acc[i][c][2] = fmaf(pv[i][u], v.z, acc[i][c][2]); acc[i][c][3] = fmaf(pv[i][u], v.w, acc[i][c][3]);
+          }
+        }
+    }
+  }
+  bool bad[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int r = ty * 4 + i;
+    const float inv = lim[i] > 0 ? 1.f / l[i] : 0.f;
+    bad[i] = false;
+    if (r >= rows) continue;
+    const size_t at = ((size_t)(s.q0 + row0 + r) * a.H + h) * dk;
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        const int col = c * 64 + tx * 4 + x;
+        const float y = lim[i] > 0 ? acc[i][c][x] * inv : 0.f;
+        if (col < dk) {
+          bad[i] |= !(fabsf(y) <= 3.4028234663852886e38f);
+          if (F32) reinterpret_cast<float*>(a.o)[at + col] = y;
+          else reinterpret_cast<__nv_bfloat16*>(a.o)[at + col] = __float2bfloat16_rn(y);
+        }
+      }
+  }
+  // rows with a number that is not finite: once more, from what they attend alone
+  __syncwarp();
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const unsigned any = __ballot_sync(0xffffffffu, bad[i]);
+    const int r = (ty & ~1) * 4 + i;                             // the warp's rows: 4 of its lower half, 4 of its upper
+    if (any & 0x0000ffffu) slim_attn_row(a, tile.x, row0 + r, h);
+    if (any & 0xffff0000u) slim_attn_row(a, tile.x, row0 + r + 4, h);
+  }
+}
+
+template <int DKP>
+cudaError_t launch_attn(const SlimAttn& a, int most_tiles, cudaStream_t st) {
+  const size_t smem = sizeof(float) * (TR * (DKP + 4) + TK * (DKP + 4) + TK * DKP + TR * (TK + 4));
+  auto kern = a.f32 ? attn_kernel<DKP, true> : attn_kernel<DKP, false>;
+  cudaError_t e = cudaFuncSetAttribute((const void*)kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  if (e != cudaSuccess) return e;
+  return slim_launch_pdl(kern, dim3((unsigned)(most_tiles * a.H)), dim3(THREADS), smem, st, a);
+}
+
+inline size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
+
+}  // namespace
+
+SlimAttnLayout slim_attn_layout(const slim_ctx* ctx, int kv_heads, int batch, int total_q, int total_k) {
+  SlimAttnLayout L;
+  size_t off = 0;
+  L.qr = off; off = align256(off + 4 * (size_t)total_q * ctx->d);
+  L.kr = off; off = align256(off + 4 * (size_t)total_k * kv_heads * ctx->d_k);
+  L.vb = off; off = align256(off + (slim_attn_tc_ok(ctx) ? 2 * (size_t)total_k * kv_heads * ctx->d_k : 0));
+  L.tiles = off; off = align256(off + sizeof(int4) * ((size_t)total_q / SLIM_ATTN_ROWS + batch + 1));
+  L.n_tiles = off; off = align256(off + sizeof(int));
+  L.total = off;
+  return L;
+}
+
+int slim_attn_tc_ok(const slim_ctx*) { return 0; }
+
+cudaError_t slim_launch_attn(const slim_ctx* ctx, SlimAttn a, char* ws, int tc, cudaStream_t st) {
+  const SlimAttnLayout L = slim_attn_layout(ctx, a.KV, a.batch, a.total_q, a.total_k);
+  a.qr = ws + L.qr; a.kr = ws + L.kr; a.vb = ws + L.vb;
+  a.tiles = reinterpret_cast<int4*>(ws + L.tiles);
+  a.n_tiles = reinterpret_cast<int*>(ws + L.n_tiles);
+  a.tile_rows = SLIM_ATTN_ROWS;
+  const int most = a.most_tiles = a.total_q / a.tile_rows + a.batch;
+  const int rows = a.total_q + a.total_k;
+  const int blocks = 1 + (int)((rows + 7ll) / 8 < 8ll * ctx->num_sms ? (rows + 7ll) / 8 : 8ll * ctx->num_sms);
+  const size_t smem = sizeof(int) * (a.batch + 1 + BINS);
+  cudaError_t e = a.f32 ? slim_launch_pdl(attn_prepare_kernel<true>, dim3(blocks), dim3(THREADS), smem, st, a)
+                        : slim_launch_pdl(attn_prepare_kernel<false>, dim3(blocks), dim3(THREADS), smem, st, a);
+  if (e != cudaSuccess) return e;
+  return a.d_k <= 64 ? launch_attn<64>(a, most, st) : a.d_k <= 128 ? launch_attn<128>(a, most, st)
+         : a.d_k <= 192 ? launch_attn<192>(a, most, st) : launch_attn<256>(a, most, st);
+}

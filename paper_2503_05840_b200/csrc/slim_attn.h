@@ -1,0 +1,125 @@
+// Attention over packed prompts (slim_prompt_attention): what its kernels share.
+#pragma once
+#include "slim_internal.h"
+
+// Arguments and scratch of one call.
+struct SlimAttn {
+  int H, KV, d_k, half;          // query heads, key heads (H / KV query heads share one), head width and half of it
+  int batch, total_q, total_k, max_k, causal;
+  int f32, v32;                  // types of q, k and o (else bf16), and of v
+  float qscale;                  // log2(e) / sqrt(d_k)
+  const void* q;                 // [total_q][H][d_k]
+  const void* k;                 // [total_k][KV][d_k]
+  const void* v;                 // [total_k][KV][d_k]
+  void* o;                       // [total_q][H][d_k]
+  const int32_t* cu_q;           // [batch + 1]
+  const int32_t* cu_k;           // [batch + 1]
+  const float2* rope_base;       // position tables; NULL without rotation
+  const float2* rope_off;
+  int* status;
+  // workspace
+  void* qr;                      // rotated queries and keys, layout of q and k: float32 (CUDA cores) or float16 (tensor cores)
+  void* kr;
+  void* vb;                      // tensor cores with float32 values: the values as bf16
+  int4* tiles;                   // (sequence, first query row, -, -), most keys first
+  int* n_tiles;
+  int tile_rows, most_tiles;
+};
+
+struct SlimAttnLayout { size_t qr, kr, vb, tiles, n_tiles, total; };
+
+constexpr int SLIM_ATTN_ROWS = 64;       // query rows of a tile, CUDA cores
+constexpr int SLIM_ATTN_TC_ROWS = 256;   // tensor cores: two tiles of 128
+
+int slim_attn_tc_ok(const slim_ctx* ctx);
+cudaError_t slim_launch_attn_tc(const slim_ctx* ctx, const SlimAttn& a, int most_tiles, cudaStream_t st);
+SlimAttnLayout slim_attn_layout(const slim_ctx* ctx, int kv_heads, int batch, int total_q, int total_k);
+cudaError_t slim_launch_attn(const slim_ctx* ctx, SlimAttn a, char* ws, int tc, cudaStream_t st);
+
+#ifdef __CUDACC__
+struct SlimSeq { int q0, nq, k0, nk; };
+// Sequence b; none (nq = 0) where its starts do not ascend within the arrays or it has more than max_k keys.
+__device__ __forceinline__ SlimSeq slim_attn_seq(const SlimAttn& a, int b) {
+  SlimSeq s;
+  s.q0 = a.cu_q[b]; s.k0 = a.cu_k[b];
+  const int q1 = a.cu_q[b + 1], k1 = a.cu_k[b + 1];
+  if (s.q0 < 0 || q1 < s.q0 || q1 > a.total_q || s.k0 < 0 || k1 < s.k0 || k1 > a.total_k || k1 - s.k0 > a.max_k) {
+    atomicMax(a.status, (int)SLIM_ERR_CAPACITY);
+    s.nq = s.nk = 0;
+    return s;
+  }
+  s.nq = q1 - s.q0; s.nk = k1 - s.k0;
+  return s;
+}
+// Keys that query row i of a sequence attends: the first so many.
+__device__ __forceinline__ int slim_attn_keys(const SlimAttn& a, const SlimSeq& s, int i) {
+  return a.causal ? max(0, min(s.nk, i + 1 + s.nk - s.nq)) : s.nk;
+}
+__device__ __forceinline__ float2 slim_attn_turn(const SlimAttn& a, int pos, int j) {
+  const float2 cb = __ldg(a.rope_base + (size_t)(pos / SLIM_TT) * a.half + j), co = __ldg(a.rope_off + (pos % SLIM_TT) * a.half + j);
+  return make_float2(cb.x * co.x - cb.y * co.y, cb.y * co.x + cb.x * co.y);
+}
+__device__ __forceinline__ float slim_attn_ld(const void* p, size_t i, int f32) {
+  return f32 ? __ldg(reinterpret_cast<const float*>(p) + i) : __bfloat162float(__ldg(reinterpret_cast<const __nv_bfloat16*>(p) + i));
+}
+
+// One output row by one warp, from the inputs themselves, in float32: for the rows that the tiled kernels leave with a
+// number that is not finite.  Those come from keys and values that the row does not attend but shares a tile with
+// (0 times infinity), from keys beyond float16, or from what the row does attend; here only the last reach it.
+static __device__ __noinline__ void slim_attn_row(const SlimAttn& a, int b, int i, int h) {
+  const SlimSeq s = slim_attn_seq(a, b);
+  const int lane = threadIdx.x & 31, kvh = h / (a.H / a.KV), dk = a.d_k, half = a.half;
+  const int n = slim_attn_keys(a, s, i), qpos = i + s.nk - s.nq;
+  const size_t qi = ((size_t)(s.q0 + i) * a.H + h) * dk;
+  float m = -INFINITY, l = 0.f, acc[8];
+#pragma unroll
+  for (int x = 0; x < 8; ++x) acc[x] = 0.f;
+  for (int t0 = 0; t0 < n; t0 += 32) {
+    const int t = t0 + lane;
+    float sv = -INFINITY;
+    if (t < n) {
+      const size_t ki = ((size_t)(s.k0 + t) * a.KV + kvh) * dk;
+      sv = 0.f;
+      for (int j = 0; j < half; ++j) {
+        float q1 = slim_attn_ld(a.q, qi + j, a.f32), q2 = slim_attn_ld(a.q, qi + j + half, a.f32);
+        float k1 = slim_attn_ld(a.k, ki + j, a.f32), k2 = slim_attn_ld(a.k, ki + j + half, a.f32);
+        if (a.rope_base) {
+          const float2 cq = slim_attn_turn(a, qpos, j), ck = slim_attn_turn(a, t, j);
+          const float x1 = q1 * cq.x + q2 * cq.y, x2 = q2 * cq.x - q1 * cq.y, y1 = k1 * ck.x + k2 * ck.y, y2 = k2 * ck.x - k1 * ck.y;
+          q1 = x1; q2 = x2; k1 = y1; k2 = y2;
+        }
+        sv += q1 * k1 + q2 * k2;
+      }
+      sv *= a.qscale;
+    }
+    float mx = sv;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+    const float m_new = fmaxf(m, mx);
+    const float p = sv == -INFINITY ? 0.f : exp2f(sv - m_new);
+    const float alpha = m == m_new ? 1.f : exp2f(m - m_new);
+    float ps = p;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) ps += __shfl_xor_sync(0xffffffffu, ps, o);
+    l = l * alpha + ps;
+    m = m_new;
+#pragma unroll
+    for (int x = 0; x < 8; ++x) acc[x] *= alpha;
+    for (int u = 0; u < 32 && t0 + u < n; ++u) {
+      const float pu = __shfl_sync(0xffffffffu, p, u);
+      const size_t vi = ((size_t)(s.k0 + t0 + u) * a.KV + kvh) * dk;
+#pragma unroll
+      for (int x = 0; x < 8; ++x)
+        if (lane + 32 * x < dk) acc[x] = fmaf(pu, slim_attn_ld(a.v, vi + lane + 32 * x, a.v32), acc[x]);
+    }
+  }
+#pragma unroll
+  for (int x = 0; x < 8; ++x) {
+    if (lane + 32 * x < dk) {
+      const float y = n > 0 ? acc[x] / l : 0.f;
+      if (a.f32) reinterpret_cast<float*>(a.o)[qi + lane + 32 * x] = y;
+      else reinterpret_cast<__nv_bfloat16*>(a.o)[qi + lane + 32 * x] = __float2bfloat16_rn(y);
+    }
+  }
+}
+#endif

@@ -25,6 +25,7 @@ struct SlimDecodeParams {
   int dtype;                     // slim_dtype of q and W_KV (f32 or bf16)
   int kdtype;                    // slim_dtype of the cache elements (f32, bf16 or fp8 codes)
   const signed char* k_exp;      // fp8 cache: [batch][t_cap][H] exponents (stored key = code * 2^exponent), else NULL
+  const unsigned char* k_sc4;    // 4-bit cache: the scales behind the codes (slim_fp4.cuh), else NULL
   int workers;                   // context-split workers (W)
   int cl;                        // tensor-core path: CTAs per worker (1 or 2)
   int min_tiles;                 // a worker gets at least this many tiles if it gets any
@@ -42,6 +43,7 @@ struct SlimDecodeParams {
   int* unit_flags;               // [units][2]   1 = unit must be redone exactly (one word per CTA of the pair)
   float* u;                      // [batch][H][d] combined
   float* o;                      // [batch][d]
+  int o_bf16;                    // o holds bf16 values, rounded once as they are stored (slim_store_o)
   int* status;                   // sticky device status word
   int* any_flag;                 // set to 1 by a kernel that flags a unit
   const float* ext_scores;       // X-cache scheme: precomputed softmax arguments [batch][H][t_cap] (else NULL)
@@ -64,7 +66,7 @@ struct slim_old_table { float2* dev; slim_old_table* next; };
 struct slim_ctx {
   int d, H, d_k, dtype;          // d: width of a cache row; dtype: q and W_KV (f32 or bf16)
   int e;                         // width of q and o: H * d_k; differs from d only for an X-cache context with non-square projections
-  int kdtype;                    // cache elements: dtype, or SLIM_FP8
+  int kdtype;                    // cache elements: dtype, SLIM_FP8 or SLIM_FP4
   double rope_theta;
   int device;
   int num_sms;
@@ -108,6 +110,7 @@ struct slim_cache {
   slim_ctx* ctx;
   void* k;
   signed char* k_exp;            // fp8 cache: exponents behind the codes, else NULL
+  unsigned char* k_sc4;          // 4-bit cache: scales behind the codes, else NULL
   int batch, t_cap;              // paged: t_cap = max_pages * page_rows
   const int32_t* block_table;    // paged: device [batch][max_pages]; NULL for a contiguous cache
   int page_rows, max_pages, num_pages;
@@ -170,6 +173,12 @@ cudaError_t slim_proj_make_wmap(slim_ctx* ctx);
 cudaError_t slim_launch_proj(const slim_ctx* ctx, const SlimDecodeParams& p, unsigned char* u_tiled, float* u32, float* su,
                              cudaStream_t st);
 cudaError_t slim_launch_sum_slices(const float* o_part, float* o, int n, int nsplit, cudaStream_t st);
+#ifdef __CUDACC__
+__device__ __forceinline__ void slim_store_o(float* o, int o_bf16, size_t i, float v) {
+  if (o_bf16) reinterpret_cast<__nv_bfloat16*>(o)[i] = __float2bfloat16_rn(v);
+  else o[i] = v;
+}
+#endif
 
 // ---- programmatic dependent launch ---------------------------------------------
 // The kernels of one decode step run back to back on one stream.  Launched with
@@ -209,6 +218,12 @@ cudaError_t slim_launch_rank_combine(const slim_ctx* ctx, const SlimDecodeParams
 // prompt phase: V = K W_KV for n rows (slim_prompt.cu)
 cudaError_t slim_launch_values(const slim_ctx* ctx, const void* K, int n, float* V, cudaStream_t st,
                                const slim_cache* cache = nullptr, const int32_t* positions = nullptr, int n_new = 0);
+
+// packed rows into and out of a float32, bf16 or 4-bit cache, the uniform append of a 4-bit cache (slim_rows.cu)
+cudaError_t slim_launch_rows(const slim_ctx* ctx, const slim_cache* c, void* wide, const int32_t* positions, const int32_t* cu, int total,
+                             int to_cache, cudaStream_t st);
+cudaError_t slim_launch_append_fp4(const slim_ctx* ctx, const slim_cache* c, const void* k_new, const int32_t* positions, int n_new,
+                                   int pos_is_length, cudaStream_t st);
 
 // drafted tokens (slim_tree.cu, slim_tree_tc.cu, slim_draft.cu)
 cudaError_t slim_tree_make_table(slim_ctx* ctx);

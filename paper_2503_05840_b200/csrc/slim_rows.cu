@@ -1,0 +1,226 @@
+// Rows into and out of a K-cache: packed rows of several sequences (slim_append_rows, slim_read_rows) for float32, bf16
+// and 4-bit caches, and the uniform append of a 4-bit cache (slim_append_k, slim_decode_step, slim_prefill).
+//
+// Both directions are bound by HBM: a row of d bf16 keys is read (2 d bytes) and d/2 + d/32 bytes are written, or the
+// other way round.  A warp takes 256 columns of a row at a time: 16 bytes a lane on the wide side, one 32-bit word of
+// eight codes on the other; four lanes share a scale.
+#include "slim_fp4.cuh"
+
+namespace {
+
+struct RowsArgs {
+  void* wide;                    // [total][d] packed rows (f32 or bf16): source of an append, destination of a read
+  const int32_t* positions;      // [batch] first cache row of a sequence
+  const int32_t* cu;             // [batch + 1] packed row where a sequence begins; NULL: n_new rows each
+  int n_new, pos_is_length;      // uniform form; positions hold the lengths after the append
+  int total, batch, d, t_cap;
+  unsigned char* codes;          // cache rows (f32 and bf16 caches: the keys)
+  unsigned char* scales;
+  int pitch, spitch;             // bytes of a row
+  const int32_t* block_table;
+  int page_rows, max_pages, num_pages;
+  int* status;
+  int parts, chunks;             // a warp's share of a row: chunks of 256 columns (copies: of 512 bytes)
+};
+
+// Cache row of packed row r; -1 if it has none (outside every sequence, or not to be touched).  All lanes of a warp agree.
+__device__ long long rows_target(const RowsArgs& a, int r) {
+  int b, i, n;
+  if (a.cu) {
+    int lo = 0, hi = a.batch;                       // the last sequence that begins at or before r
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (a.cu[mid] <= r) lo = mid; else hi = mid;
+    }
+    b = lo;
+    const int first = a.cu[b], end = a.cu[b + 1];
+    if (first < 0 || r < first || r >= end || end > a.total) return -1;
+    i = r - first; n = end - first;
+  } else {
+    b = r / a.n_new; i = r - b * a.n_new; n = a.n_new;
+  }
+  int pos = a.positions[b];
+  if (a.pos_is_length) {
+    if (pos <= 0) return -1;
+    pos -= 1;
+  }
+  if (pos < 0 || n > a.t_cap || pos > a.t_cap - n) { atomicMax(a.status, (int)SLIM_ERR_CAPACITY); return -1; }
+  const int t = pos + i;
+  if (!a.block_table) return (long long)b * a.t_cap + t;
+  const int pg = a.block_table[(size_t)b * a.max_pages + t / a.page_rows];
+  if (pg < 0 || pg >= a.num_pages) { atomicMax(a.status, (int)SLIM_ERR_CAPACITY); return -1; }
+  return (long long)pg * a.page_rows + t % a.page_rows;
+}
+
+// Starts of packed sequences that do not ascend from 0 to at most `total` are reported (their rows are left out above).
+__device__ void rows_check(const RowsArgs& a) {
+  if (!a.cu || blockIdx.x != 0) return;
+  for (int b = threadIdx.x; b < a.batch; b += blockDim.x)
+    if (a.cu[b] < 0 || a.cu[b + 1] < a.cu[b] || a.cu[b + 1] > a.total) atomicMax(a.status, (int)SLIM_ERR_CAPACITY);
+}
+
+// bf16 rows -> 4 bits
+__global__ void __launch_bounds__(256) rows_quantise_kernel(const RowsArgs a) {
+  slim_pdl_trigger();
+  slim_pdl_wait();
+  rows_check(a);
+  const int lane = threadIdx.x & 31;
+  const long long w = (long long)blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5);
+  const long long rr = w / a.parts;
+  if (rr >= a.total) return;
+  const int part = (int)(w - rr * a.parts);
+  const long long row = rows_target(a, (int)rr);
+  if (row < 0) return;
+  const unsigned short* src = reinterpret_cast<const unsigned short*>(a.wide) + (size_t)rr * a.d;
+  unsigned char* dst = a.codes + (size_t)row * a.pitch;
+  unsigned char* sdst = a.scales + (size_t)row * a.spitch;
+  const bool whole = (a.d & 7) == 0 && ((uintptr_t)a.wide & 15) == 0;
+#pragma unroll 4
+  for (int c = 0; c < a.chunks; ++c) {
+    const int col = (part * a.chunks + c) * 256 + lane * 8;
+    uint32_t w4[4] = {0u, 0u, 0u, 0u};
+    if (col < a.d) {
+      if (whole) {
+        const uint4 v = __ldcs(reinterpret_cast<const uint4*>(src + col));
+        w4[0] = v.x; w4[1] = v.y; w4[2] = v.z; w4[3] = v.w;
+      } else {
+        for (int e = 0; e < 8 && col + e < a.d; ++e) w4[e >> 1] |= (uint32_t)src[col + e] << (16 * (e & 1));
+      }
+    }
+    float k[8], amax = 0.f;
+    bool bad = false;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      k[e] = __uint_as_float(e & 1 ? w4[e >> 1] & 0xffff0000u : w4[e >> 1] << 16);
+      bad |= !(fabsf(k[e]) <= 3.4028234663852886e38f);
+      amax = fmaxf(amax, fabsf(k[e]));
+    }
+#pragma unroll
+    for (int o = 1; o < 4; o <<= 1) {
+      amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
+      bad |= __shfl_xor_sync(0xffffffffu, (int)bad, o) != 0;
+    }
+    const int sb = slim_fp4_scale_byte(amax, bad);
+    const float s = bad ? 1.f : slim_fp4_scale((unsigned char)sb);
+    uint32_t out = 0u;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) out |= (bad ? 0u : slim_fp4_code(k[e], s)) << (4 * e);
+    if (col < a.d) {
+      if (col + 8 <= a.d || whole) {
+        *reinterpret_cast<uint32_t*>(dst + (col >> 1)) = out;
+      } else {
+        for (int e = 0; 2 * e < a.d - col; ++e) dst[(col >> 1) + e] = (unsigned char)(out >> (8 * e));
+      }
+      if ((lane & 3) == 0) sdst[col / FP4_GROUP] = (unsigned char)sb;
+    }
+  }
+}
+
+// 4 bits -> bf16 rows (exact)
+__global__ void __launch_bounds__(256) rows_expand_kernel(const RowsArgs a) {
+  slim_pdl_trigger();
+  slim_pdl_wait();
+  rows_check(a);
+  const int lane = threadIdx.x & 31;
+  const long long w = (long long)blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5);
+  const long long rr = w / a.parts;
+  if (rr >= a.total) return;
+  const int part = (int)(w - rr * a.parts);
+  const long long row = rows_target(a, (int)rr);
+  if (row < 0) return;
+  unsigned short* dst = reinterpret_cast<unsigned short*>(a.wide) + (size_t)rr * a.d;
+  const unsigned char* src = a.codes + (size_t)row * a.pitch;
+  const unsigned char* ssrc = a.scales + (size_t)row * a.spitch;
+  const bool whole = (a.d & 7) == 0 && ((uintptr_t)a.wide & 15) == 0;
+#pragma unroll 4
+  for (int c = 0; c < a.chunks; ++c) {
+    const int col = (part * a.chunks + c) * 256 + lane * 8;
+    if (col >= a.d) continue;
+    const uint32_t w4 = __ldcs(reinterpret_cast<const unsigned int*>(src + (col >> 1)));      // (rows are padded to 16 bytes)
+    const float s = slim_fp4_scale(__ldg(ssrc + col / FP4_GROUP));
+    uint32_t out[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float lo = slim_fp4_value((w4 >> (8 * e)) & 15u) * s, hi = slim_fp4_value((w4 >> (8 * e + 4)) & 15u) * s;
+      const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+      out[e] = *reinterpret_cast<const uint32_t*>(&v);
+    }
+    if (whole) __stcs(reinterpret_cast<uint4*>(dst + col), make_uint4(out[0], out[1], out[2], out[3]));
+    else
+      for (int e = 0; e < 8 && col + e < a.d; ++e) dst[col + e] = (unsigned short)(out[e >> 1] >> (16 * (e & 1)));
+  }
+}
+
+// rows of a float32 or bf16 cache, to it or from it, in units of U bytes
+template <typename U>
+__global__ void __launch_bounds__(256) rows_copy_kernel(const RowsArgs a, int to_cache) {
+  slim_pdl_trigger();
+  slim_pdl_wait();
+  rows_check(a);
+  const int lane = threadIdx.x & 31;
+  const long long w = (long long)blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5);
+  const long long rr = w / a.parts;
+  if (rr >= a.total) return;
+  const int part = (int)(w - rr * a.parts);
+  const long long row = rows_target(a, (int)rr);
+  if (row < 0) return;
+  const int units = a.pitch / (int)sizeof(U);
+  U* cache = reinterpret_cast<U*>(a.codes + (size_t)row * a.pitch);
+  U* wide = reinterpret_cast<U*>(reinterpret_cast<unsigned char*>(a.wide) + (size_t)rr * a.pitch);
+  U* dst = to_cache ? cache : wide;
+  const U* src = to_cache ? wide : cache;
+#pragma unroll 4
+  for (int c = 0; c < a.chunks; ++c) {
+    const int i = (part * a.chunks + c) * 32 + lane;
+    if (i < units) dst[i] = src[i];
+  }
+}
+
+cudaError_t launch_rows(const slim_ctx* ctx, RowsArgs a, int to_cache, cudaStream_t st) {
+  if (a.total <= 0) return cudaSuccess;
+  const bool fp4 = ctx->kdtype == SLIM_FP4;
+  size_t unit = 16;
+  if (!fp4) while ((a.pitch % unit) || (((uintptr_t)a.wide | (uintptr_t)a.codes) % unit)) unit >>= 1;
+  const int span = fp4 ? 256 : 32;                                     // columns (units) a warp takes at a time
+  const int n = ((fp4 ? a.d : a.pitch / (int)unit) + span - 1) / span;
+  // Four chunks a warp keep four loads of a lane in flight; fewer where the rows alone would not give every SM 16 warps.
+  a.chunks = (long long)a.total * n >= 64ll * ctx->num_sms ? 4 : 1;
+  a.parts = (n + a.chunks - 1) / a.chunks;
+  const long long warps = (long long)a.total * a.parts;
+  const dim3 grid((unsigned)((warps + 7) / 8)), block(256);
+  if (fp4) return slim_launch_pdl(to_cache ? rows_quantise_kernel : rows_expand_kernel, grid, block, 0, st, a);
+  switch (unit) {
+    case 16: return slim_launch_pdl(rows_copy_kernel<uint4>, grid, block, 0, st, a, to_cache);
+    case 8: return slim_launch_pdl(rows_copy_kernel<uint2>, grid, block, 0, st, a, to_cache);
+    case 4: return slim_launch_pdl(rows_copy_kernel<uint32_t>, grid, block, 0, st, a, to_cache);
+    default: return slim_launch_pdl(rows_copy_kernel<unsigned short>, grid, block, 0, st, a, to_cache);
+  }
+}
+
+RowsArgs rows_args(const slim_ctx* ctx, const slim_cache* c, void* wide, const int32_t* positions) {
+  RowsArgs a = {};
+  a.wide = wide; a.positions = positions;
+  a.batch = c->batch; a.d = ctx->d; a.t_cap = c->t_cap;
+  a.codes = reinterpret_cast<unsigned char*>(c->k); a.scales = c->k_sc4;
+  a.pitch = ctx->kdtype == SLIM_FP4 ? slim_fp4_code_pitch(ctx->d) : ctx->d * (ctx->dtype == SLIM_BF16 ? 2 : 4);
+  a.spitch = slim_fp4_scale_pitch(ctx->d);
+  a.block_table = c->block_table; a.page_rows = c->page_rows; a.max_pages = c->max_pages; a.num_pages = c->num_pages;
+  a.status = ctx->status;
+  return a;
+}
+
+}  // namespace
+
+cudaError_t slim_launch_rows(const slim_ctx* ctx, const slim_cache* c, void* wide, const int32_t* positions, const int32_t* cu, int total,
+                             int to_cache, cudaStream_t st) {
+  RowsArgs a = rows_args(ctx, c, wide, positions);
+  a.cu = cu; a.total = total;
+  return launch_rows(ctx, a, to_cache, st);
+}
+
+cudaError_t slim_launch_append_fp4(const slim_ctx* ctx, const slim_cache* c, const void* k_new, const int32_t* positions, int n_new,
+                                   int pos_is_length, cudaStream_t st) {
+  RowsArgs a = rows_args(ctx, c, const_cast<void*>(k_new), positions);
+  a.n_new = n_new; a.pos_is_length = pos_is_length; a.total = c->batch * n_new;
+  return launch_rows(ctx, a, 1, st);
+}

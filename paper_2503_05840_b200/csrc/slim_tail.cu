@@ -123,14 +123,14 @@ __global__ void __launch_bounds__(256) slim_tail1_kernel(SlimDecodeParams p, int
 }
 
 __global__ void __launch_bounds__(256) slim_tail2_kernel(const float* __restrict__ o_part, float* __restrict__ o,
-                                                         int n, int nsplit) {
+                                                         int n, int nsplit, int o_bf16) {
   slim_pdl_trigger();
   slim_pdl_wait();
   const int i = blockIdx.x * blockDim.x + threadIdx.x;
   if (i >= n) return;
   float a = 0.f;
   for (int s = 0; s < nsplit; ++s) a += o_part[(size_t)s * n + i];
-  o[i] = a;
+  slim_store_o(o, o_bf16, i, a);
 }
 
 template <typename KT>
@@ -263,7 +263,7 @@ size_t slim_tail_opart_floats(int d, int e, int batch) {
 }
 
 cudaError_t slim_launch_sum_slices(const float* o_part, float* o, int n, int nsplit, cudaStream_t st) {
-  return slim_launch_pdl(slim_tail2_kernel, dim3((n + 255) / 256), dim3(256), 0, st, o_part, o, n, nsplit);
+  return slim_launch_pdl(slim_tail2_kernel, dim3((n + 255) / 256), dim3(256), 0, st, o_part, o, n, nsplit, 0);
 }
 
 cudaError_t slim_launch_tail(const slim_ctx* ctx, const SlimDecodeParams& p, cudaStream_t st) {
@@ -292,12 +292,13 @@ cudaError_t slim_launch_tail(const slim_ctx* ctx, const SlimDecodeParams& p, cud
   e = cudaGetLastError();
   if (e != cudaSuccess) return e;
   const int n = p.batch * p.e;
-  slim_tail2_kernel<<<(n + 255) / 256, 256, 0, st>>>(o_part, p.o, n, nsplit);
+  slim_tail2_kernel<<<(n + 255) / 256, 256, 0, st>>>(o_part, p.o, n, nsplit, p.o_bf16);
   return cudaGetLastError();
 }
 
 cudaError_t slim_launch_append(const slim_ctx* ctx, const slim_cache* c, const void* k_new,
                                const int32_t* positions, int n_new, int pos_is_length, cudaStream_t st) {
+  if (ctx->kdtype == SLIM_FP4) return slim_launch_append_fp4(ctx, c, k_new, positions, n_new, pos_is_length, st);
   dim3 grid(c->batch, n_new);
   if (ctx->kdtype == SLIM_FP8)
     return slim_launch_pdl(slim_append_fp8_kernel, grid, dim3(256), 0, st, (unsigned char*)c->k, c->k_exp,

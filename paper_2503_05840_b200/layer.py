@@ -56,11 +56,11 @@ class SlimLayer:
             raise ValueError(f"scratch: a Scratch on {self.device} is needed, e.g. another layer's .scratch")
         self.d, self.H, self.d_k, self.batch, self.t_cap = d, H, d_k, batch, t_cap
         self.dtype = dtype
-        # type of q, of new key rows and of W_KV; an "fp8" layer keeps only its cache in 8 bits
+        # type of q, of new key rows and of W_KV; an "fp8" ("fp4") layer keeps only its cache in 8 (4) bits
         self.tdtype = torch.float32 if dtype == "f32" else torch.bfloat16
         with torch.cuda.device(self.device):
-            self.ctx = B.slim_create(d, H, d_k, rope_theta, {"f32": B.SLIM_F32, "bf16": B.SLIM_BF16, "fp8": B.SLIM_FP8}[dtype])
-            if dtype == "fp8":     # codes [batch][t_cap][d], then the exponents: filled through append_k only
+            self.ctx = B.slim_create(d, H, d_k, rope_theta, {"f32": B.SLIM_F32, "bf16": B.SLIM_BF16, "fp8": B.SLIM_FP8, "fp4": B.SLIM_FP4}[dtype])
+            if dtype in ("fp8", "fp4"):     # codes of all rows, then their exponents (scales): filled through the append calls only
                 self.k = torch.zeros(B.slim_cache_bytes(self.ctx, batch, t_cap), dtype=torch.uint8, device=self.device)
             else:
                 self.k = torch.zeros((batch, t_cap, d), dtype=self.tdtype, device=self.device)
@@ -107,6 +107,66 @@ class SlimLayer:
         B.slim_decode_step(self.ctx, q, k_new, self.cache, lengths, o, self.workspace,
                            torch.cuda.current_stream(self.device).cuda_stream)
         return o
+
+    def decode_typed(self, q: torch.Tensor, lengths: torch.Tensor, k_new: "torch.Tensor | None" = None,
+                     o: "torch.Tensor | None" = None) -> torch.Tensor:
+        """decode, or with k_new decode_step, with o in its own type: float32, or bfloat16 (the default of a bf16 layer)."""
+        self._arg("q", q, (self.batch, self.d), self.tdtype)
+        self._arg("lengths", lengths, (self.batch,), torch.int32)
+        if k_new is not None:
+            self._arg("k_new", k_new, (self.batch, self.d), self.tdtype)
+        if o is None:
+            o = torch.empty((self.batch, self.d), dtype=self.tdtype, device=self.device)
+        elif o.dtype not in (torch.float32, torch.bfloat16):
+            raise ValueError(f"o: float32 or bfloat16 is needed, got {o.dtype}")
+        self._arg("o", o, (self.batch, self.d), o.dtype)
+        with torch.cuda.device(self.device):
+            B.slim_decode_typed(self.ctx, q, k_new, self.cache, lengths, o, B.SLIM_F32 if o.dtype == torch.float32 else B.SLIM_BF16,
+                                self.workspace, torch.cuda.current_stream(self.device).cuda_stream)
+        return o
+
+    # ---- packed prompts -----------------------------------------------------------
+    def prompt_attention(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_q: torch.Tensor, cu_k: torch.Tensor, max_k: int,
+                         causal: bool = True, o: "torch.Tensor | None" = None) -> torch.Tensor:
+        """Attention of packed prompts (binding.slim_prompt_attention): q [rows, H, d_k] (or [rows, d]), k and v [rows, heads, d_k]
+        with as many heads as divide H; v float32, or bfloat16 in a layer that is not float32.  Positions below the layer's t_cap are there;
+        longer prompts need binding.slim_reserve_positions."""
+        if q.dim() not in (2, 3) or k.dim() not in (2, 3):
+            raise ValueError("q, k: [rows, heads, d_k] or [rows, heads * d_k] is needed")
+        kv = k[0:1].numel() // self.d_k if k.shape[0] else self.H
+        self._arg("q", q, (q.shape[0],) + ((self.d,) if q.dim() == 2 else (self.H, self.d_k)), self.tdtype)
+        self._arg("k", k, (k.shape[0],) + ((kv * self.d_k,) if k.dim() == 2 else (kv, self.d_k)), self.tdtype)
+        if v.dtype not in (torch.float32, self.tdtype):
+            raise ValueError(f"v: {torch.float32} or {self.tdtype} is needed, got {v.dtype}")
+        self._arg("v", v, k.shape if v.dim() == k.dim() else (k.shape[0],) + ((kv * self.d_k,) if v.dim() == 2 else (kv, self.d_k)), v.dtype)
+        if cu_q.dim() != 1 or cu_q.numel() < 2:
+            raise ValueError("cu_q: [sequences + 1] is needed")
+        self._arg("cu_q", cu_q, cu_q.shape, torch.int32)
+        self._arg("cu_k", cu_k, cu_q.shape, torch.int32)
+        o = torch.empty_like(q) if o is None else self._arg("o", o, q.shape, self.tdtype)
+        n = cu_q.numel() - 1
+        with torch.cuda.device(self.device):
+            ws = self.scratch.take(B.slim_prompt_workspace_bytes(self.ctx, kv, n, q.shape[0], k.shape[0]))
+            B.slim_prompt_attention(self.ctx, q, k, v, B.SLIM_F32 if v.dtype == torch.float32 else B.SLIM_BF16, kv, cu_q, cu_k, n, q.shape[0],
+                                    k.shape[0], int(max_k), causal, o, ws, torch.cuda.current_stream(self.device).cuda_stream)
+        return o
+
+    def append_rows(self, k_new: torch.Tensor, positions: torch.Tensor, cu_rows: torch.Tensor) -> None:
+        """Packed rows [rows, d] of the layer's sequences into the cache (binding.slim_append_rows)."""
+        self._arg("k_new", k_new, (k_new.shape[0], self.d), self.tdtype)
+        self._arg("positions", positions, (self.batch,), torch.int32)
+        self._arg("cu_rows", cu_rows, (self.batch + 1,), torch.int32)
+        with torch.cuda.device(self.device):
+            B.slim_append_rows(self.ctx, self.cache, k_new, positions, cu_rows, k_new.shape[0], torch.cuda.current_stream(self.device).cuda_stream)
+
+    def read_rows(self, positions: torch.Tensor, cu_rows: torch.Tensor, rows: int, out: "torch.Tensor | None" = None) -> torch.Tensor:
+        """`rows` packed rows [rows, d] as the cache holds them (binding.slim_read_rows)."""
+        self._arg("positions", positions, (self.batch,), torch.int32)
+        self._arg("cu_rows", cu_rows, (self.batch + 1,), torch.int32)
+        out = torch.zeros((rows, self.d), dtype=self.tdtype, device=self.device) if out is None else self._arg("out", out, (rows, self.d), self.tdtype)
+        with torch.cuda.device(self.device):
+            B.slim_read_rows(self.ctx, self.cache, positions, cu_rows, int(rows), out, torch.cuda.current_stream(self.device).cuda_stream)
+        return out
 
     # ---- drafted tokens, cache budget -------------------------------------------
     def _arg(self, name: str, x: torch.Tensor, shape, dtype) -> torch.Tensor:

@@ -1,0 +1,270 @@
+"""Attention over packed prompts against the float64 definition."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import prompt_oracle as po
+from paper_2503_05840_b200 import binding as B
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+def _starts(n, first=0):
+    return np.concatenate([[first], first + np.cumsum(n)]).astype(np.int32)
+
+
+class Case:
+    """Inputs of a packed batch with `lead` rows in front of the first and behind the last sequence."""
+
+    def __init__(self, dtype, H, KV, dk, theta, nq, nk, v32=True, seed=0, lead=3, max_k=None):
+        g = torch.Generator().manual_seed(seed)
+        self.H, self.KV, self.dk, self.theta, self.nq, self.nk = H, KV, dk, theta, nq, nk
+        self.f32, self.v32 = dtype == "f32", v32
+        td = torch.float32 if self.f32 else torch.bfloat16
+        self.tq, self.tk = sum(nq) + 2 * lead, sum(nk) + 2 * lead
+        self.cu_q, self.cu_k = _starts(nq, lead), _starts(nk, lead)
+        self.q = torch.randn(self.tq, H, dk, generator=g).to(td)
+        self.k = torch.randn(self.tk, KV, dk, generator=g).to(td)
+        self.v = torch.randn(self.tk, KV, dk, generator=g).to(torch.float32 if v32 else td)
+        self.max_k = max(nk) if max_k is None else max_k
+        self.ctx = B.slim_create(H * dk, H, dk, theta, B.SLIM_F32 if self.f32 else B.SLIM_BF16)
+        if theta:
+            B.slim_reserve_positions(self.ctx, max(self.max_k, 1))
+
+    def close(self):
+        B.slim_destroy(self.ctx)
+
+    def buffers(self):
+        need = B.slim_prompt_workspace_bytes(self.ctx, self.KV, len(self.nq), self.tq, self.tk)
+        assert need > 0
+        return dict(q=self.q.to(DEV), k=self.k.to(DEV), v=self.v.to(DEV), cu_q=torch.from_numpy(self.cu_q).to(DEV), cu_k=torch.from_numpy(self.cu_k).to(DEV),
+                    o=torch.full((self.tq, self.H, self.dk), 7.0, dtype=self.q.dtype, device=DEV), ws=torch.empty(need, dtype=torch.uint8, device=DEV))
+
+    def call(self, b, causal, stream=None):
+        st = torch.cuda.current_stream().cuda_stream if stream is None else stream
+        B.slim_prompt_attention(self.ctx, b["q"], b["k"], b["v"], B.SLIM_F32 if self.v32 else B.SLIM_BF16, self.KV, b["cu_q"], b["cu_k"], len(self.nq),
+                                self.tq, self.tk, self.max_k, causal, b["o"], b["ws"], st)
+
+    def reference(self, causal):
+        """(o, allowed difference), rows outside every sequence 7."""
+        o, tol = np.full((self.tq, self.H, self.dk), 7.0), np.zeros((self.tq, self.H, self.dk))
+        q, k, v = (x.float().numpy() for x in (self.q, self.k, self.v))
+        for b in range(len(self.nq)):
+            s, t = slice(self.cu_q[b], self.cu_q[b + 1]), slice(self.cu_k[b], self.cu_k[b + 1])
+            o[s], pv, qk = po.attention(q[s], k[t], v[t], self.theta, causal)
+            # Scores: products and sums of d_k terms in float32, rotations of two float32 products and tables (2^-22 each side),
+            # and in bf16 both rotated operands rounded to 11 bits (2^-11 each).  exp and the softmax sum: 2^-20.
+            ds = ((self.dk + 16) * 2.0 ** -24 + 2.0 ** -21) * qk + 2.0 ** -20
+            if not self.f32:
+                ds = ds + (2 * 2.0 ** -11 + 2.0 ** -22) * qk
+            # a relative change of every p by at most ds changes the weighted mean by at most 2 ds sum p |v|; probabilities rounded
+            # to bf16 (2^-8, in the sum or not: twice), float32 values rounded to bf16, the output rounded once
+            rel = 2 * ds[..., None] + (0 if self.f32 else 2 * 2.0 ** -8 + (2.0 ** -8 if self.v32 else 0))
+            tol[s] = rel * pv + (2.0 ** -23 if self.f32 else 2.0 ** -8) * np.abs(o[s]) + 1e-30
+        return o, tol
+
+    def check(self, causal, b=None):
+        b = b or self.buffers()
+        self.call(b, causal)
+        torch.cuda.synchronize()
+        assert B.slim_device_status(self.ctx) == B.SLIM_OK
+        got = b["o"].double().cpu().numpy()
+        want, tol = self.reference(causal)
+        bad = ~(np.abs(got - want) <= tol)
+        assert not bad.any(), (np.argwhere(bad)[:5], got[bad][:5], want[bad][:5], tol[bad][:5])
+        return got
+
+
+# head layouts, head widths and types; lengths around the tiles of 64 and 128; one token; no token; no key
+SHAPES = [
+    ("f32", 6, 6, 64, 0.0, True), ("f32", 4, 2, 96, 1e4, True), ("f32", 5, 1, 40, 1e4, False), ("f32", 2, 2, 256, 1e4, True), ("f32", 1, 1, 2, 1e4, True), ("f32", 2, 1, 130, 0.0, False),
+    ("bf16", 4, 4, 128, 1e6, True), ("bf16", 8, 2, 128, 1e6, True), ("bf16", 4, 1, 64, 1e4, True), ("bf16", 3, 3, 64, 0.0, False), ("bf16", 4, 4, 96, 1e4, True),
+    ("bf16", 6, 3, 96, 0.0, False), ("bf16", 5, 5, 100, 1e4, True), ("bf16", 3, 1, 128, 0.0, False), ("bf16", 2, 2, 18, 1e4, True), ("bf16", 1, 1, 200, 1e4, True),
+]
+
+
+@pytest.mark.parametrize("dtype,H,KV,dk,theta,causal", SHAPES)
+@pytest.mark.parametrize("v32", [True, False])
+def test_packed_lengths(dtype, H, KV, dk, theta, causal, v32):
+    if dtype == "f32" and not v32:
+        pytest.skip("float32 contexts take float32 values")
+    nq = [1, 0, 130, 63, 257, 5, 128, 2]
+    nk = [1, 4, 130, 200, 257, 0, 384, 1]
+    c = Case(dtype, H, KV, dk, theta, nq, nk, v32, seed=H * dk)
+    c.check(causal)
+    c.close()
+
+
+@pytest.mark.parametrize("n,before", [(1, 0), (1, 1000), (129, 0), (700, 333), (512, 513), (1025, 0)])
+@pytest.mark.parametrize("H,KV,dk", [(2, 2, 128), (4, 1, 64)])
+def test_one_sequence(n, before, H, KV, dk):
+    c = Case("bf16", H, KV, dk, 1e6, [n], [n + before], v32=False, seed=n, lead=0)
+    c.check(True)
+    c.check(False)
+    c.close()
+
+
+def test_more_queries_than_keys():
+    c = Case("bf16", 2, 2, 128, 1e4, [300, 140], [170, 3], v32=False)
+    got = c.check(True)
+    assert not got[3:3 + 130].any() and not got[303:303 + 137].any()       # they attend nothing
+    c.close()
+
+
+def test_many_sequences_of_any_length():
+    rng = np.random.default_rng(5)
+    nq = [int(x) for x in rng.integers(0, 40, 300)]
+    nk = [n + int(x) for n, x in zip(nq, rng.integers(0, 90, 300))]
+    c = Case("bf16", 2, 1, 64, 1e4, nq, nk, v32=False)
+    c.check(True)
+    c.close()
+
+
+@pytest.mark.parametrize("dtype,H,dk", [("f32", 2, 64), ("bf16", 2, 128), ("bf16", 2, 100)])
+def test_numbers_that_are_not_finite_stay_with_the_rows_that_attend_them(dtype, H, dk):
+    c = Case(dtype, H, H, dk, 1e4, [200, 90], [200, 90], v32=dtype == "f32")
+    c.v[3 + 150, 0, 1] = float("nan")          # value of key 150, head 0, one column
+    c.k[3 + 170, 1, :] = float("inf")          # key 170, head 1
+    c.q[3 + 20, 1, 3] = float("nan")           # query 20, head 1
+    c.v[3 + 200 + 89, :, :] = float("-inf")    # last value of the second sequence
+    c.k[0] = float("nan")                      # a row in front of the first sequence
+    c.v[0] = float("nan")
+    b = c.buffers()
+    c.call(b, True)
+    torch.cuda.synchronize()
+    got = b["o"].double().cpu().numpy()
+    want, tol = c.reference(True)
+    touched = np.zeros(got.shape, dtype=bool)
+    touched[3 + 150:203, 0, 1] = touched[3 + 170:203, 1] = touched[23, 1] = touched[3 + 200 + 89] = True
+    assert not np.isfinite(got[touched]).any()
+    assert (np.abs(got - want)[~touched] <= tol[~touched]).all()
+    c.close()
+
+
+@pytest.mark.parametrize("scale_q,scale_k", [(1e-20, 1e20), (2e4, 1e-6), (1.0, 1e30), (3e-3, 3e4), (1e30, 1e-30)])
+def test_magnitudes_beyond_16_bits(scale_q, scale_k):
+    c = Case("bf16", 2, 2, 128, 1e4, [140], [140], v32=False)
+    c.q, c.k = (c.q.float() * scale_q).bfloat16(), (c.k.float() * scale_k).bfloat16()
+    if scale_q * scale_k > 1e3:                # one key takes all the weight: nothing to compare but that it is a value
+        b = c.buffers()
+        c.call(b, True)
+        got = b["o"][3:143].float().cpu()
+        assert torch.isfinite(got).all() and (got.abs() <= c.v.float().abs().max()).all()
+    else:
+        c.check(True)
+    c.close()
+
+
+def test_values_beyond_16_bits():
+    c = Case("bf16", 2, 2, 64, 1e4, [150], [150], v32=True)
+    c.v = c.v * 1e30
+    c.check(True)
+    c.close()
+
+
+def test_starts_that_do_not_ascend_are_reported():
+    c = Case("bf16", 2, 2, 64, 1e4, [20, 20, 20], [20, 20, 20], v32=False)
+    for cu in ([3, 2, 43, 63], [-1, 23, 43, 63], [3, 23, 43, 67], [3, 2000000000, 43, 63]):
+        for which in ("cu_q", "cu_k"):
+            b = c.buffers()
+            b[which] = torch.tensor(cu, dtype=torch.int32, device=DEV)
+            c.call(b, True)
+            assert B.slim_device_status(c.ctx) == B.SLIM_ERR_CAPACITY
+    b = c.buffers()                            # longer than max_k: left out
+    c.max_k = 19
+    c.call(b, True)
+    assert B.slim_device_status(c.ctx) == B.SLIM_ERR_CAPACITY
+    assert (b["o"] == 7).all()
+    c.close()
+
+
+def test_refusals():
+    c = Case("bf16", 4, 2, 64, 1e4, [20], [20], v32=False)
+    b = c.buffers()
+    args = [c.ctx, b["q"], b["k"], b["v"], B.SLIM_BF16, 2, b["cu_q"], b["cu_k"], 1, c.tq, c.tk, 20, True, b["o"], b["ws"]]
+
+    def status(i, x):
+        a = list(args)
+        a[i] = x
+        try:
+            B.slim_prompt_attention(*a)
+        except B.SlimError as e:
+            return e.status
+        return B.SLIM_OK
+
+    for i in (1, 2, 3, 6, 7, 13, 14):
+        assert status(i, None) == B.SLIM_ERR_INVALID_ARG
+    for i, x in ((5, 0), (8, 0), (9, 0), (10, -1), (11, -1), (4, B.SLIM_FP8), (4, B.SLIM_FP4)):
+        assert status(i, x) == B.SLIM_ERR_INVALID_ARG
+    for i in (1, 2, 3, 13):
+        assert status(i, args[i].data_ptr() + 2) == B.SLIM_ERR_INVALID_ARG
+    assert status(14, b["ws"].data_ptr() + 128) == B.SLIM_ERR_INVALID_ARG
+    assert status(5, 3) == B.SLIM_ERR_UNSUPPORTED
+    assert status(8, 5000) == B.SLIM_ERR_UNSUPPORTED
+    assert status(9, 1 << 30) == B.SLIM_ERR_UNSUPPORTED
+    assert status(11, 1 << 20) == B.SLIM_ERR_CAPACITY              # beyond the position tables
+    assert B.slim_prompt_workspace_bytes(c.ctx, 3, 1, 1, 1) == 0
+    assert status(11, 20) == B.SLIM_OK
+    c.close()
+    f = Case("f32", 2, 2, 64, 0.0, [4], [4])
+    f.v32 = False
+    with pytest.raises(B.SlimError):
+        f.call(f.buffers(), True)
+    f.close()
+
+
+def test_captured_and_replayed_on_new_inputs():
+    c = Case("bf16", 4, 2, 128, 1e4, [150, 0, 77], [300, 5, 77], v32=False)
+    b = c.buffers()
+    c.call(b, True)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        c.call(b, True)
+    d = Case("bf16", 4, 2, 128, 1e4, [10, 120, 97], [10, 120, 250], v32=False, seed=9)
+    d.tq, d.tk = c.tq, c.tk
+    for name in ("q", "k", "v"):
+        x = getattr(d, name)
+        y = torch.zeros_like(getattr(c, name))
+        y[:x.shape[0]] = x
+        setattr(d, name, y)
+        b[name].copy_(y)
+    b["cu_q"].copy_(torch.from_numpy(d.cu_q))
+    b["cu_k"].copy_(torch.from_numpy(d.cu_k))
+    b["o"].fill_(7.0)
+    graph.replay()
+    torch.cuda.synchronize()
+    got = b["o"].double().cpu().numpy()
+    want, tol = d.reference(True)
+    assert (np.abs(got - want) <= tol).all()
+    del graph
+    c.close()
+    d.close()
+
+
+def test_two_streams_with_a_workspace_each():
+    c = Case("bf16", 4, 4, 128, 1e4, [500, 31], [700, 31], v32=False)
+    bufs = [c.buffers() for _ in range(2)]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for b, s in zip(bufs, streams):
+            with torch.cuda.stream(s):
+                c.call(b, True, s.cuda_stream)
+    torch.cuda.synchronize()
+    c.call(bufs[0], True)
+    torch.cuda.synchronize()
+    assert torch.equal(bufs[0]["o"], bufs[1]["o"])
+    c.check(True)
+    c.close()
+
+
+def test_paths_agree():
+    c = Case("bf16", 4, 2, 96, 1e4, [333, 1, 64], [400, 1, 64], v32=False)
+    a = c.check(True)
+    B.slim_set_path(c.ctx, B.SLIM_PATH_GENERIC)
+    b = c.check(True)
+    want, tol = c.reference(True)
+    assert (np.abs(a - b) <= 2 * tol).all()
+    c.close()
