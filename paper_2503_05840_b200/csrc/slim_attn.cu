@@ -8,80 +8,18 @@
 #include <cuda_fp16.h>
 
 #include "slim_attn.h"
+#include "slim_attn_plan.cuh"
 
 namespace {
 
 constexpr int THREADS = 256;
-constexpr int BINS = 64;
 
 // ------------------------------------------------------------------------------------------------ preparation
-// The list of query tiles, by one CTA: a counting sort on the number of keys.
-__device__ void plan_tiles(const SlimAttn& a, int* s_mem) {
-  int* s_prefix = s_mem;                            // [batch + 1] tiles before a sequence
-  int* s_bin = s_mem + a.batch + 1;                 // [BINS]
-  const int tid = threadIdx.x;
-  for (int b = tid; b < a.batch; b += THREADS) s_prefix[b + 1] = (slim_attn_seq(a, b).nq + a.tile_rows - 1) / a.tile_rows;
-  if (tid == 0) s_prefix[0] = 0;
-  if (tid < BINS) s_bin[tid] = 0;
-  __syncthreads();
-  if (tid < 32) {
-    const int chunk = (a.batch + 31) / 32, lo = tid * chunk, hi = min(a.batch, lo + chunk);
-    int sum = 0;
-    for (int b = lo; b < hi; ++b) sum += s_prefix[b + 1];
-    int incl = sum;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int v = __shfl_up_sync(0xffffffffu, incl, o);
-      if (tid >= o) incl += v;
-    }
-    int run = incl - sum;
-    for (int b = lo; b < hi; ++b) { run += s_prefix[b + 1]; s_prefix[b + 1] = run; }
-  }
-  __syncthreads();
-  const int n = min(s_prefix[a.batch], a.most_tiles);         // (more only where sequences overlap)
-  if (tid == 0 && n < s_prefix[a.batch]) atomicMax(a.status, (int)SLIM_ERR_CAPACITY);
-  for (int pass = 0; pass < 2; ++pass) {
-    for (int g = tid; g < n; g += THREADS) {
-      int lo = 0, hi = a.batch;
-      while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (s_prefix[mid] <= g) lo = mid; else hi = mid;
-      }
-      const SlimSeq s = slim_attn_seq(a, lo);
-      const int row = (g - s_prefix[lo]) * a.tile_rows;
-      const int keys = slim_attn_keys(a, s, min(s.nq, row + a.tile_rows) - 1);
-      const int bin = BINS - 1 - (int)((long long)keys * (BINS - 1) / max(a.max_k, 1));
-      if (pass == 0) atomicAdd(&s_bin[bin], 1);
-      else a.tiles[atomicAdd(&s_bin[bin], 1)] = make_int4(lo, row, 0, 0);
-    }
-    __syncthreads();
-    if (pass == 0 && tid == 0) {
-      int run = 0;
-      for (int i = 0; i < BINS; ++i) { const int c = s_bin[i]; s_bin[i] = run; run += c; }
-      *a.n_tiles = n;
-    }
-    __syncthreads();
-  }
-}
-
-// Position of packed row r among the queries (keys); -1: it belongs to no sequence.
-__device__ int packed_position(const SlimAttn& a, int r, bool query) {
-  const int32_t* cu = query ? a.cu_q : a.cu_k;
-  int lo = 0, hi = a.batch;
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (cu[mid] <= r) lo = mid; else hi = mid;
-  }
-  const SlimSeq s = slim_attn_seq(a, lo);
-  if (query) return r >= s.q0 && r < s.q0 + s.nq ? r - s.q0 + s.nk - s.nq : -1;
-  return r >= s.k0 && r < s.k0 + s.nk ? r - s.k0 : -1;
-}
-
 // One warp a packed row: all its heads, rotated.  A query before the first key (negative position) attends nothing.
 template <bool F32>
 __device__ void rotate_row(const SlimAttn& a, int r, bool query) {
   const int lane = threadIdx.x & 31, heads = query ? a.H : a.KV;
-  const int pos = packed_position(a, r, query);
+  const int pos = slim_attn_position(a, r, query);
   if (pos < 0) return;
   const size_t at = (size_t)r * heads * a.d_k;
   const void* src = query ? a.q : a.k;
@@ -102,7 +40,7 @@ __global__ void __launch_bounds__(THREADS) attn_prepare_kernel(const __grid_cons
   extern __shared__ int s_mem[];
   slim_pdl_trigger();
   slim_pdl_wait();
-  if (blockIdx.x == 0) { plan_tiles(a, s_mem); return; }
+  if (blockIdx.x == 0) { slim_attn_plan(a, s_mem); return; }
   const int warps = (gridDim.x - 1) * (THREADS / 32);
   for (int r = (blockIdx.x - 1) * (THREADS / 32) + (threadIdx.x >> 5); r < a.total_q + a.total_k; r += warps)
     rotate_row<F32>(a, r < a.total_q ? r : r - a.total_q, r < a.total_q);
@@ -282,18 +220,18 @@ SlimAttnLayout slim_attn_layout(const slim_ctx* ctx, int kv_heads, int batch, in
   return L;
 }
 
-int slim_attn_tc_ok(const slim_ctx*) { return 0; }
-
 cudaError_t slim_launch_attn(const slim_ctx* ctx, SlimAttn a, char* ws, int tc, cudaStream_t st) {
   const SlimAttnLayout L = slim_attn_layout(ctx, a.KV, a.batch, a.total_q, a.total_k);
   a.qr = ws + L.qr; a.kr = ws + L.kr; a.vb = ws + L.vb;
   a.tiles = reinterpret_cast<int4*>(ws + L.tiles);
   a.n_tiles = reinterpret_cast<int*>(ws + L.n_tiles);
-  a.tile_rows = SLIM_ATTN_ROWS;
+  tc = tc && a.total_k > 0;                              // (a tensor map needs a row)
+  a.tile_rows = tc ? SLIM_ATTN_TC_ROWS : SLIM_ATTN_ROWS;
   const int most = a.most_tiles = a.total_q / a.tile_rows + a.batch;
+  if (tc) return slim_launch_attn_tc(ctx, a, most, st);
   const int rows = a.total_q + a.total_k;
   const int blocks = 1 + (int)((rows + 7ll) / 8 < 8ll * ctx->num_sms ? (rows + 7ll) / 8 : 8ll * ctx->num_sms);
-  const size_t smem = sizeof(int) * (a.batch + 1 + BINS);
+  const size_t smem = slim_attn_plan_smem(a.batch);
   cudaError_t e = a.f32 ? slim_launch_pdl(attn_prepare_kernel<true>, dim3(blocks), dim3(THREADS), smem, st, a)
                         : slim_launch_pdl(attn_prepare_kernel<false>, dim3(blocks), dim3(THREADS), smem, st, a);
   if (e != cudaSuccess) return e;

@@ -20,7 +20,7 @@ struct SlimAttn {
   // workspace
   void* qr;                      // rotated queries and keys, layout of q and k: float32 (CUDA cores) or float16 (tensor cores)
   void* kr;
-  void* vb;                      // tensor cores with float32 values: the values as bf16
+  void* vb;                      // tensor cores with float32 values: the values times 16 as float16
   int4* tiles;                   // (sequence, first query row, -, -), most keys first
   int* n_tiles;
   int tile_rows, most_tiles;

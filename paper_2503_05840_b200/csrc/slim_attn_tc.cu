@@ -1,0 +1,423 @@
+// Attention over packed prompts on the tensor cores (bf16, d_k in {64, 96, 128}).
+//
+// attn_tc_prepare_kernel  rotated queries and keys as float16 in the workspace (11 bits: bf16's 8 would cost as much accuracy
+//                         as the rounding of P), float32 values as float16 too, the list of query tiles.
+// attn_tc_kernel          one CTA a (tile of 2 x 128 query rows, head).  Per key tile of 128 rows and query tile i:
+//                           S_i = Q_i K^T       float16, both operands from shared memory, S in tensor memory
+//                           P_i = 2^(S_i - m)   a thread a row: S to registers, maximum, exponentials, P as bf16 over S's
+//                                               columns in tensor memory
+//                           O_i += P_i V        P from tensor memory, V as it lies (MN-major); bf16 where the values are, float16
+//                                               where they were float32 (a second rounding to 8 bits would cost as much as P's)
+//                         While one query tile's softmax runs, the tensor core works for the other.
+//   The reference m of a row moves only when its maximum has grown by more than 2^8: then its warp multiplies the row of O
+//   (and l) by 2^(m - m'); P stays below 2^8 otherwise, which float32 sums do not mind.
+//   What float16 cannot hold (|q| > 4096, |k| > 16384, |v| > 4000, numbers that are not finite) enters as NaN, and rows that
+//   come out not finite are computed once more by slim_attn_row; so are rows that share a tile with a value that is not
+//   finite and that they do not attend (0 times infinity).  Float32 values enter times 16: float16's smallest step is then
+//   2^-28, and rows whose outputs all stay below 2^-18 are computed once more as well.
+#include <cuda_fp16.h>
+
+#include "slim_attn.h"
+#include "slim_attn_plan.cuh"
+#include "slim_ptx.cuh"
+
+using namespace slim_ptx;
+
+namespace {
+
+// ------------------------------------------------------------------------------------------------ preparation
+constexpr int PREP_THREADS = 256;
+constexpr float V_UP = 16.f;                         // factor of float32 values on their way into float16
+
+__device__ __forceinline__ uint32_t half2_checked(float a, float b, float most) {
+  const bool fine = fabsf(a) <= most && fabsf(b) <= most;
+  const __half2 v = __floats2half2_rn(a, b);
+  return fine ? *reinterpret_cast<const uint32_t*>(&v) : 0x7fff7fffu;
+}
+
+// One warp a packed row.  A lane has eight pairs (j, j + d_k/2) of a head, the same j in every head, so its angles are
+// formed once; d_k / 16 lanes make a head.
+template <int DK>
+__device__ void prepare_row(const SlimAttn& a, int r, bool query) {
+  constexpr int LPH = DK / 16, HPW = 32 / LPH;
+  const int lane = threadIdx.x & 31, heads = query ? a.H : a.KV;
+  const int pos = slim_attn_position(a, r, query);
+  if (pos < 0 || lane >= LPH * HPW) return;
+  const int jl = lane % LPH, hw = lane / LPH;
+  const unsigned short* src = reinterpret_cast<const unsigned short*>(query ? a.q : a.k) + (size_t)r * heads * DK + 8 * jl;
+  unsigned short* dst = reinterpret_cast<unsigned short*>(query ? a.qr : a.kr) + (size_t)r * heads * DK + 8 * jl;
+  const float most = query ? 4096.f : 16384.f;
+  float cs[8], sn[8];
+#pragma unroll
+  for (int x = 0; x < 8; ++x) {
+    const float2 t = a.rope_base ? slim_attn_turn(a, pos, 8 * jl + x) : make_float2(1.f, 0.f);
+    cs[x] = t.x; sn[x] = t.y;
+  }
+#pragma unroll 4
+  for (int h = hw; h < heads; h += HPW) {
+    const uint4 u = __ldcs(reinterpret_cast<const uint4*>(src + h * DK)), v = __ldcs(reinterpret_cast<const uint4*>(src + h * DK + DK / 2));
+    float lo[8], hi[8];
+    unpack8(u, lo);
+    unpack8(v, hi);
+    uint32_t ol[4], oh[4];
+#pragma unroll
+    for (int x = 0; x < 8; x += 2) {
+      float y[4];
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        y[e] = lo[x + e] * cs[x + e] + hi[x + e] * sn[x + e];
+        y[2 + e] = hi[x + e] * cs[x + e] - lo[x + e] * sn[x + e];
+      }
+      ol[x / 2] = half2_checked(y[0], y[1], most);
+      oh[x / 2] = half2_checked(y[2], y[3], most);
+    }
+    *reinterpret_cast<uint4*>(dst + h * DK) = make_uint4(ol[0], ol[1], ol[2], ol[3]);
+    *reinterpret_cast<uint4*>(dst + h * DK + DK / 2) = make_uint4(oh[0], oh[1], oh[2], oh[3]);
+  }
+}
+
+template <int DK>
+__global__ void __launch_bounds__(PREP_THREADS) attn_tc_prepare_kernel(const __grid_constant__ SlimAttn a) {
+  extern __shared__ int s_mem[];
+  slim_pdl_trigger();
+  slim_pdl_wait();
+  if (blockIdx.x == 0) { slim_attn_plan(a, s_mem); return; }
+  const int warps = (gridDim.x - 1) * (PREP_THREADS / 32), lane = threadIdx.x & 31;
+  const int rows = a.total_q + a.total_k + (a.v32 ? a.total_k : 0);
+  for (int r = (blockIdx.x - 1) * (PREP_THREADS / 32) + (threadIdx.x >> 5); r < rows; r += warps) {
+    if (r < a.total_q) { prepare_row<DK>(a, r, true); continue; }
+    if (r < a.total_q + a.total_k) { prepare_row<DK>(a, r - a.total_q, false); continue; }
+    const int n = a.KV * DK;
+    const size_t at = (size_t)(r - a.total_q - a.total_k) * n;
+    const float4* src = reinterpret_cast<const float4*>(reinterpret_cast<const float*>(a.v) + at);
+    uint2* dst = reinterpret_cast<uint2*>(reinterpret_cast<unsigned short*>(a.vb) + at);
+#pragma unroll 4
+    for (int i = lane; i < n / 4; i += 32) {
+      const float4 v = __ldcs(src + i);
+      dst[i] = make_uint2(half2_checked(v.x * V_UP, v.y * V_UP, 64000.f), half2_checked(v.z * V_UP, v.w * V_UP, 64000.f));
+    }
+  }
+}
+
+// ------------------------------------------------------------------------------------------------ attention
+constexpr int TM = 128, TN = 128;                    // rows of a query tile, keys of a key tile
+constexpr int THREADS = 384;                         // two groups of four softmax warps, MMA warp, load warp, two without work
+constexpr float TAU = 8.f;                           // log2 units by which a row's maximum may pass its reference
+
+template <int DK>
+struct Shape {
+  static constexpr int CH = (DK + 63) / 64;          // 64-column chunks of a head
+  static constexpr int TILE = CH * TN * 128;         // bytes of a tile of Q, K or V
+  static constexpr int NS = DK == 64 ? 8 : 5;        // ring of K and V tiles
+  static constexpr int SMEM = 1024 + (2 + NS) * TILE + 8 * (2 * NS + 8) + 32;
+};
+
+__device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t* r) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
+      "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
+      "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};"
+      ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
+        "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]),
+        "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]),
+        "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]) : "memory");
+}
+__device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+// A from shared memory / from tensor memory
+__device__ __forceinline__ void umma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
+  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+               ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(acc) : "memory");
+}
+__device__ __forceinline__ void umma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
+  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+               ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(acc) : "memory");
+}
+__device__ __forceinline__ uint32_t bf162_of(float lo, float hi) {
+  uint32_t d; asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo)); return d;
+}
+__device__ __forceinline__ uint32_t half2_of(float lo, float hi) {
+  uint32_t d; asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo)); return d;
+}
+__device__ __forceinline__ void split(f32x2 v, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v)); }
+
+template <int DK, bool VH>
+__global__ void __launch_bounds__(THREADS, 1)
+attn_tc_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap,
+               const __grid_constant__ SlimAttn a) {
+  typedef Shape<DK> S;
+  constexpr int NS = S::NS, CH = S::CH, KSTEPS = DK / 16;
+  constexpr uint32_t TILE = S::TILE;
+  // S = Q K^T: float16, both K-major;  O = P V: float16 (VH) or bf16, V MN-major
+  constexpr uint32_t IDESC_S = (1u << 4) | ((TN >> 3) << 17) | ((TM >> 4) << 24);
+  constexpr uint32_t IDESC_O = (1u << 4) | (VH ? 0u : (1u << 7) | (1u << 10)) | (1u << 16) | ((DK >> 3) << 17) | ((TM >> 4) << 24);
+  extern __shared__ unsigned char smem_raw[];
+  const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+  unsigned char* sm = smem_raw + (base - smem_u32(smem_raw));
+  const uint32_t s_q = base, s_kv = base + 2 * TILE;
+  const uint32_t bars = s_kv + NS * TILE;
+  const uint32_t bar_full = bars, bar_empty = bars + 8 * NS, bar_q = bars + 16 * NS;
+  const uint32_t bar_s = bar_q + 8, bar_p = bar_s + 16, bar_o = bar_p + 16;                  // two each
+  unsigned char* misc = sm + (bar_o + 16 - base);
+  uint32_t* s_tmem = reinterpret_cast<uint32_t*>(misc);
+  volatile int* s_abort = reinterpret_cast<volatile int*>(misc + 4);
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+
+  if (tid == 0) {
+    prefetch_tensormap(&qmap); prefetch_tensormap(&kmap); prefetch_tensormap(&vmap);
+    for (int i = 0; i < NS; ++i) { mbar_init(bar_full + 8 * i, 1); mbar_init(bar_empty + 8 * i, 1); }
+    mbar_init(bar_q, 1);
+    for (int i = 0; i < 2; ++i) { mbar_init(bar_s + 8 * i, 1); mbar_init(bar_p + 8 * i, 4); mbar_init(bar_o + 8 * i, 1); }
+    *s_abort = 0;
+    fence_mbar_init();
+  }
+  slim_pdl_trigger();
+  slim_pdl_wait();
+  const int item = blockIdx.x / a.H, h = blockIdx.x % a.H;
+  if (item >= *a.n_tiles) return;
+  if (warp == 8) tmem_alloc(smem_u32(s_tmem), 512);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *s_tmem;
+
+  const int4 tile = a.tiles[item];
+  const SlimSeq s = slim_attn_seq(a, tile.x);
+  const int row0 = tile.y, kvh = h / (a.H / a.KV);
+  // key tiles of the two query tiles (the second may have no rows)
+  const int nt0 = (slim_attn_keys(a, s, min(s.nq, row0 + TM) - 1) + TN - 1) / TN;
+  const int nt1 = row0 + TM < s.nq ? (slim_attn_keys(a, s, min(s.nq, row0 + 2 * TM) - 1) + TN - 1) / TN : 0;
+  const int nt = max(nt0, nt1);
+
+  if (warp < 8) {
+    // 168 registers a thread at launch: the last four warps hand 112 of theirs to the softmax warps' 56 (224 x 256 + 56 x 128 = 168 x 384)
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
+    // =========================== softmax ===========================
+    const int i = warp >> 2;
+    const int n = i ? nt1 : nt0;
+    const int row = row0 + i * TM + (warp & 3) * 32 + lane;
+    const int lim = slim_attn_keys(a, s, row);
+    const uint32_t t_s = tmem + ((uint32_t)((warp & 3) * 32) << 16) + (uint32_t)(i * TN);
+    const uint32_t t_o = tmem + ((uint32_t)((warp & 3) * 32) << 16) + (uint32_t)(2 * TN + i * 128);
+    const float scale = a.qscale;
+    const f32x2 scale2 = pack2(scale, scale);
+    float m = -INFINITY;                            // reference, log2 units
+    f32x2 l2 = pack2(0.f, 0.f);
+    bool ok = true;
+    for (int j = 0; j < n; ++j) {
+      ok = mbar_wait<false>(bar_s + 8 * i, j & 1, s_abort, a.status);
+      ok = __all_sync(0xffffffffu, ok);
+      if (!ok) break;
+      tc_fence_after();
+      uint32_t r[4][32];
+#pragma unroll
+      for (int c = 0; c < 4; ++c) tmem_ld32_issue(t_s + 32 * c, r[c]);
+      tmem_ld_wait();
+      if (__any_sync(0xffffffffu, (j + 1) * TN > lim)) {
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+#pragma unroll
+          for (int x = 0; x < 32; ++x)
+            if (j * TN + 32 * c + x >= lim) r[c][x] = 0xff800000u;
+      }
+      float mx[4];
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        mx[c] = __uint_as_float(r[c][0]);
+#pragma unroll
+        for (int x = 1; x < 32; ++x) mx[c] = fmaxf(mx[c], __uint_as_float(r[c][x]));
+      }
+      const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * scale;
+      const bool move = top > m + TAU;              // (m = -inf: the first keys of the row)
+      if (__any_sync(0xffffffffu, move)) {
+        const float m_new = move ? top : m;
+        const float f = move ? ex2_approx(m - m_new) : 1.f;
+        m = m_new;
+        float lo, hi;
+        split(l2, lo, hi);
+        l2 = pack2(lo * f, hi * f);
+        if (j > 0) {
+          // O_i is at rest: S_i(j) was completed after O_i += P_i(j - 1) V, and the next product waits for P_i(j)
+#pragma unroll
+          for (int c = 0; c < DK / 32; ++c) {
+            uint32_t o[32];
+            tmem_ld32(t_o + 32 * c, o);
+#pragma unroll
+            for (int x = 0; x < 32; ++x) o[x] = __float_as_uint(__uint_as_float(o[x]) * f);
+            tmem_st32(t_o + 32 * c, o);
+          }
+        }
+      }
+      const float mm = m == -INFINITY ? 0.f : -m;
+      const f32x2 m2 = pack2(mm, mm);
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+#pragma unroll
+        for (int x = 0; x < 32; x += 2) {
+          f32x2 v = pack2(__uint_as_float(r[c][x]), __uint_as_float(r[c][x + 1]));
+          v = fma2(v, scale2, m2);
+          float lo, hi;
+          split(v, lo, hi);
+          lo = ex2_approx(lo); hi = ex2_approx(hi);
+          l2 = add2(l2, pack2(lo, hi));
+          r[c >> 1][(c & 1) * 16 + x / 2] = VH ? half2_of(lo, hi) : bf162_of(lo, hi);
+        }
+      }
+      tmem_st32(t_s, r[0]);
+      tmem_st32(t_s + 32, r[1]);
+      tmem_st_wait();
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar_p + 8 * i);
+    }
+    // ---- output ----
+    if (ok && n > 0) {
+      ok = mbar_wait<false>(bar_o + 8 * i, 0, s_abort, a.status);
+      ok = __all_sync(0xffffffffu, ok);
+      tc_fence_after();
+    }
+    const bool there = row < s.nq && (i == 0 || nt1 > 0 || row0 + TM < s.nq);
+    const float inv = lim > 0 ? (VH ? 1.f / V_UP : 1.f) / sum2(l2) : 0.f;
+    __nv_bfloat16* dst = reinterpret_cast<__nv_bfloat16*>(a.o) + ((size_t)(s.q0 + row) * a.H + h) * DK;
+    bool bad = false;
+    float most = 0.f;
+    if (ok) {
+#pragma unroll
+      for (int c = 0; c < DK / 32; ++c) {
+        uint32_t o[32];
+        if (n > 0) tmem_ld32(t_o + 32 * c, o);
+#pragma unroll
+        for (int x = 0; x < 32; x += 8) {
+          uint32_t w[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            float lo = __uint_as_float(o[x + 2 * e]) * inv, hi = __uint_as_float(o[x + 2 * e + 1]) * inv;
+            if (lim == 0) lo = hi = 0.f;
+            bad |= !(fabsf(lo) <= 3.3895313892515355e38f && fabsf(hi) <= 3.3895313892515355e38f);
+            if (VH) most = fmaxf(most, fmaxf(fabsf(lo), fabsf(hi)));
+            w[e] = bf162_of(lo, hi);
+          }
+          if (there) *reinterpret_cast<uint4*>(dst + 32 * c + x) = make_uint4(w[0], w[1], w[2], w[3]);
+        }
+      }
+      if (VH) bad |= lim > 0 && most < 3.8e-6f;      // 2^-18
+      unsigned redo = __ballot_sync(0xffffffffu, bad && there);
+      while (redo) {
+        const int x = __ffs(redo) - 1;
+        redo &= redo - 1;
+        __syncwarp();
+        slim_attn_row(a, tile.x, row0 + i * TM + (warp & 3) * 32 + x, h);
+      }
+    }
+  } else if (warp == 8) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+    // =========================== MMA issuer ===========================
+    if (lane == 0 && nt > 0) {
+      bool ok = mbar_wait<false>(bar_q, 0, s_abort, a.status);
+      auto full = [&](int k) { return mbar_wait<false>(bar_full + 8 * (k % NS), (k / NS) & 1, s_abort, a.status); };
+      auto scores = [&](int i, int k) {
+#pragma unroll
+        for (int x = 0; x < KSTEPS; ++x) {
+          const uint32_t off = (uint32_t)((x >> 2) * TN * 128 + (x & 3) * 32);
+          umma_ss(tmem + i * TN, desc_kmajor_sw128(s_q + i * TILE + off), desc_kmajor_sw128(s_kv + (k % NS) * TILE + off), IDESC_S, x > 0);
+        }
+        umma_commit(bar_s + 8 * i);
+      };
+      ok = ok && full(0);
+      if (ok) {
+        tc_fence_after();
+        if (nt0 > 0) scores(0, 0);
+        if (nt1 > 0) scores(1, 0);
+        umma_commit(bar_empty);
+      }
+      for (int j = 0; j < nt && ok; ++j) {
+        const int kv = 2 * j + 1, kk = 2 * j + 2;
+        ok = full(kv);
+        if (j + 1 < nt) ok = ok && full(kk);
+        for (int i = 0; i < 2 && ok; ++i) {
+          const int n = i ? nt1 : nt0;
+          if (j >= n) continue;
+          ok = mbar_wait<false>(bar_p + 8 * i, j & 1, s_abort, a.status);
+          if (!ok) break;
+          tc_fence_after();
+#pragma unroll
+          for (int x = 0; x < TN / 16; ++x)
+            umma_ts(tmem + 2 * TN + i * 128, tmem + i * TN + 8 * x, desc_a(s_kv + (kv % NS) * TILE + x * 2048, TN * 128), IDESC_O, j > 0 || x > 0);
+          if (j + 1 < n) scores(i, kk);
+          else umma_commit(bar_o + 8 * i);
+        }
+        if (!ok) break;
+        umma_commit(bar_empty + 8 * (kv % NS));
+        if (j + 1 < nt) umma_commit(bar_empty + 8 * (kk % NS));
+      }
+      // the last commit's arrival must not find this CTA gone
+      if (ok) mbar_wait<false>(bar_empty + 8 * ((2 * nt - 1) % NS), ((2 * nt - 1) / NS) & 1, s_abort, a.status);
+    }
+  } else if (warp == 9) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+    // =========================== loads ===========================
+    if (lane == 0 && nt > 0) {
+      const uint32_t tiles_q = nt1 > 0 ? 2 : 1;
+      mbar_arrive_expect_tx(bar_q, tiles_q * TILE);
+      for (uint32_t i = 0; i < tiles_q; ++i)
+        for (int c = 0; c < CH; ++c) tma_load_3d(s_q + i * TILE + c * TM * 128, &qmap, bar_q, h * DK + 64 * c, s.q0 + row0 + (int)i * TM, 0);
+      bool ok = true;
+      int k = 0;
+      for (; k < 2 * nt; ++k) {
+        ok = mbar_wait<false>(bar_empty + 8 * (k % NS), ((k / NS) & 1) ^ 1, s_abort, a.status);
+        if (!ok) break;
+        const uint32_t bar = bar_full + 8 * (k % NS), dst = s_kv + (k % NS) * TILE;
+        mbar_arrive_expect_tx(bar, TILE);
+        for (int c = 0; c < CH; ++c)
+          tma_load_3d(dst + c * TN * 128, k & 1 ? &vmap : &kmap, bar, kvh * DK + 64 * c, s.k0 + (k >> 1) * TN, 0);
+      }
+      if (!ok) {
+        // gave up: let the loads that were issued land before the CTA goes away
+        const unsigned long long t0 = globaltimer();
+        while (!mbar_try_wait(bar_q, 0) && globaltimer() - t0 < SLIM_WAIT_NS) {}
+        for (int x = max(0, k - NS); x < k; ++x)
+          while (!mbar_try_wait(bar_full + 8 * (x % NS), (x / NS) & 1) && globaltimer() - t0 < SLIM_WAIT_NS) {}
+      }
+    }
+  } else {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+  }
+  __syncwarp();
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 8) {
+    tc_fence_after();
+    tmem_dealloc(tmem, 512);
+  }
+}
+
+cudaError_t make_map(CUtensorMap* map, const void* p, int cols, int rows) {
+  const unsigned long long dims[3] = {(unsigned long long)cols, (unsigned long long)rows, 1};
+  const unsigned long long strides[2] = {(unsigned long long)cols * 2, (unsigned long long)cols * 2 * rows};
+  const unsigned int box[3] = {64, TN, 1};
+  return slim_tmap_encode_3d(map, const_cast<void*>(p), dims, strides, box);
+}
+
+template <int DK, bool VH>
+cudaError_t launch(const slim_ctx* ctx, const SlimAttn& a, int most_tiles, cudaStream_t st) {
+  CUtensorMap qmap, kmap, vmap;
+  cudaError_t e = make_map(&qmap, a.qr, a.H * DK, a.total_q);
+  if (e == cudaSuccess) e = make_map(&kmap, a.kr, a.KV * DK, a.total_k);
+  if (e == cudaSuccess) e = make_map(&vmap, a.v32 ? a.vb : a.v, a.KV * DK, a.total_k);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute((const void*)attn_tc_kernel<DK, VH>, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape<DK>::SMEM);
+  if (e != cudaSuccess) return e;
+  const long long rows = (long long)a.total_q + a.total_k + (a.v32 ? a.total_k : 0), fill = 8ll * ctx->num_sms;
+  const int blocks = 1 + (int)((rows + 7) / 8 < fill ? (rows + 7) / 8 : fill);
+  e = slim_launch_pdl(attn_tc_prepare_kernel<DK>, dim3(blocks), dim3(PREP_THREADS), slim_attn_plan_smem(a.batch), st, a);
+  if (e != cudaSuccess) return e;
+  return slim_launch_pdl(attn_tc_kernel<DK, VH>, dim3((unsigned)most_tiles * a.H), dim3(THREADS), Shape<DK>::SMEM, st, qmap, kmap, vmap, a);
+}
+
+}  // namespace
+
+int slim_attn_tc_ok(const slim_ctx* ctx) { return ctx->dtype == SLIM_BF16 && (ctx->d_k == 64 || ctx->d_k == 96 || ctx->d_k == 128); }
+
+cudaError_t slim_launch_attn_tc(const slim_ctx* ctx, const SlimAttn& a, int most_tiles, cudaStream_t st) {
+  if (a.v32)
+    return a.d_k == 64 ? launch<64, true>(ctx, a, most_tiles, st) : a.d_k == 96 ? launch<96, true>(ctx, a, most_tiles, st) : launch<128, true>(ctx, a, most_tiles, st);
+  return a.d_k == 64 ? launch<64, false>(ctx, a, most_tiles, st) : a.d_k == 96 ? launch<96, false>(ctx, a, most_tiles, st) : launch<128, false>(ctx, a, most_tiles, st);
+}
