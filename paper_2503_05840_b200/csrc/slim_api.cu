@@ -28,7 +28,7 @@ inline size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 inline size_t esize(int dtype) { return dtype == SLIM_BF16 ? 2 : 4; }
 
 struct WsLayout {
-  size_t part_u, part_m, part_l, flags, o_part, scores, u_tiled, u32, su, kscratch, total;
+  size_t part_u, part_m, part_l, flags, o_part, scores, u_tiled, u32, su, kscratch, umax, total;
   int units;
 };
 
@@ -47,6 +47,7 @@ WsLayout ws_layout(const slim_ctx* ctx, int batch, int t_cap) {
   L.su = off; off = align256(off + (ctx->proj_ok ? sizeof(float) * (size_t)((batch + 15) / 16) * 16 * ctx->H : 0));
   // 8-bit cache on the tensor-core path: one layer's keys as bf16 (the cache itself stays in 8 bits)
   L.kscratch = off; off = align256(off + ((ctx->kdtype == SLIM_FP8 && ctx->tc_ok) ? 2 * (size_t)batch * t_cap * ctx->d : 0));
+  L.umax = off; off = align256(off + (ctx->kdtype == SLIM_FP4 ? sizeof(float) * (size_t)L.units * ctx->H : 0));      // 4-bit cache, tensor cores
   L.total = off;
   return L;
 }
@@ -242,7 +243,8 @@ slim_status create_impl(slim_ctx** out, int d, int H, int d_k, double rope_theta
   }
   c->tc_ok = 0;
   for (int cl = 1; cl <= 2; ++cl) {
-    c->tc_workers[cl - 1] = (prop.major == 10 && slim_tc_shape_ok(d, H, d_k, dtype, rope_theta != 0.0, cl)) ? slim_tc_workers(c, cl) : 0;
+    if (kdtype == SLIM_FP4) c->tc_workers[cl - 1] = prop.major == 10 && cl == 2 ? slim_fp4_tc_workers(c) : 0;
+    else c->tc_workers[cl - 1] = (prop.major == 10 && slim_tc_shape_ok(d, H, d_k, dtype, rope_theta != 0.0, cl)) ? slim_tc_workers(c, cl) : 0;
     if (c->tc_workers[cl - 1] < 0) c->tc_workers[cl - 1] = 0;
     if (c->tc_workers[cl - 1] > 0) c->tc_ok = 1;
   }
@@ -498,12 +500,13 @@ slim_status decode_impl(slim_ctx* ctx, const void* q, const slim_cache* cache, c
   if (!xcache && ctx->e != ctx->d) return SLIM_ERR_UNSUPPORTED;   // the K-cache scheme needs square projections
   if (xcache && cache->block_table) return SLIM_ERR_UNSUPPORTED;
   const bool fp4 = ctx->kdtype == SLIM_FP4;
-  if (fp4) path = SLIM_PATH_GENERIC;
   if (path < 0) return SLIM_ERR_UNSUPPORTED;
   // CTAs per worker: the pair when the kernel computes the scores, the lone CTA with external scores
   int cl = 0;
   const bool fp8_tc = path == SLIM_PATH_TC && ctx->kdtype == SLIM_FP8;      // decoded into a bf16 scratch first
-  if (path == SLIM_PATH_TC) {
+  if (path == SLIM_PATH_TC && fp4) {
+    cl = 2;
+  } else if (path == SLIM_PATH_TC) {
     const int pref = xcache ? 1 : 2, other = 3 - pref;
     if (ctx->tc_workers[pref - 1] > 0 && (fp8_tc || cache->has_tmap[pref - 1])) cl = pref;
     else if (ctx->tc_workers[other - 1] > 0 && (fp8_tc || cache->has_tmap[other - 1])) cl = other;
@@ -538,7 +541,7 @@ slim_status decode_impl(slim_ctx* ctx, const void* q, const slim_cache* cache, c
   p.num_pages = cache->num_pages;
   // K-cache path on the tensor cores: the decode kernel writes the newest key rows itself, and a sequence
   // with a flagged unit is recomputed by the combine kernel (no append kernel, no redo kernel)
-  const bool tc_kcache = !xcache && path == SLIM_PATH_TC && !ctx->opt_legacy_flow;
+  const bool tc_kcache = !xcache && path == SLIM_PATH_TC && !fp4 && !ctx->opt_legacy_flow;
   p.k_new = (tc_kcache && !fp8_tc) ? k_new : nullptr;        // (new rows of an 8-bit cache go through the quantising append)
   p.redo_in_combine = (tc_kcache && ctx->proj_ok && !part) ? 1 : 0;
   p.pos_tiles = part ? part->first_tile : nullptr;
@@ -593,6 +596,9 @@ slim_status decode_impl(slim_ctx* ctx, const void* q, const slim_cache* cache, c
         launches += 1;
       }
     }
+  } else if (fp4 && path == SLIM_PATH_TC) {
+    e = slim_launch_fp4_tc(ctx, p, reinterpret_cast<float*>(ws + L.umax), st);
+    ++launches;
   } else if (path == SLIM_PATH_TC) {
     e = slim_launch_tc(ctx, tc_cache, p, st);
     ++launches;
