@@ -433,6 +433,7 @@ slim_status slim_cache_create(slim_ctx* ctx, slim_cache** out, void* k_storage, 
     if (slim_xscores_make_tmap(ctx, c) == cudaSuccess) c->has_xmap = 1;
     else cudaGetLastError();
   }
+  if (ctx->kdtype == SLIM_FP4 && ctx->tc_ok && slim_fp4_tc_make_tmaps(ctx, c) != cudaSuccess) cudaGetLastError();
   *out = c;
   return SLIM_OK;
 }
@@ -462,6 +463,7 @@ slim_status slim_cache_create_paged(slim_ctx* ctx, slim_cache** out, void* pool,
       else cudaGetLastError();
     }
   }
+  if (ctx->kdtype == SLIM_FP4 && ctx->tc_ok && slim_fp4_tc_make_tmaps(ctx, c) != cudaSuccess) cudaGetLastError();
   c->has_xmap = 0;                                     // the X-cache scheme takes contiguous caches only
   *out = c;
   return SLIM_OK;
@@ -505,7 +507,7 @@ slim_status decode_impl(slim_ctx* ctx, const void* q, const slim_cache* cache, c
   int cl = 0;
   const bool fp8_tc = path == SLIM_PATH_TC && ctx->kdtype == SLIM_FP8;      // decoded into a bf16 scratch first
   if (path == SLIM_PATH_TC && fp4) {
-    cl = 2;
+    cl = cache->has_tmap[0] && cache->has_tmap[1] ? 2 : 0;
   } else if (path == SLIM_PATH_TC) {
     const int pref = xcache ? 1 : 2, other = 3 - pref;
     if (ctx->tc_workers[pref - 1] > 0 && (fp8_tc || cache->has_tmap[pref - 1])) cl = pref;
@@ -597,7 +599,7 @@ slim_status decode_impl(slim_ctx* ctx, const void* q, const slim_cache* cache, c
       }
     }
   } else if (fp4 && path == SLIM_PATH_TC) {
-    e = slim_launch_fp4_tc(ctx, p, reinterpret_cast<float*>(ws + L.umax), st);
+    e = slim_launch_fp4_tc(ctx, cache, p, reinterpret_cast<float*>(ws + L.umax), st);
     ++launches;
   } else if (path == SLIM_PATH_TC) {
     e = slim_launch_tc(ctx, tc_cache, p, st);

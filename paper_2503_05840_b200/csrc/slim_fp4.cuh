@@ -59,4 +59,5 @@ __device__ __forceinline__ unsigned slim_fp4_code(float k, float s) {
 cudaError_t slim_launch_fp4_decode(const slim_ctx* ctx, const SlimDecodeParams& p, float* scores, cudaStream_t st);
 // tensor cores (slim_fp4_tc.cu): pairs of CTAs that fit the device, 0 = not this shape; umax: [units][H] scratch
 int slim_fp4_tc_workers(const slim_ctx* ctx);
-cudaError_t slim_launch_fp4_tc(const slim_ctx* ctx, const SlimDecodeParams& p, float* umax, cudaStream_t st);
+cudaError_t slim_fp4_tc_make_tmaps(const slim_ctx* ctx, slim_cache* c);       // codes in tmap[0], scales in tmap[1]
+cudaError_t slim_launch_fp4_tc(const slim_ctx* ctx, const slim_cache* c, const SlimDecodeParams& p, float* umax, cudaStream_t st);

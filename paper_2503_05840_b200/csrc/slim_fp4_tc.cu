@@ -4,22 +4,24 @@
 // The work is split as in the bf16 kernel (slim_tc.cu): a worker is a pair of CTAs, each with half of the columns and the
 // heads that live in them; both walk the worker's tiles of 16 rows; U^T[d x heads] stays in tensor memory; a unit's
 // (reference, l, U) goes to the common combine and projection.  What differs is that a tile has to be decoded:
-//   load warp    a tile's code and scale rows, one bulk copy a row, into a ring (a quarter of bf16's bytes)
-//   score warps  one head each.  A thread (g, j) = (lane / 4, lane % 4) has rows g and g + 8 and a quarter of the head's
-//                rotation pairs.  Codes become float16 pairs (exact: code times scale has six significant bits), which
+//   load thread  a tile's codes and scales, one TMA load each, into a ring (a quarter of bf16's bytes)
+//   score warps  one or two heads each.  A thread (g, j) = (lane / 4, lane % 4) has rows g and g + 8 and a quarter of the
+//                head's rotation pairs.  Codes become float16 pairs (exact: code times scale has six significant bits), which
 //                  - are stored as the tile that the tensor core reads (MN-major, 128-byte swizzle), and
 //                  - are rotated by g and fed to m16n8k16 products with the query.  Key row t0 + g (+ 8) rotated by g meets the
 //                    query turned back to t0 (column 0) or t0 + 8 (column 1), so the rotation factors of a thread are
 //                    the same for every tile and live in registers; half of each is taken, so that nothing leaves float16.
+//                The warp turns its heads' queries back by a tile (float32, re-seeded from the tables every 64 tiles) behind each
+//                tile and lays the two columns down in the order the products read them.
 //                Then p = 2^(s - m) in float16, into the P tile.
-//   query warp   turns the queries of all heads back by 16 positions a tile (float32, re-seeded from the tables every 64
-//                tiles) and lays the two columns down in the order the products read them
 //   MMA thread   of the even CTA: U^T[256 columns x 32 heads] += K^T[256 x 16] P^T[16 x 32] a pair of 128-column chunks, each
-//                CTA supplying its own 128 columns and its own 16 heads' P (cta_group::2), so no probabilities travel
+//                CTA supplying its own 128 columns and its own 16 heads' P (cta_group::2), so no probabilities travel; the odd
+//                CTA's passes on that its tile is complete
 // float16 P: the reference is the first tile's maximum plus 8 (log2 units), so p reaches up to 2^15 for scores 23 above that
 // maximum and keeps 11 bits down to 2^-14; smaller ones lose bits against terms 2^6 their size.  A score further up flags
 // the unit; flagged units are walked again at the end, with the largest score as reference (known by then).
 #include <cuda.h>
+#include <cstring>
 
 #include "slim_fp4.cuh"
 #include "slim_ptx.cuh"
@@ -30,7 +32,6 @@ using namespace slim_ptx;
 namespace {
 
 constexpr int MAX_ST = 4, MAX_PK = 8;    // float16 stages, stages of packed tiles
-constexpr int NQ = 2;                    // stages of query columns
 constexpr int RESEED = 64;
 constexpr float BIAS = 8.f, XMAX = 15.f;
 
@@ -43,12 +44,11 @@ struct Lane {
 };
 
 struct Geom {
-  int dsl, hl, nch;                      // columns, heads, 128-column chunks of a CTA
-  int sets, nsw, nswl;                   // score-warp sets, warps of a set (one head each), launched score / epilogue warps
+  int dsl, hl, nch, hpw;                 // columns, heads, 128-column chunks of a CTA; heads of a score warp
+  int sets, nsw, nswl;                   // score-warp sets, warps of a set, launched score / epilogue warps
   int nst, npk;
-  int stage, pk;                         // bytes of a float16 stage and of a packed one
-  int pp, spw, cb;                       // packed row pitches (codes, scales), bytes of a row's codes
-  int pitch, spitch;                     // of the cache
+  int stage, pk;                         // bytes of a float16 stage and of a packed one (codes in chunks of 64 bytes x 16 rows, scales)
+  int win, s_lo[2], s_shift[2];          // bytes of a row's scales in a stage; where each CTA's begin, and its first among them
   int tmem_cols;
   int off_p, off_pk, off_q, off_bar, smem;
 };
@@ -74,11 +74,28 @@ __device__ __forceinline__ uint32_t half2_of(f32x2 v) {
   asm("{\n\t.reg .f32 lo, hi;\n\tmov.b64 {lo, hi}, %1;\n\tcvt.rn.f16x2.f32 %0, hi, lo;\n\t}" : "=r"(d) : "l"(v));
   return d;
 }
+__device__ __forceinline__ uint32_t hneg2(uint32_t a) { uint32_t d; asm("neg.f16x2 %0, %1;" : "=r"(d) : "r"(a)); return d; }
+__device__ __forceinline__ uint32_t prmt(uint32_t a, uint32_t sel) { uint32_t d; asm("prmt.b32 %0, %1, 0, %2;" : "=r"(d) : "r"(a), "r"(sel)); return d; }
 __device__ __forceinline__ uint32_t lds_u8(uint32_t a) { uint32_t v; asm volatile("ld.shared.u8 %0, [%1];" : "=r"(v) : "r"(a)); return v; }
 __device__ __forceinline__ uint32_t lds_u16(uint32_t a) { uint32_t v; asm volatile("ld.shared.u16 %0, [%1];" : "=r"(v) : "r"(a)); return v; }
 __device__ __forceinline__ uint32_t lds32(uint32_t a) { uint32_t v; asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(a)); return v; }
 __device__ __forceinline__ uint2 lds64(uint32_t a) { uint2 v; asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(a)); return v; }
 __device__ __forceinline__ void sts64(uint32_t a, uint32_t x, uint32_t y) { asm volatile("st.shared.v2.u32 [%0], {%1, %2};" ::"r"(a), "r"(x), "r"(y) : "memory"); }
+// Arrival on a barrier of the other CTA that orders nothing beyond this CTA.  Enough where the other CTA's threads read nothing
+// of what this one wrote: each tensor core reads its own SM's shared memory, made visible to it before.  (Release at cluster
+// scope took 1500 clocks a tile.)
+__device__ __forceinline__ void mbar_arrive_remote(uint32_t cluster_bar) {
+  asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
+}
+__device__ __forceinline__ bool elect_one() {
+  uint32_t v;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.b32 %0, 1, 0, p;\n\t}" : "=r"(v));
+  return v != 0;
+}
+__device__ __forceinline__ void umma2_f16(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
+  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+               ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(acc) : "memory");
+}
 // 2^e that brings x (> 0, finite) into [1, 2); 1 for anything else
 __device__ __forceinline__ float pow2_to_one(float x) {
   if (!(x > 0.f) || !(x <= 3.4e38f)) return 1.f;
@@ -86,35 +103,45 @@ __device__ __forceinline__ float pow2_to_one(float x) {
   return __int_as_float((e + 127) << 23);
 }
 
-template <int DK, bool ROPE, int MAXT>
-__global__ void __launch_bounds__(MAXT, 1) fp4_tc_kernel(const SlimDecodeParams p, const Geom g, float* __restrict__ umax) {
+// A ring's next stage and the phase of its barriers
+struct Ring {
+  int st;
+  uint32_t ph;
+  __device__ __forceinline__ void step(int by, int n) {
+    st += by;
+    if (st >= n) { st -= n; ph ^= 1u; }
+  }
+};
+
+template <int DK, bool ROPE, int HPW, int MAXT>
+__global__ void __launch_bounds__(MAXT, 1) fp4_tc_kernel(const __grid_constant__ CUtensorMap cmap, const __grid_constant__ CUtensorMap smap,
+                                                         const SlimDecodeParams p, const Geom g, float* __restrict__ umax) {
   typedef Lane<DK> L;
   constexpr int HALF = L::HALF, PE = L::PE, NP = L::NP, KS = L::KS, SB = L::SB, HB = 8 * SB;
   extern __shared__ unsigned char smem_raw[];
   const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
   unsigned char* sm = smem_raw + (base - raw);
-  const uint32_t s_p = base + g.off_p, s_pk = base + g.off_pk, s_qb = base + g.off_q;
+  const uint32_t s_p = base + g.off_p, s_pk = base + g.off_pk, s_q = base + g.off_q;
   const uint32_t bars = base + g.off_bar;
-  const uint32_t b_pkf = bars, b_pke = b_pkf + 8 * MAX_PK, b_pf = b_pke + 8 * MAX_PK, b_ke = b_pf + 8 * MAX_ST;
-  const uint32_t b_qf = b_ke + 8 * MAX_ST, b_qe = b_qf + 8 * NQ, b_uf = b_qe + 8 * NQ, b_ue = b_uf + 8, b_xm = b_ue + 8, b_xl = b_xm + 8;
+  const uint32_t b_pkf = bars, b_pke = b_pkf + 8 * MAX_PK, b_pf = b_pke + 8 * MAX_PK, b_px = b_pf + 8 * MAX_ST, b_ke = b_px + 8 * MAX_ST;
+  const uint32_t b_uf = b_ke + 8 * MAX_ST, b_ue = b_uf + 8, b_xm = b_ue + 8, b_xl = b_xm + 8;
   unsigned char* misc = sm + (b_xl + 8 - base);
   uint32_t* s_tmem = reinterpret_cast<uint32_t*>(misc);
   volatile int* s_abort = reinterpret_cast<volatile int*>(misc + 4);
-  float* s_qs = reinterpret_cast<float*>(misc + 8);           // [2][16] what a unit's query columns were divided by
-  float* s_xm = s_qs + 32;                                    // [16] reference, from the set that has a unit's first tile
+  float* s_xm = reinterpret_cast<float*>(misc + 8);           // [16] reference, from the set that has a unit's first tile
   float* s_xl = s_xm + 16;                                    // [16] the other set's share of l
   float* s_xx = s_xl + 16;                                    // [16] and its largest score
   int* s_prefix = reinterpret_cast<int*>(s_xx + 16);
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const uint32_t rank = cluster_ctarank();
   const int w = blockIdx.x / 2;
-  const int w_load = g.nswl, w_mma = g.nswl + 1, w_query = g.nswl + 2;
+  const int w_load = g.nswl, w_mma = g.nswl + 1;
   const int nepi = (g.nswl / 4) * 4;
 
   if (tid == 0) {
+    prefetch_tensormap(&cmap); prefetch_tensormap(&smap);
     for (int i = 0; i < MAX_PK; ++i) { mbar_init(b_pkf + 8 * i, 1); mbar_init(b_pke + 8 * i, g.nsw); }
-    for (int i = 0; i < MAX_ST; ++i) { mbar_init(b_pf + 8 * i, 2 * g.nsw); mbar_init(b_ke + 8 * i, 1); }
-    for (int i = 0; i < NQ; ++i) { mbar_init(b_qf + 8 * i, 1); mbar_init(b_qe + 8 * i, ROPE ? g.nsw : g.nsw * g.sets); }
+    for (int i = 0; i < MAX_ST; ++i) { mbar_init(b_pf + 8 * i, g.nsw); mbar_init(b_px + 8 * i, 1); mbar_init(b_ke + 8 * i, 1); }
     mbar_init(b_uf, 1);
     mbar_init(b_ue, 2 * nepi);
     mbar_init(b_xm, g.nsw);
@@ -136,8 +163,10 @@ __global__ void __launch_bounds__(MAXT, 1) fp4_tc_kernel(const SlimDecodeParams 
   const int g_begin = in_range ? slim_worker_start(sc, w) : 0;
   const int g_end = in_range ? slim_worker_start(sc, w + 1) : 0;
 
-  // Where a role stands, over both sweeps: tiles (it) and units (uc) so far.
+  // Where a role stands, over both sweeps: tiles (it) and units (uc) so far, the next stage of each ring.
   int it = 0, uc = 0;
+  const int set = warp < g.nswl && warp >= g.nsw ? 1 : 0;      // score warps: a set takes every g.sets-th tile
+  Ring rp = {set, 0u}, rk = {set, 0u};
   bool ok = true;
   for (int sweep = 0; sweep < 2; ++sweep) {
     // units of this sweep: all, then those flagged in either CTA
@@ -145,9 +174,8 @@ __global__ void __launch_bounds__(MAXT, 1) fp4_tc_kernel(const SlimDecodeParams 
     if (warp < g.nswl) {
       // =========================== score / epilogue warps ===========================
       const bool scorer = warp < g.nsw * g.sets;
-      const int set = warp >= g.nsw ? 1 : 0, hd = warp - set * g.nsw;       // a set takes every g.sets-th tile; head within the CTA
+      const int hd0 = (warp - set * g.nsw) * HPW;                            // the warp's first head within the CTA
       const int gr = lane >> 2, j = lane & 3;
-      const int head = (int)rank * g.hl + hd;
       uint32_t cs[NP * PE / 2], sn[NP * PE / 2];                 // half of cos and sin of gr theta, the thread's pairs
       if (ROPE && scorer) {
 #pragma unroll
@@ -159,18 +187,46 @@ __global__ void __launch_bounds__(MAXT, 1) fp4_tc_kernel(const SlimDecodeParams 
             sn[x * (PE / 2) + e] = half2_of(0.5f * a.y, 0.5f * b.y);
           }
       }
-      // byte offsets of the thread's pieces: codes in a packed row, scales, place in the float16 tile
-      const uint32_t c_off = (uint32_t)(gr * g.pp + (hd * DK + L::col(j, 0)) / 2);
-      const int s_shift = (int)((rank * (g.dsl / FP4_GROUP)) & 15);
-      const uint32_t s_off = (uint32_t)(16 * g.pp + gr * g.spw + s_shift);
-      auto tile_off = [&](int half, int x) {
+      // Offsets of the thread's pieces for its first head (the others follow at fixed distances; d_k = 96 goes piece by piece):
+      // codes (64-byte chunks of 16 rows, 64-byte swizzle), scales, float16 tile (64-column chunks of 16 rows, 128-byte swizzle)
+      const int sw = (gr >> 1) & 3;
+      auto code_off = [&](int hd, int half, int x) {
+        const int o = hd * (DK / 2) + half * (HALF / 2) + L::col(j, x) / 2;
+        return (uint32_t)((o >> 6) * 1024 + gr * 64 + ((((o >> 4) & 3) ^ sw) << 4) + (o & 15));
+      };
+      auto tile_off = [&](int hd, int half, int x) {
         const int c = hd * DK + half * HALF + L::col(j, x);
         return (uint32_t)((c >> 6) * 2048 + gr * 128 + ((((c & 63) >> 3) ^ gr) << 4) + (c & 7) * 2);
       };
-      uint32_t qb[2 * KS];
+      const uint32_t c0 = code_off(hd0, 0, 0), t0_off = tile_off(hd0, 0, 0);
+      const int s_at = rank ? g.s_shift[1] : g.s_shift[0];
+      auto scale_off = [&](int i) { return (uint32_t)(8 * g.dsl + ((s_at + i) >> 4) * 256 + gr * 16 + ((s_at + i) & 15)); };       // of the CTA's group i
+      // byte of a head's scale word -> the low byte of both halves of a register: first half of the head, second half
+      const uint32_t sel0 = DK == 128 ? 0x4040u + 0x0101u * (uint32_t)(j >> 1) : 0x4040u, sel1 = sel0 + (DK == 128 ? 0x0202u : 0x0101u);
+      const uint32_t q_own = s_q + (uint32_t)((set * g.hl + hd0) * HB);      // the warp's query columns
+      // A product's column depends on its own column of the query operand only, so all eight are put to use: columns 0, 3 (and 4, 7)
+      // are the first (second) head's two, and what the others hold does not matter.  Thread (gr, j) then finds in its own
+      // sums the score of row gr + 8 (j & 1) under head hd0 + (j >> 1), and no score has to move.
+      const uint32_t q_rd = q_own + (uint32_t)((HPW == 2 ? gr >> 2 : 0) * HB + (((gr & 3) >> 1) * 4 + j) * SB);
+      const int mine = HPW == 2 ? j >> 1 : 0, odd = j & 1;                   // the thread's head and row half
+      const bool scores = HPW == 2 || j < 2;
+      const uint32_t p_off = (uint32_t)(((hd0 + mine) & 7) * 16 + ((hd0 + mine) >> 3) * 256 + odd * 128 + gr * 2);
+      // Queries: lane l has pairs 2 l, 2 l + 1 of a head, for the thread and step that read them
+      const bool live = lane < HALF / 2;
+      int jj, xx;
+      if (DK == 128) { jj = lane / 8; xx = lane % 8; }
+      else if (DK == 64) { jj = (lane / 4) & 3; xx = lane % 4; }
+      else { jj = (lane >> 1) & 3; xx = 2 * (lane >> 3) + (lane & 1); }
+      const uint32_t q_wr = q_own + (uint32_t)(jj * SB + xx * 8);
+      f32x2 q1[HPW], q2[HPW], cst = 0, sst = 0, nst = 0, c8 = 0, s8 = 0, n8 = 0;       // cos and sin of a set's step, and of 8 theta
 #pragma unroll
-      for (int x = 0; x < 2 * KS; ++x) qb[x] = 0u;
-      float qs = 1.f;
+      for (int u = 0; u < HPW; ++u) q1[u] = q2[u] = 0;
+      if (ROPE && live && scorer) {
+        const float2 a = p.rope_base[g.sets * HALF + 2 * lane], b = p.rope_base[g.sets * HALF + 2 * lane + 1];
+        const float2 c = p.rope_off[8 * HALF + 2 * lane], d = p.rope_off[8 * HALF + 2 * lane + 1];
+        cst = pack2(a.x, b.x); sst = pack2(a.y, b.y); nst = pack2(-a.y, -b.y);
+        c8 = pack2(c.x, d.x); s8 = pack2(c.y, d.y); n8 = pack2(-c.y, -d.y);
+      }
       for (int gg = g_begin; gg < g_end && ok;) {
         const int b = slim_seq_of_tile(s_prefix, p.batch, gg);
         const int seg_end = min(g_end, s_prefix[b + 1]);
@@ -180,146 +236,216 @@ __global__ void __launch_bounds__(MAXT, 1) fp4_tc_kernel(const SlimDecodeParams 
         const int len = min(max(p.lengths[b], 0), p.t_cap);
         const int kt0 = g.sets == 1 ? 0 : ((set - it) & 1);          // this set's first tile of the unit
         const bool owner = kt0 == 0;
-        float mref = 0.f, lsum = 0.f, rmax = -INFINITY;
-        if (scorer) {
-          if (!ROPE) {
-            ok = mbar_wait<false>(b_qf + 8 * (uc & 1), (uc >> 1) & 1, s_abort, p.status);
-            if (gr < 2) {
-#pragma unroll
-              for (int x = 0; x < KS / 2; ++x) {
-                const uint4 v = lds128(s_qb + (uint32_t)((uc & 1) * g.hl * HB + hd * HB + (gr * 4 + j) * SB + 16 * x));
-                qb[4 * x] = v.x; qb[4 * x + 1] = v.y; qb[4 * x + 2] = v.z; qb[4 * x + 3] = v.w;
-              }
-            }
-            qs = s_qs[(uc & 1) * 16 + hd];
-            __syncwarp();
-            if (lane == 0) mbar_arrive(b_qe + 8 * (uc & 1));
+        float qs = 1.f, mref = 0.f, lsum = 0.f, rmax = -INFINITY;    // of the thread's head
+        // The warp's queries at position pos, divided by a power of two a head
+        auto seed = [&](int pos) {
+          f32x2 c = pack2(1.f, 1.f), s = pack2(0.f, 0.f), ns = s;
+          if (ROPE && live) {
+            const float2 ba = __ldg(p.rope_base + (size_t)(pos / SLIM_TT) * HALF + 2 * lane), bb = __ldg(p.rope_base + (size_t)(pos / SLIM_TT) * HALF + 2 * lane + 1);
+            const float2 oa = __ldg(p.rope_off + (pos % SLIM_TT) * HALF + 2 * lane), ob = __ldg(p.rope_off + (pos % SLIM_TT) * HALF + 2 * lane + 1);
+            const float sa = ba.y * oa.x + ba.x * oa.y, sb = bb.y * ob.x + bb.x * ob.y;
+            c = pack2(ba.x * oa.x - ba.y * oa.y, bb.x * ob.x - bb.y * ob.y);
+            s = pack2(sa, sb); ns = pack2(-sa, -sb);
           }
-          for (int kt = kt0; kt < ntile && ok; kt += g.sets) {
-            const int n = it + kt, st = n % g.nst, ps = n % g.npk;
+          const uint32_t* Q = reinterpret_cast<const uint32_t*>(p.q);
+#pragma unroll
+          for (int u = 0; u < HPW; ++u) {
+            const size_t qi = (((size_t)b * p.d + (size_t)((int)rank * g.hl + hd0 + u) * DK) >> 1) + lane;
+            const f32x2 x = live ? unpack2(__ldg(Q + qi)) : 0, y = live ? unpack2(__ldg(Q + qi + HALF / 2)) : 0;
+            float m0, m1, m2, m3;
+            asm("mov.b64 {%0, %1}, %2;" : "=f"(m0), "=f"(m1) : "l"(x));
+            asm("mov.b64 {%0, %1}, %2;" : "=f"(m2), "=f"(m3) : "l"(y));
+            float mx = fmaxf(fmaxf(fabsf(m0), fabsf(m1)), fmaxf(fabsf(m2), fabsf(m3)));
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+            const float up = pow2_to_one(mx);                        // the largest element of a head into [1, 2)
+            const f32x2 f = pack2(up, up), xf = mul2(x, f), yf = mul2(y, f);
+            q1[u] = ROPE ? fma2(yf, s, mul2(xf, c)) : xf;
+            q2[u] = ROPE ? fma2(xf, ns, mul2(yf, c)) : yf;
+            if (u == mine) qs = (ROPE ? 2.f : 1.f) * p.qscale / up;  // what turns sums into scores (the factors on the keys are halved)
+          }
+        };
+        auto lay = [&]() {                                           // the two columns of the next tile; the queries a step back
+#pragma unroll
+          for (int u = 0; u < HPW; ++u) {
+            if (live) {
+              sts64(q_wr + u * HB, half2_of(q1[u]), half2_of(q2[u]));
+              if (ROPE) sts64(q_wr + u * HB + 4 * SB, half2_of(fma2(q2[u], n8, mul2(q1[u], c8))), half2_of(fma2(q1[u], s8, mul2(q2[u], c8))));
+              else sts64(q_wr + u * HB + 4 * SB, half2_of(q1[u]), half2_of(q2[u]));
+            }
+            if (ROPE) {
+              const f32x2 x = fma2(q2[u], nst, mul2(q1[u], cst));
+              q2[u] = fma2(q1[u], sst, mul2(q2[u], cst));
+              q1[u] = x;
+            }
+          }
+        };
+        if (scorer) {
+          int fresh = 0;                                             // tiles since the queries came from the tables
+          if (kt0 < ntile) {
+            // q(len - 1) against keys turned by t - t0: the query at len - 1 - t0 (not negative: t0 < len)
+            seed(len - 1 - (tile0 + kt0) * SLIM_TT);
+            lay();
+          }
+          for (int kt = kt0; kt < ntile && ok; kt += g.sets, rp.step(g.sets, g.npk), rk.step(g.sets, g.nst)) {
             const int t0 = (tile0 + kt) * SLIM_TT;
-            ok = mbar_wait<false>(b_pkf + 8 * ps, (n / g.npk) & 1, s_abort, p.status);
-            if (ROPE) ok = mbar_wait<false>(b_qf + 8 * (n & 1), (n >> 1) & 1, s_abort, p.status) && ok;
-            ok = mbar_wait<false>(b_ke + 8 * st, ((n / g.nst) & 1) ^ 1, s_abort, p.status) && ok;
+            const uint32_t pk = s_pk + (uint32_t)(rp.st * g.pk), kh = base + (uint32_t)(rk.st * g.stage);
+            ok = mbar_wait<false>(b_pkf + 8 * rp.st, rp.ph, s_abort, p.status);
+            ok = mbar_wait<false>(b_ke + 8 * rk.st, rk.ph ^ 1u, s_abort, p.status) && ok;
             ok = __all_sync(0xffffffffu, ok);
             if (!ok) break;
-            if (ROPE) {
-              if (gr < 2) {
-#pragma unroll
-                for (int x = 0; x < KS / 2; ++x) {
-                  const uint4 v = lds128(s_qb + (uint32_t)((n & 1) * g.hl * HB + hd * HB + (gr * 4 + j) * SB + 16 * x));
-                  qb[4 * x] = v.x; qb[4 * x + 1] = v.y; qb[4 * x + 2] = v.z; qb[4 * x + 3] = v.w;
-                }
-              }
-              if (kt == kt0) qs = s_qs[(uc & 1) * 16 + hd];
-            }
-            const uint32_t pk = s_pk + (uint32_t)(ps * g.pk), kh = base + (uint32_t)(st * g.stage);
-            // codes of rows gr and gr + 8: first and second half of the head
-            uint32_t cw[2][2][NP];
-#pragma unroll
-            for (int r = 0; r < 2; ++r)
-#pragma unroll
-              for (int half = 0; half < 2; ++half) {
-                const uint32_t at = pk + c_off + (uint32_t)(r * 8 * g.pp + half * HALF / 2);
-                if constexpr (DK == 128) {
-                  const uint2 v = lds64(at);
-                  cw[r][half][0] = v.x; cw[r][half][1] = v.y;
-                } else if constexpr (DK == 64) {
-                  cw[r][half][0] = lds32(at);
-                } else {
-#pragma unroll
-                  for (int x = 0; x < NP; ++x) cw[r][half][x] = lds_u16(at + 8 * x);
-                }
-              }
+            __syncwarp();                                              // the query columns are down
             const bool in0 = t0 + gr < len, in1 = t0 + gr + 8 < len;
-            float acc[2][4];
+            // codes and scales of rows gr and gr + 8, first and second half of the heads
+            uint32_t cw[HPW][2][2][NP], sc[HPW][2][2][DK == 96 ? NP : 1], qb[2 * KS];
+            if constexpr (DK != 96) {
+              const uint32_t ca = pk + c0, cb = ca ^ (DK == 128 ? 32u : 16u);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) acc[0][i] = acc[1][i] = 0.f;
-            uint32_t sc2[2][2];
-#pragma unroll
-            for (int x = 0; x < NP; ++x) {
-              uint32_t k[2][2][4];                                   // [row][half][pair of columns]
-#pragma unroll
-              for (int half = 0; half < 2; ++half) {
-                const uint32_t to = kh + tile_off(half, x);
-                uint32_t both[4];                                    // pieces of four columns: the two rows side by side
-                if (PE == 4) decode8(cw[0][half][x] | (cw[1][half][x] << 16), both);
+              for (int u = 0; u < HPW; ++u)
 #pragma unroll
                 for (int r = 0; r < 2; ++r) {
-                  if (x == 0 || DK == 96) {                          // (a thread's pieces of a half share a group elsewhere)
-                    const uint32_t byte = lds_u8(pk + s_off + (uint32_t)(r * 8 * g.spw + (hd * DK + half * HALF + L::col(j, x)) / FP4_GROUP));
-                    sc2[r][half] = (r ? in1 : in0) ? byte * 0x00800080u : 0u;       // rows behind the sequence become zeros
+                  if constexpr (DK == 128) {
+                    const uint2 v = lds64(ca + u * 1024 + r * 512), y = lds64(cb + u * 1024 + r * 512);
+                    cw[u][r][0][0] = v.x; cw[u][r][0][1] = v.y;
+                    cw[u][r][1][0] = y.x; cw[u][r][1][1] = y.y;
+                  } else {
+                    // heads two by two in a chunk: the second 32 bytes further, across the swizzle (hd0 is even where HPW is 2)
+                    cw[u][r][0][0] = lds32((u ? ca ^ 32u : ca) + r * 512);
+                    cw[u][r][1][0] = lds32((u ? cb ^ 32u : cb) + r * 512);
                   }
-                  if (PE == 8) decode8(cw[r][half][x], k[r][half]);
-                  else { k[r][half][0] = both[2 * r]; k[r][half][1] = both[2 * r + 1]; }
-#pragma unroll
-                  for (int e = 0; e < PE / 2; ++e) k[r][half][e] = hmul2(k[r][half][e], sc2[r][half]);
-                  if (PE == 8) sts128(to + r * 1024, make_uint4(k[r][half][0], k[r][half][1], k[r][half][2], k[r][half][3]));
-                  else sts64(to + r * 1024, k[r][half][0], k[r][half][1]);
+                  const uint32_t at = pk + scale_off((hd0 + u) * (DK / FP4_GROUP)) + r * 128;
+                  uint32_t word = DK == 128 ? lds32(at) : lds_u16(at);
+                  word = (r ? in1 : in0) ? word : 0u;                  // rows behind the sequence become zeros
+                  sc[u][r][0][0] = prmt(word, sel0) << 7;
+                  sc[u][r][1][0] = prmt(word, sel1) << 7;
                 }
-              }
+            } else {
 #pragma unroll
-              for (int e = 0; e < PE / 2; ++e) {
-                const int i = x * (PE / 2) + e;
-                uint32_t a0 = k[0][0][e], a1 = k[1][0][e], a2 = k[0][1][e], a3 = k[1][1][e];
-                if (ROPE) {
-                  const uint32_t c = cs[i], s = sn[i], ns = s ^ 0x80008000u;
-                  const uint32_t r0 = hfma2(a2, s, hmul2(a0, c)), r2 = hfma2(a0, ns, hmul2(a2, c));
-                  const uint32_t r1 = hfma2(a3, s, hmul2(a1, c)), r3 = hfma2(a1, ns, hmul2(a3, c));
-                  a0 = r0; a1 = r1; a2 = r2; a3 = r3;
+              for (int u = 0; u < HPW; ++u)
+#pragma unroll
+                for (int r = 0; r < 2; ++r)
+#pragma unroll
+                  for (int half = 0; half < 2; ++half)
+#pragma unroll
+                    for (int x = 0; x < NP; ++x) {
+                      cw[u][r][half][x] = lds_u16(pk + code_off(hd0 + u, half, x) + r * 512);
+                      const uint32_t byte = lds_u8(pk + scale_off(((hd0 + u) * DK + half * HALF + L::col(j, x)) / FP4_GROUP) + r * 128);
+                      sc[u][r][half][x] = (r ? in1 : in0) ? byte * 0x00800080u : 0u;
+                    }
+            }
+#pragma unroll
+            for (int x = 0; x < KS / 2; ++x) {
+              const uint4 v = lds128(q_rd + 16 * x);
+              qb[4 * x] = v.x; qb[4 * x + 1] = v.y; qb[4 * x + 2] = v.z; qb[4 * x + 3] = v.w;
+            }
+            if (ROPE) {
+              __syncwarp();
+              lay();                                                   // of the next tile
+            }
+            const uint32_t ta = kh + t0_off;
+            float acc[HPW][2][4];
+#pragma unroll
+            for (int u = 0; u < HPW; ++u)
+#pragma unroll
+              for (int i = 0; i < 4; ++i) acc[u][0][i] = acc[u][1][i] = 0.f;
+#pragma unroll
+            for (int x = 0; x < NP; ++x) {
+#pragma unroll
+              for (int u = 0; u < HPW; ++u) {
+                uint32_t k[2][2][4];                                   // [row][half][pair of columns]
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                  uint32_t to;
+                  if (DK == 128) to = (x ? ta ^ 16u : ta) + u * 4096 + half * 2048;
+                  else if (DK == 64) to = (half ? ta ^ 64u : ta) + u * 2048;
+                  else to = kh + tile_off(hd0 + u, half, x);
+                  uint32_t both[4];                                    // pieces of four columns: the two rows side by side
+                  if (PE == 4) decode8(cw[u][0][half][x] | (cw[u][1][half][x] << 16), both);
+#pragma unroll
+                  for (int r = 0; r < 2; ++r) {
+                    if (PE == 8) decode8(cw[u][r][half][x], k[r][half]);
+                    else { k[r][half][0] = both[2 * r]; k[r][half][1] = both[2 * r + 1]; }
+#pragma unroll
+                    for (int e = 0; e < PE / 2; ++e) k[r][half][e] = hmul2(k[r][half][e], sc[u][r][half][DK == 96 ? x : 0]);
+                    if (PE == 8) sts128(to + r * 1024, make_uint4(k[r][half][0], k[r][half][1], k[r][half][2], k[r][half][3]));
+                    else sts64(to + r * 1024, k[r][half][0], k[r][half][1]);
+                  }
                 }
-                mma_f16(acc[i & 1], a0, a1, a2, a3, qb[2 * i], qb[2 * i + 1]);
+#pragma unroll
+                for (int e = 0; e < PE / 2; ++e) {
+                  const int i = x * (PE / 2) + e;
+                  uint32_t a0 = k[0][0][e], a1 = k[1][0][e], a2 = k[0][1][e], a3 = k[1][1][e];
+                  if (ROPE) {
+                    const uint32_t cc = cs[i], ss = sn[i], ns = hneg2(ss);
+                    const uint32_t r0 = hfma2(a2, ss, hmul2(a0, cc)), r2 = hfma2(a0, ns, hmul2(a2, cc));
+                    const uint32_t r1 = hfma2(a3, ss, hmul2(a1, cc)), r3 = hfma2(a1, ns, hmul2(a3, cc));
+                    a0 = r0; a1 = r1; a2 = r2; a3 = r3;
+                  }
+                  mma_f16(acc[u][i & 1], a0, a1, a2, a3, qb[2 * i], qb[2 * i + 1]);
+                }
               }
             }
-            // column 0 for row gr, column 1 for row gr + 8: both with thread j = 0
-            const float s0 = (acc[0][0] + acc[1][0]) * qs, s1 = (acc[0][3] + acc[1][3]) * qs;
-            const bool v0 = in0 && j == 0, v1 = in1 && j == 0;
+            float s;
+            {
+              const float e0 = acc[0][0][0] + acc[0][1][0], e1 = acc[0][0][3] + acc[0][1][3];
+              s = odd ? e1 : e0;
+              if (HPW == 2) {
+                const float f0 = acc[HPW - 1][0][0] + acc[HPW - 1][1][0], f1 = acc[HPW - 1][0][3] + acc[HPW - 1][1][3];
+                s = mine ? (odd ? f1 : f0) : s;
+              }
+              s *= qs;
+            }
+            const bool v = scores && (odd ? in1 : in0);
             if (kt == kt0) {
               if (sweep == 1) {
-                mref = __ldcg(umax + (size_t)unit * p.H + head);
+                if (scores) mref = __ldcg(umax + (size_t)unit * p.H + (int)rank * g.hl + hd0 + mine);
               } else if (owner) {
-                float mx = fmaxf(v0 ? s0 : -INFINITY, v1 ? s1 : -INFINITY);
+                float mx = v ? s : -INFINITY;
 #pragma unroll
-                for (int o = 4; o < 32; o <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
-                mx = __shfl_sync(0xffffffffu, mx, 0);
+                for (int o = 1; o < 32; o = o == 1 ? 4 : 2 * o) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
                 mref = mx + BIAS;
                 if (g.sets == 2) {
-                  if (lane == 0) s_xm[hd] = mref;
+                  if (lane == 0) {
+                    s_xm[hd0] = mref;
+                    mbar_arrive(b_xm);
+                  }
                   __syncwarp();
-                  if (lane == 0) mbar_arrive(b_xm);
                 }
               } else {
                 ok = mbar_wait<false>(b_xm, uc & 1, s_abort, p.status);
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
-                mref = s_xm[hd];
+                mref = s_xm[hd0];
               }
-              if (!(mref > -INFINITY)) mref = 0.f;                   // nothing but NaN so far
+              if (!(mref > -INFINITY)) mref = 0.f;                     // nothing but NaN so far
             }
-            if (v0) rmax = fmaxf(rmax, s0);
-            if (v1) rmax = fmaxf(rmax, s1);
-            float x0 = s0 - mref, x1 = s1 - mref;
-            if (((v0 && x0 > XMAX) || (v1 && x1 > XMAX)) && sweep == 0) p.unit_flags[2 * unit + (int)rank] = 1;
-            x0 = x0 > XMAX ? XMAX : x0;
-            x1 = x1 > XMAX ? XMAX : x1;
-            const __half p0 = __float2half_rn(v0 ? ex2_approx(x0) : 0.f), p1 = __float2half_rn(v1 ? ex2_approx(x1) : 0.f);
-            if (j == 0) {
-              lsum += __half2float(p0) + __half2float(p1);
-              sts_u16(s_p + (uint32_t)(st * 512) + p_offset(hd, gr), __half_as_ushort(p0));
-              sts_u16(s_p + (uint32_t)(st * 512) + p_offset(hd, gr + 8), __half_as_ushort(p1));
+            if (v) rmax = fmaxf(rmax, s);
+            float xv = s - mref;
+            if (v && xv > XMAX && sweep == 0) p.unit_flags[2 * unit + (int)rank] = 1;
+            xv = xv > XMAX ? XMAX : xv;
+            const __half pv = __float2half_rn(v ? ex2_approx(xv) : 0.f);
+            if (scores) {
+              lsum += __half2float(pv);
+              sts_u16(s_p + (uint32_t)(rk.st * 512) + p_off, __half_as_ushort(pv));
             }
             fence_proxy_async_smem();            // keys and probabilities -> tensor core
             __syncwarp();
             if (lane == 0) {
-              mbar_arrive_cluster(mapa(b_pf + 8 * st, 0));
-              mbar_arrive(b_pke + 8 * ps);
-              if (ROPE) mbar_arrive(b_qe + 8 * (n & 1));
+              mbar_arrive(b_pf + 8 * rk.st);
+              mbar_arrive(b_pke + 8 * rp.st);
+            }
+            if (ROPE && ++fresh == RESEED) {                           // (what was laid down for the next tile is replaced)
+              fresh = 0;
+              if (kt + g.sets < ntile) {
+                seed(len - 1 - (tile0 + kt + g.sets) * SLIM_TT);
+                lay();
+              }
             }
           }
           if (!ok) break;
           // ---- (reference, l) and the largest score of the unit ----
 #pragma unroll
-          for (int o = 4; o < 32; o <<= 1) {
+          for (int o = 1; o < 32; o = o == 1 ? 4 : 2 * o) {
             lsum += __shfl_xor_sync(0xffffffffu, lsum, o);
             rmax = fmaxf(rmax, __shfl_xor_sync(0xffffffffu, rmax, o));
           }
@@ -332,23 +458,24 @@ __global__ void __launch_bounds__(MAXT, 1) fp4_tc_kernel(const SlimDecodeParams 
               ok = mbar_wait<false>(b_xl, uc & 1, s_abort, p.status);
               ok = __all_sync(0xffffffffu, ok);
               if (!ok) break;
-              lsum += s_xl[hd];
-              rmax = fmaxf(rmax, s_xx[hd]);
+              lsum += s_xl[hd0];
+              rmax = fmaxf(rmax, s_xx[hd0]);
             } else {
               ok = mbar_wait<false>(b_xm, uc & 1, s_abort, p.status);
               ok = __all_sync(0xffffffffu, ok);
               if (!ok) break;
               if (lane == 0) {
-                s_xl[hd] = lsum; s_xx[hd] = rmax;
+                s_xl[hd0] = lsum; s_xx[hd0] = rmax;
                 mbar_arrive(b_xl);
               }
               __syncwarp();
             }
           }
-          if (owner && lane == 0) {
-            p.part_m[(size_t)unit * p.H + head] = mref;
-            p.part_l[(size_t)unit * p.H + head] = lsum;
-            if (sweep == 0) umax[(size_t)unit * p.H + head] = rmax;
+          if (owner && scores && gr == 0 && odd == 0) {
+            const size_t at = (size_t)unit * p.H + (int)rank * g.hl + hd0 + mine;
+            p.part_m[at] = mref;
+            p.part_l[at] = lsum;
+            if (sweep == 0) umax[at] = rmax;
           }
         }
         if (warp < nepi) {
@@ -384,168 +511,74 @@ __global__ void __launch_bounds__(MAXT, 1) fp4_tc_kernel(const SlimDecodeParams 
         __threadfence_block();
         __syncwarp();
       }
-      const unsigned char* codes = reinterpret_cast<const unsigned char*>(p.k) + (size_t)rank * g.cb;
-      const int s_lo = ((int)rank * (g.dsl / FP4_GROUP)) & ~15;
-      const int s_bytes = (((int)(rank + 1) * (g.dsl / FP4_GROUP) + 15) & ~15) - s_lo;
-      for (int gg = g_begin; gg < g_end && ok;) {
-        const int b = slim_seq_of_tile(s_prefix, p.batch, gg);
-        const int seg_end = min(g_end, s_prefix[b + 1]);
-        const int tile0 = gg - s_prefix[b], ntile = seg_end - gg, unit = w + b;
-        gg = seg_end;
-        if (!wanted(unit)) continue;
-        const int len = min(max(p.lengths[b], 0), p.t_cap);
-        for (int kt = 0; kt < ntile; ++kt, ++it) {
-          const int ps = it % g.npk, t0 = (tile0 + kt) * SLIM_TT;
-          ok = mbar_wait<false>(b_pke + 8 * ps, ((it / g.npk) & 1) ^ 1, s_abort, p.status);
-          ok = __all_sync(0xffffffffu, ok);
-          if (!ok) break;
-          const int rows = min(SLIM_TT, len - t0);                   // (rows behind the sequence may lie behind the storage)
-          if (lane == 0) mbar_arrive_expect_tx(b_pkf + 8 * ps, (uint32_t)(rows * (g.cb + s_bytes)));
-          const long long row = slim_cache_row(p, b, t0) + (lane & 15);
-          __syncwarp();
-          const uint32_t dst = s_pk + (uint32_t)(ps * g.pk);
-          if ((lane & 15) < rows) {
-            if (lane < 16) bulk_load(dst + (uint32_t)(lane * g.pp), codes + (size_t)row * g.pitch, (uint32_t)g.cb, b_pkf + 8 * ps);
-            else bulk_load(dst + (uint32_t)(16 * g.pp + (lane & 15) * g.spw), p.k_sc4 + (size_t)row * g.spitch + s_lo, (uint32_t)s_bytes, b_pkf + 8 * ps);
-          }
-        }
-        ++uc;
-      }
-      if (!ok && lane == 0) {
-        // gave up: let the copies that were issued land before the CTA goes away
-        const unsigned long long t = globaltimer();
-        for (int n = max(0, it - g.npk); n < it; ++n)
-          while (!mbar_try_wait(b_pkf + 8 * (n % g.npk), (n / g.npk) & 1) && globaltimer() - t < SLIM_WAIT_NS) {}
-      }
-      __syncwarp();
-    } else if (warp == w_mma) {
-      // =========================== MMA issuer (even CTA) ===========================
       if (lane == 0) {
-        constexpr uint32_t IDESC = (1u << 4) | (1u << 15) | ((32u >> 3) << 17) | ((256u >> 4) << 24);      // float16, A MN-major, M = 256, N = 32
-        const uint64_t ad = desc_a(base), bd = desc_b(s_p);
-        const uint32_t a_lo = (uint32_t)ad, a_hi = (uint32_t)(ad >> 32), b_lo = (uint32_t)bd, b_hi = (uint32_t)(bd >> 32);
+        const uint64_t once = l2_policy_evict_first();
         for (int gg = g_begin; gg < g_end && ok;) {
           const int b = slim_seq_of_tile(s_prefix, p.batch, gg);
           const int seg_end = min(g_end, s_prefix[b + 1]);
-          const int ntile = seg_end - gg, unit = w + b;
+          const int tile0 = gg - s_prefix[b], ntile = seg_end - gg, unit = w + b;
           gg = seg_end;
           if (!wanted(unit)) continue;
-          if (rank == 0) {
-            for (int kt = 0; kt < ntile; ++kt) {
-              const int n = it + kt, st = n % g.nst;
-              ok = mbar_wait<true>(b_pf + 8 * st, (n / g.nst) & 1, s_abort, p.status);
-              if (ok && kt == 0 && uc > 0) ok = mbar_wait<true>(b_ue, (uc - 1) & 1, s_abort, p.status);
-              if (!ok) break;
-              fence_proxy_async_smem();
-              tc_fence_after();
-              uint32_t al = a_lo + (uint32_t)((st * g.stage) >> 4), dcol = tmem;
-              const uint32_t bl = b_lo + (uint32_t)(st * (512 >> 4));
-              for (int c = 0; c < g.nch; ++c, al += 4096u >> 4, dcol += 32u) umma2_bf16_words(dcol, al, a_hi, bl, b_hi, IDESC, kt > 0 ? 1u : 0u);
-              umma2_commit_pair(b_ke + 8 * st);
-            }
-            if (ok) umma2_commit_pair(b_uf);
+          for (int kt = 0; kt < ntile; ++kt, ++it, rp.step(1, g.npk)) {
+            ok = mbar_wait<false>(b_pke + 8 * rp.st, rp.ph ^ 1u, s_abort, p.status);
+            if (!ok) break;
+            const int row = (int)slim_cache_row(p, b, (tile0 + kt) * SLIM_TT);       // (rows behind the storage come as zeros)
+            const uint32_t dst = s_pk + (uint32_t)(rp.st * g.pk), bar = b_pkf + 8 * rp.st;
+            mbar_arrive_expect_tx(bar, (uint32_t)(8 * g.dsl + 16 * g.win));
+            tma_load_3d_hint(dst, &cmap, bar, 0, row, (int)rank * (g.dsl / 128), once);
+            tma_load_3d_hint(dst + 8 * g.dsl, &smap, bar, 0, row, (rank ? g.s_lo[1] : g.s_lo[0]) / 16, once);
           }
-          it += ntile;
           ++uc;
         }
-        // the last commit's arrival must not find this CTA gone
-        if (ok && it > 0) ok = mbar_wait<false>(b_ke + 8 * ((it - 1) % g.nst), ((it - 1) / g.nst) & 1, s_abort, p.status);
+        if (!ok) {
+          // gave up: let the loads that were issued land before the CTA goes away
+          const unsigned long long t = globaltimer();
+          for (int n = max(0, it - g.npk); n < it; ++n)
+            while (!mbar_try_wait(b_pkf + 8 * (n % g.npk), (n / g.npk) & 1) && globaltimer() - t < SLIM_WAIT_NS) {}
+        }
       }
       __syncwarp();
-    } else if (warp == w_query) {
-      // =========================== query columns ===========================
-      // lane l: pairs 2 l, 2 l + 1 of every head
-      const bool live = lane < HALF / 2;
-      int jj, xx;                                                    // the thread and step that read them
-      if (DK == 128) { jj = lane / 8; xx = lane % 8; }
-      else if (DK == 64) { jj = (lane / 4) & 3; xx = lane % 4; }
-      else { jj = (lane >> 1) & 3; xx = 2 * (lane >> 3) + (lane & 1); }
-      const uint32_t at = s_qb + (uint32_t)(jj * SB + xx * 8);
-      f32x2 c16 = 0, s16 = 0, n16 = 0, c8 = 0, s8 = 0, n8 = 0;       // cos and sin of 16 theta and of 8 theta
-      if (ROPE && live) {
-        const float2 a = p.rope_base[HALF + 2 * lane], b = p.rope_base[HALF + 2 * lane + 1];
-        const float2 c = p.rope_off[8 * HALF + 2 * lane], d = p.rope_off[8 * HALF + 2 * lane + 1];
-        c16 = pack2(a.x, b.x); s16 = pack2(a.y, b.y); n16 = pack2(-a.y, -b.y);
-        c8 = pack2(c.x, d.x); s8 = pack2(c.y, d.y); n8 = pack2(-c.y, -d.y);
-      }
-      const uint32_t* Q = reinterpret_cast<const uint32_t*>(p.q);
-      f32x2 q1[16], q2[16];
+    } else if (warp == w_mma) {
+      // =========================== MMA issuer (even CTA), messenger (odd CTA) ===========================
+      // The warp stays together and one elected lane issues: the operands then live in uniform registers, and an instruction costs
+      // 39 clocks instead of the 74 that a lone lane needed to feed it (16 chunks; the operand reads alone are 32).
+      constexpr uint32_t IDESC = (1u << 4) | (1u << 15) | ((32u >> 3) << 17) | ((256u >> 4) << 24);      // float16, A MN-major, M = 256, N = 32
+      const uint64_t a0 = desc_a(base), b0 = desc_b(s_p);
       for (int gg = g_begin; gg < g_end && ok;) {
         const int b = slim_seq_of_tile(s_prefix, p.batch, gg);
         const int seg_end = min(g_end, s_prefix[b + 1]);
-        const int tile0 = gg - s_prefix[b], ntile = seg_end - gg, unit = w + b;
+        const int ntile = seg_end - gg, unit = w + b;
         gg = seg_end;
         if (!wanted(unit)) continue;
-        const int len = min(max(p.lengths[b], 0), p.t_cap);
-        // the queries at position pos, divided by a power of two a head; `say`: also leave that for the score warps
-        auto seed = [&](int pos, bool say) {
-          f32x2 c = pack2(1.f, 1.f), s = pack2(0.f, 0.f), ns = s;
-          if (ROPE && live) {
-            const float2 ba = __ldg(p.rope_base + (size_t)(pos / SLIM_TT) * HALF + 2 * lane), bb = __ldg(p.rope_base + (size_t)(pos / SLIM_TT) * HALF + 2 * lane + 1);
-            const float2 oa = __ldg(p.rope_off + (pos % SLIM_TT) * HALF + 2 * lane), ob = __ldg(p.rope_off + (pos % SLIM_TT) * HALF + 2 * lane + 1);
-            const float sa = ba.y * oa.x + ba.x * oa.y, sb = bb.y * ob.x + bb.x * ob.y;
-            c = pack2(ba.x * oa.x - ba.y * oa.y, bb.x * ob.x - bb.y * ob.y);
-            s = pack2(sa, sb); ns = pack2(-sa, -sb);
-          }
-#pragma unroll
-          for (int h = 0; h < 16; ++h) {
-            if (h >= g.hl) break;
-            const size_t qi = (((size_t)b * p.d + (size_t)((int)rank * g.hl + h) * DK) >> 1) + lane;
-            const f32x2 u = live ? unpack2(__ldg(Q + qi)) : 0, v = live ? unpack2(__ldg(Q + qi + HALF / 2)) : 0;
-            float m0, m1, m2, m3;
-            asm("mov.b64 {%0, %1}, %2;" : "=f"(m0), "=f"(m1) : "l"(u));
-            asm("mov.b64 {%0, %1}, %2;" : "=f"(m2), "=f"(m3) : "l"(v));
-            float mx = fmaxf(fmaxf(fabsf(m0), fabsf(m1)), fmaxf(fabsf(m2), fabsf(m3)));
-#pragma unroll
-            for (int o = 16; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
-            const float up = pow2_to_one(mx);
-            const f32x2 f = pack2(up, up);
-            const f32x2 x = mul2(u, f), y = mul2(v, f);
-            q1[h] = fma2(y, s, mul2(x, c));
-            q2[h] = fma2(x, ns, mul2(y, c));
-            if (say && lane == 0) s_qs[(uc & 1) * 16 + h] = (ROPE ? 2.f : 1.f) * p.qscale / up;      // (the factors on the keys are halved)
-          }
-        };
-        auto lay = [&](int stage) {
-#pragma unroll
-          for (int h = 0; h < 16; ++h) {
-            if (h >= g.hl) break;
-            const uint32_t to = at + (uint32_t)((stage * g.hl + h) * HB);
-            if (live) {
-              sts64(to, half2_of(q1[h]), half2_of(q2[h]));
-              // turned back by 8 more: column 1
-              if (ROPE) sts64(to + 4 * SB, half2_of(fma2(q2[h], n8, mul2(q1[h], c8))), half2_of(fma2(q1[h], s8, mul2(q2[h], c8))));
-              else sts64(to + 4 * SB, half2_of(q1[h]), half2_of(q2[h]));
-            }
-            if (ROPE) {
-              const f32x2 a = fma2(q2[h], n16, mul2(q1[h], c16));
-              q2[h] = fma2(q1[h], s16, mul2(q2[h], c16));
-              q1[h] = a;
-            }
-          }
-          __syncwarp();
-          if (lane == 0) mbar_arrive(b_qf + 8 * stage);
-        };
-        if (!ROPE) {
-          ok = mbar_wait<false>(b_qe + 8 * (uc & 1), ((uc >> 1) & 1) ^ 1, s_abort, p.status);
-          ok = __all_sync(0xffffffffu, ok);
-          if (!ok) break;
-          seed(0, true);
-          lay(uc & 1);
-          it += ntile;
-        } else {
-          for (int kt = 0; kt < ntile; ++kt, ++it) {
-            ok = mbar_wait<false>(b_qe + 8 * (it & 1), ((it >> 1) & 1) ^ 1, s_abort, p.status);
+        for (int kt = 0; kt < ntile; ++kt, ++it, rk.step(1, g.nst)) {
+          ok = mbar_wait<false>(b_pf + 8 * rk.st, rk.ph, s_abort, p.status);
+          if (rank != 0) {
             ok = __all_sync(0xffffffffu, ok);
             if (!ok) break;
-            // q(len - 1) against keys turned by t - t0: the query at len - 1 - t0 (not negative: t0 < len)
-            if (kt % RESEED == 0) seed(len - 1 - (tile0 + kt) * SLIM_TT, kt == 0);
-            lay(it & 1);
+            if (elect_one()) mbar_arrive_remote(mapa(b_px + 8 * rk.st, 0));
+            continue;
           }
+          ok = mbar_wait<false>(b_px + 8 * rk.st, rk.ph, s_abort, p.status) && ok;
+          if (kt == 0 && uc > 0) ok = mbar_wait<true>(b_ue, (uc - 1) & 1, s_abort, p.status) && ok;
+          ok = __all_sync(0xffffffffu, ok);
           if (!ok) break;
+          tc_fence_after();
+          if (elect_one()) {
+            uint64_t ad = a0 + (uint64_t)((uint32_t)(rk.st * g.stage) >> 4);
+            const uint64_t bd = b0 + (uint64_t)(rk.st * (512 >> 4));
+            uint32_t dcol = tmem;
+            const uint32_t acc = kt > 0 ? 1u : 0u;
+#pragma unroll 4
+            for (int c = 0; c < g.nch; ++c, ad += 4096u >> 4, dcol += 32u) umma2_f16(dcol, ad, bd, IDESC, acc);
+            umma2_commit_pair(b_ke + 8 * rk.st);
+            if (kt + 1 == ntile) umma2_commit_pair(b_uf);
+          }
+          __syncwarp();
         }
         ++uc;
       }
+      // the last commit's arrival must not find this CTA gone
+      if (ok && it > 0) ok = mbar_wait<false>(b_ke + 8 * ((it - 1) % g.nst), ((it - 1) / g.nst) & 1, s_abort, p.status);
       __syncwarp();
     }
     if (sweep == 0) {
@@ -553,6 +586,10 @@ __global__ void __launch_bounds__(MAXT, 1) fp4_tc_kernel(const SlimDecodeParams 
       ok = __shfl_sync(0xffffffffu, (int)ok, 0) != 0;
       it = __shfl_sync(0xffffffffu, it, 0);
       uc = __shfl_sync(0xffffffffu, uc, 0);
+      rp.st = __shfl_sync(0xffffffffu, rp.st, 0);
+      rp.ph = __shfl_sync(0xffffffffu, rp.ph, 0);
+      rk.st = __shfl_sync(0xffffffffu, rk.st, 0);
+      rk.ph = __shfl_sync(0xffffffffu, rk.ph, 0);
       __threadfence();
       __syncthreads();
       cluster_sync_all();
@@ -577,30 +614,33 @@ __global__ void __launch_bounds__(MAXT, 1) fp4_tc_kernel(const SlimDecodeParams 
 
 constexpr int SMEM_LIMIT = 227 * 1024;
 
-template <int DK>
-int query_bytes(int hl) { return NQ * hl * 8 * Lane<DK>::SB; }
+int threads_of(const Geom& g) { return 32 * (g.nswl + 2); }
 
 // false: the shape does not fit
 bool make_geom(int d, int H, int d_k, int batch, Geom& g) {
   if ((d_k != 64 && d_k != 96 && d_k != 128) || (H & 1) || H < 2 || H > 32 || d % 256 || d > 4096) return false;
   g.dsl = d / 2; g.hl = H / 2; g.nch = g.dsl / 128;
-  g.nsw = g.hl;
-  g.sets = 2 * g.nsw <= 20 ? 2 : 1;
+  // More than ten heads: two a warp (a tile's fixed steps are then shared by two heads, and a thread has the registers for it).
+  // Up to ten: one a warp, in two sets that take the tiles in turn, since a small tile is bound by its chain of steps.
+  g.hpw = g.hl > 10 && g.hl % 2 == 0 ? 2 : 1;
+  g.nsw = g.hl / g.hpw;
+  g.sets = g.hl > 10 ? 1 : 2;
   g.nswl = g.nsw * g.sets < 4 ? 4 : g.nsw * g.sets;
   g.stage = 32 * g.dsl;
-  g.cb = g.dsl / 2;
-  const int want = d_k == 128 ? 32 : 16;                       // rows of a warp's reads side by side in the banks
-  g.pp = g.cb;
-  while (g.pp % 128 != want) g.pp += 16;
-  g.pitch = slim_fp4_code_pitch(d); g.spitch = slim_fp4_scale_pitch(d);
-  const int per = g.dsl / FP4_GROUP, lo0 = 0, hi0 = (per + 15) & ~15, lo1 = per & ~15, hi1 = (2 * per + 15) & ~15;
-  g.spw = hi0 - lo0 > hi1 - lo1 ? hi0 - lo0 : hi1 - lo1;
-  g.pk = 16 * (g.pp + g.spw);
+  const int per = g.dsl / FP4_GROUP;
+  int hi[2];
+  for (int r = 0; r < 2; ++r) {
+    g.s_lo[r] = (r * per) & ~15;
+    g.s_shift[r] = (r * per) & 15;
+    hi[r] = ((r + 1) * per + 15) & ~15;
+  }
+  g.win = hi[0] > hi[1] - g.s_lo[1] ? hi[0] : hi[1] - g.s_lo[1];
   int cols = 32;
   while (cols < 32 * g.nch) cols <<= 1;
   g.tmem_cols = cols;
-  const int qbytes = d_k == 128 ? query_bytes<128>(g.hl) : d_k == 96 ? query_bytes<96>(g.hl) : query_bytes<64>(g.hl);
-  const int fixed = 1024 + qbytes + 8 * (2 * MAX_PK + 2 * MAX_ST + 2 * NQ + 4) + 8 + 4 * (32 + 48) + 4 * (batch + 1) + 64;
+  g.pk = (8 * g.dsl + 16 * g.win + 1023) & ~1023;
+  const int qbytes = g.sets * g.hl * 8 * (d_k == 128 ? Lane<128>::SB : d_k == 96 ? Lane<96>::SB : Lane<64>::SB);
+  const int fixed = 1024 + qbytes + 8 * (2 * MAX_PK + 3 * MAX_ST + 4) + 8 + 4 * 48 + 4 * (batch + 1) + 64;
   // two float16 stages at least; more of them, and of packed ones, while they fit
   g.nst = 2; g.npk = 2;
   auto total = [&](int st, int pk) { return fixed + st * (g.stage + 512) + pk * g.pk; };
@@ -608,32 +648,32 @@ bool make_geom(int d, int H, int d_k, int batch, Geom& g) {
   while (g.npk < 4 && total(g.nst, g.npk + 1) <= SMEM_LIMIT) ++g.npk;
   while (g.nst + 2 <= MAX_ST && total(g.nst + 2, g.npk) <= SMEM_LIMIT) g.nst += 2;
   while (g.npk < MAX_PK && total(g.nst, g.npk + 1) <= SMEM_LIMIT) ++g.npk;
-  g.off_p = g.nst * g.stage;
-  g.off_pk = g.off_p + g.nst * 512;
-  g.off_q = g.off_pk + g.npk * g.pk;
+  g.off_pk = g.nst * g.stage;
+  g.off_p = g.off_pk + g.npk * g.pk;
+  g.off_q = g.off_p + g.nst * 512;
   g.off_bar = g.off_q + qbytes;
   g.smem = total(g.nst, g.npk);
   if (g.smem < 120 * 1024) g.smem = 120 * 1024;                // one CTA an SM: tensor memory is not shared
   return true;
 }
 
-typedef void (*kernel_t)(const SlimDecodeParams, const Geom, float*);
+typedef void (*kernel_t)(const CUtensorMap, const CUtensorMap, const SlimDecodeParams, const Geom, float*);
 template <int DK, bool ROPE>
-kernel_t pick_threads(int threads) { return threads <= 640 ? fp4_tc_kernel<DK, ROPE, 640> : fp4_tc_kernel<DK, ROPE, 768>; }
-kernel_t pick(int d_k, bool rope, int threads) {
-  if (d_k == 64) return rope ? pick_threads<64, true>(threads) : pick_threads<64, false>(threads);
-  if (d_k == 96) return rope ? pick_threads<96, true>(threads) : pick_threads<96, false>(threads);
-  return rope ? pick_threads<128, true>(threads) : pick_threads<128, false>(threads);
+kernel_t pick_heads(const Geom& g) {
+  return g.hpw == 2 ? fp4_tc_kernel<DK, ROPE, 2, 384> : threads_of(g) <= 640 ? fp4_tc_kernel<DK, ROPE, 1, 640> : fp4_tc_kernel<DK, ROPE, 1, 768>;
 }
-
-int threads_of(const Geom& g) { return 32 * (g.nswl + 3); }
+kernel_t pick(int d_k, bool rope, const Geom& g) {
+  if (d_k == 64) return rope ? pick_heads<64, true>(g) : pick_heads<64, false>(g);
+  if (d_k == 96) return rope ? pick_heads<96, true>(g) : pick_heads<96, false>(g);
+  return rope ? pick_heads<128, true>(g) : pick_heads<128, false>(g);
+}
 
 }  // namespace
 
 int slim_fp4_tc_workers(const slim_ctx* ctx) {
   Geom g;
   if (!make_geom(ctx->d, ctx->H, ctx->d_k, SLIM_MAX_BATCH, g)) return 0;
-  kernel_t kern = pick(ctx->d_k, ctx->rope_theta != 0.0, threads_of(g));
+  kernel_t kern = pick(ctx->d_k, ctx->rope_theta != 0.0, g);
   if (cudaFuncSetAttribute((const void*)kern, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_LIMIT) != cudaSuccess) { cudaGetLastError(); return 0; }
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(2 * (ctx->num_sms / 2));
@@ -648,10 +688,31 @@ int slim_fp4_tc_workers(const slim_ctx* ctx) {
   return n < ctx->num_sms / 2 ? n : ctx->num_sms / 2;
 }
 
-cudaError_t slim_launch_fp4_tc(const slim_ctx* ctx, const SlimDecodeParams& p, float* umax, cudaStream_t st) {
+cudaError_t slim_fp4_tc_make_tmaps(const slim_ctx* ctx, slim_cache* c) {
+  c->has_tmap[0] = c->has_tmap[1] = 0;
+  Geom g;
+  if (!make_geom(ctx->d, ctx->H, ctx->d_k, SLIM_MAX_BATCH, g)) return cudaErrorNotSupported;
+  const unsigned long long rows = (unsigned long long)c->total_rows, pitch = (unsigned long long)slim_fp4_code_pitch(ctx->d), spitch = (unsigned long long)slim_fp4_scale_pitch(ctx->d);
+  {
+    // codes: 64-byte chunks of the rows; a box is the chunks of a CTA's half, 16 rows
+    const unsigned long long dims[3] = {32, rows, pitch / 64}, strides[2] = {pitch, 64};
+    const unsigned int box[3] = {32, SLIM_TT, (unsigned int)(g.dsl / 128)};
+    const cudaError_t e = slim_tmap_encode_3d(c->tmap[0], c->k, dims, strides, box, 64);
+    if (e != cudaSuccess) return e;
+    c->has_tmap[0] = 1;
+  }
+  // scales: 16-byte chunks, so that the eight rows of a warp's load lie in different banks
+  const unsigned long long dims[3] = {8, rows, spitch / 16}, strides[2] = {spitch, 16};
+  const unsigned int box[3] = {8, SLIM_TT, (unsigned int)(g.win / 16)};
+  const cudaError_t e = slim_tmap_encode_3d(c->tmap[1], c->k_sc4, dims, strides, box, 0);
+  if (e == cudaSuccess) c->has_tmap[1] = 1;
+  return e;
+}
+
+cudaError_t slim_launch_fp4_tc(const slim_ctx* ctx, const slim_cache* c, const SlimDecodeParams& p, float* umax, cudaStream_t st) {
   Geom g;
   if (!make_geom(ctx->d, ctx->H, ctx->d_k, p.batch, g)) return cudaErrorNotSupported;
-  kernel_t kern = pick(ctx->d_k, ctx->rope_theta != 0.0, threads_of(g));
+  kernel_t kern = pick(ctx->d_k, ctx->rope_theta != 0.0, g);
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(2 * p.workers);
   cfg.blockDim = dim3(threads_of(g));
@@ -663,5 +724,8 @@ cudaError_t slim_launch_fp4_tc(const slim_ctx* ctx, const SlimDecodeParams& p, f
   attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr; cfg.numAttrs = 2;
-  return cudaLaunchKernelEx(&cfg, kern, p, g, umax);
+  CUtensorMap cmap, smap;
+  memcpy(&cmap, c->tmap[0], sizeof(cmap));
+  memcpy(&smap, c->tmap[1], sizeof(smap));
+  return cudaLaunchKernelEx(&cfg, kern, cmap, smap, p, g, umax);
 }
