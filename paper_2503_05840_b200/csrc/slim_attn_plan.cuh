@@ -57,12 +57,7 @@ static __device__ void slim_attn_plan(const SlimAttn& a, int* s_mem) {
 // Position of packed row r among the queries (keys); -1: it belongs to no sequence.
 static __device__ int slim_attn_position(const SlimAttn& a, int r, bool query) {
   const int32_t* cu = query ? a.cu_q : a.cu_k;
-  int lo = 0, hi = a.batch;
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (cu[mid] <= r) lo = mid; else hi = mid;
-  }
-  const SlimSeq s = slim_attn_seq(a, lo);
+  const SlimSeq s = slim_attn_seq(a, slim_warp_find(cu, a.batch, r));
   if (query) return r >= s.q0 && r < s.q0 + s.nq ? r - s.q0 + s.nk - s.nq : -1;
   return r >= s.k0 && r < s.k0 + s.nk ? r - s.k0 : -1;
 }

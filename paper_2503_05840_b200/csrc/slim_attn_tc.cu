@@ -311,43 +311,56 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
   } else if (warp == 8) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
     // =========================== MMA issuer ===========================
-    if (lane == 0 && nt > 0) {
+    // The warp stays together and one elected lane issues, so that the descriptors live in uniform registers.
+    if (nt > 0) {
       bool ok = mbar_wait<false>(bar_q, 0, s_abort, a.status);
       auto full = [&](int k) { return mbar_wait<false>(bar_full + 8 * (k % NS), (k / NS) & 1, s_abort, a.status); };
+      const uint64_t dq = desc_kmajor_sw128(s_q), dk = desc_kmajor_sw128(s_kv), dv = desc_a(s_kv, TN * 128);
       auto scores = [&](int i, int k) {
+        const uint64_t qd = dq + (uint64_t)(i * (TILE >> 4)), kd = dk + (uint64_t)((k % NS) * (TILE >> 4));
 #pragma unroll
         for (int x = 0; x < KSTEPS; ++x) {
-          const uint32_t off = (uint32_t)((x >> 2) * TN * 128 + (x & 3) * 32);
-          umma_ss(tmem + i * TN, desc_kmajor_sw128(s_q + i * TILE + off), desc_kmajor_sw128(s_kv + (k % NS) * TILE + off), IDESC_S, x > 0);
+          const uint32_t off = (uint32_t)((x >> 2) * TN * 128 + (x & 3) * 32) >> 4;
+          umma_ss(tmem + i * TN, qd + off, kd + off, IDESC_S, x > 0);
         }
         umma_commit(bar_s + 8 * i);
       };
-      ok = ok && full(0);
-      if (ok) {
-        tc_fence_after();
+      ok = full(0) && ok;
+      ok = __all_sync(0xffffffffu, ok);
+      tc_fence_after();
+      if (ok && elect_one()) {
         if (nt0 > 0) scores(0, 0);
         if (nt1 > 0) scores(1, 0);
         umma_commit(bar_empty);
       }
+      __syncwarp();
       for (int j = 0; j < nt && ok; ++j) {
         const int kv = 2 * j + 1, kk = 2 * j + 2;
         ok = full(kv);
-        if (j + 1 < nt) ok = ok && full(kk);
+        if (j + 1 < nt) ok = full(kk) && ok;
         for (int i = 0; i < 2 && ok; ++i) {
           const int n = i ? nt1 : nt0;
           if (j >= n) continue;
-          ok = mbar_wait<false>(bar_p + 8 * i, j & 1, s_abort, a.status);
+          ok = mbar_wait<false>(bar_p + 8 * i, j & 1, s_abort, a.status) && ok;
+          ok = __all_sync(0xffffffffu, ok);
           if (!ok) break;
           tc_fence_after();
+          if (elect_one()) {
+            const uint64_t vd = dv + (uint64_t)((kv % NS) * (TILE >> 4));
 #pragma unroll
-          for (int x = 0; x < TN / 16; ++x)
-            umma_ts(tmem + 2 * TN + i * 128, tmem + i * TN + 8 * x, desc_a(s_kv + (kv % NS) * TILE + x * 2048, TN * 128), IDESC_O, j > 0 || x > 0);
-          if (j + 1 < n) scores(i, kk);
-          else umma_commit(bar_o + 8 * i);
+            for (int x = 0; x < TN / 16; ++x)
+              umma_ts(tmem + 2 * TN + i * 128, tmem + i * TN + 8 * x, vd + x * (2048 >> 4), IDESC_O, j > 0 || x > 0);
+            if (j + 1 < n) scores(i, kk);
+            else umma_commit(bar_o + 8 * i);
+          }
+          __syncwarp();
         }
         if (!ok) break;
-        umma_commit(bar_empty + 8 * (kv % NS));
-        if (j + 1 < nt) umma_commit(bar_empty + 8 * (kk % NS));
+        if (elect_one()) {
+          umma_commit(bar_empty + 8 * (kv % NS));
+          if (j + 1 < nt) umma_commit(bar_empty + 8 * (kk % NS));
+        }
+        __syncwarp();
       }
       // the last commit's arrival must not find this CTA gone
       if (ok) mbar_wait<false>(bar_empty + 8 * ((2 * nt - 1) % NS), ((2 * nt - 1) / NS) & 1, s_abort, a.status);

@@ -43,16 +43,18 @@ __device__ __forceinline__ int slim_fp4_scale_byte(float amax, bool bad) {
   if (b < FP4_SCALE_MAX && 6.f * slim_fp4_scale((unsigned char)b) < amax) ++b;
   return b;
 }
-// Code of k under the scale s: the nearest of the eight magnitudes times s, on a border the even code.  The borders
-// (0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5) s are exact in float32, so no division and no rounding of a quotient is needed.
-__device__ __forceinline__ unsigned slim_fp4_code(float k, float s) {
-  const float a = fabsf(k);
-  const bool upper = a >= 1.75f * s;                               // codes 4 .. 7
-  const float b1 = upper ? 3.5f * s : 0.75f * s;                   // on it: up to the even code 6 or 2
-  const bool u1 = a >= b1;
-  const float b0 = upper ? (u1 ? 5.f * s : 2.5f * s) : (u1 ? 1.25f * s : 0.25f * s);      // on it: down, to 6, 4, 2 or 0
-  const unsigned m = (upper ? 4u : 0u) + (u1 ? 2u : 0u) + (a > b0 ? 1u : 0u);
-  return m && a > 0.f ? m | (k < 0.f ? 8u : 0u) : 0u;           // (all borders are 0 in a group of zeros)
+// eight codes -> four float16 pairs
+__device__ __forceinline__ void slim_fp4_decode8(uint32_t w, uint32_t (&h)[4]) {
+  asm("{\n\t.reg .b8 b0, b1, b2, b3;\n\tmov.b32 {b0, b1, b2, b3}, %4;\n\tcvt.rn.f16x2.e2m1x2 %0, b0;\n\tcvt.rn.f16x2.e2m1x2 %1, b1;\n\t"
+      "cvt.rn.f16x2.e2m1x2 %2, b2;\n\tcvt.rn.f16x2.e2m1x2 %3, b3;\n\t}" : "=r"(h[0]), "=r"(h[1]), "=r"(h[2]), "=r"(h[3]) : "r"(w));
+}
+// eight numbers -> codes, to nearest, on a border to the even code
+__device__ __forceinline__ uint32_t slim_fp4_encode8(const float (&y)[8]) {
+  uint32_t d;
+  asm("{\n\t.reg .b8 b0, b1, b2, b3;\n\tcvt.rn.satfinite.e2m1x2.f32 b0, %2, %1;\n\tcvt.rn.satfinite.e2m1x2.f32 b1, %4, %3;\n\t"
+      "cvt.rn.satfinite.e2m1x2.f32 b2, %6, %5;\n\tcvt.rn.satfinite.e2m1x2.f32 b3, %8, %7;\n\tmov.b32 %0, {b0, b1, b2, b3};\n\t}"
+      : "=r"(d) : "f"(y[0]), "f"(y[1]), "f"(y[2]), "f"(y[3]), "f"(y[4]), "f"(y[5]), "f"(y[6]), "f"(y[7]));
+  return d;
 }
 #endif
 

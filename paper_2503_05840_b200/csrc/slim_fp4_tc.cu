@@ -57,11 +57,6 @@ __device__ __forceinline__ void mma_f16(float (&c)[4], uint32_t a0, uint32_t a1,
   asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
       : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
-// eight codes -> four float16 pairs
-__device__ __forceinline__ void decode8(uint32_t w, uint32_t (&h)[4]) {
-  asm("{\n\t.reg .b8 b0, b1, b2, b3;\n\tmov.b32 {b0, b1, b2, b3}, %4;\n\tcvt.rn.f16x2.e2m1x2 %0, b0;\n\tcvt.rn.f16x2.e2m1x2 %1, b1;\n\t"
-      "cvt.rn.f16x2.e2m1x2 %2, b2;\n\tcvt.rn.f16x2.e2m1x2 %3, b3;\n\t}" : "=r"(h[0]), "=r"(h[1]), "=r"(h[2]), "=r"(h[3]) : "r"(w));
-}
 __device__ __forceinline__ uint32_t hmul2(uint32_t a, uint32_t b) { uint32_t d; asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b)); return d; }
 __device__ __forceinline__ uint32_t hfma2(uint32_t a, uint32_t b, uint32_t c) {
   uint32_t d; asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(b), "r"(c)); return d;
@@ -86,11 +81,6 @@ __device__ __forceinline__ void sts64(uint32_t a, uint32_t x, uint32_t y) { asm 
 // scope took 1500 clocks a tile.)
 __device__ __forceinline__ void mbar_arrive_remote(uint32_t cluster_bar) {
   asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
-}
-__device__ __forceinline__ bool elect_one() {
-  uint32_t v;
-  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.b32 %0, 1, 0, p;\n\t}" : "=r"(v));
-  return v != 0;
 }
 __device__ __forceinline__ void umma2_f16(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
   asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}"
@@ -157,6 +147,28 @@ __global__ void __launch_bounds__(MAXT, 1) fp4_tc_kernel(const __grid_constant__
   cluster_sync_all();
   tc_fence_after();
   const uint32_t tmem = *s_tmem;
+  const bool scorer = warp < g.nsw * g.sets;
+  const int gr = lane >> 2, j = lane & 3;
+  // Rotation factors, the same for every tile: half of cos and sin of gr theta for the thread's pairs (keys), cos and sin of a
+  // set's step and of 8 theta for pairs 2 lane, 2 lane + 1 (queries).  No kernel before this one writes the tables.
+  uint32_t cs[NP * PE / 2], sn[NP * PE / 2];
+  f32x2 cst = 0, sst = 0, nst = 0, c8 = 0, s8 = 0, n8 = 0;
+  if (ROPE && scorer) {
+#pragma unroll
+    for (int x = 0; x < NP; ++x)
+#pragma unroll
+      for (int e = 0; e < PE / 2; ++e) {
+        const float2 a = __ldg(p.rope_off + gr * HALF + L::col(j, x) + 2 * e), b = __ldg(p.rope_off + gr * HALF + L::col(j, x) + 2 * e + 1);
+        cs[x * (PE / 2) + e] = half2_of(0.5f * a.x, 0.5f * b.x);
+        sn[x * (PE / 2) + e] = half2_of(0.5f * a.y, 0.5f * b.y);
+      }
+    if (lane < HALF / 2) {
+      const float2 a = __ldg(p.rope_base + g.sets * HALF + 2 * lane), b = __ldg(p.rope_base + g.sets * HALF + 2 * lane + 1);
+      const float2 c = __ldg(p.rope_off + 8 * HALF + 2 * lane), d = __ldg(p.rope_off + 8 * HALF + 2 * lane + 1);
+      cst = pack2(a.x, b.x); sst = pack2(a.y, b.y); nst = pack2(-a.y, -b.y);
+      c8 = pack2(c.x, d.x); s8 = pack2(c.y, d.y); n8 = pack2(-c.y, -d.y);
+    }
+  }
   slim_pdl_wait();
   const SlimSched sc = slim_sched_build(p.lengths, p.batch, p.t_cap, p.workers, p.min_tiles, s_prefix, p.status, p.unit_cost);
   const bool in_range = sc.total_tiles > 0 && w < sc.workers_eff;
@@ -173,20 +185,7 @@ __global__ void __launch_bounds__(MAXT, 1) fp4_tc_kernel(const __grid_constant__
     auto wanted = [&](int unit) { return sweep == 0 || (__ldcg(p.unit_flags + 2 * unit) | __ldcg(p.unit_flags + 2 * unit + 1)) != 0; };
     if (warp < g.nswl) {
       // =========================== score / epilogue warps ===========================
-      const bool scorer = warp < g.nsw * g.sets;
       const int hd0 = (warp - set * g.nsw) * HPW;                            // the warp's first head within the CTA
-      const int gr = lane >> 2, j = lane & 3;
-      uint32_t cs[NP * PE / 2], sn[NP * PE / 2];                 // half of cos and sin of gr theta, the thread's pairs
-      if (ROPE && scorer) {
-#pragma unroll
-        for (int x = 0; x < NP; ++x)
-#pragma unroll
-          for (int e = 0; e < PE / 2; ++e) {
-            const float2 a = __ldg(p.rope_off + gr * HALF + L::col(j, x) + 2 * e), b = __ldg(p.rope_off + gr * HALF + L::col(j, x) + 2 * e + 1);
-            cs[x * (PE / 2) + e] = half2_of(0.5f * a.x, 0.5f * b.x);
-            sn[x * (PE / 2) + e] = half2_of(0.5f * a.y, 0.5f * b.y);
-          }
-      }
       // Offsets of the thread's pieces for its first head (the others follow at fixed distances; d_k = 96 goes piece by piece):
       // codes (64-byte chunks of 16 rows, 64-byte swizzle), scales, float16 tile (64-column chunks of 16 rows, 128-byte swizzle)
       const int sw = (gr >> 1) & 3;
@@ -198,9 +197,12 @@ __global__ void __launch_bounds__(MAXT, 1) fp4_tc_kernel(const __grid_constant__
         const int c = hd * DK + half * HALF + L::col(j, x);
         return (uint32_t)((c >> 6) * 2048 + gr * 128 + ((((c & 63) >> 3) ^ gr) << 4) + (c & 7) * 2);
       };
-      const uint32_t c0 = code_off(hd0, 0, 0), t0_off = tile_off(hd0, 0, 0);
       const int s_at = rank ? g.s_shift[1] : g.s_shift[0];
       auto scale_off = [&](int i) { return (uint32_t)(8 * g.dsl + ((s_at + i) >> 4) * 256 + gr * 16 + ((s_at + i) & 15)); };       // of the CTA's group i
+      const uint32_t c0 = code_off(hd0, 0, 0), t0_off = tile_off(hd0, 0, 0);
+      uint32_t sc_off[HPW];
+#pragma unroll
+      for (int u = 0; u < HPW; ++u) sc_off[u] = scale_off((hd0 + u) * (DK / FP4_GROUP));
       // byte of a head's scale word -> the low byte of both halves of a register: first half of the head, second half
       const uint32_t sel0 = DK == 128 ? 0x4040u + 0x0101u * (uint32_t)(j >> 1) : 0x4040u, sel1 = sel0 + (DK == 128 ? 0x0202u : 0x0101u);
       const uint32_t q_own = s_q + (uint32_t)((set * g.hl + hd0) * HB);      // the warp's query columns
@@ -218,15 +220,9 @@ __global__ void __launch_bounds__(MAXT, 1) fp4_tc_kernel(const __grid_constant__
       else if (DK == 64) { jj = (lane / 4) & 3; xx = lane % 4; }
       else { jj = (lane >> 1) & 3; xx = 2 * (lane >> 3) + (lane & 1); }
       const uint32_t q_wr = q_own + (uint32_t)(jj * SB + xx * 8);
-      f32x2 q1[HPW], q2[HPW], cst = 0, sst = 0, nst = 0, c8 = 0, s8 = 0, n8 = 0;       // cos and sin of a set's step, and of 8 theta
+      f32x2 q1[HPW], q2[HPW];
 #pragma unroll
       for (int u = 0; u < HPW; ++u) q1[u] = q2[u] = 0;
-      if (ROPE && live && scorer) {
-        const float2 a = p.rope_base[g.sets * HALF + 2 * lane], b = p.rope_base[g.sets * HALF + 2 * lane + 1];
-        const float2 c = p.rope_off[8 * HALF + 2 * lane], d = p.rope_off[8 * HALF + 2 * lane + 1];
-        cst = pack2(a.x, b.x); sst = pack2(a.y, b.y); nst = pack2(-a.y, -b.y);
-        c8 = pack2(c.x, d.x); s8 = pack2(c.y, d.y); n8 = pack2(-c.y, -d.y);
-      }
       for (int gg = g_begin; gg < g_end && ok;) {
         const int b = slim_seq_of_tile(s_prefix, p.batch, gg);
         const int seg_end = min(g_end, s_prefix[b + 1]);
@@ -290,8 +286,8 @@ __global__ void __launch_bounds__(MAXT, 1) fp4_tc_kernel(const __grid_constant__
           for (int kt = kt0; kt < ntile && ok; kt += g.sets, rp.step(g.sets, g.npk), rk.step(g.sets, g.nst)) {
             const int t0 = (tile0 + kt) * SLIM_TT;
             const uint32_t pk = s_pk + (uint32_t)(rp.st * g.pk), kh = base + (uint32_t)(rk.st * g.stage);
-            ok = mbar_wait<false>(b_pkf + 8 * rp.st, rp.ph, s_abort, p.status);
-            ok = mbar_wait<false>(b_ke + 8 * rk.st, rk.ph ^ 1u, s_abort, p.status) && ok;
+            // the keys are there (even lanes look) and the float16 stage is free (odd lanes)
+            ok = mbar_wait<false>(lane & 1 ? b_ke + 8 * rk.st : b_pkf + 8 * rp.st, lane & 1 ? rk.ph ^ 1u : rp.ph, s_abort, p.status);
             ok = __all_sync(0xffffffffu, ok);
             if (!ok) break;
             __syncwarp();                                              // the query columns are down
@@ -313,7 +309,7 @@ __global__ void __launch_bounds__(MAXT, 1) fp4_tc_kernel(const __grid_constant__
                     cw[u][r][0][0] = lds32((u ? ca ^ 32u : ca) + r * 512);
                     cw[u][r][1][0] = lds32((u ? cb ^ 32u : cb) + r * 512);
                   }
-                  const uint32_t at = pk + scale_off((hd0 + u) * (DK / FP4_GROUP)) + r * 128;
+                  const uint32_t at = pk + sc_off[u] + r * 128;
                   uint32_t word = DK == 128 ? lds32(at) : lds_u16(at);
                   word = (r ? in1 : in0) ? word : 0u;                  // rows behind the sequence become zeros
                   sc[u][r][0][0] = prmt(word, sel0) << 7;
@@ -360,10 +356,10 @@ __global__ void __launch_bounds__(MAXT, 1) fp4_tc_kernel(const __grid_constant__
                   else if (DK == 64) to = (half ? ta ^ 64u : ta) + u * 2048;
                   else to = kh + tile_off(hd0 + u, half, x);
                   uint32_t both[4];                                    // pieces of four columns: the two rows side by side
-                  if (PE == 4) decode8(cw[u][0][half][x] | (cw[u][1][half][x] << 16), both);
+                  if (PE == 4) slim_fp4_decode8(cw[u][0][half][x] | (cw[u][1][half][x] << 16), both);
 #pragma unroll
                   for (int r = 0; r < 2; ++r) {
-                    if (PE == 8) decode8(cw[u][r][half][x], k[r][half]);
+                    if (PE == 8) slim_fp4_decode8(cw[u][r][half][x], k[r][half]);
                     else { k[r][half][0] = both[2 * r]; k[r][half][1] = both[2 * r + 1]; }
 #pragma unroll
                     for (int e = 0; e < PE / 2; ++e) k[r][half][e] = hmul2(k[r][half][e], sc[u][r][half][DK == 96 ? x : 0]);
@@ -430,10 +426,7 @@ __global__ void __launch_bounds__(MAXT, 1) fp4_tc_kernel(const __grid_constant__
             }
             fence_proxy_async_smem();            // keys and probabilities -> tensor core
             __syncwarp();
-            if (lane == 0) {
-              mbar_arrive(b_pf + 8 * rk.st);
-              mbar_arrive(b_pke + 8 * rp.st);
-            }
+            if (lane < 2) mbar_arrive(lane ? b_pke + 8 * rp.st : b_pf + 8 * rk.st);
             if (ROPE && ++fresh == RESEED) {                           // (what was laid down for the next tile is replaced)
               fresh = 0;
               if (kt + g.sets < ntile) {

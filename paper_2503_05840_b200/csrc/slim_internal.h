@@ -190,6 +190,21 @@ __device__ __forceinline__ void slim_store_o(float* o, int o_bf16, size_t i, flo
 __device__ __forceinline__ void slim_pdl_trigger() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 __device__ __forceinline__ void slim_pdl_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 
+// The last i < n with starts[i] <= r (0 if there is none), by a whole warp: 32 places are looked at in one go, so that up to
+// 32 sequences take one trip to memory.
+__device__ __forceinline__ int slim_warp_find(const int32_t* __restrict__ starts, int n, int r) {
+  const int lane = threadIdx.x & 31;
+  int lo = 0;
+  while (n > 1) {
+    const int step = (n + 31) / 32, at = lane * step;
+    const int k = __popc(__ballot_sync(0xffffffffu, at < n && starts[lo + min(at, n - 1)] <= r));
+    const int skip = max(k - 1, 0) * step;
+    lo += skip;
+    n = min(step, n - skip);
+  }
+  return lo;
+}
+
 template <typename... KArgs, typename... Args>
 inline cudaError_t slim_launch_pdl(void (*kern)(KArgs...), dim3 grid, dim3 block, size_t smem, cudaStream_t st,
                                    Args... args) {

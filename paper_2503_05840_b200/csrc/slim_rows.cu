@@ -2,8 +2,8 @@
 // and 4-bit caches, and the uniform append of a 4-bit cache (slim_append_k, slim_decode_step, slim_prefill).
 //
 // Both directions are bound by HBM: a row of d bf16 keys is read (2 d bytes) and d/2 + d/32 bytes are written, or the
-// other way round.  A warp takes 256 columns of a row at a time: 16 bytes a lane on the wide side, one 32-bit word of
-// eight codes on the other; four lanes share a scale.
+// other way round.  A warp takes 256 columns of a row at a time, four such chunks in flight: 16 bytes a lane on the wide
+// side, one 32-bit word of eight codes on the other; four lanes share a scale.
 #include "slim_fp4.cuh"
 
 namespace {
@@ -27,12 +27,7 @@ struct RowsArgs {
 __device__ long long rows_target(const RowsArgs& a, int r) {
   int b, i, n;
   if (a.cu) {
-    int lo = 0, hi = a.batch;                       // the last sequence that begins at or before r
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) >> 1;
-      if (a.cu[mid] <= r) lo = mid; else hi = mid;
-    }
-    b = lo;
+    b = slim_warp_find(a.cu, a.batch, r);
     const int first = a.cu[b], end = a.cu[b + 1];
     if (first < 0 || r < first || r >= end || end > a.total) return -1;
     i = r - first; n = end - first;
@@ -53,13 +48,48 @@ __device__ long long rows_target(const RowsArgs& a, int r) {
 }
 
 // Starts of packed sequences that do not ascend from 0 to at most `total` are reported (their rows are left out above).
+// By the last block, which has no rows.
 __device__ void rows_check(const RowsArgs& a) {
-  if (!a.cu || blockIdx.x != 0) return;
+  if (!a.cu || blockIdx.x != gridDim.x - 1) return;
   for (int b = threadIdx.x; b < a.batch; b += blockDim.x)
     if (a.cu[b] < 0 || a.cu[b + 1] < a.cu[b] || a.cu[b + 1] > a.total) atomicMax(a.status, (int)SLIM_ERR_CAPACITY);
 }
 
-// bf16 rows -> 4 bits
+// 256 columns of a row: eight a lane, from bf16 rows of any alignment
+__device__ __forceinline__ uint4 load8(const unsigned short* row, int col, int d, bool whole) {
+  if (whole) return __ldcs(reinterpret_cast<const uint4*>(row + col));
+  uint32_t w[4] = {0u, 0u, 0u, 0u};
+  for (int e = 0; e < 8 && col + e < d; ++e) w[e >> 1] |= (uint32_t)row[col + e] << (16 * (e & 1));
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// Eight keys and the largest magnitude of their group -> codes and the scale byte.
+// Codes are rounded by the conversion instruction, from k / s as k times the reciprocal of s.  That is off by some 2^-23,
+// which only matters on a border between two codes (k is a bf16 number, of 8 bits, and border times scale has 7: k / s is the
+// border itself or further than 2^-8 of it away).  Rounding to multiples of 2^-12 first brings the border's quotients
+// back onto it and leaves the others on their side.
+__device__ __forceinline__ uint32_t quantise8(const uint4& v, float amax, int& byte) {
+  const bool bad = !(amax <= 3.4028234663852886e38f);
+  byte = slim_fp4_scale_byte(amax, bad);
+  const float s = slim_fp4_scale((unsigned char)byte);
+  const float up = bad || !(amax > 0.f) ? 0.f : __frcp_rn(s);
+  const float magic = 0x1.8p11f;                                       // float32 steps of 2^-12 around it
+  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+  float y[8];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    y[2 * e] = (__uint_as_float(w[e] << 16) * up + magic) - magic;
+    y[2 * e + 1] = (__uint_as_float(w[e] & 0xffff0000u) * up + magic) - magic;
+  }
+  const uint32_t out = slim_fp4_encode8(y);
+  if (bad) return 0u;
+  // codes of magnitude 0 have no sign
+  const uint32_t some = (out | (out >> 1) | (out >> 2)) & 0x11111111u;
+  return out & (0x77777777u | (some << 3));
+}
+
+// bf16 rows -> 4 bits; CH: chunks of 256 columns whose loads are in flight together
+template <int CH>
 __global__ void __launch_bounds__(256) rows_quantise_kernel(const RowsArgs a) {
   slim_pdl_trigger();
   slim_pdl_wait();
@@ -69,54 +99,41 @@ __global__ void __launch_bounds__(256) rows_quantise_kernel(const RowsArgs a) {
   const long long rr = w / a.parts;
   if (rr >= a.total) return;
   const int part = (int)(w - rr * a.parts);
+  const unsigned short* src = reinterpret_cast<const unsigned short*>(a.wide) + (size_t)rr * a.d;
+  const bool whole = (a.d & 7) == 0 && ((uintptr_t)a.wide & 15) == 0;
   const long long row = rows_target(a, (int)rr);
   if (row < 0) return;
-  const unsigned short* src = reinterpret_cast<const unsigned short*>(a.wide) + (size_t)rr * a.d;
   unsigned char* dst = a.codes + (size_t)row * a.pitch;
   unsigned char* sdst = a.scales + (size_t)row * a.spitch;
-  const bool whole = (a.d & 7) == 0 && ((uintptr_t)a.wide & 15) == 0;
-#pragma unroll 4
-  for (int c = 0; c < a.chunks; ++c) {
-    const int col = (part * a.chunks + c) * 256 + lane * 8;
-    uint32_t w4[4] = {0u, 0u, 0u, 0u};
-    if (col < a.d) {
-      if (whole) {
-        const uint4 v = __ldcs(reinterpret_cast<const uint4*>(src + col));
-        w4[0] = v.x; w4[1] = v.y; w4[2] = v.z; w4[3] = v.w;
-      } else {
-        for (int e = 0; e < 8 && col + e < a.d; ++e) w4[e >> 1] |= (uint32_t)src[col + e] << (16 * (e & 1));
+  for (int c0 = 0; c0 < a.chunks; c0 += CH) {
+    uint4 v[CH];
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+      const int col = (part * a.chunks + c0 + c) * 256 + lane * 8;
+      v[c] = col < a.d ? load8(src, col, a.d, whole) : make_uint4(0u, 0u, 0u, 0u);
+    }
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+      const int col = (part * a.chunks + c0 + c) * 256 + lane * 8;
+      // largest magnitude of the group's 32 columns, NaN if there is one: the sign cleared, the bits of bf16 numbers order as integers
+      uint32_t m = __vmaxu2(__vmaxu2(v[c].x & 0x7fff7fffu, v[c].y & 0x7fff7fffu), __vmaxu2(v[c].z & 0x7fff7fffu, v[c].w & 0x7fff7fffu));
+      m = __vmaxu2(m, __shfl_xor_sync(0xffffffffu, m, 1));
+      m = __vmaxu2(m, __shfl_xor_sync(0xffffffffu, m, 2));
+      const float amax = __uint_as_float(max(m << 16, m & 0xffff0000u));
+      int byte;
+      const uint32_t out = quantise8(v[c], amax, byte);
+      if (col < a.d) {
+        if (col + 8 <= a.d) *reinterpret_cast<uint32_t*>(dst + (col >> 1)) = out;
+        else
+          for (int e = 0; 2 * e < a.d - col; ++e) dst[(col >> 1) + e] = (unsigned char)(out >> (8 * e));
+        if ((lane & 3) == 0) sdst[col / FP4_GROUP] = (unsigned char)byte;
       }
-    }
-    float k[8], amax = 0.f;
-    bool bad = false;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      k[e] = __uint_as_float(e & 1 ? w4[e >> 1] & 0xffff0000u : w4[e >> 1] << 16);
-      bad |= !(fabsf(k[e]) <= 3.4028234663852886e38f);
-      amax = fmaxf(amax, fabsf(k[e]));
-    }
-#pragma unroll
-    for (int o = 1; o < 4; o <<= 1) {
-      amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
-      bad |= __shfl_xor_sync(0xffffffffu, (int)bad, o) != 0;
-    }
-    const int sb = slim_fp4_scale_byte(amax, bad);
-    const float s = bad ? 1.f : slim_fp4_scale((unsigned char)sb);
-    uint32_t out = 0u;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) out |= (bad ? 0u : slim_fp4_code(k[e], s)) << (4 * e);
-    if (col < a.d) {
-      if (col + 8 <= a.d || whole) {
-        *reinterpret_cast<uint32_t*>(dst + (col >> 1)) = out;
-      } else {
-        for (int e = 0; 2 * e < a.d - col; ++e) dst[(col >> 1) + e] = (unsigned char)(out >> (8 * e));
-      }
-      if ((lane & 3) == 0) sdst[col / FP4_GROUP] = (unsigned char)sb;
     }
   }
 }
 
-// 4 bits -> bf16 rows (exact)
+// 4 bits -> bf16 rows (exact: a value has six significant bits)
+template <int CH>
 __global__ void __launch_bounds__(256) rows_expand_kernel(const RowsArgs a) {
   slim_pdl_trigger();
   slim_pdl_wait();
@@ -132,22 +149,32 @@ __global__ void __launch_bounds__(256) rows_expand_kernel(const RowsArgs a) {
   const unsigned char* src = a.codes + (size_t)row * a.pitch;
   const unsigned char* ssrc = a.scales + (size_t)row * a.spitch;
   const bool whole = (a.d & 7) == 0 && ((uintptr_t)a.wide & 15) == 0;
-#pragma unroll 4
-  for (int c = 0; c < a.chunks; ++c) {
-    const int col = (part * a.chunks + c) * 256 + lane * 8;
-    if (col >= a.d) continue;
-    const uint32_t w4 = __ldcs(reinterpret_cast<const unsigned int*>(src + (col >> 1)));      // (rows are padded to 16 bytes)
-    const float s = slim_fp4_scale(__ldg(ssrc + col / FP4_GROUP));
-    uint32_t out[4];
+  for (int c0 = 0; c0 < a.chunks; c0 += CH) {
+    uint32_t v[CH], s[CH];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const float lo = slim_fp4_value((w4 >> (8 * e)) & 15u) * s, hi = slim_fp4_value((w4 >> (8 * e + 4)) & 15u) * s;
-      const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
-      out[e] = *reinterpret_cast<const uint32_t*>(&v);
+    for (int c = 0; c < CH; ++c) {
+      const int col = (part * a.chunks + c0 + c) * 256 + lane * 8;
+      v[c] = col < a.d ? __ldcs(reinterpret_cast<const unsigned int*>(src + (col >> 1))) : 0u;      // (rows are padded to 16 bytes)
+      s[c] = col < a.d ? __ldg(ssrc + col / FP4_GROUP) : 0u;
     }
-    if (whole) __stcs(reinterpret_cast<uint4*>(dst + col), make_uint4(out[0], out[1], out[2], out[3]));
-    else
-      for (int e = 0; e < 8 && col + e < a.d; ++e) dst[col + e] = (unsigned short)(out[e >> 1] >> (16 * (e & 1)));
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+      const int col = (part * a.chunks + c0 + c) * 256 + lane * 8;
+      if (col >= a.d) continue;
+      const uint32_t scale = s[c] * 0x00800080u;                       // a float16 pair
+      uint32_t h[4], out[4];
+      slim_fp4_decode8(v[c], h);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const __half2 x = __hmul2(*reinterpret_cast<const __half2*>(&h[e]), *reinterpret_cast<const __half2*>(&scale));
+        const float2 f = __half22float2(x);
+        const __nv_bfloat162 y = __floats2bfloat162_rn(f.x, f.y);
+        out[e] = *reinterpret_cast<const uint32_t*>(&y);
+      }
+      if (whole) __stcs(reinterpret_cast<uint4*>(dst + col), make_uint4(out[0], out[1], out[2], out[3]));
+      else
+        for (int e = 0; e < 8 && col + e < a.d; ++e) dst[col + e] = (unsigned short)(out[e >> 1] >> (16 * (e & 1)));
+    }
   }
 }
 
@@ -183,12 +210,15 @@ cudaError_t launch_rows(const slim_ctx* ctx, RowsArgs a, int to_cache, cudaStrea
   if (!fp4) while ((a.pitch % unit) || (((uintptr_t)a.wide | (uintptr_t)a.codes) % unit)) unit >>= 1;
   const int span = fp4 ? 256 : 32;                                     // columns (units) a warp takes at a time
   const int n = ((fp4 ? a.d : a.pitch / (int)unit) + span - 1) / span;
-  // Four chunks a warp keep four loads of a lane in flight; fewer where the rows alone would not give every SM 16 warps.
-  a.chunks = (long long)a.total * n >= 64ll * ctx->num_sms ? 4 : 1;
+  // A row a warp where the rows alone give every SM 64 warps (the row's place is then looked up once); with fewer rows they are
+  // split, down to one chunk a warp.
+  a.chunks = n;
+  while (a.chunks > 1 && (long long)a.total * ((n + a.chunks - 1) / a.chunks) < 64ll * ctx->num_sms) a.chunks = (a.chunks + 1) / 2;
   a.parts = (n + a.chunks - 1) / a.chunks;
   const long long warps = (long long)a.total * a.parts;
-  const dim3 grid((unsigned)((warps + 7) / 8)), block(256);
-  if (fp4) return slim_launch_pdl(to_cache ? rows_quantise_kernel : rows_expand_kernel, grid, block, 0, st, a);
+  const dim3 grid((unsigned)((warps + 7) / 8) + 1), block(256);
+  if (fp4 && a.chunks > 1) return slim_launch_pdl(to_cache ? rows_quantise_kernel<4> : rows_expand_kernel<4>, grid, block, 0, st, a);
+  if (fp4) return slim_launch_pdl(to_cache ? rows_quantise_kernel<1> : rows_expand_kernel<1>, grid, block, 0, st, a);
   switch (unit) {
     case 16: return slim_launch_pdl(rows_copy_kernel<uint4>, grid, block, 0, st, a, to_cache);
     case 8: return slim_launch_pdl(rows_copy_kernel<uint2>, grid, block, 0, st, a, to_cache);
