@@ -63,8 +63,8 @@ __global__ void __launch_bounds__(THREADS) attn_kernel(const __grid_constant__ S
   slim_pdl_wait();
   const int item = blockIdx.x / a.H, h = blockIdx.x % a.H;
   if (item >= *a.n_tiles) return;
-  const int4 tile = a.tiles[item];
-  const SlimSeq s = slim_attn_seq(a, tile.x);
+  const int4 tile = a.tiles[2 * item], range = a.tiles[2 * item + 1];
+  const SlimSeq s = {range.x, range.y, range.z, range.w};
   const int row0 = tile.y, rows = min(TR, s.nq - row0), dk = a.d_k, kvh = h / (a.H / a.KV);
   const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
   const float* qr = reinterpret_cast<const float*>(a.qr) + ((size_t)(s.q0 + row0) * a.H + h) * dk;
@@ -214,7 +214,7 @@ SlimAttnLayout slim_attn_layout(const slim_ctx* ctx, int kv_heads, int batch, in
   L.qr = off; off = align256(off + 4 * (size_t)total_q * ctx->d);
   L.kr = off; off = align256(off + 4 * (size_t)total_k * kv_heads * ctx->d_k);
   L.vb = off; off = align256(off + (slim_attn_tc_ok(ctx) ? 2 * (size_t)total_k * kv_heads * ctx->d_k : 0));
-  L.tiles = off; off = align256(off + sizeof(int4) * ((size_t)total_q / SLIM_ATTN_ROWS + batch + 1));
+  L.tiles = off; off = align256(off + 2 * sizeof(int4) * ((size_t)total_q / SLIM_ATTN_ROWS + batch + 1));
   L.n_tiles = off; off = align256(off + sizeof(int));
   L.total = off;
   return L;

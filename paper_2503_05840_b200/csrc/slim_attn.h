@@ -21,7 +21,7 @@ struct SlimAttn {
   void* qr;                      // rotated queries and keys, layout of q and k: float32 (CUDA cores) or float16 (tensor cores)
   void* kr;
   void* vb;                      // tensor cores with float32 values: the values times 16 as float16
-  int4* tiles;                   // (sequence, first query row, -, -), most keys first
+  int4* tiles;                   // query tiles, most keys first, two entries each: (sequence, first query row, -, -), (q0, nq, k0, nk)
   int* n_tiles;
   int tile_rows, most_tiles;
 };

@@ -42,7 +42,11 @@ static __device__ void slim_attn_plan(const SlimAttn& a, int* s_mem) {
       const int keys = slim_attn_keys(a, s, min(s.nq, row + a.tile_rows) - 1);
       const int bin = SLIM_ATTN_BINS - 1 - (int)((long long)keys * (SLIM_ATTN_BINS - 1) / max(a.max_k, 1));
       if (pass == 0) atomicAdd(&s_bin[bin], 1);
-      else a.tiles[atomicAdd(&s_bin[bin], 1)] = make_int4(lo, row, 0, 0);
+      else {
+        int4* to = a.tiles + 2 * atomicAdd(&s_bin[bin], 1);
+        to[0] = make_int4(lo, row, 0, 0);
+        to[1] = make_int4(s.q0, s.nq, s.k0, s.nk);
+      }
     }
     __syncthreads();
     if (pass == 0 && tid == 0) {

@@ -109,7 +109,7 @@ struct Shape {
   static constexpr int CH = (DK + 63) / 64;          // 64-column chunks of a head
   static constexpr int TILE = CH * TN * 128;         // bytes of a tile of Q, K or V
   static constexpr int NS = DK == 64 ? 8 : 5;        // ring of K and V tiles
-  static constexpr int SMEM = 1024 + (2 + NS) * TILE + 8 * (2 * NS + 8) + 32;
+  static constexpr int SMEM = 1024 + (2 + NS) * TILE + 8 * (2 * NS + 9) + 32;
 };
 
 __device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t* r) {
@@ -121,6 +121,19 @@ __device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t* r) {
         "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]),
         "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]),
         "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]) : "memory");
+}
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t* r) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];\n\t"
+      "tcgen05.wait::ld.sync.aligned;"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]),
+        "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]) : "r"(taddr) : "memory");
+}
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t* r) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
+      ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]),
+        "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]) : "memory");
 }
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 // A from shared memory / from tensor memory
@@ -156,7 +169,8 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
   const uint32_t s_q = base, s_kv = base + 2 * TILE;
   const uint32_t bars = s_kv + NS * TILE;
   const uint32_t bar_full = bars, bar_empty = bars + 8 * NS, bar_q = bars + 16 * NS;
-  const uint32_t bar_s = bar_q + 8, bar_p = bar_s + 16, bar_o = bar_p + 16;                  // two each
+  const uint32_t bar_qe = bar_q + 8;
+  const uint32_t bar_s = bar_qe + 8, bar_p = bar_s + 16, bar_o = bar_p + 16;                 // two each
   unsigned char* misc = sm + (bar_o + 16 - base);
   uint32_t* s_tmem = reinterpret_cast<uint32_t*>(misc);
   volatile int* s_abort = reinterpret_cast<volatile int*>(misc + 4);
@@ -166,233 +180,272 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
     prefetch_tensormap(&qmap); prefetch_tensormap(&kmap); prefetch_tensormap(&vmap);
     for (int i = 0; i < NS; ++i) { mbar_init(bar_full + 8 * i, 1); mbar_init(bar_empty + 8 * i, 1); }
     mbar_init(bar_q, 1);
+    mbar_init(bar_qe, 1);
     for (int i = 0; i < 2; ++i) { mbar_init(bar_s + 8 * i, 1); mbar_init(bar_p + 8 * i, 4); mbar_init(bar_o + 8 * i, 1); }
     *s_abort = 0;
     fence_mbar_init();
   }
-  slim_pdl_trigger();
-  slim_pdl_wait();
-  const int item = blockIdx.x / a.H, h = blockIdx.x % a.H;
-  if (item >= *a.n_tiles) return;
   if (warp == 8) tmem_alloc(smem_u32(s_tmem), 512);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = *s_tmem;
-
-  const int4 tile = a.tiles[item];
-  const SlimSeq s = slim_attn_seq(a, tile.x);
-  const int row0 = tile.y, kvh = h / (a.H / a.KV);
-  // key tiles of the two query tiles (the second may have no rows)
-  const int nt0 = (slim_attn_keys(a, s, min(s.nq, row0 + TM) - 1) + TN - 1) / TN;
-  const int nt1 = row0 + TM < s.nq ? (slim_attn_keys(a, s, min(s.nq, row0 + 2 * TM) - 1) + TN - 1) / TN : 0;
-  const int nt = max(nt0, nt1);
+  slim_pdl_trigger();
+  slim_pdl_wait();
+  const int n_items = *a.n_tiles * a.H, share = a.H / a.KV;
+  // Item number r of this CTA: the list, most keys first, is dealt out in rounds of alternating direction.
+  struct Item { SlimSeq s; int b, row0, h, nt0, nt1; };
+  auto item = [&](int r, Item& it) {
+    const long long at = (long long)r * gridDim.x + (r & 1 ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
+    if (at >= n_items) return false;
+    const int tile = (int)(at / a.H);
+    it.h = (int)(at - (long long)tile * a.H);
+    const int4 x = __ldg(a.tiles + 2 * tile), y = __ldg(a.tiles + 2 * tile + 1);
+    it.b = x.x; it.row0 = x.y;
+    it.s.q0 = y.x; it.s.nq = y.y; it.s.k0 = y.z; it.s.nk = y.w;
+    // key tiles of the two query tiles (the second may have no rows)
+    it.nt0 = (slim_attn_keys(a, it.s, min(it.s.nq, it.row0 + TM) - 1) + TN - 1) / TN;
+    it.nt1 = it.row0 + TM < it.s.nq ? (slim_attn_keys(a, it.s, min(it.s.nq, it.row0 + 2 * TM) - 1) + TN - 1) / TN : 0;
+    return true;
+  };
+  Item it;
+  bool ok = true;
 
   if (warp < 8) {
-    // 168 registers a thread at launch: the last four warps hand 112 of theirs to the softmax warps' 56 (224 x 256 + 56 x 128 = 168 x 384)
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
+    // 168 registers a thread at launch; the last four warps leave 128 of theirs to the others (232 x 256 + 40 x 128 = 168 x 384)
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 232;");
     // =========================== softmax ===========================
     const int i = warp >> 2;
-    const int n = i ? nt1 : nt0;
-    const int row = row0 + i * TM + (warp & 3) * 32 + lane;
-    const int lim = slim_attn_keys(a, s, row);
     const uint32_t t_s = tmem + ((uint32_t)((warp & 3) * 32) << 16) + (uint32_t)(i * TN);
     const uint32_t t_o = tmem + ((uint32_t)((warp & 3) * 32) << 16) + (uint32_t)(2 * TN + i * 128);
     const float scale = a.qscale;
     const f32x2 scale2 = pack2(scale, scale);
-    float m = -INFINITY;                            // reference, log2 units
-    f32x2 l2 = pack2(0.f, 0.f);
-    bool ok = true;
-    for (int j = 0; j < n; ++j) {
-      ok = mbar_wait<false>(bar_s + 8 * i, j & 1, s_abort, a.status);
-      ok = __all_sync(0xffffffffu, ok);
-      if (!ok) break;
-      tc_fence_after();
-      uint32_t r[4][32];
+    uint32_t ps = 0, po = 0;                        // phases of bar_s, bar_o
+    for (int r_ = 0; ok && item(r_, it); ++r_) {
+      const int n = i ? it.nt1 : it.nt0;
+      const int lim = slim_attn_keys(a, it.s, it.row0 + i * TM + (warp & 3) * 32 + lane);
+      float m = -INFINITY;                            // reference, log2 units
+      f32x2 l2 = pack2(0.f, 0.f);
+      for (int j = 0; j < n; ++j) {
+        ok = mbar_wait<false>(bar_s + 8 * i, ps, s_abort, a.status);
+        ps ^= 1u;
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) break;
+        tc_fence_after();
+        uint32_t r[4][32];
 #pragma unroll
-      for (int c = 0; c < 4; ++c) tmem_ld32_issue(t_s + 32 * c, r[c]);
-      tmem_ld_wait();
-      if (__any_sync(0xffffffffu, (j + 1) * TN > lim)) {
+        for (int c = 0; c < 4; ++c) tmem_ld32_issue(t_s + 32 * c, r[c]);
+        tmem_ld_wait();
+        if (__any_sync(0xffffffffu, (j + 1) * TN > lim)) {
 #pragma unroll
-        for (int c = 0; c < 4; ++c)
+          for (int c = 0; c < 4; ++c)
 #pragma unroll
-          for (int x = 0; x < 32; ++x)
-            if (j * TN + 32 * c + x >= lim) r[c][x] = 0xff800000u;
-      }
-      float mx[4];
-#pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        mx[c] = __uint_as_float(r[c][0]);
-#pragma unroll
-        for (int x = 1; x < 32; ++x) mx[c] = fmaxf(mx[c], __uint_as_float(r[c][x]));
-      }
-      const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * scale;
-      const bool move = top > m + TAU;              // (m = -inf: the first keys of the row)
-      if (__any_sync(0xffffffffu, move)) {
-        const float m_new = move ? top : m;
-        const float f = move ? ex2_approx(m - m_new) : 1.f;
-        m = m_new;
-        float lo, hi;
-        split(l2, lo, hi);
-        l2 = pack2(lo * f, hi * f);
-        if (j > 0) {
-          // O_i is at rest: S_i(j) was completed after O_i += P_i(j - 1) V, and the next product waits for P_i(j)
-#pragma unroll
-          for (int c = 0; c < DK / 32; ++c) {
-            uint32_t o[32];
-            tmem_ld32(t_o + 32 * c, o);
-#pragma unroll
-            for (int x = 0; x < 32; ++x) o[x] = __float_as_uint(__uint_as_float(o[x]) * f);
-            tmem_st32(t_o + 32 * c, o);
-          }
+            for (int x = 0; x < 32; ++x)
+              if (j * TN + 32 * c + x >= lim) r[c][x] = 0xff800000u;
         }
-      }
-      const float mm = m == -INFINITY ? 0.f : -m;
-      const f32x2 m2 = pack2(mm, mm);
+        float mx[4];
 #pragma unroll
-      for (int c = 0; c < 4; ++c) {
+        for (int c = 0; c < 4; ++c) {
+          mx[c] = __uint_as_float(r[c][0]);
 #pragma unroll
-        for (int x = 0; x < 32; x += 2) {
-          f32x2 v = pack2(__uint_as_float(r[c][x]), __uint_as_float(r[c][x + 1]));
-          v = fma2(v, scale2, m2);
+          for (int x = 1; x < 32; ++x) mx[c] = fmaxf(mx[c], __uint_as_float(r[c][x]));
+        }
+        const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * scale;
+        const bool move = top > m + TAU;              // (m = -inf: the first keys of the row)
+        if (__any_sync(0xffffffffu, move)) {
+          const float m_new = move ? top : m;
+          const float f = move ? ex2_approx(m - m_new) : 1.f;
+          m = m_new;
           float lo, hi;
-          split(v, lo, hi);
-          lo = ex2_approx(lo); hi = ex2_approx(hi);
-          l2 = add2(l2, pack2(lo, hi));
-          r[c >> 1][(c & 1) * 16 + x / 2] = VH ? half2_of(lo, hi) : bf162_of(lo, hi);
-        }
-      }
-      tmem_st32(t_s, r[0]);
-      tmem_st32(t_s + 32, r[1]);
-      tmem_st_wait();
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(bar_p + 8 * i);
-    }
-    // ---- output ----
-    if (ok && n > 0) {
-      ok = mbar_wait<false>(bar_o + 8 * i, 0, s_abort, a.status);
-      ok = __all_sync(0xffffffffu, ok);
-      tc_fence_after();
-    }
-    const bool there = row < s.nq && (i == 0 || nt1 > 0 || row0 + TM < s.nq);
-    const float inv = lim > 0 ? (VH ? 1.f / V_UP : 1.f) / sum2(l2) : 0.f;
-    __nv_bfloat16* dst = reinterpret_cast<__nv_bfloat16*>(a.o) + ((size_t)(s.q0 + row) * a.H + h) * DK;
-    bool bad = false;
-    float most = 0.f;
-    if (ok) {
+          split(l2, lo, hi);
+          l2 = pack2(lo * f, hi * f);
+          if (j > 0) {
+            // O_i is at rest: S_i(j) was completed after O_i += P_i(j - 1) V, and the next product waits for P_i(j)
 #pragma unroll
-      for (int c = 0; c < DK / 32; ++c) {
-        uint32_t o[32];
-        if (n > 0) tmem_ld32(t_o + 32 * c, o);
+            for (int c = 0; c < DK / 16; ++c) {       // (16 columns at a time: S is in registers too)
+              uint32_t o[16];
+              tmem_ld16(t_o + 16 * c, o);
 #pragma unroll
-        for (int x = 0; x < 32; x += 8) {
-          uint32_t w[4];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            float lo = __uint_as_float(o[x + 2 * e]) * inv, hi = __uint_as_float(o[x + 2 * e + 1]) * inv;
-            if (lim == 0) lo = hi = 0.f;
-            bad |= !(fabsf(lo) <= 3.3895313892515355e38f && fabsf(hi) <= 3.3895313892515355e38f);
-            if (VH) most = fmaxf(most, fmaxf(fabsf(lo), fabsf(hi)));
-            w[e] = bf162_of(lo, hi);
+              for (int x = 0; x < 16; ++x) o[x] = __float_as_uint(__uint_as_float(o[x]) * f);
+              tmem_st16(t_o + 16 * c, o);
+            }
           }
-          if (there) *reinterpret_cast<uint4*>(dst + 32 * c + x) = make_uint4(w[0], w[1], w[2], w[3]);
         }
-      }
-      if (VH) bad |= lim > 0 && most < 3.8e-6f;      // 2^-18
-      unsigned redo = __ballot_sync(0xffffffffu, bad && there);
-      while (redo) {
-        const int x = __ffs(redo) - 1;
-        redo &= redo - 1;
+        const float mm = m == -INFINITY ? 0.f : -m;
+        const f32x2 m2 = pack2(mm, mm);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+#pragma unroll
+          for (int x = 0; x < 32; x += 2) {
+            f32x2 v = pack2(__uint_as_float(r[c][x]), __uint_as_float(r[c][x + 1]));
+            v = fma2(v, scale2, m2);
+            float lo, hi;
+            split(v, lo, hi);
+            lo = ex2_approx(lo); hi = ex2_approx(hi);
+            l2 = add2(l2, pack2(lo, hi));
+            r[c >> 1][(c & 1) * 16 + x / 2] = VH ? half2_of(lo, hi) : bf162_of(lo, hi);
+          }
+        }
+        tmem_st32(t_s, r[0]);
+        tmem_st32(t_s + 32, r[1]);
+        tmem_st_wait();
+        tc_fence_before();
         __syncwarp();
-        slim_attn_row(a, tile.x, row0 + i * TM + (warp & 3) * 32 + x, h);
+        if (lane == 0) mbar_arrive(bar_p + 8 * i);
+      }
+      // ---- output ----
+      item(r_, it);                                   // (once more: nothing of it has to be kept while S is in registers)
+      const SlimSeq s = it.s;
+      const int row = it.row0 + i * TM + (warp & 3) * 32 + lane, h = it.h;
+      if (ok && n > 0) {
+        ok = mbar_wait<false>(bar_o + 8 * i, po, s_abort, a.status);
+        po ^= 1u;
+        ok = __all_sync(0xffffffffu, ok);
+        tc_fence_after();
+      }
+      const bool there = row < s.nq;
+      const float inv = lim > 0 ? (VH ? 1.f / V_UP : 1.f) / sum2(l2) : 0.f;
+      __nv_bfloat16* dst = reinterpret_cast<__nv_bfloat16*>(a.o) + ((size_t)(s.q0 + row) * a.H + h) * DK;
+      bool bad = false;
+      float most = 0.f;
+      if (ok) {
+#pragma unroll
+        for (int c = 0; c < DK / 32; ++c) {
+          uint32_t o[32];
+          if (n > 0) tmem_ld32(t_o + 32 * c, o);
+#pragma unroll
+          for (int x = 0; x < 32; x += 8) {
+            uint32_t w[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              float lo = __uint_as_float(o[x + 2 * e]) * inv, hi = __uint_as_float(o[x + 2 * e + 1]) * inv;
+              if (lim == 0) lo = hi = 0.f;
+              bad |= !(fabsf(lo) <= 3.3895313892515355e38f && fabsf(hi) <= 3.3895313892515355e38f);
+              if (VH) most = fmaxf(most, fmaxf(fabsf(lo), fabsf(hi)));
+              w[e] = bf162_of(lo, hi);
+            }
+            if (there) *reinterpret_cast<uint4*>(dst + 32 * c + x) = make_uint4(w[0], w[1], w[2], w[3]);
+          }
+        }
+        if (VH) bad |= lim > 0 && most < 3.8e-6f;      // 2^-18
+        unsigned redo = __ballot_sync(0xffffffffu, bad && there);
+        while (redo) {
+          const int x = __ffs(redo) - 1;
+          redo &= redo - 1;
+          __syncwarp();
+          slim_attn_row(a, it.b, it.row0 + i * TM + (warp & 3) * 32 + x, h);
+        }
       }
     }
   } else if (warp == 8) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
     // =========================== MMA issuer ===========================
     // The warp stays together and one elected lane issues, so that the descriptors live in uniform registers.
-    if (nt > 0) {
-      bool ok = mbar_wait<false>(bar_q, 0, s_abort, a.status);
-      auto full = [&](int k) { return mbar_wait<false>(bar_full + 8 * (k % NS), (k / NS) & 1, s_abort, a.status); };
-      const uint64_t dq = desc_kmajor_sw128(s_q), dk = desc_kmajor_sw128(s_kv), dv = desc_a(s_kv, TN * 128);
-      auto scores = [&](int i, int k) {
-        const uint64_t qd = dq + (uint64_t)(i * (TILE >> 4)), kd = dk + (uint64_t)((k % NS) * (TILE >> 4));
+    const uint64_t dq = desc_kmajor_sw128(s_q), dk = desc_kmajor_sw128(s_kv), dv = desc_a(s_kv, TN * 128);
+    uint32_t pq = 0, pf = 0, pp0 = 0, pp1 = 0;      // phases: queries, ring, P of the two tiles
+    int st = 0;                                     // next stage of the ring
+    uint32_t last = 0xffffffffu, last_ph = 0;       // stage committed last, and its phase
+    auto scores = [&](int i, uint32_t stage) {
+      const uint64_t qd = dq + (uint64_t)(i * (TILE >> 4)), kd = dk + (uint64_t)(stage * (TILE >> 4));
 #pragma unroll
-        for (int x = 0; x < KSTEPS; ++x) {
-          const uint32_t off = (uint32_t)((x >> 2) * TN * 128 + (x & 3) * 32) >> 4;
-          umma_ss(tmem + i * TN, qd + off, kd + off, IDESC_S, x > 0);
-        }
-        umma_commit(bar_s + 8 * i);
-      };
-      ok = full(0) && ok;
+      for (int x = 0; x < KSTEPS; ++x) {
+        const uint32_t off = (uint32_t)((x >> 2) * TN * 128 + (x & 3) * 32) >> 4;
+        umma_ss(tmem + i * TN, qd + off, kd + off, IDESC_S, x > 0);
+      }
+      umma_commit(bar_s + 8 * i);
+    };
+    for (int r_ = 0; ok && item(r_, it); ++r_) {
+      const int nt = max(it.nt0, it.nt1);
+      if (nt == 0) continue;
+      ok = mbar_wait<false>(bar_q, pq, s_abort, a.status);
+      pq ^= 1u;
+      ok = mbar_wait<false>(bar_full + 8 * st, pf, s_abort, a.status) && ok;
       ok = __all_sync(0xffffffffu, ok);
+      if (!ok) break;
       tc_fence_after();
-      if (ok && elect_one()) {
-        if (nt0 > 0) scores(0, 0);
-        if (nt1 > 0) scores(1, 0);
-        umma_commit(bar_empty);
+      if (elect_one()) {
+        if (it.nt0 > 0) scores(0, (uint32_t)st);
+        if (it.nt1 > 0) scores(1, (uint32_t)st);
+        umma_commit(bar_empty + 8 * st);
+        if (nt == 1) umma_commit(bar_qe);
       }
       __syncwarp();
+      if (++st == NS) { st = 0; pf ^= 1u; }
       for (int j = 0; j < nt && ok; ++j) {
-        const int kv = 2 * j + 1, kk = 2 * j + 2;
-        ok = full(kv);
-        if (j + 1 < nt) ok = full(kk) && ok;
-        for (int i = 0; i < 2 && ok; ++i) {
-          const int n = i ? nt1 : nt0;
-          if (j >= n) continue;
-          ok = mbar_wait<false>(bar_p + 8 * i, j & 1, s_abort, a.status) && ok;
-          ok = __all_sync(0xffffffffu, ok);
-          if (!ok) break;
-          tc_fence_after();
-          if (elect_one()) {
-            const uint64_t vd = dv + (uint64_t)((kv % NS) * (TILE >> 4));
+        const int kv = st, kk = st + 1 == NS ? 0 : st + 1;
+        const uint32_t pkv = pf, pkk = kk == 0 ? pf ^ 1u : pf;
+        ok = mbar_wait<false>(bar_full + 8 * kv, pkv, s_abort, a.status);
+        if (j + 1 < nt) ok = mbar_wait<false>(bar_full + 8 * kk, pkk, s_abort, a.status) && ok;
 #pragma unroll
-            for (int x = 0; x < TN / 16; ++x)
-              umma_ts(tmem + 2 * TN + i * 128, tmem + i * TN + 8 * x, vd + x * (2048 >> 4), IDESC_O, j > 0 || x > 0);
-            if (j + 1 < n) scores(i, kk);
-            else umma_commit(bar_o + 8 * i);
+        for (int i = 0; i < 2; ++i) {
+          const int n = i ? it.nt1 : it.nt0;
+          if (j < n && ok) {
+            uint32_t& pp = i ? pp1 : pp0;
+            ok = mbar_wait<false>(bar_p + 8 * i, pp, s_abort, a.status);
+            pp ^= 1u;
+            ok = __all_sync(0xffffffffu, ok);
+            tc_fence_after();
+            if (ok && elect_one()) {
+              const uint64_t vd = dv + (uint64_t)(kv * (int)(TILE >> 4));
+#pragma unroll
+              for (int x = 0; x < TN / 16; ++x)
+                umma_ts(tmem + 2 * TN + i * 128, tmem + i * TN + 8 * x, vd + x * (2048 >> 4), IDESC_O, j > 0 || x > 0);
+              if (j + 1 < n) scores(i, (uint32_t)kk);
+              else umma_commit(bar_o + 8 * i);
+            }
+            __syncwarp();
           }
-          __syncwarp();
         }
         if (!ok) break;
         if (elect_one()) {
-          umma_commit(bar_empty + 8 * (kv % NS));
-          if (j + 1 < nt) umma_commit(bar_empty + 8 * (kk % NS));
+          umma_commit(bar_empty + 8 * kv);
+          if (j + 1 < nt) umma_commit(bar_empty + 8 * kk);
+          if (j + 2 == nt) umma_commit(bar_qe);     // the item's last scores are behind it
         }
         __syncwarp();
+        last = (uint32_t)kv; last_ph = pkv;
+        const int used = j + 1 < nt ? 2 : 1;
+        for (int x = 0; x < used; ++x)
+          if (++st == NS) { st = 0; pf ^= 1u; }
       }
-      // the last commit's arrival must not find this CTA gone
-      if (ok) mbar_wait<false>(bar_empty + 8 * ((2 * nt - 1) % NS), ((2 * nt - 1) / NS) & 1, s_abort, a.status);
     }
+    // the last commit's arrival must not find this CTA gone
+    if (ok && last != 0xffffffffu) mbar_wait<false>(bar_empty + 8 * last, last_ph, s_abort, a.status);
+    __syncwarp();
   } else if (warp == 9) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
     // =========================== loads ===========================
-    if (lane == 0 && nt > 0) {
-      const uint32_t tiles_q = nt1 > 0 ? 2 : 1;
-      mbar_arrive_expect_tx(bar_q, tiles_q * TILE);
-      for (uint32_t i = 0; i < tiles_q; ++i)
-        for (int c = 0; c < CH; ++c) tma_load_3d(s_q + i * TILE + c * TM * 128, &qmap, bar_q, h * DK + 64 * c, s.q0 + row0 + (int)i * TM, 0);
-      bool ok = true;
-      int k = 0;
-      for (; k < 2 * nt; ++k) {
-        ok = mbar_wait<false>(bar_empty + 8 * (k % NS), ((k / NS) & 1) ^ 1, s_abort, a.status);
+    if (lane == 0) {
+      int st = 0;                                   // next stage
+      uint32_t pe = 1u, pqe = 1u;                   // phases of bar_empty, bar_qe (the first pass finds everything empty)
+      for (int r_ = 0; ok && item(r_, it); ++r_) {
+        const int nt = max(it.nt0, it.nt1), kvh = it.h / share;
+        if (nt == 0) continue;
+        ok = mbar_wait<false>(bar_qe, pqe, s_abort, a.status);
         if (!ok) break;
-        const uint32_t bar = bar_full + 8 * (k % NS), dst = s_kv + (k % NS) * TILE;
-        mbar_arrive_expect_tx(bar, TILE);
-        for (int c = 0; c < CH; ++c)
-          tma_load_3d(dst + c * TN * 128, k & 1 ? &vmap : &kmap, bar, kvh * DK + 64 * c, s.k0 + (k >> 1) * TN, 0);
+        pqe ^= 1u;
+        const uint32_t tiles_q = it.nt1 > 0 ? 2 : 1;
+        mbar_arrive_expect_tx(bar_q, tiles_q * TILE);
+        for (uint32_t i = 0; i < tiles_q; ++i)
+          for (int c = 0; c < CH; ++c) tma_load_3d(s_q + i * TILE + c * TM * 128, &qmap, bar_q, it.h * DK + 64 * c, it.s.q0 + it.row0 + (int)i * TM, 0);
+        for (int k = 0; k < 2 * nt; ++k) {
+          ok = mbar_wait<false>(bar_empty + 8 * st, pe, s_abort, a.status);
+          if (!ok) break;
+          const uint32_t bar = bar_full + 8 * st, dst = s_kv + (uint32_t)st * TILE;
+          mbar_arrive_expect_tx(bar, TILE);
+          for (int c = 0; c < CH; ++c)                                 // K(0), V(0), K(1), ..: the order in which they are needed
+            tma_load_3d(dst + c * TN * 128, k & 1 ? &vmap : &kmap, bar, kvh * DK + 64 * c, it.s.k0 + (k >> 1) * TN, 0);
+          if (++st == NS) { st = 0; pe ^= 1u; }
+        }
       }
       if (!ok) {
-        // gave up: let the loads that were issued land before the CTA goes away
+        // gave up, two seconds after the last of a ring's loads: a quarter of a second more for any of them that is still on its way
         const unsigned long long t0 = globaltimer();
-        while (!mbar_try_wait(bar_q, 0) && globaltimer() - t0 < SLIM_WAIT_NS) {}
-        for (int x = max(0, k - NS); x < k; ++x)
-          while (!mbar_try_wait(bar_full + 8 * (x % NS), (x / NS) & 1) && globaltimer() - t0 < SLIM_WAIT_NS) {}
+        while (globaltimer() - t0 < SLIM_WAIT_NS / 8) {}
       }
     }
   } else {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
   }
   __syncwarp();
   tc_fence_before();
@@ -422,7 +475,8 @@ cudaError_t launch(const slim_ctx* ctx, const SlimAttn& a, int most_tiles, cudaS
   const int blocks = 1 + (int)((rows + 7) / 8 < fill ? (rows + 7) / 8 : fill);
   e = slim_launch_pdl(attn_tc_prepare_kernel<DK>, dim3(blocks), dim3(PREP_THREADS), slim_attn_plan_smem(a.batch), st, a);
   if (e != cudaSuccess) return e;
-  return slim_launch_pdl(attn_tc_kernel<DK, VH>, dim3((unsigned)most_tiles * a.H), dim3(THREADS), Shape<DK>::SMEM, st, qmap, kmap, vmap, a);
+  const long long items = (long long)most_tiles * a.H;
+  return slim_launch_pdl(attn_tc_kernel<DK, VH>, dim3((unsigned)(items < ctx->num_sms ? items : ctx->num_sms)), dim3(THREADS), Shape<DK>::SMEM, st, qmap, kmap, vmap, a);
 }
 
 }  // namespace
