@@ -315,11 +315,13 @@ slim_status slim_combine_project(slim_ctx* ctx, const float* lse_all, const floa
  *   max_k      no sequence has more keys (more: left out, SLIM_ERR_CAPACITY on the device).  With RoPE the position tables
  *              have to cover it: slim_reserve_positions, or a cache of that capacity; else SLIM_ERR_CAPACITY, nothing launched
  *   causal     1: query i attends keys 0 .. nk - nq + i; 0: all nk.  A query that attends no key gets a zero row
+ *              Not causal, with RoPE and more queries than keys, the tables have to cover nq - nk positions too (SLIM_ERR_CAPACITY
+ *              on the device, positions clamped)
  *   o          device [total_q][H][d_k], ctx dtype.  q, k, v, o 16-byte aligned and contiguous; o may not overlap the inputs
  *   workspace  device, >= slim_prompt_workspace_bytes (0 on bad arguments), 256-byte aligned; contents are scratch, shared
  *              like that of slim_tree_decode
- *   Softmax sums and weighted sums are float32; in a bf16 context rotated queries and keys are rounded to 11 bits, and the
- *   probabilities and float32 values to bf16.  A number that is not finite in a key or a value reaches the rows that attend it, and
+ *   Softmax sums and weighted sums are float32; in a bf16 context rotated queries and keys are rounded to 11 bits, the
+ *   probabilities to bf16 (beside float32 values, probabilities and values to 11 bits).  A number that is not finite in a key or a value reaches the rows that attend it, and
  *   no other.  bf16, d_k in {64, 96, 128}: tensor cores; other shapes: CUDA cores (slim_set_path chooses as for slim_decode).
  *   No weights need to be set.  total_q, total_k at most 2^29.
  *

@@ -814,7 +814,7 @@ slim_status slim_prompt_attention(slim_ctx* ctx, const void* q, const void* k, c
   a.f32 = ctx->dtype == SLIM_F32; a.v32 = v_dtype == SLIM_F32;
   a.qscale = (float)(1.4426950408889634 / std::sqrt((double)ctx->d_k));
   a.q = q; a.k = k; a.v = v; a.o = o; a.cu_q = cu_q; a.cu_k = cu_k;
-  if (ctx->rope_theta != 0.0) { a.rope_base = ctx->rope_base; a.rope_off = ctx->rope_off; }
+  if (ctx->rope_theta != 0.0) { a.rope_base = ctx->rope_base; a.rope_off = ctx->rope_off; a.rope_rows = ctx->rope_base_tiles * SLIM_TT; }
   a.status = ctx->status;
   return launched(slim_launch_attn(ctx, a, static_cast<char*>(workspace), tc, (cudaStream_t)stream));
 }

@@ -15,12 +15,12 @@ namespace {
 constexpr int THREADS = 256;
 
 // ------------------------------------------------------------------------------------------------ preparation
-// One warp a packed row: all its heads, rotated.  A query before the first key (negative position) attends nothing.
+// One warp a packed row: all its heads, rotated.
 template <bool F32>
 __device__ void rotate_row(const SlimAttn& a, int r, bool query) {
   const int lane = threadIdx.x & 31, heads = query ? a.H : a.KV;
-  const int pos = slim_attn_position(a, r, query);
-  if (pos < 0) return;
+  int pos;
+  if (!slim_attn_position(a, r, query, pos)) return;
   const size_t at = (size_t)r * heads * a.d_k;
   const void* src = query ? a.q : a.k;
   void* dst = query ? a.qr : a.kr;

@@ -16,6 +16,7 @@ struct SlimAttn {
   const int32_t* cu_k;           // [batch + 1]
   const float2* rope_base;       // position tables; NULL without rotation
   const float2* rope_off;
+  int rope_rows;                 // positions that the tables cover
   int* status;
   // workspace
   void* qr;                      // rotated queries and keys, layout of q and k: float32 (CUDA cores) or float16 (tensor cores)
@@ -55,9 +56,12 @@ __device__ __forceinline__ SlimSeq slim_attn_seq(const SlimAttn& a, int b) {
 __device__ __forceinline__ int slim_attn_keys(const SlimAttn& a, const SlimSeq& s, int i) {
   return a.causal ? max(0, min(s.nk, i + 1 + s.nk - s.nq)) : s.nk;
 }
+// (cos, sin) of a position's angle; a query in front of the first key has a negative one
 __device__ __forceinline__ float2 slim_attn_turn(const SlimAttn& a, int pos, int j) {
-  const float2 cb = __ldg(a.rope_base + (size_t)(pos / SLIM_TT) * a.half + j), co = __ldg(a.rope_off + (pos % SLIM_TT) * a.half + j);
-  return make_float2(cb.x * co.x - cb.y * co.y, cb.y * co.x + cb.x * co.y);
+  const int at = min(abs(pos), a.rope_rows - 1);
+  const float2 cb = __ldg(a.rope_base + (size_t)(at / SLIM_TT) * a.half + j), co = __ldg(a.rope_off + (at % SLIM_TT) * a.half + j);
+  const float s = cb.y * co.x + cb.x * co.y;
+  return make_float2(cb.x * co.x - cb.y * co.y, pos < 0 ? -s : s);
 }
 __device__ __forceinline__ float slim_attn_ld(const void* p, size_t i, int f32) {
   return f32 ? __ldg(reinterpret_cast<const float*>(p) + i) : __bfloat162float(__ldg(reinterpret_cast<const __nv_bfloat16*>(p) + i));

@@ -58,10 +58,12 @@ static __device__ void slim_attn_plan(const SlimAttn& a, int* s_mem) {
   }
 }
 
-// Position of packed row r among the queries (keys); -1: it belongs to no sequence.
-static __device__ int slim_attn_position(const SlimAttn& a, int r, bool query) {
+// Position of packed row r among the queries (keys); false: nothing needs the row (it belongs to no sequence, or attends nothing).
+static __device__ bool slim_attn_position(const SlimAttn& a, int r, bool query, int& pos) {
   const int32_t* cu = query ? a.cu_q : a.cu_k;
   const SlimSeq s = slim_attn_seq(a, slim_warp_find(cu, a.batch, r));
-  if (query) return r >= s.q0 && r < s.q0 + s.nq ? r - s.q0 + s.nk - s.nq : -1;
-  return r >= s.k0 && r < s.k0 + s.nk ? r - s.k0 : -1;
+  pos = query ? r - s.q0 + s.nk - s.nq : r - s.k0;
+  if (query ? r < s.q0 || r >= s.q0 + s.nq || (a.causal && pos < 0) : r < s.k0 || r >= s.k0 + s.nk) return false;
+  if (a.rope_base && pos <= -a.rope_rows) atomicMax(a.status, (int)SLIM_ERR_CAPACITY);       // (taken as the last covered one)
+  return true;
 }

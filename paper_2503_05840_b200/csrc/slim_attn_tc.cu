@@ -41,8 +41,8 @@ template <int DK>
 __device__ void prepare_row(const SlimAttn& a, int r, bool query) {
   constexpr int LPH = DK / 16, HPW = 32 / LPH;
   const int lane = threadIdx.x & 31, heads = query ? a.H : a.KV;
-  const int pos = slim_attn_position(a, r, query);
-  if (pos < 0 || lane >= LPH * HPW) return;
+  int pos;
+  if (!slim_attn_position(a, r, query, pos) || lane >= LPH * HPW) return;
   const int jl = lane % LPH, hw = lane / LPH;
   const unsigned short* src = reinterpret_cast<const unsigned short*>(query ? a.q : a.k) + (size_t)r * heads * DK + 8 * jl;
   unsigned short* dst = reinterpret_cast<unsigned short*>(query ? a.qr : a.kr) + (size_t)r * heads * DK + 8 * jl;
@@ -102,14 +102,43 @@ __global__ void __launch_bounds__(PREP_THREADS) attn_tc_prepare_kernel(const __g
 // ------------------------------------------------------------------------------------------------ attention
 constexpr int TM = 128, TN = 128;                    // rows of a query tile, keys of a key tile
 constexpr int THREADS = 384;                         // two groups of four softmax warps, MMA warp, load warp, two without work
+constexpr int SPLIT = 96;                            // keys of a tile whose probabilities are handed over first
 constexpr float TAU = 8.f;                           // log2 units by which a row's maximum may pass its reference
+
+constexpr int EMU = 2;                               // of eight pairs of exponentials so many are formed on the FMA pipe
+
+// 2^x of two arguments up to 2^6 or so without the special-function unit: x = i + f with |f| <= 1/2, the nearest integer coming from
+// the addition of 1.5 * 2^23 + 127, whose low bits then hold i + 127, the exponent of 2^i; a cubic for 2^f with the smallest
+// largest relative error on [-1/2, 1/2], 7.5e-5 (fitted by reweighted least squares).  Below -126.5 it is 0 (a masked score must
+// not meet its value with any weight), and of a NaN it is one.
+__device__ __forceinline__ void exp2_pair(f32x2 x, float& lo, float& hi) {
+  const f32x2 magic = pack2(12583039.f, 12583039.f), minus = pack2(-12583039.f, -12583039.f), neg = pack2(-1.f, -1.f);
+  float a, b;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(x));
+  asm("max.NaN.f32 %0, %0, %1;" : "+f"(a) : "f"(-127.f));
+  asm("max.NaN.f32 %0, %0, %1;" : "+f"(b) : "f"(-127.f));
+  x = pack2(a, b);
+  const f32x2 t = add2(x, magic);
+  const f32x2 f = fma2(add2(t, minus), neg, x);
+  f32x2 y = fma2(f, pack2(0.055171601474285126f, 0.055171601474285126f), pack2(0.2426111251115799f, 0.2426111251115799f));
+  y = fma2(f, y, pack2(0.6932609677314758f, 0.6932609677314758f));
+  y = fma2(f, y, pack2(0.9999280571937561f, 0.9999280571937561f));
+  uint32_t i0, i1;
+  asm("mov.b64 {%0, %1}, %2;" : "=r"(i0), "=r"(i1) : "l"(t));
+  y = mul2(y, pack2(__uint_as_float(i0 << 23), __uint_as_float(i1 << 23)));
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(y));
+}
+
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float d; asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c)); return d;
+}
 
 template <int DK>
 struct Shape {
   static constexpr int CH = (DK + 63) / 64;          // 64-column chunks of a head
   static constexpr int TILE = CH * TN * 128;         // bytes of a tile of Q, K or V
   static constexpr int NS = DK == 64 ? 8 : 5;        // ring of K and V tiles
-  static constexpr int SMEM = 1024 + (2 + NS) * TILE + 8 * (2 * NS + 9) + 32;
+  static constexpr int SMEM = 1024 + (2 + NS) * TILE + 8 * (2 * NS + 11) + 32;
 };
 
 __device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t* r) {
@@ -153,6 +182,24 @@ __device__ __forceinline__ uint32_t half2_of(float lo, float hi) {
 }
 __device__ __forceinline__ void split(f32x2 v, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v)); }
 
+// Scores LO .. HI - 1 of a row -> probabilities in 16 bits, pairs from r[LO / 2] on; l2 gathers their sum.
+template <int LO, int HI, bool VH>
+__device__ __forceinline__ void exponentials(uint32_t (&r)[TN], f32x2 scale2, f32x2 m2, f32x2& l2) {
+#pragma unroll
+  for (int x = LO; x < HI; x += 2) {
+    const f32x2 v = fma2(pack2(__uint_as_float(r[x]), __uint_as_float(r[x + 1])), scale2, m2);
+    float lo, hi;
+    if ((x / 2 * 3) % 8 < EMU) {
+      exp2_pair(v, lo, hi);
+    } else {
+      split(v, lo, hi);
+      lo = ex2_approx(lo); hi = ex2_approx(hi);
+    }
+    l2 = add2(l2, pack2(lo, hi));
+    r[x / 2] = VH ? half2_of(lo, hi) : bf162_of(lo, hi);
+  }
+}
+
 template <int DK, bool VH>
 __global__ void __launch_bounds__(THREADS, 1)
 attn_tc_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap,
@@ -170,8 +217,8 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
   const uint32_t bars = s_kv + NS * TILE;
   const uint32_t bar_full = bars, bar_empty = bars + 8 * NS, bar_q = bars + 16 * NS;
   const uint32_t bar_qe = bar_q + 8;
-  const uint32_t bar_s = bar_qe + 8, bar_p = bar_s + 16, bar_o = bar_p + 16;                 // two each
-  unsigned char* misc = sm + (bar_o + 16 - base);
+  const uint32_t bar_s = bar_qe + 8, bar_p = bar_s + 16, bar_o = bar_p + 16, bar_ph = bar_o + 16;      // two each
+  unsigned char* misc = sm + (bar_ph + 16 - base);
   uint32_t* s_tmem = reinterpret_cast<uint32_t*>(misc);
   volatile int* s_abort = reinterpret_cast<volatile int*>(misc + 4);
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -181,7 +228,7 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
     for (int i = 0; i < NS; ++i) { mbar_init(bar_full + 8 * i, 1); mbar_init(bar_empty + 8 * i, 1); }
     mbar_init(bar_q, 1);
     mbar_init(bar_qe, 1);
-    for (int i = 0; i < 2; ++i) { mbar_init(bar_s + 8 * i, 1); mbar_init(bar_p + 8 * i, 4); mbar_init(bar_o + 8 * i, 1); }
+    for (int i = 0; i < 2; ++i) { mbar_init(bar_s + 8 * i, 1); mbar_init(bar_ph + 8 * i, 4); mbar_init(bar_p + 8 * i, 4); mbar_init(bar_o + 8 * i, 1); }
     *s_abort = 0;
     fence_mbar_init();
   }
@@ -227,30 +274,28 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
       float m = -INFINITY;                            // reference, log2 units
       f32x2 l2 = pack2(0.f, 0.f);
       for (int j = 0; j < n; ++j) {
-        ok = mbar_wait<false>(bar_s + 8 * i, ps, s_abort, a.status);
+        ok = mbar_wait<false>(bar_s + 8 * i, ps, s_abort, a.status) && ok;
         ps ^= 1u;
         ok = __all_sync(0xffffffffu, ok);
         if (!ok) break;
         tc_fence_after();
-        uint32_t r[4][32];
+        uint32_t r[TN];
 #pragma unroll
-        for (int c = 0; c < 4; ++c) tmem_ld32_issue(t_s + 32 * c, r[c]);
+        for (int c = 0; c < 4; ++c) tmem_ld32_issue(t_s + 32 * c, *reinterpret_cast<uint32_t (*)[32]>(r + 32 * c));
         tmem_ld_wait();
         if (__any_sync(0xffffffffu, (j + 1) * TN > lim)) {
 #pragma unroll
-          for (int c = 0; c < 4; ++c)
-#pragma unroll
-            for (int x = 0; x < 32; ++x)
-              if (j * TN + 32 * c + x >= lim) r[c][x] = 0xff800000u;
+          for (int x = 0; x < TN; ++x)
+            if (j * TN + x >= lim) r[x] = 0xff800000u;
         }
-        float mx[4];
+        float mx[8];
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          mx[c] = __uint_as_float(r[c][0]);
+        for (int c = 0; c < 8; ++c) mx[c] = fmaxf(__uint_as_float(r[c]), __uint_as_float(r[c + 8]));
 #pragma unroll
-          for (int x = 1; x < 32; ++x) mx[c] = fmaxf(mx[c], __uint_as_float(r[c][x]));
-        }
-        const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * scale;
+        for (int x = 16; x < TN; x += 16)
+#pragma unroll
+          for (int c = 0; c < 8; ++c) mx[c] = max3(mx[c], __uint_as_float(r[x + c]), __uint_as_float(r[x + c + 8]));
+        const float top = max3(max3(mx[0], mx[1], mx[2]), max3(mx[3], mx[4], mx[5]), fmaxf(mx[6], mx[7])) * scale;
         const bool move = top > m + TAU;              // (m = -inf: the first keys of the row)
         if (__any_sync(0xffffffffu, move)) {
           const float m_new = move ? top : m;
@@ -273,21 +318,16 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
         }
         const float mm = m == -INFINITY ? 0.f : -m;
         const f32x2 m2 = pack2(mm, mm);
-#pragma unroll
-        for (int c = 0; c < 4; ++c) {
-#pragma unroll
-          for (int x = 0; x < 32; x += 2) {
-            f32x2 v = pack2(__uint_as_float(r[c][x]), __uint_as_float(r[c][x + 1]));
-            v = fma2(v, scale2, m2);
-            float lo, hi;
-            split(v, lo, hi);
-            lo = ex2_approx(lo); hi = ex2_approx(hi);
-            l2 = add2(l2, pack2(lo, hi));
-            r[c >> 1][(c & 1) * 16 + x / 2] = VH ? half2_of(lo, hi) : bf162_of(lo, hi);
-          }
-        }
-        tmem_st32(t_s, r[0]);
-        tmem_st32(t_s + 32, r[1]);
+        // P in two parts: the tensor core begins with the first three quarters while the exponentials of the last are formed
+        exponentials<0, SPLIT, VH>(r, scale2, m2, l2);
+        tmem_st32(t_s, r);
+        tmem_st16(t_s + 32, r + 32);
+        tmem_st_wait();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar_ph + 8 * i);
+        exponentials<SPLIT, TN, VH>(r, scale2, m2, l2);
+        tmem_st16(t_s + SPLIT / 2, r + SPLIT / 2);
         tmem_st_wait();
         tc_fence_before();
         __syncwarp();
@@ -381,15 +421,24 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
           const int n = i ? it.nt1 : it.nt0;
           if (j < n && ok) {
             uint32_t& pp = i ? pp1 : pp0;
-            ok = mbar_wait<false>(bar_p + 8 * i, pp, s_abort, a.status);
+            const uint64_t vd = dv + (uint64_t)(kv * (int)(TILE >> 4));
+            ok = mbar_wait<false>(bar_ph + 8 * i, pp, s_abort, a.status);
+            ok = __all_sync(0xffffffffu, ok);
+            tc_fence_after();
+            if (ok && elect_one()) {
+#pragma unroll
+              for (int x = 0; x < SPLIT / 16; ++x)
+                umma_ts(tmem + 2 * TN + i * 128, tmem + i * TN + 8 * x, vd + x * (2048 >> 4), IDESC_O, j > 0 || x > 0);
+            }
+            __syncwarp();
+            ok = mbar_wait<false>(bar_p + 8 * i, pp, s_abort, a.status) && ok;
             pp ^= 1u;
             ok = __all_sync(0xffffffffu, ok);
             tc_fence_after();
             if (ok && elect_one()) {
-              const uint64_t vd = dv + (uint64_t)(kv * (int)(TILE >> 4));
 #pragma unroll
-              for (int x = 0; x < TN / 16; ++x)
-                umma_ts(tmem + 2 * TN + i * 128, tmem + i * TN + 8 * x, vd + x * (2048 >> 4), IDESC_O, j > 0 || x > 0);
+              for (int x = SPLIT / 16; x < TN / 16; ++x)
+                umma_ts(tmem + 2 * TN + i * 128, tmem + i * TN + 8 * x, vd + x * (2048 >> 4), IDESC_O, 1u);
               if (j + 1 < n) scores(i, (uint32_t)kk);
               else umma_commit(bar_o + 8 * i);
             }

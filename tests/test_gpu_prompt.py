@@ -112,6 +112,35 @@ def test_more_queries_than_keys():
     c.close()
 
 
+@pytest.mark.parametrize("dtype,H,dk", [("bf16", 2, 128), ("bf16", 2, 40), ("f32", 2, 64)])
+def test_queries_in_front_of_the_first_key_attend_all_keys_where_not_causal(dtype, H, dk):
+    c = Case(dtype, H, H, dk, 1e4, [90, 300], [60, 17], v32=dtype == "f32", max_k=400)
+    c.check(False)
+    c.close()
+    c = Case(dtype, H, H, dk, 1e4, [300], [2], v32=dtype == "f32")         # the tables end before position -298
+    b = c.buffers()
+    c.call(b, False)
+    assert B.slim_device_status(c.ctx) == B.SLIM_ERR_CAPACITY
+    c.close()
+
+
+@pytest.mark.parametrize("H,dk,v32", [(2, 128, False), (2, 64, True), (2, 96, False)])
+def test_huge_values_in_masked_places_have_no_weight(H, dk, v32):
+    c = Case("bf16", H, H, dk, 0.0, [140, 30], [140, 30], v32=v32)
+    c.v = c.v.float()
+    c.v[3 + 100:3 + 140] = 3e38 if not v32 else 3e30       # rows that queries 0 .. 99 do not attend
+    c.v[-2:] = 3e38 if not v32 else 3e30                   # behind the last sequence
+    c.v = c.v.to(torch.float32 if v32 else torch.bfloat16)
+    b = c.buffers()
+    c.call(b, True)
+    torch.cuda.synchronize()
+    got = b["o"].double().cpu().numpy()
+    want, tol = c.reference(True)
+    rows = np.r_[0:103, 143:got.shape[0]]
+    assert (np.abs(got - want)[rows] <= tol[rows]).all()
+    c.close()
+
+
 def test_many_sequences_of_any_length():
     rng = np.random.default_rng(5)
     nq = [int(x) for x in rng.integers(0, 40, 300)]
