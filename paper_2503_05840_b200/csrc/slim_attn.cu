@@ -4,13 +4,15 @@
 //
 // Preparation (one kernel): rotated queries and keys into the workspace, each once instead of once a tile that reads them,
 // and the list of query tiles, most keys first, so that the last tiles to start are the short ones.
-// attn_kernel: one CTA a (tile of 64 query rows, head); online softmax over tiles of 64 keys, everything float32.
+// attn_kernel: one CTA a (tile of 64 or 32 query rows, head); online softmax over tiles of 64 keys, everything float32.
 #include <cuda_fp16.h>
 
 #include "slim_attn.h"
 #include "slim_attn_plan.cuh"
+#include "slim_ptx.cuh"
 
 namespace {
+using namespace slim_ptx;
 
 constexpr int THREADS = 256;
 
@@ -47,18 +49,24 @@ __global__ void __launch_bounds__(THREADS) attn_prepare_kernel(const __grid_cons
 }
 
 // ------------------------------------------------------------------------------------------------ CUDA cores
-constexpr int TR = SLIM_ATTN_ROWS, TK = 64;
-// DKP: the head width rounded up to a multiple of 64, columns behind d_k are zero.
-// Thread (ty, tx) = (tid / 16, tid % 16): rows 4 ty .. 4 ty + 3; scores of keys tx, tx + 16, ..; outputs 4 tx + 64 c.
-template <int DKP, bool F32>
-__global__ void __launch_bounds__(THREADS) attn_kernel(const __grid_constant__ SlimAttn a) {
+constexpr int TK = 64;
+// TR: query rows of a tile, 64 or 32; DKP: the head width rounded up to a multiple of 64, columns behind d_k are zero.
+// Thread (ty, tx) = (tid / 16, tid % 16) of 4 TR: rows 4 ty .. 4 ty + 3; scores of keys tx, tx + 16, ..; outputs 4 tx + 64 c.
+// Products in packed float32: even and odd columns of a score, neighbouring outputs.
+__host__ __device__ constexpr int attn_stages(int dkp) { return dkp <= 128 ? 2 : 1; }      // (two of wider ones do not fit)
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool in) {          // zeros where `in` does not hold
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(in ? 16 : 0) : "memory");
+}
+template <int DKP, int TR, bool F32>
+__global__ void __launch_bounds__(4 * TR) attn_kernel(const __grid_constant__ SlimAttn a) {
   constexpr int PQ = DKP + 4, PP = TK + 4;                       // pitches that spread rows over the banks
-  constexpr int NC = DKP / 64;
+  constexpr int NC = DKP / 64, NT = 4 * TR;
   extern __shared__ __align__(16) float smem[];
+  constexpr int ST = attn_stages(DKP), KS = TK * PQ, VS = TK * DKP;      // key tiles in shared memory
   float* s_q = smem;                                             // [TR][PQ]
-  float* s_k = s_q + TR * PQ;                                    // [TK][PQ]
-  float* s_v = s_k + TK * PQ;                                    // [TK][DKP]
-  float* s_p = s_v + TK * DKP;                                   // [TR][PP]
+  float* s_k0 = s_q + TR * PQ;                                   // [ST][TK][PQ]
+  float* s_v0 = s_k0 + ST * KS;                                  // [ST][TK][DKP]
+  float* s_p = s_v0 + ST * VS;                                   // [TR][PP]
   slim_pdl_trigger();
   slim_pdl_wait();
   const int item = blockIdx.x / a.H, h = blockIdx.x % a.H;
@@ -69,58 +77,81 @@ __global__ void __launch_bounds__(THREADS) attn_kernel(const __grid_constant__ S
   const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
   const float* qr = reinterpret_cast<const float*>(a.qr) + ((size_t)(s.q0 + row0) * a.H + h) * dk;
   const float* kr = reinterpret_cast<const float*>(a.kr) + ((size_t)s.k0 * a.KV + kvh) * dk;
-  for (int e = tid; e < TR * DKP; e += THREADS) {
+#pragma unroll 8
+  for (int e = tid; e < TR * DKP; e += NT) {
     const int r = e / DKP, c = e % DKP;
     s_q[r * PQ + c] = r < rows && c < dk ? qr[(size_t)r * a.H * dk + c] * a.qscale : 0.f;
   }
   int lim[4];
-  float m[4], l[4], acc[4][NC][4];
+  float m[4], l[4];
+  f32x2 acc[4][NC][2];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     lim[i] = slim_attn_keys(a, s, row0 + ty * 4 + i);
     m[i] = -INFINITY; l[i] = 0.f;
 #pragma unroll
-    for (int c = 0; c < NC; ++c)
-#pragma unroll
-      for (int x = 0; x < 4; ++x) acc[i][c][x] = 0.f;
+    for (int c = 0; c < NC; ++c) acc[i][c][0] = acc[i][c][1] = pack2(0.f, 0.f);
   }
   const int keys = slim_attn_keys(a, s, row0 + rows - 1);
-  for (int t0 = 0; t0 < keys; t0 += TK) {
-    __syncthreads();
-    for (int e = tid; e < TK * DKP; e += THREADS) {
-      const int r = e / DKP, c = e % DKP;
-      const bool in = t0 + r < keys && c < dk;
-      s_k[r * PQ + c] = in ? kr[(size_t)(t0 + r) * a.KV * dk + c] : 0.f;
-      s_v[r * DKP + c] = in ? slim_attn_ld(a.v, ((size_t)(s.k0 + t0 + r) * a.KV + kvh) * dk + c, a.v32) : 0.f;
+  // Key tile t0 into stage st: 16 bytes at a time behind the products of the tile before it, or element by element (d_k not a
+  // multiple of four, bf16 values)
+  const bool vec = (dk & 3) == 0 && a.v32;
+  const float* vr = reinterpret_cast<const float*>(a.v) + ((size_t)s.k0 * a.KV + kvh) * dk;
+  auto load = [&](int t0, int st) {
+    float* s_k = s_k0 + st * KS;
+    float* s_v = s_v0 + st * VS;
+    if (vec) {
+#pragma unroll 8
+      for (int e = tid; e < TK * DKP / 4; e += NT) {
+        const int r = e / (DKP / 4), c = e % (DKP / 4) * 4;
+        const bool in = t0 + r < keys && c < dk;
+        const size_t at = in ? (size_t)(t0 + r) * a.KV * dk + c : 0;
+        cp_async16(smem_u32(s_k + r * PQ + c), kr + at, in);
+        cp_async16(smem_u32(s_v + r * DKP + c), vr + at, in);
+      }
+    } else {
+#pragma unroll 8
+      for (int e = tid; e < TK * DKP; e += NT) {
+        const int r = e / DKP, c = e % DKP;
+        const bool in = t0 + r < keys && c < dk;
+        s_k[r * PQ + c] = in ? kr[(size_t)(t0 + r) * a.KV * dk + c] : 0.f;
+        s_v[r * DKP + c] = in ? slim_attn_ld(a.v, ((size_t)(s.k0 + t0 + r) * a.KV + kvh) * dk + c, a.v32) : 0.f;
+      }
     }
-    __syncthreads();
-    float sv[4][4];
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+  if (keys > 0) load(0, 0);
+  int st = 0;
+  for (int t0 = 0; t0 < keys; t0 += TK) {
+    asm volatile("cp.async.wait_group 0;" ::: "memory");
+    __syncthreads();                                             // this tile is there, and nobody reads the one before it any more
+    const float* s_k = s_k0 + st * KS;
+    const float* s_v = s_v0 + st * VS;
+    if (ST == 2 && t0 + TK < keys) load(t0 + TK, st ^ 1);
+    f32x2 sv2[4][4];
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) sv[i][j] = 0.f;
+      for (int j = 0; j < 4; ++j) sv2[i][j] = pack2(0.f, 0.f);
 #pragma unroll 4
     for (int c = 0; c < DKP; c += 4) {
-      float4 qv[4], kv[4];
+      ulonglong2 qv[4], kv[4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) qv[i] = *reinterpret_cast<const float4*>(s_q + (ty * 4 + i) * PQ + c);
+      for (int i = 0; i < 4; ++i) qv[i] = *reinterpret_cast<const ulonglong2*>(s_q + (ty * 4 + i) * PQ + c);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) kv[j] = *reinterpret_cast<const float4*>(s_k + (tx + 16 * j) * PQ + c);
+      for (int j = 0; j < 4; ++j) kv[j] = *reinterpret_cast<const ulonglong2*>(s_k + (tx + 16 * j) * PQ + c);
 #pragma unroll
       for (int i = 0; i < 4; ++i)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          sv[i][j] = fmaf(qv[i].x, kv[j].x, sv[i][j]); sv[i][j] = fmaf(qv[i].y, kv[j].y, sv[i][j]);
-          sv[i][j] = fmaf(qv[i].z, kv[j].z, sv[i][j]); sv[i][j] = fmaf(qv[i].w, kv[j].w, sv[i][j]);
-        }
+        for (int j = 0; j < 4; ++j) sv2[i][j] = fma2(qv[i].y, kv[j].y, fma2(qv[i].x, kv[j].x, sv2[i][j]));
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      float mx = m[i];
+      float mx = m[i], sv[4];
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        if (t0 + tx + 16 * j >= lim[i]) sv[i][j] = -INFINITY;
-        mx = fmaxf(mx, sv[i][j]);
+        sv[j] = t0 + tx + 16 * j >= lim[i] ? -INFINITY : sum2(sv2[i][j]);
+        mx = fmaxf(mx, sv[j]);
       }
 #pragma unroll
       for (int o = 8; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
@@ -128,7 +159,7 @@ __global__ void __launch_bounds__(THREADS) attn_kernel(const __grid_constant__ S
       float ps = 0.f;
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const float p = t0 + tx + 16 * j >= lim[i] ? 0.f : exp2f(sv[i][j] - mx);
+        const float p = t0 + tx + 16 * j >= lim[i] ? 0.f : exp2f(sv[j] - mx);
         s_p[(ty * 4 + i) * PP + tx + 16 * j] = p;
         ps += p;
       }
@@ -136,10 +167,9 @@ __global__ void __launch_bounds__(THREADS) attn_kernel(const __grid_constant__ S
       for (int o = 8; o > 0; o >>= 1) ps += __shfl_xor_sync(0xffffffffu, ps, o);
       l[i] = l[i] * alpha + ps;
       m[i] = mx;
+      const f32x2 al = pack2(alpha, alpha);
 #pragma unroll
-      for (int c = 0; c < NC; ++c)
-#pragma unroll
-        for (int x = 0; x < 4; ++x) acc[i][c][x] *= alpha;
+      for (int c = 0; c < NC; ++c) { acc[i][c][0] = mul2(acc[i][c][0], al); acc[i][c][1] = mul2(acc[i][c][1], al); }
     }
     __syncwarp();                                                // a row's probabilities come from its own half warp
 #pragma unroll 2
@@ -154,13 +184,20 @@ __global__ void __launch_bounds__(THREADS) attn_kernel(const __grid_constant__ S
       for (int u = 0; u < 4; ++u)
 #pragma unroll
         for (int c = 0; c < NC; ++c) {
-          const float4 v = *reinterpret_cast<const float4*>(s_v + (t + u) * DKP + c * 64 + tx * 4);
+          const ulonglong2 v = *reinterpret_cast<const ulonglong2*>(s_v + (t + u) * DKP + c * 64 + tx * 4);
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            acc[i][c][0] = fmaf(pv[i][u], v.x, acc[i][c][0]); acc[i][c][1] = fmaf(pv[i][u], v.y, acc[i][c][1]);
-            acc[i][c][2] = fmaf(pv[i][u], v.z, acc[i][c][2]); acc[i][c][3] = fmaf(pv[i][u], v.w, acc[i][c][3]);
+            const f32x2 pp = pack2(pv[i][u], pv[i][u]);
+            acc[i][c][0] = fma2(pp, v.x, acc[i][c][0]);
+            acc[i][c][1] = fma2(pp, v.y, acc[i][c][1]);
           }
         }
+    }
+    if (ST == 2) {
+      st ^= 1;
+    } else if (t0 + TK < keys) {
+      __syncthreads();
+      load(t0 + TK, 0);
     }
   }
   bool bad[4];
@@ -176,7 +213,9 @@ __global__ void __launch_bounds__(THREADS) attn_kernel(const __grid_constant__ S
 #pragma unroll
       for (int x = 0; x < 4; ++x) {
         const int col = c * 64 + tx * 4 + x;
-        const float y = lim[i] > 0 ? acc[i][c][x] * inv : 0.f;
+        float lo, hi;
+        asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(acc[i][c][x >> 1]));
+        const float y = lim[i] > 0 ? (x & 1 ? hi : lo) * inv : 0.f;
         if (col < dk) {
           bad[i] |= !(fabsf(y) <= 3.4028234663852886e38f);
           if (F32) reinterpret_cast<float*>(a.o)[at + col] = y;
@@ -195,14 +234,16 @@ __global__ void __launch_bounds__(THREADS) attn_kernel(const __grid_constant__ S
   }
 }
 
-template <int DKP>
-cudaError_t launch_attn(const SlimAttn& a, int most_tiles, cudaStream_t st) {
-  const size_t smem = sizeof(float) * (TR * (DKP + 4) + TK * (DKP + 4) + TK * DKP + TR * (TK + 4));
-  auto kern = a.f32 ? attn_kernel<DKP, true> : attn_kernel<DKP, false>;
+template <int DKP, int TR>
+cudaError_t launch_attn(const SlimAttn& a, cudaStream_t st) {
+  const size_t smem = sizeof(float) * (TR * (DKP + 4) + attn_stages(DKP) * (TK * (DKP + 4) + TK * DKP) + TR * (TK + 4));
+  auto kern = a.f32 ? attn_kernel<DKP, TR, true> : attn_kernel<DKP, TR, false>;
   cudaError_t e = cudaFuncSetAttribute((const void*)kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
   if (e != cudaSuccess) return e;
-  return slim_launch_pdl(kern, dim3((unsigned)(most_tiles * a.H)), dim3(THREADS), smem, st, a);
+  return slim_launch_pdl(kern, dim3((unsigned)(a.most_tiles * a.H)), dim3(4 * TR), smem, st, a);
 }
+template <int DKP>
+cudaError_t launch_attn(const SlimAttn& a, cudaStream_t st) { return a.tile_rows == 32 ? launch_attn<DKP, 32>(a, st) : launch_attn<DKP, 64>(a, st); }
 
 inline size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
@@ -214,7 +255,7 @@ SlimAttnLayout slim_attn_layout(const slim_ctx* ctx, int kv_heads, int batch, in
   L.qr = off; off = align256(off + 4 * (size_t)total_q * ctx->d);
   L.kr = off; off = align256(off + 4 * (size_t)total_k * kv_heads * ctx->d_k);
   L.vb = off; off = align256(off + (slim_attn_tc_ok(ctx) ? 2 * (size_t)total_k * kv_heads * ctx->d_k : 0));
-  L.tiles = off; off = align256(off + 2 * sizeof(int4) * ((size_t)total_q / SLIM_ATTN_ROWS + batch + 1));
+  L.tiles = off; off = align256(off + 2 * sizeof(int4) * ((size_t)total_q / 32 + batch + 1));
   L.n_tiles = off; off = align256(off + sizeof(int));
   L.total = off;
   return L;
@@ -226,15 +267,16 @@ cudaError_t slim_launch_attn(const slim_ctx* ctx, SlimAttn a, char* ws, int tc, 
   a.tiles = reinterpret_cast<int4*>(ws + L.tiles);
   a.n_tiles = reinterpret_cast<int*>(ws + L.n_tiles);
   tc = tc && a.total_k > 0;                              // (a tensor map needs a row)
-  a.tile_rows = tc ? SLIM_ATTN_TC_ROWS : SLIM_ATTN_ROWS;
-  const int most = a.most_tiles = a.total_q / a.tile_rows + a.batch;
-  if (tc) return slim_launch_attn_tc(ctx, a, most, st);
+  // Tiles of 32 query rows where those of 64 would not give every SM one (one sequence of 448 tokens, 6 heads, float32:
+  // the attention kernel 33 us instead of 58).
+  a.tile_rows = tc ? SLIM_ATTN_TC_ROWS : (long long)(a.total_q / 64 + a.batch) * a.H < ctx->num_sms ? 32 : 64;
+  a.most_tiles = a.total_q / a.tile_rows + a.batch;
+  if (tc) return slim_launch_attn_tc(ctx, a, a.most_tiles, st);
   const int rows = a.total_q + a.total_k;
   const int blocks = 1 + (int)((rows + 7ll) / 8 < 8ll * ctx->num_sms ? (rows + 7ll) / 8 : 8ll * ctx->num_sms);
   const size_t smem = slim_attn_plan_smem(a.batch);
   cudaError_t e = a.f32 ? slim_launch_pdl(attn_prepare_kernel<true>, dim3(blocks), dim3(THREADS), smem, st, a)
                         : slim_launch_pdl(attn_prepare_kernel<false>, dim3(blocks), dim3(THREADS), smem, st, a);
   if (e != cudaSuccess) return e;
-  return a.d_k <= 64 ? launch_attn<64>(a, most, st) : a.d_k <= 128 ? launch_attn<128>(a, most, st)
-         : a.d_k <= 192 ? launch_attn<192>(a, most, st) : launch_attn<256>(a, most, st);
+  return a.d_k <= 64 ? launch_attn<64>(a, st) : a.d_k <= 128 ? launch_attn<128>(a, st) : a.d_k <= 192 ? launch_attn<192>(a, st) : launch_attn<256>(a, st);
 }

@@ -29,8 +29,7 @@ struct SlimAttn {
 
 struct SlimAttnLayout { size_t qr, kr, vb, tiles, n_tiles, total; };
 
-constexpr int SLIM_ATTN_ROWS = 64;       // query rows of a tile, CUDA cores
-constexpr int SLIM_ATTN_TC_ROWS = 256;   // tensor cores: two tiles of 128
+constexpr int SLIM_ATTN_TC_ROWS = 256;   // query rows of an item on the tensor cores: two tiles of 128
 
 int slim_attn_tc_ok(const slim_ctx* ctx);
 cudaError_t slim_launch_attn_tc(const slim_ctx* ctx, const SlimAttn& a, int most_tiles, cudaStream_t st);
