@@ -268,7 +268,7 @@ cudaError_t slim_launch_attn(const slim_ctx* ctx, SlimAttn a, char* ws, int tc, 
   a.n_tiles = reinterpret_cast<int*>(ws + L.n_tiles);
   tc = tc && a.total_k > 0;                              // (a tensor map needs a row)
   // Tiles of 32 query rows where those of 64 would not give every SM one (one sequence of 448 tokens, 6 heads, float32:
-  // the attention kernel 33 us instead of 58).
+  // the attention kernel 29 us instead of 40).
   a.tile_rows = tc ? SLIM_ATTN_TC_ROWS : (long long)(a.total_q / 64 + a.batch) * a.H < ctx->num_sms ? 32 : 64;
   a.most_tiles = a.total_q / a.tile_rows + a.batch;
   if (tc) return slim_launch_attn_tc(ctx, a, a.most_tiles, st);

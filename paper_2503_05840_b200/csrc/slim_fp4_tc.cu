@@ -211,7 +211,7 @@ __global__ void __launch_bounds__(MAXT, 1) fp4_tc_kernel(const __grid_constant__
       // sums the score of row gr + 8 (j & 1) under head hd0 + (j >> 1), and no score has to move.
       const uint32_t q_rd = q_own + (uint32_t)((HPW == 2 ? gr >> 2 : 0) * HB + (((gr & 3) >> 1) * 4 + j) * SB);
       const int mine = HPW == 2 ? j >> 1 : 0, odd = j & 1;                   // the thread's head and row half
-      const bool scores = HPW == 2 || j < 2;
+      const bool scores = HPW == 2 || j < 2, speaks = scores && gr == 0 && odd == 0;      // (one thread a head)
       const uint32_t p_off = (uint32_t)(((hd0 + mine) & 7) * 16 + ((hd0 + mine) >> 3) * 256 + odd * 128 + gr * 2);
       // Queries: lane l has pairs 2 l, 2 l + 1 of a head, for the thread and step that read them
       const bool live = lane < HALF / 2;
@@ -401,17 +401,15 @@ __global__ void __launch_bounds__(MAXT, 1) fp4_tc_kernel(const __grid_constant__
                 for (int o = 1; o < 32; o = o == 1 ? 4 : 2 * o) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
                 mref = mx + BIAS;
                 if (g.sets == 2) {
-                  if (lane == 0) {
-                    s_xm[hd0] = mref;
-                    mbar_arrive(b_xm);
-                  }
+                  if (speaks) s_xm[hd0 + mine] = mref;
                   __syncwarp();
+                  if (lane == 0) mbar_arrive(b_xm);
                 }
               } else {
                 ok = mbar_wait<false>(b_xm, uc & 1, s_abort, p.status);
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
-                mref = s_xm[hd0];
+                mref = s_xm[hd0 + mine];
               }
               if (!(mref > -INFINITY)) mref = 0.f;                     // nothing but NaN so far
             }
@@ -451,20 +449,18 @@ __global__ void __launch_bounds__(MAXT, 1) fp4_tc_kernel(const __grid_constant__
               ok = mbar_wait<false>(b_xl, uc & 1, s_abort, p.status);
               ok = __all_sync(0xffffffffu, ok);
               if (!ok) break;
-              lsum += s_xl[hd0];
-              rmax = fmaxf(rmax, s_xx[hd0]);
+              lsum += s_xl[hd0 + mine];
+              rmax = fmaxf(rmax, s_xx[hd0 + mine]);
             } else {
               ok = mbar_wait<false>(b_xm, uc & 1, s_abort, p.status);
               ok = __all_sync(0xffffffffu, ok);
               if (!ok) break;
-              if (lane == 0) {
-                s_xl[hd0] = lsum; s_xx[hd0] = rmax;
-                mbar_arrive(b_xl);
-              }
+              if (speaks) { s_xl[hd0 + mine] = lsum; s_xx[hd0 + mine] = rmax; }
               __syncwarp();
+              if (lane == 0) mbar_arrive(b_xl);
             }
           }
-          if (owner && scores && gr == 0 && odd == 0) {
+          if (owner && speaks) {
             const size_t at = (size_t)unit * p.H + (int)rank * g.hl + hd0 + mine;
             p.part_m[at] = mref;
             p.part_l[at] = lsum;
@@ -613,9 +609,10 @@ int threads_of(const Geom& g) { return 32 * (g.nswl + 2); }
 bool make_geom(int d, int H, int d_k, int batch, Geom& g) {
   if ((d_k != 64 && d_k != 96 && d_k != 128) || (H & 1) || H < 2 || H > 32 || d % 256 || d > 4096) return false;
   g.dsl = d / 2; g.hl = H / 2; g.nch = g.dsl / 128;
-  // More than ten heads: two a warp (a tile's fixed steps are then shared by two heads, and a thread has the registers for it).
-  // Up to ten: one a warp, in two sets that take the tiles in turn, since a small tile is bound by its chain of steps.
-  g.hpw = g.hl > 10 && g.hl % 2 == 0 ? 2 : 1;
+  // Two heads a warp where their number is even: a tile's fixed steps are shared by them.  Up to ten heads the warps come in two
+  // sets that take the tiles in turn, since a small tile is bound by its chain of steps (more do not leave a thread the
+  // registers for it).  64 x 1500 rows of 1280: the call 89 us with one head a warp, 81 with two.
+  g.hpw = g.hl % 2 == 0 ? 2 : 1;
   g.nsw = g.hl / g.hpw;
   g.sets = g.hl > 10 ? 1 : 2;
   g.nswl = g.nsw * g.sets < 4 ? 4 : g.nsw * g.sets;
