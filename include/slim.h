@@ -300,9 +300,9 @@ slim_status slim_combine_project(slim_ctx* ctx, const float* lse_all, const floa
 /* ---- Prompts of several sequences, packed ------------------------------------------------------
  * (Eq. 4 and 5 for a whole prompt, Fig. 3(a): the values are formed once from the keys, the attention is the usual one.)
  * Sequences of different lengths lie one behind another in one array; cu_* (device int32 [batch + 1]) says where each
- * begins, sequence b being rows cu[b] .. cu[b + 1] - 1.  Starts that do not ascend from 0 or more to the array's rows raise SLIM_ERR_CAPACITY
- * on the device, and the sequences that they bound are left out.  Rows in front of the first and behind the last sequence are
- * neither read nor written.
+ * begins, sequence b being rows cu[b] .. cu[b + 1] - 1.  Starts that do not ascend from 0 or more to the array's rows raise
+ * SLIM_ERR_CAPACITY on the device; the sequences that they bound are left out, in whole or in part, and nothing outside the
+ * arrays is touched.  Rows in front of the first and behind the last sequence may hold anything and are not written.
  *     slim_prompt_attention (values from slim_prefill or slim_values_from_keys)  and  slim_append_rows;
  *     for the next chunk of a prompt: slim_read_rows gives the keys that are cached, slim_values_from_keys their values
  *
@@ -321,16 +321,16 @@ slim_status slim_combine_project(slim_ctx* ctx, const float* lse_all, const floa
  *   workspace  device, >= slim_prompt_workspace_bytes (0 on bad arguments), 256-byte aligned; contents are scratch, shared
  *              like that of slim_tree_decode
  *   Softmax sums and weighted sums are float32; in a bf16 context rotated queries and keys are rounded to 11 bits, the
- *   probabilities to bf16 (beside float32 values, probabilities and values to 11 bits).  A number that is not finite in a key or a value reaches the rows that attend it, and
- *   no other.  bf16, d_k in {64, 96, 128}: tensor cores; other shapes: CUDA cores (slim_set_path chooses as for slim_decode).
- *   No weights need to be set.  total_q, total_k at most 2^29.
+ *   probabilities to bf16 (beside float32 values, probabilities and values to 11 bits).  A number that is not finite in a key or
+ *   a value reaches the rows that attend it, and no other.  bf16, d_k in {64, 96, 128}: tensor cores; other shapes: CUDA cores (slim_set_path chooses as for slim_decode).
+ *   No weights need to be set.  total_q from 1, total_k from 0 (k, v may then be NULL), both at most 2^29.
  *
  * slim_append_rows  packed rows k_new [total][d] (device, ctx dtype, un-rotated) into the cache: the rows of sequence b go to cache
  *   rows positions[b], positions[b] + 1, ..  A sequence whose rows would pass t_cap is left unwritten (SLIM_ERR_CAPACITY); a row on
  *   a page outside the pool likewise.  A 4-bit cache quantises them.
  * slim_read_rows    the inverse: those cache rows as they are stored, to k_out [total][d] (device, ctx dtype; a 4-bit cache's
  *   keys are exact in bf16); rows that cannot be read are left as they were.
- *   Both: f32, bf16 and 4-bit caches, contiguous or paged (not SLIM_FP8: SLIM_ERR_UNSUPPORTED); cu_rows[batch] <= total <= 2^30. */
+ *   Both: f32, bf16 and 4-bit caches, contiguous or paged (not SLIM_FP8: SLIM_ERR_UNSUPPORTED); cu_rows[batch] <= total, 1 <= total <= 2^30. */
 size_t      slim_prompt_workspace_bytes(const slim_ctx* ctx, int kv_heads, int batch, int total_q, int total_k);
 slim_status slim_prompt_attention(slim_ctx* ctx, const void* q, const void* k, const void* v, int v_dtype, int kv_heads,
                                   const int32_t* cu_q, const int32_t* cu_k, int batch, int total_q, int total_k, int max_k,
@@ -411,7 +411,7 @@ slim_status slim_tree_commit(slim_ctx* ctx, slim_cache* cache, const void* k_tre
  * slim_accumulate_weights  acc[b][t] += sum_h softmax_t(q_h . K_h / sqrt(d_k)), t < lengths[b], for the query of
  *   slim_decode (un-rotated, at position lengths[b]-1; same arguments).  acc: device float32 [batch][t_cap],
  *   other elements are left alone.  A NaN in an attended row or in the query makes every acc of its sequence NaN.  Any
- *   cache of keys that slim_decode takes.  workspace: device, >= slim_weights_workspace_bytes(ctx, batch, t_cap), 256-byte
+ *   cache of keys that slim_decode takes, but SLIM_FP4 (SLIM_ERR_UNSUPPORTED).  workspace: device, >= slim_weights_workspace_bytes(ctx, batch, t_cap), 256-byte
  *   aligned.
  *
  * slim_evict  brings every sequence that is longer than `budget` rows down to it: the last `recent` rows stay
@@ -419,7 +419,7 @@ slim_status slim_tree_commit(slim_ctx* ctx, slim_cache* cache, const void* k_tre
  *   lower row; NaN counts as the lowest value).  The kept rows move, in order, to rows 0 .. budget-1, in place; their
  *   acc moves along and the acc of the rows that became free is cleared.  Keys are cached un-rotated, so a
  *   row that moved sits at its new position from then on.  The caller clamps lengths to the budget
- *   after the last layer.  Shorter sequences stay as they are.  Any cache of the library (a paged one
+ *   after the last layer.  Shorter sequences stay as they are.  Any cache of the library but SLIM_FP4 (a paged one
  *   keeps its block table; the pages behind the budget are free to be given back).  Rows move in place: a sequence that
  *   is brought down must not share a page with another one, whose rows would change with it.
  *   A page id outside the pool raises SLIM_ERR_CAPACITY; the rows on that page do not move.

@@ -650,7 +650,7 @@ bool make_geom(int d, int H, int d_k, int batch, Geom& g) {
 typedef void (*kernel_t)(const CUtensorMap, const CUtensorMap, const SlimDecodeParams, const Geom, float*);
 template <int DK, bool ROPE>
 kernel_t pick_heads(const Geom& g) {
-  return g.hpw == 2 ? fp4_tc_kernel<DK, ROPE, 2, 384> : threads_of(g) <= 640 ? fp4_tc_kernel<DK, ROPE, 1, 640> : fp4_tc_kernel<DK, ROPE, 1, 768>;
+  return g.hpw == 2 ? fp4_tc_kernel<DK, ROPE, 2, 384> : fp4_tc_kernel<DK, ROPE, 1, 640>;      // (most warps: 10 and 18, and two)
 }
 kernel_t pick(int d_k, bool rope, const Geom& g) {
   if (d_k == 64) return rope ? pick_heads<64, true>(g) : pick_heads<64, false>(g);

@@ -16,7 +16,7 @@ def _device(device) -> torch.device:
 
 
 class Scratch:
-    """Device memory of SlimLayer.tree_decode, accumulate_weights and evict.  Layers whose calls run one after another on a
+    """Device memory of SlimLayer.prompt_attention, tree_decode, accumulate_weights and evict.  Layers whose calls run one after another on a
     stream may share one.  It grows with the largest call so far; what it grew out of is given back, unless a graph has been
     captured on it."""
 

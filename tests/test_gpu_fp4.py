@@ -413,3 +413,90 @@ def test_rows_on_two_streams():
     want = torch.from_numpy(po.fp4_values(*po.fp4_quantise(x[::50].double().cpu().numpy())))
     assert torch.equal(got[::50].double().cpu(), want)
     layer.close()
+
+
+# one to sixteen heads a CTA: one or two a warp, one or two sets of warps
+HEADS = [(256, 2, 128, 0.0), (1280, 10, 128, 1e4), (2304, 18, 128, 1e6), (2560, 20, 128, 1e4), (2816, 22, 128, 1e4), (2304, 24, 96, 1e4),
+         (3584, 28, 128, 1e4), (3840, 30, 128, 0.0), (1792, 28, 64, 1e4), (2048, 32, 64, 0.0)]
+
+
+@pytest.mark.parametrize("d,H,d_k,theta", HEADS)
+def test_decode_head_counts(d, H, d_k, theta):
+    lengths = [1, 200, 16, 95, 0, 31]
+    layer, q, Ks, W = _decode_case(d, H, d_k, theta, lengths, 203, H)
+    _check(layer, q, Ks, W, H, theta, lengths)
+    layer.close()
+
+
+@pytest.mark.parametrize("d,H,d_k,theta", HEADS[::2] + [(4096, 32, 128, 1e6)])
+def test_scores_run_away_in_some_units(d, H, d_k, theta):
+    """Keys that repeat the query late in a sequence: the units that hold them are walked twice, their neighbours once."""
+    lengths = [300, 40, 700, 3]
+    layer, q, _, W = _decode_case(d, H, d_k, theta, lengths, 704, 5)
+    x = _keys(700, d, 8, wide=False).float()
+    at = [150, 151, 290, 420, 699]
+    for i, t in enumerate(at):
+        qt = po.turned(q[2].double().numpy().reshape(1, H, d_k), [lengths[2] - 1 - t], theta)[0]      # meets the query turned by its distance
+        x[t] = torch.from_numpy(qt.reshape(-1)).float() * (1 + i)
+    layer.append_rows(x.bfloat16().to(DEV), _i32([0] * 4), _i32([0, 0, 0, 700, 700]))
+    K = layer.read_rows(_i32([0] * 4), _i32(_starts(lengths)), sum(lengths)).double().cpu().numpy()
+    s = _starts(lengths)
+    _check(layer, q, [K[a:b] for a, b in zip(s[:-1], s[1:])], W, H, theta, lengths)
+    layer.close()
+
+
+def test_more_sequences_than_workers():
+    lengths = [(7 * i) % 50 for i in range(400)]
+    layer, q, Ks, W = _decode_case(512, 4, 128, 1e4, lengths, 50, 1)
+    _check(layer, q, Ks, W, 4, 1e4, lengths)
+    layer.close()
+
+
+@pytest.mark.parametrize("d,H,d_k", [(512, 4, 128), (250, 5, 50)])
+def test_lengths_beyond_the_cache_are_clamped(d, H, d_k):
+    layer, q, Ks, W = _decode_case(d, H, d_k, 1e4, [40, 40], 40, 4)
+    want = layer.decode_typed(q.to(DEV), _i32([40, 0]))
+    kept = layer.k.clone()
+    got = layer.decode_typed(q.to(DEV), _i32([41, -7]), k_new=_keys(2, d, 1).to(DEV))
+    assert layer.device_status() == B.SLIM_ERR_CAPACITY
+    assert torch.equal(got, want) and torch.equal(layer.k, kept) and not got[1].any()
+    layer.close()
+
+
+def test_two_steps_at_once():
+    """Two caches of one context on two streams, each with its own workspace."""
+    layer, q, Ks, W = _decode_case(1024, 8, 128, 1e4, [900, 33], 1000, 6)
+    other = torch.empty_like(layer.k).copy_(layer.k)
+    cache = B.slim_cache_create(layer.ctx, other, 2, 1000)
+    ws, o = torch.empty_like(layer.workspace), torch.empty(2, 1024, dtype=torch.bfloat16, device=DEV)
+    qd, lens, l2 = q.to(DEV), _i32([900, 33]), _i32([17, 500])
+    want, want2 = layer.decode_typed(qd, lens).clone(), layer.decode_typed(qd, l2).clone()
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    for _ in range(5):
+        got = layer.decode_typed(qd, lens)
+        B.slim_decode_typed(layer.ctx, qd, None, cache, l2, o, B.SLIM_BF16, ws, s.cuda_stream)
+        torch.cuda.synchronize()
+        assert torch.equal(got, want) and torch.equal(o, want2)
+    B.slim_cache_destroy(cache)
+    layer.close()
+
+
+@pytest.mark.parametrize("d,H,t_cap", [(4096, 32, 2200003), (16384, 64, 300007)])
+def test_offsets_beyond_32_bits(d, H, t_cap):
+    """The second sequence's last rows lie more than 2^32 bytes into the storage."""
+    layer = SlimLayer(d, H, d // H, 0.0, "fp4", 2, t_cap, DEV)
+    x = _keys(50, d, 3, wide=False).to(DEV)
+    layer.append_rows(x, _i32([0, 0]), _i32([0, 0, 50]))
+    layer.append_rows(x[:3], _i32([0, t_cap - 3]), _i32([0, 0, 3]))
+    both = torch.cat([layer.read_rows(_i32([0, 0]), _i32([0, 0, 50]), 50), layer.read_rows(_i32([0, t_cap - 3]), _i32([0, 0, 3]), 3)])
+    assert layer.device_status() == B.SLIM_OK
+    want = torch.from_numpy(po.fp4_values(*po.fp4_quantise(x.double().cpu().numpy())))
+    assert torch.equal(both.double().cpu(), torch.cat([want, want[:3]]))
+    if d == 4096:
+        g = torch.Generator().manual_seed(3)
+        W = (torch.randn(d, d, generator=g) / d ** 0.5).bfloat16().float().numpy().astype(np.float64)
+        layer.set_wkv(W)
+        q = torch.randn(2, d, generator=g).bfloat16()
+        _check(layer, q, [want.numpy()[:0], want.numpy()], W, H, 0.0, [0, 50])
+    layer.close()

@@ -297,3 +297,32 @@ def test_paths_agree():
     want, tol = c.reference(True)
     assert (np.abs(a - b) <= 2 * tol).all()
     c.close()
+
+
+def test_offsets_beyond_32_bits():
+    """More than 2^31 elements, 2^32 bytes, of queries and outputs: the last sequence is checked."""
+    H, dk, n, last = 32, 128, 4096, 77
+    seqs = 2 ** 31 // (H * dk) // n + 1
+    total = seqs * n + last
+    ctx = B.slim_create(H * dk, H, dk, 1e4, B.SLIM_BF16)
+    B.slim_reserve_positions(ctx, n)
+    g = torch.Generator(device=DEV).manual_seed(1)
+    q = torch.empty(total, H, dk, dtype=torch.bfloat16, device=DEV).normal_(generator=g)
+    k, v = (torch.empty(total, 1, dk, dtype=torch.bfloat16, device=DEV).normal_(generator=g) for _ in range(2))
+    cu = torch.tensor([i * n for i in range(seqs + 1)] + [total], dtype=torch.int32, device=DEV)
+    few = torch.zeros(seqs + 2, dtype=torch.int32, device=DEV)         # only the last two sequences have queries
+    few[:] = cu
+    few[:seqs] = cu[seqs - 1]
+    o = torch.empty_like(q)
+    ws = torch.empty(B.slim_prompt_workspace_bytes(ctx, 1, seqs + 1, total, total), dtype=torch.uint8, device=DEV)
+    B.slim_prompt_attention(ctx, q, k, v, B.SLIM_BF16, 1, few, cu, seqs + 1, total, total, n, True, o, ws, torch.cuda.current_stream().cuda_stream)
+    torch.cuda.synchronize()
+    assert B.slim_device_status(ctx) == B.SLIM_OK
+    got = o[-last:].double().cpu().numpy()
+    alone = torch.empty(last, H, dk, dtype=torch.bfloat16, device=DEV)
+    cu1 = torch.tensor([0, last], dtype=torch.int32, device=DEV)
+    B.slim_prompt_attention(ctx, q[-last:].clone(), k[-last:].clone(), v[-last:].clone(), B.SLIM_BF16, 1, cu1, cu1, 1, last, last, last, True, alone, ws,
+                            torch.cuda.current_stream().cuda_stream)
+    torch.cuda.synchronize()
+    assert np.array_equal(got, alone.double().cpu().numpy())
+    B.slim_destroy(ctx)
