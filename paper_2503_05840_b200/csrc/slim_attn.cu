@@ -27,7 +27,7 @@ __device__ void rotate_row(const SlimAttn& a, int r, bool query) {
   const void* src = query ? a.q : a.k;
   void* dst = query ? a.qr : a.kr;
   for (int j = lane; j < a.half; j += 32) {
-    const float2 cs = a.rope_base ? slim_attn_turn(a, pos, j) : make_float2(1.f, 0.f);
+    const float2 cs = a.rope_base ? slim_attn_turn(a, pos, j) : make_float2(1.f, 0.f);      // (bf16 rows are widened all the same)
     for (int h = 0; h < heads; ++h) {
       const size_t i = at + (size_t)h * a.d_k + j;
       const float x1 = slim_attn_ld(src, i, F32), x2 = slim_attn_ld(src, i + a.half, F32);
@@ -43,7 +43,7 @@ __global__ void __launch_bounds__(THREADS) attn_prepare_kernel(const __grid_cons
   slim_pdl_trigger();
   slim_pdl_wait();
   if (blockIdx.x == 0) { slim_attn_plan(a, s_mem); return; }
-  const int warps = (gridDim.x - 1) * (THREADS / 32);
+  const int warps = (gridDim.x - 1) * (THREADS / 32);                  // (none where the inputs are read where they lie)
   for (int r = (blockIdx.x - 1) * (THREADS / 32) + (threadIdx.x >> 5); r < a.total_q + a.total_k; r += warps)
     rotate_row<F32>(a, r < a.total_q ? r : r - a.total_q, r < a.total_q);
 }
@@ -58,9 +58,9 @@ __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool i
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(in ? 16 : 0) : "memory");
 }
 template <int DKP, int TR, bool F32>
-__global__ void __launch_bounds__(4 * TR) attn_kernel(const __grid_constant__ SlimAttn a) {
+__global__ void __launch_bounds__(THREADS) attn_kernel(const __grid_constant__ SlimAttn a) {
   constexpr int PQ = DKP + 4, PP = TK + 4;                       // pitches that spread rows over the banks
-  constexpr int NC = DKP / 64, NT = 4 * TR;
+  constexpr int NC = DKP / 64, NT = THREADS, RT = 16 * TR / NT;
   extern __shared__ __align__(16) float smem[];
   constexpr int ST = attn_stages(DKP), KS = TK * PQ, VS = TK * DKP;      // key tiles in shared memory
   float* s_q = smem;                                             // [TR][PQ]
@@ -82,12 +82,12 @@ __global__ void __launch_bounds__(4 * TR) attn_kernel(const __grid_constant__ Sl
     const int r = e / DKP, c = e % DKP;
     s_q[r * PQ + c] = r < rows && c < dk ? qr[(size_t)r * a.H * dk + c] * a.qscale : 0.f;
   }
-  int lim[4];
-  float m[4], l[4];
-  f32x2 acc[4][NC][2];
+  int lim[RT];
+  float m[RT], l[RT];
+  f32x2 acc[RT][NC][2];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    lim[i] = slim_attn_keys(a, s, row0 + ty * 4 + i);
+  for (int i = 0; i < RT; ++i) {
+    lim[i] = slim_attn_keys(a, s, row0 + ty * RT + i);
     m[i] = -INFINITY; l[i] = 0.f;
 #pragma unroll
     for (int c = 0; c < NC; ++c) acc[i][c][0] = acc[i][c][1] = pack2(0.f, 0.f);
@@ -128,25 +128,25 @@ __global__ void __launch_bounds__(4 * TR) attn_kernel(const __grid_constant__ Sl
     const float* s_k = s_k0 + st * KS;
     const float* s_v = s_v0 + st * VS;
     if (ST == 2 && t0 + TK < keys) load(t0 + TK, st ^ 1);
-    f32x2 sv2[4][4];
+    f32x2 sv2[RT][4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < RT; ++i)
 #pragma unroll
       for (int j = 0; j < 4; ++j) sv2[i][j] = pack2(0.f, 0.f);
 #pragma unroll 4
     for (int c = 0; c < DKP; c += 4) {
-      ulonglong2 qv[4], kv[4];
+      ulonglong2 qv[RT], kv[4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) qv[i] = *reinterpret_cast<const ulonglong2*>(s_q + (ty * 4 + i) * PQ + c);
+      for (int i = 0; i < RT; ++i) qv[i] = *reinterpret_cast<const ulonglong2*>(s_q + (ty * RT + i) * PQ + c);
 #pragma unroll
       for (int j = 0; j < 4; ++j) kv[j] = *reinterpret_cast<const ulonglong2*>(s_k + (tx + 16 * j) * PQ + c);
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
+      for (int i = 0; i < RT; ++i)
 #pragma unroll
         for (int j = 0; j < 4; ++j) sv2[i][j] = fma2(qv[i].y, kv[j].y, fma2(qv[i].x, kv[j].x, sv2[i][j]));
     }
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < RT; ++i) {
       float mx = m[i], sv[4];
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
@@ -160,7 +160,7 @@ __global__ void __launch_bounds__(4 * TR) attn_kernel(const __grid_constant__ Sl
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const float p = t0 + tx + 16 * j >= lim[i] ? 0.f : exp2f(sv[j] - mx);
-        s_p[(ty * 4 + i) * PP + tx + 16 * j] = p;
+        s_p[(ty * RT + i) * PP + tx + 16 * j] = p;
         ps += p;
       }
 #pragma unroll
@@ -174,10 +174,10 @@ __global__ void __launch_bounds__(4 * TR) attn_kernel(const __grid_constant__ Sl
     __syncwarp();                                                // a row's probabilities come from its own half warp
 #pragma unroll 2
     for (int t = 0; t < TK; t += 4) {
-      float pv[4][4];
+      float pv[RT][4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float4 v = *reinterpret_cast<const float4*>(s_p + (ty * 4 + i) * PP + t);
+      for (int i = 0; i < RT; ++i) {
+        const float4 v = *reinterpret_cast<const float4*>(s_p + (ty * RT + i) * PP + t);
         pv[i][0] = v.x; pv[i][1] = v.y; pv[i][2] = v.z; pv[i][3] = v.w;
       }
 #pragma unroll
@@ -186,7 +186,7 @@ __global__ void __launch_bounds__(4 * TR) attn_kernel(const __grid_constant__ Sl
         for (int c = 0; c < NC; ++c) {
           const ulonglong2 v = *reinterpret_cast<const ulonglong2*>(s_v + (t + u) * DKP + c * 64 + tx * 4);
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
+          for (int i = 0; i < RT; ++i) {
             const f32x2 pp = pack2(pv[i][u], pv[i][u]);
             acc[i][c][0] = fma2(pp, v.x, acc[i][c][0]);
             acc[i][c][1] = fma2(pp, v.y, acc[i][c][1]);
@@ -200,10 +200,10 @@ __global__ void __launch_bounds__(4 * TR) attn_kernel(const __grid_constant__ Sl
       load(t0 + TK, 0);
     }
   }
-  bool bad[4];
+  bool bad[RT];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int r = ty * 4 + i;
+  for (int i = 0; i < RT; ++i) {
+    const int r = ty * RT + i;
     const float inv = lim[i] > 0 ? 1.f / l[i] : 0.f;
     bad[i] = false;
     if (r >= rows) continue;
@@ -226,11 +226,11 @@ __global__ void __launch_bounds__(4 * TR) attn_kernel(const __grid_constant__ Sl
   // rows with a number that is not finite: once more, from what they attend alone
   __syncwarp();
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
+  for (int i = 0; i < RT; ++i) {
     const unsigned any = __ballot_sync(0xffffffffu, bad[i]);
-    const int r = (ty & ~1) * 4 + i;                             // the warp's rows: 4 of its lower half, 4 of its upper
+    const int r = (ty & ~1) * RT + i;                            // the warp's rows: RT of its lower half, RT of its upper
     if (any & 0x0000ffffu) slim_attn_row(a, tile.x, row0 + r, h);
-    if (any & 0xffff0000u) slim_attn_row(a, tile.x, row0 + r + 4, h);
+    if (any & 0xffff0000u) slim_attn_row(a, tile.x, row0 + r + RT, h);
   }
 }
 
@@ -240,7 +240,7 @@ cudaError_t launch_attn(const SlimAttn& a, cudaStream_t st) {
   auto kern = a.f32 ? attn_kernel<DKP, TR, true> : attn_kernel<DKP, TR, false>;
   cudaError_t e = cudaFuncSetAttribute((const void*)kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
   if (e != cudaSuccess) return e;
-  return slim_launch_pdl(kern, dim3((unsigned)(a.most_tiles * a.H)), dim3(4 * TR), smem, st, a);
+  return slim_launch_pdl(kern, dim3((unsigned)(a.most_tiles * a.H)), dim3(THREADS), smem, st, a);
 }
 template <int DKP>
 cudaError_t launch_attn(const SlimAttn& a, cudaStream_t st) { return a.tile_rows == 32 ? launch_attn<DKP, 32>(a, st) : launch_attn<DKP, 64>(a, st); }
@@ -272,7 +272,9 @@ cudaError_t slim_launch_attn(const slim_ctx* ctx, SlimAttn a, char* ws, int tc, 
   a.tile_rows = tc ? SLIM_ATTN_TC_ROWS : (long long)(a.total_q / 64 + a.batch) * a.H < ctx->num_sms ? 32 : 64;
   a.most_tiles = a.total_q / a.tile_rows + a.batch;
   if (tc) return slim_launch_attn_tc(ctx, a, a.most_tiles, st);
-  const int rows = a.total_q + a.total_k;
+  const bool as_is = a.f32 && !a.rope_base;              // nothing to rotate, nothing to widen
+  if (as_is) { a.qr = const_cast<void*>(a.q); a.kr = const_cast<void*>(a.k); }
+  const int rows = as_is ? 0 : a.total_q + a.total_k;
   const int blocks = 1 + (int)((rows + 7ll) / 8 < 8ll * ctx->num_sms ? (rows + 7ll) / 8 : 8ll * ctx->num_sms);
   const size_t smem = slim_attn_plan_smem(a.batch);
   cudaError_t e = a.f32 ? slim_launch_pdl(attn_prepare_kernel<true>, dim3(blocks), dim3(THREADS), smem, st, a)

@@ -1,9 +1,10 @@
 // Attention over packed prompts on the tensor cores (bf16, d_k in {64, 96, 128}).
 //
 // attn_tc_prepare_kernel  rotated queries and keys as float16 in the workspace (11 bits: bf16's 8 would cost as much accuracy
-//                         as the rounding of P), float32 values as float16 too, the list of query tiles.
+//                         as the rounding of P; without rotation they are read where they lie), float32 values as float16
+//                         too, the list of query tiles.
 // attn_tc_kernel          one CTA a (tile of 2 x 128 query rows, head).  Per key tile of 128 rows and query tile i:
-//                           S_i = Q_i K^T       float16, both operands from shared memory, S in tensor memory
+//                           S_i = Q_i K^T       float16 (bf16 without rotation), both operands from shared memory, S in tensor memory
 //                           P_i = 2^(S_i - m)   a thread a row: S to registers, maximum, exponentials, P as bf16 over S's
 //                                               columns in tensor memory
 //                           O_i += P_i V        P from tensor memory, V as it lies (MN-major); bf16 where the values are, float16
@@ -50,7 +51,7 @@ __device__ void prepare_row(const SlimAttn& a, int r, bool query) {
   float cs[8], sn[8];
 #pragma unroll
   for (int x = 0; x < 8; ++x) {
-    const float2 t = a.rope_base ? slim_attn_turn(a, pos, 8 * jl + x) : make_float2(1.f, 0.f);
+    const float2 t = slim_attn_turn(a, pos, 8 * jl + x);
     cs[x] = t.x; sn[x] = t.y;
   }
 #pragma unroll 4
@@ -83,12 +84,11 @@ __global__ void __launch_bounds__(PREP_THREADS) attn_tc_prepare_kernel(const __g
   slim_pdl_wait();
   if (blockIdx.x == 0) { slim_attn_plan(a, s_mem); return; }
   const int warps = (gridDim.x - 1) * (PREP_THREADS / 32), lane = threadIdx.x & 31;
-  const int rows = a.total_q + a.total_k + (a.v32 ? a.total_k : 0);
+  const int turned = a.rope_base ? a.total_q + a.total_k : 0, rows = turned + (a.v32 ? a.total_k : 0);
   for (int r = (blockIdx.x - 1) * (PREP_THREADS / 32) + (threadIdx.x >> 5); r < rows; r += warps) {
-    if (r < a.total_q) { prepare_row<DK>(a, r, true); continue; }
-    if (r < a.total_q + a.total_k) { prepare_row<DK>(a, r - a.total_q, false); continue; }
+    if (r < turned) { prepare_row<DK>(a, r < a.total_q ? r : r - a.total_q, r < a.total_q); continue; }
     const int n = a.KV * DK;
-    const size_t at = (size_t)(r - a.total_q - a.total_k) * n;
+    const size_t at = (size_t)(r - turned) * n;
     const float4* src = reinterpret_cast<const float4*>(reinterpret_cast<const float*>(a.v) + at);
     uint2* dst = reinterpret_cast<uint2*>(reinterpret_cast<unsigned short*>(a.vb) + at);
 #pragma unroll 4
@@ -207,8 +207,8 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
   typedef Shape<DK> S;
   constexpr int NS = S::NS, CH = S::CH, KSTEPS = DK / 16;
   constexpr uint32_t TILE = S::TILE;
-  // S = Q K^T: float16, both K-major;  O = P V: float16 (VH) or bf16, V MN-major
-  constexpr uint32_t IDESC_S = (1u << 4) | ((TN >> 3) << 17) | ((TM >> 4) << 24);
+  // S = Q K^T: float16, or bf16 where nothing was rotated, both K-major;  O = P V: float16 (VH) or bf16, V MN-major
+  const uint32_t IDESC_S = (1u << 4) | (a.rope_base ? 0u : (1u << 7) | (1u << 10)) | ((TN >> 3) << 17) | ((TM >> 4) << 24);
   constexpr uint32_t IDESC_O = (1u << 4) | (VH ? 0u : (1u << 7) | (1u << 10)) | (1u << 16) | ((DK >> 3) << 17) | ((TM >> 4) << 24);
   extern __shared__ unsigned char smem_raw[];
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
@@ -515,12 +515,12 @@ cudaError_t make_map(CUtensorMap* map, const void* p, int cols, int rows) {
 template <int DK, bool VH>
 cudaError_t launch(const slim_ctx* ctx, const SlimAttn& a, int most_tiles, cudaStream_t st) {
   CUtensorMap qmap, kmap, vmap;
-  cudaError_t e = make_map(&qmap, a.qr, a.H * DK, a.total_q);
-  if (e == cudaSuccess) e = make_map(&kmap, a.kr, a.KV * DK, a.total_k);
+  cudaError_t e = make_map(&qmap, a.rope_base ? a.qr : a.q, a.H * DK, a.total_q);
+  if (e == cudaSuccess) e = make_map(&kmap, a.rope_base ? a.kr : a.k, a.KV * DK, a.total_k);
   if (e == cudaSuccess) e = make_map(&vmap, a.v32 ? a.vb : a.v, a.KV * DK, a.total_k);
   if (e == cudaSuccess) e = cudaFuncSetAttribute((const void*)attn_tc_kernel<DK, VH>, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape<DK>::SMEM);
   if (e != cudaSuccess) return e;
-  const long long rows = (long long)a.total_q + a.total_k + (a.v32 ? a.total_k : 0), fill = 8ll * ctx->num_sms;
+  const long long rows = (a.rope_base ? (long long)a.total_q + a.total_k : 0) + (a.v32 ? a.total_k : 0), fill = 8ll * ctx->num_sms;
   const int blocks = 1 + (int)((rows + 7) / 8 < fill ? (rows + 7) / 8 : fill);
   e = slim_launch_pdl(attn_tc_prepare_kernel<DK>, dim3(blocks), dim3(PREP_THREADS), slim_attn_plan_smem(a.batch), st, a);
   if (e != cudaSuccess) return e;
