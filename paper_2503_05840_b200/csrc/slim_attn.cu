@@ -71,7 +71,7 @@ __global__ void __launch_bounds__(THREADS) attn_kernel(const __grid_constant__ S
   slim_pdl_wait();
   const int item = blockIdx.x / a.H, h = blockIdx.x % a.H;
   if (item >= *a.n_tiles) return;
-  const int4 tile = a.tiles[2 * item], range = a.tiles[2 * item + 1];
+  const int4 tile = a.tiles[3 * item], range = a.tiles[3 * item + 1], piece = a.tiles[3 * item + 2];
   const SlimSeq s = {range.x, range.y, range.z, range.w};
   const int row0 = tile.y, rows = min(TR, s.nq - row0), dk = a.d_k, kvh = h / (a.H / a.KV);
   const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
@@ -92,7 +92,7 @@ __global__ void __launch_bounds__(THREADS) attn_kernel(const __grid_constant__ S
 #pragma unroll
     for (int c = 0; c < NC; ++c) acc[i][c][0] = acc[i][c][1] = pack2(0.f, 0.f);
   }
-  const int keys = slim_attn_keys(a, s, row0 + rows - 1);
+  const int first = piece.x * TK, keys = min(slim_attn_keys(a, s, row0 + rows - 1), (int)min((long long)piece.y * TK, 0x7fffffffll));
   // Key tile t0 into stage st: 16 bytes at a time behind the products of the tile before it, or element by element (d_k not a
   // multiple of four, bf16 values)
   const bool vec = (dk & 3) == 0 && a.v32;
@@ -120,9 +120,9 @@ __global__ void __launch_bounds__(THREADS) attn_kernel(const __grid_constant__ S
     }
     asm volatile("cp.async.commit_group;" ::: "memory");
   };
-  if (keys > 0) load(0, 0);
+  if (first < keys) load(first, 0);
   int st = 0;
-  for (int t0 = 0; t0 < keys; t0 += TK) {
+  for (int t0 = first; t0 < keys; t0 += TK) {
     asm volatile("cp.async.wait_group 0;" ::: "memory");
     __syncthreads();                                             // this tile is there, and nobody reads the one before it any more
     const float* s_k = s_k0 + st * KS;
@@ -200,6 +200,48 @@ __global__ void __launch_bounds__(THREADS) attn_kernel(const __grid_constant__ S
       load(t0 + TK, 0);
     }
   }
+  if (tile.w > 1) {
+    // A piece of the keys: its sums go to the workspace, and the last piece of the tile to arrive joins them, in their order
+    constexpr int WIDE = DKP + 2;
+    const size_t slot0 = (size_t)piece.z * a.H + h;              // of the tile's piece i: slot0 + i H
+    float* mine = a.part + (slot0 + (size_t)tile.z * a.H) * (TR * WIDE);
+#pragma unroll
+    for (int i = 0; i < RT; ++i) {
+      const int r = ty * RT + i;
+#pragma unroll
+      for (int c = 0; c < NC; ++c) *reinterpret_cast<ulonglong2*>(mine + r * DKP + c * 64 + tx * 4) = make_ulonglong2(acc[i][c][0], acc[i][c][1]);
+      if (tx == 0) *reinterpret_cast<float2*>(mine + TR * DKP + 2 * r) = make_float2(m[i], l[i]);
+    }
+    __threadfence();
+    __syncthreads();
+    if (tid == 0) s_p[0] = __int_as_float(atomicAdd(a.arrivals + 8 * slot0, 1));
+    __syncthreads();
+    if (__float_as_int(s_p[0]) != tile.w - 1) return;
+    __threadfence();
+#pragma unroll
+    for (int i = 0; i < RT; ++i) {
+      const int r = ty * RT + i;
+      const float* from = a.part + slot0 * (TR * WIDE);
+      const size_t step = (size_t)a.H * (TR * WIDE);
+      m[i] = -INFINITY; l[i] = 0.f;
+      for (int x = 0; x < tile.w; ++x) m[i] = fmaxf(m[i], __ldcg(from + x * step + TR * DKP + 2 * r));
+#pragma unroll
+      for (int c = 0; c < NC; ++c) acc[i][c][0] = acc[i][c][1] = pack2(0.f, 0.f);
+      for (int x = 0; x < tile.w; ++x) {
+        const float2 ml = __ldcg(reinterpret_cast<const float2*>(from + x * step + TR * DKP + 2 * r));
+        if (ml.x == -INFINITY && ml.y == 0.f) continue;          // the row attends nothing there
+        const float f = exp2f(ml.x - m[i]);
+        const f32x2 f2 = pack2(f, f);
+        l[i] = fmaf(ml.y, f, l[i]);
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+          const ulonglong2 v = __ldcg(reinterpret_cast<const ulonglong2*>(from + x * step + r * DKP + c * 64 + tx * 4));
+          acc[i][c][0] = fma2(f2, v.x, acc[i][c][0]);
+          acc[i][c][1] = fma2(f2, v.y, acc[i][c][1]);
+        }
+      }
+    }
+  }
   bool bad[RT];
 #pragma unroll
   for (int i = 0; i < RT; ++i) {
@@ -240,23 +282,51 @@ cudaError_t launch_attn(const SlimAttn& a, cudaStream_t st) {
   auto kern = a.f32 ? attn_kernel<DKP, TR, true> : attn_kernel<DKP, TR, false>;
   cudaError_t e = cudaFuncSetAttribute((const void*)kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
   if (e != cudaSuccess) return e;
-  return slim_launch_pdl(kern, dim3((unsigned)(a.most_tiles * a.H)), dim3(THREADS), smem, st, a);
+  return slim_launch_pdl(kern, dim3((unsigned)((a.most_tiles + (a.slots + a.H - 1) / a.H) * a.H)), dim3(THREADS), smem, st, a);
 }
 template <int DKP>
 cudaError_t launch_attn(const SlimAttn& a, cudaStream_t st) { return a.tile_rows == 32 ? launch_attn<DKP, 32>(a, st) : launch_attn<DKP, 64>(a, st); }
 
 inline size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
+// Tiles of one path, and the pieces that they may be split into
+void shape_of(const slim_ctx* ctx, SlimAttn& a, bool tc) {
+  // Tiles of 32 query rows where those of 64 would not give every SM one (one sequence of 448 tokens, 6 heads, float32:
+  // the attention kernel 29 us instead of 40).
+  a.tile_rows = tc ? SLIM_ATTN_TC_ROWS : (long long)(a.total_q / 64 + a.batch) * a.H < ctx->num_sms ? 32 : 64;
+  a.most_tiles = a.total_q / a.tile_rows + a.batch;
+  a.key_rows = tc ? 128 : TK;
+  a.least = tc ? 4 : 2;
+  a.beside = tc ? 4 : 1;
+  a.share_of = ctx->num_sms * (!tc && ctx->d_k <= 64 ? 2 : 1);          // (two CTAs of the narrow CUDA-core kernel fit an SM)
+  const long long run = (long long)a.key_rows * a.least, pieces = (a.total_k + run - 1) / run;
+  // (two query tiles for every SM or more: nothing is split)
+  const long long all = pieces > 1 && (long long)(a.total_q / a.tile_rows) * a.H < 2ll * ctx->num_sms ? (long long)a.most_tiles * a.H * pieces : 0;
+  a.slots = (int)(all < 2ll * a.share_of ? all : 2ll * a.share_of);
+}
+size_t part_bytes(const SlimAttn& a, int columns) { return sizeof(float) * (size_t)a.slots * a.tile_rows * (columns + 2); }
+
 }  // namespace
 
 SlimAttnLayout slim_attn_layout(const slim_ctx* ctx, int kv_heads, int batch, int total_q, int total_k) {
   SlimAttnLayout L;
+  SlimAttn a = {};
+  a.H = ctx->H; a.batch = batch; a.total_q = total_q; a.total_k = total_k;
+  shape_of(ctx, a, false);
+  size_t part = part_bytes(a, (ctx->d_k + 63) / 64 * 64), tiles = (size_t)a.most_tiles + a.slots;
+  if (slim_attn_tc_ok(ctx)) {
+    shape_of(ctx, a, true);
+    if (part_bytes(a, ctx->d_k) > part) part = part_bytes(a, ctx->d_k);
+    if ((size_t)a.most_tiles + a.slots > tiles) tiles = (size_t)a.most_tiles + a.slots;
+  }
   size_t off = 0;
   L.qr = off; off = align256(off + 4 * (size_t)total_q * ctx->d);
   L.kr = off; off = align256(off + 4 * (size_t)total_k * kv_heads * ctx->d_k);
   L.vb = off; off = align256(off + (slim_attn_tc_ok(ctx) ? 2 * (size_t)total_k * kv_heads * ctx->d_k : 0));
-  L.tiles = off; off = align256(off + 2 * sizeof(int4) * ((size_t)total_q / 32 + batch + 1));
+  L.tiles = off; off = align256(off + 3 * sizeof(int4) * tiles);
   L.n_tiles = off; off = align256(off + sizeof(int));
+  L.part = off; off = align256(off + part);
+  L.arrivals = off; off = align256(off + sizeof(int) * 8 * 4 * (size_t)ctx->num_sms);
   L.total = off;
   return L;
 }
@@ -266,12 +336,11 @@ cudaError_t slim_launch_attn(const slim_ctx* ctx, SlimAttn a, char* ws, int tc, 
   a.qr = ws + L.qr; a.kr = ws + L.kr; a.vb = ws + L.vb;
   a.tiles = reinterpret_cast<int4*>(ws + L.tiles);
   a.n_tiles = reinterpret_cast<int*>(ws + L.n_tiles);
+  a.part = reinterpret_cast<float*>(ws + L.part);
+  a.arrivals = reinterpret_cast<int*>(ws + L.arrivals);
   tc = tc && a.total_k > 0;                              // (a tensor map needs a row)
-  // Tiles of 32 query rows where those of 64 would not give every SM one (one sequence of 448 tokens, 6 heads, float32:
-  // the attention kernel 29 us instead of 40).
-  a.tile_rows = tc ? SLIM_ATTN_TC_ROWS : (long long)(a.total_q / 64 + a.batch) * a.H < ctx->num_sms ? 32 : 64;
-  a.most_tiles = a.total_q / a.tile_rows + a.batch;
-  if (tc) return slim_launch_attn_tc(ctx, a, a.most_tiles, st);
+  shape_of(ctx, a, tc);
+  if (tc) return slim_launch_attn_tc(ctx, a, st);
   const bool as_is = a.f32 && !a.rope_base;              // nothing to rotate, nothing to widen
   if (as_is) { a.qr = const_cast<void*>(a.q); a.kr = const_cast<void*>(a.k); }
   const int rows = as_is ? 0 : a.total_q + a.total_k;

@@ -22,17 +22,23 @@ struct SlimAttn {
   void* qr;                      // rotated queries and keys, layout of q and k: float32 (CUDA cores) or float16 (tensor cores)
   void* kr;
   void* vb;                      // tensor cores with float32 values: the values times 16 as float16
-  int4* tiles;                   // query tiles, most keys first, two entries each: (sequence, first query row, -, -), (q0, nq, k0, nk)
+  int4* tiles;                   // items, longest first, three entries each: (sequence, first query row, piece, pieces of the tile),
+                                 // (q0, nq, k0, nk), (first key tile, key tile behind the last, slot of the tile's first piece, -)
   int* n_tiles;
-  int tile_rows, most_tiles;
+  int tile_rows, most_tiles;     // query rows of a tile; tiles at most
+  int key_rows, least, beside;   // keys of a key tile; key tiles of a piece at least; key tiles that a piece costs beside its own
+  int share_of;                  // CTAs that run at a time
+  int slots;                     // pieces times heads whose sums fit the workspace (0: nothing is split)
+  float* part;                   // [slots][tile_rows][columns + 2]: sums of the pieces (a kernel's own order)
+  int* arrivals;                 // [slots][8]
 };
 
-struct SlimAttnLayout { size_t qr, kr, vb, tiles, n_tiles, total; };
+struct SlimAttnLayout { size_t qr, kr, vb, tiles, n_tiles, part, arrivals, total; };
 
 constexpr int SLIM_ATTN_TC_ROWS = 256;   // query rows of an item on the tensor cores: two tiles of 128
 
 int slim_attn_tc_ok(const slim_ctx* ctx);
-cudaError_t slim_launch_attn_tc(const slim_ctx* ctx, const SlimAttn& a, int most_tiles, cudaStream_t st);
+cudaError_t slim_launch_attn_tc(const slim_ctx* ctx, const SlimAttn& a, cudaStream_t st);
 SlimAttnLayout slim_attn_layout(const slim_ctx* ctx, int kv_heads, int batch, int total_q, int total_k);
 cudaError_t slim_launch_attn(const slim_ctx* ctx, SlimAttn a, char* ws, int tc, cudaStream_t st);
 
@@ -51,6 +57,8 @@ __device__ __forceinline__ SlimSeq slim_attn_seq(const SlimAttn& a, int b) {
   s.nq = q1 - s.q0; s.nk = k1 - s.k0;
   return s;
 }
+// Pieces of a query tile with so many key tiles, where a piece is to have `most` at most
+__device__ __forceinline__ int slim_attn_pieces(int tiles, int most) { return tiles > most ? (tiles + most - 1) / most : 1; }
 // Keys that query row i of a sequence attends: the first so many.
 __device__ __forceinline__ int slim_attn_keys(const SlimAttn& a, const SlimSeq& s, int i) {
   return a.causal ? max(0, min(s.nk, i + 1 + s.nk - s.nq)) : s.nk;

@@ -241,18 +241,21 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
   slim_pdl_wait();
   const int n_items = *a.n_tiles * a.H, share = a.H / a.KV;
   // Item number r of this CTA: the list, most keys first, is dealt out in rounds of alternating direction.
-  struct Item { SlimSeq s; int b, row0, h, nt0, nt1; };
+  struct Item { SlimSeq s; int b, row0, h, nt0, nt1, first, piece, pieces, slot; };
   auto item = [&](int r, Item& it) {
     const long long at = (long long)r * gridDim.x + (r & 1 ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
     if (at >= n_items) return false;
     const int tile = (int)(at / a.H);
     it.h = (int)(at - (long long)tile * a.H);
-    const int4 x = __ldg(a.tiles + 2 * tile), y = __ldg(a.tiles + 2 * tile + 1);
-    it.b = x.x; it.row0 = x.y;
+    const int4 x = __ldg(a.tiles + 3 * tile), y = __ldg(a.tiles + 3 * tile + 1), z = __ldg(a.tiles + 3 * tile + 2);
+    it.b = x.x; it.row0 = x.y; it.piece = x.z; it.pieces = x.w;
     it.s.q0 = y.x; it.s.nq = y.y; it.s.k0 = y.z; it.s.nk = y.w;
-    // key tiles of the two query tiles (the second may have no rows)
+    it.first = z.x; it.slot = z.z;
+    // key tiles of the two query tiles, within the piece (the second may have no rows)
     it.nt0 = (slim_attn_keys(a, it.s, min(it.s.nq, it.row0 + TM) - 1) + TN - 1) / TN;
     it.nt1 = it.row0 + TM < it.s.nq ? (slim_attn_keys(a, it.s, min(it.s.nq, it.row0 + 2 * TM) - 1) + TN - 1) / TN : 0;
+    it.nt0 = max(min(it.nt0, z.y) - z.x, 0);
+    it.nt1 = max(min(it.nt1, z.y) - z.x, 0);
     return true;
   };
   Item it;
@@ -270,7 +273,8 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
     uint32_t ps = 0, po = 0;                        // phases of bar_s, bar_o
     for (int r_ = 0; ok && item(r_, it); ++r_) {
       const int n = i ? it.nt1 : it.nt0;
-      const int lim = slim_attn_keys(a, it.s, it.row0 + i * TM + (warp & 3) * 32 + lane);
+      const int all = slim_attn_keys(a, it.s, it.row0 + i * TM + (warp & 3) * 32 + lane);     // keys of the row
+      const int lim = all - it.first * TN;                                                   // behind the piece's first
       float m = -INFINITY;                            // reference, log2 units
       f32x2 l2 = pack2(0.f, 0.f);
       for (int j = 0; j < n; ++j) {
@@ -344,7 +348,47 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
         tc_fence_after();
       }
       const bool there = row < s.nq;
-      const float inv = lim > 0 ? (VH ? 1.f / V_UP : 1.f) / sum2(l2) : 0.f;
+      float l = sum2(l2);
+      if (it.pieces > 1) {
+        // A piece of the keys: the warp's sums go to the workspace, a column of four times 256 rows at a time, and the last of
+        // the tile's pieces to arrive there joins them, in their order
+        constexpr size_t SLOT = (size_t)SLIM_ATTN_TC_ROWS * (DK + 2);
+        const size_t slot0 = (size_t)it.slot * a.H + h, step = SLOT * a.H;
+        const int lane_row = i * TM + (warp & 3) * 32 + lane;
+        float* mine = a.part + (slot0 + (size_t)it.piece * a.H) * SLOT;
+        if (ok) {
+          if (n > 0) {
+#pragma unroll
+            for (int c = 0; c < DK / 32; ++c) {
+              uint32_t o[32];
+              tmem_ld32(t_o + 32 * c, o);
+#pragma unroll
+              for (int x = 0; x < 32; x += 4)
+                *reinterpret_cast<uint4*>(mine + ((size_t)(8 * c + x / 4) * SLIM_ATTN_TC_ROWS + lane_row) * 4) = make_uint4(o[x], o[x + 1], o[x + 2], o[x + 3]);
+            }
+          }
+          mine[SLIM_ATTN_TC_ROWS * DK + lane_row] = m;
+          mine[SLIM_ATTN_TC_ROWS * (DK + 1) + lane_row] = l;
+        }
+        tc_fence_before();                            // (O has been read: the next item's first product overwrites it)
+        __threadfence();
+        __syncwarp();
+        int before = 0;
+        if (lane == 0 && ok) before = atomicAdd(a.arrivals + 8 * slot0 + warp, 1);
+        before = __shfl_sync(0xffffffffu, before, 0);
+        if (!ok || before != it.pieces - 1) continue;
+        __threadfence();
+        const float* from = a.part + slot0 * SLOT;
+        const int pieces = it.pieces;
+        m = -INFINITY;
+        for (int x = 0; x < pieces; ++x) m = fmaxf(m, __ldcg(from + x * step + SLIM_ATTN_TC_ROWS * DK + lane_row));
+        l = 0.f;
+        for (int x = 0; x < pieces; ++x) {
+          const float mx = __ldcg(from + x * step + SLIM_ATTN_TC_ROWS * DK + lane_row), lx = __ldcg(from + x * step + SLIM_ATTN_TC_ROWS * (DK + 1) + lane_row);
+          if (!(mx == -INFINITY && lx == 0.f)) l = fmaf(lx, ex2_approx(mx - m), l);
+        }
+      }
+      const float inv = all > 0 ? (VH ? 1.f / V_UP : 1.f) / l : 0.f;
       __nv_bfloat16* dst = reinterpret_cast<__nv_bfloat16*>(a.o) + ((size_t)(s.q0 + row) * a.H + h) * DK;
       bool bad = false;
       float most = 0.f;
@@ -352,14 +396,36 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
 #pragma unroll
         for (int c = 0; c < DK / 32; ++c) {
           uint32_t o[32];
-          if (n > 0) tmem_ld32(t_o + 32 * c, o);
+          if (it.pieces > 1) {
+            constexpr size_t SLOT = (size_t)SLIM_ATTN_TC_ROWS * (DK + 2);
+            const float* from = a.part + ((size_t)it.slot * a.H + h) * SLOT;
+            const int lane_row = i * TM + (warp & 3) * 32 + lane;
+#pragma unroll
+            for (int x = 0; x < 32; ++x) o[x] = 0u;
+#pragma unroll 2
+            for (int y = 0; y < it.pieces; ++y, from += SLOT * a.H) {
+              const float mx = __ldcg(from + SLIM_ATTN_TC_ROWS * DK + lane_row), lx = __ldcg(from + SLIM_ATTN_TC_ROWS * (DK + 1) + lane_row);
+              const bool some = !(mx == -INFINITY && lx == 0.f);         // (else the row attends nothing there)
+              const float f = some ? ex2_approx(mx - m) : 0.f;
+              float4 u[8];
+#pragma unroll
+              for (int x = 0; x < 8; ++x)
+                u[x] = some ? __ldcg(reinterpret_cast<const float4*>(from + ((size_t)(8 * c + x) * SLIM_ATTN_TC_ROWS + lane_row) * 4)) : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+              for (int x = 0; x < 32; x += 4) {
+                const float4 v = u[x / 4];
+                o[x] = __float_as_uint(fmaf(v.x, f, __uint_as_float(o[x]))); o[x + 1] = __float_as_uint(fmaf(v.y, f, __uint_as_float(o[x + 1])));
+                o[x + 2] = __float_as_uint(fmaf(v.z, f, __uint_as_float(o[x + 2]))); o[x + 3] = __float_as_uint(fmaf(v.w, f, __uint_as_float(o[x + 3])));
+              }
+            }
+          } else if (n > 0) tmem_ld32(t_o + 32 * c, o);
 #pragma unroll
           for (int x = 0; x < 32; x += 8) {
             uint32_t w[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
               float lo = __uint_as_float(o[x + 2 * e]) * inv, hi = __uint_as_float(o[x + 2 * e + 1]) * inv;
-              if (lim == 0) lo = hi = 0.f;
+              if (all == 0) lo = hi = 0.f;
               bad |= !(fabsf(lo) <= 3.3895313892515355e38f && fabsf(hi) <= 3.3895313892515355e38f);
               if (VH) most = fmaxf(most, fmaxf(fabsf(lo), fabsf(hi)));
               w[e] = bf162_of(lo, hi);
@@ -367,7 +433,7 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
             if (there) *reinterpret_cast<uint4*>(dst + 32 * c + x) = make_uint4(w[0], w[1], w[2], w[3]);
           }
         }
-        if (VH) bad |= lim > 0 && most < 3.8e-6f;      // 2^-18
+        if (VH) bad |= all > 0 && most < 3.8e-6f;      // 2^-18
         unsigned redo = __ballot_sync(0xffffffffu, bad && there);
         while (redo) {
           const int x = __ffs(redo) - 1;
@@ -483,7 +549,7 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
           const uint32_t bar = bar_full + 8 * st, dst = s_kv + (uint32_t)st * TILE;
           mbar_arrive_expect_tx(bar, TILE);
           for (int c = 0; c < CH; ++c)                                 // K(0), V(0), K(1), ..: the order in which they are needed
-            tma_load_3d(dst + c * TN * 128, k & 1 ? &vmap : &kmap, bar, kvh * DK + 64 * c, it.s.k0 + (k >> 1) * TN, 0);
+            tma_load_3d(dst + c * TN * 128, k & 1 ? &vmap : &kmap, bar, kvh * DK + 64 * c, it.s.k0 + (it.first + (k >> 1)) * TN, 0);
           if (++st == NS) { st = 0; pe ^= 1u; }
         }
       }
@@ -513,7 +579,7 @@ cudaError_t make_map(CUtensorMap* map, const void* p, int cols, int rows) {
 }
 
 template <int DK, bool VH>
-cudaError_t launch(const slim_ctx* ctx, const SlimAttn& a, int most_tiles, cudaStream_t st) {
+cudaError_t launch(const slim_ctx* ctx, const SlimAttn& a, cudaStream_t st) {
   CUtensorMap qmap, kmap, vmap;
   cudaError_t e = make_map(&qmap, a.rope_base ? a.qr : a.q, a.H * DK, a.total_q);
   if (e == cudaSuccess) e = make_map(&kmap, a.rope_base ? a.kr : a.k, a.KV * DK, a.total_k);
@@ -524,7 +590,7 @@ cudaError_t launch(const slim_ctx* ctx, const SlimAttn& a, int most_tiles, cudaS
   const int blocks = 1 + (int)((rows + 7) / 8 < fill ? (rows + 7) / 8 : fill);
   e = slim_launch_pdl(attn_tc_prepare_kernel<DK>, dim3(blocks), dim3(PREP_THREADS), slim_attn_plan_smem(a.batch), st, a);
   if (e != cudaSuccess) return e;
-  const long long items = (long long)most_tiles * a.H;
+  const long long items = (long long)a.most_tiles * a.H + a.slots;
   return slim_launch_pdl(attn_tc_kernel<DK, VH>, dim3((unsigned)(items < ctx->num_sms ? items : ctx->num_sms)), dim3(THREADS), Shape<DK>::SMEM, st, qmap, kmap, vmap, a);
 }
 
@@ -532,8 +598,8 @@ cudaError_t launch(const slim_ctx* ctx, const SlimAttn& a, int most_tiles, cudaS
 
 int slim_attn_tc_ok(const slim_ctx* ctx) { return ctx->dtype == SLIM_BF16 && (ctx->d_k == 64 || ctx->d_k == 96 || ctx->d_k == 128); }
 
-cudaError_t slim_launch_attn_tc(const slim_ctx* ctx, const SlimAttn& a, int most_tiles, cudaStream_t st) {
+cudaError_t slim_launch_attn_tc(const slim_ctx* ctx, const SlimAttn& a, cudaStream_t st) {
   if (a.v32)
-    return a.d_k == 64 ? launch<64, true>(ctx, a, most_tiles, st) : a.d_k == 96 ? launch<96, true>(ctx, a, most_tiles, st) : launch<128, true>(ctx, a, most_tiles, st);
-  return a.d_k == 64 ? launch<64, false>(ctx, a, most_tiles, st) : a.d_k == 96 ? launch<96, false>(ctx, a, most_tiles, st) : launch<128, false>(ctx, a, most_tiles, st);
+    return a.d_k == 64 ? launch<64, true>(ctx, a, st) : a.d_k == 96 ? launch<96, true>(ctx, a, st) : launch<128, true>(ctx, a, st);
+  return a.d_k == 64 ? launch<64, false>(ctx, a, st) : a.d_k == 96 ? launch<96, false>(ctx, a, st) : launch<128, false>(ctx, a, st);
 }

@@ -326,3 +326,51 @@ def test_offsets_beyond_32_bits():
     torch.cuda.synchronize()
     assert np.array_equal(got, alone.double().cpu().numpy())
     B.slim_destroy(ctx)
+
+
+# few query tiles over many keys: the tiles are split along their keys and joined
+SPLIT = [("f32", 6, 6, 64, 0.0, [448], [448]), ("f32", 2, 1, 40, 1e4, [1, 33, 0, 70], [1999, 700, 40, 70]), ("f32", 1, 1, 256, 1e4, [65], [1300]),
+         ("bf16", 2, 2, 128, 1e6, [1], [5000]), ("bf16", 4, 1, 64, 1e4, [300, 1], [3000, 2049]), ("bf16", 2, 2, 96, 0.0, [130, 1, 700, 257], [2000, 900, 700, 3500]),
+         ("bf16", 8, 2, 128, 0.0, [512], [4096]), ("bf16", 3, 3, 50, 1e4, [90, 200], [1500, 200])]
+
+
+@pytest.mark.parametrize("dtype,H,KV,dk,theta,nq,nk", SPLIT)
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("v32", [True, False])
+def test_long_keys_in_pieces(dtype, H, KV, dk, theta, nq, nk, causal, v32):
+    if dtype == "f32" and not v32:
+        pytest.skip("float32 contexts take float32 values")
+    c = Case(dtype, H, KV, dk, theta, nq, nk, v32=v32, seed=dk)
+    b = c.buffers()
+    first = c.check(causal, b)
+    for _ in range(3):                                   # whichever piece comes last, the sums are the same
+        b["o"].fill_(7)
+        c.call(b, causal)
+        torch.cuda.synchronize()
+        assert np.array_equal(b["o"].double().cpu().numpy(), first)
+    c.close()
+
+
+@pytest.mark.parametrize("dtype,H,dk", [("bf16", 2, 128), ("f32", 2, 64)])
+def test_numbers_that_are_not_finite_in_one_piece(dtype, H, dk):
+    """An infinite key and a NaN value far behind: the rows that attend them get NaN, the others what they would get without them, up to
+    rounding (those that share a tile of keys with the two are formed another way)."""
+    n = 2600
+    c = Case(dtype, H, H, dk, 1e4, [n // 4], [n], seed=9)
+    b = c.buffers()
+    c.check(True, b)
+    row = 400                                            # a query; key at its place, a lead of 3 rows
+    at = 3 + n - n // 4 + row
+    b["k"][at, 0] = float("inf")
+    b["v"][at, 1, 5] = float("nan")
+    b["o"].fill_(7)
+    c.call(b, True)
+    torch.cuda.synchronize()
+    got = b["o"].double().cpu().numpy()
+    lo, hi = slice(3, 3 + row), slice(3 + row, 3 + n // 4)
+    ref, tol = c.reference(True)
+    assert (np.abs(got[lo] - ref[lo]) <= tol[lo]).all()
+    assert np.isnan(got[hi, 0]).all() and np.isnan(got[hi, 1, 5]).all()
+    rest = np.delete(got[hi, 1], 5, axis=1)
+    assert np.isfinite(rest).all()
+    c.close()
