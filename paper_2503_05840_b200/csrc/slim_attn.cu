@@ -316,13 +316,15 @@ SlimAttnLayout slim_attn_layout(const slim_ctx* ctx, int kv_heads, int batch, in
   size_t part = part_bytes(a, (ctx->d_k + 63) / 64 * 64), tiles = (size_t)a.most_tiles + a.slots;
   if (slim_attn_tc_ok(ctx)) {
     shape_of(ctx, a, true);
-    if (part_bytes(a, ctx->d_k) > part) part = part_bytes(a, ctx->d_k);
+    if (part_bytes(a, slim_attn_width(ctx->d_k)) > part) part = part_bytes(a, slim_attn_width(ctx->d_k));
     if ((size_t)a.most_tiles + a.slots > tiles) tiles = (size_t)a.most_tiles + a.slots;
   }
   size_t off = 0;
-  L.qr = off; off = align256(off + 4 * (size_t)total_q * ctx->d);
-  L.kr = off; off = align256(off + 4 * (size_t)total_k * kv_heads * ctx->d_k);
-  L.vb = off; off = align256(off + (slim_attn_tc_ok(ctx) ? 2 * (size_t)total_k * kv_heads * ctx->d_k : 0));
+  // bytes of a head: float32, or 16 bits and widened
+  const size_t wide = slim_attn_tc_ok(ctx) ? 2 * (size_t)slim_attn_width(ctx->d_k) : 0, head = wide > 4 * (size_t)ctx->d_k ? wide : 4 * (size_t)ctx->d_k;
+  L.qr = off; off = align256(off + head * total_q * ctx->H);
+  L.kr = off; off = align256(off + head * total_k * kv_heads);
+  L.vb = off; off = align256(off + wide * total_k * kv_heads);
   L.tiles = off; off = align256(off + 3 * sizeof(int4) * tiles);
   L.n_tiles = off; off = align256(off + sizeof(int));
   L.part = off; off = align256(off + part);

@@ -19,9 +19,9 @@ struct SlimAttn {
   int rope_rows;                 // positions that the tables cover
   int* status;
   // workspace
-  void* qr;                      // rotated queries and keys, layout of q and k: float32 (CUDA cores) or float16 (tensor cores)
-  void* kr;
-  void* vb;                      // tensor cores with float32 values: the values times 16 as float16
+  void* qr;                      // rotated queries and keys, layout of q and k: float32 (CUDA cores) or float16 (tensor cores, heads
+  void* kr;                      // widened to slim_attn_width with zeros)
+  void* vb;                      // tensor cores: float32 values times 16 as float16, or bf16 values of widened heads
   int4* tiles;                   // items, longest first, three entries each: (sequence, first query row, piece, pieces of the tile),
                                  // (q0, nq, k0, nk), (first key tile, key tile behind the last, slot of the tile's first piece, -)
   int* n_tiles;
@@ -35,6 +35,8 @@ struct SlimAttn {
 
 struct SlimAttnLayout { size_t qr, kr, vb, tiles, n_tiles, part, arrivals, total; };
 
+// Columns that a head has on the tensor cores
+__host__ __device__ inline int slim_attn_width(int d_k) { return d_k <= 64 ? 64 : d_k <= 96 ? 96 : 128; }
 constexpr int SLIM_ATTN_TC_ROWS = 256;   // query rows of an item on the tensor cores: two tiles of 128
 
 int slim_attn_tc_ok(const slim_ctx* ctx);

@@ -1,4 +1,5 @@
-// Attention over packed prompts on the tensor cores (bf16, d_k in {64, 96, 128}).
+// Attention over packed prompts on the tensor cores (bf16, d_k up to 128; heads of other widths than 64, 96 and 128 are widened
+// with zeros on their way into the workspace).
 //
 // attn_tc_prepare_kernel  rotated queries and keys as float16 in the workspace (11 bits: bf16's 8 would cost as much accuracy
 //                         as the rounding of P; without rotation they are read where they lie), float32 values as float16
@@ -37,26 +38,26 @@ __device__ __forceinline__ uint32_t half2_checked(float a, float b, float most) 
 }
 
 // One warp a packed row.  A lane has eight pairs (j, j + d_k/2) of a head, the same j in every head, so its angles are
-// formed once; d_k / 16 lanes make a head.
-template <int DK>
+// formed once; d_k / 16 lanes make a head.  NARROW: heads of fewer columns than DK, a multiple of 16.
+template <int DK, bool NARROW>
 __device__ void prepare_row(const SlimAttn& a, int r, bool query) {
-  constexpr int LPH = DK / 16, HPW = 32 / LPH;
+  const int dk = NARROW ? a.d_k : DK, LPH = dk / 16, HPW = 32 / LPH;
   const int lane = threadIdx.x & 31, heads = query ? a.H : a.KV;
   int pos;
   if (!slim_attn_position(a, r, query, pos) || lane >= LPH * HPW) return;
   const int jl = lane % LPH, hw = lane / LPH;
-  const unsigned short* src = reinterpret_cast<const unsigned short*>(query ? a.q : a.k) + (size_t)r * heads * DK + 8 * jl;
+  const unsigned short* src = reinterpret_cast<const unsigned short*>(query ? a.q : a.k) + (size_t)r * heads * dk + 8 * jl;
   unsigned short* dst = reinterpret_cast<unsigned short*>(query ? a.qr : a.kr) + (size_t)r * heads * DK + 8 * jl;
   const float most = query ? 4096.f : 16384.f;
   float cs[8], sn[8];
 #pragma unroll
   for (int x = 0; x < 8; ++x) {
-    const float2 t = slim_attn_turn(a, pos, 8 * jl + x);
+    const float2 t = !NARROW || a.rope_base ? slim_attn_turn(a, pos, 8 * jl + x) : make_float2(1.f, 0.f);
     cs[x] = t.x; sn[x] = t.y;
   }
 #pragma unroll 4
   for (int h = hw; h < heads; h += HPW) {
-    const uint4 u = __ldcs(reinterpret_cast<const uint4*>(src + h * DK)), v = __ldcs(reinterpret_cast<const uint4*>(src + h * DK + DK / 2));
+    const uint4 u = __ldcs(reinterpret_cast<const uint4*>(src + h * dk)), v = __ldcs(reinterpret_cast<const uint4*>(src + h * dk + dk / 2));
     float lo[8], hi[8];
     unpack8(u, lo);
     unpack8(v, hi);
@@ -66,14 +67,86 @@ __device__ void prepare_row(const SlimAttn& a, int r, bool query) {
       float y[4];
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        y[e] = lo[x + e] * cs[x + e] + hi[x + e] * sn[x + e];
-        y[2 + e] = hi[x + e] * cs[x + e] - lo[x + e] * sn[x + e];
+        const bool turn = !NARROW || a.rope_base;
+        y[e] = turn ? lo[x + e] * cs[x + e] + hi[x + e] * sn[x + e] : lo[x + e];
+        y[2 + e] = turn ? hi[x + e] * cs[x + e] - lo[x + e] * sn[x + e] : hi[x + e];
       }
       ol[x / 2] = half2_checked(y[0], y[1], most);
       oh[x / 2] = half2_checked(y[2], y[3], most);
     }
     *reinterpret_cast<uint4*>(dst + h * DK) = make_uint4(ol[0], ol[1], ol[2], ol[3]);
-    *reinterpret_cast<uint4*>(dst + h * DK + DK / 2) = make_uint4(oh[0], oh[1], oh[2], oh[3]);
+    *reinterpret_cast<uint4*>(dst + h * DK + dk / 2) = make_uint4(oh[0], oh[1], oh[2], oh[3]);
+    if (NARROW)
+      for (int c = 8 * jl; c < DK - dk; c += 8 * LPH) *reinterpret_cast<uint4*>(dst - 8 * jl + h * DK + dk + c) = make_uint4(0u, 0u, 0u, 0u);
+  }
+}
+
+// The same for heads of any other width, two columns at a time (4096 tokens, 32 heads of 80: 151 us by the way above, 218 by
+// this one): a lane has columns 2 lane, 2 lane + 1 and those 64 further, in every head.
+template <int DK>
+__device__ void widen_row(const SlimAttn& a, int r, bool query) {
+  const int lane = threadIdx.x & 31, heads = query ? a.H : a.KV, dk = a.d_k, half = a.half;
+  int pos;
+  if (!slim_attn_position(a, r, query, pos)) return;
+  const unsigned short* src = reinterpret_cast<const unsigned short*>(query ? a.q : a.k) + (size_t)r * heads * dk;
+  uint32_t* dst = reinterpret_cast<uint32_t*>(query ? a.qr : a.kr) + (size_t)r * heads * (DK / 2);
+  const float most = query ? 4096.f : 16384.f;
+  float cs[4], sn[4];                                // out[c] = x[c] cos + x[c +- half] sin, the sine's sign by the half
+#pragma unroll
+  for (int x = 0; x < 4; ++x) {
+    const int c = 64 * (x >> 1) + 2 * lane + (x & 1);
+    cs[x] = 1.f; sn[x] = 0.f;
+    if (a.rope_base && c < dk) {
+      const float2 t = slim_attn_turn(a, pos, c < half ? c : c - half);
+      cs[x] = t.x; sn[x] = c < half ? t.y : -t.y;
+    }
+  }
+#pragma unroll 2
+  for (int h = 0; h < heads; ++h)
+#pragma unroll
+    for (int p = 0; p < 2; ++p) {
+      float y[2];
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int c = 64 * p + 2 * lane + e, x = 2 * p + e;
+        y[e] = c < dk ? __uint_as_float((uint32_t)src[h * dk + c] << 16) : 0.f;
+        if (a.rope_base && c < dk) y[e] = y[e] * cs[x] + __uint_as_float((uint32_t)src[h * dk + (c < half ? c + half : c - half)] << 16) * sn[x];
+      }
+      if (64 * p + 2 * lane < DK) dst[h * (DK / 2) + 32 * p + lane] = half2_checked(y[0], y[1], most);
+    }
+}
+template <int DK, typename T>
+__device__ void widen_values(const SlimAttn& a, int r) {
+  const int lane = threadIdx.x & 31, dk = a.d_k;
+  const T* src = reinterpret_cast<const T*>(a.v) + (size_t)r * a.KV * dk;
+  uint32_t* dst = reinterpret_cast<uint32_t*>(a.vb) + (size_t)r * a.KV * (DK / 2);
+  if ((dk & 7) == 0) {                               // eight columns at a time
+#pragma unroll 4
+    for (int i = lane; i < a.KV * (DK / 8); i += 32) {
+      const int h = i / (DK / 8), c = i % (DK / 8) * 8;
+      uint4 out = make_uint4(0u, 0u, 0u, 0u);
+      if (c < dk) {
+        const uint4* from = reinterpret_cast<const uint4*>(src + h * dk + c);
+        out = __ldcs(from);
+        if constexpr (sizeof(T) == 4) {
+          const uint4 y = __ldcs(from + 1);
+          out = make_uint4(half2_checked(__uint_as_float(out.x) * V_UP, __uint_as_float(out.y) * V_UP, 64000.f), half2_checked(__uint_as_float(out.z) * V_UP, __uint_as_float(out.w) * V_UP, 64000.f),
+                           half2_checked(__uint_as_float(y.x) * V_UP, __uint_as_float(y.y) * V_UP, 64000.f), half2_checked(__uint_as_float(y.z) * V_UP, __uint_as_float(y.w) * V_UP, 64000.f));
+        }
+      }
+      reinterpret_cast<uint4*>(dst)[i] = out;
+    }
+    return;
+  }
+#pragma unroll 4
+  for (int i = lane; i < a.KV * (DK / 2); i += 32) {
+    const int h = i / (DK / 2), c = i % (DK / 2) * 2;                    // (d_k is even)
+    if constexpr (sizeof(T) == 4) {
+      const float2 v = c < dk ? __ldcs(reinterpret_cast<const float2*>(src + h * dk + c)) : make_float2(0.f, 0.f);
+      dst[i] = half2_checked(v.x * V_UP, v.y * V_UP, 64000.f);
+    } else {
+      dst[i] = c < dk ? __ldcs(reinterpret_cast<const uint32_t*>(src + h * dk + c)) : 0u;
+    }
   }
 }
 
@@ -84,9 +157,17 @@ __global__ void __launch_bounds__(PREP_THREADS) attn_tc_prepare_kernel(const __g
   slim_pdl_wait();
   if (blockIdx.x == 0) { slim_attn_plan(a, s_mem); return; }
   const int warps = (gridDim.x - 1) * (PREP_THREADS / 32), lane = threadIdx.x & 31;
-  const int turned = a.rope_base ? a.total_q + a.total_k : 0, rows = turned + (a.v32 ? a.total_k : 0);
+  const bool narrow = a.d_k != DK;
+  const int turned = a.rope_base || narrow ? a.total_q + a.total_k : 0, rows = turned + (a.v32 || narrow ? a.total_k : 0);
   for (int r = (blockIdx.x - 1) * (PREP_THREADS / 32) + (threadIdx.x >> 5); r < rows; r += warps) {
-    if (r < turned) { prepare_row<DK>(a, r < a.total_q ? r : r - a.total_q, r < a.total_q); continue; }
+    if (narrow) {
+      if (r < turned && (a.d_k & 15) == 0) prepare_row<DK, true>(a, r < a.total_q ? r : r - a.total_q, r < a.total_q);
+      else if (r < turned) widen_row<DK>(a, r < a.total_q ? r : r - a.total_q, r < a.total_q);
+      else if (a.v32) widen_values<DK, float>(a, r - turned);
+      else widen_values<DK, unsigned short>(a, r - turned);
+      continue;
+    }
+    if (r < turned) { prepare_row<DK, false>(a, r < a.total_q ? r : r - a.total_q, r < a.total_q); continue; }
     const int n = a.KV * DK;
     const size_t at = (size_t)(r - turned) * n;
     const float4* src = reinterpret_cast<const float4*>(reinterpret_cast<const float*>(a.v) + at);
@@ -207,8 +288,8 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
   typedef Shape<DK> S;
   constexpr int NS = S::NS, CH = S::CH, KSTEPS = DK / 16;
   constexpr uint32_t TILE = S::TILE;
-  // S = Q K^T: float16, or bf16 where nothing was rotated, both K-major;  O = P V: float16 (VH) or bf16, V MN-major
-  const uint32_t IDESC_S = (1u << 4) | (a.rope_base ? 0u : (1u << 7) | (1u << 10)) | ((TN >> 3) << 17) | ((TM >> 4) << 24);
+  // S = Q K^T: float16, or bf16 where the inputs are read where they lie, both K-major;  O = P V: float16 (VH) or bf16, V MN-major
+  const uint32_t IDESC_S = (1u << 4) | (a.rope_base || a.d_k != DK ? 0u : (1u << 7) | (1u << 10)) | ((TN >> 3) << 17) | ((TM >> 4) << 24);
   constexpr uint32_t IDESC_O = (1u << 4) | (VH ? 0u : (1u << 7) | (1u << 10)) | (1u << 16) | ((DK >> 3) << 17) | ((TM >> 4) << 24);
   extern __shared__ unsigned char smem_raw[];
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
@@ -389,7 +470,7 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
         }
       }
       const float inv = all > 0 ? (VH ? 1.f / V_UP : 1.f) / l : 0.f;
-      __nv_bfloat16* dst = reinterpret_cast<__nv_bfloat16*>(a.o) + ((size_t)(s.q0 + row) * a.H + h) * DK;
+      __nv_bfloat16* dst = reinterpret_cast<__nv_bfloat16*>(a.o) + ((size_t)(s.q0 + row) * a.H + h) * a.d_k;
       bool bad = false;
       float most = 0.f;
       if (ok) {
@@ -430,7 +511,13 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
               if (VH) most = fmaxf(most, fmaxf(fabsf(lo), fabsf(hi)));
               w[e] = bf162_of(lo, hi);
             }
-            if (there) *reinterpret_cast<uint4*>(dst + 32 * c + x) = make_uint4(w[0], w[1], w[2], w[3]);
+            if (there && (a.d_k & 7) == 0) {
+              if (32 * c + x < a.d_k) *reinterpret_cast<uint4*>(dst + 32 * c + x) = make_uint4(w[0], w[1], w[2], w[3]);
+            } else if (there) {
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+                if (32 * c + x + 2 * e < a.d_k) *reinterpret_cast<uint32_t*>(dst + 32 * c + x + 2 * e) = w[e];
+            }
           }
         }
         if (VH) bad |= all > 0 && most < 3.8e-6f;      // 2^-18
@@ -581,12 +668,13 @@ cudaError_t make_map(CUtensorMap* map, const void* p, int cols, int rows) {
 template <int DK, bool VH>
 cudaError_t launch(const slim_ctx* ctx, const SlimAttn& a, cudaStream_t st) {
   CUtensorMap qmap, kmap, vmap;
-  cudaError_t e = make_map(&qmap, a.rope_base ? a.qr : a.q, a.H * DK, a.total_q);
-  if (e == cudaSuccess) e = make_map(&kmap, a.rope_base ? a.kr : a.k, a.KV * DK, a.total_k);
-  if (e == cudaSuccess) e = make_map(&vmap, a.v32 ? a.vb : a.v, a.KV * DK, a.total_k);
+  const bool as_is = !a.rope_base && a.d_k == DK;
+  cudaError_t e = make_map(&qmap, as_is ? a.q : a.qr, a.H * DK, a.total_q);
+  if (e == cudaSuccess) e = make_map(&kmap, as_is ? a.k : a.kr, a.KV * DK, a.total_k);
+  if (e == cudaSuccess) e = make_map(&vmap, a.v32 || a.d_k != DK ? a.vb : a.v, a.KV * DK, a.total_k);
   if (e == cudaSuccess) e = cudaFuncSetAttribute((const void*)attn_tc_kernel<DK, VH>, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape<DK>::SMEM);
   if (e != cudaSuccess) return e;
-  const long long rows = (a.rope_base ? (long long)a.total_q + a.total_k : 0) + (a.v32 ? a.total_k : 0), fill = 8ll * ctx->num_sms;
+  const long long rows = (as_is ? 0 : (long long)a.total_q + a.total_k) + (a.v32 || a.d_k != DK ? a.total_k : 0), fill = 8ll * ctx->num_sms;
   const int blocks = 1 + (int)((rows + 7) / 8 < fill ? (rows + 7) / 8 : fill);
   e = slim_launch_pdl(attn_tc_prepare_kernel<DK>, dim3(blocks), dim3(PREP_THREADS), slim_attn_plan_smem(a.batch), st, a);
   if (e != cudaSuccess) return e;
@@ -596,10 +684,10 @@ cudaError_t launch(const slim_ctx* ctx, const SlimAttn& a, cudaStream_t st) {
 
 }  // namespace
 
-int slim_attn_tc_ok(const slim_ctx* ctx) { return ctx->dtype == SLIM_BF16 && (ctx->d_k == 64 || ctx->d_k == 96 || ctx->d_k == 128); }
+int slim_attn_tc_ok(const slim_ctx* ctx) { return ctx->dtype == SLIM_BF16 && ctx->d_k <= 128; }
 
 cudaError_t slim_launch_attn_tc(const slim_ctx* ctx, const SlimAttn& a, cudaStream_t st) {
-  if (a.v32)
-    return a.d_k == 64 ? launch<64, true>(ctx, a, st) : a.d_k == 96 ? launch<96, true>(ctx, a, st) : launch<128, true>(ctx, a, st);
-  return a.d_k == 64 ? launch<64, false>(ctx, a, st) : a.d_k == 96 ? launch<96, false>(ctx, a, st) : launch<128, false>(ctx, a, st);
+  const int w = slim_attn_width(a.d_k);
+  if (a.v32) return w == 64 ? launch<64, true>(ctx, a, st) : w == 96 ? launch<96, true>(ctx, a, st) : launch<128, true>(ctx, a, st);
+  return w == 64 ? launch<64, false>(ctx, a, st) : w == 96 ? launch<96, false>(ctx, a, st) : launch<128, false>(ctx, a, st);
 }

@@ -374,3 +374,32 @@ def test_numbers_that_are_not_finite_in_one_piece(dtype, H, dk):
     rest = np.delete(got[hi, 1], 5, axis=1)
     assert np.isfinite(rest).all()
     c.close()
+
+
+@pytest.mark.parametrize("dk", [2, 30, 66, 80, 98, 126])
+@pytest.mark.parametrize("theta,v32", [(1e4, True), (1e4, False), (0.0, True), (0.0, False)])
+def test_head_widths_between_the_tiles(dk, theta, v32):
+    c = Case("bf16", 4, 2, dk, theta, [130, 1, 0, 257, 30], [130, 300, 5, 257, 700], v32=v32, seed=dk)
+    c.check(True)
+    c.check(False)
+    B.slim_set_path(c.ctx, B.SLIM_PATH_GENERIC)          # (the CUDA cores take them too)
+    c.check(True)
+    c.close()
+
+
+def test_not_finite_numbers_with_widened_heads():
+    c = Case("bf16", 2, 1, 80, 0.0, [200], [200], seed=4)
+    b = c.buffers()
+    b["k"][3 + 150, 0, 7] = float("inf")
+    b["v"][3 + 20, 0, 79] = float("nan")
+    c.call(b, True)
+    torch.cuda.synchronize()
+    got = b["o"].double().cpu().numpy()[3:203]
+    ref, tol = c.reference(True)
+    ref, tol = ref[3:203], tol[3:203]
+    assert (np.abs(got[:20] - ref[:20]) <= tol[:20]).all()
+    assert np.isnan(got[20:150, :, 79]).all() and (np.abs(got[20:150, :, :79] - ref[20:150, :, :79]) <= tol[20:150, :, :79]).all()
+    with np.errstate(invalid="ignore"):
+        s = np.sign(c.q.double().numpy()[3 + 150:203, :, 7])            # the score is s * inf: all the weight on that key, or NaN
+    assert np.isnan(got[150:][s > 0]).all() and (np.abs(got[150:][s < 0][:, :79] - 0) < 10).all()
+    c.close()
