@@ -9,7 +9,7 @@ inline size_t slim_attn_plan_smem(int batch) { return sizeof(int) * ((size_t)bat
 // Where the longest query tile has more than twice the key tiles that are a CTA's share of the whole work, query tiles are split
 // along their keys into pieces of a share or somewhat more (`least` key tiles at least), whose sums are joined by the last of
 // them to finish: else a few long tiles keep their CTAs while the others have nothing left (512 queries over 8192 keys, 16
-// heads: the attention kernel 134 us in one piece, 50 in pieces).  Below that the pieces' sums cost more than they give (512
+// heads: the attention kernel 113 us in one piece, 50 in pieces).  Below that the pieces' sums cost more than they give (512
 // queries over 4096 keys and 512 over 1536, 32 heads, 1.4 shares: the call 145 us in one piece and 164 in pieces).
 // With c key tiles in a tile, H heads, n CTAs and L tiles a piece, a split tile (c > L) has less than c / L + 1 < 2 c / L pieces, and
 // L is at least H sum(c) / n, so H times all their pieces stay below 2 n.

