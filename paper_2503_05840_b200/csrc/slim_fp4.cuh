@@ -34,12 +34,13 @@ __device__ __forceinline__ float slim_fp4_at(const unsigned char* c, const unsig
 }
 
 // Scale byte of a group whose largest magnitude is amax (bad: it holds a number that is not finite): the smallest s with
-// 6 s >= amax.  6 s has at most six significant bits, so the comparison is exact.
+// 6 s >= amax.  6 s has at most six significant bits, so the comparison is exact.  amax / 6 is rounded down, both times; it
+// cannot fall behind a scale that lies below amax / 6 itself, because amax (a bf16 number, of eight bits) is 6 s or
+// further than 2^-8 of it away.
 __device__ __forceinline__ int slim_fp4_scale_byte(float amax, bool bad) {
   if (bad) return FP4_SCALE_NAN;
-  const float want = fminf(amax, 61440.f) * (1.f / 6.f);
-  int b = (int)(__half_as_ushort(__float2half_rz(want)) >> 7);     // at most one step off, either way
-  if (b > 0 && 6.f * slim_fp4_scale((unsigned char)(b - 1)) >= amax) --b;
+  const float want = __fmul_rz(fminf(amax, 61440.f), 0x1.555554p-3f);      // (the float32 below 1/6)
+  int b = (int)(__half_as_ushort(__float2half_rz(want)) >> 7);     // the scale or the one before it
   if (b < FP4_SCALE_MAX && 6.f * slim_fp4_scale((unsigned char)b) < amax) ++b;
   return b;
 }

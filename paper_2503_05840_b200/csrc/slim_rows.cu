@@ -7,6 +7,7 @@
 // read back 69 us (5.7 TB/s, 0.87 of a copy); 31k rows in pages read in 54 us; 16 rows 5 us either way (three dependent
 // loads: start, position, page).
 #include "slim_fp4.cuh"
+#include "slim_ptx.cuh"
 
 namespace {
 
@@ -49,6 +50,14 @@ __device__ long long rows_target(const RowsArgs& a, int r) {
   return (long long)pg * a.page_rows + t % a.page_rows;
 }
 
+// The warp's row and part of it (below 2^31 warps: at most 2^30 rows, and parts only where they are few)
+__device__ __forceinline__ bool rows_share(const RowsArgs& a, int& r, int& part) {
+  const unsigned w = blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5), parts = (unsigned)a.parts;
+  r = (int)(parts == 1 ? w : w / parts);
+  part = (int)(w - (unsigned)r * parts);
+  return r < a.total;
+}
+
 // Starts of packed sequences that do not ascend from 0 to at most `total` are reported (their rows are left out above).
 // By the last block, which has no rows.
 __device__ void rows_check(const RowsArgs& a) {
@@ -66,7 +75,7 @@ __device__ __forceinline__ uint4 load8(const unsigned short* row, int col, int d
 }
 
 // Eight keys and the largest magnitude of their group -> codes and the scale byte.
-// Codes are rounded by the conversion instruction, from k / s as k times the reciprocal of s.  That is off by some 2^-23,
+// Codes are rounded by the conversion instruction, from k / s as k times the reciprocal of s.  That is off by some 2^-22,
 // which only matters on a border between two codes (k is a bf16 number, of 8 bits, and border times scale has 7: k / s is the
 // border itself or further than 2^-8 of it away).  Rounding to multiples of 2^-12 first brings the border's quotients
 // back onto it and leaves the others on their side.
@@ -74,14 +83,16 @@ __device__ __forceinline__ uint32_t quantise8(const uint4& v, float amax, int& b
   const bool bad = !(amax <= 3.4028234663852886e38f);
   byte = slim_fp4_scale_byte(amax, bad);
   const float s = slim_fp4_scale((unsigned char)byte);
-  const float up = bad || !(amax > 0.f) ? 0.f : __frcp_rn(s);
-  const float magic = 0x1.8p11f;                                       // float32 steps of 2^-12 around it
+  const float up = bad || !(amax > 0.f) ? 0.f : __fdividef(1.f, s);
+  const slim_ptx::f32x2 up2 = slim_ptx::pack2(up, up), magic = slim_ptx::pack2(0x1.8p11f, 0x1.8p11f);      // float32 steps of 2^-12 around it
+  const slim_ptx::f32x2 back = slim_ptx::pack2(-0x1.8p11f, -0x1.8p11f);
   const uint32_t w[4] = {v.x, v.y, v.z, v.w};
   float y[8];
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
-    y[2 * e] = (__uint_as_float(w[e] << 16) * up + magic) - magic;
-    y[2 * e + 1] = (__uint_as_float(w[e] & 0xffff0000u) * up + magic) - magic;
+    const slim_ptx::f32x2 k = slim_ptx::pack2(__uint_as_float(w[e] << 16), __uint_as_float(w[e] & 0xffff0000u));
+    const slim_ptx::f32x2 z = slim_ptx::add2(slim_ptx::fma2(k, up2, magic), back);
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(y[2 * e]), "=f"(y[2 * e + 1]) : "l"(z));
   }
   const uint32_t out = slim_fp4_encode8(y);
   if (bad) return 0u;
@@ -97,13 +108,11 @@ __global__ void __launch_bounds__(256) rows_quantise_kernel(const RowsArgs a) {
   slim_pdl_wait();
   rows_check(a);
   const int lane = threadIdx.x & 31;
-  const long long w = (long long)blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5);
-  const long long rr = w / a.parts;
-  if (rr >= a.total) return;
-  const int part = (int)(w - rr * a.parts);
+  int rr, part;
+  if (!rows_share(a, rr, part)) return;
   const unsigned short* src = reinterpret_cast<const unsigned short*>(a.wide) + (size_t)rr * a.d;
   const bool whole = (a.d & 7) == 0 && ((uintptr_t)a.wide & 15) == 0;
-  const long long row = rows_target(a, (int)rr);
+  const long long row = rows_target(a, rr);
   if (row < 0) return;
   unsigned char* dst = a.codes + (size_t)row * a.pitch;
   unsigned char* sdst = a.scales + (size_t)row * a.spitch;
@@ -141,11 +150,9 @@ __global__ void __launch_bounds__(256) rows_expand_kernel(const RowsArgs a) {
   slim_pdl_wait();
   rows_check(a);
   const int lane = threadIdx.x & 31;
-  const long long w = (long long)blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5);
-  const long long rr = w / a.parts;
-  if (rr >= a.total) return;
-  const int part = (int)(w - rr * a.parts);
-  const long long row = rows_target(a, (int)rr);
+  int rr, part;
+  if (!rows_share(a, rr, part)) return;
+  const long long row = rows_target(a, rr);
   if (row < 0) return;
   unsigned short* dst = reinterpret_cast<unsigned short*>(a.wide) + (size_t)rr * a.d;
   const unsigned char* src = a.codes + (size_t)row * a.pitch;
@@ -187,11 +194,9 @@ __global__ void __launch_bounds__(256) rows_copy_kernel(const RowsArgs a, int to
   slim_pdl_wait();
   rows_check(a);
   const int lane = threadIdx.x & 31;
-  const long long w = (long long)blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5);
-  const long long rr = w / a.parts;
-  if (rr >= a.total) return;
-  const int part = (int)(w - rr * a.parts);
-  const long long row = rows_target(a, (int)rr);
+  int rr, part;
+  if (!rows_share(a, rr, part)) return;
+  const long long row = rows_target(a, rr);
   if (row < 0) return;
   const int units = a.pitch / (int)sizeof(U);
   U* cache = reinterpret_cast<U*>(a.codes + (size_t)row * a.pitch);
