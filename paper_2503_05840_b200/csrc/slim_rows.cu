@@ -3,9 +3,9 @@
 //
 // What HBM has to move: a row of d bf16 keys (2 d bytes) one way and d/2 + d/32 bytes the other.  A warp takes 256 columns of a row at a time, four such chunks in flight: 16 bytes a lane on the wide
 // side, one 32-bit word of eight codes on the other; four lanes share a scale.
-// Measured, rows of 4096: 37.5k rows written 107 us (389 MB, 3.6 TB/s: the issue slots are 79 % full, the rounding's steps) and
-// read back 69 us (5.7 TB/s, 0.87 of a copy); 31k rows in pages read in 54 us; 16 rows 5 us either way (three dependent
-// loads: start, position, page).
+// Measured, rows of 4096: 37.5k rows written 92 us (389 MB, 4.2 TB/s: the issue slots are 77 % full, the rounding's steps; more
+// warps an SM changed nothing) and read back 65 us (6.0 TB/s, 0.92 of a copy); 31k rows in pages read in 54 us; 16 rows 5 us
+// either way (three dependent loads: start, position, page).
 #include "slim_fp4.cuh"
 #include "slim_ptx.cuh"
 
