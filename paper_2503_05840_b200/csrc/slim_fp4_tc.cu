@@ -17,9 +17,12 @@
 //   MMA thread   of the even CTA: U^T[256 columns x 32 heads] += K^T[256 x 16] P^T[16 x 32] a pair of 128-column chunks, each
 //                CTA supplying its own 128 columns and its own 16 heads' P (cta_group::2), so no probabilities travel; the odd
 //                CTA's passes on that its tile is complete
-// float16 P: the reference is the first tile's maximum plus 8 (log2 units), so p reaches up to 2^15 for scores 23 above that
-// maximum and keeps 11 bits down to 2^-14; smaller ones lose bits against terms 2^6 their size.  A score further up flags
-// the unit; flagged units are walked again at the end, with the largest score as reference (known by then).
+// float16 P keeps its 11 bits from 2^-14 up to 2^15, so the reference m of a unit has to leave room on both sides: m is the mean
+// of the first tile's scores plus 2 (log2 units), or its maximum less 11 where that is more.  Without a dominant key scores
+// may then come out 15 above and 14 below the second; with one in the first tile (the first token of a context often is)
+// 4 above it, and down to 25 below.  A unit is flagged by a score further up, or where the probabilities below 2^-14 are more
+// than 2^-20 of l (float32 sums; what is lost stays below that).  Flagged units are walked again at the end, with the largest
+// score, known by then, less 14 as reference: 11 bits down to 2^-28 of the largest probability, steps of 2^-38 of it below.
 //
 // Bound by the score warps.  A tile of 16 x 2048 keys takes a CTA 2650 clocks: a warp issues some 600 instructions for two
 // heads (64 conversions of codes, 64 products with the scale, 128 of the rotation, 16 m16n8k16, 16 stores), two warps share a
@@ -41,7 +44,8 @@ namespace {
 
 constexpr int MAX_ST = 4, MAX_PK = 8;    // float16 stages, stages of packed tiles
 constexpr int RESEED = 64;
-constexpr float BIAS = 8.f, XMAX = 15.f;
+constexpr float XMAX = 15.f, XMIN = -14.f;            // log2 of the probabilities that float16 holds with all its bits
+constexpr float ABOVE_MEAN = 2.f, BELOW_MAX = 11.f, TOP = 14.f, LOST = 0x1p-20f;
 
 // How a thread's pairs lie: pieces of PE consecutive columns of the first half of the head, and the same of the second
 template <int DK>
@@ -128,8 +132,9 @@ __global__ void __launch_bounds__(MAXT, 1) fp4_tc_kernel(const __grid_constant__
   volatile int* s_abort = reinterpret_cast<volatile int*>(misc + 4);
   float* s_xm = reinterpret_cast<float*>(misc + 8);           // [16] reference, from the set that has a unit's first tile
   float* s_xl = s_xm + 16;                                    // [16] the other set's share of l
-  float* s_xx = s_xl + 16;                                    // [16] and its largest score
-  int* s_prefix = reinterpret_cast<int*>(s_xx + 16);
+  float* s_xx = s_xl + 16;                                    // [16] its largest score
+  float* s_xs = s_xx + 16;                                    // [16] and its sum of small probabilities
+  int* s_prefix = reinterpret_cast<int*>(s_xs + 16);
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const uint32_t rank = cluster_ctarank();
   const int w = blockIdx.x / 2;
@@ -240,7 +245,7 @@ __global__ void __launch_bounds__(MAXT, 1) fp4_tc_kernel(const __grid_constant__
         const int len = min(max(p.lengths[b], 0), p.t_cap);
         const int kt0 = g.sets == 1 ? 0 : ((set - it) & 1);          // this set's first tile of the unit
         const bool owner = kt0 == 0;
-        float qs = 1.f, mref = 0.f, lsum = 0.f, rmax = -INFINITY;    // of the thread's head
+        float qs = 1.f, mref = 0.f, lsum = 0.f, lsub = 0.f, rmax = -INFINITY;    // of the thread's head
         // The warp's queries at position pos, divided by a power of two a head
         auto seed = [&](int pos) {
           f32x2 c = pack2(1.f, 1.f), s = pack2(0.f, 0.f), ns = s;
@@ -402,12 +407,15 @@ __global__ void __launch_bounds__(MAXT, 1) fp4_tc_kernel(const __grid_constant__
             const bool v = scores && (odd ? in1 : in0);
             if (kt == kt0) {
               if (sweep == 1) {
-                if (scores) mref = __ldcg(umax + (size_t)unit * p.H + (int)rank * g.hl + hd0 + mine);
+                if (scores) mref = __ldcg(umax + (size_t)unit * p.H + (int)rank * g.hl + hd0 + mine) - TOP;
               } else if (owner) {
-                float mx = v ? s : -INFINITY;
+                float mx = v ? s : -INFINITY, mean = v ? s : 0.f;
 #pragma unroll
-                for (int o = 1; o < 32; o = o == 1 ? 4 : 2 * o) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
-                mref = mx + BIAS;
+                for (int o = 1; o < 32; o = o == 1 ? 4 : 2 * o) {
+                  mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+                  mean += __shfl_xor_sync(0xffffffffu, mean, o);
+                }
+                mref = fmaxf(mean / (float)min(SLIM_TT, len - t0) + ABOVE_MEAN, mx - BELOW_MAX);      // (a NaN leaves the maximum)
                 if (g.sets == 2) {
                   if (speaks) s_xm[hd0 + mine] = mref;
                   __syncwarp();
@@ -425,7 +433,9 @@ __global__ void __launch_bounds__(MAXT, 1) fp4_tc_kernel(const __grid_constant__
             float xv = s - mref;
             if (v && xv > XMAX && sweep == 0) p.unit_flags[2 * unit + (int)rank] = 1;
             xv = xv > XMAX ? XMAX : xv;
-            const __half pv = __float2half_rn(v ? ex2_approx(xv) : 0.f);
+            const float pf = v ? ex2_approx(xv) : 0.f;
+            if (xv < XMIN) lsub += pf;
+            const __half pv = __float2half_rn(pf);
             if (scores) {
               lsum += __half2float(pv);
               sts_u16(s_p + (uint32_t)(rk.st * 512) + p_off, __half_as_ushort(pv));
@@ -446,6 +456,7 @@ __global__ void __launch_bounds__(MAXT, 1) fp4_tc_kernel(const __grid_constant__
 #pragma unroll
           for (int o = 1; o < 32; o = o == 1 ? 4 : 2 * o) {
             lsum += __shfl_xor_sync(0xffffffffu, lsum, o);
+            lsub += __shfl_xor_sync(0xffffffffu, lsub, o);
             rmax = fmaxf(rmax, __shfl_xor_sync(0xffffffffu, rmax, o));
           }
           if (g.sets == 2) {
@@ -458,12 +469,13 @@ __global__ void __launch_bounds__(MAXT, 1) fp4_tc_kernel(const __grid_constant__
               ok = __all_sync(0xffffffffu, ok);
               if (!ok) break;
               lsum += s_xl[hd0 + mine];
+              lsub += s_xs[hd0 + mine];
               rmax = fmaxf(rmax, s_xx[hd0 + mine]);
             } else {
               ok = mbar_wait<false>(b_xm, uc & 1, s_abort, p.status);
               ok = __all_sync(0xffffffffu, ok);
               if (!ok) break;
-              if (speaks) { s_xl[hd0 + mine] = lsum; s_xx[hd0 + mine] = rmax; }
+              if (speaks) { s_xl[hd0 + mine] = lsum; s_xs[hd0 + mine] = lsub; s_xx[hd0 + mine] = rmax; }
               __syncwarp();
               if (lane == 0) mbar_arrive(b_xl);
             }
@@ -472,7 +484,10 @@ __global__ void __launch_bounds__(MAXT, 1) fp4_tc_kernel(const __grid_constant__
             const size_t at = (size_t)unit * p.H + (int)rank * g.hl + hd0 + mine;
             p.part_m[at] = mref;
             p.part_l[at] = lsum;
-            if (sweep == 0) umax[at] = rmax;
+            if (sweep == 0) {
+              umax[at] = rmax;
+              if (lsub > LOST * lsum) p.unit_flags[2 * unit + (int)rank] = 1;
+            }
           }
         }
         if (warp < nepi) {
@@ -638,7 +653,7 @@ bool make_geom(int d, int H, int d_k, int batch, Geom& g) {
   g.tmem_cols = cols;
   g.pk = (8 * g.dsl + 16 * g.win + 1023) & ~1023;
   const int qbytes = g.sets * g.hl * 8 * (d_k == 128 ? Lane<128>::SB : d_k == 96 ? Lane<96>::SB : Lane<64>::SB);
-  const int fixed = 1024 + qbytes + 8 * (2 * MAX_PK + 3 * MAX_ST + 4) + 8 + 4 * 48 + 4 * (batch + 1) + 64;
+  const int fixed = 1024 + qbytes + 8 * (2 * MAX_PK + 3 * MAX_ST + 4) + 8 + 4 * 64 + 4 * (batch + 1) + 64;
   // two float16 stages at least; more of them, and of packed ones, while they fit
   g.nst = 2; g.npk = 2;
   auto total = [&](int st, int pk) { return fixed + st * (g.stage + 512) + pk * g.pk; };

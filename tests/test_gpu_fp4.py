@@ -500,3 +500,42 @@ def test_offsets_beyond_32_bits(d, H, t_cap):
         q = torch.randn(2, d, generator=g).bfloat16()
         _check(layer, q, [want.numpy()[:0], want.numpy()], W, H, 0.0, [0, 50])
     layer.close()
+
+
+@pytest.mark.parametrize("d,H,d_k", [(512, 4, 128), (256, 2, 128), (2816, 22, 128), (1280, 20, 64), (1536, 16, 96), (4096, 32, 128), (500, 5, 100)])
+@pytest.mark.parametrize("where", ["first", "tenth", "last"])
+def test_keys_beside_a_dominant_one_keep_their_weight(d, H, d_k, where):
+    """One key 7 to 17 nats above thousands of others, which alone hold values in most columns: those columns are what the others make of them."""
+    lengths, dom = [9000, 20, 9000], {"first": 0, "tenth": 9, "last": 8999}[where]
+    g = torch.Generator().manual_seed(d)
+    layer = SlimLayer(d, H, d_k, 0.0, "fp4", 3, 9000, DEV)
+    layer.set_wkv(np.eye(d))
+    # A head's score is its column 0 times a query's only element.  Keys are values of the format with scale 1, so scores are exact.
+    gap = 7 + (torch.arange(H) * 3 % 11).float()                                # nats
+    x = torch.tensor([0.5, 1, 1.5, 2, 3, 4, 6])[torch.randint(0, 7, (sum(lengths), H, d_k), generator=g)]
+    x[:, :, 0] = torch.tensor([-0.5, 0, 0, 0.5])[torch.randint(0, 4, (sum(lengths), H), generator=g)]
+    x.view(-1, d)[:, 5::32] = 6                                                 # (a group's largest)
+    for s in (0, lengths[0] + lengths[1]):
+        x[s + dom] = 0
+        x[s + dom, :, 0] = 6
+    q = torch.zeros(3, H, d_k)
+    q[:, :, 0] = gap * d_k ** 0.5 / 6
+    q = q.bfloat16()
+    x = x.reshape(-1, d).bfloat16()
+    layer.append_rows(x.to(DEV), _i32([0] * 3), _i32(_starts(lengths)))
+    o = torch.empty(3, d, device=DEV)
+    layer.decode_typed(q.view(3, d).to(DEV), _i32(lengths), o=o)
+    K = layer.read_rows(_i32([0] * 3), _i32(_starts(lengths)), sum(lengths)).double()
+    assert layer.device_status() == B.SLIM_OK
+    for b, (lo, hi) in enumerate(zip(_starts(lengths)[:-1], _starts(lengths)[1:])):
+        Kb, qb = K[lo:hi], q[b].to(DEV).double()
+        p = torch.softmax(torch.einsum("thc,hc->ht", Kb.view(-1, H, d_k), qb) / d_k ** 0.5, 1)
+        for h in range(H):
+            c = slice(h * d_k, (h + 1) * d_k)
+            want, ua = p[h] @ Kb[:, c], p[h] @ Kb.abs()
+            # Scores in float32, up to 25 log2 units: 2^-18, in the sum and beside it.  Probabilities in 11 bits, likewise.  The
+            # projection's operands are two terms of 11 bits, steps of 2^-24 of the row's largest; float32 sums of 9000 and d terms in
+            # any order, 2^-24 each (their errors are averaged: a hundred steps).
+            tol = (2 * 2.0 ** -18 + 2 * 2.0 ** -11 + 100 * 2.0 ** -24) * ua[c] + 2.0 ** -22 * ua.max()
+            assert ((o[b, c].double() - want).abs() <= tol).all(), (b, h, float(gap[h]), ((o[b, c].double() - want).abs() / tol).max())
+    layer.close()
