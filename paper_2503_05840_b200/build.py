@@ -11,7 +11,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libslim.so")
 SOURCES = ["slim_api.cu", "slim_generic.cu", "slim_tail.cu", "slim_wkv.cu", "slim_tc.cu", "slim_proj.cu", "slim_xscores.cu", "slim_prompt.cu", "slim_split.cu",
            "slim_tree.cu", "slim_tree_tc.cu", "slim_draft.cu", "slim_budget.cu", "slim_rows.cu", "slim_fp4.cu", "slim_fp4_tc.cu", "slim_attn.cu", "slim_attn_tc.cu"]
-HEADERS = ["slim_internal.h", "slim_sched.cuh", "slim_ptx.cuh", "slim_combine.cuh", "slim_tree.h", "slim_fp4.cuh", "slim_attn.h", "slim_attn_plan.cuh"]
+HEADERS = ["slim_internal.h", "slim_sched.cuh", "slim_ptx.cuh", "slim_combine.cuh", "slim_tree.h", "slim_fp4.cuh", "slim_attn.h", "slim_attn_plan.cuh", "slim_attn_tile.cuh"]
 FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
          "-Xcompiler", "-fPIC"]
 

@@ -31,9 +31,10 @@ struct SlimAttn {
   int slots;                     // pieces times heads whose sums fit the workspace (0: nothing is split)
   float* part;                   // [slots][tile_rows][columns + 2]: sums of the pieces (a kernel's own order)
   int* arrivals;                 // [slots][8]
+  uint32_t* redo;                // tensor cores: rows to be formed once more, a bit each, 8 words an item and head
 };
 
-struct SlimAttnLayout { size_t qr, kr, vb, tiles, n_tiles, part, arrivals, total; };
+struct SlimAttnLayout { size_t qr, kr, vb, tiles, n_tiles, part, arrivals, redo, total; };
 
 // Columns that a head has on the tensor cores
 __host__ __device__ inline int slim_attn_width(int d_k) { return d_k <= 64 ? 64 : d_k <= 96 ? 96 : 128; }
@@ -74,65 +75,5 @@ __device__ __forceinline__ float2 slim_attn_turn(const SlimAttn& a, int pos, int
 }
 __device__ __forceinline__ float slim_attn_ld(const void* p, size_t i, int f32) {
   return f32 ? __ldg(reinterpret_cast<const float*>(p) + i) : __bfloat162float(__ldg(reinterpret_cast<const __nv_bfloat16*>(p) + i));
-}
-
-// One output row by one warp, from the inputs themselves, in float32: for the rows that the tiled kernels leave with a
-// number that is not finite.  Those come from keys and values that the row does not attend but shares a tile with
-// (0 times infinity), from keys beyond float16, or from what the row does attend; here only the last reach it.
-static __device__ __noinline__ void slim_attn_row(const SlimAttn& a, int b, int i, int h) {
-  const SlimSeq s = slim_attn_seq(a, b);
-  const int lane = threadIdx.x & 31, kvh = h / (a.H / a.KV), dk = a.d_k, half = a.half;
-  const int n = slim_attn_keys(a, s, i), qpos = i + s.nk - s.nq;
-  const size_t qi = ((size_t)(s.q0 + i) * a.H + h) * dk;
-  float m = -INFINITY, l = 0.f, acc[8];
-#pragma unroll
-  for (int x = 0; x < 8; ++x) acc[x] = 0.f;
-  for (int t0 = 0; t0 < n; t0 += 32) {
-    const int t = t0 + lane;
-    float sv = -INFINITY;
-    if (t < n) {
-      const size_t ki = ((size_t)(s.k0 + t) * a.KV + kvh) * dk;
-      sv = 0.f;
-      for (int j = 0; j < half; ++j) {
-        float q1 = slim_attn_ld(a.q, qi + j, a.f32), q2 = slim_attn_ld(a.q, qi + j + half, a.f32);
-        float k1 = slim_attn_ld(a.k, ki + j, a.f32), k2 = slim_attn_ld(a.k, ki + j + half, a.f32);
-        if (a.rope_base) {
-          const float2 cq = slim_attn_turn(a, qpos, j), ck = slim_attn_turn(a, t, j);
-          const float x1 = q1 * cq.x + q2 * cq.y, x2 = q2 * cq.x - q1 * cq.y, y1 = k1 * ck.x + k2 * ck.y, y2 = k2 * ck.x - k1 * ck.y;
-          q1 = x1; q2 = x2; k1 = y1; k2 = y2;
-        }
-        sv += q1 * k1 + q2 * k2;
-      }
-      sv *= a.qscale;
-    }
-    float mx = sv;
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
-    const float m_new = fmaxf(m, mx);
-    const float p = sv == -INFINITY ? 0.f : exp2f(sv - m_new);
-    const float alpha = m == m_new ? 1.f : exp2f(m - m_new);
-    float ps = p;
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) ps += __shfl_xor_sync(0xffffffffu, ps, o);
-    l = l * alpha + ps;
-    m = m_new;
-#pragma unroll
-    for (int x = 0; x < 8; ++x) acc[x] *= alpha;
-    for (int u = 0; u < 32 && t0 + u < n; ++u) {
-      const float pu = __shfl_sync(0xffffffffu, p, u);
-      const size_t vi = ((size_t)(s.k0 + t0 + u) * a.KV + kvh) * dk;
-#pragma unroll
-      for (int x = 0; x < 8; ++x)
-        if (lane + 32 * x < dk) acc[x] = fmaf(pu, slim_attn_ld(a.v, vi + lane + 32 * x, a.v32), acc[x]);
-    }
-  }
-#pragma unroll
-  for (int x = 0; x < 8; ++x) {
-    if (lane + 32 * x < dk) {
-      const float y = n > 0 ? acc[x] / l : 0.f;
-      if (a.f32) reinterpret_cast<float*>(a.o)[qi + lane + 32 * x] = y;
-      else reinterpret_cast<__nv_bfloat16*>(a.o)[qi + lane + 32 * x] = __float2bfloat16_rn(y);
-    }
-  }
 }
 #endif

@@ -14,9 +14,10 @@
 //   The reference m of a row moves only when its maximum has grown by more than 2^8: then its warp multiplies the row of O
 //   (and l) by 2^(m - m'); P stays below 2^8 otherwise, which float32 sums do not mind.
 //   What float16 cannot hold (|q| > 4096, |k| > 16384, |v| > 4000, numbers that are not finite) enters as NaN, and rows that
-//   come out not finite are computed once more by slim_attn_row; so are rows that share a tile with a value that is not
-//   finite and that they do not attend (0 times infinity).  Float32 values enter times 16: float16's smallest step is then
-//   2^-28, and rows whose outputs all stay below 2^-18 are computed once more as well.
+//   come out not finite are formed once more on the CUDA cores, in float32 from the inputs; so are rows that share a tile with
+//   a value that is not finite and that they do not attend (0 times infinity).  Float32 values enter times 16: float16's
+//   smallest step is then 2^-28, and rows whose outputs all stay below 2^-18 are formed once more as well.  A CTA does that
+//   behind its last item, when none of its warps waits for another one any more: it may take long.
 // Tiles of 2 x 128 queries: both take each tile of keys from shared memory, and tensor memory holds exactly S and O of two.
 // Bound by the softmax: for d_k = 128 a pair of 128 x 128 tiles costs the tensor core 1024 clocks for S and 1024 for O, the
 // exponentials about 1500 of the special-function unit a scheduler (a quarter of them go to the FMA pipe for that reason), with
@@ -29,6 +30,7 @@
 
 #include "slim_attn.h"
 #include "slim_attn_plan.cuh"
+#include "slim_attn_tile.cuh"
 #include "slim_ptx.cuh"
 
 using namespace slim_ptx;
@@ -289,6 +291,32 @@ __device__ __forceinline__ void exponentials(uint32_t (&r)[TN], f32x2 scale2, f3
   }
 }
 
+// Number of a CTA's item r: the list, most keys first, is dealt out in rounds of alternating direction.
+__device__ __forceinline__ long long item_place(int r) {
+  return (long long)r * gridDim.x + (r & 1 ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
+}
+
+// Rows of a CTA's items once more, tiles of 64, by the first 256 threads, which meet at barrier 1
+template <int DK>
+__device__ __noinline__ void again(const SlimAttn& a, float* smem) {
+  typedef SlimAttnTile<DK == 64 ? 64 : 128, 64, true> Tile;
+  static_assert(Tile::SMEM <= (2 + Shape<DK>::NS) * Shape<DK>::TILE, "fits the operands' place");
+  const int n_items = *a.n_tiles * a.H;
+  for (int r = 0; item_place(r) < n_items; ++r) {
+    const int tile = (int)(item_place(r) / a.H), h = (int)(item_place(r) - (long long)tile * a.H);
+    const int4 x = a.tiles[3 * tile], y = a.tiles[3 * tile + 1];
+    const SlimSeq s = {y.x, y.y, y.z, y.w};
+    for (int i = 0; i < SLIM_ATTN_TC_ROWS / 64; ++i) {
+      const uint2 which = *reinterpret_cast<const uint2*>(a.redo + 8 * item_place(r) + 2 * i);
+      if (!(which.x | which.y)) continue;
+      const int row0 = x.y + 64 * i, rows = min(64, s.nq - row0);
+      Tile t;
+      t.run(a, s, row0, rows, h, 0, 0x7fffffff, smem, 1);
+      t.store(a, s, row0, rows, h, (unsigned long long)which.y << 32 | which.x);
+    }
+  }
+}
+
 template <int DK, bool VH>
 __global__ void __launch_bounds__(THREADS, 1)
 attn_tc_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap,
@@ -310,6 +338,7 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
   unsigned char* misc = sm + (bar_ph + 16 - base);
   uint32_t* s_tmem = reinterpret_cast<uint32_t*>(misc);
   volatile int* s_abort = reinterpret_cast<volatile int*>(misc + 4);
+  volatile int* s_redo = reinterpret_cast<volatile int*>(misc + 8);        // some item has rows to be formed once more
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
 
   if (tid == 0) {
@@ -319,6 +348,7 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
     mbar_init(bar_qe, 1);
     for (int i = 0; i < 2; ++i) { mbar_init(bar_s + 8 * i, 1); mbar_init(bar_ph + 8 * i, 4); mbar_init(bar_p + 8 * i, 4); mbar_init(bar_o + 8 * i, 1); }
     *s_abort = 0;
+    *s_redo = 0;
     fence_mbar_init();
   }
   if (warp == 8) tmem_alloc(smem_u32(s_tmem), 512);
@@ -329,15 +359,14 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
   slim_pdl_trigger();
   slim_pdl_wait();
   const int n_items = *a.n_tiles * a.H, share = a.H / a.KV;
-  // Item number r of this CTA: the list, most keys first, is dealt out in rounds of alternating direction.
-  struct Item { SlimSeq s; int b, row0, h, nt0, nt1, first, piece, pieces, slot; };
+  struct Item { SlimSeq s; int row0, h, nt0, nt1, first, piece, pieces, slot; };
   auto item = [&](int r, Item& it) {
-    const long long at = (long long)r * gridDim.x + (r & 1 ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
+    const long long at = item_place(r);
     if (at >= n_items) return false;
     const int tile = (int)(at / a.H);
     it.h = (int)(at - (long long)tile * a.H);
     const int4 x = __ldg(a.tiles + 3 * tile), y = __ldg(a.tiles + 3 * tile + 1), z = __ldg(a.tiles + 3 * tile + 2);
-    it.b = x.x; it.row0 = x.y; it.piece = x.z; it.pieces = x.w;
+    it.row0 = x.y; it.piece = x.z; it.pieces = x.w;
     it.s.q0 = y.x; it.s.nq = y.y; it.s.k0 = y.z; it.s.nk = y.w;
     it.first = z.x; it.slot = z.z;
     // key tiles of the two query tiles, within the piece (the second may have no rows)
@@ -465,6 +494,7 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
         int before = 0;
         if (lane == 0 && ok) before = atomicAdd(a.arrivals + 8 * slot0 + warp, 1);
         before = __shfl_sync(0xffffffffu, before, 0);
+        if (lane == 0) a.redo[8 * item_place(r_) + warp] = 0u;
         if (!ok || before != it.pieces - 1) continue;
         __threadfence();
         const float* from = a.part + slot0 * SLOT;
@@ -529,15 +559,17 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
           }
         }
         if (VH) bad |= all > 0 && most < 3.8e-6f;      // 2^-18
-        unsigned redo = __ballot_sync(0xffffffffu, bad && there);
-        while (redo) {
-          const int x = __ffs(redo) - 1;
-          redo &= redo - 1;
-          __syncwarp();
-          slim_attn_row(a, it.b, it.row0 + i * TM + (warp & 3) * 32 + x, h);
+        const unsigned redo = __ballot_sync(0xffffffffu, bad && there);
+        __syncwarp();
+        if (lane == 0) {
+          a.redo[8 * item_place(r_) + warp] = redo;
+          if (redo) *s_redo = 1;
         }
       }
     }
+    // ---- rows once more: the operands' shared memory is free, the eight warps are together ----
+    asm volatile("bar.sync 1, 256;" ::: "memory");
+    if (*s_redo && !*s_abort) again<DK>(a, reinterpret_cast<float*>(sm));
   } else if (warp == 8) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
     // =========================== MMA issuer ===========================

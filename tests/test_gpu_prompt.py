@@ -403,3 +403,64 @@ def test_not_finite_numbers_with_widened_heads():
         s = np.sign(c.q.double().numpy()[3 + 150:203, :, 7])            # the score is s * inf: all the weight on that key, or NaN
     assert np.isnan(got[150:][s > 0]).all() and (np.abs(got[150:][s < 0][:, :79] - 0) < 10).all()
     c.close()
+
+
+def _beyond_float16(c, starts):
+    """A key that float16 cannot hold at these rows, in a column that queries hardly look at: every row that attends one is formed again."""
+    c.q[:, :, [1, 1 + c.dk // 2]] *= 2.0 ** -14
+    c.k[starts, :, 1] = 20000.0
+
+
+@pytest.mark.parametrize("H,KV,dk,v32", [(4, 2, 128, False), (4, 1, 128, True), (3, 3, 96, True), (6, 2, 64, False), (2, 1, 80, False), (2, 2, 80, True)])
+@pytest.mark.parametrize("causal", [True, False])
+def test_rows_formed_again_of_many_items(H, KV, dk, v32, causal):
+    """More items than CTAs, some in pieces; all rows of some sequences are formed again, and what a key behind them touches of others."""
+    nq = [300, 1, 65, 190, 0, 64] + [70] * 75
+    nk = [2600, 900, 65, 190, 5, 20] + [70] * 75
+    c = Case("bf16", H, KV, dk, 1e4, nq, nk, v32=v32, seed=dk, max_k=4300)
+    _beyond_float16(c, [int(c.cu_k[b]) for b in range(0, len(nk), 3)] + [int(c.cu_k[1]) + 250, int(c.cu_k[4 + 1]) + 11])
+    c.check(causal)
+    c.close()
+
+
+def test_rows_formed_again_of_long_keys_do_not_hold_up_the_others():
+    """Every row over many keys is formed again; the call ends with all rows written and no wait run out."""
+    nq, nk = [300, 40] * 3, [60000, 20] * 3
+    c = Case("bf16", 8, 1, 64, 1e4, nq, nk, v32=False, seed=1)
+    _beyond_float16(c, [int(x) for x in c.cu_k[:-1]])
+    b = c.buffers()
+    c.call(b, True)
+    torch.cuda.synchronize()
+    assert B.slim_device_status(c.ctx) == B.SLIM_OK
+    got = b["o"].double().cpu().numpy()
+    for s in (1, 4, 5):
+        lo = int(c.cu_q[s])
+        rows = np.arange(lo + nq[s] - 3, lo + nq[s])
+        o, pv, qk = po.attention(c.q[rows].float().numpy(), c.k[c.cu_k[s]:c.cu_k[s + 1]].float().numpy(), c.v[c.cu_k[s]:c.cu_k[s + 1]].float().numpy(), 1e4, True)
+        # float32 throughout; the output rounded once
+        assert (np.abs(got[rows] - o) <= (2 * (2.0 ** -20 * qk[..., None] + 2.0 ** -18)) * pv + 2.0 ** -8 * np.abs(o)).all()
+    c.close()
+
+
+def test_rows_formed_again_take_the_time_of_the_cuda_cores():
+    """Rows that the tensor cores cannot form are formed by tiles as on the path without them (one by one they took 20 times as long and more)."""
+    c = Case("bf16", 8, 8, 128, 1e4, [4096], [4096], v32=False, lead=0)
+    _beyond_float16(c, [0])
+    b = c.buffers()
+
+    def time():
+        t = []
+        for _ in range(4):
+            e = [torch.cuda.Event(enable_timing=True) for _ in range(2)]
+            e[0].record()
+            c.call(b, True)
+            e[1].record()
+            torch.cuda.synchronize()
+            t.append(e[0].elapsed_time(e[1]))
+        return min(t[1:])
+
+    auto = time()
+    B.slim_set_path(c.ctx, B.SLIM_PATH_GENERIC)
+    generic = time()
+    assert auto < 10 * generic, (auto, generic)
+    c.close()
