@@ -143,6 +143,13 @@ void shape_of(const slim_ctx* ctx, SlimAttn& a, bool tc) {
   const long long all = pieces > 1 && (long long)(a.total_q / a.tile_rows) * a.H < 2ll * ctx->num_sms ? (long long)a.most_tiles * a.H * pieces : 0;
   a.slots = (int)(all < 2ll * a.share_of ? all : 2ll * a.share_of);
 }
+// Blocks of columns of the widened heads; runs of rows whose values are converted together: 64 rows at least, and two pieces of
+// work for each block of the preparation, or 64 runs
+int v_blocks(const slim_ctx* ctx, int kv_heads) { return (kv_heads * slim_attn_width(ctx->d_k) + SLIM_ATTN_V_COLS - 1) / SLIM_ATTN_V_COLS; }
+int v_runs(const slim_ctx* ctx, int kv_heads, int total_k) {
+  const int all = 16 * ctx->num_sms / v_blocks(ctx, kv_heads), most = all > 64 ? all : 64, runs = (total_k + 63) / 64;
+  return runs < most ? runs : most;
+}
 size_t part_bytes(const SlimAttn& a, int columns) { return sizeof(float) * (size_t)a.slots * a.tile_rows * (columns + 2); }
 
 }  // namespace
@@ -165,6 +172,9 @@ SlimAttnLayout slim_attn_layout(const slim_ctx* ctx, int kv_heads, int batch, in
   L.qr = off; off = align256(off + head * total_q * ctx->H);
   L.kr = off; off = align256(off + head * total_k * kv_heads);
   L.vb = off; off = align256(off + wide * total_k * kv_heads);
+  const size_t columns = wide ? (size_t)v_blocks(ctx, kv_heads) * SLIM_ATTN_V_COLS : 0;
+  L.v_max = off; off = align256(off + sizeof(float) * columns * v_runs(ctx, kv_heads, total_k));
+  L.v_more = off; off = align256(off + sizeof(float) * columns);
   L.tiles = off; off = align256(off + 3 * sizeof(int4) * tiles);
   L.n_tiles = off; off = align256(off + sizeof(int));
   L.part = off; off = align256(off + part);
@@ -177,6 +187,8 @@ SlimAttnLayout slim_attn_layout(const slim_ctx* ctx, int kv_heads, int batch, in
 cudaError_t slim_launch_attn(const slim_ctx* ctx, SlimAttn a, char* ws, int tc, cudaStream_t st) {
   const SlimAttnLayout L = slim_attn_layout(ctx, a.KV, a.batch, a.total_q, a.total_k);
   a.qr = ws + L.qr; a.kr = ws + L.kr; a.vb = ws + L.vb;
+  a.v_max = reinterpret_cast<float*>(ws + L.v_max); a.v_more = reinterpret_cast<float*>(ws + L.v_more);
+  a.v_runs = v_runs(ctx, a.KV, a.total_k);
   a.tiles = reinterpret_cast<int4*>(ws + L.tiles);
   a.n_tiles = reinterpret_cast<int*>(ws + L.n_tiles);
   a.part = reinterpret_cast<float*>(ws + L.part);

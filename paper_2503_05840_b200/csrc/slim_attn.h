@@ -21,7 +21,10 @@ struct SlimAttn {
   // workspace
   void* qr;                      // rotated queries and keys, layout of q and k: float32 (CUDA cores) or float16 (tensor cores, heads
   void* kr;                      // widened to slim_attn_width with zeros)
-  void* vb;                      // tensor cores: float32 values times 16 as float16, or bf16 values of widened heads
+  void* vb;                      // tensor cores: float32 values as float16, or bf16 values of widened heads
+  float* v_max;                  // float32 values on the tensor cores: [v_runs][columns] largest finite magnitudes of a run of rows
+  float* v_more;                 // [columns] what outputs are to be multiplied by, where a column has a factor of its own
+  int v_runs;
   int4* tiles;                   // items, longest first, three entries each: (sequence, first query row, piece, pieces of the tile),
                                  // (q0, nq, k0, nk), (first key tile, key tile behind the last, slot of the tile's first piece, -)
   int* n_tiles;
@@ -34,10 +37,11 @@ struct SlimAttn {
   uint32_t* redo;                // tensor cores: rows to be formed once more, a bit each, 8 words an item and head
 };
 
-struct SlimAttnLayout { size_t qr, kr, vb, tiles, n_tiles, part, arrivals, redo, total; };
+struct SlimAttnLayout { size_t qr, kr, vb, v_max, v_more, tiles, n_tiles, part, arrivals, redo, total; };
 
 // Columns that a head has on the tensor cores
 __host__ __device__ inline int slim_attn_width(int d_k) { return d_k <= 64 ? 64 : d_k <= 96 ? 96 : 128; }
+constexpr int SLIM_ATTN_V_COLS = 128;    // columns whose float32 values a block converts
 constexpr int SLIM_ATTN_TC_ROWS = 256;   // query rows of an item on the tensor cores: two tiles of 128
 
 int slim_attn_tc_ok(const slim_ctx* ctx);

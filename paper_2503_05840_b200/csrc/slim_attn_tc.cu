@@ -1,9 +1,10 @@
 // Attention over packed prompts on the tensor cores (bf16, d_k up to 128; heads of other widths than 64, 96 and 128 are widened
 // with zeros on their way into the workspace).
 //
-// attn_tc_prepare_kernel  rotated queries and keys as float16 in the workspace (11 bits: bf16's 8 would cost as much accuracy
-//                         as the rounding of P; without rotation they are read where they lie), float32 values as float16
-//                         too, the list of query tiles.
+// attn_tc_values_kernel   float32 values as float16 in the workspace, and the largest of each column.
+// attn_tc_prepare_kernel  rotated queries and keys as float16 (11 bits: bf16's 8 would cost as much accuracy as the rounding of P;
+//                         without rotation they are read where they lie), the list of query tiles, the columns of values that
+//                         need another factor.
 // attn_tc_kernel          one CTA a (tile of 2 x 128 query rows, head).  Per key tile of 128 rows and query tile i:
 //                           S_i = Q_i K^T       float16 (bf16 without rotation), both operands from shared memory, S in tensor memory
 //                           P_i = 2^(S_i - m)   a thread a row: S to registers, maximum, exponentials, P as bf16 over S's
@@ -13,11 +14,10 @@
 //                         While one query tile's softmax runs, the tensor core works for the other.
 //   The reference m of a row moves only when its maximum has grown by more than 2^8: then its warp multiplies the row of O
 //   (and l) by 2^(m - m'); P stays below 2^8 otherwise, which float32 sums do not mind.
-//   What float16 cannot hold (|q| > 4096, |k| > 16384, |v| > 4000, numbers that are not finite) enters as NaN, and rows that
-//   come out not finite are formed once more on the CUDA cores, in float32 from the inputs; so are rows that share a tile with
-//   a value that is not finite and that they do not attend (0 times infinity).  Float32 values enter times 16: float16's
-//   smallest step is then 2^-28, and rows whose outputs all stay below 2^-18 are formed once more as well.  A CTA does that
-//   behind its last item, when none of its warps waits for another one any more: it may take long.
+//   What float16 cannot hold (|q| > 4096, |k| > 16384, numbers that are not finite, see V_UP) enters as NaN, and rows that come out not
+//   finite are formed once more on the CUDA cores, in float32 from the inputs; so are rows that share a tile with a value that is
+//   not finite and that they do not attend (0 times infinity).  A CTA does that behind its last item, when none of its warps
+//   waits for another one any more: it may take long.
 // Tiles of 2 x 128 queries: both take each tile of keys from shared memory, and tensor memory holds exactly S and O of two.
 // Bound by the softmax: for d_k = 128 a pair of 128 x 128 tiles costs the tensor core 1024 clocks for S and 1024 for O, the
 // exponentials about 1500 of the special-function unit a scheduler (a quarter of them go to the FMA pipe for that reason), with
@@ -25,7 +25,8 @@
 // Measured: 16384 tokens, 32 heads of 128, causal: 1.77 ms (1.24 PFLOP/s, 0.76 of the measured GEMM; 2.1 ms at the power limit)
 // and 87 us of preparation; twelve prompts of 1 to 4096 tokens, 8 key heads: 325 us + 53; 8 x 1500 frames, 20 heads of 64,
 // not causal: 152 us (0.6 PFLOP/s: half the products an exponential) + 5; chunks of 512, 512, 333 and 1 queries over 4096,
-// 1536, 333 and 2048 keys, float32 values: 70 us, as long as the longest tile takes (1.4 times a CTA's share), + 75.
+// 1536, 333 and 2048 keys, float32 values: 69 us, as long as the longest tile takes (1.4 times a CTA's share), + 33 for the values
+// (201 MB) + 31.
 #include <cuda_fp16.h>
 
 #include "slim_attn.h"
@@ -39,7 +40,9 @@ namespace {
 
 // ------------------------------------------------------------------------------------------------ preparation
 constexpr int PREP_THREADS = 256;
-constexpr float V_UP = 16.f;                         // factor of float32 values on their way into float16
+constexpr float V_UP = 16.f;                         // factor of float32 values on their way into float16, where it suits a column
+static_assert(V_UP == 0x1p4f, "an exponent below");
+constexpr int V_COLS = SLIM_ATTN_V_COLS, V_PARTS = 4;
 
 __device__ __forceinline__ uint32_t half2_checked(float a, float b, float most) {
   const bool fine = fabsf(a) <= most && fabsf(b) <= most;
@@ -125,68 +128,149 @@ __device__ void widen_row(const SlimAttn& a, int r, bool query) {
       if (64 * p + 2 * lane < DK) dst[h * (DK / 2) + 32 * p + lane] = half2_checked(y[0], y[1], most);
     }
 }
-template <int DK, typename T>
+template <int DK>
 __device__ void widen_values(const SlimAttn& a, int r) {
   const int lane = threadIdx.x & 31, dk = a.d_k;
-  const T* src = reinterpret_cast<const T*>(a.v) + (size_t)r * a.KV * dk;
+  const unsigned short* src = reinterpret_cast<const unsigned short*>(a.v) + (size_t)r * a.KV * dk;
   uint32_t* dst = reinterpret_cast<uint32_t*>(a.vb) + (size_t)r * a.KV * (DK / 2);
   if ((dk & 7) == 0) {                               // eight columns at a time
 #pragma unroll 4
     for (int i = lane; i < a.KV * (DK / 8); i += 32) {
       const int h = i / (DK / 8), c = i % (DK / 8) * 8;
-      uint4 out = make_uint4(0u, 0u, 0u, 0u);
-      if (c < dk) {
-        const uint4* from = reinterpret_cast<const uint4*>(src + h * dk + c);
-        out = __ldcs(from);
-        if constexpr (sizeof(T) == 4) {
-          const uint4 y = __ldcs(from + 1);
-          out = make_uint4(half2_checked(__uint_as_float(out.x) * V_UP, __uint_as_float(out.y) * V_UP, 64000.f), half2_checked(__uint_as_float(out.z) * V_UP, __uint_as_float(out.w) * V_UP, 64000.f),
-                           half2_checked(__uint_as_float(y.x) * V_UP, __uint_as_float(y.y) * V_UP, 64000.f), half2_checked(__uint_as_float(y.z) * V_UP, __uint_as_float(y.w) * V_UP, 64000.f));
-        }
-      }
-      reinterpret_cast<uint4*>(dst)[i] = out;
+      reinterpret_cast<uint4*>(dst)[i] = c < dk ? __ldcs(reinterpret_cast<const uint4*>(src + h * dk + c)) : make_uint4(0u, 0u, 0u, 0u);
     }
     return;
   }
 #pragma unroll 4
   for (int i = lane; i < a.KV * (DK / 2); i += 32) {
     const int h = i / (DK / 2), c = i % (DK / 2) * 2;                    // (d_k is even)
-    if constexpr (sizeof(T) == 4) {
-      const float2 v = c < dk ? __ldcs(reinterpret_cast<const float2*>(src + h * dk + c)) : make_float2(0.f, 0.f);
-      dst[i] = half2_checked(v.x * V_UP, v.y * V_UP, 64000.f);
-    } else {
-      dst[i] = c < dk ? __ldcs(reinterpret_cast<const uint32_t*>(src + h * dk + c)) : 0u;
+    dst[i] = c < dk ? __ldcs(reinterpret_cast<const uint32_t*>(src + h * dk + c)) : 0u;
+  }
+}
+
+// Float32 values as float16, each column times a power of two: V_UP, unless the column's largest finite magnitude M is above
+// V_MOST or below V_LEAST, then the one that brings M into [2^14, 2^15).  With V_UP float16's smallest step is 2^-28 (2^-20 of M
+// at most).  With another factor values keep their 11 bits down to 2^-28 M; smaller ones, which no column has unless its largest
+// stand apart (in rows of another sequence, say), enter as NaN like what float16 cannot hold.  M is known only behind a pass
+// over all rows; the pass converts with V_UP, and columns that need another factor are converted again (settle_columns).
+constexpr float V_MOST = 4000.f, V_LEAST = 0x1p-8f;
+__device__ __forceinline__ unsigned short half_checked(float x) { return fabsf(x) <= 64000.f ? __half_as_ushort(__float2half_rn(x)) : (unsigned short)0x7fff; }
+__device__ __forceinline__ float finite_abs(float x) { const float y = fabsf(x); return y <= 3.4028234663852886e38f ? y : 0.f; }
+
+// Unit u: V_COLS columns (of the widened heads) of a run of rows, by a block, W columns a thread at a time
+template <int DK, int W>
+__device__ void convert_values(const SlimAttn& a, int u, float* s_max) {
+  constexpr int TPR = V_COLS / W, RPP = PREP_THREADS / TPR;
+  const int tid = threadIdx.x, dk = a.d_k, width = a.KV * DK, blocks = (width + V_COLS - 1) / V_COLS;
+  const int run = u / blocks, c0 = u % blocks * V_COLS, col = c0 + tid % TPR * W, h = col / DK, c = col - h * DK;
+  const int lo = (int)((long long)a.total_k * run / a.v_runs), hi = (int)((long long)a.total_k * (run + 1) / a.v_runs);
+  const bool there = col < width, live = there && c < dk;
+  const float* src = reinterpret_cast<const float*>(a.v) + (size_t)h * dk + c;
+  unsigned short* dst = reinterpret_cast<unsigned short*>(a.vb) + col;
+  float m[W];
+#pragma unroll
+  for (int x = 0; x < W; ++x) m[x] = 0.f;
+  constexpr int FLY = 24 / W;                        // rows of a thread whose loads are in flight together
+  for (int r0 = lo + tid / TPR; r0 < hi; r0 += FLY * RPP) {
+    float v[FLY][W];
+#pragma unroll
+    for (int i = 0; i < FLY; ++i) {
+      const int r = r0 + i * RPP;
+#pragma unroll
+      for (int x = 0; x < W; ++x) v[i][x] = 0.f;
+      if (live && r < hi) {
+        if constexpr (W == 4) *reinterpret_cast<float4*>(v[i]) = __ldcs(reinterpret_cast<const float4*>(src + (size_t)r * a.KV * dk));
+        else *reinterpret_cast<float2*>(v[i]) = __ldcs(reinterpret_cast<const float2*>(src + (size_t)r * a.KV * dk));
+      }
     }
+#pragma unroll
+    for (int i = 0; i < FLY; ++i) {
+      const int r = r0 + i * RPP;
+      uint32_t w[W / 2];
+#pragma unroll
+      for (int x = 0; x < W; x += 2) {
+        m[x] = fmaxf(m[x], finite_abs(v[i][x])); m[x + 1] = fmaxf(m[x + 1], finite_abs(v[i][x + 1]));
+        w[x / 2] = half_checked(v[i][x] * V_UP) | (uint32_t)half_checked(v[i][x + 1] * V_UP) << 16;
+      }
+      if (there && r < hi) {
+        if constexpr (W == 4) *reinterpret_cast<uint2*>(dst + (size_t)r * width) = make_uint2(w[0], w[1]);
+        else *reinterpret_cast<uint32_t*>(dst + (size_t)r * width) = w[0];
+      }
+    }
+  }
+  __syncthreads();                                   // (the unit before this one has been read)
+#pragma unroll
+  for (int x = 0; x < W; ++x) s_max[tid / TPR * V_COLS + tid % TPR * W + x] = m[x];
+  __syncthreads();
+  if (tid < V_COLS) {
+    float most = s_max[tid];
+#pragma unroll
+    for (int i = 1; i < RPP; ++i) most = fmaxf(most, s_max[i * V_COLS + tid]);
+    a.v_max[(size_t)run * blocks * V_COLS + c0 + tid] = most;
+  }
+}
+
+template <int DK>
+__global__ void __launch_bounds__(PREP_THREADS) attn_tc_values_kernel(const __grid_constant__ SlimAttn a) {
+  __shared__ float s_max[8 * V_COLS];
+  slim_pdl_trigger();
+  slim_pdl_wait();
+  const int units = a.v_runs * ((a.KV * DK + V_COLS - 1) / V_COLS);
+  for (int u = blockIdx.x; u < units; u += gridDim.x) {
+    if ((a.d_k & 3) == 0) convert_values<DK, 4>(a, u, s_max);
+    else convert_values<DK, 2>(a, u, s_max);
+  }
+}
+
+// Behind it, by a block: the factors of V_COLS columns, and part y of V_PARTS of the columns that V_UP does not suit once more
+template <int DK>
+__device__ void settle_columns(const SlimAttn& a, int block, int blocks, int y, float* s_max) {
+  const int tid = threadIdx.x, width = a.KV * DK, col = block * V_COLS + tid % V_COLS, part = tid / V_COLS;
+  constexpr int parts = PREP_THREADS / V_COLS;
+  float most = 0.f;
+#pragma unroll 16
+  for (int r = part; r < a.v_runs; r += parts) most = fmaxf(most, __ldg(a.v_max + (size_t)r * blocks * V_COLS + col));
+  __syncthreads();                                   // (the unit before this one has been read)
+  s_max[tid] = most;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < parts; ++i) most = fmaxf(most, s_max[i * V_COLS + tid % V_COLS]);
+  const bool other = most > V_MOST || (most > 0.f && most < V_LEAST);
+  // 2^14 over the power of two in M (a denormal one's is taken as 2^-112: no column asks for more than 2^126)
+  const int e = max(__float_as_int(most) >> 23, 15) - 127;
+  if (y == 0 && part == 0) a.v_more[col] = other ? __int_as_float((e - 14 + 4 + 127) << 23) : 1.f;      // V_UP over the column's factor
+  const int h = col / DK, c = col - h * DK, dk = a.d_k;
+  if (!other || col >= width) return;
+  const float up = __int_as_float((14 - e + 127) << 23);
+  const float* src = reinterpret_cast<const float*>(a.v) + (size_t)h * dk + c;
+  unsigned short* dst = reinterpret_cast<unsigned short*>(a.vb) + col;
+#pragma unroll 4
+  for (int r = parts * y + part; r < a.total_k; r += parts * V_PARTS) {
+    const float v = __ldg(src + (size_t)r * a.KV * dk);
+    dst[(size_t)r * width] = v == 0.f || fabsf(v * up) >= 0x1p-14f ? half_checked(v * up) : (unsigned short)0x7fff;
   }
 }
 
 template <int DK>
 __global__ void __launch_bounds__(PREP_THREADS) attn_tc_prepare_kernel(const __grid_constant__ SlimAttn a) {
   extern __shared__ int s_mem[];
+  __shared__ float s_max[PREP_THREADS];
   slim_pdl_trigger();
   slim_pdl_wait();
   if (blockIdx.x == 0) { slim_attn_plan(a, s_mem); return; }
-  const int warps = (gridDim.x - 1) * (PREP_THREADS / 32), lane = threadIdx.x & 31;
+  if (a.v32) {
+    const int blocks = (a.KV * DK + V_COLS - 1) / V_COLS;              // by the last blocks, which have fewer rows
+    for (int u = gridDim.x - 1 - blockIdx.x; u < blocks * V_PARTS; u += gridDim.x - 1) settle_columns<DK>(a, u % blocks, blocks, u / blocks, s_max);
+  }
+  const int warps = (gridDim.x - 1) * (PREP_THREADS / 32);
   const bool narrow = a.d_k != DK;
-  const int turned = a.rope_base || narrow ? a.total_q + a.total_k : 0, rows = turned + (a.v32 || narrow ? a.total_k : 0);
+  const int turned = a.rope_base || narrow ? a.total_q + a.total_k : 0, rows = turned + (!a.v32 && narrow ? a.total_k : 0);
   for (int r = (blockIdx.x - 1) * (PREP_THREADS / 32) + (threadIdx.x >> 5); r < rows; r += warps) {
-    if (narrow) {
-      if (r < turned && (a.d_k & 15) == 0) prepare_row<DK, true>(a, r < a.total_q ? r : r - a.total_q, r < a.total_q);
-      else if (r < turned) widen_row<DK>(a, r < a.total_q ? r : r - a.total_q, r < a.total_q);
-      else if (a.v32) widen_values<DK, float>(a, r - turned);
-      else widen_values<DK, unsigned short>(a, r - turned);
-      continue;
-    }
-    if (r < turned) { prepare_row<DK, false>(a, r < a.total_q ? r : r - a.total_q, r < a.total_q); continue; }
-    const int n = a.KV * DK;
-    const size_t at = (size_t)(r - turned) * n;
-    const float4* src = reinterpret_cast<const float4*>(reinterpret_cast<const float*>(a.v) + at);
-    uint2* dst = reinterpret_cast<uint2*>(reinterpret_cast<unsigned short*>(a.vb) + at);
-#pragma unroll 4
-    for (int i = lane; i < n / 4; i += 32) {
-      const float4 v = __ldcs(src + i);
-      dst[i] = make_uint2(half2_checked(v.x * V_UP, v.y * V_UP, 64000.f), half2_checked(v.z * V_UP, v.w * V_UP, 64000.f));
-    }
+    const bool query = r < a.total_q;
+    if (r >= turned) widen_values<DK>(a, r - turned);
+    else if (!narrow) prepare_row<DK, false>(a, query ? r : r - a.total_q, query);
+    else if ((a.d_k & 15) == 0) prepare_row<DK, true>(a, query ? r : r - a.total_q, query);
+    else widen_row<DK>(a, query ? r : r - a.total_q, query);
   }
 }
 
@@ -288,6 +372,15 @@ __device__ __forceinline__ void exponentials(uint32_t (&r)[TN], f32x2 scale2, f3
     }
     l2 = add2(l2, pack2(lo, hi));
     r[x / 2] = VH ? half2_of(lo, hi) : bf162_of(lo, hi);
+  }
+}
+
+// A row of outputs times its columns' powers of two: exact but at the ends of bf16's range
+__device__ __noinline__ void scale_row(__nv_bfloat16* o, const float* f, int n) {
+  for (int c = 0; c < n; c += 2) {                   // (d_k is even)
+    uint32_t* at = reinterpret_cast<uint32_t*>(o + c);
+    const uint32_t w = *at;
+    *at = bf162_of(__uint_as_float(w << 16) * __ldg(f + c), __uint_as_float(w & 0xffff0000u) * __ldg(f + c + 1));
   }
 }
 
@@ -510,7 +603,6 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
       const float inv = all > 0 ? (VH ? 1.f / V_UP : 1.f) / l : 0.f;
       __nv_bfloat16* dst = reinterpret_cast<__nv_bfloat16*>(a.o) + ((size_t)(s.q0 + row) * a.H + h) * a.d_k;
       bool bad = false;
-      float most = 0.f;
       if (ok) {
 #pragma unroll
         for (int c = 0; c < DK / 32; ++c) {
@@ -546,7 +638,6 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
               float lo = __uint_as_float(o[x + 2 * e]) * inv, hi = __uint_as_float(o[x + 2 * e + 1]) * inv;
               if (all == 0) lo = hi = 0.f;
               bad |= !(fabsf(lo) <= 3.3895313892515355e38f && fabsf(hi) <= 3.3895313892515355e38f);
-              if (VH) most = fmaxf(most, fmaxf(fabsf(lo), fabsf(hi)));
               w[e] = bf162_of(lo, hi);
             }
             if (there && (a.d_k & 7) == 0) {
@@ -558,8 +649,12 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
             }
           }
         }
-        if (VH) bad |= all > 0 && most < 3.8e-6f;      // 2^-18
         const unsigned redo = __ballot_sync(0xffffffffu, bad && there);
+        if (VH) {
+          // columns with a factor of their own (mostly none)
+          const float4 f = 4 * lane < DK ? __ldg(reinterpret_cast<const float4*>(a.v_more + h / share * DK) + lane) : make_float4(1.f, 1.f, 1.f, 1.f);
+          if (__any_sync(0xffffffffu, f.x != 1.f || f.y != 1.f || f.z != 1.f || f.w != 1.f) && there) scale_row(dst, a.v_more + h / share * DK, a.d_k);
+        }
         __syncwarp();
         if (lane == 0) {
           a.redo[8 * item_place(r_) + warp] = redo;
@@ -714,9 +809,16 @@ cudaError_t launch(const slim_ctx* ctx, const SlimAttn& a, cudaStream_t st) {
   if (e == cudaSuccess) e = make_map(&vmap, a.v32 || a.d_k != DK ? a.vb : a.v, a.KV * DK, a.total_k);
   if (e == cudaSuccess) e = cudaFuncSetAttribute((const void*)attn_tc_kernel<DK, VH>, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape<DK>::SMEM);
   if (e != cudaSuccess) return e;
-  const long long rows = (as_is ? 0 : (long long)a.total_q + a.total_k) + (a.v32 || a.d_k != DK ? a.total_k : 0), fill = 8ll * ctx->num_sms;
-  const int blocks = 1 + (int)((rows + 7) / 8 < fill ? (rows + 7) / 8 : fill);
-  e = slim_launch_pdl(attn_tc_prepare_kernel<DK>, dim3(blocks), dim3(PREP_THREADS), slim_attn_plan_smem(a.batch), st, a);
+  const long long fill = 8ll * ctx->num_sms;
+  const long long columns = (a.KV * DK + V_COLS - 1) / V_COLS, units = a.v_runs * columns;
+  if (a.v32) {
+    e = slim_launch_pdl(attn_tc_values_kernel<DK>, dim3((unsigned)(units < fill ? units : fill)), dim3(PREP_THREADS), 0, st, a);
+    if (e != cudaSuccess) return e;
+  }
+  const long long rows = (as_is ? 0 : (long long)a.total_q + a.total_k) + (!a.v32 && a.d_k != DK ? a.total_k : 0);
+  long long blocks = (rows + 7) / 8;
+  if (a.v32 && blocks < columns * V_PARTS) blocks = columns * V_PARTS;
+  e = slim_launch_pdl(attn_tc_prepare_kernel<DK>, dim3(1 + (unsigned)(blocks < fill ? blocks : fill)), dim3(PREP_THREADS), slim_attn_plan_smem(a.batch), st, a);
   if (e != cudaSuccess) return e;
   const long long items = (long long)a.most_tiles * a.H + a.slots;
   return slim_launch_pdl(attn_tc_kernel<DK, VH>, dim3((unsigned)(items < ctx->num_sms ? items : ctx->num_sms)), dim3(THREADS), Shape<DK>::SMEM, st, qmap, kmap, vmap, a);

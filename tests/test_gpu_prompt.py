@@ -464,3 +464,91 @@ def test_rows_formed_again_take_the_time_of_the_cuda_cores():
     generic = time()
     assert auto < 10 * generic, (auto, generic)
     c.close()
+
+
+def _scaled(kind, v):
+    KV, dk = v.shape[1:]
+    if kind == "columns":                                 # of one head, nine orders of magnitude, one column beyond float16
+        v *= 10.0 ** -(torch.arange(dk) % 9).float()
+        v[:, 0, 3] *= 1e5
+    elif kind == "one column":
+        v[:, :, dk - 1] *= 1e-8
+        v[:, KV - 1, 0] *= 1e20
+    elif kind == "heads":
+        v *= 10.0 ** -(4.0 * torch.arange(KV))[:, None]
+        v[:, 0] = 0
+    elif kind == "ends":
+        v *= torch.where(torch.arange(dk) % 2 == 0, 1e37, 1e-37)
+    else:
+        v *= kind
+
+
+@pytest.mark.parametrize("H,KV,dk", [(2, 2, 64), (6, 3, 128), (2, 2, 96), (4, 2, 80), (3, 3, 50)])
+@pytest.mark.parametrize("kind", [1e-5, 1e-7, 1e5, "columns", "one column", "heads", "ends"])
+def test_float32_values_of_any_scale(H, KV, dk, kind):
+    c = Case("bf16", H, KV, dk, 1e4, [1, 130, 257, 3], [1, 130, 600, 70], v32=True, seed=dk)
+    _scaled(kind, c.v)
+    b = c.buffers()
+    c.call(b, True)
+    torch.cuda.synchronize()
+    assert B.slim_device_status(c.ctx) == B.SLIM_OK
+    got = b["o"].double().cpu().numpy()
+    want, tol = c.reference(True)
+    # steps of 2^-28 in columns of ordinary size (bf16 outputs end at 2^-133)
+    most = np.repeat(c.v.abs().amax(0).double().numpy(), H // KV, axis=0)
+    tol = tol + np.where((most >= 2.0 ** -8) & (most <= 4000), 2.0 ** -29, 2.0 ** -134)
+    bad = ~(np.abs(got - want) <= tol)
+    assert not bad.any(), (np.argwhere(bad)[:5], got[bad][:5], want[bad][:5], tol[bad][:5])
+    c.close()
+
+
+def test_heads_whose_values_are_zero_or_small_take_no_longer():
+    c = Case("bf16", 8, 8, 128, 1e4, [2048], [2048], v32=True, lead=0)
+    b = c.buffers()
+
+    def time():
+        t = []
+        for _ in range(4):
+            e = [torch.cuda.Event(enable_timing=True) for _ in range(2)]
+            e[0].record()
+            c.call(b, True)
+            e[1].record()
+            torch.cuda.synchronize()
+            t.append(e[0].elapsed_time(e[1]))
+        return min(t[1:])
+
+    ordinary = time()
+    b["v"][:, 3] = 0
+    b["v"][:, 5] *= 1e-7
+    b["v"][:, 6] *= 1e7
+    assert time() < 3 * ordinary                          # (row by row it was some 200 times)
+    assert not b["o"][:, 3].any()
+    c.close()
+
+
+@pytest.mark.parametrize("H,dk", [(2, 64), (1, 128), (2, 96)])
+def test_float32_values_and_the_probabilities_beside_them_keep_11_bits(H, dk):
+    """Values, then probabilities, half way between two bf16 numbers and of signs that cancel: 8 bits would leave 2^-8."""
+    n = 512
+    c = Case("bf16", H, H, dk, 0.0, [n], [n], v32=True, lead=0)
+    c.q[:], c.k[:] = 0, 0
+    even = torch.arange(n) % 2 == 0
+    c.v[:] = torch.where(even, 1 + 2.0 ** -8 - 2.0 ** -10, -(1 + 2.0 ** -8 + 2.0 ** -10))[:, None, None]
+    b = c.buffers()
+    for part in range(2):
+        c.call(b, False)
+        torch.cuda.synchronize()
+        got = b["o"].double().cpu().numpy()
+        o, pv, qk = po.attention(c.q.float().numpy(), c.k.float().numpy(), c.v.numpy(), 0.0, False)
+        # Scores in float32.  Probabilities: 2^-11, a quarter of the exponentials off by 7.5e-5; values 2^-11; the output in bf16.
+        tol = (2 * 2.0 ** -20 * (1 + qk[..., None]) + 2.0 ** -11 + 2 * 7.5e-5 + 2.0 ** -11) * pv + 2.0 ** -8 * np.abs(o)
+        assert tol.max() < 0.6 * (2.0 ** -8 if part == 0 else 0.00195 / 1.50195)
+        assert (np.abs(got - o) <= tol).all(), (part, np.abs(got - o).max(), tol.min())
+        # the odd keys' probability is 0.50195 of the even ones', half way between the bf16 numbers 0.5 and 0.5039
+        x, y = {64: (2.953125, 1.8671875), 96: (4.34375, 1.5546875), 128: (5.28125, 1.4765625)}[dk]
+        p = float(np.exp(-x * y / dk ** 0.5))
+        b["q"][:, :, 0], b["k"][1::2, :, 0] = x, -y
+        c.q, c.k = b["q"].cpu(), b["k"].cpu()
+        b["v"][0::2], b["v"][1::2] = -p, 1.0
+        c.v = b["v"].cpu()
+    c.close()
