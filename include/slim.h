@@ -323,8 +323,8 @@ slim_status slim_combine_project(slim_ctx* ctx, const float* lse_all, const floa
  *   workspace  device, >= slim_prompt_workspace_bytes (0 on bad arguments), 256-byte aligned; contents are scratch, shared
  *              like that of slim_tree_decode
  *   Softmax sums and weighted sums are float32; in a bf16 context rotated queries and keys are rounded to 11 bits, the
- *   probabilities to bf16 (beside float32 values, probabilities and values to 11 bits, values in steps of 2^-28 at the least
- *   unless all of their column are below 2^-8).  A number that is not finite in a key or
+ *   probabilities to bf16 (beside float32 values, probabilities and values to 11 bits, in steps of 2^-31 of the row's largest
+ *   probability and 2^-28 at the least, values finer where all of their column are below 2^-8).  A number that is not finite in a key or
  *   a value reaches the rows that attend it, and no other.  With RoPE, rows that have a query above 4096 or attend a key above
  *   16384, and rows that meet a number that is not finite, are formed in float32 and take the CUDA cores' time.  bf16, d_k up to 128: tensor cores; other shapes: CUDA cores (slim_set_path chooses as for slim_decode).
  *   Few queries over many keys are worked off in pieces of the keys, whose sums are joined in a fixed order: the last bits of a

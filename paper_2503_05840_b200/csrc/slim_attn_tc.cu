@@ -13,7 +13,8 @@
 //                                               where they were float32 (a second rounding to 8 bits would cost as much as P's)
 //                         While one query tile's softmax runs, the tensor core works for the other.
 //   The reference m of a row moves only when its maximum has grown by more than 2^8: then its warp multiplies the row of O
-//   (and l) by 2^(m - m'); P stays below 2^8 otherwise, which float32 sums do not mind.
+//   (and l) by 2^(m - m'); P stays below 2^8 otherwise, which float32 sums do not mind.  Float16 P is 2^7 times as large, so that
+//   its 11 bits reach down to 2^-21 of the row's largest, its steps to 2^-31.
 //   What float16 cannot hold (|q| > 4096, |k| > 16384, numbers that are not finite, see V_UP) enters as NaN, and rows that come out not
 //   finite are formed once more on the CUDA cores, in float32 from the inputs; so are rows that share a tile with a value that is
 //   not finite and that they do not attend (0 times infinity).  A CTA does that behind its last item, when none of its warps
@@ -483,6 +484,7 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
     const f32x2 scale2 = pack2(scale, scale);
     uint32_t ps = 0, po = 0;                        // phases of bar_s, bar_o
     for (int r_ = 0; ok && item(r_, it); ++r_) {
+      constexpr float LIFT = VH ? 7.f : 0.f;
       const int n = i ? it.nt1 : it.nt0;
       const int all = slim_attn_keys(a, it.s, it.row0 + i * TM + (warp & 3) * 32 + lane);     // keys of the row
       const int lim = all - it.first * TN;                                                   // behind the piece's first
@@ -511,9 +513,9 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
 #pragma unroll
           for (int c = 0; c < 8; ++c) mx[c] = max3(mx[c], __uint_as_float(r[x + c]), __uint_as_float(r[x + c + 8]));
         const float top = max3(max3(mx[0], mx[1], mx[2]), max3(mx[3], mx[4], mx[5]), fmaxf(mx[6], mx[7])) * scale;
-        const bool move = top > m + TAU;              // (m = -inf: the first keys of the row)
+        const bool move = top > m + (TAU + LIFT);     // (m = -inf: the first keys of the row)
         if (__any_sync(0xffffffffu, move)) {
-          const float m_new = move ? top : m;
+          const float m_new = move ? top - LIFT : m;
           const float f = move ? ex2_approx(m - m_new) : 1.f;
           m = m_new;
           float lo, hi;

@@ -552,3 +552,28 @@ def test_float32_values_and_the_probabilities_beside_them_keep_11_bits(H, dk):
         b["v"][0::2], b["v"][1::2] = -p, 1.0
         c.v = b["v"].cpu()
     c.close()
+
+
+@pytest.mark.parametrize("dk", [64, 96, 128])
+@pytest.mark.parametrize("gap", [12, 14, 15.5])
+@pytest.mark.parametrize("at", [0, 1000, 5999])
+def test_keys_beside_a_dominant_one_keep_their_weight(dk, gap, at):
+    """One key above thousands of others, which alone have values: the output is what the others make of them."""
+    n = 6000
+    c = Case("bf16", 1, 1, dk, 0.0, [130], [n], v32=True, lead=0, seed=dk)
+    c.q[:], c.k[:] = 0, 0
+    c.q[:, :, 0], c.k[at, 0, 0] = gap * dk ** 0.5 / 8, 8.0
+    c.v = 1 + torch.rand(c.v.shape, generator=torch.Generator().manual_seed(1))
+    c.v[at] = 0
+    b = c.buffers()
+    c.call(b, False)
+    torch.cuda.synchronize()
+    got = b["o"].double().cpu().numpy()
+    s = float(c.q[0, 0, 0]) * c.k[:, 0, 0].double() / dk ** 0.5
+    p = torch.softmax(s, 0).numpy()
+    o = p @ c.v[:, 0].double().numpy()
+    # Scores in float32; probabilities: 2^-11 in steps of 2^-31 of the largest, a quarter of the exponentials off by 7.5e-5; values
+    # 2^-11; sums of n positive terms in float32 (n / 2 half steps each way average out far below n 2^-26); the output in bf16.
+    tol = (2 * 2.0 ** -18 + 2.0 ** -11 + 2 * 7.5e-5 + 2.0 ** -11 + n * 2.0 ** -26 + 2.0 ** -8) * o + n * 2.0 ** -32 * 2
+    assert (np.abs(got[:, 0] - o) <= tol).all(), (np.abs(got[:, 0] - o) / tol).max()
+    c.close()
