@@ -1,11 +1,13 @@
 // Rows into and out of a K-cache: packed rows of several sequences (slim_append_rows, slim_read_rows) for float32, bf16
 // and 4-bit caches, and the uniform append of a 4-bit cache (slim_append_k, slim_decode_step, slim_prefill).
 //
-// What HBM has to move: a row of d bf16 keys (2 d bytes) one way and d/2 + d/32 bytes the other.  A warp takes 256 columns of a row at a time, four such chunks in flight: 16 bytes a lane on the wide
-// side, one 32-bit word of eight codes on the other; four lanes share a scale.
+// What HBM has to move: a row of d bf16 keys (2 d bytes) one way and d/2 + d/32 bytes the other.  A warp takes 256 columns of a
+// row at a time, four such chunks in flight: 16 bytes a lane on the wide side, one 32-bit word of eight codes on the other; four
+// lanes share a scale.
 // Measured, rows of 4096: 37.5k rows written 92 us (389 MB, 4.2 TB/s: the issue slots are 77 % full, the rounding's steps; more
 // warps an SM changed nothing) and read back 65 us (6.0 TB/s, 0.92 of a copy); 31k rows in pages read in 54 us; 16 rows 5 us
-// either way (three dependent loads: start, position, page).
+// either way (three dependent loads: start, position, page).  One prompt, 2000 rows: written in 7.6 us, read back in 5.0.  Rows of a bf16
+// cache, both ways: 37.5k of 4096 101 us (6.1 TB/s), 2000 5.1 us, 9500 of 1280 6.4 us.
 #include "slim_fp4.cuh"
 #include "slim_ptx.cuh"
 
@@ -101,8 +103,9 @@ __device__ __forceinline__ uint32_t quantise8(const uint4& v, float amax, int& b
   return out & (0x77777777u | (some << 3));
 }
 
-// bf16 rows -> 4 bits; CH: chunks of 256 columns whose loads are in flight together
-template <int CH>
+// bf16 rows -> 4 bits; CH: chunks of 256 columns whose loads are in flight together; RAGGED: a warp's share is no multiple of it
+// (37.5k rows of 4096: 82 us, 85 with the test for the end of the share between the chunks)
+template <int CH, bool RAGGED>
 __global__ void __launch_bounds__(256) rows_quantise_kernel(const RowsArgs a) {
   slim_pdl_trigger();
   slim_pdl_wait();
@@ -116,15 +119,17 @@ __global__ void __launch_bounds__(256) rows_quantise_kernel(const RowsArgs a) {
   if (row < 0) return;
   unsigned char* dst = a.codes + (size_t)row * a.pitch;
   unsigned char* sdst = a.scales + (size_t)row * a.spitch;
+  const int end = RAGGED ? min(a.d, (part + 1) * a.chunks * 256) : a.d;      // where the warp's share ends
   for (int c0 = 0; c0 < a.chunks; c0 += CH) {
     uint4 v[CH];
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
       const int col = (part * a.chunks + c0 + c) * 256 + lane * 8;
-      v[c] = col < a.d ? load8(src, col, a.d, whole) : make_uint4(0u, 0u, 0u, 0u);
+      v[c] = col < end ? load8(src, col, a.d, whole) : make_uint4(0u, 0u, 0u, 0u);
     }
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
+      if (RAGGED && c0 + c >= a.chunks) break;                         // (all lanes)
       const int col = (part * a.chunks + c0 + c) * 256 + lane * 8;
       // largest magnitude of the group's 32 columns, NaN if there is one: the sign cleared, the bits of bf16 numbers order as integers
       uint32_t m = __vmaxu2(__vmaxu2(v[c].x & 0x7fff7fffu, v[c].y & 0x7fff7fffu), __vmaxu2(v[c].z & 0x7fff7fffu, v[c].w & 0x7fff7fffu));
@@ -133,7 +138,7 @@ __global__ void __launch_bounds__(256) rows_quantise_kernel(const RowsArgs a) {
       const float amax = __uint_as_float(max(m << 16, m & 0xffff0000u));
       int byte;
       const uint32_t out = quantise8(v[c], amax, byte);
-      if (col < a.d) {
+      if (col < end) {
         if (col + 8 <= a.d) *reinterpret_cast<uint32_t*>(dst + (col >> 1)) = out;
         else
           for (int e = 0; 2 * e < a.d - col; ++e) dst[(col >> 1) + e] = (unsigned char)(out >> (8 * e));
@@ -158,18 +163,20 @@ __global__ void __launch_bounds__(256) rows_expand_kernel(const RowsArgs a) {
   const unsigned char* src = a.codes + (size_t)row * a.pitch;
   const unsigned char* ssrc = a.scales + (size_t)row * a.spitch;
   const bool whole = (a.d & 7) == 0 && ((uintptr_t)a.wide & 15) == 0;
+  const int end = min(a.d, (part + 1) * a.chunks * 256);               // where the warp's share ends
   for (int c0 = 0; c0 < a.chunks; c0 += CH) {
     uint32_t v[CH], s[CH];
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
       const int col = (part * a.chunks + c0 + c) * 256 + lane * 8;
-      v[c] = col < a.d ? __ldcs(reinterpret_cast<const unsigned int*>(src + (col >> 1))) : 0u;      // (rows are padded to 16 bytes)
-      s[c] = col < a.d ? __ldg(ssrc + col / FP4_GROUP) : 0u;
+      v[c] = col < end ? __ldcs(reinterpret_cast<const unsigned int*>(src + (col >> 1))) : 0u;      // (rows are padded to 16 bytes)
+      s[c] = col < end ? __ldg(ssrc + col / FP4_GROUP) : 0u;
     }
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
+      if (c0 + c >= a.chunks) break;
       const int col = (part * a.chunks + c0 + c) * 256 + lane * 8;
-      if (col >= a.d) continue;
+      if (col >= end) continue;
       const uint32_t scale = s[c] * 0x00800080u;                       // a float16 pair
       uint32_t h[4], out[4];
       slim_fp4_decode8(v[c], h);
@@ -218,14 +225,18 @@ cudaError_t launch_rows(const slim_ctx* ctx, RowsArgs a, int to_cache, cudaStrea
   const int span = fp4 ? 256 : 32;                                     // columns (units) a warp takes at a time
   const int n = ((fp4 ? a.d : a.pitch / (int)unit) + span - 1) / span;
   // A row a warp where the rows alone give every SM 64 warps (the row's place is then looked up once); with fewer rows they are
-  // split, down to one chunk a warp.
+  // split, down to four chunks a warp, whose loads are in flight together, and to one where an SM has fewer than 96 of them
+  // (2367 rows of 4096, 4 bits: written in 8.2 us by four, 10.2 by two; 900 rows 5.4 either way; 2367 rows of 1280 5.2 and 4.4).
+  const int four = (n + 3) / 4, least = (n + four - 1) / four;
   a.chunks = n;
-  while (a.chunks > 1 && (long long)a.total * ((n + a.chunks - 1) / a.chunks) < 64ll * ctx->num_sms) a.chunks = (a.chunks + 1) / 2;
+  while (a.chunks > least && (long long)a.total * ((n + a.chunks - 1) / a.chunks) < 64ll * ctx->num_sms) a.chunks = (a.chunks + 1) / 2 > least ? (a.chunks + 1) / 2 : least;
+  if ((long long)a.total * n < 96ll * ctx->num_sms) a.chunks = 1;
   a.parts = (n + a.chunks - 1) / a.chunks;
   const long long warps = (long long)a.total * a.parts;
   const dim3 grid((unsigned)((warps + 7) / 8) + 1), block(256);
-  if (fp4 && a.chunks > 1) return slim_launch_pdl(to_cache ? rows_quantise_kernel<4> : rows_expand_kernel<4>, grid, block, 0, st, a);
-  if (fp4) return slim_launch_pdl(to_cache ? rows_quantise_kernel<1> : rows_expand_kernel<1>, grid, block, 0, st, a);
+  if (fp4 && a.chunks == 1) return slim_launch_pdl(to_cache ? rows_quantise_kernel<1, false> : rows_expand_kernel<1>, grid, block, 0, st, a);
+  if (fp4 && !to_cache) return slim_launch_pdl(rows_expand_kernel<4>, grid, block, 0, st, a);
+  if (fp4) return slim_launch_pdl(a.chunks % 4 == 0 ? rows_quantise_kernel<4, false> : rows_quantise_kernel<4, true>, grid, block, 0, st, a);
   switch (unit) {
     case 16: return slim_launch_pdl(rows_copy_kernel<uint4>, grid, block, 0, st, a, to_cache);
     case 8: return slim_launch_pdl(rows_copy_kernel<uint2>, grid, block, 0, st, a, to_cache);

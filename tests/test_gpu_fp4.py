@@ -539,3 +539,42 @@ def test_keys_beside_a_dominant_one_keep_their_weight(d, H, d_k, where):
             tol = (2 * 2.0 ** -18 + 2 * 2.0 ** -11 + 100 * 2.0 ** -24) * ua[c] + 2.0 ** -22 * ua.max()
             assert ((o[b, c].double() - want).abs() <= tol).all(), (b, h, float(gap[h]), ((o[b, c].double() - want).abs() / tol).max())
     layer.close()
+
+
+@pytest.mark.parametrize("d,H", [(4096, 32), (1280, 20)])
+def test_rows_are_moved_once_whatever_share_of_them_a_warp_has(d, H):
+    """Two numbers of rows that differ by 16, between which a warp's share of a row changes: the fewer rows are not slower."""
+    sms = torch.cuda.get_device_properties(0).multi_processor_count
+    few, more = (16 * sms - 8, 16 * sms + 8) if d == 4096 else (32 * sms - 8, 32 * sms + 8)
+    layer = SlimLayer(d, H, d // H, 0.0, "fp4", 1, more, DEV)
+    x, pos = _keys(more, d, 1).to(DEV), _i32([0])
+    out = torch.empty_like(x)
+
+    def call(n, write):
+        cu = cus[n]
+        if write:
+            B.slim_append_rows(layer.ctx, layer.cache, x, pos, cu, n, torch.cuda.current_stream().cuda_stream)
+        else:
+            B.slim_read_rows(layer.ctx, layer.cache, pos, cu, n, out, torch.cuda.current_stream().cuda_stream)
+
+    def time(n, write):
+        t, graph = [], torch.cuda.CUDAGraph()
+        call(n, write)
+        torch.cuda.synchronize()
+        with torch.cuda.graph(graph):
+            for _ in range(40):
+                call(n, write)
+        for _ in range(12):
+            e = [torch.cuda.Event(enable_timing=True) for _ in range(2)]
+            e[0].record()
+            graph.replay()
+            e[1].record()
+            torch.cuda.synchronize()
+            t.append(e[0].elapsed_time(e[1]) * 25)
+        return min(t[2:])
+
+    cus = {n: _i32([0, n]) for n in (few, more)}
+    for write in (True, False):
+        a, b = time(few, write), time(more, write)
+        assert a < 1.15 * b, (write, a, b)
+    layer.close()
