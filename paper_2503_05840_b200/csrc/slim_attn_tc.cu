@@ -755,6 +755,7 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
     asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
     // =========================== loads ===========================
     if (lane == 0) {
+      fence_proxy_async_global();                   // (queries, keys and values are an earlier kernel's ordinary stores)
       int st = 0;                                   // next stage
       uint32_t pe = 1u, pqe = 1u;                   // phases of bar_empty, bar_qe (the first pass finds everything empty)
       for (int r_ = 0; ok && item(r_, it); ++r_) {

@@ -524,6 +524,7 @@ __global__ void __launch_bounds__(MAXT, 1) fp4_tc_kernel(const __grid_constant__
         __syncwarp();
       }
       if (lane == 0) {
+        if (sweep == 0) fence_proxy_async_global();                    // (the rows may be an earlier kernel's ordinary stores)
         const uint64_t once = l2_policy_evict_first();
         for (int gg = g_begin; gg < g_end && ok;) {
           const int b = slim_seq_of_tile(s_prefix, p.batch, gg);

@@ -305,6 +305,7 @@ slim_proj_tc_kernel(const __grid_constant__ CUtensorMap wmap, const float* __res
 
   if (warp == 0 && lane == 0) {
     // =========================== producer ===========================
+    fence_proxy_async_global();                                // (ordinary stores there, bulk copies here)
     const unsigned char* usrc = u_tiled + ((size_t)(bg * g.hg + hg) * (d / 16) + row0 / 16) * ((size_t)1024 * g.hp);
     int s = 0;
     bool ok = true;

@@ -67,6 +67,7 @@ slim_values_tc_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_con
   slim_pdl_wait();
 
   if (warp == 0 && lane == 0) {
+    fence_proxy_async_global();                            // (the keys may be an earlier kernel's ordinary stores)
     int s = 0;
     bool ok = true;
     for (; s < nst; ++s) {
@@ -214,6 +215,7 @@ slim_values_pair_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_c
 
   if (warp == 0) {
     if (lane == 0) {
+      fence_proxy_async_global();                          // (the keys may be an earlier kernel's ordinary stores)
       // ---- producer: this CTA's 128 key rows and its half of the tile's W_KV columns, stage after stage ----
       int g = 0;                                           // stages issued so far (all tiles)
       bool ok = true;

@@ -110,6 +110,7 @@ slim_xscores_tc_kernel(const __grid_constant__ CUtensorMap xmap, const SlimDecod
   slim_pdl_wait();                                             // the query tiles come from the kernel before
 
   if (warp == 0 && lane == 0) {
+    fence_proxy_async_global();                                // (ordinary stores there, bulk copies here)
     const unsigned char* qsrc = qt_tiled + (size_t)b * (p.d / 16) * 2048;
     int s = 0;
     bool ok = true;

@@ -578,3 +578,34 @@ def test_rows_are_moved_once_whatever_share_of_them_a_warp_has(d, H):
         a, b = time(few, write), time(more, write)
         assert a < 1.15 * b, (write, a, b)
     layer.close()
+
+
+def test_rows_are_read_right_behind_the_kernels_that_wrote_them():
+    """Prompts written, read back and attended over, and a step, again and again without a pause: what each call does behind one."""
+    d, H, d_k, n = 1024, 8, 128, 700
+    layer, _, _, W = _decode_case(d, H, d_k, 1e4, [0, 0], 720, 2)
+    cu, cu_step, zero, lens, st = _i32([0, n, 2 * n]), _i32([0, 1, 2]), _i32([0, 0]), _i32([n + 1, n + 1]), torch.cuda.current_stream().cuda_stream
+    sets = [(_keys(2 * n, d, 50 + i, wide=False).to(DEV), _keys(2, d, 90 + i, wide=False).to(DEV)) for i in range(4)]
+
+    def go(i, pause):
+        x, new = sets[i % 4]
+        steps = [lambda: layer.append_rows(x, zero, cu), lambda: layer.read_rows(zero, cu, 2 * n),
+                 lambda: B.slim_values_from_keys(layer.ctx, k, 2 * n, v, st), lambda: layer.prompt_attention(x, k, v, cu, cu, n),
+                 lambda: layer.prompt_attention(x, k, v.bfloat16(), cu, cu, n, False), lambda: layer.decode_typed(new, lens, k_new=new)]
+        v, out = torch.empty(2 * n, d, device=DEV), []
+        for s, step in enumerate(steps):
+            r = step()
+            if s == 1:
+                k = r
+            if pause:
+                torch.cuda.synchronize()
+            out.append(r)
+        return [r for r in out if r is not None] + [v]
+
+    layer.prompt_attention(sets[0][0], sets[0][0], sets[0][0], cu, cu, n)
+    want = [go(i, True) for i in range(4)]
+    got = [go(i, False) for i in range(40)]
+    assert layer.device_status() == B.SLIM_OK
+    for i, g in enumerate(got):
+        assert all(torch.equal(a, b) for a, b in zip(g, want[i % 4])), i
+    layer.close()
