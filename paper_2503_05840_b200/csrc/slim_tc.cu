@@ -540,9 +540,9 @@ slim_tc_kernel(const __grid_constant__ CUtensorMap tmap, const SlimDecodeParams 
           uint4* dst = reinterpret_cast<uint4*>(reinterpret_cast<__nv_bfloat16*>(const_cast<void*>(p.k)) + (size_t)row * p.d + (size_t)rank * g.dsl);
           for (int e = lane; e < g.dsl / 8; e += 32) dst[e] = __ldg(src + e);
         }
-        fence_proxy_async_global();
-        __syncwarp();
       }
+      fence_proxy_async_global();                      // (other rows may be an earlier kernel's ordinary stores)
+      __syncwarp();
       if (lane == 0) {
         int it = 0, st = 0;
         uint32_t kph = 0;
