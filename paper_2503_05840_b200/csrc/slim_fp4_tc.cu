@@ -88,11 +88,12 @@ __device__ __forceinline__ uint32_t lds_u16(uint32_t a) { uint32_t v; asm volati
 __device__ __forceinline__ uint32_t lds32(uint32_t a) { uint32_t v; asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(a)); return v; }
 __device__ __forceinline__ uint2 lds64(uint32_t a) { uint2 v; asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(a)); return v; }
 __device__ __forceinline__ void sts64(uint32_t a, uint32_t x, uint32_t y) { asm volatile("st.shared.v2.u32 [%0], {%1, %2};" ::"r"(a), "r"(x), "r"(y) : "memory"); }
-// Arrival on a barrier of the other CTA that orders nothing beyond this CTA.  Enough where the other CTA's threads read nothing
-// of what this one wrote: each tensor core reads its own SM's shared memory, made visible to it before.  (Release at cluster
-// scope took 1500 clocks a tile.)
+// Arrival on a barrier of the other CTA behind what this CTA wrote to its own shared memory, and only that: a release of
+// everything at cluster scope takes 1500 clocks a tile (16 contexts of 8-16k rows: the call 295 -> 310 us, 64 x 1500 rows of 1280
+// 73 -> 98).
 __device__ __forceinline__ void mbar_arrive_remote(uint32_t cluster_bar) {
-  asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
+  asm volatile("fence.release.sync_restrict::shared::cta.cluster;" ::: "memory");
+  asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
 }
 __device__ __forceinline__ void umma2_f16(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
   asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}"
@@ -571,7 +572,7 @@ __global__ void __launch_bounds__(MAXT, 1) fp4_tc_kernel(const __grid_constant__
             if (elect_one()) mbar_arrive_remote(mapa(b_px + 8 * rk.st, 0));
             continue;
           }
-          ok = mbar_wait<false>(b_px + 8 * rk.st, rk.ph, s_abort, p.status) && ok;
+          ok = mbar_wait<true>(b_px + 8 * rk.st, rk.ph, s_abort, p.status) && ok;
           if (kt == 0 && uc > 0) ok = mbar_wait<true>(b_ue, (uc - 1) & 1, s_abort, p.status) && ok;
           ok = __all_sync(0xffffffffu, ok);
           if (!ok) break;
