@@ -706,6 +706,8 @@ attn_tc_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
         const uint32_t pkv = pf, pkk = kk == 0 ? pf ^ 1u : pf;
         ok = mbar_wait<false>(bar_full + 8 * kv, pkv, s_abort, a.status);
         if (j + 1 < nt) ok = mbar_wait<false>(bar_full + 8 * kk, pkk, s_abort, a.status) && ok;
+        ok = __all_sync(0xffffffffu, ok);           // (a wait that runs out may do so for some lanes only)
+        if (!ok) break;
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
           const int n = i ? it.nt1 : it.nt0;
