@@ -16,8 +16,8 @@ def _device(device) -> torch.device:
 
 
 class Scratch:
-    """Device memory of SlimLayer.prompt_attention, tree_decode, accumulate_weights and evict.  Layers whose calls run one after another on a
-    stream may share one.  It grows with the largest call so far; what it grew out of is given back, unless a graph has been
+    """Device memory of SlimLayer.prompt_attention, tree_decode, accumulate_weights and evict.  Layers whose calls run one
+    after another on a stream may share one.  It grows with the largest call so far; what it grew out of is given back, unless a graph has been
     captured on it."""
 
     def __init__(self, device):
@@ -130,10 +130,10 @@ class SlimLayer:
                          causal: bool = True, o: "torch.Tensor | None" = None) -> torch.Tensor:
         """Attention of packed prompts (binding.slim_prompt_attention): q [rows, H, d_k] (or [rows, d]), k and v [rows, heads, d_k]
         with as many heads as divide H; v float32, or bfloat16 in a layer that is not float32.  Positions below the layer's t_cap are there;
-        longer prompts need binding.slim_reserve_positions."""
+        longer prompts need binding.slim_reserve_positions.  k, v of no rows: every output row is zero."""
         if q.dim() not in (2, 3) or k.dim() not in (2, 3):
             raise ValueError("q, k: [rows, heads, d_k] or [rows, heads * d_k] is needed")
-        kv = k[0:1].numel() // self.d_k if k.shape[0] else self.H
+        kv = k.shape[1] if k.dim() == 3 else k.shape[1] // self.d_k
         self._arg("q", q, (q.shape[0],) + ((self.d,) if q.dim() == 2 else (self.H, self.d_k)), self.tdtype)
         self._arg("k", k, (k.shape[0],) + ((kv * self.d_k,) if k.dim() == 2 else (kv, self.d_k)), self.tdtype)
         if v.dtype not in (torch.float32, self.tdtype):
@@ -145,6 +145,8 @@ class SlimLayer:
         self._arg("cu_k", cu_k, cu_q.shape, torch.int32)
         o = torch.empty_like(q) if o is None else self._arg("o", o, q.shape, self.tdtype)
         n = cu_q.numel() - 1
+        if q.shape[0] == 0:
+            return o
         with torch.cuda.device(self.device):
             ws = self.scratch.take(B.slim_prompt_workspace_bytes(self.ctx, kv, n, q.shape[0], k.shape[0]))
             B.slim_prompt_attention(self.ctx, q, k, v, B.SLIM_F32 if v.dtype == torch.float32 else B.SLIM_BF16, kv, cu_q, cu_k, n, q.shape[0],
@@ -156,6 +158,8 @@ class SlimLayer:
         self._arg("k_new", k_new, (k_new.shape[0], self.d), self.tdtype)
         self._arg("positions", positions, (self.batch,), torch.int32)
         self._arg("cu_rows", cu_rows, (self.batch + 1,), torch.int32)
+        if k_new.shape[0] == 0:
+            return
         with torch.cuda.device(self.device):
             B.slim_append_rows(self.ctx, self.cache, k_new, positions, cu_rows, k_new.shape[0], torch.cuda.current_stream(self.device).cuda_stream)
 
@@ -164,6 +168,8 @@ class SlimLayer:
         self._arg("positions", positions, (self.batch,), torch.int32)
         self._arg("cu_rows", cu_rows, (self.batch + 1,), torch.int32)
         out = torch.zeros((rows, self.d), dtype=self.tdtype, device=self.device) if out is None else self._arg("out", out, (rows, self.d), self.tdtype)
+        if rows == 0:
+            return out
         with torch.cuda.device(self.device):
             B.slim_read_rows(self.ctx, self.cache, positions, cu_rows, int(rows), out, torch.cuda.current_stream(self.device).cuda_stream)
         return out
@@ -175,13 +181,18 @@ class SlimLayer:
                              f"{x.dtype} {tuple(x.shape)} on {x.device}" + ("" if x.is_contiguous() else ", not contiguous"))
         return x
 
-    def reserve_scratch(self, n: int = 0) -> None:
-        """Size the scratch for trees of up to n tokens, accumulate_weights and evict at once (before a capture, for instance).
+    def reserve_scratch(self, n: int = 0, prompts: int = 0, q_rows: int = 0, k_rows: int = 0, kv_heads: "int | None" = None) -> None:
+        """Size the scratch for trees of up to n tokens, accumulate_weights and evict at once (before a capture, for instance), and for
+        prompt_attention of `prompts` sequences with q_rows rows of queries and k_rows of keys (kv_heads heads, H if None).
         Without it the scratch grows with the calls."""
         sizes = [B.slim_tree_workspace_bytes(self.ctx, self.batch, self.t_cap, i) for i in range(1, n + 1)]
         if n < 0 or 0 in sizes:
             raise ValueError(f"n: 0 to {B.SLIM_MAX_TREE} drafted tokens are possible, got {n}")
         sizes += [B.slim_weights_workspace_bytes(self.ctx, self.batch, self.t_cap), B.slim_evict_workspace_bytes(self.ctx, self.batch, self.t_cap)]
+        if prompts or q_rows or k_rows:
+            sizes.append(B.slim_prompt_workspace_bytes(self.ctx, self.H if kv_heads is None else kv_heads, prompts, q_rows, k_rows))
+            if sizes[-1] == 0:
+                raise ValueError(f"prompts: no call has {prompts} sequences, {q_rows} rows of queries and {k_rows} of keys")
         with torch.cuda.device(self.device):
             self.scratch.take(max(sizes))
 

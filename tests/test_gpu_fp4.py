@@ -609,3 +609,35 @@ def test_rows_are_read_right_behind_the_kernels_that_wrote_them():
     for i, g in enumerate(got):
         assert all(torch.equal(a, b) for a, b in zip(g, want[i % 4])), i
     layer.close()
+
+
+def test_calls_without_rows_and_scratch_sized_ahead():
+    layer, q, Ks, W = _decode_case(512, 4, 128, 1e4, [20, 0], 64, 2)
+    none, x = torch.empty(0, 512, dtype=torch.bfloat16, device=DEV), _keys(6, 512, 1).to(DEV)
+    kept = layer.k.clone()
+    layer.append_rows(none, _i32([0, 0]), _i32([0, 0, 0]))
+    assert layer.read_rows(_i32([0, 0]), _i32([0, 0, 0]), 0).shape == (0, 512) and torch.equal(layer.k, kept)
+    for k in (none, none.view(0, 4, 128), none[:, :256].contiguous().view(0, 2, 128), none[:, :128].contiguous()):
+        for v in (k, k.float()):
+            assert not layer.prompt_attention(x, k, v, _i32([0, 6]), _i32([0, 0]), 0).any()          # no keys: rows of zeros
+    assert layer.prompt_attention(none, x, x, _i32([0, 0]), _i32([0, 6]), 6).shape == (0, 512)
+    three = torch.empty(0, 3, 128, dtype=torch.bfloat16, device=DEV)
+    with pytest.raises(ValueError):
+        layer.prompt_attention(x, three, three, _i32([0, 6]), _i32([0, 0]), 0)
+    # a scratch sized ahead takes a capture of these sizes, and no larger one
+    fresh = SlimLayer(512, 4, 128, 1e4, "fp4", 2, 64, DEV)
+    cu, o = _i32([0, 6]), torch.empty_like(x)
+    with pytest.raises(ValueError):
+        fresh.reserve_scratch(prompts=1, q_rows=0, k_rows=6)
+    with pytest.raises(ValueError):
+        fresh.reserve_scratch(prompts=1, q_rows=6, k_rows=6, kv_heads=3)
+    fresh.reserve_scratch(prompts=1, q_rows=6, k_rows=6)
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        fresh.prompt_attention(x, x, x, cu, cu, 6, o=o)
+    graph.replay()
+    assert torch.equal(o, layer.prompt_attention(x, x, x, cu, cu, 6))
+    del graph
+    fresh.close()
+    layer.close()
