@@ -628,7 +628,7 @@ cudaError_t slim_launch_weights(const slim_ctx* ctx, const SlimDecodeParams& p_i
     auto kern = p.kdtype == SLIM_BF16 ? SLIM_WL(__nv_bfloat16) : SLIM_WL(float);
 #undef SLIM_WL
 #undef SLIM_W
-    if ((e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem)) != cudaSuccess) return e;
+    if ((e = slim_allow_smem((const void*)kern)) != cudaSuccess) return e;
     e = slim_launch_pdl(kern, dim3(p.workers), dim3(WT), smem, st, p, scores, part, ring);
     if (e == cudaSuccess)
       e = slim_launch_pdl(slim_weights_join_kernel, dim3((p.H + 7) / 8, p.batch), dim3(256), sizeof(int) * (p.batch + 1), st, p,

@@ -162,7 +162,7 @@ cudaError_t launch_accum(const SlimDecodeParams& p, const float* scores, cudaStr
 cudaError_t slim_launch_fp4_decode(const slim_ctx* ctx, const SlimDecodeParams& p, float* scores, cudaStream_t st) {
   const size_t smem = sizeof(float) * p.d + sizeof(int) * (p.batch + 1);
   if (smem > 48 * 1024) {
-    cudaError_t e = cudaFuncSetAttribute(fp4_scores_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    cudaError_t e = slim_allow_smem((const void*)fp4_scores_kernel);
     if (e != cudaSuccess) return e;
   }
   fp4_scores_kernel<<<4 * ctx->num_sms, THREADS, smem, st>>>(p, scores);

@@ -532,7 +532,7 @@ cudaError_t launch_exact(const SlimDecodeParams& p, int only_flagged, cudaStream
   const size_t smem = sizeof(float) * (p.d + 2 * HP * SLIM_TT + 3 * HP) + sizeof(int) * (p.batch + 1);
   auto kern = slim_exact_kernel<KT, HP, COLS>;
   if (smem > 48 * 1024) {
-    cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    cudaError_t e = slim_allow_smem((const void*)kern);
     if (e != cudaSuccess) return e;
   }
   dim3 grid(dsplit, p.workers);
@@ -545,7 +545,7 @@ cudaError_t launch_scores(const slim_ctx* ctx, const SlimDecodeParams& p, float*
   const size_t smem = sizeof(float) * (p.d + SLIM_TT * (p.d / (2 * VEC))) + sizeof(int) * (p.batch + 1);
   auto kern = slim_scores_kernel<KT>;
   if (smem > 48 * 1024) {
-    cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    cudaError_t e = slim_allow_smem((const void*)kern);
     if (e != cudaSuccess) return e;
   }
   kern<<<4 * ctx->num_sms, GEN_THREADS, smem, st>>>(p, scores);
@@ -559,7 +559,7 @@ cudaError_t launch_xscores(const SlimDecodeParams& p, float* scores, const float
   if (e != cudaSuccess) return e;
   const size_t smem = sizeof(float) * (XS_ROWS * (XS_DC + 1) + 8 + (size_t)p.H * XS_DC);
   auto kern = slim_xscores_kernel<KT>;
-  e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  e = slim_allow_smem((const void*)kern);
   if (e != cudaSuccess) return e;
   kern<<<dim3((p.t_cap + XS_ROWS - 1) / XS_ROWS, p.batch), GEN_THREADS, smem, st>>>(p, xc_qt, scores);
   return cudaGetLastError();

@@ -205,6 +205,16 @@ __device__ __forceinline__ int slim_warp_find(const int32_t* __restrict__ starts
   return lo;
 }
 
+// Lets a kernel have the dynamic shared memory that a block can get.  Always all of it: the limit belongs to the function and the
+// device, so one that followed a call's sizes would fall short for a context, or a thread, of other sizes in between.
+inline cudaError_t slim_allow_smem(const void* kern) {
+  cudaFuncAttributes fa;
+  cudaError_t e = cudaFuncGetAttributes(&fa, kern);
+  if (e != cudaSuccess) return e;
+  const int room = 227 * 1024 - (int)fa.sharedSizeBytes;
+  return fa.maxDynamicSharedSizeBytes == room ? cudaSuccess : cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, room);
+}
+
 template <typename... KArgs, typename... Args>
 inline cudaError_t slim_launch_pdl(void (*kern)(KArgs...), dim3 grid, dim3 block, size_t smem, cudaStream_t st,
                                    Args... args) {

@@ -747,9 +747,7 @@ cudaError_t slim_proj_make_wmap(slim_ctx* ctx) {
   cudaError_t e = slim_tmap_encode_3d(ctx->wmap, ctx->wkv, dims, strides, box);
   if (e == cudaSuccess) e = slim_tmap_encode_3d(ctx->wmap_h, ctx->wkv_h, dims, strides, box);
   if (e != cudaSuccess) return e;
-  const ProjGeom g = make_proj_geom(d, H, d_k, 1, PJ_NS);      // the largest stage count a sweep may ask for
-  return cudaFuncSetAttribute((const void*)slim_proj_tc_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                              (int)proj_smem_bytes(g));
+  return slim_allow_smem((const void*)slim_proj_tc_kernel);
 }
 
 // Small batches (fewer than two (head, sequence) pairs per SM): the combine is split over column slices
@@ -798,12 +796,8 @@ static cudaError_t launch_fused(const slim_ctx* ctx, const SlimDecodeParams& p, 
   const bool r4 = g.hp * (g.nst * PJ_ROWS) <= 128 * 4;      // rounds of 256 (item, column group) pairs per CTA
   void (*kern)(const CUtensorMap, const SlimDecodeParams, const float*, float*, const ProjGeom, const int) =
       r4 ? slim_tail_fused_kernel<4> : slim_tail_fused_kernel<8>;
-  static size_t attr_set[64][2] = {};              // function attributes are kept per device
-  if (ctx->device < 0 || ctx->device >= 64 || attr_set[ctx->device][r4] < smem) {
-    cudaError_t e = cudaFuncSetAttribute((const void*)kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-    if (e != cudaSuccess) return e;
-    if (ctx->device >= 0 && ctx->device < 64) attr_set[ctx->device][r4] = smem;
-  }
+  cudaError_t e = slim_allow_smem((const void*)kern);
+  if (e != cudaSuccess) return e;
   CUtensorMap map;
   memcpy(&map, ctx->wmap_h, sizeof(map));
   cudaLaunchConfig_t cfg = {};
@@ -846,7 +840,7 @@ cudaError_t slim_launch_proj(const slim_ctx* ctx, const SlimDecodeParams& p, uns
       const size_t smem = sizeof(float) * p.workers + sizeof(int) * (4 + p.batch + 1) + 16 + sizeof(float) * (p.d_k + 2 * SLIM_TT + 4 + 36) +
                           sizeof(float) * (p.d <= COMBINE_SMEM_ROW ? p.d : 0) + 16;
       if (smem > 48 * 1024) {
-        e = cudaFuncSetAttribute((const void*)slim_combine_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        e = slim_allow_smem((const void*)slim_combine_kernel);
         if (e != cudaSuccess) return e;
       }
       e = slim_launch_pdl(slim_combine_kernel, grid, dim3(256), smem, st, p, u_tiled, u32, su, g.hp);

@@ -280,12 +280,12 @@ cudaError_t slim_launch_tail(const slim_ctx* ctx, const SlimDecodeParams& p, cud
   dim3 grid(p.H, nsplit);
   if (p.dtype == SLIM_BF16) {
     auto kern = slim_tail1_kernel<__nv_bfloat16>;
-    e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    e = slim_allow_smem((const void*)kern);
     if (e != cudaSuccess) return e;
     kern<<<grid, threads, smem, st>>>(p, bg_count, o_part);
   } else {
     auto kern = slim_tail1_kernel<float>;
-    e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    e = slim_allow_smem((const void*)kern);
     if (e != cudaSuccess) return e;
     kern<<<grid, threads, smem, st>>>(p, bg_count, o_part);
   }

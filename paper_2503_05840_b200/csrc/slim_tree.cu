@@ -373,7 +373,7 @@ template <typename KT>
 cudaError_t launch_generic(const slim_ctx* ctx, const SlimDecodeParams& p, const SlimTreeView& t, const int32_t* parents, void* o, cudaStream_t st) {
   const size_t dk4 = (p.d_k + 3) & ~3, smem = sizeof(float) * (TS_KEYS * (dk4 + 1) + t.n * dk4);
   auto ks = slim_tree_scores_kernel<KT>;
-  cudaError_t e = cudaFuncSetAttribute(ks, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  cudaError_t e = slim_allow_smem((const void*)ks);
   if (e != cudaSuccess) return e;
   const int R = p.H * t.n;
   e = slim_launch_pdl(ks, dim3((p.t_cap + TS_KEYS - 1) / TS_KEYS + 1, p.H, p.batch), dim3(256), smem, st, p, t, parents);

@@ -1298,7 +1298,7 @@ cudaError_t launch_u(const slim_ctx* ctx, const SlimDecodeParams& p, const SlimT
                      const CUtensorMap& tailmap, cudaStream_t st) {
   auto kern = slim_tree_u_kernel<MT>;
   const size_t smem = SumShape<MT>::smem(p.batch, t.g_pairs);
-  cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  cudaError_t e = slim_allow_smem((const void*)kern);
   if (e != cudaSuccess) return e;
   return slim_launch_pdl(kern, dim3(2 * t.g_pairs), dim3(SU_THREADS), smem, st, pmap, kmap, tailmap, p, t);
 }

@@ -641,3 +641,22 @@ def test_calls_without_rows_and_scratch_sized_ahead():
     del graph
     fresh.close()
     layer.close()
+
+
+@pytest.mark.parametrize("dtype", ["fp4", "bf16", "f32"])
+def test_layers_of_other_shapes_beside_one_another(dtype):
+    """Each layer's calls go on as before when layers of other shapes come after it: limits that a launch needs are not a context's."""
+    shapes = [(1280, 20, 64, 1e4, 23), (4096, 32, 128, 1e6, 3), (1536, 16, 96, 0.0, 9), (500, 5, 100, 1e4, 2), (512, 8, 64, 0.0, 40), (256, 2, 128, 1e4, 1)]
+    td = torch.float32 if dtype == "f32" else torch.bfloat16
+    layers = []
+    for d, H, d_k, theta, n in shapes:
+        g = torch.Generator().manual_seed(d)
+        layer = SlimLayer(d, H, d_k, theta, dtype, n, 64, DEV)
+        layer.set_wkv((torch.randn(d, d, generator=g) / d ** 0.5).numpy())
+        layer.append_k(torch.randn(n, 40, d, generator=g).to(DEV, td), _i32([0] * n))
+        q, lens = torch.randn(n, d, generator=g).to(DEV, td), _i32([40 - i % 9 for i in range(n)])
+        layers.append((layer, q, lens, layer.decode(q, lens).clone()))
+    for layer, q, lens, want in layers + layers[::-1]:
+        assert torch.equal(layer.decode(q, lens), want)
+    for layer, *_ in layers:
+        layer.close()
