@@ -199,6 +199,15 @@ __device__ void convert_values(const SlimAttn& a, int u, float* s_max) {
       }
     }
   }
+  // Rows in front of the first and behind the last sequence may hold anything: a run that has some is looked at once more without
+  const int k0 = max(lo, __ldg(a.cu_k)), k1 = min(hi, __ldg(a.cu_k + a.batch));
+  if (k0 > lo || k1 < hi) {
+#pragma unroll
+    for (int x = 0; x < W; ++x) m[x] = 0.f;
+    for (int r = k0 + tid / TPR; live && r < k1; r += RPP)
+#pragma unroll
+      for (int x = 0; x < W; ++x) m[x] = fmaxf(m[x], finite_abs(__ldg(src + (size_t)r * a.KV * dk + x)));
+  }
   __syncthreads();                                   // (the unit before this one has been read)
 #pragma unroll
   for (int x = 0; x < W; ++x) s_max[tid / TPR * V_COLS + tid % TPR * W + x] = m[x];
@@ -212,7 +221,7 @@ __device__ void convert_values(const SlimAttn& a, int u, float* s_max) {
 }
 
 template <int DK>
-__global__ void __launch_bounds__(PREP_THREADS) attn_tc_values_kernel(const __grid_constant__ SlimAttn a) {
+__global__ void __launch_bounds__(PREP_THREADS, 4) attn_tc_values_kernel(const __grid_constant__ SlimAttn a) {
   __shared__ float s_max[8 * V_COLS];
   slim_pdl_trigger();
   slim_pdl_wait();

@@ -577,3 +577,58 @@ def test_keys_beside_a_dominant_one_keep_their_weight(dk, gap, at):
     tol = (2 * 2.0 ** -18 + 2.0 ** -11 + 2 * 7.5e-5 + 2.0 ** -11 + n * 2.0 ** -26 + 2.0 ** -8) * o + n * 2.0 ** -32 * 2
     assert (np.abs(got[:, 0] - o) <= tol).all(), (np.abs(got[:, 0] - o) / tol).max()
     c.close()
+
+
+def test_replays_take_the_forms_that_their_inputs_need():
+    """One captured call with float32 values, replayed on ordinary inputs, on small values, on keys beyond float16, on values that are not
+    finite behind the sequences, and on ordinary ones again."""
+    c = Case("bf16", 4, 2, 128, 1e4, [300, 70], [900, 70], v32=True)
+    b = c.buffers()
+    c.call(b, True)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        c.call(b, True)
+    q, k, v = c.q.clone(), c.k.clone(), c.v.clone()
+    for kind in ("ordinary", "small", "keys", "behind", "ordinary"):
+        c.q, c.k, c.v = q.clone(), k.clone(), v.clone()
+        if kind == "small":
+            c.v[:, 1] *= 1e-9
+        elif kind == "keys":
+            _beyond_float16(c, [3, 3 + 900 + 20])
+        elif kind == "behind":
+            c.v[-3:], c.k[-3:] = float("nan"), float("inf")
+        for name in ("q", "k", "v"):
+            b[name].copy_(getattr(c, name))
+        b["o"].fill_(7.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        got = b["o"].double().cpu().numpy()
+        want, tol = c.reference(True)
+        assert B.slim_device_status(c.ctx) == B.SLIM_OK
+        assert (np.abs(got - want) <= tol).all(), kind
+    del graph
+    c.close()
+
+
+def test_numbers_outside_the_sequences_take_no_longer():
+    """Rows in front of the first and behind the last sequence hold huge values: what lies between is converted as if they were not there."""
+    c = Case("bf16", 8, 8, 128, 1e4, [2048], [2048], v32=True, lead=40)
+    b = c.buffers()
+
+    def time():
+        t = []
+        for _ in range(4):
+            e = [torch.cuda.Event(enable_timing=True) for _ in range(2)]
+            e[0].record()
+            c.call(b, True)
+            e[1].record()
+            torch.cuda.synchronize()
+            t.append(e[0].elapsed_time(e[1]))
+        return min(t[1:])
+
+    ordinary, want = time(), b["o"].clone()
+    b["v"][:40], b["v"][-40:] = 1e30, -1e33
+    assert time() < 3 * ordinary                          # (all rows by the CUDA cores: some 30 times)
+    assert torch.equal(b["o"], want)
+    c.close()
