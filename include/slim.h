@@ -325,8 +325,10 @@ slim_status slim_combine_project(slim_ctx* ctx, const float* lse_all, const floa
  *   Softmax sums and weighted sums are float32; in a bf16 context rotated queries and keys are rounded to 11 bits, the
  *   probabilities to bf16 (beside float32 values, probabilities and values to 11 bits, in steps of 2^-31 of the row's largest
  *   probability and 2^-28 at the least, values finer where all of their column are below 2^-8).  A number that is not finite in a key or
- *   a value reaches the rows that attend it, and no other.  With RoPE, rows that have a query above 4096 or attend a key above
- *   16384, and rows that meet a number that is not finite, are formed in float32 and take the CUDA cores' time.  bf16, d_k up to 128: tensor cores; other shapes: CUDA cores (slim_set_path chooses as for slim_decode).
+ *   a value reaches the rows that attend it, and no other.  With RoPE, or d_k other than 64, 96 and 128,
+ *   rows that have a query above 4096 or attend a key above 16384 are formed in float32 on the CUDA cores (some 50 times as long), as
+ *   are rows that meet a number that is not finite and, beside float32 values, rows that attend a value below 2^-28 of its column's
+ *   largest where that is above 4000 or below 2^-8.  bf16, d_k up to 128: tensor cores; other shapes: CUDA cores (slim_set_path chooses as for slim_decode).
  *   Few queries over many keys are worked off in pieces of the keys, whose sums are joined in a fixed order: the last bits of a
  *   row may depend on what else is in the batch, but not on the run.
  *   No weights need to be set.  total_q from 1, total_k from 0 (k, v may then be NULL), both at most 2^29.

@@ -27,8 +27,8 @@
 // Bound by the score warps.  A tile of 16 x 2048 keys takes a CTA 2650 clocks: a warp issues some 600 instructions for two
 // heads (64 conversions of codes, 64 products with the scale, 128 of the rotation, 16 m16n8k16, 16 stores), two warps share a
 // scheduler (registers: 168 a thread), the pipe that the float16 products need is half full, the issue slots 42 %; the tensor
-// core works 560 clocks, HBM is at 18 %.  Measured: 131001 rows of 4096 in pages 196 us (285 MB, 1.46 TB/s), 16 contexts of
-// 8-16k rows 288 us, 64 contexts of 1500 rows of 1280 55 us; the combine and the projection follow (32, 32 and 24 us).
+// core works 560 clocks, HBM is at 18 %.  Measured: 131001 rows of 4096 in pages 187-196 us (285 MB, 1.5 TB/s), 16 contexts of
+// 8-16k rows 288 us, 64 contexts of 1500 rows of 1280 54 us; the combine and the projection follow (32, 32 and 24 us).
 // Tried without gain: fetching a tile's codes into registers behind the tile before (four warps' registers lent to the
 // score warps, 304 -> 338 us), one head a warp and 16 warps (351 -> 455 us at the time).
 #include <cuda.h>
