@@ -132,7 +132,7 @@ slim_status slim_set_wkv(slim_ctx* ctx, const void* W_KV, int host_dtype);
  * Such a cache is filled through slim_append_k, slim_append_rows, slim_decode_step, slim_decode_typed or slim_prefill, and
  * may be paged: a pool takes slim_cache_bytes(ctx, num_pages, page_rows).  Where the shape fits the tensor-core kernel, a decode
  * rounds rotated keys, queries and probabilities to 11 bits; what it neglects of probabilities far below the largest is at
- * most 2^-20 of their sum.  The CUDA-core kernels compute in float32.  slim_decode_partial, slim_tree_*,
+ * most 2^-16 of their sum.  The CUDA-core kernels compute in float32.  slim_decode_partial, slim_tree_*,
  * slim_accumulate_weights, slim_evict and the X-cache calls do not take it (SLIM_ERR_UNSUPPORTED).          */
 size_t slim_cache_bytes(const slim_ctx* ctx, int batch, int t_cap);
 size_t slim_workspace_bytes(const slim_ctx* ctx, int batch, int t_cap);

@@ -17,12 +17,12 @@
 //   MMA thread   of the even CTA: U^T[256 columns x 32 heads] += K^T[256 x 16] P^T[16 x 32] a pair of 128-column chunks, each
 //                CTA supplying its own 128 columns and its own 16 heads' P (cta_group::2), so no probabilities travel; the odd
 //                CTA's passes on that its tile is complete
-// float16 P keeps its 11 bits from 2^-14 up to 2^15, so the reference m of a unit has to leave room on both sides: m is the mean
-// of the first tile's scores plus 2 (log2 units), or its maximum less 11 where that is more.  Without a dominant key scores
-// may then come out 15 above and 14 below the second; with one in the first tile (the first token of a context often is)
-// 4 above it, and down to 25 below.  A unit is flagged by a score further up, or where the probabilities below 2^-14 are more
-// than 2^-20 of l (float32 sums; what is lost stays below that).  Flagged units are walked again at the end, with the largest
-// score, known by then, less 14 as reference: 11 bits down to 2^-28 of the largest probability, steps of 2^-38 of it below.
+// float16 P keeps its 11 bits from 2^-14 up to 2^15, so the reference m of a unit has to leave room on both sides.  m is the mean of
+// the first tile's scores plus 10 (log2 units), or that tile's maximum less 11 where that is more.  So scores may come out 25 above
+// an ordinary first tile's mean, and 25 below a dominant key in it (the first token of a context often is one).  A unit is flagged by
+// a score further up, or where what P's rounding below 2^-14 may lose (2^-25 a key, or the key) is more than 2^-16 of l.  Flagged
+// units are walked again at the end, with the largest score, known by then, less 14 as reference.  For normal scores of up to 3
+// nats' deviation, a first key 20 nats above them or not, one head of a unit in 10000 asks for that at most (3.5 nats: one in 500).
 //
 // Bound by the score warps.  A tile of 16 x 2048 keys takes a CTA 2650 clocks: a warp issues some 600 instructions for two
 // heads (64 conversions of codes, 64 products with the scale, 128 of the rotation, 16 m16n8k16, 16 stores), two warps share a
@@ -45,7 +45,7 @@ namespace {
 constexpr int MAX_ST = 4, MAX_PK = 8;    // float16 stages, stages of packed tiles
 constexpr int RESEED = 64;
 constexpr float XMAX = 15.f, XMIN = -14.f;            // log2 of the probabilities that float16 holds with all its bits
-constexpr float ABOVE_MEAN = 2.f, BELOW_MAX = 11.f, TOP = 14.f, LOST = 0x1p-20f;
+constexpr float ABOVE = 10.f, BELOW_MAX = 11.f, TOP = 14.f, STEP = 0x1p-25f, LOST = 0x1p-16f;
 
 // How a thread's pairs lie: pieces of PE consecutive columns of the first half of the head, and the same of the second
 template <int DK>
@@ -134,7 +134,7 @@ __global__ void __launch_bounds__(MAXT, 1) fp4_tc_kernel(const __grid_constant__
   float* s_xm = reinterpret_cast<float*>(misc + 8);           // [16] reference, from the set that has a unit's first tile
   float* s_xl = s_xm + 16;                                    // [16] the other set's share of l
   float* s_xx = s_xl + 16;                                    // [16] its largest score
-  float* s_xs = s_xx + 16;                                    // [16] and its sum of small probabilities
+  float* s_xs = s_xx + 16;                                    // [16] and what it may have lost
   int* s_prefix = reinterpret_cast<int*>(s_xs + 16);
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const uint32_t rank = cluster_ctarank();
@@ -410,13 +410,20 @@ __global__ void __launch_bounds__(MAXT, 1) fp4_tc_kernel(const __grid_constant__
               if (sweep == 1) {
                 if (scores) mref = __ldcg(umax + (size_t)unit * p.H + (int)rank * g.hl + hd0 + mine) - TOP;
               } else if (owner) {
-                float mx = v ? s : -INFINITY, mean = v ? s : 0.f;
+                float mx = v ? s : -INFINITY, sum = v ? s : 0.f;
 #pragma unroll
-                for (int o = 1; o < 32; o = o == 1 ? 4 : 2 * o) {
-                  mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
-                  mean += __shfl_xor_sync(0xffffffffu, mean, o);
+                for (int o = 1; o < 32; o = o == 1 ? 4 : 2 * o) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+                if constexpr (ROPE || DK != 128) {
+#pragma unroll
+                  for (int o = 1; o < 32; o = o == 1 ? 4 : 2 * o) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+                } else {
+                  // (lane by lane where a tree costs registers: 16 contexts of 12000 rows, d_k 128 without rotation, 258 us instead of 266)
+                  const float own = sum;
+                  sum = 0.f;
+#pragma unroll 1
+                  for (int i = 0; i < SLIM_TT; ++i) sum += __shfl_sync(0xffffffffu, own, (i >> 1) * 4 + (lane & 2) + (i & 1));
                 }
-                mref = fmaxf(mean / (float)min(SLIM_TT, len - t0) + ABOVE_MEAN, mx - BELOW_MAX);      // (a NaN leaves the maximum)
+                mref = fmaxf(sum / (float)min(SLIM_TT, len - t0) + ABOVE, mx - BELOW_MAX);      // (a NaN leaves the maximum)
                 if (g.sets == 2) {
                   if (speaks) s_xm[hd0 + mine] = mref;
                   __syncwarp();
@@ -435,7 +442,7 @@ __global__ void __launch_bounds__(MAXT, 1) fp4_tc_kernel(const __grid_constant__
             if (v && xv > XMAX && sweep == 0) p.unit_flags[2 * unit + (int)rank] = 1;
             xv = xv > XMAX ? XMAX : xv;
             const float pf = v ? ex2_approx(xv) : 0.f;
-            if (xv < XMIN) lsub += pf;
+            if (xv < XMIN) lsub += fminf(pf, STEP);
             const __half pv = __float2half_rn(pf);
             if (scores) {
               lsum += __half2float(pv);
